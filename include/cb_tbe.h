@@ -386,6 +386,100 @@ cb_status cb_fm_forward(const float* y, int32_t batch, int32_t num_fields, int32
 cb_status cb_fm_backward(const float* y, const float* grad_fm, int32_t batch, int32_t num_fields,
                          int32_t dim, int64_t row_stride, float* grad_y, cudaStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Token lookup: a row of ONE table for every token of a batch of sequences, scaled, and
+ * the dense gradient of the table (not in the paper: its tables are pooled; this is the
+ * input side of a sequence model that is trained on such a table):
+ *
+ *   out[s, l, :]    = scale * E[tokens[s, l], :]
+ *   dE[v, :]  (+)=  scale * sum over all (s, l) with tokens[s, l] = v of grad_out[s, l, :]
+ *
+ * computed in fp32 and rounded once to the output's type (nearest even). Unlike the pooled
+ * calls these need no handle and no offsets, take rows of any length, and write the output
+ * or the gradient in any of the three types.
+ *   tokens      device, idx_dtype: token (s, l) at tokens[s * token_sequence_stride +
+ *               l * token_stride], any strides >= 0 in values (a slice of longer sequences
+ *               needs no copy). sequences * length < 2^30; either may be 0.
+ *   table       device [rows, dim] of table_dtype, row v at v * row_stride values,
+ *               row_stride >= dim; rows < 2^31, dim <= 2^20. Any alignment of its type;
+ *               rows in multiples of 16 bytes that start on 16 bytes are moved fastest.
+ *   out, grad_out  device, row (s, l) at s * ..._sequence_stride + l * ..._stride values,
+ *               each row contiguous; rows of `out` must not overlap (those of grad_out may).
+ *   scale       any value but NaN
+ *   error       device int, or NULL: set to CB_ERR_INDEX_OOB (if it holds 0) when a token is
+ *               outside [0, rows). Such a token gives a row of zeros and no gradient.
+ * Errors: CB_ERR_INVALID_ARG before any GPU work, CB_ERR_CUDA if a launch fails. Nothing is
+ * allocated and nothing waits, so the calls can be captured into a CUDA graph. Deterministic. */
+cb_status cb_token_forward(const void* table, cb_dtype table_dtype, int64_t rows, int32_t dim,
+                           int64_t row_stride, const void* tokens, cb_index_dtype idx_dtype,
+                           int32_t sequences, int32_t length, int64_t token_sequence_stride,
+                           int64_t token_stride, float scale, void* out, cb_dtype out_dtype,
+                           int64_t out_sequence_stride, int64_t out_stride, int* error,
+                           cudaStream_t stream);
+
+/* Bytes of workspace that cb_token_backward needs for num_tokens = sequences * length (0 for
+ * small calls). The contents need not be kept between calls. */
+int64_t cb_token_backward_workspace_bytes(int64_t num_tokens, int64_t rows, int32_t dim);
+
+/* The table's gradient, every row written: zeros for a row without a token; or
+ * (accumulate != 0) added to the gradient that is there, rows without a token left alone,
+ * as for a table tied to an output head whose gradient has been written before.
+ *   padding_idx  a token whose positions give no gradient, or -1
+ *   grad         device [rows, dim] of grad_dtype, row v at v * grad_stride values
+ *   workspace    device, 256-byte aligned, of cb_token_backward_workspace_bytes(...) at
+ *                least (CB_ERR_CAPACITY otherwise); in use until the call's work is done */
+cb_status cb_token_backward(const void* grad_out, cb_dtype go_dtype, int64_t go_sequence_stride,
+                            int64_t go_stride, const void* tokens, cb_index_dtype idx_dtype,
+                            int32_t sequences, int32_t length, int64_t token_sequence_stride,
+                            int64_t token_stride, int64_t rows, int32_t dim, float scale,
+                            int64_t padding_idx, int accumulate, void* grad, cb_dtype grad_dtype,
+                            int64_t grad_stride, void* workspace, int64_t workspace_bytes, int* error,
+                            cudaStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Matrix updates orthogonalised by Newton-Schulz products, alone and as an optimizer step
+ * (not in the paper; the step for the weight matrices beside the tables, whose own steps are
+ * cb_tbe_backward_apply and cb_tbe_apply_sparse). For each of `batch` matrices G [rows, cols]:
+ *
+ *   X = G / (||G||_F + eps);  then `steps` times, with (a, b, c) = coefficients[3k .. 3k + 2]:
+ *   A = X X^T,  X <- a X + (b A + c A A) X          (on the shorter side: X^T X if rows > cols)
+ *
+ * which moves every singular value towards 1 and keeps the singular vectors. The usual
+ * coefficients are (3.4445, -4.7750, 2.0315), five times. The products are taken in fp16 with
+ * fp32 sums; in the 2-norm the result is about 1e-3 off the exact one. They hold as long as
+ * singular values stay below about 40 throughout; coefficients that let them grow beyond give
+ * infinities. A matrix with an infinity or a NaN gives NaNs, a matrix of zeros gives zeros.
+ *   g           device, of g_dtype: matrix i at i * g_batch_stride values, row r at
+ *               r * g_row_stride, rows contiguous, g_row_stride >= cols
+ *   batch, rows, cols  each may be 0 (nothing is done); batch <= 65535, rows, cols <= 2^20
+ *   eps         >= 0;  coefficients: host array of 3 * steps finite values;  steps 1 .. 64
+ *   out         device, of out_dtype, strides as for g, matrices apart by rows * cols at least;
+ *               may be g itself, of one type and layout
+ *   workspace   device, 256-byte aligned, of cb_muon_workspace_bytes(...) at least
+ *               (CB_ERR_CAPACITY otherwise); in use until the call's work is done
+ *   error       device int, or NULL: set to CB_ERR_TIMEOUT (if it holds 0) when a bounded wait
+ *               inside a product ran out; the output is then incomplete
+ * Errors: CB_ERR_INVALID_ARG before any GPU work; CB_ERR_CUDA if a launch fails or the driver's
+ * tensor-map encoder cannot be reached. Nothing is allocated. Deterministic. */
+int64_t cb_muon_workspace_bytes(int32_t batch, int32_t rows, int32_t cols);
+cb_status cb_muon_orthogonalise(const void* g, cb_dtype g_dtype, int32_t batch, int32_t rows, int32_t cols,
+                                int64_t g_batch_stride, int64_t g_row_stride, float eps,
+                                const float* coefficients, int32_t steps, void* out, cb_dtype out_dtype,
+                                int64_t out_batch_stride, int64_t out_row_stride, void* workspace,
+                                int64_t workspace_bytes, int* error, cudaStream_t stream);
+
+/* The optimizer step, for every matrix W with momentum M (fp32) and gradient G:
+ *   M <- beta M + G;   U = G + beta M (nesterov != 0) or M;   O = the above of U;
+ *   W <- (1 - lr weight_decay) W - lr update_scale O
+ * M and W are written in place; O is added in fp32 from the last product's sums, and W rounded
+ * once to its type. lr, weight_decay, update_scale: any value but NaN; beta >= 0. */
+cb_status cb_muon_step(void* weights, cb_dtype w_dtype, int64_t w_batch_stride, int64_t w_row_stride,
+                       const void* g, cb_dtype g_dtype, int64_t g_batch_stride, int64_t g_row_stride,
+                       float* momentum, int64_t m_batch_stride, int64_t m_row_stride, int32_t batch,
+                       int32_t rows, int32_t cols, float lr, float weight_decay, float beta, int nesterov,
+                       float eps, const float* coefficients, int32_t steps, float update_scale,
+                       void* workspace, int64_t workspace_bytes, int* error, cudaStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

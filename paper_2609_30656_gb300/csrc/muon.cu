@@ -1,0 +1,852 @@
+// muon.cu -- approximate orthogonalisation of matrix updates by Newton-Schulz
+// products, alone and inside an optimizer step with momentum and weight decay.
+//
+// For a matrix G, X_0 the one of G and G^T with no more rows than columns (p <= q),
+// divided by ||G||_F + eps, and for every step with its coefficients (a, b, c)
+//     A = X X^T,   B = b A + c A A,   X <- a X + B X,
+// which takes every singular value s of X to a s + b s^3 + c s^5 and leaves the
+// singular vectors as they are. A step is 2 p^2 q + p^3 multiply-adds when the
+// symmetry of A and of A A is used, against p q values read and written: beyond
+// sizes of a few hundred it is bound by the tensor cores.
+//
+// Numbers. The products take fp16 operands and sum in fp32. fp16 rather than bf16:
+// both run at one rate, every matrix here is bounded (|x| <= ||X||_2 <= about 1.3 under
+// the usual coefficients), so the exponent's range is not needed, and the three more
+// bits are: rounding X puts noise into its small singular directions, which the first
+// steps multiply by a each (1.2e-2 off the exact result in the 2-norm with bf16, 3e-3
+// with fp16, sizes 128 to 2048). The rest of that noise goes by keeping X as the sum of
+// two fp16 values, X = hi + lo, for the term a X of the first two steps (1e-3); the
+// products take hi alone, since their error is filtered by B, which vanishes on the
+// small directions. From the third step on the term is folded into B (B + a I), and X is
+// hi alone. X is held times 2^10 and A and B times 2^8 (powers of two: exact), which
+// keeps their small values out of fp16's subnormal range and leaves a factor of 40 and
+// more below its largest value.
+//
+// The norm. Squares are summed in three classes of magnitude, each scaled to stay in
+// range, so that no finite matrix overflows or underflows it.
+//
+// Layout in the workspace: X as [p, q] with rows padded to 64 values, A and B as [p, p]
+// likewise. The transposition of a tall matrix is done where it is read (cast_kernel) and
+// where the result is written (the last product's epilogue), so the products exist in
+// one orientation only.
+#include "tbe_internal.cuh"
+#include "tensor_core.cuh"
+
+#include <cmath>
+#include <cudaTypedefs.h>
+
+namespace cbtbe {
+namespace {
+
+constexpr float kScaleX = 1024.f;  // X is stored times this,
+constexpr float kScaleA = 256.f;   // A and B times this
+constexpr int kTwoTerm = 2;        // steps whose term a X takes hi + lo
+constexpr int kMaxSteps = 64;
+
+// ---------------------------------------------------------------- norm and momentum
+
+// x^2 summed by magnitude: |x| >= 2^40 times 2^-160, |x| < 2^-40 times 2^160, the rest
+// as it is. A NaN goes with the rest.
+struct SquareSum {
+    float mid = 0.f, big = 0.f, small = 0.f;
+    __device__ __forceinline__ void add(float x) {
+        const float m = fabsf(x);
+        if (m >= 0x1p40f) {
+            const float y = x * 0x1p-80f;
+            big = fmaf(y, y, big);
+        } else if (m < 0x1p-40f) {
+            const float y = x * 0x1p80f;
+            small = fmaf(y, y, small);
+        } else {
+            mid = fmaf(x, x, mid);
+        }
+    }
+};
+
+struct MatrixIn {
+    const void* g;         // the gradient, of dtype
+    float* momentum;       // or null: the update is g itself
+    int64_t g_batch, g_row, m_batch, m_row;  // strides in values
+    int32_t dtype;
+    int32_t rows, cols;
+    float beta;
+    int32_t nesterov;
+};
+
+__device__ __forceinline__ float load_value(const void* p, int64_t i, int dtype) {
+    if (dtype == CB_F32) return static_cast<const float*>(p)[i];
+    const uint16_t h = static_cast<const uint16_t*>(p)[i];
+    if (dtype == CB_BF16) return __uint_as_float(static_cast<uint32_t>(h) << 16);
+    __half x;
+    memcpy(&x, &h, 2);
+    return __half2float(x);
+}
+__device__ __forceinline__ void store_value(void* p, int64_t i, float v, int dtype) {
+    if (dtype == CB_F32) static_cast<float*>(p)[i] = v;
+    else if (dtype == CB_BF16) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+    else static_cast<__half*>(p)[i] = __float2half_rn(v);
+}
+
+// V consecutive values (V = 1, or 4 with their alignment).
+template <int V>
+__device__ __forceinline__ void load_values(const void* p, int64_t i, int dtype, float (&v)[V]) {
+    if constexpr (V == 1) {
+        v[0] = load_value(p, i, dtype);
+    } else if (dtype == CB_F32) {
+        const float4 x = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
+        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+    } else {
+        const uint2 x = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
+        const uint32_t w[2] = {x.x, x.y};
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (dtype == CB_BF16) {
+                v[2 * k] = __uint_as_float(w[k] << 16);
+                v[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+            } else {
+                __half2 h;
+                memcpy(&h, &w[k], 4);
+                const float2 f = __half22float2(h);
+                v[2 * k] = f.x;
+                v[2 * k + 1] = f.y;
+            }
+        }
+    }
+}
+
+constexpr int kNormThreads = 256;
+constexpr int kNormBlocks = 128;  // most blocks (and partial sums) per matrix
+
+__host__ __device__ __forceinline__ float mix_momentum(float m, float g, float beta) { return fmaf(beta, m, g); }
+
+// m <- beta m + g in place, and a block's part of the squares of the update u
+// (g; m; or g + beta m). Blocks (x of a matrix, matrix).
+template <int V>
+__global__ void __launch_bounds__(kNormThreads) muon_norm_kernel(MatrixIn in, float* __restrict__ partial) {
+    begin_kernel();
+    const int b = blockIdx.y;
+    const char* g = static_cast<const char*>(in.g) + b * in.g_batch * dtype_bytes(in.dtype);
+    float* mom = in.momentum ? in.momentum + b * in.m_batch : nullptr;
+    const int vecs = in.cols / V;
+    const int64_t total = static_cast<int64_t>(in.rows) * vecs;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kNormThreads;
+    SquareSum s;
+    int64_t i = static_cast<int64_t>(blockIdx.x) * kNormThreads + threadIdx.x;
+    int64_t row = i / vecs;
+    int col = static_cast<int>(i - row * vecs);
+    const int64_t drow = step / vecs;
+    const int dcol = static_cast<int>(step - drow * vecs);
+    constexpr int U = 4;  // vectors in flight
+    while (i < total) {
+        float v[U][V], m[U][V];
+        int64_t at_m[U];
+        int live = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i < total) {
+                live = u + 1;
+                load_values<V>(g, row * in.g_row + static_cast<int64_t>(col) * V, in.dtype, v[u]);
+                at_m[u] = row * in.m_row + static_cast<int64_t>(col) * V;
+                if (mom) load_values<V>(mom, at_m[u], CB_F32, m[u]);
+            }
+            i += step;
+            row += drow;
+            col += dcol;
+            if (col >= vecs) {
+                col -= vecs;
+                ++row;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (u < live) {
+                if (mom) {
+#pragma unroll
+                    for (int k = 0; k < V; ++k) {
+                        m[u][k] = mix_momentum(m[u][k], v[u][k], in.beta);
+                        v[u][k] = in.nesterov ? mix_momentum(m[u][k], v[u][k], in.beta) : m[u][k];
+                    }
+                    if constexpr (V == 4)
+                        *reinterpret_cast<float4*>(mom + at_m[u]) = make_float4(m[u][0], m[u][1], m[u][2], m[u][3]);
+                    else
+                        mom[at_m[u]] = m[u][0];
+                }
+#pragma unroll
+                for (int k = 0; k < V; ++k) s.add(v[u][k]);
+            }
+        }
+    }
+    // A fixed order: lanes, then warps.
+    __shared__ float sh[3][kNormThreads / 32];
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) {
+        s.mid += __shfl_xor_sync(kFull, s.mid, off);
+        s.big += __shfl_xor_sync(kFull, s.big, off);
+        s.small += __shfl_xor_sync(kFull, s.small, off);
+    }
+    if (lane == 0) {
+        sh[0][wid] = s.mid;
+        sh[1][wid] = s.big;
+        sh[2][wid] = s.small;
+    }
+    __syncthreads();
+    if (threadIdx.x < 3) {
+        float t = 0.f;
+        for (int w = 0; w < kNormThreads / 32; ++w) t += sh[threadIdx.x][w];
+        partial[(static_cast<int64_t>(b) * kNormBlocks + blockIdx.x) * 3 + threadIdx.x] = t;
+    }
+}
+
+// kScaleX / (norm + eps) as a product of two floats, so that neither a huge nor a tiny
+// norm takes it out of range; from the partial sums of one matrix, by one warp.
+__device__ __forceinline__ float2 inverse_norm(const float* partial, int blocks, float eps, int lane) {
+    double t = 0.0;
+    for (int k = lane; k < blocks; k += 32)
+        t += static_cast<double>(partial[3 * k]) + static_cast<double>(partial[3 * k + 1]) * 0x1p160 +
+             static_cast<double>(partial[3 * k + 2]) * 0x1p-160;
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) t += __shfl_xor_sync(kFull, t, off);
+    const double norm = sqrt(t) + static_cast<double>(eps);
+    // A matrix of zeros with eps = 0 stays zeros.
+    const double inv = norm == 0.0 ? 0.0 : static_cast<double>(kScaleX) / norm;
+    int e = 0;
+    const double mant = frexp(inv, &e);
+    const int half = e / 2;
+    return make_float2(static_cast<float>(ldexp(1.0, half)), static_cast<float>(ldexp(mant, e - half)));
+}
+
+// ---------------------------------------------------------------- cast
+
+constexpr int kCastTile = 64;
+
+// X_0 = kScaleX u / (||u|| + eps) as hi + lo, [p, ld] rows: u as it lies, or transposed.
+// A block takes a 64 x 64 tile of u: blocks (column tile, row tile, matrix).
+template <bool TRANSPOSED>
+__global__ void __launch_bounds__(256) muon_cast_kernel(MatrixIn in, const float* __restrict__ partial, int norm_blocks,
+                                                        float eps, __half* __restrict__ hi, __half* __restrict__ lo,
+                                                        int ld, int64_t x_batch) {
+    __shared__ float2 factor;
+    __shared__ float tile[TRANSPOSED ? kCastTile : 1][kCastTile + 1];
+    begin_kernel();
+    const int b = blockIdx.z;
+    const int r0 = blockIdx.y * kCastTile, c0 = blockIdx.x * kCastTile;
+    if (threadIdx.x < 32) {
+        const float2 f = inverse_norm(partial + static_cast<int64_t>(b) * kNormBlocks * 3, norm_blocks, eps, threadIdx.x);
+        if (threadIdx.x == 0) factor = f;
+    }
+    const char* g = static_cast<const char*>(in.g) + b * in.g_batch * dtype_bytes(in.dtype);
+    const float* mom = in.momentum ? in.momentum + b * in.m_batch : nullptr;
+    const int c = threadIdx.x & 63, rq = threadIdx.x >> 6;
+    float v[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        const int row = r0 + rq + 4 * k, col = c0 + c;
+        v[k] = 0.f;
+        if (row < in.rows && col < in.cols) {
+            v[k] = load_value(g, row * in.g_row + col, in.dtype);
+            if (mom) {
+                const float m = mom[row * in.m_row + col];
+                v[k] = in.nesterov ? mix_momentum(m, v[k], in.beta) : m;
+            }
+        }
+    }
+    __syncthreads();
+    const float2 f = factor;
+    auto put = [&](int64_t at, float x) {
+        const __half h = __float2half_rn(x);
+        hi[at] = h;
+        lo[at] = __float2half_rn(x - __half2float(h));
+    };
+    const int64_t base = b * x_batch;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        const float x = (v[k] * f.x) * f.y;
+        const int row = r0 + rq + 4 * k, col = c0 + c;
+        if constexpr (TRANSPOSED) tile[rq + 4 * k][c] = x;
+        else if (row < in.rows && col < in.cols) put(base + static_cast<int64_t>(row) * ld + col, x);
+    }
+    if constexpr (TRANSPOSED) {
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const int row = r0 + c, col = c0 + rq + 4 * k;  // value (row, col) of u is X[col, row]
+            if (row < in.rows && col < in.cols) put(base + static_cast<int64_t>(col) * ld + row, tile[c][rq + 4 * k]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- products
+
+enum Product {
+    kGram,    // A = X X^T                          (symmetric)
+    kPoly,    // B = b A + c A A (+ a I)            (symmetric)
+    kUpdate,  // X' = (a X +) B X
+    kResult   // the same, into the caller's matrix
+};
+template <Product WHAT> constexpr bool kSymmetric = WHAT == kGram || WHAT == kPoly;
+
+constexpr int kTileM = 128, kTileK = 64;
+constexpr int kEpilogueWarps = 4;
+constexpr int kProductThreads = (kEpilogueWarps + 2) * 32;  // + a copying warp, + a multiplying warp
+constexpr uint32_t kBoxBytes = 64 * 64 * 2;                 // one TMA box: 64 rows of 64 fp16
+template <int BN> constexpr int kStages = BN == 256 ? 4 : (BN == 128 ? 6 : 8);
+template <int BN> constexpr uint32_t kStageBytes = (kTileM + BN) * kTileK * 2;
+
+struct ProductArgs {
+    int32_t m, n, k;          // C [m, n], K
+    int32_t batch;
+    int32_t row_tiles, col_tiles;
+    int64_t tiles;            // per matrix
+    float a, b, c;            // the step's coefficients (a = 0: no term a X, or a I)
+    const __half* term_hi;    // kPoly: A; kUpdate, kResult: X
+    const __half* term_lo;    // or null
+    int64_t term_batch;
+    int32_t term_ld;
+    __half* out_hi;
+    __half* out_lo;           // or null
+    int64_t out_batch;
+    int32_t out_ld;
+    // kResult
+    void* user;               // the caller's output, or weights
+    int64_t user_batch, user_row;
+    int32_t user_dtype;
+    int32_t transposed;       // value (i, j) of C is value (j, i) of the caller's
+    int32_t weights;          // W <- keep W - rate O, instead of O
+    float keep, rate;
+    int* error;
+};
+
+struct Tile {
+    int32_t b, i, j;
+};
+
+// Column tiles of row tile i that reach the lower triangle of 128 x 128 blocks.
+template <int BN>
+__host__ __device__ __forceinline__ int lower_tiles(int i, int col_tiles) {
+    const int need = ((i + 1) * kTileM + BN - 1) / BN;
+    return need < col_tiles ? need : col_tiles;
+}
+
+template <int BN, Product WHAT>
+__device__ __forceinline__ Tile tile_at(const ProductArgs& P, int64_t t) {
+    Tile T;
+    T.b = static_cast<int>(t / P.tiles);
+    int r = static_cast<int>(t - T.b * P.tiles);
+    if constexpr (kSymmetric<WHAT>) {
+        T.i = 0;
+        while (true) {
+            const int c = lower_tiles<BN>(T.i, P.col_tiles);
+            if (r < c) break;
+            r -= c;
+            ++T.i;
+        }
+        T.j = r;
+    } else {
+        // Eight row tiles at a time, so that concurrent tiles share operands in L2.
+        constexpr int G = 8;
+        const int group = r / (G * P.col_tiles), first = group * G;
+        const int rows = P.row_tiles - first < G ? P.row_tiles - first : G;
+        r -= group * G * P.col_tiles;
+        T.i = first + r % rows;
+        T.j = r / rows;
+    }
+    return T;
+}
+
+__device__ __forceinline__ void unpack_halves(const uint4* p, float (&v)[32]) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        float f[8];
+        unpack<CB_F16>(p[k], f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[8 * k + e] = f[e];
+    }
+}
+__device__ __forceinline__ void store_halves(__half* p, const float (&v)[32]) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const __half2 h = __floats2half2_rn(v[8 * k + 2 * e], v[8 * k + 2 * e + 1]);
+            memcpy(&w[e], &h, 4);
+        }
+        reinterpret_cast<uint4*>(p)[k] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// 32 columns [col, col + 32) of row `row` of a tile's result: `v` holds the products' sums.
+template <int BN, Product WHAT>
+__device__ __forceinline__ void finish(const ProductArgs& P, const Tile& T, int row, int col, float (&v)[32],
+                                       float (*stage)[33], int lane) {
+    const bool live = row < P.m;
+    if constexpr (WHAT == kGram) {
+        constexpr float s = kScaleA / (kScaleX * kScaleX);
+#pragma unroll
+        for (int k = 0; k < 32; ++k) v[k] *= s;
+    } else if constexpr (WHAT == kPoly) {
+        float t[32] = {};
+        if (live)
+            unpack_halves(reinterpret_cast<const uint4*>(P.term_hi + T.b * P.term_batch +
+                                                         static_cast<int64_t>(row) * P.term_ld + col), t);
+        const float c = P.c / kScaleA, diagonal = P.a * kScaleA;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+            v[k] = fmaf(c, v[k], P.b * t[k]);
+            if (row == col + k) v[k] += diagonal;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 32; ++k) v[k] *= 1.f / kScaleA;
+        if (P.a != 0.f && live) {
+            const int64_t at = T.b * P.term_batch + static_cast<int64_t>(row) * P.term_ld + col;
+            float t[32];
+            if (P.term_lo) {
+                unpack_halves(reinterpret_cast<const uint4*>(P.term_lo + at), t);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) v[k] = fmaf(P.a, t[k], v[k]);
+            }
+            unpack_halves(reinterpret_cast<const uint4*>(P.term_hi + at), t);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) v[k] = fmaf(P.a, t[k], v[k]);
+        }
+    }
+    if constexpr (kSymmetric<WHAT>) {
+        __half* out = P.out_hi + T.b * P.out_batch;
+        const int block = col / kTileM;
+        if (live && block <= T.i) store_halves(out + static_cast<int64_t>(row) * P.out_ld + col, v);
+        if (live && block < T.i) {  // whole blocks of columns below the diagonal: all within the matrix
+#pragma unroll
+            for (int k = 0; k < 32; ++k) out[static_cast<int64_t>(col + k) * P.out_ld + row] = __float2half_rn(v[k]);
+        }
+    } else if constexpr (WHAT == kUpdate) {
+        if (live) {
+            const int64_t at = T.b * P.out_batch + static_cast<int64_t>(row) * P.out_ld + col;
+            store_halves(P.out_hi + at, v);
+            if (P.out_lo) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) v[k] -= __half2float(__float2half_rn(v[k]));
+                store_halves(P.out_lo + at, v);
+            }
+        }
+    } else {
+        char* user = static_cast<char*>(P.user) + T.b * P.user_batch * dtype_bytes(P.user_dtype);
+        auto put = [&](int64_t at, float x) {
+            x *= 1.f / kScaleX;
+            if (P.weights) x = fmaf(-P.rate, x, P.keep * load_value(user, at, P.user_dtype));
+            store_value(user, at, x, P.user_dtype);
+        };
+        if (P.transposed) {  // lanes are consecutive columns of the caller's matrix
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+                if (live && col + k < P.n) put(static_cast<int64_t>(col + k) * P.user_row + row, v[k]);
+        } else {  // 32 x 32 values through shared memory, so that they are here too
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) stage[lane][k] = v[k];
+            __syncwarp();
+            const int first = row - lane;
+#pragma unroll 8
+            for (int k = 0; k < 32; ++k)
+                if (first + k < P.m && col + lane < P.n)
+                    put(static_cast<int64_t>(first + k) * P.user_row + col + lane, stage[k][lane]);
+        }
+    }
+}
+
+// C = A B in tiles of 128 x BN, tile after tile by each block. Operand A is K-major; B is
+// K-major for the symmetric products (A's own rows), and X as it lies (MN-major) for B X.
+// One warp copies tiles of 64 of K into a ring of stages, one issues the products into
+// one of two accumulators in TMEM, four take the other through the epilogue.
+template <int BN, Product WHAT>
+__global__ void __launch_bounds__(kProductThreads, 1)
+muon_product_kernel(const __grid_constant__ CUtensorMap left, const __grid_constant__ CUtensorMap right,
+                    const ProductArgs P) {
+    constexpr int S = kStages<BN>;
+    constexpr uint32_t kColumns = 2 * BN;
+    extern __shared__ unsigned char dynamic[];
+    unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~uintptr_t(1023));
+    __shared__ uint64_t full[S], empty[S], ready[2], drained[2];
+    __shared__ uint32_t tmem_at;
+    __shared__ float stage[WHAT == kResult ? kEpilogueWarps * 32 : 1][33];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S; ++s) {
+            tc::barrier_init(tc::smem_addr(full + s), 1);
+            tc::barrier_init(tc::smem_addr(empty + s), 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            tc::barrier_init(tc::smem_addr(ready + s), 1);
+            tc::barrier_init(tc::smem_addr(drained + s), kEpilogueWarps);
+        }
+        tc::barrier_init_fence();
+        tc::tma_prefetch(&left);
+        tc::tma_prefetch(&right);
+    }
+    if (warp == kEpilogueWarps) tc::tmem_alloc(tc::smem_addr(&tmem_at), kColumns);
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    const uint32_t tmem = tmem_at;
+    begin_kernel();
+    const int64_t total = P.tiles * P.batch;
+    const int ksteps = (P.k + kTileK - 1) / kTileK;
+    bool ok = true;
+
+    if (warp == kEpilogueWarps) {
+        if (lane == 0) {  // copies
+            int s = 0;
+            uint32_t phase = 0;
+            for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
+                const Tile T = tile_at<BN, WHAT>(P, t);
+                for (int k = 0; k < ksteps; ++k) {
+                    if (!(ok = tc::barrier_wait(tc::smem_addr(empty + s), phase ^ 1))) break;
+                    const uint32_t bar = tc::smem_addr(full + s);
+                    uint32_t at = tc::smem_addr(ring) + s * kStageBytes<BN>;
+                    tc::barrier_expect(bar, kStageBytes<BN>);
+#pragma unroll
+                    for (int x = 0; x < kTileM / 64; ++x, at += kBoxBytes)
+                        tc::tma_load(at, &left, bar, k * kTileK, T.i * kTileM + x * 64, T.b);
+#pragma unroll
+                    for (int x = 0; x < BN / 64; ++x, at += kBoxBytes) {
+                        if constexpr (kSymmetric<WHAT>) tc::tma_load(at, &right, bar, k * kTileK, T.j * BN + x * 64, T.b);
+                        else tc::tma_load(at, &right, bar, T.j * BN + x * 64, k * kTileK, T.b);
+                    }
+                    if (++s == S) s = 0, phase ^= 1;
+                }
+            }
+            // Copies in flight land before the block's shared memory goes away: those of
+            // stages that were never multiplied, after a wait that ran out.
+            if (!ok)
+                for (int x = 0; x < S; ++x) {
+                    if (--s < 0) s = S - 1, phase ^= 1;
+                    if (!tc::barrier_wait(tc::smem_addr(full + s), phase)) break;
+                }
+        }
+    } else if (warp == kEpilogueWarps + 1) {
+        if (lane == 0) {  // products
+            constexpr uint32_t shape = tc::mma_shape(kTileM, BN, !kSymmetric<WHAT>);
+            int s = 0, acc = 0;
+            uint32_t phase = 0, acc_phase = 0;
+            for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
+                if (!(ok = tc::barrier_wait(tc::smem_addr(drained + acc), acc_phase ^ 1))) break;
+                tc::fence_after();
+                for (int k = 0; k < ksteps; ++k) {
+                    if (!(ok = tc::barrier_wait(tc::smem_addr(full + s), phase))) break;
+                    tc::fence_after();
+                    const uint32_t at = tc::smem_addr(ring) + s * kStageBytes<BN>, bt = at + kTileM * kTileK * 2;
+#pragma unroll
+                    for (int x = 0; x < kTileK / 16; ++x) {
+                        const uint64_t da = tc::operand_k_major(at + x * 32);
+                        const uint64_t db = kSymmetric<WHAT> ? tc::operand_k_major(bt + x * 32)
+                                                            : tc::operand_mn_major(bt + x * 2048, kBoxBytes);
+                        tc::mma_f16(tmem + acc * BN, da, db, shape, k > 0 || x > 0);
+                    }
+                    tc::mma_commit(tc::smem_addr(empty + s));
+                    if (++s == S) s = 0, phase ^= 1;
+                }
+                tc::mma_commit(tc::smem_addr(ready + acc));
+                if (++acc == 2) acc = 0, acc_phase ^= 1;
+            }
+        }
+    } else {  // epilogue: warp w has the rows 32 w .. 32 w + 31 of the tile
+        int acc = 0;
+        uint32_t acc_phase = 0;
+        for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
+            const Tile T = tile_at<BN, WHAT>(P, t);
+            if (!(ok = __all_sync(kFull, tc::barrier_wait(tc::smem_addr(ready + acc), acc_phase)))) break;
+            tc::fence_after();
+            const int row = T.i * kTileM + warp * 32 + lane;
+            // 32 columns that no row of C has, or that the other triangle gives, are skipped.
+            for (int c = 0; c < BN; c += 32) {
+                const int col = T.j * BN + c;
+                if (col >= P.n || (kSymmetric<WHAT> && col / kTileM > T.i)) break;
+                float v[32];
+                tc::tmem_load32(tmem + (static_cast<uint32_t>(warp * 32) << 16) + acc * BN + c, v);
+                finish<BN, WHAT>(P, T, row, col, v, stage + (WHAT == kResult ? warp * 32 : 0), lane);
+            }
+            tc::fence_before();
+            __syncwarp();
+            if (lane == 0) tc::barrier_arrive(tc::smem_addr(drained + acc));
+            if (++acc == 2) acc = 0, acc_phase ^= 1;
+        }
+    }
+    if (!ok && lane == 0) set_error(P.error, CB_ERR_TIMEOUT);
+    __syncwarp();
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    if (warp == kEpilogueWarps) tc::tmem_free(tmem, kColumns);
+}
+
+// ---------------------------------------------------------------- host
+
+PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
+    static PFN_cuTensorMapEncodeTiled_v12000 encode = [] {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) !=
+                cudaSuccess || q != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            fn = nullptr;
+        }
+        return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
+    }();
+    return encode;
+}
+
+// [batch][rows][cols] of fp16 with rows of `ld` values, in boxes of 64 x 64; values past
+// a row or past the rows read as zeros.
+bool tensor_map(CUtensorMap* map, const void* data, int64_t cols, int64_t rows, int64_t batch, int64_t ld) {
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows),
+                                static_cast<cuuint64_t>(batch)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(ld) * rows * 2};
+    const cuuint32_t box[3] = {64, 64, 1};
+    const cuuint32_t step[3] = {1, 1, 1};
+    return tensor_map_encoder()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(data), dims, strides, box,
+                                step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+struct Workspace {
+    int64_t p, q, ldx, lda;
+    size_t hi[2], lo[2], gram, poly, partial, error, bytes;
+};
+Workspace layout(int32_t batch, int32_t rows, int32_t cols) {
+    Workspace w;
+    w.p = rows < cols ? rows : cols;
+    w.q = rows < cols ? cols : rows;
+    w.ldx = round_up(w.q, 64);
+    w.lda = round_up(w.p, 64);
+    size_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const size_t here = at;
+        at += static_cast<size_t>(round_up(bytes, 256));
+        return here;
+    };
+    const int64_t x = batch * w.p * w.ldx * 2, a = batch * w.p * w.lda * 2;
+    w.hi[0] = take(x);
+    w.hi[1] = take(x);
+    w.lo[0] = take(x);
+    w.lo[1] = take(x);
+    w.gram = take(a);
+    w.poly = take(a);
+    w.partial = take(static_cast<int64_t>(batch) * kNormBlocks * 3 * 4);
+    w.error = take(4);
+    w.bytes = at;
+    return w;
+}
+
+bool current_sms(int* sms) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) == cudaSuccess &&
+        cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && *sms > 0)
+        return true;
+    cudaGetLastError();
+    return false;
+}
+
+template <int BN, Product WHAT>
+int64_t tiles_of(int32_t m, int32_t n) {
+    const int row_tiles = (m + kTileM - 1) / kTileM, col_tiles = (n + BN - 1) / BN;
+    if (!kSymmetric<WHAT>) return static_cast<int64_t>(row_tiles) * col_tiles;
+    int64_t t = 0;
+    for (int i = 0; i < row_tiles; ++i) t += lower_tiles<BN>(i, col_tiles);
+    return t;
+}
+
+template <int BN, Product WHAT>
+bool launch_product(const CUtensorMap& left, const CUtensorMap& right, ProductArgs P, int sms, cudaStream_t s) {
+    P.row_tiles = (P.m + kTileM - 1) / kTileM;
+    P.col_tiles = (P.n + BN - 1) / BN;
+    P.tiles = tiles_of<BN, WHAT>(P.m, P.n);
+    const int64_t total = P.tiles * P.batch;
+    const size_t smem = kStages<BN> * kStageBytes<BN> + 1024;
+    if (cudaFuncSetAttribute(muon_product_kernel<BN, WHAT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             static_cast<int>(smem)) != cudaSuccess)
+        return false;
+    launch(muon_product_kernel<BN, WHAT>, dim3(static_cast<unsigned>(min64(total, sms))), dim3(kProductThreads), smem, s,
+           left, right, P);
+    return true;
+}
+
+// The tile width with the least time: rounds of tiles over the GPU, each as long as a
+// tile's products (an SM's shared memory feeds narrow tiles below the tensor cores'
+// rate) and what a tile costs besides.
+template <Product WHAT>
+bool launch_best(const CUtensorMap& left, const CUtensorMap& right, const ProductArgs& P, int sms, cudaStream_t s) {
+    auto rounds = [&](int64_t tiles) { return (tiles * P.batch + sms - 1) / sms; };
+    const int64_t t64 = rounds(tiles_of<64, WHAT>(P.m, P.n)) * 96, t128 = rounds(tiles_of<128, WHAT>(P.m, P.n)) * 144,
+                  t256 = rounds(tiles_of<256, WHAT>(P.m, P.n)) * 264;
+    if (t256 <= t128 && t256 <= t64) return launch_product<256, WHAT>(left, right, P, sms, s);
+    if (t128 <= t64) return launch_product<128, WHAT>(left, right, P, sms, s);
+    return launch_product<64, WHAT>(left, right, P, sms, s);
+}
+
+bool valid_dtype(int d) { return d == CB_F32 || d == CB_F16 || d == CB_BF16; }
+
+struct Result {
+    void* data;
+    cb_dtype dtype;
+    int64_t batch_stride, row_stride;
+    bool weights;
+    float keep, rate;
+};
+
+bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const float* coefficients, int32_t steps,
+                        const Result& out, void* workspace, int64_t workspace_bytes, int* error, cudaStream_t s) {
+    if (batch < 0 || in.rows < 0 || in.cols < 0 || batch > 65535 || in.rows > (1 << 20) || in.cols > (1 << 20))
+        return CB_ERR_INVALID_ARG;
+    if (steps < 1 || steps > kMaxSteps || !coefficients || !(eps >= 0.f) || !valid_dtype(in.dtype) ||
+        !valid_dtype(out.dtype))
+        return CB_ERR_INVALID_ARG;
+    for (int k = 0; k < 3 * steps; ++k)
+        if (!std::isfinite(coefficients[k])) return CB_ERR_INVALID_ARG;
+    if (batch == 0 || in.rows == 0 || in.cols == 0) return CB_OK;
+    const int64_t matrix = static_cast<int64_t>(in.rows) * in.cols;
+    if (!in.g || !out.data || in.g_row < in.cols || out.row_stride < in.cols ||
+        (batch > 1 && (in.g_batch < 0 || out.batch_stride < matrix)) || matrix > (int64_t(1) << 38) / batch)
+        return CB_ERR_INVALID_ARG;
+    if (in.momentum && (in.m_row < in.cols || (batch > 1 && in.m_batch < matrix))) return CB_ERR_INVALID_ARG;
+    if (!aligned(in.g, dtype_bytes(in.dtype)) || !aligned(out.data, dtype_bytes(out.dtype)) ||
+        !aligned(in.momentum, 4) || !aligned(error, 4))
+        return CB_ERR_INVALID_ARG;
+    const Workspace w = layout(batch, in.rows, in.cols);
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < static_cast<int64_t>(w.bytes)) return CB_ERR_CAPACITY;
+    int sms = 0;
+    if (!current_sms(&sms) || !tensor_map_encoder()) return CB_ERR_CUDA;
+    char* base = static_cast<char*>(workspace);
+    __half* hi[2] = {reinterpret_cast<__half*>(base + w.hi[0]), reinterpret_cast<__half*>(base + w.hi[1])};
+    __half* lo[2] = {reinterpret_cast<__half*>(base + w.lo[0]), reinterpret_cast<__half*>(base + w.lo[1])};
+    __half* gram = reinterpret_cast<__half*>(base + w.gram);
+    __half* poly = reinterpret_cast<__half*>(base + w.poly);
+    float* partial = reinterpret_cast<float*>(base + w.partial);
+    if (!error) error = reinterpret_cast<int*>(base + w.error);  // any value: read by nobody
+    const bool tall = in.rows > in.cols;
+
+    CUtensorMap map_x[2], map_gram, map_poly;
+    if (!tensor_map(&map_x[0], hi[0], w.q, w.p, batch, w.ldx) || !tensor_map(&map_x[1], hi[1], w.q, w.p, batch, w.ldx) ||
+        !tensor_map(&map_gram, gram, w.p, w.p, batch, w.lda) || !tensor_map(&map_poly, poly, w.p, w.p, batch, w.lda))
+        return CB_ERR_CUDA;
+
+    const int norm_blocks = static_cast<int>(max64(1, min64(kNormBlocks, (matrix + 8 * 1024 - 1) / (8 * 1024))));
+    const bool vector = in.cols % 4 == 0 && in.g_row % 4 == 0 && (batch == 1 || in.g_batch % 4 == 0) &&
+                        aligned(in.g, 4 * dtype_bytes(in.dtype)) &&
+                        (!in.momentum || (in.m_row % 4 == 0 && (batch == 1 || in.m_batch % 4 == 0) &&
+                                          aligned(in.momentum, 16)));
+    const dim3 norm_grid(norm_blocks, batch);
+    if (vector) launch(muon_norm_kernel<4>, norm_grid, dim3(kNormThreads), 0, s, in, partial);
+    else launch(muon_norm_kernel<1>, norm_grid, dim3(kNormThreads), 0, s, in, partial);
+    const dim3 cast_grid((in.cols + kCastTile - 1) / kCastTile, (in.rows + kCastTile - 1) / kCastTile, batch);
+    const int64_t x_batch = w.p * w.ldx, a_batch = w.p * w.lda;
+    const int ldx = static_cast<int>(w.ldx), lda = static_cast<int>(w.lda);
+    if (tall) launch(muon_cast_kernel<true>, cast_grid, dim3(256), 0, s, in, partial, norm_blocks, eps, hi[0], lo[0], ldx, x_batch);
+    else launch(muon_cast_kernel<false>, cast_grid, dim3(256), 0, s, in, partial, norm_blocks, eps, hi[0], lo[0], ldx, x_batch);
+
+    bool sent = true;
+    for (int k = 0; k < steps; ++k) {
+        const int now = k & 1, next = now ^ 1;
+        const float a = coefficients[3 * k], b = coefficients[3 * k + 1], c = coefficients[3 * k + 2];
+        const bool two_term = k < kTwoTerm;
+        ProductArgs P{};
+        P.batch = batch;
+        P.error = error;
+        P.m = P.n = static_cast<int32_t>(w.p);
+        P.k = static_cast<int32_t>(w.q);
+        P.out_hi = gram;
+        P.out_batch = a_batch;
+        P.out_ld = lda;
+        sent &= launch_best<kGram>(map_x[now], map_x[now], P, sms, s);
+        P.k = P.m;
+        P.a = two_term ? 0.f : a;
+        P.b = b;
+        P.c = c;
+        P.term_hi = gram;
+        P.term_batch = a_batch;
+        P.term_ld = lda;
+        P.out_hi = poly;
+        sent &= launch_best<kPoly>(map_gram, map_gram, P, sms, s);
+        P.n = static_cast<int32_t>(w.q);
+        P.a = two_term ? a : 0.f;
+        P.term_hi = hi[now];
+        P.term_lo = two_term ? lo[now] : nullptr;
+        P.term_batch = x_batch;
+        P.term_ld = ldx;
+        P.out_hi = hi[next];
+        P.out_lo = k + 1 < kTwoTerm ? lo[next] : nullptr;
+        P.out_batch = x_batch;
+        P.out_ld = ldx;
+        if (k + 1 < steps) {
+            sent &= launch_best<kUpdate>(map_poly, map_x[now], P, sms, s);
+        } else {
+            P.user = out.data;
+            P.user_batch = out.batch_stride;
+            P.user_row = out.row_stride;
+            P.user_dtype = out.dtype;
+            P.transposed = tall;
+            P.weights = out.weights;
+            P.keep = out.keep;
+            P.rate = out.rate;
+            sent &= launch_best<kResult>(map_poly, map_x[now], P, sms, s);
+        }
+    }
+    return cudaGetLastError() == cudaSuccess && sent ? CB_OK : CB_ERR_CUDA;
+}
+
+}  // namespace
+}  // namespace cbtbe
+
+extern "C" int64_t cb_muon_workspace_bytes(int32_t batch, int32_t rows, int32_t cols) {
+    if (batch <= 0 || rows <= 0 || cols <= 0) return 0;
+    return static_cast<int64_t>(cbtbe::layout(batch, rows, cols).bytes);
+}
+
+extern "C" cb_status cb_muon_orthogonalise(const void* g, cb_dtype g_dtype, int32_t batch, int32_t rows, int32_t cols,
+                                           int64_t g_batch_stride, int64_t g_row_stride, float eps,
+                                           const float* coefficients, int32_t steps, void* out, cb_dtype out_dtype,
+                                           int64_t out_batch_stride, int64_t out_row_stride, void* workspace,
+                                           int64_t workspace_bytes, int* error, cudaStream_t stream) {
+    using namespace cbtbe;
+    MatrixIn in{};
+    in.g = g;
+    in.g_batch = g_batch_stride;
+    in.g_row = g_row_stride;
+    in.dtype = g_dtype;
+    in.rows = rows;
+    in.cols = cols;
+    const Result r{out, out_dtype, out_batch_stride, out_row_stride, false, 0.f, 0.f};
+    return orthogonalise(in, batch, eps, coefficients, steps, r, workspace, workspace_bytes, error, stream);
+}
+
+extern "C" cb_status cb_muon_step(void* weights, cb_dtype w_dtype, int64_t w_batch_stride, int64_t w_row_stride,
+                                  const void* g, cb_dtype g_dtype, int64_t g_batch_stride, int64_t g_row_stride,
+                                  float* momentum, int64_t m_batch_stride, int64_t m_row_stride, int32_t batch,
+                                  int32_t rows, int32_t cols, float lr, float weight_decay, float beta, int nesterov,
+                                  float eps, const float* coefficients, int32_t steps, float update_scale,
+                                  void* workspace, int64_t workspace_bytes, int* error, cudaStream_t stream) {
+    using namespace cbtbe;
+    if (!(lr == lr) || !(weight_decay == weight_decay) || !(beta >= 0.f) || !(update_scale == update_scale))
+        return CB_ERR_INVALID_ARG;
+    if (!momentum && batch > 0 && rows > 0 && cols > 0) return CB_ERR_INVALID_ARG;
+    MatrixIn in{};
+    in.g = g;
+    in.momentum = momentum;
+    in.g_batch = g_batch_stride;
+    in.g_row = g_row_stride;
+    in.m_batch = m_batch_stride;
+    in.m_row = m_row_stride;
+    in.dtype = g_dtype;
+    in.rows = rows;
+    in.cols = cols;
+    in.beta = beta;
+    in.nesterov = nesterov;
+    const Result r{weights, w_dtype, w_batch_stride, w_row_stride, true,
+                   static_cast<float>(1.0 - static_cast<double>(lr) * weight_decay),
+                   static_cast<float>(static_cast<double>(lr) * update_scale)};
+    return orthogonalise(in, batch, eps, coefficients, steps, r, workspace, workspace_bytes, error, stream);
+}

@@ -1,0 +1,739 @@
+// token_embedding.cu -- a scaled row of one table for every token, and the dense
+// gradient of the table.
+//
+//   out[i, :]   = scale * E[token_i, :]
+//   dE[v, :] (+)= scale * sum over the positions i with token_i = v of grad_out[i, :]
+//
+// Both move rows and do an operation or two per value: HBM's bandwidth is their bound,
+// launches and dependent loads at a few tokens.
+#include "token_rows.cuh"
+#include "tbe_launch.h"
+
+namespace cbtbe {
+namespace {
+
+// ---------------------------------------------------------------- lookup
+
+constexpr int kLookupThreads = 256;
+constexpr int kLookupPieces = 4;  // pieces in flight per thread
+
+struct LookupArgs {
+    Tokens tokens;
+    const void* table;
+    int64_t row_stride;  // values
+    Positions out_at;
+    void* out;
+    uint32_t pieces;     // per row
+    float scale;
+    int* error;
+};
+
+// A block takes kLookupThreads * kLookupPieces consecutive pieces (of V values) of the
+// output, a thread every kLookupThreads-th: rows of any length fill the threads, stores
+// are consecutive, and each thread has its loads in flight together.
+template <int IN, int OUT, int V>
+__global__ void __launch_bounds__(kLookupThreads) token_lookup_kernel(const LookupArgs P) {
+    begin_kernel();
+    const uint64_t first = static_cast<uint64_t>(blockIdx.x) * (kLookupThreads * kLookupPieces);
+    const uint32_t row0 = static_cast<uint32_t>(first / P.pieces);
+    const uint32_t within = static_cast<uint32_t>(first - static_cast<uint64_t>(row0) * P.pieces) + threadIdx.x;
+    Piece<IN, V> x[kLookupPieces];
+    uint32_t row[kLookupPieces], piece[kLookupPieces];
+    int64_t token[kLookupPieces];
+#pragma unroll
+    for (int u = 0; u < kLookupPieces; ++u) {
+        const uint32_t k = within + u * kLookupThreads;
+        const uint32_t r = k / P.pieces;
+        row[u] = row0 + r;
+        piece[u] = k - r * P.pieces;
+        token[u] = row[u] < P.tokens.n ? P.tokens.load(row[u]) : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < kLookupPieces; ++u) {
+        const bool valid = token[u] >= 0 && token[u] < P.tokens.rows;
+        x[u] = zero_piece<IN, V>();
+        if (row[u] < P.tokens.n) {
+            if (valid)
+                x[u] = load_piece<IN, V>(static_cast<const char*>(P.table) +
+                                         (token[u] * P.row_stride + static_cast<int64_t>(piece[u]) * V) *
+                                             dtype_bytes(IN));
+            else if (P.error && piece[u] == 0) set_error(P.error, CB_ERR_INDEX_OOB);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kLookupPieces; ++u) {
+        if (row[u] < P.tokens.n) {
+            float f[V];
+            widen<IN, V>(x[u], f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) f[i] *= P.scale;
+            store_piece<OUT, V>(static_cast<char*>(P.out) +
+                                    (P.out_at.at(row[u]) + static_cast<int64_t>(piece[u]) * V) * dtype_bytes(OUT), f);
+        }
+    }
+}
+
+template <int IN, int OUT, int V>
+void launch_lookup(LookupArgs P, int32_t dim, cudaStream_t s) {
+    P.pieces = static_cast<uint32_t>(dim / V);
+    const uint64_t total = static_cast<uint64_t>(P.tokens.n) * P.pieces;
+    const uint64_t per = kLookupThreads * kLookupPieces;
+    launch(token_lookup_kernel<IN, OUT, V>, dim3(static_cast<unsigned>((total + per - 1) / per)), dim3(kLookupThreads), 0,
+           s, P);
+}
+template <int IN, int OUT>
+void launch_lookup(const LookupArgs& P, int32_t dim, int v, cudaStream_t s) {
+    if (v == 8) launch_lookup<IN, OUT, 8>(P, dim, s);
+    else if (v == 4) launch_lookup<IN, OUT, 4>(P, dim, s);
+    else launch_lookup<IN, OUT, 1>(P, dim, s);
+}
+template <int IN>
+void launch_lookup(const LookupArgs& P, int32_t dim, int v, int out_dtype, cudaStream_t s) {
+    if (out_dtype == CB_F32) launch_lookup<IN, CB_F32>(P, dim, v, s);
+    else if (out_dtype == CB_F16) launch_lookup<IN, CB_F16>(P, dim, v, s);
+    else launch_lookup<IN, CB_BF16>(P, dim, v, s);
+}
+
+// ---------------------------------------------------------------- gradient
+
+struct GradArgs {
+    Tokens tokens;
+    int64_t padding;      // the token that gets no gradient, or -1
+    const void* grad_out;
+    Positions go_at;
+    int32_t dim;
+    float scale;
+    void* grad;           // [rows, dim]
+    int64_t grad_stride;  // values
+    int32_t grad_dtype;
+    int32_t accumulate;
+    int* error;
+};
+
+// The columns of a lane in a slab of a row: J pieces of V values, 32 pieces apart.
+template <int V> constexpr int kLanePieces = V == 1 ? 4 : 1;
+template <int V> constexpr int kSlab = 32 * V * kLanePieces<V>;
+template <int DT, int V>
+struct LanePieces {
+    Piece<DT, V> x[kLanePieces<V>];
+};
+template <int DT, int V>
+__device__ __forceinline__ LanePieces<DT, V> load_go(const GradArgs& P, uint32_t position, int col) {
+    LanePieces<DT, V> r;
+    const char* p = static_cast<const char*>(P.grad_out) + (P.go_at.at(position) + col) * dtype_bytes(DT);
+#pragma unroll
+    for (int j = 0; j < kLanePieces<V>; ++j)
+        r.x[j] = col + j * 32 * V < P.dim ? load_piece<DT, V>(p + j * 32 * V * dtype_bytes(DT)) : zero_piece<DT, V>();
+    return r;
+}
+template <int V>
+struct Sum {
+    float f[kLanePieces<V>][V];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int j = 0; j < kLanePieces<V>; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) f[j][i] = 0.f;
+    }
+    template <int DT>
+    __device__ __forceinline__ void add(const LanePieces<DT, V>& r) {
+#pragma unroll
+        for (int j = 0; j < kLanePieces<V>; ++j) {
+            float y[V];
+            widen<DT, V>(r.x[j], y);
+#pragma unroll
+            for (int i = 0; i < V; ++i) f[j][i] += y[i];
+        }
+    }
+    // The lane's sums at columns col, .. of an fp32 row of `dim` values (16-byte aligned).
+    __device__ __forceinline__ void put(float* row, int col, int dim) const {
+#pragma unroll
+        for (int j = 0; j < kLanePieces<V>; ++j) {
+            float* p = row + col + j * 32 * V;
+            if (col + j * 32 * V >= dim) break;
+            if constexpr (V == 1) {
+                *p = f[j][0];
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; i += 4)
+                    *reinterpret_cast<float4*>(p + i) = make_float4(f[j][i], f[j][i + 1], f[j][i + 2], f[j][i + 3]);
+            }
+        }
+    }
+    __device__ __forceinline__ void add(const float* row, int col, int dim) {
+#pragma unroll
+        for (int j = 0; j < kLanePieces<V>; ++j) {
+            const float* p = row + col + j * 32 * V;
+            if (col + j * 32 * V >= dim) break;
+            if constexpr (V == 1) {
+                f[j][0] += *p;
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; i += 4) {
+                    const float4 x = *reinterpret_cast<const float4*>(p + i);
+                    f[j][i] += x.x;
+                    f[j][i + 1] += x.y;
+                    f[j][i + 2] += x.z;
+                    f[j][i + 3] += x.w;
+                }
+            }
+        }
+    }
+};
+
+template <int DT, int V>
+__device__ __forceinline__ void add_stored(const void* p, float (&f)[V]) {
+    const Piece<DT, V> x = load_piece<DT, V, false>(p);  // written by this kernel: not through the read-only path
+    float y[V];
+    widen<DT, V>(x, y);
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] += y[i];
+}
+
+// The finished sum of a table row: scaled, added to what is there or not, rounded once.
+template <int V>
+__device__ __forceinline__ void finish_row(const GradArgs& P, int64_t row, int col, const Sum<V>& s) {
+    char* p = static_cast<char*>(P.grad) + (row * P.grad_stride + col) * dtype_bytes(P.grad_dtype);
+#pragma unroll
+    for (int j = 0; j < kLanePieces<V>; ++j) {
+        if (col + j * 32 * V >= P.dim) break;
+        char* q = p + j * 32 * V * dtype_bytes(P.grad_dtype);
+        float f[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = s.f[j][i] * P.scale;
+        if (P.grad_dtype == CB_F32) {
+            if (P.accumulate) add_stored<CB_F32, V>(q, f);
+            store_piece<CB_F32, V>(q, f);
+        } else if (P.grad_dtype == CB_F16) {
+            if (P.accumulate) add_stored<CB_F16, V>(q, f);
+            store_piece<CB_F16, V>(q, f);
+        } else {
+            if (P.accumulate) add_stored<CB_BF16, V>(q, f);
+            store_piece<CB_BF16, V>(q, f);
+        }
+    }
+}
+template <int V>
+__device__ __forceinline__ void zero_row(const GradArgs& P, int64_t row, int lane) {
+    Sum<V> zero;
+    zero.clear();
+    for (int col = lane * V; col < P.dim; col += kSlab<V>) finish_row<V>(P, row, col, zero);
+}
+
+// The sort key of a token: its row, or `rows` (after all rows) for one without gradient.
+__device__ __forceinline__ uint32_t token_key(const GradArgs& P, int64_t token, bool report) {
+    const bool valid = token >= 0 && token < P.tokens.rows;
+    if (!valid && report && P.error) set_error(P.error, CB_ERR_INDEX_OOB);
+    return valid && token != P.padding ? static_cast<uint32_t>(token) : static_cast<uint32_t>(P.tokens.rows);
+}
+
+// ---------------------------------------------------------------- few tokens: by matching
+
+constexpr int kMatchThreads = 256;
+constexpr int kMatchWarps = kMatchThreads / 32;
+constexpr uint32_t kMatchTokens = 2048;  // most tokens of a call without a sort
+constexpr int kMatchSlabs = 8;           // slabs of a row per block
+constexpr int kFillRows = 64;            // rows of the gradient per zeroing block
+
+// One block per (token, group of slabs): the first position of its token sums all of the
+// token's positions, in order; other blocks end at once. The blocks after those write zeros
+// to the rows that no token names. n is at most kMatchTokens, so that a block reads all
+// tokens in a few loads, and the call is one launch.
+template <int DT, int V>
+__global__ void __launch_bounds__(kMatchThreads) token_match_kernel(const GradArgs P, uint32_t token_blocks,
+                                                                    int slab_groups) {
+    __shared__ uint16_t list[kMatchTokens];
+    __shared__ int counts[kMatchWarps];
+    __shared__ int touched[kFillRows];
+    __shared__ __align__(16) float part[kMatchWarps][kSlab<V>];
+    begin_kernel();
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const uint32_t n = P.tokens.n;
+    if (blockIdx.x >= token_blocks) {
+        const int64_t r0 = static_cast<int64_t>(blockIdx.x - token_blocks) * kFillRows;
+        if (threadIdx.x < kFillRows) touched[threadIdx.x] = 0;
+        __syncthreads();
+        for (uint32_t j = threadIdx.x; j < n; j += kMatchThreads) {
+            const int64_t r = static_cast<int64_t>(token_key(P, P.tokens.load(j), false)) - r0;
+            if (r >= 0 && r < kFillRows) touched[r] = 1;
+        }
+        __syncthreads();
+        for (int r = wid; r < kFillRows && r0 + r < P.tokens.rows; r += kMatchWarps)
+            if (!touched[r]) zero_row<V>(P, r0 + r, lane);
+        return;
+    }
+    const uint32_t i = blockIdx.x / slab_groups;
+    const int group = blockIdx.x % slab_groups;
+    const uint32_t key = token_key(P, P.tokens.load(i), threadIdx.x == 0 && group == 0);
+    if (key == static_cast<uint32_t>(P.tokens.rows)) return;
+    bool earlier = false;
+    for (uint32_t j = threadIdx.x; j < i; j += kMatchThreads) earlier |= token_key(P, P.tokens.load(j), false) == key;
+    if (__syncthreads_or(earlier)) return;
+    // The token's positions in order: every warp a part of the positions from i on.
+    const uint32_t per = (n - i + kMatchWarps - 1) / kMatchWarps;
+    const uint32_t lo = min(i + wid * per, n), hi = min(lo + per, n);
+    int mine = 0;
+    for (uint32_t j0 = lo; j0 < hi; j0 += 32) {
+        const uint32_t j = j0 + lane;
+        const bool same = j < hi && token_key(P, P.tokens.load(j), false) == key;
+        const uint32_t mask = __ballot_sync(kFull, same);
+        if (same) list[lo - i + mine + __popc(mask & ((1u << lane) - 1u))] = static_cast<uint16_t>(j);
+        mine += __popc(mask);
+    }
+    if (lane == 0) counts[wid] = mine;
+    __syncthreads();
+    int count = 0, before = 0;
+    for (int w = 0; w < kMatchWarps; ++w) {
+        before += w < wid ? counts[w] : 0;
+        count += counts[w];
+    }
+    uint16_t moved[kMatchTokens / kMatchWarps / 32];
+#pragma unroll
+    for (int k = 0; k < static_cast<int>(kMatchTokens / kMatchWarps / 32); ++k)
+        moved[k] = k * 32 + lane < mine ? list[lo - i + k * 32 + lane] : 0;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < static_cast<int>(kMatchTokens / kMatchWarps / 32); ++k)
+        if (k * 32 + lane < mine) list[before + k * 32 + lane] = moved[k];
+    __syncthreads();
+    // Short lists: a warp per slab. Long ones: all warps on each slab, a part of the list each.
+    constexpr int U = 4;
+    const bool split = count > 2 * kMatchWarps;
+    const int a = split ? count * wid / kMatchWarps : 0, b = split ? count * (wid + 1) / kMatchWarps : count;
+    for (int k = split ? 0 : wid; k < kMatchSlabs; k += split ? 1 : kMatchWarps) {
+        const int slab = (group * kMatchSlabs + k) * kSlab<V>;
+        if (slab >= P.dim) break;
+        const int col = slab + lane * V;
+        Sum<V> sum;
+        sum.clear();
+        for (int j = a; j < b; j += U) {
+            LanePieces<DT, V> x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (j + u < b) x[u] = load_go<DT, V>(P, list[j + u], col);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (j + u < b) sum.add(x[u]);
+        }
+        if (split) {
+            sum.put(part[wid], lane * V, P.dim - slab);
+            __syncthreads();
+            if (wid == 0) {
+                sum.clear();
+                for (int w = 0; w < kMatchWarps; ++w) sum.add(part[w], lane * V, P.dim - slab);
+                finish_row<V>(P, key, col, sum);
+            }
+            __syncthreads();
+        } else {
+            finish_row<V>(P, key, col, sum);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- many tokens: sorted
+
+constexpr int kKeyThreads = 256;
+constexpr int kRadixDigits = 256;
+
+// Pairs (key, position), a tile of the sort per block, with the first pass's digit counts of
+// the tile; the later passes' counts are cleared, and the sort's description of its one
+// "table" (keys from 0) and tiles written.
+struct SortBuffers {
+    uint32_t *keys[2], *positions[2];
+    Chunk* tiles;
+    uint32_t* digits;  // [passes][tiles][256]
+    TableDev* table;
+    int64_t *first_tile, *num_tiles, *table_pos;  // [2], [1], [2]
+};
+__global__ void __launch_bounds__(kKeyThreads) token_keys_kernel(const GradArgs P, const SortBuffers S, int passes) {
+    __shared__ uint32_t sh[kRadixDigits];
+    begin_kernel();
+    const uint32_t n = P.tokens.n, tile = blockIdx.x, tiles = gridDim.x;
+    const uint32_t first = tile * static_cast<uint32_t>(kSortTileKeys);
+    const uint32_t count = min(static_cast<uint32_t>(kSortTileKeys), n - first);
+    sh[threadIdx.x] = 0;
+    __syncthreads();
+    for (uint32_t k = threadIdx.x; k < count; k += kKeyThreads) {
+        const uint32_t key = token_key(P, P.tokens.load(first + k), true);
+        S.keys[0][first + k] = key;
+        S.positions[0][first + k] = first + k;
+        atomicAdd(&sh[key & (kRadixDigits - 1)], 1u);
+    }
+    __syncthreads();
+    S.digits[tile * kRadixDigits + threadIdx.x] = sh[threadIdx.x];
+    for (int p = 1; p < passes; ++p)
+        S.digits[(static_cast<int64_t>(p) * tiles + tile) * kRadixDigits + threadIdx.x] = 0;
+    if (threadIdx.x == 0) {
+        Chunk c{};
+        c.k0 = first;
+        c.len = count;
+        S.tiles[tile] = c;
+        if (tile == 0) {
+            TableDev t{};
+            t.rows = P.tokens.rows;
+            *S.table = t;
+            S.first_tile[0] = S.table_pos[0] = 0;
+            S.first_tile[1] = *S.num_tiles = tiles;
+            S.table_pos[1] = n;
+        }
+    }
+}
+
+struct Sorted {
+    const uint32_t *keys, *positions;
+    uint32_t chunk, chunks;  // positions per chunk
+    float *head, *tail;      // [chunks, dim] sums of runs that began before / end after a chunk
+};
+
+constexpr int kReduceThreads = 256;
+constexpr int kReduceWarps = kReduceThreads / 32;
+constexpr int kReduceRows = 8;       // rows in flight per warp
+constexpr int kFillWarpRows = 8;     // rows of the gradient per zeroing warp
+
+// A warp takes a chunk of the sorted positions and a slab of columns: it adds the rows of a
+// run of equal keys and finishes the table row at the run's end. Runs cut by the chunk's ends
+// leave their sums for token_join_kernel. Warps past those write zeros to rows without a token,
+// found by bisection of the keys.
+template <int DT, int V>
+__global__ void __launch_bounds__(kReduceThreads) token_reduce_kernel(const GradArgs P, const Sorted S, int slabs,
+                                                                      uint32_t reduce_blocks) {
+    begin_kernel();
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const uint32_t n = P.tokens.n, none = static_cast<uint32_t>(P.tokens.rows);
+    if (blockIdx.x >= reduce_blocks) {
+        const int64_t r0 = (static_cast<int64_t>(blockIdx.x - reduce_blocks) * kReduceWarps + wid) * kFillWarpRows;
+        bool absent = false;
+        if (lane < kFillWarpRows && r0 + lane < P.tokens.rows) {
+            const uint32_t key = static_cast<uint32_t>(r0 + lane);
+            uint32_t lo = 0, hi = n;
+            while (lo < hi) {
+                const uint32_t mid = (lo + hi) / 2;
+                if (S.keys[mid] < key) lo = mid + 1;
+                else hi = mid;
+            }
+            absent = lo == n || S.keys[lo] != key;
+        }
+        uint32_t mask = __ballot_sync(kFull, absent);
+        while (mask) {
+            zero_row<V>(P, r0 + __ffs(mask) - 1, lane);
+            mask &= mask - 1;
+        }
+        return;
+    }
+    const uint64_t w = static_cast<uint64_t>(blockIdx.x) * kReduceWarps + wid;
+    const uint32_t chunk = static_cast<uint32_t>(w / slabs);
+    if (chunk >= S.chunks) return;
+    const int col = static_cast<int>(w - static_cast<uint64_t>(chunk) * slabs) * kSlab<V> + lane * V;
+    const uint32_t first = chunk * S.chunk, last = min(first + S.chunk, n);
+    bool begun = first == 0 || S.keys[first - 1] != S.keys[first];
+    Sum<V> sum;
+    sum.clear();
+    for (uint32_t k0 = first; k0 < last; k0 += 32) {
+        const uint32_t k = k0 + lane;
+        const uint32_t key = k < last ? S.keys[k] : none;
+        const uint32_t position = k < last ? S.positions[k] : 0;
+        // The lane's position ends a run (the end of the keys does too).
+        const uint32_t after = k + 1 < n ? S.keys[min(k + 1, n - 1)] : ~0u;
+        const uint32_t ends = __ballot_sync(kFull, k < last && after != key);
+        const int count = static_cast<int>(min(last - k0, 32u));
+        if (__shfl_sync(kFull, key, 0) == none) return;  // keys from here on have no row
+        for (int j0 = 0; j0 < count; j0 += kReduceRows) {
+            LanePieces<DT, V> x[kReduceRows];
+#pragma unroll
+            for (int u = 0; u < kReduceRows; ++u) {
+                const uint32_t at = __shfl_sync(kFull, position, j0 + u);
+                if (j0 + u < count) x[u] = load_go<DT, V>(P, at, col);
+            }
+#pragma unroll
+            for (int u = 0; u < kReduceRows; ++u) {
+                const uint32_t row = __shfl_sync(kFull, key, j0 + u);
+                if (j0 + u < count && row != none) {
+                    sum.add(x[u]);
+                    const bool end = ends >> (j0 + u) & 1;
+                    if (end) {
+                        if (begun) finish_row<V>(P, row, col, sum);
+                        else sum.put(S.head + static_cast<int64_t>(chunk) * P.dim, col, P.dim);
+                        sum.clear();
+                        begun = true;
+                    } else if (k0 + j0 + u + 1 == last) {  // goes on in the next chunk
+                        sum.put((begun ? S.tail : S.head) + static_cast<int64_t>(chunk) * P.dim, col, P.dim);
+                    }
+                }
+            }
+        }
+    }
+}
+
+// The rows whose runs cross chunks: the chunk in which a run begins adds the pieces of the
+// chunks after it, in order, a block per such chunk and group of slabs.
+template <int V>
+__global__ void __launch_bounds__(kReduceThreads) token_join_kernel(const GradArgs P, const Sorted S, int slabs) {
+    __shared__ __align__(16) float part[kReduceWarps][kSlab<V>];
+    begin_kernel();
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const uint32_t chunk = blockIdx.x, n = P.tokens.n;
+    const uint32_t first = chunk * S.chunk, next = first + S.chunk;  // the last chunk has no block
+    const uint32_t key = S.keys[next - 1];
+    if (key == static_cast<uint32_t>(P.tokens.rows) || S.keys[next] != key) return;
+    if (first > 0 && S.keys[first - 1] == key) return;  // begun earlier
+    uint32_t lo = next, hi = n;  // the run's end
+    while (lo < hi) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (S.keys[mid] <= key) lo = mid + 1;
+        else hi = mid;
+    }
+    const uint32_t end_chunk = (lo - 1) / S.chunk;
+    const uint32_t pieces = end_chunk - chunk;  // after the tail
+    const bool split = pieces > 4;
+    const uint32_t a = split ? static_cast<uint64_t>(pieces) * wid / kReduceWarps : 0;
+    const uint32_t b = split ? static_cast<uint64_t>(pieces) * (wid + 1) / kReduceWarps : pieces;
+    for (int slab = split ? 0 : wid; slab < slabs; slab += split ? 1 : kReduceWarps) {
+        const int base = slab * kSlab<V>, col = base + lane * V;
+        Sum<V> sum;
+        sum.clear();
+        if (!split || wid == 0) sum.add(S.tail + static_cast<int64_t>(chunk) * P.dim, col, P.dim);
+#pragma unroll 4
+        for (uint32_t k = a; k < b; ++k) sum.add(S.head + static_cast<int64_t>(chunk + 1 + k) * P.dim, col, P.dim);
+        if (split) {
+            sum.put(part[wid], lane * V, P.dim - base);
+            __syncthreads();
+            if (wid == 0) {
+                sum.clear();
+                for (int w = 0; w < kReduceWarps; ++w) sum.add(part[w], lane * V, P.dim - base);
+                finish_row<V>(P, key, col, sum);
+            }
+            __syncthreads();
+        } else {
+            finish_row<V>(P, key, col, sum);
+        }
+    }
+}
+
+constexpr uint32_t kGradChunk = 32;
+
+int key_bits(int64_t rows) {  // keys are 0 .. rows
+    int bits = 1;
+    while (bits < 32 && (rows >> bits) != 0) ++bits;
+    return bits;
+}
+
+struct GradWorkspace {
+    size_t keys[2], positions[2], tiles, digits, table, scalars, head, tail, bytes;
+    int64_t num_tiles;
+    int passes;
+};
+GradWorkspace grad_layout(int64_t n, int64_t rows, int32_t dim) {
+    GradWorkspace w{};
+    if (n <= kMatchTokens) return w;
+    size_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const size_t here = at;
+        at += static_cast<size_t>((bytes + 255) / 256 * 256);
+        return here;
+    };
+    w.num_tiles = (n + kSortTileKeys - 1) / kSortTileKeys;
+    w.passes = (key_bits(rows) + 7) / 8;
+    for (int i = 0; i < 2; ++i) {
+        w.keys[i] = take(n * 4);
+        w.positions[i] = take(n * 4);
+    }
+    w.tiles = take(w.num_tiles * static_cast<int64_t>(sizeof(Chunk)));
+    w.digits = take((w.num_tiles + 1) * w.passes * kRadixDigits * 4);
+    w.table = take(sizeof(TableDev));
+    w.scalars = take(5 * 8);
+    const int64_t chunks = (n + kGradChunk - 1) / kGradChunk;
+    w.head = take(chunks * dim * 4);
+    w.tail = take(chunks * dim * 4);
+    w.bytes = at;
+    return w;
+}
+
+template <int DT, int V>
+void launch_match(const GradArgs& P, cudaStream_t s) {
+    const int groups = (P.dim + kSlab<V> * kMatchSlabs - 1) / (kSlab<V> * kMatchSlabs);
+    const uint32_t token_blocks = P.tokens.n * groups;
+    const int64_t fill = P.accumulate ? 0 : (P.tokens.rows + kFillRows - 1) / kFillRows;
+    if (token_blocks + fill == 0) return;
+    launch(token_match_kernel<DT, V>, dim3(static_cast<unsigned>(token_blocks + fill)), dim3(kMatchThreads), 0, s, P,
+           token_blocks, groups);
+}
+
+template <int DT, int V>
+void launch_sorted(const GradArgs& P, const GradWorkspace& w, char* base, cudaStream_t s) {
+    SortBuffers B{};
+    for (int i = 0; i < 2; ++i) {
+        B.keys[i] = reinterpret_cast<uint32_t*>(base + w.keys[i]);
+        B.positions[i] = reinterpret_cast<uint32_t*>(base + w.positions[i]);
+    }
+    B.tiles = reinterpret_cast<Chunk*>(base + w.tiles);
+    B.digits = reinterpret_cast<uint32_t*>(base + w.digits);
+    B.table = reinterpret_cast<TableDev*>(base + w.table);
+    int64_t* scalars = reinterpret_cast<int64_t*>(base + w.scalars);
+    B.first_tile = scalars;
+    B.table_pos = scalars + 2;
+    B.num_tiles = scalars + 4;
+    const bool few = w.num_tiles <= kFewSortTiles;
+    launch(token_keys_kernel, dim3(static_cast<unsigned>(w.num_tiles)), dim3(kKeyThreads), 0, s, P, B, w.passes);
+    const int64_t words = w.num_tiles * kRadixDigits;
+    // With many tiles every pass counts its own digits, per tile (one array) and in total.
+    uint32_t* totals = B.digits + words;
+    if (!few) cudaMemsetAsync(totals, 0, static_cast<size_t>(w.passes) * kRadixDigits * 4, s);
+    for (int p = 0; p < w.passes; ++p) {
+        SortPass S{};
+        S.keys_in = B.keys[p & 1];
+        S.vals_in = B.positions[p & 1];
+        S.keys_out = B.keys[(p + 1) & 1];
+        S.vals_out = B.positions[(p + 1) & 1];
+        S.tiles = B.tiles;
+        S.num_tiles = B.num_tiles;
+        S.table_first_tile = B.first_tile;
+        S.tables = B.table;
+        S.n = P.tokens.n;
+        S.shift = 8 * p;
+        S.table_pos = B.table_pos;
+        S.tile_digits = few ? B.digits + p * words : B.digits;
+        S.next_digits = few && p + 1 < w.passes ? S.tile_digits + words : nullptr;
+        S.table_digits = few ? nullptr : totals + p * kRadixDigits;
+        S.T = 1;
+        launch_radix_pass(S, w.num_tiles, s);
+    }
+    Sorted R{};
+    R.keys = B.keys[w.passes & 1];
+    R.positions = B.positions[w.passes & 1];
+    R.chunk = kGradChunk;
+    R.chunks = (P.tokens.n + kGradChunk - 1) / kGradChunk;
+    R.head = reinterpret_cast<float*>(base + w.head);
+    R.tail = reinterpret_cast<float*>(base + w.tail);
+    const int slabs = (P.dim + kSlab<V> - 1) / kSlab<V>;
+    const uint32_t reduce_blocks =
+        static_cast<uint32_t>((static_cast<uint64_t>(R.chunks) * slabs + kReduceWarps - 1) / kReduceWarps);
+    const int64_t rows_per_block = kReduceWarps * kFillWarpRows;
+    const int64_t fill = P.accumulate ? 0 : (P.tokens.rows + rows_per_block - 1) / rows_per_block;
+    launch(token_reduce_kernel<DT, V>, dim3(static_cast<unsigned>(reduce_blocks + fill)), dim3(kReduceThreads), 0, s, P, R,
+           slabs, reduce_blocks);
+    if (R.chunks > 1) launch(token_join_kernel<V>, dim3(R.chunks - 1), dim3(kReduceThreads), 0, s, P, R, slabs);
+}
+
+template <int DT, int V>
+void launch_grad(const GradArgs& P, const GradWorkspace& w, char* base, cudaStream_t s) {
+    if (P.tokens.n <= kMatchTokens) launch_match<DT, V>(P, s);
+    else launch_sorted<DT, V>(P, w, base, s);
+}
+template <int DT>
+void launch_grad(const GradArgs& P, const GradWorkspace& w, char* base, int v, cudaStream_t s) {
+    if (v == 8) launch_grad<DT, 8>(P, w, base, s);
+    else if (v == 4) launch_grad<DT, 4>(P, w, base, s);
+    else launch_grad<DT, 1>(P, w, base, s);
+}
+
+// ---------------------------------------------------------------- arguments
+
+bool valid_dtype(int d) { return d == CB_F32 || d == CB_F16 || d == CB_BF16; }
+
+// A row-major operand whose rows are taken in pieces of v values: v divides its dim and
+// strides, and a piece is aligned to its size (at most 16 bytes).
+bool takes(const void* p, int dtype, int32_t dim, int64_t s0, int64_t s1, int v) {
+    const int64_t bytes = min64(16, static_cast<int64_t>(v) * dtype_bytes(dtype));
+    return dim % v == 0 && s0 % v == 0 && s1 % v == 0 && reinterpret_cast<uintptr_t>(p) % bytes == 0;
+}
+
+// Sequences x length tokens, and the values of a row at each: strides that do not overlap.
+bool valid_tokens(const void* tokens, int idx_dtype, int32_t sequences, int32_t length) {
+    return (idx_dtype == CB_I32 || idx_dtype == CB_I64) && sequences >= 0 && length >= 0 &&
+           static_cast<int64_t>(sequences) * length < (int64_t(1) << 30) &&
+           (static_cast<int64_t>(sequences) * length == 0 ||
+            (tokens && reinterpret_cast<uintptr_t>(tokens) % (idx_dtype == CB_I32 ? 4 : 8) == 0));
+}
+bool aligned_to(const void* p, int dtype) { return reinterpret_cast<uintptr_t>(p) % dtype_bytes(dtype) == 0; }
+
+}  // namespace
+}  // namespace cbtbe
+
+extern "C" cb_status cb_token_forward(const void* table, cb_dtype table_dtype, int64_t rows, int32_t dim,
+                                      int64_t row_stride, const void* tokens, cb_index_dtype idx_dtype, int32_t sequences,
+                                      int32_t length, int64_t token_sequence_stride, int64_t token_stride, float scale,
+                                      void* out, cb_dtype out_dtype, int64_t out_sequence_stride, int64_t out_stride,
+                                      int* error, cudaStream_t stream) {
+    using namespace cbtbe;
+    if (!valid_tokens(tokens, idx_dtype, sequences, length) || !valid_dtype(table_dtype) || !valid_dtype(out_dtype) ||
+        rows < 0 || rows >= (int64_t(1) << 31) || dim < 0 || dim > (1 << 20) || !(scale == scale) ||
+        reinterpret_cast<uintptr_t>(error) % 4)
+        return CB_ERR_INVALID_ARG;
+    const int64_t n = static_cast<int64_t>(sequences) * length;
+    if (n == 0 || dim == 0) return CB_OK;
+    if (!out || (rows > 0 && !table) || (rows > 1 && row_stride < dim) || !aligned_to(table, table_dtype) ||
+        !aligned_to(out, out_dtype) || (length > 1 && out_stride < dim) ||
+        (sequences > 1 && out_sequence_stride < dim))
+        return CB_ERR_INVALID_ARG;
+    LookupArgs P{};
+    P.tokens = {tokens, positions(sequences, length, token_sequence_stride, token_stride), static_cast<uint32_t>(n),
+                idx_dtype == CB_I32, rows};
+    P.table = table;
+    P.row_stride = row_stride;
+    P.out_at = positions(sequences, length, out_sequence_stride, out_stride);
+    P.out = out;
+    P.scale = scale;
+    P.error = error;
+    // Pieces of 8 values where one side is in 16 bits (16 bytes there), of 4 otherwise or where
+    // only 4 fit the strides and addresses, else single values.
+    const int64_t s1 = length > 1 ? out_stride : 0, s0 = sequences > 1 ? out_sequence_stride : 0;
+    const int64_t table_stride = rows > 1 ? row_stride : 0;
+    int v = table_dtype == CB_F32 && out_dtype == CB_F32 ? 4 : 8;
+    while (v > 1 && !(takes(table, table_dtype, dim, table_stride, 0, v) && takes(out, out_dtype, dim, s0, s1, v)))
+        v = v == 8 ? 4 : 1;
+    if (table_dtype == CB_F32) launch_lookup<CB_F32>(P, dim, v, out_dtype, stream);
+    else if (table_dtype == CB_F16) launch_lookup<CB_F16>(P, dim, v, out_dtype, stream);
+    else launch_lookup<CB_BF16>(P, dim, v, out_dtype, stream);
+    return cudaGetLastError() == cudaSuccess ? CB_OK : CB_ERR_CUDA;
+}
+
+extern "C" int64_t cb_token_backward_workspace_bytes(int64_t num_tokens, int64_t rows, int32_t dim) {
+    if (num_tokens <= 0 || rows < 0 || dim <= 0) return 0;
+    return static_cast<int64_t>(cbtbe::grad_layout(num_tokens, rows, dim).bytes);
+}
+
+extern "C" cb_status cb_token_backward(const void* grad_out, cb_dtype go_dtype, int64_t go_sequence_stride,
+                                       int64_t go_stride, const void* tokens, cb_index_dtype idx_dtype, int32_t sequences,
+                                       int32_t length, int64_t token_sequence_stride, int64_t token_stride, int64_t rows,
+                                       int32_t dim, float scale, int64_t padding_idx, int accumulate, void* grad,
+                                       cb_dtype grad_dtype, int64_t grad_stride, void* workspace, int64_t workspace_bytes,
+                                       int* error, cudaStream_t stream) {
+    using namespace cbtbe;
+    if (!valid_tokens(tokens, idx_dtype, sequences, length) || !valid_dtype(go_dtype) || !valid_dtype(grad_dtype) ||
+        rows < 0 || rows >= (int64_t(1) << 31) || dim < 0 || dim > (1 << 20) || !(scale == scale) ||
+        reinterpret_cast<uintptr_t>(error) % 4)
+        return CB_ERR_INVALID_ARG;
+    const int64_t n = static_cast<int64_t>(sequences) * length;
+    if (dim == 0 || (n == 0 && (accumulate || rows == 0))) return CB_OK;
+    if ((rows > 0 && !grad) || (n > 0 && !grad_out) || (rows > 1 && grad_stride < dim) ||
+        !aligned_to(grad_out, go_dtype) || !aligned_to(grad, grad_dtype) ||
+        (length > 1 && go_stride < 0) || (sequences > 1 && go_sequence_stride < 0))
+        return CB_ERR_INVALID_ARG;
+    const GradWorkspace w = grad_layout(n, rows, dim);
+    if (w.bytes > 0 && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 ||
+                        workspace_bytes < static_cast<int64_t>(w.bytes)))
+        return CB_ERR_CAPACITY;
+    GradArgs P{};
+    P.tokens = {tokens, positions(sequences, length, token_sequence_stride, token_stride), static_cast<uint32_t>(n),
+                idx_dtype == CB_I32, rows};
+    P.padding = padding_idx;
+    P.grad_out = grad_out;
+    P.go_at = positions(sequences, length, go_sequence_stride, go_stride);
+    P.dim = dim;
+    P.scale = scale;
+    P.grad = grad;
+    P.grad_stride = grad_stride;
+    P.grad_dtype = grad_dtype;
+    P.accumulate = accumulate;
+    P.error = error;
+    const int64_t s1 = length > 1 ? go_stride : 0, s0 = sequences > 1 ? go_sequence_stride : 0;
+    const int64_t row_stride = rows > 1 ? grad_stride : 0;
+    int v = go_dtype == CB_F32 && grad_dtype == CB_F32 ? 4 : 8;
+    while (v > 1 && !(takes(grad_out, go_dtype, dim, s0, s1, v) && takes(grad, grad_dtype, dim, row_stride, 0, v)))
+        v = v == 8 ? 4 : 1;
+    char* base = static_cast<char*>(workspace);
+    if (go_dtype == CB_F32) launch_grad<CB_F32>(P, w, base, v, stream);
+    else if (go_dtype == CB_F16) launch_grad<CB_F16>(P, w, base, v, stream);
+    else launch_grad<CB_BF16>(P, w, base, v, stream);
+    return cudaGetLastError() == cudaSuccess ? CB_OK : CB_ERR_CUDA;
+}

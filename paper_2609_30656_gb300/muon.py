@@ -1,0 +1,188 @@
+"""Orthogonalised matrix updates: Newton-Schulz products, and the optimizer step around them.
+
+The Python binding of ``cb_muon_orthogonalise`` / ``cb_muon_step`` (include/cb_tbe.h):
+
+    o = newton_schulz(g)                                  # about U V^T of g = U S V^T
+    muon_step(weight, grad, momentum, lr=3e-4, weight_decay=0.1)
+
+Matrices are 2-D, or 3-D for a stack of equal shapes. All work is enqueued on the current
+stream of the tensors' device; nothing waits. The workspace (about 8 bytes per value of the
+update and 4 per value of its square Gram matrix) comes from torch's allocator.
+"""
+
+from __future__ import annotations
+
+import ctypes
+import math
+
+import torch
+
+from . import tbe
+
+# The entry points of include/cb_tbe.h that this module binds.
+EXPORTS = ("cb_muon_orthogonalise", "cb_muon_step", "cb_muon_workspace_bytes")
+
+COEFFICIENTS = (3.4445, -4.7750, 2.0315)  # every singular value in (0, 1] into about [0.7, 1.2] in five steps
+
+_bound = None
+_coefficient_arrays: dict = {}
+
+
+def _library() -> ctypes.CDLL:
+    global _bound
+    if _bound is None:
+        lib = tbe.load_library()
+        p, i32, i64, f32, c = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_int
+        lib.cb_muon_orthogonalise.argtypes = [p, c, i32, i32, i32, i64, i64, f32, p, i32, p, c, i64, i64, p, i64, p, p]
+        lib.cb_muon_step.argtypes = [p, c, i64, i64, p, c, i64, i64, p, i64, i64, i32, i32, i32, f32, f32, f32, c,
+                                     f32, p, i32, f32, p, i64, p, p]
+        lib.cb_muon_workspace_bytes.argtypes = [i32, i32, i32]
+        lib.cb_muon_orthogonalise.restype = lib.cb_muon_step.restype = c
+        lib.cb_muon_workspace_bytes.restype = i64
+        _bound = lib
+    return _bound
+
+
+def _coefficients(coefficients, steps: int):
+    """A C array of 3 * steps values: one triple for all steps, or one for each."""
+    if steps < 1:
+        raise ValueError("at least one step is needed")
+    rows = tuple(coefficients)
+    if len(rows) == 3 and not any(hasattr(x, "__len__") for x in rows):
+        rows = (rows,) * steps
+    if len(rows) != steps or any(not hasattr(r, "__len__") or len(r) != 3 for r in rows):
+        raise ValueError("coefficients must be one triple, or one triple for each step")
+    key = rows = tuple(tuple(float(x) for x in r) for r in rows)
+    if key not in _coefficient_arrays:
+        if len(_coefficient_arrays) >= 64:
+            _coefficient_arrays.clear()
+        _coefficient_arrays[key] = (ctypes.c_float * (3 * steps))(*[x for r in rows for x in r])
+    return _coefficient_arrays[key]
+
+
+def _check_matrix(t: torch.Tensor, what: str):
+    if t.device.type != "cuda" or t.dim() not in (2, 3):
+        raise ValueError(f"{what} must be a 2-D or 3-D CUDA tensor")
+    if t.dtype not in tbe._DTYPES:
+        raise ValueError(f"unsupported {what} dtype {t.dtype}")
+
+
+def _check_error(error: torch.Tensor | None, device: torch.device):
+    if error is not None and (error.device != device or error.dtype != torch.int32 or error.numel() != 1):
+        raise ValueError("error must be an int32 tensor of one value on the device")
+
+
+def _shape(t: torch.Tensor):
+    return (1, *t.shape) if t.dim() == 2 else tuple(t.shape)
+
+
+def _strides(t: torch.Tensor):
+    """(batch stride, row stride) in values; a dimension of one has the stride of a whole one."""
+    batch, rows, cols = _shape(t)
+    row = t.stride(-2) if rows > 1 else cols
+    return (t.stride(0) if t.dim() == 3 and batch > 1 else rows * row), row
+
+
+def _in_rows(t: torch.Tensor) -> bool:
+    batch, rows, cols = _shape(t)
+    return (cols <= 1 or t.stride(-1) == 1) and (rows <= 1 or t.stride(-2) >= cols)
+
+
+def _writable(t: torch.Tensor) -> bool:
+    batch, rows, cols = _shape(t)
+    return _in_rows(t) and (batch <= 1 or _strides(t)[0] >= rows * cols)
+
+
+def _workspace(lib, batch: int, rows: int, cols: int, device: torch.device):
+    nbytes = lib.cb_muon_workspace_bytes(batch, rows, cols)
+    return torch.empty(nbytes, dtype=torch.uint8, device=device), nbytes
+
+
+def newton_schulz(g: torch.Tensor, out: torch.Tensor | None = None, out_dtype: torch.dtype = torch.bfloat16,
+                  steps: int = 5, coefficients=COEFFICIENTS, eps: float = 1e-7,
+                  error: torch.Tensor | None = None) -> torch.Tensor:
+    """The approximate orthogonal factor of g, or of each matrix of a stack
+    (cb_muon_orthogonalise).
+
+    X = g / (||g||_F + eps), then `steps` times X <- a X + (b A + c A A) X with A = X X^T.
+    The products are in fp16 with fp32 sums, about 1e-3 off the exact result in the 2-norm,
+    which is why the default output type is bf16. out may be g. A g whose columns are
+    contiguous (a transposed view) is taken as it lies."""
+    lib = _library()
+    _check_matrix(g, "g")
+    _check_error(error, g.device)
+    if out is None:
+        if not _in_rows(g) and _in_rows(g.mT):
+            out = torch.empty(g.mT.shape, dtype=out_dtype, device=g.device).mT
+        else:
+            out = torch.empty(g.shape, dtype=out_dtype, device=g.device)
+    else:
+        _check_matrix(out, "out")
+        if out.device != g.device or out.shape != g.shape or not (_writable(out) or _writable(out.mT)):
+            raise ValueError("out must have g's shape and device, its rows or columns contiguous, its matrices apart")
+    if not _writable(out):  # the transpose's factor is the factor's transpose
+        newton_schulz(g.mT, out.mT, out.dtype, steps, coefficients, eps, error)
+        return out
+    if not _in_rows(g):
+        g = g.contiguous()
+    batch, rows, cols = _shape(g)
+    table = _coefficients(coefficients, steps)
+    if g.numel() == 0:
+        return out
+    work, nbytes = _workspace(lib, batch, rows, cols, g.device)
+    index = g.get_device()
+    with tbe._OnDevice(index):
+        tbe._check(lib.cb_muon_orthogonalise(g.data_ptr(), tbe._DTYPES[g.dtype], batch, rows, cols, *_strides(g), eps,
+                                             table, steps, out.data_ptr(), tbe._DTYPES[out.dtype], *_strides(out),
+                                             work.data_ptr(), nbytes, tbe._ptr(error), tbe._raw_stream(index)),
+                   "cb_muon_orthogonalise")
+    return out
+
+
+def update_scale(rows: int, cols: int, adjust: str | None) -> float:
+    """What an orthogonalised update of shape [rows, cols] is multiplied with besides lr:
+    "rms": 0.2 sqrt(max(rows, cols)), values of the size of an Adam step's; "spectral":
+    sqrt(max(1, rows / cols)), the same change of the layer's outputs for every shape; None: 1."""
+    if adjust == "rms":
+        return 0.2 * math.sqrt(max(rows, cols))
+    if adjust == "spectral":
+        return math.sqrt(max(1.0, rows / cols))
+    if adjust is None:
+        return 1.0
+    raise ValueError(f"unknown adjustment {adjust!r}")
+
+
+def muon_step(weight: torch.Tensor, grad: torch.Tensor, momentum: torch.Tensor, lr: float, beta: float = 0.95,
+              nesterov: bool = True, weight_decay: float = 0.0, adjust: str | None = "rms", steps: int = 5,
+              coefficients=COEFFICIENTS, eps: float = 1e-7, error: torch.Tensor | None = None) -> None:
+    """One optimizer step of a weight matrix, or of a stack of them, in place (cb_muon_step):
+
+        momentum <- beta momentum + grad;  u = grad + beta momentum (nesterov) or momentum
+        weight <- (1 - lr weight_decay) weight - lr update_scale(adjust) newton_schulz(u)
+
+    weight and grad: fp32 / fp16 / bf16; momentum: fp32 (a running sum keeps its 32 bits).
+    The three have one shape; weight and momentum have contiguous rows."""
+    lib = _library()
+    for t, what in ((weight, "weight"), (grad, "grad"), (momentum, "momentum")):
+        _check_matrix(t, what)
+        if t.device != weight.device or t.shape != weight.shape:
+            raise ValueError("weight, grad and momentum must have one shape and device")
+    _check_error(error, weight.device)
+    if momentum.dtype != torch.float32:
+        raise ValueError("momentum must be fp32")
+    if not _writable(weight) or not _writable(momentum):
+        raise ValueError("weight and momentum must have contiguous rows and matrices that do not overlap")
+    if not _in_rows(grad):
+        grad = grad.contiguous()
+    batch, rows, cols = _shape(weight)
+    table = _coefficients(coefficients, steps)
+    scale = update_scale(rows, cols, adjust) if cols else 1.0
+    if weight.numel() == 0:
+        return
+    work, nbytes = _workspace(lib, batch, rows, cols, weight.device)
+    index = weight.get_device()
+    with tbe._OnDevice(index):
+        tbe._check(lib.cb_muon_step(weight.data_ptr(), tbe._DTYPES[weight.dtype], *_strides(weight), grad.data_ptr(),
+                                    tbe._DTYPES[grad.dtype], *_strides(grad), momentum.data_ptr(), *_strides(momentum),
+                                    batch, rows, cols, lr, weight_decay, beta, int(nesterov), eps, table, steps, scale,
+                                    work.data_ptr(), nbytes, tbe._ptr(error), tbe._raw_stream(index)), "cb_muon_step")
