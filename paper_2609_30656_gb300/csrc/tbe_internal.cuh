@@ -148,6 +148,13 @@ __device__ __forceinline__ void begin_kernel() {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
+// A kernel of a chain whose next kernels need nothing of it may let them launch before
+// its own wait; a kernel further on that does not wait at its beginning then runs beside
+// this one (and waits at its end, so that those after it are behind all of them).
+__device__ __forceinline__ void begin_kernel_released() {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
 template <class... Params, class... Args>
 inline void launch(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, const Args&... args) {
     cudaLaunchConfig_t cfg{};

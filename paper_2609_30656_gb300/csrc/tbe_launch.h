@@ -28,6 +28,7 @@ struct SortPass {
     uint32_t* next_digits;       // few tiles: the next pass's counts, zeroed (null: last pass)
     uint32_t* table_digits;      // many tiles: [T][256] digit counts per table, zeroed
     int T;
+    int release;                 // the scatter lets the kernels after it launch at its start
     // single sweep with look-back
     const uint32_t* digit_base;  // [T][stride]: this pass's 256 first output slots per table
     int base_stride;             // passes * 256

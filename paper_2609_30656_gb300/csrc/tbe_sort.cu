@@ -432,7 +432,8 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 1024 / NT) radix_scatter_k
     __shared__ int32_t sh_goff[kRadix];                    // global destination - local index
     __shared__ int64_t sh_scan[33];
 
-    begin_kernel();
+    if (S.release) begin_kernel_released();
+    else begin_kernel();
     const int64_t tile = blockIdx.x;
     if (tile >= *S.num_tiles) return;  // the grid is an upper bound on the tiles
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;

@@ -14,7 +14,13 @@ namespace {
 
 // ---------------------------------------------------------------- lookup
 
-constexpr int kLookupThreads = 256;
+// 128 threads of 4 pieces and 16 blocks per SM (32 registers a thread, every warp that an SM
+// holds): a block is a chain of a token's load, a row's load and a store, so bytes in flight
+// decide. 262144 rows of 8 KB: 450 us, 5.7 TB/s; 504 with 6 blocks of 256 threads, 462 with
+// 8, 530 with 2 or 8 pieces a thread, 526 with 32 blocks of 64, 655 with resident blocks
+// that load the next tokens ahead (more registers, fewer warps).
+constexpr int kLookupThreads = 128;
+constexpr int kLookupBlocks = 16;
 constexpr int kLookupPieces = 4;  // pieces in flight per thread
 
 struct LookupArgs {
@@ -32,7 +38,7 @@ struct LookupArgs {
 // output, a thread every kLookupThreads-th: rows of any length fill the threads, stores
 // are consecutive, and each thread has its loads in flight together.
 template <int IN, int OUT, int V>
-__global__ void __launch_bounds__(kLookupThreads) token_lookup_kernel(const LookupArgs P) {
+__global__ void __launch_bounds__(kLookupThreads, kLookupBlocks) token_lookup_kernel(const LookupArgs P) {
     begin_kernel();
     const uint64_t first = static_cast<uint64_t>(blockIdx.x) * (kLookupThreads * kLookupPieces);
     const uint32_t row0 = static_cast<uint32_t>(first / P.pieces);
@@ -145,6 +151,12 @@ struct Sum {
             for (int i = 0; i < V; ++i) f[j][i] += y[i];
         }
     }
+    __device__ __forceinline__ void add(const Sum& o) {
+#pragma unroll
+        for (int j = 0; j < kLanePieces<V>; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) f[j][i] += o.f[j][i];
+    }
     // The lane's sums at columns col, .. of an fp32 row of `dim` values (16-byte aligned).
     __device__ __forceinline__ void put(float* row, int col, int dim) const {
 #pragma unroll
@@ -234,6 +246,7 @@ constexpr int kMatchWarps = kMatchThreads / 32;
 constexpr uint32_t kMatchTokens = 2048;  // most tokens of a call without a sort
 constexpr int kMatchSlabs = 8;           // slabs of a row per block
 constexpr int kFillRows = 64;            // rows of the gradient per zeroing block
+constexpr int kFillWarpRows = 8;         // rows per zeroing warp at a time
 
 // One block per (token, group of slabs): the first position of its token sums all of the
 // token's positions, in order; other blocks end at once. The blocks after those write zeros
@@ -332,37 +345,54 @@ __global__ void __launch_bounds__(kMatchThreads) token_match_kernel(const GradAr
 
 // ---------------------------------------------------------------- many tokens: sorted
 
-constexpr int kKeyThreads = 256;
 constexpr int kRadixDigits = 256;
+constexpr int kKeyThreads = 1024;
+constexpr int kKeysPerThread = static_cast<int>(kSortTileKeys) / kKeyThreads;
+static_assert(kKeysPerThread * kKeyThreads == kSortTileKeys && kKeyThreads >= kRadixDigits, "tiles of the sort");
 
 // Pairs (key, position), a tile of the sort per block, with the first pass's digit counts of
 // the tile; the later passes' counts are cleared, and the sort's description of its one
-// "table" (keys from 0) and tiles written.
+// "table" (keys from 0) and tiles written. `touched` (cleared before, or null) gets a 1 for
+// every row with a token.
 struct SortBuffers {
     uint32_t *keys[2], *positions[2];
     Chunk* tiles;
     uint32_t* digits;  // [passes][tiles][256]
     TableDev* table;
     int64_t *first_tile, *num_tiles, *table_pos;  // [2], [1], [2]
+    uint8_t* touched;  // [rows], padded to 8
 };
 __global__ void __launch_bounds__(kKeyThreads) token_keys_kernel(const GradArgs P, const SortBuffers S, int passes) {
     __shared__ uint32_t sh[kRadixDigits];
+    if (threadIdx.x < kRadixDigits) sh[threadIdx.x] = 0;
     begin_kernel();
     const uint32_t n = P.tokens.n, tile = blockIdx.x, tiles = gridDim.x;
     const uint32_t first = tile * static_cast<uint32_t>(kSortTileKeys);
     const uint32_t count = min(static_cast<uint32_t>(kSortTileKeys), n - first);
-    sh[threadIdx.x] = 0;
-    __syncthreads();
-    for (uint32_t k = threadIdx.x; k < count; k += kKeyThreads) {
-        const uint32_t key = token_key(P, P.tokens.load(first + k), true);
-        S.keys[0][first + k] = key;
-        S.positions[0][first + k] = first + k;
-        atomicAdd(&sh[key & (kRadixDigits - 1)], 1u);
+    int64_t token[kKeysPerThread];
+#pragma unroll
+    for (int u = 0; u < kKeysPerThread; ++u) {
+        const uint32_t k = threadIdx.x + u * kKeyThreads;
+        token[u] = k < count ? P.tokens.load(first + k) : 0;
     }
     __syncthreads();
-    S.digits[tile * kRadixDigits + threadIdx.x] = sh[threadIdx.x];
-    for (int p = 1; p < passes; ++p)
-        S.digits[(static_cast<int64_t>(p) * tiles + tile) * kRadixDigits + threadIdx.x] = 0;
+#pragma unroll
+    for (int u = 0; u < kKeysPerThread; ++u) {
+        const uint32_t k = threadIdx.x + u * kKeyThreads;
+        if (k < count) {
+            const uint32_t key = token_key(P, token[u], true);
+            S.keys[0][first + k] = key;
+            S.positions[0][first + k] = first + k;
+            atomicAdd(&sh[key & (kRadixDigits - 1)], 1u);
+            if (S.touched && key < P.tokens.rows) S.touched[key] = 1;  // by any number of threads: one value
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x < kRadixDigits) {
+        S.digits[tile * kRadixDigits + threadIdx.x] = sh[threadIdx.x];
+        for (int p = 1; p < passes; ++p)
+            S.digits[(static_cast<int64_t>(p) * tiles + tile) * kRadixDigits + threadIdx.x] = 0;
+    }
     if (threadIdx.x == 0) {
         Chunk c{};
         c.k0 = first;
@@ -379,6 +409,36 @@ __global__ void __launch_bounds__(kKeyThreads) token_keys_kernel(const GradArgs 
     }
 }
 
+__global__ void __launch_bounds__(256) token_clear_kernel(uint2* words, int64_t n) {
+    begin_kernel();
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += gridDim.x * 256ll)
+        words[i] = make_uint2(0, 0);
+}
+
+// Zeros to every row without a token. Writes alone, while the sort between the keys and the
+// sums is a chain of short kernels of few blocks: this kernel needs the flags of
+// token_keys_kernel only, is launched after the sort's last pass without waiting for it, and
+// waits at its end for those after it. Blocks stay for the whole kernel (a block that waited
+// at its end would keep a later one from starting).
+template <class T>
+__global__ void __launch_bounds__(256) token_fill_kernel(char* grad, int64_t row_bytes, int64_t used_bytes, int64_t rows,
+                                                         const uint8_t* __restrict__ touched) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int lane = threadIdx.x & 31;
+    const int64_t step = gridDim.x * 8ll * kFillWarpRows;
+    for (int64_t r0 = (blockIdx.x * 8ll + threadIdx.x / 32) * kFillWarpRows; r0 < rows; r0 += step) {
+        const uint2 flags = __ldcg(reinterpret_cast<const uint2*>(touched + r0));  // kFillWarpRows of them
+        for (int k = 0; k < kFillWarpRows && r0 + k < rows; ++k) {
+            if ((k < 4 ? flags.x >> 8 * k : flags.y >> 8 * (k - 4)) & 0xff) continue;
+            T* p = reinterpret_cast<T*>(grad + (r0 + k) * row_bytes);
+            const int count = static_cast<int>(used_bytes / sizeof(T));
+#pragma unroll 4
+            for (int i = lane; i < count; i += 32) p[i] = T{};
+        }
+    }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 struct Sorted {
     const uint32_t *keys, *positions;
     uint32_t chunk, chunks;  // positions per chunk
@@ -388,38 +448,15 @@ struct Sorted {
 constexpr int kReduceThreads = 256;
 constexpr int kReduceWarps = kReduceThreads / 32;
 constexpr int kReduceRows = 8;       // rows in flight per warp
-constexpr int kFillWarpRows = 8;     // rows of the gradient per zeroing warp
 
 // A warp takes a chunk of the sorted positions and a slab of columns: it adds the rows of a
 // run of equal keys and finishes the table row at the run's end. Runs cut by the chunk's ends
-// leave their sums for token_join_kernel. Warps past those write zeros to rows without a token,
-// found by bisection of the keys.
+// leave their sums for token_join_kernel.
 template <int DT, int V>
-__global__ void __launch_bounds__(kReduceThreads) token_reduce_kernel(const GradArgs P, const Sorted S, int slabs,
-                                                                      uint32_t reduce_blocks) {
+__global__ void __launch_bounds__(kReduceThreads) token_reduce_kernel(const GradArgs P, const Sorted S, int slabs) {
     begin_kernel();
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     const uint32_t n = P.tokens.n, none = static_cast<uint32_t>(P.tokens.rows);
-    if (blockIdx.x >= reduce_blocks) {
-        const int64_t r0 = (static_cast<int64_t>(blockIdx.x - reduce_blocks) * kReduceWarps + wid) * kFillWarpRows;
-        bool absent = false;
-        if (lane < kFillWarpRows && r0 + lane < P.tokens.rows) {
-            const uint32_t key = static_cast<uint32_t>(r0 + lane);
-            uint32_t lo = 0, hi = n;
-            while (lo < hi) {
-                const uint32_t mid = (lo + hi) / 2;
-                if (S.keys[mid] < key) lo = mid + 1;
-                else hi = mid;
-            }
-            absent = lo == n || S.keys[lo] != key;
-        }
-        uint32_t mask = __ballot_sync(kFull, absent);
-        while (mask) {
-            zero_row<V>(P, r0 + __ffs(mask) - 1, lane);
-            mask &= mask - 1;
-        }
-        return;
-    }
     const uint64_t w = static_cast<uint64_t>(blockIdx.x) * kReduceWarps + wid;
     const uint32_t chunk = static_cast<uint32_t>(w / slabs);
     if (chunk >= S.chunks) return;
@@ -444,6 +481,15 @@ __global__ void __launch_bounds__(kReduceThreads) token_reduce_kernel(const Grad
                 const uint32_t at = __shfl_sync(kFull, position, j0 + u);
                 if (j0 + u < count) x[u] = load_go<DT, V>(P, at, col);
             }
+            if (P.accumulate) {  // the rows that the runs ending here are added to, on their way too
+                const uint32_t here = ends >> j0 & ((1u << kReduceRows) - 1u);
+#pragma unroll
+                for (int u = 0; u < kReduceRows; ++u) {
+                    const uint32_t row = __shfl_sync(kFull, key, j0 + u);
+                    if (here >> u & 1 && row != none)
+                        prefetch_l1(static_cast<const char*>(P.grad) + (row * P.grad_stride + col) * dtype_bytes(P.grad_dtype));
+                }
+            }
 #pragma unroll
             for (int u = 0; u < kReduceRows; ++u) {
                 const uint32_t row = __shfl_sync(kFull, key, j0 + u);
@@ -464,52 +510,94 @@ __global__ void __launch_bounds__(kReduceThreads) token_reduce_kernel(const Grad
     }
 }
 
-// The rows whose runs cross chunks: the chunk in which a run begins adds the pieces of the
-// chunks after it, in order, a block per such chunk and group of slabs.
+// The rows whose runs cross chunks: the sum left at the end of the chunk in which a run
+// begins, and those of the chunks after it, in order. A block takes kJoinChunks chunks and a slab: a
+// lane finds out whether a run crosses its chunk's end and how far it goes; then each warp
+// joins short runs, and all warps a long one, a part of its chunks each.
+constexpr uint32_t kJoinChunks = 32;  // a lane each
+constexpr uint32_t kJoinShort = 8;  // most chunks after the first of a run joined by one warp
+constexpr int kJoinLoads = 4;
+
 template <int V>
 __global__ void __launch_bounds__(kReduceThreads) token_join_kernel(const GradArgs P, const Sorted S, int slabs) {
     __shared__ __align__(16) float part[kReduceWarps][kSlab<V>];
     begin_kernel();
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    const uint32_t chunk = blockIdx.x, n = P.tokens.n;
-    const uint32_t first = chunk * S.chunk, next = first + S.chunk;  // the last chunk has no block
-    const uint32_t key = S.keys[next - 1];
-    if (key == static_cast<uint32_t>(P.tokens.rows) || S.keys[next] != key) return;
-    if (first > 0 && S.keys[first - 1] == key) return;  // begun earlier
-    uint32_t lo = next, hi = n;  // the run's end
-    while (lo < hi) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (S.keys[mid] <= key) lo = mid + 1;
-        else hi = mid;
+    const uint32_t n = P.tokens.n;
+    const uint32_t chunk0 = blockIdx.x / slabs * kJoinChunks;
+    const int slab = static_cast<int>(blockIdx.x % slabs), base = slab * kSlab<V>, col = base + lane * V;
+    const uint32_t mine = chunk0 + lane;
+    uint32_t key = 0, pieces = 0;  // chunks after `mine` of the run that begins in it and crosses its end
+    if (mine + 1 < S.chunks) {
+        const uint32_t first = mine * S.chunk, next = first + S.chunk;
+        key = S.keys[next - 1];
+        if (key != static_cast<uint32_t>(P.tokens.rows) && S.keys[next] == key && (first == 0 || S.keys[first - 1] != key)) {
+            // The last chunk that begins with the key: steps that double, then bisection.
+            uint32_t lo = mine + 1, hi = S.chunks;
+            for (uint32_t step = 1; lo + step < hi; step *= 2) {
+                if (S.keys[(lo + step) * S.chunk] != key) hi = lo + step;
+                else lo += step;
+            }
+            while (hi - lo > 1) {
+                const uint32_t mid = (lo + hi) / 2;
+                if (S.keys[mid * S.chunk] == key) lo = mid;
+                else hi = mid;
+            }
+            pieces = lo - mine;
+        }
     }
-    const uint32_t end_chunk = (lo - 1) / S.chunk;
-    const uint32_t pieces = end_chunk - chunk;  // after the tail
-    const bool split = pieces > 4;
-    const uint32_t a = split ? static_cast<uint64_t>(pieces) * wid / kReduceWarps : 0;
-    const uint32_t b = split ? static_cast<uint64_t>(pieces) * (wid + 1) / kReduceWarps : pieces;
-    for (int slab = split ? 0 : wid; slab < slabs; slab += split ? 1 : kReduceWarps) {
-        const int base = slab * kSlab<V>, col = base + lane * V;
+    auto add_pieces = [&](Sum<V>& sum, uint32_t chunk, uint32_t a, uint32_t b) {
+        for (uint32_t k = a; k < b; k += kJoinLoads) {
+            Sum<V> x[kJoinLoads];
+#pragma unroll
+            for (int u = 0; u < kJoinLoads; ++u) {
+                x[u].clear();
+                if (k + u < b) x[u].add(S.head + static_cast<int64_t>(chunk + 1 + k + u) * P.dim, col, P.dim);
+            }
+#pragma unroll
+            for (int u = 0; u < kJoinLoads; ++u) sum.add(x[u]);
+        }
+    };
+    uint32_t shorts = __ballot_sync(kFull, pieces > 0 && pieces <= kJoinShort);
+    for (int k = 0; shorts; ++k, shorts &= shorts - 1) {
+        const int l = __ffs(shorts) - 1;
+        const uint32_t count = __shfl_sync(kFull, pieces, l), row = __shfl_sync(kFull, key, l);
+        if (k % kReduceWarps != wid) continue;
         Sum<V> sum;
         sum.clear();
-        if (!split || wid == 0) sum.add(S.tail + static_cast<int64_t>(chunk) * P.dim, col, P.dim);
-#pragma unroll 4
-        for (uint32_t k = a; k < b; ++k) sum.add(S.head + static_cast<int64_t>(chunk + 1 + k) * P.dim, col, P.dim);
-        if (split) {
-            sum.put(part[wid], lane * V, P.dim - base);
-            __syncthreads();
-            if (wid == 0) {
-                sum.clear();
-                for (int w = 0; w < kReduceWarps; ++w) sum.add(part[w], lane * V, P.dim - base);
-                finish_row<V>(P, key, col, sum);
-            }
-            __syncthreads();
-        } else {
-            finish_row<V>(P, key, col, sum);
+        sum.add(S.tail + static_cast<int64_t>(chunk0 + l) * P.dim, col, P.dim);
+        add_pieces(sum, chunk0 + l, 0, count);
+        finish_row<V>(P, row, col, sum);
+    }
+    uint32_t longs = __ballot_sync(kFull, pieces > kJoinShort);  // the same in every warp
+    for (; longs; longs &= longs - 1) {
+        const int l = __ffs(longs) - 1;
+        const uint32_t count = __shfl_sync(kFull, pieces, l), row = __shfl_sync(kFull, key, l);
+        Sum<V> sum;
+        sum.clear();
+        if (wid == 0) sum.add(S.tail + static_cast<int64_t>(chunk0 + l) * P.dim, col, P.dim);
+        add_pieces(sum, chunk0 + l, static_cast<uint32_t>(static_cast<uint64_t>(count) * wid / kReduceWarps),
+                   static_cast<uint32_t>(static_cast<uint64_t>(count) * (wid + 1) / kReduceWarps));
+        sum.put(part[wid], lane * V, P.dim - base);
+        __syncthreads();
+        if (wid == 0) {
+            sum.clear();
+            for (int w = 0; w < kReduceWarps; ++w) sum.add(part[w], lane * V, P.dim - base);
+            finish_row<V>(P, row, col, sum);
         }
+        __syncthreads();
     }
 }
 
-constexpr uint32_t kGradChunk = 32;
+// Sorted positions per chunk: short enough for the chunks and slabs of a call to give every
+// SM some 32 warps, long enough for the sums that chunks leave (two rows in fp32 at most) to
+// be few beside the rows that they read.
+uint32_t grad_chunk(int64_t n, int32_t dim) {
+    const int64_t warps = 152 * 32, slabs = (dim + 255) / 256;
+    uint32_t chunk = 128;
+    while (chunk > 16 && n * slabs / chunk < warps) chunk /= 2;
+    return chunk;
+}
 
 int key_bits(int64_t rows) {  // keys are 0 .. rows
     int bits = 1;
@@ -518,8 +606,9 @@ int key_bits(int64_t rows) {  // keys are 0 .. rows
 }
 
 struct GradWorkspace {
-    size_t keys[2], positions[2], tiles, digits, table, scalars, head, tail, bytes;
-    int64_t num_tiles;
+    size_t keys[2], positions[2], tiles, digits, table, scalars, touched, head, tail, bytes;
+    int64_t num_tiles, touched_words;
+    uint32_t chunk;
     int passes;
 };
 GradWorkspace grad_layout(int64_t n, int64_t rows, int32_t dim) {
@@ -541,7 +630,10 @@ GradWorkspace grad_layout(int64_t n, int64_t rows, int32_t dim) {
     w.digits = take((w.num_tiles + 1) * w.passes * kRadixDigits * 4);
     w.table = take(sizeof(TableDev));
     w.scalars = take(5 * 8);
-    const int64_t chunks = (n + kGradChunk - 1) / kGradChunk;
+    w.touched_words = (rows + 7) / 8;
+    w.touched = take(w.touched_words * 8);
+    w.chunk = grad_chunk(n, dim);
+    const int64_t chunks = (n + w.chunk - 1) / w.chunk;
     w.head = take(chunks * dim * 4);
     w.tail = take(chunks * dim * 4);
     w.bytes = at;
@@ -558,8 +650,26 @@ void launch_match(const GradArgs& P, cudaStream_t s) {
            token_blocks, groups);
 }
 
+template <class T>
+void launch_fill(const GradArgs& P, const uint8_t* touched, int sms, cudaStream_t s) {
+    const int64_t elem = dtype_bytes(P.grad_dtype), warps = (P.tokens.rows + kFillWarpRows - 1) / kFillWarpRows;
+    static const int resident = resident_blocks(token_fill_kernel<T>, 256);
+    const int64_t most = static_cast<int64_t>(sms) * resident;
+    launch(token_fill_kernel<T>, dim3(static_cast<unsigned>(min64((warps + 7) / 8, most))), dim3(256), 0, s,
+           static_cast<char*>(P.grad), P.grad_stride * elem, P.dim * elem, P.tokens.rows, touched);
+}
+// Rows in the widest stores that divide them and their distance.
+void launch_fill(const GradArgs& P, const uint8_t* touched, int sms, cudaStream_t s) {
+    const int64_t elem = dtype_bytes(P.grad_dtype);
+    const uint64_t all = static_cast<uint64_t>(P.grad_stride * elem) | static_cast<uint64_t>(P.dim * elem) |
+                         reinterpret_cast<uintptr_t>(P.grad);
+    if (all % 16 == 0) launch_fill<uint4>(P, touched, sms, s);
+    else if (all % 4 == 0) launch_fill<uint32_t>(P, touched, sms, s);
+    else launch_fill<uint16_t>(P, touched, sms, s);
+}
+
 template <int DT, int V>
-void launch_sorted(const GradArgs& P, const GradWorkspace& w, char* base, cudaStream_t s) {
+void launch_sorted(const GradArgs& P, const GradWorkspace& w, char* base, int sms, cudaStream_t s) {
     SortBuffers B{};
     for (int i = 0; i < 2; ++i) {
         B.keys[i] = reinterpret_cast<uint32_t*>(base + w.keys[i]);
@@ -572,7 +682,12 @@ void launch_sorted(const GradArgs& P, const GradWorkspace& w, char* base, cudaSt
     B.first_tile = scalars;
     B.table_pos = scalars + 2;
     B.num_tiles = scalars + 4;
-    const bool few = w.num_tiles <= kFewSortTiles;
+    const bool few = w.num_tiles <= kFewSortTiles, fill = !P.accumulate && P.tokens.rows > 0;
+    if (fill) {
+        B.touched = reinterpret_cast<uint8_t*>(base + w.touched);
+        launch(token_clear_kernel, dim3(static_cast<unsigned>(min64(sms, (w.touched_words + 255) / 256))), dim3(256), 0,
+               s, reinterpret_cast<uint2*>(B.touched), w.touched_words);
+    }
     launch(token_keys_kernel, dim3(static_cast<unsigned>(w.num_tiles)), dim3(kKeyThreads), 0, s, P, B, w.passes);
     const int64_t words = w.num_tiles * kRadixDigits;
     // With many tiles every pass counts its own digits, per tile (one array) and in total.
@@ -595,39 +710,50 @@ void launch_sorted(const GradArgs& P, const GradWorkspace& w, char* base, cudaSt
         S.next_digits = few && p + 1 < w.passes ? S.tile_digits + words : nullptr;
         S.table_digits = few ? nullptr : totals + p * kRadixDigits;
         S.T = 1;
+        // All but the first pass let the kernels after them launch at once: token_fill_kernel
+        // then runs beside the sort, behind the first pass's wait for the keys.
+        S.release = few && fill && p > 0;
         launch_radix_pass(S, w.num_tiles, s);
     }
+    if (fill) launch_fill(P, B.touched, sms, s);
     Sorted R{};
     R.keys = B.keys[w.passes & 1];
     R.positions = B.positions[w.passes & 1];
-    R.chunk = kGradChunk;
-    R.chunks = (P.tokens.n + kGradChunk - 1) / kGradChunk;
+    R.chunk = w.chunk;
+    R.chunks = (P.tokens.n + R.chunk - 1) / R.chunk;
     R.head = reinterpret_cast<float*>(base + w.head);
     R.tail = reinterpret_cast<float*>(base + w.tail);
     const int slabs = (P.dim + kSlab<V> - 1) / kSlab<V>;
-    const uint32_t reduce_blocks =
-        static_cast<uint32_t>((static_cast<uint64_t>(R.chunks) * slabs + kReduceWarps - 1) / kReduceWarps);
-    const int64_t rows_per_block = kReduceWarps * kFillWarpRows;
-    const int64_t fill = P.accumulate ? 0 : (P.tokens.rows + rows_per_block - 1) / rows_per_block;
-    launch(token_reduce_kernel<DT, V>, dim3(static_cast<unsigned>(reduce_blocks + fill)), dim3(kReduceThreads), 0, s, P, R,
-           slabs, reduce_blocks);
-    if (R.chunks > 1) launch(token_join_kernel<V>, dim3(R.chunks - 1), dim3(kReduceThreads), 0, s, P, R, slabs);
+    const uint64_t warps = static_cast<uint64_t>(R.chunks) * slabs;
+    launch(token_reduce_kernel<DT, V>, dim3(static_cast<unsigned>((warps + kReduceWarps - 1) / kReduceWarps)),
+           dim3(kReduceThreads), 0, s, P, R, slabs);
+    if (R.chunks > 1)
+        launch(token_join_kernel<V>, dim3((R.chunks + kJoinChunks - 1) / kJoinChunks * slabs), dim3(kReduceThreads), 0, s,
+               P, R, slabs);
 }
 
 template <int DT, int V>
-void launch_grad(const GradArgs& P, const GradWorkspace& w, char* base, cudaStream_t s) {
+void launch_grad(const GradArgs& P, const GradWorkspace& w, char* base, int sms, cudaStream_t s) {
     if (P.tokens.n <= kMatchTokens) launch_match<DT, V>(P, s);
-    else launch_sorted<DT, V>(P, w, base, s);
+    else launch_sorted<DT, V>(P, w, base, sms, s);
 }
 template <int DT>
-void launch_grad(const GradArgs& P, const GradWorkspace& w, char* base, int v, cudaStream_t s) {
-    if (v == 8) launch_grad<DT, 8>(P, w, base, s);
-    else if (v == 4) launch_grad<DT, 4>(P, w, base, s);
-    else launch_grad<DT, 1>(P, w, base, s);
+void launch_grad(const GradArgs& P, const GradWorkspace& w, char* base, int v, int sms, cudaStream_t s) {
+    if (v == 8) launch_grad<DT, 8>(P, w, base, sms, s);
+    else if (v == 4) launch_grad<DT, 4>(P, w, base, sms, s);
+    else launch_grad<DT, 1>(P, w, base, sms, s);
 }
 
 // ---------------------------------------------------------------- arguments
 
+bool current_sms(int* sms) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) == cudaSuccess &&
+        cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && *sms > 0)
+        return true;
+    cudaGetLastError();
+    return false;
+}
 bool valid_dtype(int d) { return d == CB_F32 || d == CB_F16 || d == CB_BF16; }
 
 // A row-major operand whose rows are taken in pieces of v values: v divides its dim and
@@ -731,9 +857,11 @@ extern "C" cb_status cb_token_backward(const void* grad_out, cb_dtype go_dtype, 
     int v = go_dtype == CB_F32 && grad_dtype == CB_F32 ? 4 : 8;
     while (v > 1 && !(takes(grad_out, go_dtype, dim, s0, s1, v) && takes(grad, grad_dtype, dim, row_stride, 0, v)))
         v = v == 8 ? 4 : 1;
+    int sms = 0;
+    if (!current_sms(&sms)) return CB_ERR_CUDA;
     char* base = static_cast<char*>(workspace);
-    if (go_dtype == CB_F32) launch_grad<CB_F32>(P, w, base, v, stream);
-    else if (go_dtype == CB_F16) launch_grad<CB_F16>(P, w, base, v, stream);
-    else launch_grad<CB_BF16>(P, w, base, v, stream);
+    if (go_dtype == CB_F32) launch_grad<CB_F32>(P, w, base, v, sms, stream);
+    else if (go_dtype == CB_F16) launch_grad<CB_F16>(P, w, base, v, sms, stream);
+    else launch_grad<CB_BF16>(P, w, base, v, sms, stream);
     return cudaGetLastError() == cudaSuccess ? CB_OK : CB_ERR_CUDA;
 }

@@ -248,6 +248,15 @@ def test_gradient_without_tokens():
     assert te().token_backward(go, tokens, 0).shape == (0, 16)
 
 
+@pytest.mark.parametrize("n", [10, 3000])
+def test_gradient_and_lookup_of_a_table_without_rows(n):
+    tokens = torch.zeros(n, dtype=torch.int64, device=DEV)
+    error = torch.zeros(1, dtype=torch.int32, device=DEV)
+    assert te().token_backward(torch.ones(n, 16, device=DEV), tokens, 0, error=error).shape == (0, 16)
+    assert error.item() == 2
+    assert not te().token_forward(torch.empty(0, 16, device=DEV), tokens).any()
+
+
 def test_gradient_with_many_sort_tiles():
     # More tiles than the one-kernel radix pass takes.
     n, rows = 2_200_000, 100_003
