@@ -35,6 +35,15 @@
 #include <cmath>
 #include <cudaTypedefs.h>
 
+#ifndef CB_STEP64
+#define CB_STEP64 450
+#endif
+#ifndef CB_STEP128
+#define CB_STEP128 700
+#endif
+#ifndef CB_PAIRX
+#define CB_PAIRX 3000
+#endif
 namespace cbtbe {
 namespace {
 
@@ -46,9 +55,16 @@ constexpr int kMaxSteps = 64;
 // ---------------------------------------------------------------- norm and momentum
 
 // x^2 summed by magnitude: |x| >= 2^40 times 2^-160, |x| < 2^-40 times 2^160, the rest
-// as it is. A NaN goes with the rest.
+// as it is, with what its additions and squares round off kept beside it: the norm then is
+// the same whatever the order of its sum (for a transposed or strided matrix, too). A NaN
+// goes with the rest.
 struct SquareSum {
-    float mid = 0.f, big = 0.f, small = 0.f;
+    float mid = 0.f, rest = 0.f, big = 0.f, small = 0.f;
+    __device__ __forceinline__ void add_mid(float x) {  // the exact error of a sum of two floats
+        const float t = mid + x, y = t - mid;
+        rest += (mid - (t - y)) + (x - y);
+        mid = t;
+    }
     __device__ __forceinline__ void add(float x) {
         const float m = fabsf(x);
         if (m >= 0x1p40f) {
@@ -58,7 +74,26 @@ struct SquareSum {
             const float y = x * 0x1p80f;
             small = fmaf(y, y, small);
         } else {
-            mid = fmaf(x, x, mid);
+            const float p = x * x;
+            rest += fmaf(x, x, -p);
+            add_mid(p);
+        }
+    }
+    __device__ __forceinline__ void add(const SquareSum& o) {
+        add_mid(o.mid);
+        rest += o.rest;
+        big += o.big;
+        small += o.small;
+    }
+    __device__ __forceinline__ void add_lanes() {  // lane 0 gets the warp's sum
+#pragma unroll
+        for (int off = 16; off >= 1; off >>= 1) {
+            SquareSum o;
+            o.mid = __shfl_down_sync(kFull, mid, off);
+            o.rest = __shfl_down_sync(kFull, rest, off);
+            o.big = __shfl_down_sync(kFull, big, off);
+            o.small = __shfl_down_sync(kFull, small, off);
+            add(o);
         }
     }
 };
@@ -85,6 +120,24 @@ __device__ __forceinline__ void store_value(void* p, int64_t i, float v, int dty
     if (dtype == CB_F32) static_cast<float*>(p)[i] = v;
     else if (dtype == CB_BF16) static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
     else static_cast<__half*>(p)[i] = __float2half_rn(v);
+}
+template <int DT>
+__device__ __forceinline__ void store_values4(void* p, int64_t i, const float (&v)[4]) {
+    if constexpr (DT == CB_F32) {
+        *reinterpret_cast<float4*>(static_cast<float*>(p) + i) = make_float4(v[0], v[1], v[2], v[3]);
+    } else {
+        uint2 w;
+        if constexpr (DT == CB_BF16) {
+            const __nv_bfloat162 a = __floats2bfloat162_rn(v[0], v[1]), b = __floats2bfloat162_rn(v[2], v[3]);
+            memcpy(&w.x, &a, 4);
+            memcpy(&w.y, &b, 4);
+        } else {
+            const __half2 a = __floats2half2_rn(v[0], v[1]), b = __floats2half2_rn(v[2], v[3]);
+            memcpy(&w.x, &a, 4);
+            memcpy(&w.y, &b, 4);
+        }
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) = w;
+    }
 }
 
 // V consecutive values (V = 1, or 4 with their alignment).
@@ -115,14 +168,14 @@ __device__ __forceinline__ void load_values(const void* p, int64_t i, int dtype,
 }
 
 constexpr int kNormThreads = 256;
-constexpr int kNormBlocks = 128;  // most blocks (and partial sums) per matrix
+constexpr int kNormBlocks = 1024;  // most blocks (and partial sums) per matrix
 
 __host__ __device__ __forceinline__ float mix_momentum(float m, float g, float beta) { return fmaf(beta, m, g); }
 
 // m <- beta m + g in place, and a block's part of the squares of the update u
 // (g; m; or g + beta m). Blocks (x of a matrix, matrix).
 template <int V>
-__global__ void __launch_bounds__(kNormThreads) muon_norm_kernel(MatrixIn in, float* __restrict__ partial) {
+__global__ void __launch_bounds__(kNormThreads) muon_norm_kernel(MatrixIn in, SquareSum* __restrict__ partial) {
     begin_kernel();
     const int b = blockIdx.y;
     const char* g = static_cast<const char*>(in.g) + b * in.g_batch * dtype_bytes(in.dtype);
@@ -176,44 +229,50 @@ __global__ void __launch_bounds__(kNormThreads) muon_norm_kernel(MatrixIn in, fl
             }
         }
     }
-    // A fixed order: lanes, then warps.
-    __shared__ float sh[3][kNormThreads / 32];
-    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-#pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) {
-        s.mid += __shfl_xor_sync(kFull, s.mid, off);
-        s.big += __shfl_xor_sync(kFull, s.big, off);
-        s.small += __shfl_xor_sync(kFull, s.small, off);
-    }
-    if (lane == 0) {
-        sh[0][wid] = s.mid;
-        sh[1][wid] = s.big;
-        sh[2][wid] = s.small;
-    }
+    __shared__ __align__(16) unsigned char raw[kNormThreads / 32 * sizeof(SquareSum)];
+    SquareSum* sh = reinterpret_cast<SquareSum*>(raw);
+    s.add_lanes();
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
     __syncthreads();
-    if (threadIdx.x < 3) {
-        float t = 0.f;
-        for (int w = 0; w < kNormThreads / 32; ++w) t += sh[threadIdx.x][w];
-        partial[(static_cast<int64_t>(b) * kNormBlocks + blockIdx.x) * 3 + threadIdx.x] = t;
+    if (threadIdx.x == 0) {
+#pragma unroll
+        for (int w = 1; w < kNormThreads / 32; ++w) s.add(sh[w]);
+        partial[static_cast<int64_t>(b) * kNormBlocks + blockIdx.x] = s;
     }
 }
 
 // kScaleX / (norm + eps) as a product of two floats, so that neither a huge nor a tiny
-// norm takes it out of range; from the partial sums of one matrix, by one warp.
-__device__ __forceinline__ float2 inverse_norm(const float* partial, int blocks, float eps, int lane) {
-    double t = 0.0;
-    for (int k = lane; k < blocks; k += 32)
-        t += static_cast<double>(partial[3 * k]) + static_cast<double>(partial[3 * k + 1]) * 0x1p160 +
-             static_cast<double>(partial[3 * k + 2]) * 0x1p-160;
+// norm takes it out of range; from the partial sums of one matrix, by a block of 256 threads.
+// One thread finishes it, in fp64 only where fp32's range asks for it (every block of a large
+// matrix does this, and fp64 is slow: 140 us for 4096 x 4096 when all threads did).
+__device__ __forceinline__ float2 inverse_norm(const SquareSum* partial, int blocks, float eps) {
+    __shared__ __align__(16) unsigned char raw[8 * sizeof(SquareSum)];
+    SquareSum* sh = reinterpret_cast<SquareSum*>(raw);
+    __shared__ float2 result;
+    SquareSum t;
+    for (int k = threadIdx.x; k < blocks; k += 256) t.add(partial[k]);
+    t.add_lanes();
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = t;
+    __syncthreads();
+    if (threadIdx.x == 0) {
 #pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) t += __shfl_xor_sync(kFull, t, off);
-    const double norm = sqrt(t) + static_cast<double>(eps);
-    // A matrix of zeros with eps = 0 stays zeros.
-    const double inv = norm == 0.0 ? 0.0 : static_cast<double>(kScaleX) / norm;
-    int e = 0;
-    const double mant = frexp(inv, &e);
-    const int half = e / 2;
-    return make_float2(static_cast<float>(ldexp(1.0, half)), static_cast<float>(ldexp(mant, e - half)));
+        for (int w = 1; w < 8; ++w) t.add(sh[w]);
+        const float mid = t.mid + t.rest;
+        if (t.big == 0.f && mid >= 0x1p-60f) {  // the small class is below fp32's precision then
+            result = make_float2(1.f, kScaleX / (sqrtf(mid) + eps));
+        } else {
+            const double norm = sqrt(static_cast<double>(mid) + static_cast<double>(t.big) * 0x1p160 +
+                                     static_cast<double>(t.small) * 0x1p-160) + static_cast<double>(eps);
+            // A matrix of zeros with eps = 0 stays zeros.
+            const double inv = norm == 0.0 ? 0.0 : static_cast<double>(kScaleX) / norm;
+            int e = 0;
+            const double mant = frexp(inv, &e);
+            const int half = e / 2;
+            result = make_float2(static_cast<float>(ldexp(1.0, half)), static_cast<float>(ldexp(mant, e - half)));
+        }
+    }
+    __syncthreads();
+    return result;
 }
 
 // ---------------------------------------------------------------- cast
@@ -221,57 +280,77 @@ __device__ __forceinline__ float2 inverse_norm(const float* partial, int blocks,
 constexpr int kCastTile = 64;
 
 // X_0 = kScaleX u / (||u|| + eps) as hi + lo, [p, ld] rows: u as it lies, or transposed.
-// A block takes a 64 x 64 tile of u: blocks (column tile, row tile, matrix).
-template <bool TRANSPOSED>
-__global__ void __launch_bounds__(256) muon_cast_kernel(MatrixIn in, const float* __restrict__ partial, int norm_blocks,
+// A block takes a 64 x 64 tile of u, a thread four times 4 consecutive values of it (V = 4: in
+// one load each) and of X: blocks (column tile, row tile, matrix). Rows of X are padded to 64
+// values, so its tiles are stored whole along a row.
+template <bool TRANSPOSED, int V>
+__global__ void __launch_bounds__(256) muon_cast_kernel(MatrixIn in, const SquareSum* __restrict__ partial, int norm_blocks,
                                                         float eps, __half* __restrict__ hi, __half* __restrict__ lo,
                                                         int ld, int64_t x_batch) {
-    __shared__ float2 factor;
     __shared__ float tile[TRANSPOSED ? kCastTile : 1][kCastTile + 1];
     begin_kernel();
     const int b = blockIdx.z;
     const int r0 = blockIdx.y * kCastTile, c0 = blockIdx.x * kCastTile;
-    if (threadIdx.x < 32) {
-        const float2 f = inverse_norm(partial + static_cast<int64_t>(b) * kNormBlocks * 3, norm_blocks, eps, threadIdx.x);
-        if (threadIdx.x == 0) factor = f;
-    }
     const char* g = static_cast<const char*>(in.g) + b * in.g_batch * dtype_bytes(in.dtype);
     const float* mom = in.momentum ? in.momentum + b * in.m_batch : nullptr;
-    const int c = threadIdx.x & 63, rq = threadIdx.x >> 6;
-    float v[16];
+    const int c = (threadIdx.x & 15) * 4, rq = threadIdx.x >> 4;
+    float v[4][4], m[4][4];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        const int row = r0 + rq + 4 * k, col = c0 + c;
-        v[k] = 0.f;
-        if (row < in.rows && col < in.cols) {
-            v[k] = load_value(g, row * in.g_row + col, in.dtype);
-            if (mom) {
-                const float m = mom[row * in.m_row + col];
-                v[k] = in.nesterov ? mix_momentum(m, v[k], in.beta) : m;
+    for (int k = 0; k < 4; ++k) {
+        const int64_t row = r0 + rq + 16 * k;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[k][e] = m[k][e] = 0.f;
+        if (row >= in.rows) continue;
+        if constexpr (V == 4) {
+            if (c0 + c < in.cols) {
+                load_values<4>(g, row * in.g_row + c0 + c, in.dtype, v[k]);
+                if (mom) load_values<4>(mom, row * in.m_row + c0 + c, CB_F32, m[k]);
             }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (c0 + c + e < in.cols) {
+                    v[k][e] = load_value(g, row * in.g_row + c0 + c + e, in.dtype);
+                    if (mom) m[k][e] = mom[row * in.m_row + c0 + c + e];
+                }
         }
     }
-    __syncthreads();
-    const float2 f = factor;
-    auto put = [&](int64_t at, float x) {
-        const __half h = __float2half_rn(x);
-        hi[at] = h;
-        lo[at] = __float2half_rn(x - __half2float(h));
+    const float2 f = inverse_norm(partial + static_cast<int64_t>(b) * kNormBlocks, norm_blocks, eps);
+    auto put = [&](int64_t at, const float (&x)[4]) {
+        uint32_t h[2], l[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const __half2 top = __floats2half2_rn(x[2 * e], x[2 * e + 1]);
+            const float2 back = __half22float2(top);
+            const __half2 rest = __floats2half2_rn(x[2 * e] - back.x, x[2 * e + 1] - back.y);
+            memcpy(&h[e], &top, 4);
+            memcpy(&l[e], &rest, 4);
+        }
+        *reinterpret_cast<uint2*>(hi + at) = make_uint2(h[0], h[1]);
+        *reinterpret_cast<uint2*>(lo + at) = make_uint2(l[0], l[1]);
     };
     const int64_t base = b * x_batch;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        const float x = (v[k] * f.x) * f.y;
-        const int row = r0 + rq + 4 * k, col = c0 + c;
-        if constexpr (TRANSPOSED) tile[rq + 4 * k][c] = x;
-        else if (row < in.rows && col < in.cols) put(base + static_cast<int64_t>(row) * ld + col, x);
+    for (int k = 0; k < 4; ++k) {
+        const int row = r0 + rq + 16 * k;
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float u = !mom ? v[k][e] : (in.nesterov ? mix_momentum(m[k][e], v[k][e], in.beta) : m[k][e]);
+            x[e] = (u * f.x) * f.y;
+            if constexpr (TRANSPOSED) tile[rq + 16 * k][c + e] = x[e];
+        }
+        if (!TRANSPOSED && row < in.rows) put(base + static_cast<int64_t>(row) * ld + c0 + c, x);
     }
     if constexpr (TRANSPOSED) {
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            const int row = r0 + c, col = c0 + rq + 4 * k;  // value (row, col) of u is X[col, row]
-            if (row < in.rows && col < in.cols) put(base + static_cast<int64_t>(col) * ld + row, tile[c][rq + 4 * k]);
+        for (int k = 0; k < 4; ++k) {
+            const int col = c0 + rq + 16 * k;  // value (row, col) of u is X[col, row]
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = tile[c + e][rq + 16 * k];
+            if (col < in.cols) put(base + static_cast<int64_t>(col) * ld + r0 + c, x);
         }
     }
 }
@@ -287,16 +366,17 @@ enum Product {
 template <Product WHAT> constexpr bool kSymmetric = WHAT == kGram || WHAT == kPoly;
 
 constexpr int kTileM = 128, kTileK = 64;
-constexpr int kEpilogueWarps = 4;
+constexpr int kEpilogueWarps = 8;  // two for each quarter of TMEM's lanes, every other 32 columns each
 constexpr int kProductThreads = (kEpilogueWarps + 2) * 32;  // + a copying warp, + a multiplying warp
-constexpr uint32_t kBoxBytes = 64 * 64 * 2;                 // one TMA box: 64 rows of 64 fp16
-template <int BN> constexpr int kStages = BN == 256 ? 4 : (BN == 128 ? 6 : 8);
+constexpr uint32_t kBoxBytes = 64 * 64 * 2;                 // 64 rows of 64 fp16
+template <int BN> constexpr int kStages = BN == 128 ? 6 : 8;
 template <int BN> constexpr uint32_t kStageBytes = (kTileM + BN) * kTileK * 2;
 
 struct ProductArgs {
     int32_t m, n, k;          // C [m, n], K
     int32_t batch;
     int32_t row_tiles, col_tiles;
+    int32_t width;            // columns of a tile
     int64_t tiles;            // per matrix
     float a, b, c;            // the step's coefficients (a = 0: no term a X, or a I)
     const __half* term_hi;    // kPoly: A; kUpdate, kResult: X
@@ -312,6 +392,7 @@ struct ProductArgs {
     int64_t user_batch, user_row;
     int32_t user_dtype;
     int32_t transposed;       // value (i, j) of C is value (j, i) of the caller's
+    int32_t user_vector;      // its rows can be taken 4 values at a time
     int32_t weights;          // W <- keep W - rate O, instead of O
     float keep, rate;
     int* error;
@@ -321,14 +402,13 @@ struct Tile {
     int32_t b, i, j;
 };
 
-// Column tiles of row tile i that reach the lower triangle of 128 x 128 blocks.
-template <int BN>
-__host__ __device__ __forceinline__ int lower_tiles(int i, int col_tiles) {
-    const int need = ((i + 1) * kTileM + BN - 1) / BN;
+// Column tiles of `width` of row tile i (of `height`) that reach the lower triangle.
+__host__ __device__ __forceinline__ int lower_tiles(int i, int height, int width, int col_tiles) {
+    const int need = ((i + 1) * height + width - 1) / width;
     return need < col_tiles ? need : col_tiles;
 }
 
-template <int BN, Product WHAT>
+template <int HEIGHT, Product WHAT>
 __device__ __forceinline__ Tile tile_at(const ProductArgs& P, int64_t t) {
     Tile T;
     T.b = static_cast<int>(t / P.tiles);
@@ -336,7 +416,7 @@ __device__ __forceinline__ Tile tile_at(const ProductArgs& P, int64_t t) {
     if constexpr (kSymmetric<WHAT>) {
         T.i = 0;
         while (true) {
-            const int c = lower_tiles<BN>(T.i, P.col_tiles);
+            const int c = lower_tiles(T.i, HEIGHT, P.width, P.col_tiles);
             if (r < c) break;
             r -= c;
             ++T.i;
@@ -376,20 +456,92 @@ __device__ __forceinline__ void store_halves(__half* p, const float (&v)[32]) {
     }
 }
 
+// 16 columns of a warp's 32 rows into the caller's matrix, through shared memory so that
+// lanes run along the caller's rows, 4 values each: loads (of weights) first, then stores.
+constexpr int kStageFloats = 32 * 20;  // rows of 16 (or, transposed, 32) values padded to 20 (36)
+template <int DT>
+__device__ __forceinline__ void finish_result(const ProductArgs& P, int batch, int row, int col, const float* v,
+                                              float* stage, int lane) {
+    char* user = static_cast<char*>(P.user) + batch * P.user_batch * dtype_bytes(DT);
+    __syncwarp();
+    if (P.transposed) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) stage[k * 36 + lane] = v[k];
+    } else {
+#pragma unroll
+        for (int k = 0; k < 16; k += 4)
+            *reinterpret_cast<float4*>(stage + lane * 20 + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+    }
+    __syncwarp();
+    const int row0 = P.transposed ? col : row - lane, col0 = P.transposed ? row - lane : col;
+    const int rows = P.transposed ? P.n : P.m, cols = P.transposed ? P.m : P.n;  // of the caller's matrix
+    const int wide = P.transposed ? 8 : 4, pitch = P.transposed ? 36 : 20;       // lanes per row
+    const int c = lane % wide * 4, r = lane / wide, step = 32 / wide;
+    const int64_t at = static_cast<int64_t>(row0 + r) * P.user_row + col0 + c, down = step * P.user_row;
+    float w[4][4] = {};
+    if (P.weights) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (row0 + r + k * step >= rows) break;
+            if (P.user_vector) {
+                if (col0 + c < cols) load_values<4>(user, at + k * down, DT, w[k]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (col0 + c + e < cols) w[k][e] = load_value(user, at + k * down + e, DT);
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (row0 + r + k * step >= rows) break;
+        const float4 s = *reinterpret_cast<const float4*>(stage + (r + k * step) * pitch + c);
+        float x[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[e] *= 1.f / kScaleX;
+            if (P.weights) x[e] = fmaf(-P.rate, x[e], P.keep * w[k][e]);
+        }
+        if (P.user_vector) {
+            if (col0 + c < cols) store_values4<DT>(user, at + k * down, x);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (col0 + c + e < cols) store_value(user, at + k * down + e, x[e], DT);
+        }
+    }
+}
+
+// What the result at a lane's 32 columns has added to it: loaded a turn ahead of its use.
+struct Term {
+    uint4 hi[4], lo[4];
+};
+template <Product WHAT>
+__device__ __forceinline__ void load_term(const ProductArgs& P, int batch, int row, int col, Term& t) {
+    if (row >= P.m || col >= P.n || WHAT == kGram || (WHAT != kPoly && P.a == 0.f)) return;
+    const int64_t at = batch * P.term_batch + static_cast<int64_t>(row) * P.term_ld + col;
+    const uint4* hi = reinterpret_cast<const uint4*>(P.term_hi + at);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) t.hi[k] = hi[k];
+    if (WHAT != kPoly && P.term_lo) {
+        const uint4* lo = reinterpret_cast<const uint4*>(P.term_lo + at);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) t.lo[k] = lo[k];
+    }
+}
+
 // 32 columns [col, col + 32) of row `row` of a tile's result: `v` holds the products' sums.
-template <int BN, Product WHAT>
-__device__ __forceinline__ void finish(const ProductArgs& P, const Tile& T, int row, int col, float (&v)[32],
-                                       float (*stage)[33], int lane) {
+template <Product WHAT>
+__device__ __forceinline__ void finish(const ProductArgs& P, int batch, int row, int col, float (&v)[32],
+                                       const Term& term, float* stage, int lane) {
     const bool live = row < P.m;
     if constexpr (WHAT == kGram) {
         constexpr float s = kScaleA / (kScaleX * kScaleX);
 #pragma unroll
         for (int k = 0; k < 32; ++k) v[k] *= s;
     } else if constexpr (WHAT == kPoly) {
-        float t[32] = {};
-        if (live)
-            unpack_halves(reinterpret_cast<const uint4*>(P.term_hi + T.b * P.term_batch +
-                                                         static_cast<int64_t>(row) * P.term_ld + col), t);
+        float t[32];
+        unpack_halves(term.hi, t);
         const float c = P.c / kScaleA, diagonal = P.a * kScaleA;
 #pragma unroll
         for (int k = 0; k < 32; ++k) {
@@ -399,30 +551,29 @@ __device__ __forceinline__ void finish(const ProductArgs& P, const Tile& T, int 
     } else {
 #pragma unroll
         for (int k = 0; k < 32; ++k) v[k] *= 1.f / kScaleA;
-        if (P.a != 0.f && live) {
-            const int64_t at = T.b * P.term_batch + static_cast<int64_t>(row) * P.term_ld + col;
+        if (P.a != 0.f) {
             float t[32];
             if (P.term_lo) {
-                unpack_halves(reinterpret_cast<const uint4*>(P.term_lo + at), t);
+                unpack_halves(term.lo, t);
 #pragma unroll
                 for (int k = 0; k < 32; ++k) v[k] = fmaf(P.a, t[k], v[k]);
             }
-            unpack_halves(reinterpret_cast<const uint4*>(P.term_hi + at), t);
+            unpack_halves(term.hi, t);
 #pragma unroll
             for (int k = 0; k < 32; ++k) v[k] = fmaf(P.a, t[k], v[k]);
         }
     }
     if constexpr (kSymmetric<WHAT>) {
-        __half* out = P.out_hi + T.b * P.out_batch;
-        const int block = col / kTileM;
-        if (live && block <= T.i) store_halves(out + static_cast<int64_t>(row) * P.out_ld + col, v);
-        if (live && block < T.i) {  // whole blocks of columns below the diagonal: all within the matrix
+        __half* out = P.out_hi + batch * P.out_batch;
+        const int block = col / kTileM, row_block = row / kTileM;
+        if (live && block <= row_block) store_halves(out + static_cast<int64_t>(row) * P.out_ld + col, v);
+        if (live && block < row_block) {  // whole blocks of columns below the diagonal: all within the matrix
 #pragma unroll
             for (int k = 0; k < 32; ++k) out[static_cast<int64_t>(col + k) * P.out_ld + row] = __float2half_rn(v[k]);
         }
     } else if constexpr (WHAT == kUpdate) {
         if (live) {
-            const int64_t at = T.b * P.out_batch + static_cast<int64_t>(row) * P.out_ld + col;
+            const int64_t at = batch * P.out_batch + static_cast<int64_t>(row) * P.out_ld + col;
             store_halves(P.out_hi + at, v);
             if (P.out_lo) {
 #pragma unroll
@@ -431,28 +582,37 @@ __device__ __forceinline__ void finish(const ProductArgs& P, const Tile& T, int 
             }
         }
     } else {
-        char* user = static_cast<char*>(P.user) + T.b * P.user_batch * dtype_bytes(P.user_dtype);
-        auto put = [&](int64_t at, float x) {
-            x *= 1.f / kScaleX;
-            if (P.weights) x = fmaf(-P.rate, x, P.keep * load_value(user, at, P.user_dtype));
-            store_value(user, at, x, P.user_dtype);
-        };
-        if (P.transposed) {  // lanes are consecutive columns of the caller's matrix
 #pragma unroll
-            for (int k = 0; k < 32; ++k)
-                if (live && col + k < P.n) put(static_cast<int64_t>(col + k) * P.user_row + row, v[k]);
-        } else {  // 32 x 32 values through shared memory, so that they are here too
-            __syncwarp();
-#pragma unroll
-            for (int k = 0; k < 32; ++k) stage[lane][k] = v[k];
-            __syncwarp();
-            const int first = row - lane;
-#pragma unroll 8
-            for (int k = 0; k < 32; ++k)
-                if (first + k < P.m && col + lane < P.n)
-                    put(static_cast<int64_t>(first + k) * P.user_row + col + lane, stage[k][lane]);
+        for (int h = 0; h < 32; h += 16) {
+            if (P.user_dtype == CB_F32) finish_result<CB_F32>(P, batch, row, col + h, v + h, stage, lane);
+            else if (P.user_dtype == CB_BF16) finish_result<CB_BF16>(P, batch, row, col + h, v + h, stage, lane);
+            else finish_result<CB_F16>(P, batch, row, col + h, v + h, stage, lane);
         }
     }
+}
+
+// The epilogue of a tile: a warp's rows row0 .. row0 + 31, every other 32 columns. Those that no
+// row of C has, or that the other triangle gives, are skipped.
+template <Product WHAT>
+__device__ __forceinline__ void finish_tile(const ProductArgs& P, int batch, int row0, int col0, int width, uint32_t tmem,
+                                            uint32_t ready, uint32_t parity, float* stage, int warp, int lane, bool& ok) {
+    const int row = row0 + lane;
+    auto skip = [&](int c) { return c >= width || col0 + c >= P.n || (kSymmetric<WHAT> && (col0 + c) / kTileM > row0 / kTileM); };
+    int c = warp / 4 * 32;
+    Term next{};
+    if (!skip(c)) load_term<WHAT>(P, batch, row, col0 + c, next);
+    ok = __all_sync(kFull, tc::barrier_wait(ready, parity));
+    if (!ok) return;
+    tc::fence_after();
+    for (; !skip(c); c += 64) {
+        const Term term = next;
+        float v[32];
+        tc::tmem_load32(tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16) + c, v);
+        if (!skip(c + 64)) load_term<WHAT>(P, batch, row, col0 + c + 64, next);
+        finish<WHAT>(P, batch, row, col0 + c, v, term, stage, lane);
+    }
+    tc::fence_before();
+    __syncwarp();
 }
 
 // C = A B in tiles of 128 x BN, tile after tile by each block. Operand A is K-major; B is
@@ -469,7 +629,7 @@ muon_product_kernel(const __grid_constant__ CUtensorMap left, const __grid_const
     unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~uintptr_t(1023));
     __shared__ uint64_t full[S], empty[S], ready[2], drained[2];
     __shared__ uint32_t tmem_at;
-    __shared__ float stage[WHAT == kResult ? kEpilogueWarps * 32 : 1][33];
+    __shared__ __align__(16) float stage[WHAT == kResult ? kEpilogueWarps * kStageFloats : 4];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
@@ -484,7 +644,7 @@ muon_product_kernel(const __grid_constant__ CUtensorMap left, const __grid_const
         tc::tma_prefetch(&left);
         tc::tma_prefetch(&right);
     }
-    if (warp == kEpilogueWarps) tc::tmem_alloc(tc::smem_addr(&tmem_at), kColumns);
+    if (warp == kEpilogueWarps) tc::tmem_alloc<1>(tc::smem_addr(&tmem_at), kColumns);
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
@@ -499,7 +659,7 @@ muon_product_kernel(const __grid_constant__ CUtensorMap left, const __grid_const
             int s = 0;
             uint32_t phase = 0;
             for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
-                const Tile T = tile_at<BN, WHAT>(P, t);
+                const Tile T = tile_at<kTileM, WHAT>(P, t);
                 for (int k = 0; k < ksteps; ++k) {
                     if (!(ok = tc::barrier_wait(tc::smem_addr(empty + s), phase ^ 1))) break;
                     const uint32_t bar = tc::smem_addr(full + s);
@@ -541,33 +701,24 @@ muon_product_kernel(const __grid_constant__ CUtensorMap left, const __grid_const
                         const uint64_t da = tc::operand_k_major(at + x * 32);
                         const uint64_t db = kSymmetric<WHAT> ? tc::operand_k_major(bt + x * 32)
                                                             : tc::operand_mn_major(bt + x * 2048, kBoxBytes);
-                        tc::mma_f16(tmem + acc * BN, da, db, shape, k > 0 || x > 0);
+                        tc::mma_f16<1>(tmem + acc * BN, da, db, shape, k > 0 || x > 0);
                     }
-                    tc::mma_commit(tc::smem_addr(empty + s));
+                    tc::mma_commit<1>(tc::smem_addr(empty + s));
                     if (++s == S) s = 0, phase ^= 1;
                 }
-                tc::mma_commit(tc::smem_addr(ready + acc));
+                tc::mma_commit<1>(tc::smem_addr(ready + acc));
                 if (++acc == 2) acc = 0, acc_phase ^= 1;
             }
         }
-    } else {  // epilogue: warp w has the rows 32 w .. 32 w + 31 of the tile
+    } else {  // epilogue
         int acc = 0;
         uint32_t acc_phase = 0;
         for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
-            const Tile T = tile_at<BN, WHAT>(P, t);
-            if (!(ok = __all_sync(kFull, tc::barrier_wait(tc::smem_addr(ready + acc), acc_phase)))) break;
-            tc::fence_after();
-            const int row = T.i * kTileM + warp * 32 + lane;
-            // 32 columns that no row of C has, or that the other triangle gives, are skipped.
-            for (int c = 0; c < BN; c += 32) {
-                const int col = T.j * BN + c;
-                if (col >= P.n || (kSymmetric<WHAT> && col / kTileM > T.i)) break;
-                float v[32];
-                tc::tmem_load32(tmem + (static_cast<uint32_t>(warp * 32) << 16) + acc * BN + c, v);
-                finish<BN, WHAT>(P, T, row, col, v, stage + (WHAT == kResult ? warp * 32 : 0), lane);
-            }
-            tc::fence_before();
-            __syncwarp();
+            const Tile T = tile_at<kTileM, WHAT>(P, t);
+            finish_tile<WHAT>(P, T.b, T.i * kTileM + warp % 4 * 32, T.j * BN, BN, tmem + acc * BN,
+                              tc::smem_addr(ready + acc), acc_phase, stage + (WHAT == kResult ? warp * kStageFloats : 0), warp,
+                              lane, ok);
+            if (!ok) break;
             if (lane == 0) tc::barrier_arrive(tc::smem_addr(drained + acc));
             if (++acc == 2) acc = 0, acc_phase ^= 1;
         }
@@ -577,7 +728,131 @@ muon_product_kernel(const __grid_constant__ CUtensorMap left, const __grid_const
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
-    if (warp == kEpilogueWarps) tc::tmem_free(tmem, kColumns);
+    if (warp == kEpilogueWarps) tc::tmem_free<1>(tmem, kColumns);
+}
+
+// The same in tiles of 256 x P.width by pairs of blocks on two SMs: each block copies and
+// keeps 128 rows of A and half of the columns of B, one thread of the first block issues the
+// products of both, and each block has 128 rows of the sums in its TMEM. A 128 x 128 tile
+// reads and writes 256 bytes of shared memory a clock at the tensor cores' rate, twice what
+// an SM has; a pair's 256 x 256 tile 128 bytes. P.width is a multiple of 32 (a block's
+// half of the columns, of 16; 128 are copied) so that a few rounds of tiles can be made to
+// fill the GPU. Operands that are K-major come in boxes of 128 rows, fewer copies than of 64.
+constexpr int kPairM = 256, kPairWidth = 256, kPairStages = 6;
+constexpr uint32_t kPairStageBytes = (128 + kPairWidth / 2) * kTileK * 2;
+
+template <Product WHAT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
+muon_pair_kernel(const __grid_constant__ CUtensorMap left, const __grid_constant__ CUtensorMap right,
+                 const ProductArgs P) {
+    constexpr int S = kPairStages;
+    constexpr uint32_t kColumns = 2 * kPairWidth;
+    extern __shared__ unsigned char dynamic[];
+    unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~uintptr_t(1023));
+    // full, drained: those of the first block count for both; empty, ready: each block's own.
+    __shared__ uint64_t full[S], empty[S], ready[2], drained[2];
+    __shared__ uint32_t tmem_at;
+    __shared__ __align__(16) float stage[WHAT == kResult ? kEpilogueWarps * kStageFloats : 4];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = static_cast<int>(tc::cluster_rank());
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S; ++s) {
+            tc::barrier_init(tc::smem_addr(full + s), 1);
+            tc::barrier_init(tc::smem_addr(empty + s), 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            tc::barrier_init(tc::smem_addr(ready + s), 1);
+            tc::barrier_init(tc::smem_addr(drained + s), 2 * kEpilogueWarps);
+        }
+        tc::barrier_init_fence();
+        tc::tma_prefetch(&left);
+        tc::tma_prefetch(&right);
+    }
+    if (warp == kEpilogueWarps) tc::tmem_alloc<2>(tc::smem_addr(&tmem_at), kColumns);
+    tc::fence_before();
+    tc::cluster_sync();
+    tc::fence_after();
+    const uint32_t tmem = tmem_at;
+    begin_kernel();
+    const int64_t total = P.tiles * P.batch;
+    const int64_t first = blockIdx.x / 2, step = gridDim.x / 2;
+    const int ksteps = (P.k + kTileK - 1) / kTileK, half = P.width / 2;
+    bool ok = true;
+
+    if (warp == kEpilogueWarps) {
+        if (lane == 0) {  // copies
+            int s = 0;
+            uint32_t phase = 0;
+            for (int64_t t = first; t < total && ok; t += step) {
+                const Tile T = tile_at<kPairM, WHAT>(P, t);
+                const int row = T.i * kPairM + rank * 128, col = T.j * P.width + rank * half;
+                for (int k = 0; k < ksteps; ++k) {
+                    if (!(ok = tc::barrier_wait(tc::smem_addr(empty + s), phase ^ 1))) break;
+                    const uint32_t bar = tc::in_first_block(tc::smem_addr(full + s));
+                    uint32_t at = tc::smem_addr(ring) + s * kPairStageBytes;
+                    if (rank == 0) tc::barrier_expect(tc::smem_addr(full + s), 2 * kPairStageBytes);
+                    tc::tma_load_pair(at, &left, bar, k * kTileK, row, T.b);
+                    at += 2 * kBoxBytes;
+                    if constexpr (kSymmetric<WHAT>) {
+                        tc::tma_load_pair(at, &right, bar, k * kTileK, col, T.b);
+                    } else {
+                        tc::tma_load_pair(at, &right, bar, col, k * kTileK, T.b);
+                        tc::tma_load_pair(at + kBoxBytes, &right, bar, col + 64, k * kTileK, T.b);
+                    }
+                    if (++s == S) s = 0, phase ^= 1;
+                }
+            }
+            if (!ok && rank == 0)  // copies in flight land before the blocks' shared memory goes away
+                for (int x = 0; x < S; ++x) {
+                    if (--s < 0) s = S - 1, phase ^= 1;
+                    if (!tc::barrier_wait(tc::smem_addr(full + s), phase)) break;
+                }
+        }
+    } else if (warp == kEpilogueWarps + 1) {
+        if (lane == 0 && rank == 0) {  // products of both blocks
+            const uint32_t shape = tc::mma_shape(kPairM, P.width, !kSymmetric<WHAT>);
+            int s = 0, acc = 0;
+            uint32_t phase = 0, acc_phase = 0;
+            for (int64_t t = first; t < total && ok; t += step) {
+                if (!(ok = tc::barrier_wait(tc::smem_addr(drained + acc), acc_phase ^ 1))) break;
+                tc::fence_after();
+                for (int k = 0; k < ksteps; ++k) {
+                    if (!(ok = tc::barrier_wait(tc::smem_addr(full + s), phase))) break;
+                    tc::fence_after();
+                    const uint32_t at = tc::smem_addr(ring) + s * kPairStageBytes, bt = at + 2 * kBoxBytes;
+#pragma unroll
+                    for (int x = 0; x < kTileK / 16; ++x) {
+                        const uint64_t da = tc::operand_k_major(at + x * 32);
+                        const uint64_t db = kSymmetric<WHAT> ? tc::operand_k_major(bt + x * 32)
+                                                             : tc::operand_mn_major(bt + x * 2048, kBoxBytes);
+                        tc::mma_f16<2>(tmem + acc * kPairWidth, da, db, shape, k > 0 || x > 0);
+                    }
+                    tc::mma_commit<2>(tc::smem_addr(empty + s));
+                    if (++s == S) s = 0, phase ^= 1;
+                }
+                tc::mma_commit<2>(tc::smem_addr(ready + acc));
+                if (++acc == 2) acc = 0, acc_phase ^= 1;
+            }
+        }
+    } else {  // epilogue
+        int acc = 0;
+        uint32_t acc_phase = 0;
+        for (int64_t t = first; t < total && ok; t += step) {
+            const Tile T = tile_at<kPairM, WHAT>(P, t);
+            finish_tile<WHAT>(P, T.b, T.i * kPairM + rank * 128 + warp % 4 * 32, T.j * P.width, P.width,
+                              tmem + acc * kPairWidth, tc::smem_addr(ready + acc), acc_phase,
+                              stage + (WHAT == kResult ? warp * kStageFloats : 0), warp, lane, ok);
+            if (!ok) break;
+            if (lane == 0) tc::barrier_arrive_cluster(tc::in_first_block(tc::smem_addr(drained + acc)));
+            if (++acc == 2) acc = 0, acc_phase ^= 1;
+        }
+    }
+    if (!ok && lane == 0) set_error(P.error, CB_ERR_TIMEOUT);
+    __syncwarp();
+    tc::fence_before();
+    tc::cluster_sync();  // neither block ends while the other may signal its barriers
+    tc::fence_after();
+    if (warp == kEpilogueWarps) tc::tmem_free<2>(tmem, kColumns);
 }
 
 // ---------------------------------------------------------------- host
@@ -596,13 +871,14 @@ PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
     return encode;
 }
 
-// [batch][rows][cols] of fp16 with rows of `ld` values, in boxes of 64 x 64; values past
-// a row or past the rows read as zeros.
-bool tensor_map(CUtensorMap* map, const void* data, int64_t cols, int64_t rows, int64_t batch, int64_t ld) {
+// [batch][rows][cols] of fp16 with rows of `ld` values, in boxes of 64 values of box_rows rows;
+// values past a row or past the rows read as zeros.
+bool tensor_map(CUtensorMap* map, const void* data, int64_t cols, int64_t rows, int64_t batch, int64_t ld,
+                uint32_t box_rows) {
     const cuuint64_t dims[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows),
                                 static_cast<cuuint64_t>(batch)};
     const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, static_cast<cuuint64_t>(ld) * rows * 2};
-    const cuuint32_t box[3] = {64, 64, 1};
+    const cuuint32_t box[3] = {64, box_rows, 1};
     const cuuint32_t step[3] = {1, 1, 1};
     return tensor_map_encoder()(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(data), dims, strides, box,
                                 step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
@@ -634,7 +910,7 @@ Workspace layout(int32_t batch, int32_t rows, int32_t cols) {
     w.lo[1] = take(x);
     w.gram = take(a);
     w.poly = take(a);
-    w.partial = take(static_cast<int64_t>(batch) * kNormBlocks * 3 * 4);
+    w.partial = take(static_cast<int64_t>(batch) * kNormBlocks * static_cast<int64_t>(sizeof(SquareSum)));
     w.error = take(4);
     w.bytes = at;
     return w;
@@ -649,41 +925,75 @@ bool current_sms(int* sms) {
     return false;
 }
 
-template <int BN, Product WHAT>
-int64_t tiles_of(int32_t m, int32_t n) {
-    const int row_tiles = (m + kTileM - 1) / kTileM, col_tiles = (n + BN - 1) / BN;
+template <Product WHAT>
+int64_t tiles_of(int32_t m, int32_t n, int height, int width) {
+    const int row_tiles = (m + height - 1) / height, col_tiles = (n + width - 1) / width;
     if (!kSymmetric<WHAT>) return static_cast<int64_t>(row_tiles) * col_tiles;
     int64_t t = 0;
-    for (int i = 0; i < row_tiles; ++i) t += lower_tiles<BN>(i, col_tiles);
+    for (int i = 0; i < row_tiles; ++i) t += lower_tiles(i, height, width, col_tiles);
     return t;
+}
+template <Product WHAT>
+void set_tiles(ProductArgs& P, int height, int width) {
+    P.row_tiles = (P.m + height - 1) / height;
+    P.col_tiles = (P.n + width - 1) / width;
+    P.width = width;
+    P.tiles = tiles_of<WHAT>(P.m, P.n, height, width);
+}
+template <class KernelT>
+bool shared_memory(KernelT kernel, size_t bytes) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)) == cudaSuccess;
 }
 
 template <int BN, Product WHAT>
 bool launch_product(const CUtensorMap& left, const CUtensorMap& right, ProductArgs P, int sms, cudaStream_t s) {
-    P.row_tiles = (P.m + kTileM - 1) / kTileM;
-    P.col_tiles = (P.n + BN - 1) / BN;
-    P.tiles = tiles_of<BN, WHAT>(P.m, P.n);
-    const int64_t total = P.tiles * P.batch;
-    const size_t smem = kStages<BN> * kStageBytes<BN> + 1024;
-    if (cudaFuncSetAttribute(muon_product_kernel<BN, WHAT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             static_cast<int>(smem)) != cudaSuccess)
-        return false;
-    launch(muon_product_kernel<BN, WHAT>, dim3(static_cast<unsigned>(min64(total, sms))), dim3(kProductThreads), smem, s,
-           left, right, P);
+    set_tiles<WHAT>(P, kTileM, BN);
+    constexpr size_t smem = kStages<BN> * kStageBytes<BN> + 1024;
+    static const bool ready = shared_memory(muon_product_kernel<BN, WHAT>, smem);
+    if (!ready) return false;
+    launch(muon_product_kernel<BN, WHAT>, dim3(static_cast<unsigned>(min64(P.tiles * P.batch, sms))),
+           dim3(kProductThreads), smem, s, left, right, P);
+    return true;
+}
+template <Product WHAT>
+bool launch_pairs(const CUtensorMap& left, const CUtensorMap& right, ProductArgs P, int width, int sms, cudaStream_t s) {
+    set_tiles<WHAT>(P, kPairM, width);
+    constexpr size_t smem = kPairStages * kPairStageBytes + 1024;
+    static const bool ready = shared_memory(muon_pair_kernel<WHAT>, smem);
+    if (!ready) return false;
+    launch(muon_pair_kernel<WHAT>, dim3(static_cast<unsigned>(2 * min64(P.tiles * P.batch, sms / 2))),
+           dim3(kProductThreads), smem, s, left, right, P);
     return true;
 }
 
-// The tile width with the least time: rounds of tiles over the GPU, each as long as a
-// tile's products (an SM's shared memory feeds narrow tiles below the tensor cores'
-// rate) and what a tile costs besides.
+// A matrix of the workspace as an operand, by the boxes that a kernel copies.
+struct Operand {
+    CUtensorMap box64, box128;
+    bool set(const void* data, int64_t cols, int64_t rows, int64_t batch, int64_t ld) {
+        return tensor_map(&box64, data, cols, rows, batch, ld, 64) && tensor_map(&box128, data, cols, rows, batch, ld, 128);
+    }
+};
+
+// The tiles with the least time, in clocks: rounds of tiles over the GPU, the time that 64 of K
+// take a tile, and what a kernel takes besides.
 template <Product WHAT>
-bool launch_best(const CUtensorMap& left, const CUtensorMap& right, const ProductArgs& P, int sms, cudaStream_t s) {
-    auto rounds = [&](int64_t tiles) { return (tiles * P.batch + sms - 1) / sms; };
-    const int64_t t64 = rounds(tiles_of<64, WHAT>(P.m, P.n)) * 96, t128 = rounds(tiles_of<128, WHAT>(P.m, P.n)) * 144,
-                  t256 = rounds(tiles_of<256, WHAT>(P.m, P.n)) * 264;
-    if (t256 <= t128 && t256 <= t64) return launch_product<256, WHAT>(left, right, P, sms, s);
-    if (t128 <= t64) return launch_product<128, WHAT>(left, right, P, sms, s);
-    return launch_product<64, WHAT>(left, right, P, sms, s);
+bool launch_best(const Operand& left, const Operand& right, const ProductArgs& P, int sms, cudaStream_t s) {
+    const int64_t ksteps = (P.k + kTileK - 1) / kTileK;
+    auto time = [&](int height, int width, int at_once, int64_t step) {
+        return (tiles_of<WHAT>(P.m, P.n, height, width) * P.batch + at_once - 1) / at_once * ksteps * step;
+    };
+    int64_t best = time(kTileM, 64, sms, CB_STEP64);
+    int width = 64;
+    const int64_t t128 = time(kTileM, 128, sms, CB_STEP128);
+    if (t128 < best) best = t128, width = 128;
+    bool pair = false;
+    for (int w = 160; w <= kPairWidth; w += 32) {
+        const int64_t t = time(kPairM, w, sms / 2, 290 + 11 * w / 8) + CB_PAIRX;
+        if (t < best) best = t, width = w, pair = true;
+    }
+    if (pair) return launch_pairs<WHAT>(left.box128, kSymmetric<WHAT> ? right.box128 : right.box64, P, width, sms, s);
+    if (width == 128) return launch_product<128, WHAT>(left.box64, right.box64, P, sms, s);
+    return launch_product<64, WHAT>(left.box64, right.box64, P, sms, s);
 }
 
 bool valid_dtype(int d) { return d == CB_F32 || d == CB_F16 || d == CB_BF16; }
@@ -725,16 +1035,18 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
     __half* lo[2] = {reinterpret_cast<__half*>(base + w.lo[0]), reinterpret_cast<__half*>(base + w.lo[1])};
     __half* gram = reinterpret_cast<__half*>(base + w.gram);
     __half* poly = reinterpret_cast<__half*>(base + w.poly);
-    float* partial = reinterpret_cast<float*>(base + w.partial);
+    SquareSum* partial = reinterpret_cast<SquareSum*>(base + w.partial);
     if (!error) error = reinterpret_cast<int*>(base + w.error);  // any value: read by nobody
     const bool tall = in.rows > in.cols;
 
-    CUtensorMap map_x[2], map_gram, map_poly;
-    if (!tensor_map(&map_x[0], hi[0], w.q, w.p, batch, w.ldx) || !tensor_map(&map_x[1], hi[1], w.q, w.p, batch, w.ldx) ||
-        !tensor_map(&map_gram, gram, w.p, w.p, batch, w.lda) || !tensor_map(&map_poly, poly, w.p, w.p, batch, w.lda))
+    Operand op_x[2], op_gram, op_poly;
+    if (!op_x[0].set(hi[0], w.q, w.p, batch, w.ldx) || !op_x[1].set(hi[1], w.q, w.p, batch, w.ldx) ||
+        !op_gram.set(gram, w.p, w.p, batch, w.lda) || !op_poly.set(poly, w.p, w.p, batch, w.lda))
         return CB_ERR_CUDA;
 
-    const int norm_blocks = static_cast<int>(max64(1, min64(kNormBlocks, (matrix + 8 * 1024 - 1) / (8 * 1024))));
+    // 4096 values a block, on up to 8 blocks per SM in all.
+    const int norm_blocks = static_cast<int>(
+        max64(1, min64(min64(kNormBlocks, 8 * sms / batch), (matrix + 4 * 1024 - 1) / (4 * 1024))));
     const bool vector = in.cols % 4 == 0 && in.g_row % 4 == 0 && (batch == 1 || in.g_batch % 4 == 0) &&
                         aligned(in.g, 4 * dtype_bytes(in.dtype)) &&
                         (!in.momentum || (in.m_row % 4 == 0 && (batch == 1 || in.m_batch % 4 == 0) &&
@@ -745,8 +1057,10 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
     const dim3 cast_grid((in.cols + kCastTile - 1) / kCastTile, (in.rows + kCastTile - 1) / kCastTile, batch);
     const int64_t x_batch = w.p * w.ldx, a_batch = w.p * w.lda;
     const int ldx = static_cast<int>(w.ldx), lda = static_cast<int>(w.lda);
-    if (tall) launch(muon_cast_kernel<true>, cast_grid, dim3(256), 0, s, in, partial, norm_blocks, eps, hi[0], lo[0], ldx, x_batch);
-    else launch(muon_cast_kernel<false>, cast_grid, dim3(256), 0, s, in, partial, norm_blocks, eps, hi[0], lo[0], ldx, x_batch);
+    auto cast = tall ? (vector ? muon_cast_kernel<true, 4> : muon_cast_kernel<true, 1>)
+                     : (vector ? muon_cast_kernel<false, 4> : muon_cast_kernel<false, 1>);
+    launch(cast, cast_grid, dim3(256), 0, s, in, static_cast<const SquareSum*>(partial), norm_blocks, eps, hi[0], lo[0], ldx,
+           x_batch);
 
     bool sent = true;
     for (int k = 0; k < steps; ++k) {
@@ -761,7 +1075,7 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
         P.out_hi = gram;
         P.out_batch = a_batch;
         P.out_ld = lda;
-        sent &= launch_best<kGram>(map_x[now], map_x[now], P, sms, s);
+        sent &= launch_best<kGram>(op_x[now], op_x[now], P, sms, s);
         P.k = P.m;
         P.a = two_term ? 0.f : a;
         P.b = b;
@@ -770,7 +1084,7 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
         P.term_batch = a_batch;
         P.term_ld = lda;
         P.out_hi = poly;
-        sent &= launch_best<kPoly>(map_gram, map_gram, P, sms, s);
+        sent &= launch_best<kPoly>(op_gram, op_gram, P, sms, s);
         P.n = static_cast<int32_t>(w.q);
         P.a = two_term ? a : 0.f;
         P.term_hi = hi[now];
@@ -782,17 +1096,19 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
         P.out_batch = x_batch;
         P.out_ld = ldx;
         if (k + 1 < steps) {
-            sent &= launch_best<kUpdate>(map_poly, map_x[now], P, sms, s);
+            sent &= launch_best<kUpdate>(op_poly, op_x[now], P, sms, s);
         } else {
             P.user = out.data;
             P.user_batch = out.batch_stride;
             P.user_row = out.row_stride;
             P.user_dtype = out.dtype;
             P.transposed = tall;
+            P.user_vector = in.cols % 4 == 0 && out.row_stride % 4 == 0 && (batch == 1 || out.batch_stride % 4 == 0) &&
+                            aligned(out.data, 4 * dtype_bytes(out.dtype));
             P.weights = out.weights;
             P.keep = out.keep;
             P.rate = out.rate;
-            sent &= launch_best<kResult>(map_poly, map_x[now], P, sms, s);
+            sent &= launch_best<kResult>(op_poly, op_x[now], P, sms, s);
         }
     }
     return cudaGetLastError() == cudaSuccess && sent ? CB_OK : CB_ERR_CUDA;

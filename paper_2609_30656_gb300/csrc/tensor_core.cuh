@@ -62,14 +62,26 @@ __device__ __forceinline__ void tma_prefetch(const CUtensorMap* map) {
 
 // ---------------------------------------------------------------- TMEM
 
-// A whole warp; the first column's address arrives in shared memory at `dst`.
+// A whole warp (of each block of a pair: GROUP = 2); the first column's address arrives in
+// shared memory at `dst`.
+template <int GROUP>
 __device__ __forceinline__ void tmem_alloc(uint32_t dst, uint32_t columns) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(columns)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    if constexpr (GROUP == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(columns)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(columns)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
 }
+template <int GROUP>
 __device__ __forceinline__ void tmem_free(uint32_t tmem, uint32_t columns) {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns));
+    if constexpr (GROUP == 1)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns));
+    else
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns));
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -117,17 +129,69 @@ __host__ __device__ constexpr uint32_t mma_shape(int m, int n, bool b_mn_major) 
     return 1u << 4 | (b_mn_major ? 1u << 16 : 0u) | static_cast<uint32_t>(n >> 3) << 17 |
            static_cast<uint32_t>(m >> 4) << 24;
 }
-// One thread: D (+)= A B over 16 values of K.
+// One thread (of the first block of a pair): D (+)= A B over 16 values of K. A pair takes M = 256
+// with 128 rows of A, 128 rows of D and half of the columns of B in each block.
+template <int GROUP>
 __device__ __forceinline__ void mma_f16(uint32_t tmem, uint64_t a, uint64_t b, uint32_t shape, bool add) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem),
-        "l"(a), "l"(b), "r"(shape), "r"(static_cast<uint32_t>(add))
-        : "memory");
+    if constexpr (GROUP == 1)
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem),
+            "l"(a), "l"(b), "r"(shape), "r"(static_cast<uint32_t>(add))
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+            "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem),
+            "l"(a), "l"(b), "r"(shape), "r"(static_cast<uint32_t>(add))
+            : "memory");
 }
-// `bar` gets one arrival when the thread's products so far are done.
+// `bar` (of both blocks of a pair) gets one arrival when the thread's products so far are done.
+template <int GROUP>
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    if constexpr (GROUP == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
+                     : "memory");
+    else
+        asm volatile(
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                bar),
+            "h"(static_cast<uint16_t>(3))
+            : "memory");
+}
+
+// ---------------------------------------------------------------- pairs of blocks
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// Every thread of both blocks.
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+}
+// The same shared-memory place in the first block of the cluster.
+__device__ __forceinline__ uint32_t in_first_block(uint32_t addr) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+    return r;
+}
+// What a block's waits on the other's arrivals order is TMEM (by the tcgen05 fences around them)
+// and shared memory that the tensor core and TMA alone touch, so the default scope will do: a
+// wait that acquires from the cluster takes hundreds of clocks, once for every tile of K.
+__device__ __forceinline__ void barrier_arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// A tile into this block's shared memory, its bytes counted by a barrier of the pair's first block.
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int32_t x, int32_t y,
+                                              int32_t z) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "r"(z)
+        : "memory");
 }
 
 }  // namespace tc
