@@ -35,15 +35,6 @@
 #include <cmath>
 #include <cudaTypedefs.h>
 
-#ifndef CB_STEP64
-#define CB_STEP64 450
-#endif
-#ifndef CB_STEP128
-#define CB_STEP128 700
-#endif
-#ifndef CB_PAIRX
-#define CB_PAIRX 3000
-#endif
 namespace cbtbe {
 namespace {
 
@@ -77,6 +68,23 @@ struct SquareSum {
             const float p = x * x;
             rest += fmaf(x, x, -p);
             add_mid(p);
+        }
+    }
+    template <int N>
+    __device__ __forceinline__ void add(const float (&x)[N]) {  // the usual magnitudes without a branch for each
+        bool usual = true;
+#pragma unroll
+        for (int k = 0; k < N; ++k) usual &= x[k] == 0.f || (fabsf(x[k]) >= 0x1p-40f && fabsf(x[k]) < 0x1p40f);
+        if (usual) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const float p = x[k] * x[k];
+                rest += fmaf(x[k], x[k], -p);
+                add_mid(p);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) add(x[k]);
         }
     }
     __device__ __forceinline__ void add(const SquareSum& o) {
@@ -140,11 +148,22 @@ __device__ __forceinline__ void store_values4(void* p, int64_t i, const float (&
     }
 }
 
-// V consecutive values (V = 1, or 4 with their alignment).
+// V consecutive values (V = 1, or 4 or 8 with the alignment of 16 bytes or of all of them).
 template <int V>
 __device__ __forceinline__ void load_values(const void* p, int64_t i, int dtype, float (&v)[V]) {
     if constexpr (V == 1) {
         v[0] = load_value(p, i, dtype);
+    } else if constexpr (V == 8) {
+        if (dtype == CB_F32) {
+            const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
+            const float4 x = q[0], y = q[1];
+            v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+            v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+        } else {
+            const uint4 x = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i);
+            if (dtype == CB_BF16) unpack<CB_BF16>(x, v);
+            else unpack<CB_F16>(x, v);
+        }
     } else if (dtype == CB_F32) {
         const float4 x = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
         v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
@@ -167,10 +186,15 @@ __device__ __forceinline__ void load_values(const void* p, int64_t i, int dtype,
     }
 }
 
-constexpr int kNormThreads = 256;
-constexpr int kNormBlocks = 1024;  // most blocks (and partial sums) per matrix
-
 __host__ __device__ __forceinline__ float mix_momentum(float m, float g, float beta) { return fmaf(beta, m, g); }
+// m <- beta m + g, and the update from it.
+__device__ __forceinline__ float update_value(const MatrixIn& in, float g, float& m) {
+    m = mix_momentum(m, g, in.beta);
+    return in.nesterov ? mix_momentum(m, g, in.beta) : m;
+}
+
+constexpr int kNormThreads = 512;
+constexpr int kNormBlocks = 304;  // most blocks (and partial sums) per matrix
 
 // m <- beta m + g in place, and a block's part of the squares of the update u
 // (g; m; or g + beta m). Blocks (x of a matrix, matrix).
@@ -189,7 +213,7 @@ __global__ void __launch_bounds__(kNormThreads) muon_norm_kernel(MatrixIn in, Sq
     int col = static_cast<int>(i - row * vecs);
     const int64_t drow = step / vecs;
     const int dcol = static_cast<int>(step - drow * vecs);
-    constexpr int U = 4;  // vectors in flight
+    constexpr int U = V == 8 ? 2 : 4;  // vectors in flight
     while (i < total) {
         float v[U][V], m[U][V];
         int64_t at_m[U];
@@ -215,17 +239,17 @@ __global__ void __launch_bounds__(kNormThreads) muon_norm_kernel(MatrixIn in, Sq
             if (u < live) {
                 if (mom) {
 #pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        m[u][k] = mix_momentum(m[u][k], v[u][k], in.beta);
-                        v[u][k] = in.nesterov ? mix_momentum(m[u][k], v[u][k], in.beta) : m[u][k];
-                    }
-                    if constexpr (V == 4)
-                        *reinterpret_cast<float4*>(mom + at_m[u]) = make_float4(m[u][0], m[u][1], m[u][2], m[u][3]);
-                    else
+                    for (int k = 0; k < V; ++k) v[u][k] = update_value(in, v[u][k], m[u][k]);
+                    if constexpr (V == 1) {
                         mom[at_m[u]] = m[u][0];
-                }
+                    } else {
 #pragma unroll
-                for (int k = 0; k < V; ++k) s.add(v[u][k]);
+                        for (int k = 0; k < V; k += 4)
+                            *reinterpret_cast<float4*>(mom + at_m[u] + k) =
+                                make_float4(m[u][k], m[u][k + 1], m[u][k + 2], m[u][k + 3]);
+                    }
+                }
+                s.add(v[u]);
             }
         }
     }
@@ -242,9 +266,22 @@ __global__ void __launch_bounds__(kNormThreads) muon_norm_kernel(MatrixIn in, Sq
 }
 
 // kScaleX / (norm + eps) as a product of two floats, so that neither a huge nor a tiny
-// norm takes it out of range; from the partial sums of one matrix, by a block of 256 threads.
-// One thread finishes it, in fp64 only where fp32's range asks for it (every block of a large
-// matrix does this, and fp64 is slow: 140 us for 4096 x 4096 when all threads did).
+// norm takes it out of range; in fp64 only where fp32's range asks for it.
+__device__ __forceinline__ float2 inverse_norm(const SquareSum& t, float eps) {
+    const float mid = t.mid + t.rest;
+    if (t.big == 0.f && mid >= 0x1p-60f)  // the small class is below fp32's precision then
+        return make_float2(1.f, kScaleX / (sqrtf(mid) + eps));
+    const double norm = sqrt(static_cast<double>(mid) + static_cast<double>(t.big) * 0x1p160 +
+                             static_cast<double>(t.small) * 0x1p-160) + static_cast<double>(eps);
+    // A matrix of zeros with eps = 0 stays zeros.
+    const double inv = norm == 0.0 ? 0.0 : static_cast<double>(kScaleX) / norm;
+    int e = 0;
+    const double mant = frexp(inv, &e);
+    const int half = e / 2;
+    return make_float2(static_cast<float>(ldexp(1.0, half)), static_cast<float>(ldexp(mant, e - half)));
+}
+// The same from the partial sums of one matrix, by a block of 256 threads. One thread finishes
+// it (every block of a large matrix does this; 140 us for 4096 x 4096 when all threads did).
 __device__ __forceinline__ float2 inverse_norm(const SquareSum* partial, int blocks, float eps) {
     __shared__ __align__(16) unsigned char raw[8 * sizeof(SquareSum)];
     SquareSum* sh = reinterpret_cast<SquareSum*>(raw);
@@ -257,19 +294,7 @@ __device__ __forceinline__ float2 inverse_norm(const SquareSum* partial, int blo
     if (threadIdx.x == 0) {
 #pragma unroll
         for (int w = 1; w < 8; ++w) t.add(sh[w]);
-        const float mid = t.mid + t.rest;
-        if (t.big == 0.f && mid >= 0x1p-60f) {  // the small class is below fp32's precision then
-            result = make_float2(1.f, kScaleX / (sqrtf(mid) + eps));
-        } else {
-            const double norm = sqrt(static_cast<double>(mid) + static_cast<double>(t.big) * 0x1p160 +
-                                     static_cast<double>(t.small) * 0x1p-160) + static_cast<double>(eps);
-            // A matrix of zeros with eps = 0 stays zeros.
-            const double inv = norm == 0.0 ? 0.0 : static_cast<double>(kScaleX) / norm;
-            int e = 0;
-            const double mant = frexp(inv, &e);
-            const int half = e / 2;
-            result = make_float2(static_cast<float>(ldexp(1.0, half)), static_cast<float>(ldexp(mant, e - half)));
-        }
+        result = inverse_norm(t, eps);
     }
     __syncthreads();
     return result;
@@ -281,76 +306,85 @@ constexpr int kCastTile = 64;
 
 // X_0 = kScaleX u / (||u|| + eps) as hi + lo, [p, ld] rows: u as it lies, or transposed.
 // A block takes a 64 x 64 tile of u, a thread four times 4 consecutive values of it (V = 4: in
-// one load each) and of X: blocks (column tile, row tile, matrix). Rows of X are padded to 64
-// values, so its tiles are stored whole along a row.
+// one load each) and of X, one row of tiles after another: blocks (column tile, first row tile,
+// matrix). Rows of X are padded to 64 values, so its tiles are stored whole along a row.
 template <bool TRANSPOSED, int V>
-__global__ void __launch_bounds__(256) muon_cast_kernel(MatrixIn in, const SquareSum* __restrict__ partial, int norm_blocks,
+__global__ void __launch_bounds__(256, 4) muon_cast_kernel(MatrixIn in, const SquareSum* __restrict__ partial, int norm_blocks,
                                                         float eps, __half* __restrict__ hi, __half* __restrict__ lo,
                                                         int ld, int64_t x_batch) {
     __shared__ float tile[TRANSPOSED ? kCastTile : 1][kCastTile + 1];
     begin_kernel();
-    const int b = blockIdx.z;
-    const int r0 = blockIdx.y * kCastTile, c0 = blockIdx.x * kCastTile;
+    const int b = blockIdx.z, c0 = blockIdx.x * kCastTile;
     const char* g = static_cast<const char*>(in.g) + b * in.g_batch * dtype_bytes(in.dtype);
     const float* mom = in.momentum ? in.momentum + b * in.m_batch : nullptr;
     const int c = (threadIdx.x & 15) * 4, rq = threadIdx.x >> 4;
-    float v[4][4], m[4][4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int64_t row = r0 + rq + 16 * k;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[k][e] = m[k][e] = 0.f;
-        if (row >= in.rows) continue;
-        if constexpr (V == 4) {
-            if (c0 + c < in.cols) {
-                load_values<4>(g, row * in.g_row + c0 + c, in.dtype, v[k]);
-                if (mom) load_values<4>(mom, row * in.m_row + c0 + c, CB_F32, m[k]);
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (c0 + c + e < in.cols) {
-                    v[k][e] = load_value(g, row * in.g_row + c0 + c + e, in.dtype);
-                    if (mom) m[k][e] = mom[row * in.m_row + c0 + c + e];
-                }
-        }
-    }
-    const float2 f = inverse_norm(partial + static_cast<int64_t>(b) * kNormBlocks, norm_blocks, eps);
-    auto put = [&](int64_t at, const float (&x)[4]) {
-        uint32_t h[2], l[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const __half2 top = __floats2half2_rn(x[2 * e], x[2 * e + 1]);
-            const float2 back = __half22float2(top);
-            const __half2 rest = __floats2half2_rn(x[2 * e] - back.x, x[2 * e + 1] - back.y);
-            memcpy(&h[e], &top, 4);
-            memcpy(&l[e], &rest, 4);
-        }
-        *reinterpret_cast<uint2*>(hi + at) = make_uint2(h[0], h[1]);
-        *reinterpret_cast<uint2*>(lo + at) = make_uint2(l[0], l[1]);
-    };
-    const int64_t base = b * x_batch;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int row = r0 + rq + 16 * k;
-        float x[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float u = !mom ? v[k][e] : (in.nesterov ? mix_momentum(m[k][e], v[k][e], in.beta) : m[k][e]);
-            x[e] = (u * f.x) * f.y;
-            if constexpr (TRANSPOSED) tile[rq + 16 * k][c + e] = x[e];
-        }
-        if (!TRANSPOSED && row < in.rows) put(base + static_cast<int64_t>(row) * ld + c0 + c, x);
-    }
-    if constexpr (TRANSPOSED) {
-        __syncthreads();
+    float2 f = make_float2(0.f, 0.f);
+    for (int r0 = blockIdx.y * kCastTile; r0 < in.rows; r0 += gridDim.y * kCastTile) {
+        float v[4][4], m[4][4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int col = c0 + rq + 16 * k;  // value (row, col) of u is X[col, row]
+            const int64_t row = r0 + rq + 16 * k;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[k][e] = m[k][e] = 0.f;
+            if (row >= in.rows) continue;
+            if constexpr (V == 4) {
+                if (c0 + c < in.cols) {
+                    load_values<4>(g, row * in.g_row + c0 + c, in.dtype, v[k]);
+                    if (mom) load_values<4>(mom, row * in.m_row + c0 + c, CB_F32, m[k]);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c0 + c + e < in.cols) {
+                        v[k][e] = load_value(g, row * in.g_row + c0 + c + e, in.dtype);
+                        if (mom) m[k][e] = mom[row * in.m_row + c0 + c + e];
+                    }
+            }
+        }
+        if (mom) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[k][e] = in.nesterov ? mix_momentum(m[k][e], v[k][e], in.beta) : m[k][e];
+        }
+        if (r0 == static_cast<int>(blockIdx.y) * kCastTile)  // behind the first tile's loads
+            f = inverse_norm(partial + static_cast<int64_t>(b) * kNormBlocks, norm_blocks, eps);
+        auto put = [&](int64_t at, const float (&x)[4]) {
+            uint32_t h[2], l[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const __half2 top = __floats2half2_rn(x[2 * e], x[2 * e + 1]);
+                const float2 back = __half22float2(top);
+                const __half2 rest = __floats2half2_rn(x[2 * e] - back.x, x[2 * e + 1] - back.y);
+                memcpy(&h[e], &top, 4);
+                memcpy(&l[e], &rest, 4);
+            }
+            *reinterpret_cast<uint2*>(hi + at) = make_uint2(h[0], h[1]);
+            *reinterpret_cast<uint2*>(lo + at) = make_uint2(l[0], l[1]);
+        };
+        const int64_t base = b * x_batch;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int row = r0 + rq + 16 * k;
             float x[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = tile[c + e][rq + 16 * k];
-            if (col < in.cols) put(base + static_cast<int64_t>(col) * ld + r0 + c, x);
+            for (int e = 0; e < 4; ++e) {
+                x[e] = (v[k][e] * f.x) * f.y;
+                if constexpr (TRANSPOSED) tile[rq + 16 * k][c + e] = x[e];
+            }
+            if (!TRANSPOSED && row < in.rows) put(base + static_cast<int64_t>(row) * ld + c0 + c, x);
+        }
+        if constexpr (TRANSPOSED) {
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int col = c0 + rq + 16 * k;  // value (row, col) of u is X[col, row]
+                float x[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = tile[c + e][rq + 16 * k];
+                if (col < in.cols) put(base + static_cast<int64_t>(col) * ld + r0 + c, x);
+            }
+            __syncthreads();
         }
     }
 }
@@ -855,6 +889,320 @@ muon_pair_kernel(const __grid_constant__ CUtensorMap left, const __grid_constant
     if (warp == kEpilogueWarps) tc::tmem_free<2>(tmem, kColumns);
 }
 
+// ---------------------------------------------------------------- small matrices in one launch
+
+// Up to 128 x 2048: all steps of a matrix in one kernel, by a cluster of blocks that each keep
+// up to 256 columns of X in shared memory (fp16, for the products) and in TMEM (fp32, a X as
+// the sums that B X is added to). The Gram matrix of the blocks' columns is added up
+// across the cluster, in a fixed order, a share of its rows in each block; A A and B are
+// taken by every block for itself. What is left of a step is a chain of three products
+// of half a microsecond and their epilogues, in which a thread of TN / 128 has 32 columns of
+// its row at a time: 512 threads a block (128 x 256, five steps: 34 us, 42 with 256), or 256 of
+// two blocks per SM where narrow matrices would otherwise queue (300 of 128 x 128: 34 us, 47).
+constexpr int kSmallRows = 128, kSmallCols = 256, kSmallCluster = 8;
+constexpr uint32_t kSlab = 128 * 128;  // bytes of 128 rows of 64 values
+
+struct SmallArgs {
+    int32_t p, q, cols;      // X [p, q], columns per block (a multiple of 64)
+    int32_t transposed, blocks, steps;
+    float eps;
+    float coefficients[3 * kMaxSteps];
+    void* user;
+    int64_t user_batch, user_row;
+    int32_t user_dtype, user_vector, in_vector;
+    int32_t weights;
+    float keep, rate;
+    int* error;
+};
+
+// 16 bytes (8 values from column c of 64) of a row of a slab, swizzled as TMA would.
+__device__ __forceinline__ uint32_t slab_at(int row, int c) { return row * 128 + ((c / 8 ^ (row & 7)) << 4); }
+__device__ __forceinline__ void store_slab32(unsigned char* slab, int row, int c, const float (&v)[32]) {
+#pragma unroll
+    for (int k = 0; k < 32; k += 8) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const __half2 h = __floats2half2_rn(v[k + 2 * e], v[k + 2 * e + 1]);
+            memcpy(&w[e], &h, 4);
+        }
+        *reinterpret_cast<uint4*>(slab + slab_at(row, c + k)) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+template <bool CLUSTER, int NT>
+__global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const __grid_constant__ SmallArgs P) {
+    extern __shared__ unsigned char dynamic[];
+    unsigned char* X = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~uintptr_t(1023));
+    unsigned char* A = X + P.cols / 64 * kSlab;  // A, then B
+    float* sums = reinterpret_cast<float*>(A + 2 * kSlab);  // CLUSTER: this block's part of A, fp32 [128][128]
+    __shared__ uint64_t done;
+    __shared__ uint32_t tmem_at;
+    __shared__ float2 factor;
+    __shared__ __align__(16) float squares[NT / 32 + 1][4];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = CLUSTER ? static_cast<int>(tc::cluster_rank()) : 0;
+    const int b = blockIdx.x / P.blocks;
+    const uint32_t columns = P.cols <= 128 ? 256 : 512;
+    if (threadIdx.x == 0) {
+        tc::barrier_init(tc::smem_addr(&done), 1);
+        tc::barrier_init_fence();
+    }
+    if (warp == 0) tc::tmem_alloc<1>(tc::smem_addr(&tmem_at), columns);
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    const uint32_t lanes = static_cast<uint32_t>(warp % 4 * 32) << 16;
+    const uint32_t sum_x = tmem_at, sum_a = tmem_at + columns / 2;
+    begin_kernel();
+
+    // The update: a thread has row `row` of X, and 32 of every NT / 4 of the block's columns.
+    const int row = warp % 4 * 32 + lane, first = warp / 4 * 32, col0 = rank * P.cols;
+    const char* g = static_cast<const char*>(in.g) + b * in.g_batch * dtype_bytes(in.dtype);
+    float* mom = in.momentum ? in.momentum + b * in.m_batch : nullptr;
+    SquareSum squared;
+    for (int c = first; c < P.cols; c += NT / 4) {
+        float v[32], m[32];
+#pragma unroll
+        for (int k = 0; k < 32; k += 4) {
+            float x[4] = {}, y[4] = {};
+            const int col = col0 + c + k;
+            if (row < P.p) {
+                if (!P.transposed && P.in_vector) {
+                    if (col < P.q) {
+                        load_values<4>(g, row * in.g_row + col, in.dtype, x);
+                        if (mom) load_values<4>(mom, row * in.m_row + col, CB_F32, y);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (col + e < P.q) {
+                            const int64_t r = P.transposed ? col + e : row, i = P.transposed ? row : col + e;
+                            x[e] = load_value(g, r * in.g_row + i, in.dtype);
+                            if (mom) y[e] = mom[r * in.m_row + i];
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[k + e] = x[e], m[k + e] = y[e];
+        }
+        if (mom) {
+#pragma unroll
+            for (int k = 0; k < 32; ++k) {
+                v[k] = update_value(in, v[k], m[k]);
+                const int col = col0 + c + k;
+                if (row < P.p && col < P.q)
+                    mom[P.transposed ? static_cast<int64_t>(col) * in.m_row + row : row * in.m_row + col] = m[k];
+            }
+        }
+        squared.add(v);
+        tc::tmem_store32(sum_x + lanes + c, v);
+    }
+    auto put = [](float (&to)[4], const SquareSum& s) { to[0] = s.mid, to[1] = s.rest, to[2] = s.big, to[3] = s.small; };
+    auto get = [](const float4& f) {
+        SquareSum s;
+        s.mid = f.x, s.rest = f.y, s.big = f.z, s.small = f.w;
+        return s;
+    };
+    squared.add_lanes();
+    if (lane == 0) put(squares[warp], squared);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < NT / 32; ++w) squared.add(get(*reinterpret_cast<const float4*>(squares[w])));
+        put(squares[NT / 32], squared);
+    }
+    if constexpr (CLUSTER) tc::cluster_sync();
+    if (threadIdx.x == 0) {
+        if constexpr (CLUSTER) {
+            const uint32_t at = tc::smem_addr(squares[NT / 32]);
+            squared = get(tc::load_cluster(tc::in_block(at, 0)));
+            for (int r = 1; r < P.blocks; ++r) squared.add(get(tc::load_cluster(tc::in_block(at, r))));
+        }
+        factor = inverse_norm(squared, P.eps);
+    }
+    __syncthreads();
+    const float2 f = factor;
+    for (int c = first; c < P.cols; c += NT / 4) {
+        float v[32];
+        tc::tmem_load32(sum_x + lanes + c, v);
+#pragma unroll
+        for (int k = 0; k < 32; ++k) v[k] = (v[k] * f.x) * f.y;
+        store_slab32(X + c / 64 * kSlab, row, c % 64, v);
+        const float a = P.coefficients[0] * kScaleA;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) v[k] *= a;
+        tc::tmem_store32(sum_x + lanes + c, v);
+    }
+
+    // A wait that ran out is reported, and the rest is then computed without waiting: the
+    // cluster's blocks stay in step.
+    bool ok = true;
+    uint32_t phase = 0;
+    auto handed_over = [&] {  // what all threads stored, to the tensor core
+        tc::fence_to_tensor_core();
+        tc::fence_before();
+        __syncthreads();
+    };
+    auto products_done = [&] {
+        ok = ok && tc::barrier_wait(tc::smem_addr(&done), phase);
+        phase ^= 1;
+        tc::fence_after();
+    };
+    const uint32_t x_at = tc::smem_addr(X), a_at = tc::smem_addr(A);
+    for (int step = 0; step < P.steps; ++step) {
+        const float a = P.coefficients[3 * step], bb = P.coefficients[3 * step + 1], cc = P.coefficients[3 * step + 2];
+        const bool two_term = step < kTwoTerm;
+        handed_over();
+        if (threadIdx.x == 0) {  // A = X X^T
+            tc::fence_after();
+            constexpr uint32_t shape = tc::mma_shape(128, 128, false);
+            for (int x = 0; x < P.cols / 16; ++x) {
+                const uint64_t d = tc::operand_k_major(x_at + x / 4 * kSlab + x % 4 * 32);
+                tc::mma_f16<1>(sum_a, d, d, shape, x > 0);
+            }
+            tc::mma_commit<1>(tc::smem_addr(&done));
+        }
+        products_done();
+        constexpr float scale = kScaleA / (kScaleX * kScaleX);
+        for (int c = first; c < 128; c += NT / 4) {
+            float v[32];
+            tc::tmem_load32(sum_a + lanes + c, v);
+            if constexpr (CLUSTER) {  // 16-byte pieces of a row, swizzled over the banks
+#pragma unroll
+                for (int k = 0; k < 32; k += 4)
+                    *reinterpret_cast<float4*>(sums + row * 128 + (((c + k) / 4 ^ lane) << 2)) =
+                        make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) v[k] *= scale;
+                store_slab32(A + c / 64 * kSlab, row, c % 64, v);
+            }
+        }
+        if constexpr (CLUSTER) {
+            tc::cluster_sync();
+            const int share = 128 / P.blocks;  // rows that this block adds up, for all
+            for (int i = threadIdx.x; i < share * 32; i += NT) {
+                const int r = rank * share + i / 32, c4 = i % 32;
+                const uint32_t at = tc::smem_addr(sums + r * 128 + ((c4 ^ (r & 31)) << 2));
+                float4 part[kSmallCluster];
+#pragma unroll
+                for (int k = 0; k < kSmallCluster; ++k)
+                    part[k] = k < P.blocks ? tc::load_cluster(tc::in_block(at, k)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                float4 t = part[0];
+#pragma unroll
+                for (int k = 1; k < kSmallCluster; ++k) {
+                    t.x += part[k].x;
+                    t.y += part[k].y;
+                    t.z += part[k].z;
+                    t.w += part[k].w;
+                }
+                const __half2 h0 = __floats2half2_rn(t.x * scale, t.y * scale), h1 = __floats2half2_rn(t.z * scale, t.w * scale);
+                uint2 w;
+                memcpy(&w.x, &h0, 4);
+                memcpy(&w.y, &h1, 4);
+                const uint32_t to = a_at + c4 / 16 * kSlab + slab_at(r, c4 % 16 * 4) + c4 % 2 * 8;
+                for (int k = 0; k < P.blocks; ++k) tc::store_cluster(tc::in_block(to, k), w);
+            }
+            tc::fence_to_tensor_core();
+            tc::cluster_sync();
+        }
+        handed_over();
+        if (threadIdx.x == 0) {  // A A
+            tc::fence_after();
+            constexpr uint32_t shape = tc::mma_shape(128, 128, false);
+            for (int x = 0; x < 8; ++x) {
+                const uint64_t d = tc::operand_k_major(a_at + x / 4 * kSlab + x % 4 * 32);
+                tc::mma_f16<1>(sum_a, d, d, shape, x > 0);
+            }
+            tc::mma_commit<1>(tc::smem_addr(&done));
+        }
+        products_done();
+        for (int c = first; c < 128; c += NT / 4) {  // B in the place of A
+            float v[32];
+            tc::tmem_load32(sum_a + lanes + c, v);
+#pragma unroll
+            for (int k = 0; k < 32; k += 8) {
+                float t[8];
+                unpack<CB_F16>(*reinterpret_cast<const uint4*>(A + c / 64 * kSlab + slab_at(row, c % 64 + k)), t);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    v[k + e] = fmaf(cc / kScaleA, v[k + e], bb * t[e]);
+                    if (!two_term && row == c + k + e) v[k + e] += a * kScaleA;
+                }
+            }
+            store_slab32(A + c / 64 * kSlab, row, c % 64, v);
+        }
+        handed_over();
+        if (threadIdx.x == 0) {  // X <- (a X +) B X
+            tc::fence_after();
+            const uint32_t shape = tc::mma_shape(128, P.cols, true);
+            for (int x = 0; x < 8; ++x)
+                tc::mma_f16<1>(sum_x, tc::operand_k_major(a_at + x / 4 * kSlab + x % 4 * 32),
+                               tc::operand_mn_major(x_at + x * 2048, kSlab), shape, two_term || x > 0);
+            tc::mma_commit<1>(tc::smem_addr(&done));
+        }
+        products_done();
+        const bool final = step + 1 == P.steps;
+        for (int c = first; c < P.cols; c += NT / 4) {
+            float v[32];
+            tc::tmem_load32(sum_x + lanes + c, v);
+            if (!final) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) v[k] *= 1.f / kScaleA;
+                store_slab32(X + c / 64 * kSlab, row, c % 64, v);
+                if (step + 1 < kTwoTerm) {
+                    const float next = P.coefficients[3 * step + 3] * kScaleA;
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) v[k] *= next;
+                    tc::tmem_store32(sum_x + lanes + c, v);
+                }
+            } else if (row < P.p) {
+                char* user = static_cast<char*>(P.user) + b * P.user_batch * dtype_bytes(P.user_dtype);
+                const bool vector = P.user_vector && !P.transposed;
+#pragma unroll
+                for (int k = 0; k < 32; k += 4) {
+                    const int col = col0 + c + k;
+                    float w[4] = {}, o[4];
+                    auto at = [&](int e) {
+                        return P.transposed ? static_cast<int64_t>(col + e) * P.user_row + row : row * P.user_row + col + e;
+                    };
+                    if (P.weights) {
+                        if (vector) {
+                            if (col < P.q) load_values<4>(user, at(0), P.user_dtype, w);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (col + e < P.q) w[e] = load_value(user, at(e), P.user_dtype);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        o[e] = v[k + e] * (1.f / (kScaleA * kScaleX));
+                        if (P.weights) o[e] = fmaf(-P.rate, o[e], P.keep * w[e]);
+                    }
+                    if (vector) {
+                        if (col < P.q) {
+                            if (P.user_dtype == CB_F32) store_values4<CB_F32>(user, at(0), o);
+                            else if (P.user_dtype == CB_BF16) store_values4<CB_BF16>(user, at(0), o);
+                            else store_values4<CB_F16>(user, at(0), o);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (col + e < P.q) store_value(user, at(e), o[e], P.user_dtype);
+                    }
+                }
+            }
+        }
+    }
+    if (!ok && lane == 0) set_error(P.error, CB_ERR_TIMEOUT);
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    if (warp == 0) tc::tmem_free<1>(tmem_at, columns);
+}
+
 // ---------------------------------------------------------------- host
 
 PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
@@ -887,6 +1235,13 @@ bool tensor_map(CUtensorMap* map, const void* data, int64_t cols, int64_t rows, 
 
 int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
+// Blocks per matrix of muon_small_kernel (a power of two), 0 where it does not apply.
+int small_blocks(int64_t p, int64_t q) {
+    if (p > kSmallRows || q > kSmallCols * kSmallCluster) return 0;
+    int blocks = 1;
+    while (blocks * kSmallCols < q) blocks *= 2;
+    return blocks;
+}
 struct Workspace {
     int64_t p, q, ldx, lda;
     size_t hi[2], lo[2], gram, poly, partial, error, bytes;
@@ -903,14 +1258,15 @@ Workspace layout(int32_t batch, int32_t rows, int32_t cols) {
         at += static_cast<size_t>(round_up(bytes, 256));
         return here;
     };
-    const int64_t x = batch * w.p * w.ldx * 2, a = batch * w.p * w.lda * 2;
+    const bool small = small_blocks(w.p, w.q) > 0;  // one kernel, which keeps all in its blocks
+    const int64_t x = small ? 0 : batch * w.p * w.ldx * 2, a = small ? 0 : batch * w.p * w.lda * 2;
     w.hi[0] = take(x);
     w.hi[1] = take(x);
     w.lo[0] = take(x);
     w.lo[1] = take(x);
     w.gram = take(a);
     w.poly = take(a);
-    w.partial = take(static_cast<int64_t>(batch) * kNormBlocks * static_cast<int64_t>(sizeof(SquareSum)));
+    w.partial = take(small ? 0 : static_cast<int64_t>(batch) * kNormBlocks * static_cast<int64_t>(sizeof(SquareSum)));
     w.error = take(4);
     w.bytes = at;
     return w;
@@ -974,26 +1330,54 @@ struct Operand {
     }
 };
 
-// The tiles with the least time, in clocks: rounds of tiles over the GPU, the time that 64 of K
-// take a tile, and what a kernel takes besides.
+// The tiles with the least time, in clocks: rounds of tiles over the GPU, each the steps of 64
+// of K that it takes, and what a kernel takes besides. Fitted to all three products at sizes
+// of 200 to 4096, each with tiles of one kind forced, in clocks a step: 590 (128 x 64), 630 (128
+// x 128), 654 to 692 (256 x 160 to 256 by a pair; about 700 at any width where B is MN-major; the
+// tensor cores need 320 to 512 of them: shared memory and the way there bound it). Whole calls
+// with the kind chosen, and with the best single kind: 1024 x 1024 138 us (64 wide), 4 x 1024 x
+// 1024 201 us (128; 223 by pairs, 279 at 64), 2048 x 2048 283 us, 4096 x 4096 1060 us (pairs;
+// 1661 at 128, 2860 at 64).
 template <Product WHAT>
 bool launch_best(const Operand& left, const Operand& right, const ProductArgs& P, int sms, cudaStream_t s) {
     const int64_t ksteps = (P.k + kTileK - 1) / kTileK;
-    auto time = [&](int height, int width, int at_once, int64_t step) {
-        return (tiles_of<WHAT>(P.m, P.n, height, width) * P.batch + at_once - 1) / at_once * ksteps * step;
+    auto time = [&](int height, int width, int at_once, int64_t step, int64_t fixed) {
+        return (tiles_of<WHAT>(P.m, P.n, height, width) * P.batch + at_once - 1) / at_once * ksteps * step + fixed;
     };
-    int64_t best = time(kTileM, 64, sms, CB_STEP64);
+    int64_t best = time(kTileM, 64, sms, 590, 7000);
     int width = 64;
-    const int64_t t128 = time(kTileM, 128, sms, CB_STEP128);
+    const int64_t t128 = time(kTileM, 128, sms, 630, 8900);
     if (t128 < best) best = t128, width = 128;
     bool pair = false;
     for (int w = 160; w <= kPairWidth; w += 32) {
-        const int64_t t = time(kPairM, w, sms / 2, 290 + 11 * w / 8) + CB_PAIRX;
-        if (t < best) best = t, width = w, pair = true;
+        const int64_t t = kSymmetric<WHAT> ? time(kPairM, w, sms / 2, 590 + 2 * w / 5, 6000 + 30 * w)
+                                           : time(kPairM, w, sms / 2, 700, 13700);
+        if (t < best || (pair && t == best)) best = t, width = w, pair = true;
     }
     if (pair) return launch_pairs<WHAT>(left.box128, kSymmetric<WHAT> ? right.box128 : right.box64, P, width, sms, s);
     if (width == 128) return launch_product<128, WHAT>(left.box64, right.box64, P, sms, s);
     return launch_product<64, WHAT>(left.box64, right.box64, P, sms, s);
+}
+
+template <bool CLUSTER, int NT>
+bool launch_small(const MatrixIn& in, const SmallArgs& P, int32_t batch, cudaStream_t s) {
+    const size_t most = (kSmallCols / 64 + 2) * kSlab + (CLUSTER ? 128 * 128 * 4 : 0) + 1024;
+    static const bool ready = shared_memory(muon_small_kernel<CLUSTER, NT>, most);
+    if (!ready) return false;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(batch) * P.blocks);
+    cfg.blockDim = dim3(NT);
+    cfg.dynamicSmemBytes = (P.cols / 64 + 2) * kSlab + (CLUSTER ? 128 * 128 * 4 : 0) + 1024;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2]{};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = P.blocks;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = CLUSTER ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, muon_small_kernel<CLUSTER, NT>, in, P) == cudaSuccess;
 }
 
 bool valid_dtype(int d) { return d == CB_F32 || d == CB_F16 || d == CB_BF16; }
@@ -1026,35 +1410,71 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
     if (!aligned(in.g, dtype_bytes(in.dtype)) || !aligned(out.data, dtype_bytes(out.dtype)) ||
         !aligned(in.momentum, 4) || !aligned(error, 4))
         return CB_ERR_INVALID_ARG;
+    const bool tall = in.rows > in.cols;
+    auto vectors_of = [&](int v) {
+        return in.cols % v == 0 && in.g_row % v == 0 && (batch == 1 || in.g_batch % v == 0) &&
+               aligned(in.g, min64(16, v * dtype_bytes(in.dtype))) &&
+               (!in.momentum ||
+                (in.m_row % v == 0 && (batch == 1 || in.m_batch % v == 0) && aligned(in.momentum, 16)));
+    };
+    const bool vector = vectors_of(4), wide = vectors_of(8);
+    const bool user_vector = in.cols % 4 == 0 && out.row_stride % 4 == 0 && (batch == 1 || out.batch_stride % 4 == 0) &&
+                             aligned(out.data, 4 * dtype_bytes(out.dtype));
     const Workspace w = layout(batch, in.rows, in.cols);
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < static_cast<int64_t>(w.bytes)) return CB_ERR_CAPACITY;
+    char* base = static_cast<char*>(workspace);
+    if (!error) error = reinterpret_cast<int*>(base + w.error);  // any value: read by nobody
+    if (const int blocks = small_blocks(w.p, w.q)) {
+        SmallArgs P{};
+        P.p = static_cast<int32_t>(w.p);
+        P.q = static_cast<int32_t>(w.q);
+        P.cols = static_cast<int32_t>(round_up((w.q + blocks - 1) / blocks, 64));
+        P.transposed = tall;
+        P.blocks = blocks;
+        P.steps = steps;
+        P.eps = eps;
+        for (int k = 0; k < 3 * steps; ++k) P.coefficients[k] = coefficients[k];
+        P.user = out.data;
+        P.user_batch = out.batch_stride;
+        P.user_row = out.row_stride;
+        P.user_dtype = out.dtype;
+        P.user_vector = user_vector;
+        P.in_vector = vector;
+        P.weights = out.weights;
+        P.keep = out.keep;
+        P.rate = out.rate;
+        P.error = error;
+        int sms = 0;
+        if (!current_sms(&sms)) return CB_ERR_CUDA;
+        const bool sent = blocks > 1                       ? launch_small<true, 512>(in, P, batch, s)
+                          : P.cols <= 128 && batch > sms ? launch_small<false, 256>(in, P, batch, s)
+                                                           : launch_small<false, 512>(in, P, batch, s);
+        return cudaGetLastError() == cudaSuccess && sent ? CB_OK : CB_ERR_CUDA;
+    }
     int sms = 0;
     if (!current_sms(&sms) || !tensor_map_encoder()) return CB_ERR_CUDA;
-    char* base = static_cast<char*>(workspace);
     __half* hi[2] = {reinterpret_cast<__half*>(base + w.hi[0]), reinterpret_cast<__half*>(base + w.hi[1])};
     __half* lo[2] = {reinterpret_cast<__half*>(base + w.lo[0]), reinterpret_cast<__half*>(base + w.lo[1])};
     __half* gram = reinterpret_cast<__half*>(base + w.gram);
     __half* poly = reinterpret_cast<__half*>(base + w.poly);
     SquareSum* partial = reinterpret_cast<SquareSum*>(base + w.partial);
-    if (!error) error = reinterpret_cast<int*>(base + w.error);  // any value: read by nobody
-    const bool tall = in.rows > in.cols;
 
     Operand op_x[2], op_gram, op_poly;
     if (!op_x[0].set(hi[0], w.q, w.p, batch, w.ldx) || !op_x[1].set(hi[1], w.q, w.p, batch, w.ldx) ||
         !op_gram.set(gram, w.p, w.p, batch, w.lda) || !op_poly.set(poly, w.p, w.p, batch, w.lda))
         return CB_ERR_CUDA;
 
-    // 4096 values a block, on up to 8 blocks per SM in all.
+    // 8192 values a block, on up to 2 blocks per SM in all.
     const int norm_blocks = static_cast<int>(
-        max64(1, min64(min64(kNormBlocks, 8 * sms / batch), (matrix + 4 * 1024 - 1) / (4 * 1024))));
-    const bool vector = in.cols % 4 == 0 && in.g_row % 4 == 0 && (batch == 1 || in.g_batch % 4 == 0) &&
-                        aligned(in.g, 4 * dtype_bytes(in.dtype)) &&
-                        (!in.momentum || (in.m_row % 4 == 0 && (batch == 1 || in.m_batch % 4 == 0) &&
-                                          aligned(in.momentum, 16)));
+        max64(1, min64(min64(kNormBlocks, 2 * sms / batch), (matrix + 8 * 1024 - 1) / (8 * 1024))));
     const dim3 norm_grid(norm_blocks, batch);
-    if (vector) launch(muon_norm_kernel<4>, norm_grid, dim3(kNormThreads), 0, s, in, partial);
+    if (wide) launch(muon_norm_kernel<8>, norm_grid, dim3(kNormThreads), 0, s, in, partial);
+    else if (vector) launch(muon_norm_kernel<4>, norm_grid, dim3(kNormThreads), 0, s, in, partial);
     else launch(muon_norm_kernel<1>, norm_grid, dim3(kNormThreads), 0, s, in, partial);
-    const dim3 cast_grid((in.cols + kCastTile - 1) / kCastTile, (in.rows + kCastTile - 1) / kCastTile, batch);
+    const int cast_cols = (in.cols + kCastTile - 1) / kCastTile, cast_rows = (in.rows + kCastTile - 1) / kCastTile;
+    const dim3 cast_grid(cast_cols,
+                         static_cast<unsigned>(max64(1, min64(cast_rows, 8 * sms / (static_cast<int64_t>(cast_cols) * batch)))),
+                         batch);
     const int64_t x_batch = w.p * w.ldx, a_batch = w.p * w.lda;
     const int ldx = static_cast<int>(w.ldx), lda = static_cast<int>(w.lda);
     auto cast = tall ? (vector ? muon_cast_kernel<true, 4> : muon_cast_kernel<true, 1>)
@@ -1103,8 +1523,7 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
             P.user_row = out.row_stride;
             P.user_dtype = out.dtype;
             P.transposed = tall;
-            P.user_vector = in.cols % 4 == 0 && out.row_stride % 4 == 0 && (batch == 1 || out.batch_stride % 4 == 0) &&
-                            aligned(out.data, 4 * dtype_bytes(out.dtype));
+            P.user_vector = user_vector;
             P.weights = out.weights;
             P.keep = out.keep;
             P.rate = out.rate;
