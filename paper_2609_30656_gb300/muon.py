@@ -45,6 +45,10 @@ def _library() -> ctypes.CDLL:
 
 def _coefficients(coefficients, steps: int):
     """A C array of 3 * steps values: one triple for all steps, or one for each."""
+    key = (coefficients, steps) if type(coefficients) is tuple else None
+    array = _coefficient_arrays.get(key)
+    if array is not None:
+        return array
     if steps < 1:
         raise ValueError("at least one step is needed")
     rows = tuple(coefficients)
@@ -52,50 +56,41 @@ def _coefficients(coefficients, steps: int):
         rows = (rows,) * steps
     if len(rows) != steps or any(not hasattr(r, "__len__") or len(r) != 3 for r in rows):
         raise ValueError("coefficients must be one triple, or one triple for each step")
-    key = rows = tuple(tuple(float(x) for x in r) for r in rows)
-    if key not in _coefficient_arrays:
+    array = (ctypes.c_float * (3 * steps))(*[float(x) for r in rows for x in r])
+    if key is not None and all(isinstance(x, (float, int, tuple)) for x in coefficients):
         if len(_coefficient_arrays) >= 64:
             _coefficient_arrays.clear()
-        _coefficient_arrays[key] = (ctypes.c_float * (3 * steps))(*[x for r in rows for x in r])
-    return _coefficient_arrays[key]
+        _coefficient_arrays[key] = array
+    return array
 
 
-def _check_matrix(t: torch.Tensor, what: str):
-    if t.device.type != "cuda" or t.dim() not in (2, 3):
+def _check_matrix(t: torch.Tensor, what: str) -> int:
+    if t.get_device() < 0 or t.dim() not in (2, 3):
         raise ValueError(f"{what} must be a 2-D or 3-D CUDA tensor")
-    if t.dtype not in tbe._DTYPES:
+    kind = tbe._DTYPES.get(t.dtype)
+    if kind is None:
         raise ValueError(f"unsupported {what} dtype {t.dtype}")
+    return kind
 
 
-def _check_error(error: torch.Tensor | None, device: torch.device):
-    if error is not None and (error.device != device or error.dtype != torch.int32 or error.numel() != 1):
+def _check_error(error: torch.Tensor, index: int):
+    if error.get_device() != index or error.dtype != torch.int32 or error.numel() != 1:
         raise ValueError("error must be an int32 tensor of one value on the device")
 
 
-def _shape(t: torch.Tensor):
-    return (1, *t.shape) if t.dim() == 2 else tuple(t.shape)
-
-
-def _strides(t: torch.Tensor):
-    """(batch stride, row stride) in values; a dimension of one has the stride of a whole one."""
-    batch, rows, cols = _shape(t)
-    row = t.stride(-2) if rows > 1 else cols
-    return (t.stride(0) if t.dim() == 3 and batch > 1 else rows * row), row
-
-
-def _in_rows(t: torch.Tensor) -> bool:
-    batch, rows, cols = _shape(t)
-    return (cols <= 1 or t.stride(-1) == 1) and (rows <= 1 or t.stride(-2) >= cols)
-
-
-def _writable(t: torch.Tensor) -> bool:
-    batch, rows, cols = _shape(t)
-    return _in_rows(t) and (batch <= 1 or _strides(t)[0] >= rows * cols)
-
-
-def _workspace(lib, batch: int, rows: int, cols: int, device: torch.device):
-    nbytes = lib.cb_muon_workspace_bytes(batch, rows, cols)
-    return torch.empty(nbytes, dtype=torch.uint8, device=device), nbytes
+def _layout(t: torch.Tensor):
+    """(batch stride, row stride, rows contiguous, no two values in one place) in values; a
+    dimension of one has the stride of a whole one."""
+    shape = t.shape
+    rows, cols = shape[-2:]
+    if t.is_contiguous():
+        return rows * cols, cols, True, True
+    stride = t.stride()
+    row = stride[-2] if rows > 1 else cols
+    many = t.dim() == 3 and shape[0] > 1
+    batch = stride[0] if many else rows * row
+    in_rows = (cols <= 1 or stride[-1] == 1) and row >= cols
+    return batch, row, in_rows, in_rows and (not many or batch >= rows * cols)
 
 
 def newton_schulz(g: torch.Tensor, out: torch.Tensor | None = None, out_dtype: torch.dtype = torch.bfloat16,
@@ -108,34 +103,41 @@ def newton_schulz(g: torch.Tensor, out: torch.Tensor | None = None, out_dtype: t
     The products are in fp16 with fp32 sums, about 1e-3 off the exact result in the 2-norm,
     which is why the default output type is bf16. out may be g. A g whose columns are
     contiguous (a transposed view) is taken as it lies."""
-    lib = _library()
-    _check_matrix(g, "g")
-    _check_error(error, g.device)
+    lib = _bound or _library()
+    kind = _check_matrix(g, "g")
+    index = g.get_device()
+    if error is not None:
+        _check_error(error, index)
+    layout = _layout(g)
     if out is None:
-        if not _in_rows(g) and _in_rows(g.mT):
+        if not layout[2] and _layout(g.mT)[2]:
             out = torch.empty(g.mT.shape, dtype=out_dtype, device=g.device).mT
         else:
             out = torch.empty(g.shape, dtype=out_dtype, device=g.device)
-    else:
-        _check_matrix(out, "out")
-        if out.device != g.device or out.shape != g.shape or not (_writable(out) or _writable(out.mT)):
-            raise ValueError("out must have g's shape and device, its rows or columns contiguous, its matrices apart")
-    if not _writable(out):  # the transpose's factor is the factor's transpose
+    out_kind = _check_matrix(out, "out")
+    out_layout = _layout(out)
+    if out.get_device() != index or out.shape != g.shape or not (out_layout[3] or _layout(out.mT)[3]):
+        raise ValueError("out must have g's shape and device, its rows or columns contiguous, its matrices apart")
+    if not out_layout[3]:  # the transpose's factor is the factor's transpose
         newton_schulz(g.mT, out.mT, out.dtype, steps, coefficients, eps, error)
         return out
-    if not _in_rows(g):
+    if not layout[2]:
         g = g.contiguous()
-    batch, rows, cols = _shape(g)
+        layout = _layout(g)
+    shape = g.shape
+    rows, cols = shape[-2:]
+    batch = shape[0] if len(shape) == 3 else 1
     table = _coefficients(coefficients, steps)
     if g.numel() == 0:
         return out
-    work, nbytes = _workspace(lib, batch, rows, cols, g.device)
-    index = g.get_device()
+    nbytes = lib.cb_muon_workspace_bytes(batch, rows, cols)
+    work = torch.empty(nbytes, dtype=torch.uint8, device=g.device)
     with tbe._OnDevice(index):
-        tbe._check(lib.cb_muon_orthogonalise(g.data_ptr(), tbe._DTYPES[g.dtype], batch, rows, cols, *_strides(g), eps,
-                                             table, steps, out.data_ptr(), tbe._DTYPES[out.dtype], *_strides(out),
-                                             work.data_ptr(), nbytes, tbe._ptr(error), tbe._raw_stream(index)),
-                   "cb_muon_orthogonalise")
+        status = lib.cb_muon_orthogonalise(g.data_ptr(), kind, batch, rows, cols, layout[0], layout[1], eps, table, steps,
+                                           out.data_ptr(), out_kind, out_layout[0], out_layout[1], work.data_ptr(), nbytes,
+                                           None if error is None else error.data_ptr(), tbe._raw_stream(index))
+    if status:
+        tbe._check(status, "cb_muon_orthogonalise")
     return out
 
 
@@ -162,27 +164,35 @@ def muon_step(weight: torch.Tensor, grad: torch.Tensor, momentum: torch.Tensor, 
 
     weight and grad: fp32 / fp16 / bf16; momentum: fp32 (a running sum keeps its 32 bits).
     The three have one shape; weight and momentum have contiguous rows."""
-    lib = _library()
-    for t, what in ((weight, "weight"), (grad, "grad"), (momentum, "momentum")):
-        _check_matrix(t, what)
-        if t.device != weight.device or t.shape != weight.shape:
+    lib = _bound or _library()
+    index = weight.get_device()
+    kinds = [_check_matrix(t, what) for t, what in ((weight, "weight"), (grad, "grad"), (momentum, "momentum"))]
+    shape = weight.shape
+    for t in (grad, momentum):
+        if t.get_device() != index or t.shape != shape:
             raise ValueError("weight, grad and momentum must have one shape and device")
-    _check_error(error, weight.device)
+    if error is not None:
+        _check_error(error, index)
     if momentum.dtype != torch.float32:
         raise ValueError("momentum must be fp32")
-    if not _writable(weight) or not _writable(momentum):
+    w, m, g = _layout(weight), _layout(momentum), _layout(grad)
+    if not w[3] or not m[3]:
         raise ValueError("weight and momentum must have contiguous rows and matrices that do not overlap")
-    if not _in_rows(grad):
+    if not g[2]:
         grad = grad.contiguous()
-    batch, rows, cols = _shape(weight)
+        g = _layout(grad)
+    rows, cols = shape[-2:]
+    batch = shape[0] if len(shape) == 3 else 1
     table = _coefficients(coefficients, steps)
     scale = update_scale(rows, cols, adjust) if cols else 1.0
     if weight.numel() == 0:
         return
-    work, nbytes = _workspace(lib, batch, rows, cols, weight.device)
-    index = weight.get_device()
+    nbytes = lib.cb_muon_workspace_bytes(batch, rows, cols)
+    work = torch.empty(nbytes, dtype=torch.uint8, device=weight.device)
     with tbe._OnDevice(index):
-        tbe._check(lib.cb_muon_step(weight.data_ptr(), tbe._DTYPES[weight.dtype], *_strides(weight), grad.data_ptr(),
-                                    tbe._DTYPES[grad.dtype], *_strides(grad), momentum.data_ptr(), *_strides(momentum),
-                                    batch, rows, cols, lr, weight_decay, beta, int(nesterov), eps, table, steps, scale,
-                                    work.data_ptr(), nbytes, tbe._ptr(error), tbe._raw_stream(index)), "cb_muon_step")
+        status = lib.cb_muon_step(weight.data_ptr(), kinds[0], w[0], w[1], grad.data_ptr(), kinds[1], g[0], g[1],
+                                  momentum.data_ptr(), m[0], m[1], batch, rows, cols, lr, weight_decay, beta, nesterov,
+                                  eps, table, steps, scale, work.data_ptr(), nbytes,
+                                  None if error is None else error.data_ptr(), tbe._raw_stream(index))
+    if status:
+        tbe._check(status, "cb_muon_step")

@@ -38,14 +38,26 @@ def _library() -> ctypes.CDLL:
     return _bound
 
 
-def _check_tokens(tokens: torch.Tensor, device: torch.device):
-    if tokens.device != device or tokens.dtype not in tbe._IDX:
+# A call here launches one kernel or a few, so on small batches the binding's own time is the
+# call's: tensors' devices are compared by number, and contiguous tokens (one sequence to the
+# library) are told apart first.
+def _check_tokens(tokens: torch.Tensor, index: int) -> int:
+    kind = tbe._IDX.get(tokens.dtype)
+    if kind is None or tokens.get_device() != index:
         raise ValueError("tokens must be int32 or int64 on the device of the other tensors")
+    return kind
 
 
-def _check_error(error: torch.Tensor | None, device: torch.device):
-    if error is not None and (error.device != device or error.dtype != torch.int32 or error.numel() != 1):
+def _check_error(error: torch.Tensor, index: int):
+    if error.get_device() != index or error.dtype != torch.int32 or error.numel() != 1:
         raise ValueError("error must be an int32 tensor of one value on the device")
+
+
+def _dtype(t: torch.Tensor, what: str) -> int:
+    kind = tbe._DTYPES.get(t.dtype)
+    if kind is None:
+        raise ValueError(f"unsupported {what} dtype {t.dtype}")
+    return kind
 
 
 def _as_sequences(t: torch.Tensor, dims: int):
@@ -61,11 +73,6 @@ def _as_sequences(t: torch.Tensor, dims: int):
     return t, shape[0], shape[1], stride[0], stride[1]
 
 
-def _check_values(t: torch.Tensor, what: str):
-    if t.dtype not in tbe._DTYPES:
-        raise ValueError(f"unsupported {what} dtype {t.dtype}")
-
-
 def token_forward(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out: torch.Tensor | None = None,
                   out_dtype: torch.dtype | None = None, error: torch.Tensor | None = None) -> torch.Tensor:
     """out[..., :] = scale * table[tokens[...], :] (cb_token_forward).
@@ -74,37 +81,45 @@ def token_forward(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0,
     int64 of any shape. out: [*tokens.shape, dim] of out_dtype (default: the table's type),
     rows contiguous. A token outside [0, rows) gives zeros and sets `error` (an int32 tensor of
     one value on the device) to CB_ERR_INDEX_OOB if it holds 0."""
-    lib = _library()
-    if table.device.type != "cuda" or table.dim() != 2:
+    lib = _bound or _library()
+    index = table.get_device()
+    if index < 0 or table.dim() != 2:
         raise ValueError("table must be a 2-D CUDA tensor [rows, dim]")
-    _check_values(table, "table")
-    _check_tokens(tokens, table.device)
-    _check_error(error, table.device)
+    table_dtype = _dtype(table, "table")
+    index_dtype = _check_tokens(tokens, index)
+    if error is not None:
+        _check_error(error, index)
     rows, dim = table.shape
-    if dim > 1 and table.stride(1) != 1:
+    row_stride, step = table.stride()
+    if dim > 1 and step != 1:
         raise ValueError("table rows must be contiguous")
-    if rows > 1 and table.stride(0) < dim:
+    if rows <= 1:
+        row_stride = dim
+    elif row_stride < dim:
         raise ValueError("table rows must not overlap")
-    shape = (*tokens.shape, dim)
-    if out is None:
-        out = torch.empty(shape, dtype=out_dtype or table.dtype, device=table.device)
+    fresh = out is None
+    if fresh:
+        out = torch.empty((*tokens.shape, dim), dtype=out_dtype or table.dtype, device=table.device)
     else:
-        if out.device != table.device or tuple(out.shape) != shape or (dim > 1 and out.stride(-1) != 1):
+        if out.get_device() != index or out.shape != (*tokens.shape, dim) or (dim > 1 and out.stride(-1) != 1):
             raise ValueError("out must be [*tokens.shape, dim] on the table's device, its rows contiguous")
         if out_dtype is not None and out.dtype != out_dtype:
             raise TypeError(f"out must be {out_dtype}")
-    _check_values(out, "output")
-    n_dims = tokens.dim()
-    tok, sequences, length, tok0, tok1 = _as_sequences(tokens, n_dims)
-    target, _, _, out0, out1 = _as_sequences(out, n_dims)
-    if n_dims > 2 and target.data_ptr() != out.data_ptr():
-        raise ValueError("out must be describable by two strides and contiguous rows")
-    index = table.get_device()
+    kind = _dtype(out, "output")
+    if tokens.is_contiguous() and (fresh or out.is_contiguous()):
+        tok, sequences, length, tok0, tok1, out0, out1 = tokens, 1, tokens.numel(), 0, 1, 0, dim
+    else:
+        n_dims = tokens.dim()
+        tok, sequences, length, tok0, tok1 = _as_sequences(tokens, n_dims)
+        target, _, _, out0, out1 = _as_sequences(out, n_dims)
+        if n_dims > 2 and target.data_ptr() != out.data_ptr():
+            raise ValueError("out must be describable by two strides and contiguous rows")
     with tbe._OnDevice(index):
-        tbe._check(lib.cb_token_forward(table.data_ptr(), tbe._DTYPES[table.dtype], rows, dim,
-                                        table.stride(0) if rows > 1 else dim, tok.data_ptr(), tbe._IDX[tok.dtype],
-                                        sequences, length, tok0, tok1, scale, out.data_ptr(), tbe._DTYPES[out.dtype],
-                                        out0, out1, tbe._ptr(error), tbe._raw_stream(index)), "cb_token_forward")
+        status = lib.cb_token_forward(table.data_ptr(), table_dtype, rows, dim, row_stride, tok.data_ptr(), index_dtype,
+                                      sequences, length, tok0, tok1, scale, out.data_ptr(), kind, out0, out1,
+                                      None if error is None else error.data_ptr(), tbe._raw_stream(index))
+    if status:
+        tbe._check(status, "cb_token_forward")
     return out
 
 
@@ -118,38 +133,50 @@ def token_backward(grad_out: torch.Tensor, tokens: torch.Tensor, num_rows: int, 
     With accumulate=True that is added to `out` in place and rows without a token are left
     alone; otherwise every row is written. Positions that hold padding_idx give nothing, nor
     do tokens outside [0, num_rows), which set `error` as in token_forward."""
-    lib = _library()
-    if grad_out.device.type != "cuda" or grad_out.dim() != tokens.dim() + 1 or grad_out.shape[:-1] != tokens.shape:
+    lib = _bound or _library()
+    index = grad_out.get_device()
+    shape = grad_out.shape
+    if index < 0 or not shape or shape[:-1] != tokens.shape:
         raise ValueError("grad_out must be a CUDA tensor [*tokens.shape, dim]")
-    _check_values(grad_out, "gradient")
-    _check_tokens(tokens, grad_out.device)
-    _check_error(error, grad_out.device)
-    dim = grad_out.shape[-1]
+    go_dtype = _dtype(grad_out, "gradient")
+    index_dtype = _check_tokens(tokens, index)
+    if error is not None:
+        _check_error(error, index)
+    dim = shape[-1]
     if num_rows < 0:
         raise ValueError("num_rows must not be negative")
-    if padding_idx is not None and not 0 <= padding_idx < num_rows:
+    if padding_idx is None:
+        padding_idx = -1
+    elif not 0 <= padding_idx < num_rows:
         raise ValueError("padding_idx must be a row of the table")
+    row_stride = dim
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs the gradient to add to")
         out = torch.empty(num_rows, dim, dtype=out_dtype, device=grad_out.device)
-    elif (out.device != grad_out.device or tuple(out.shape) != (num_rows, dim) or (dim > 1 and out.stride(1) != 1)
-          or (num_rows > 1 and out.stride(0) < dim)):
-        raise ValueError("out must be [num_rows, dim] on the gradient's device, its rows contiguous")
-    _check_values(out, "gradient")
-    if dim > 1 and grad_out.stride(-1) != 1:
-        grad_out = grad_out.contiguous()
-    n_dims = tokens.dim()
-    tok, sequences, length, tok0, tok1 = _as_sequences(tokens, n_dims)
-    go, _, _, go0, go1 = _as_sequences(grad_out, n_dims)
-    index = grad_out.get_device()
+    else:
+        if out.get_device() != index or out.shape != (num_rows, dim):
+            raise ValueError("out must be [num_rows, dim] on the gradient's device")
+        if num_rows > 1:
+            row_stride = out.stride(0)
+        if (dim > 1 and out.stride(1) != 1) or row_stride < dim:
+            raise ValueError("out's rows must be contiguous and must not overlap")
+    kind = _dtype(out, "gradient")
+    if tokens.is_contiguous() and grad_out.is_contiguous():
+        tok, sequences, length, tok0, tok1, go, go0, go1 = tokens, 1, tokens.numel(), 0, 1, grad_out, 0, dim
+    else:
+        if dim > 1 and grad_out.stride(-1) != 1:
+            grad_out = grad_out.contiguous()
+        n_dims = tokens.dim()
+        tok, sequences, length, tok0, tok1 = _as_sequences(tokens, n_dims)
+        go, _, _, go0, go1 = _as_sequences(grad_out, n_dims)
     nbytes = lib.cb_token_backward_workspace_bytes(sequences * length, num_rows, dim)
     work = torch.empty(nbytes, dtype=torch.uint8, device=grad_out.device) if nbytes else None
     with tbe._OnDevice(index):
-        tbe._check(lib.cb_token_backward(go.data_ptr(), tbe._DTYPES[go.dtype], go0, go1, tok.data_ptr(),
-                                         tbe._IDX[tok.dtype], sequences, length, tok0, tok1, num_rows, dim, scale,
-                                         -1 if padding_idx is None else padding_idx, int(accumulate), out.data_ptr(),
-                                         tbe._DTYPES[out.dtype], out.stride(0) if num_rows > 1 else dim,
-                                         tbe._ptr(work), nbytes, tbe._ptr(error), tbe._raw_stream(index)),
-                   "cb_token_backward")
+        status = lib.cb_token_backward(go.data_ptr(), go_dtype, go0, go1, tok.data_ptr(), index_dtype, sequences, length,
+                                       tok0, tok1, num_rows, dim, scale, padding_idx, accumulate, out.data_ptr(), kind,
+                                       row_stride, None if work is None else work.data_ptr(), nbytes,
+                                       None if error is None else error.data_ptr(), tbe._raw_stream(index))
+    if status:
+        tbe._check(status, "cb_token_backward")
     return out
