@@ -404,6 +404,18 @@ constexpr int kEpilogueWarps = 8;  // two for each quarter of TMEM's lanes, ever
 constexpr int kProductThreads = (kEpilogueWarps + 2) * 32;  // + a copying warp, + a multiplying warp
 constexpr uint32_t kBoxBytes = 64 * 64 * 2;                 // 64 rows of 64 fp16
 template <int BN> constexpr int kStages = BN == 128 ? 6 : 8;
+constexpr int kPartsMost = 4;
+
+// Parts of K in which A = X X^T is summed, the parts' sums then added in order: as many blocks
+// can share a tile (muon_split_kernel), and a result is the same whether they do or one block
+// takes the parts in turn, so that a matrix gives the same bits alone and in a stack. Two or
+// four, of a dozen steps of 64 at least, where a matrix is of few tiles.
+int gram_parts(int64_t p, int64_t k) {
+    const int64_t ksteps = (k + 63) / 64;
+    return p > 512 || ksteps < 24 ? 1 : (ksteps < 48 ? 2 : 4);
+}
+// Sums of a tile in TMEM: two of its width, or of every part's.
+template <int BN, Product WHAT> constexpr int kSumColumns = WHAT == kGram && BN == 64 ? kPartsMost * BN : BN;
 template <int BN> constexpr uint32_t kStageBytes = (kTileM + BN) * kTileK * 2;
 
 struct ProductArgs {
@@ -411,6 +423,7 @@ struct ProductArgs {
     int32_t batch;
     int32_t row_tiles, col_tiles;
     int32_t width;            // columns of a tile
+    int32_t parts;            // kGram: parts of K summed apart (gram_parts)
     int64_t tiles;            // per matrix
     float a, b, c;            // the step's coefficients (a = 0: no term a X, or a I)
     const __half* term_hi;    // kPoly: A; kUpdate, kResult: X
@@ -629,7 +642,8 @@ __device__ __forceinline__ void finish(const ProductArgs& P, int batch, int row,
 // row of C has, or that the other triangle gives, are skipped.
 template <Product WHAT>
 __device__ __forceinline__ void finish_tile(const ProductArgs& P, int batch, int row0, int col0, int width, uint32_t tmem,
-                                            uint32_t ready, uint32_t parity, float* stage, int warp, int lane, bool& ok) {
+                                            uint32_t ready, uint32_t parity, float* stage, int warp, int lane, bool& ok,
+                                            int parts = 1) {
     const int row = row0 + lane;
     auto skip = [&](int c) { return c >= width || col0 + c >= P.n || (kSymmetric<WHAT> && (col0 + c) / kTileM > row0 / kTileM); };
     int c = warp / 4 * 32;
@@ -641,7 +655,16 @@ __device__ __forceinline__ void finish_tile(const ProductArgs& P, int batch, int
     for (; !skip(c); c += 64) {
         const Term term = next;
         float v[32];
-        tc::tmem_load32(tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16) + c, v);
+        const uint32_t at = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16) + c;
+        tc::tmem_load32(at, v);
+        if constexpr (WHAT == kGram) {
+            for (int k = 1; k < parts; ++k) {
+                float more[32];
+                tc::tmem_load32(at + k * width, more);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] += more[i];
+            }
+        }
         if (!skip(c + 64)) load_term<WHAT>(P, batch, row, col0 + c + 64, next);
         finish<WHAT>(P, batch, row, col0 + c, v, term, stage, lane);
     }
@@ -658,7 +681,8 @@ __global__ void __launch_bounds__(kProductThreads, 1)
 muon_product_kernel(const __grid_constant__ CUtensorMap left, const __grid_constant__ CUtensorMap right,
                     const ProductArgs P) {
     constexpr int S = kStages<BN>;
-    constexpr uint32_t kColumns = 2 * BN;
+    constexpr int kSums = kSumColumns<BN, WHAT>;
+    constexpr uint32_t kColumns = 2 * kSums;
     extern __shared__ unsigned char dynamic[];
     unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~uintptr_t(1023));
     __shared__ uint64_t full[S], empty[S], ready[2], drained[2];
@@ -686,6 +710,7 @@ muon_product_kernel(const __grid_constant__ CUtensorMap left, const __grid_const
     begin_kernel();
     const int64_t total = P.tiles * P.batch;
     const int ksteps = (P.k + kTileK - 1) / kTileK;
+    const int per = kSums > BN ? (ksteps + P.parts - 1) / P.parts : ksteps;  // of a part
     bool ok = true;
 
     if (warp == kEpilogueWarps) {
@@ -726,17 +751,21 @@ muon_product_kernel(const __grid_constant__ CUtensorMap left, const __grid_const
             for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
                 if (!(ok = tc::barrier_wait(tc::smem_addr(drained + acc), acc_phase ^ 1))) break;
                 tc::fence_after();
+                uint32_t sums = tmem + acc * kSums;
+                int within = 0;  // steps done of a part
                 for (int k = 0; k < ksteps; ++k) {
                     if (!(ok = tc::barrier_wait(tc::smem_addr(full + s), phase))) break;
                     tc::fence_after();
+                    if (kSums > BN && within == per) within = 0, sums += BN;
                     const uint32_t at = tc::smem_addr(ring) + s * kStageBytes<BN>, bt = at + kTileM * kTileK * 2;
 #pragma unroll
                     for (int x = 0; x < kTileK / 16; ++x) {
                         const uint64_t da = tc::operand_k_major(at + x * 32);
                         const uint64_t db = kSymmetric<WHAT> ? tc::operand_k_major(bt + x * 32)
                                                             : tc::operand_mn_major(bt + x * 2048, kBoxBytes);
-                        tc::mma_f16<1>(tmem + acc * BN, da, db, shape, k > 0 || x > 0);
+                        tc::mma_f16<1>(sums, da, db, shape, within > 0 || x > 0);
                     }
+                    ++within;
                     tc::mma_commit<1>(tc::smem_addr(empty + s));
                     if (++s == S) s = 0, phase ^= 1;
                 }
@@ -749,9 +778,9 @@ muon_product_kernel(const __grid_constant__ CUtensorMap left, const __grid_const
         uint32_t acc_phase = 0;
         for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
             const Tile T = tile_at<kTileM, WHAT>(P, t);
-            finish_tile<WHAT>(P, T.b, T.i * kTileM + warp % 4 * 32, T.j * BN, BN, tmem + acc * BN,
+            finish_tile<WHAT>(P, T.b, T.i * kTileM + warp % 4 * 32, T.j * BN, BN, tmem + acc * kSums,
                               tc::smem_addr(ready + acc), acc_phase, stage + (WHAT == kResult ? warp * kStageFloats : 0), warp,
-                              lane, ok);
+                              lane, ok, kSums > BN ? (ksteps + per - 1) / per : 1);
             if (!ok) break;
             if (lane == 0) tc::barrier_arrive(tc::smem_addr(drained + acc));
             if (++acc == 2) acc = 0, acc_phase ^= 1;
@@ -889,17 +918,144 @@ muon_pair_kernel(const __grid_constant__ CUtensorMap left, const __grid_constant
     if (warp == kEpilogueWarps) tc::tmem_free<2>(tmem, kColumns);
 }
 
+// A = X X^T of few tiles and a long K: a cluster of P.parts blocks takes a tile of 128 x 64, a
+// part of K each, and every block adds up a share of the tile's rows over all of them, in
+// order, from their shared memory.
+
+__global__ void __launch_bounds__(kProductThreads, 1)
+muon_split_kernel(const __grid_constant__ CUtensorMap rows, const ProductArgs P) {
+    constexpr int BN = 64, S = kStages<BN>;
+    extern __shared__ unsigned char dynamic[];
+    unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~uintptr_t(1023));
+    float* sums = reinterpret_cast<float*>(ring);  // [128][64], once the products are done
+    __shared__ uint64_t full[S], empty[S], ready;
+    __shared__ uint32_t tmem_at;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S; ++s) {
+            tc::barrier_init(tc::smem_addr(full + s), 1);
+            tc::barrier_init(tc::smem_addr(empty + s), 1);
+        }
+        tc::barrier_init(tc::smem_addr(&ready), 1);
+        tc::barrier_init_fence();
+        tc::tma_prefetch(&rows);
+    }
+    if (warp == kEpilogueWarps) tc::tmem_alloc<1>(tc::smem_addr(&tmem_at), BN);
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    const uint32_t tmem = tmem_at;
+    begin_kernel();
+    const int rank = static_cast<int>(tc::cluster_rank());
+    const Tile T = tile_at<kTileM, kGram>(P, blockIdx.x / P.parts);
+    const int all = (P.k + kTileK - 1) / kTileK, per = (all + P.parts - 1) / P.parts;
+    const int first = rank * per, count = max(0, min(per, all - first));
+    bool ok = true;
+
+    if (warp == kEpilogueWarps) {
+        if (lane == 0) {  // copies
+            int k = 0;
+            for (; k < count; ++k) {
+                const int s = k % S;
+                if (!(ok = tc::barrier_wait(tc::smem_addr(empty + s), (k / S & 1) ^ 1))) break;
+                const uint32_t bar = tc::smem_addr(full + s);
+                const uint32_t at = tc::smem_addr(ring) + s * kStageBytes<BN>;
+                const int x = (first + k) * kTileK;
+                tc::barrier_expect(bar, kStageBytes<BN>);
+                tc::tma_load(at, &rows, bar, x, T.i * kTileM, T.b);
+                tc::tma_load(at + kBoxBytes, &rows, bar, x, T.i * kTileM + 64, T.b);
+                tc::tma_load(at + 2 * kBoxBytes, &rows, bar, x, T.j * BN, T.b);
+            }
+            if (!ok)  // copies in flight land before the block's shared memory goes away
+                for (int x = max(0, k - S); x < k; ++x)
+                    if (!tc::barrier_wait(tc::smem_addr(full + x % S), x / S & 1)) break;
+        }
+    } else if (warp == kEpilogueWarps + 1) {
+        if (lane == 0) {  // products
+            constexpr uint32_t shape = tc::mma_shape(kTileM, BN, false);
+            for (int k = 0; k < count && ok; ++k) {
+                const int s = k % S;
+                if (!(ok = tc::barrier_wait(tc::smem_addr(full + s), k / S & 1))) break;
+                tc::fence_after();
+                const uint32_t at = tc::smem_addr(ring) + s * kStageBytes<BN>, bt = at + 2 * kBoxBytes;
+#pragma unroll
+                for (int x = 0; x < kTileK / 16; ++x)
+                    tc::mma_f16<1>(tmem, tc::operand_k_major(at + x * 32), tc::operand_k_major(bt + x * 32), shape,
+                                   k > 0 || x > 0);
+                tc::mma_commit<1>(tc::smem_addr(empty + s));
+            }
+            if (ok && count > 0) tc::mma_commit<1>(tc::smem_addr(&ready));
+        }
+    } else {
+        const int row = warp % 4 * 32 + lane, c = warp / 4 * 32;
+        float v[32] = {};
+        if (count > 0) {
+            ok = __all_sync(kFull, tc::barrier_wait(tc::smem_addr(&ready), 0));
+            tc::fence_after();
+            tc::tmem_load32(tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16) + c, v);
+        }
+        // After a wait that ran out copies may still be on their way into the ring: the sums
+        // then stay unwritten (the result is reported as incomplete).
+        if (ok) {
+#pragma unroll
+            for (int k = 0; k < 32; k += 4)  // 16-byte pieces of a row, swizzled over the banks
+                *reinterpret_cast<float4*>(sums + row * BN + (((c + k) / 4 ^ (row & 15)) << 2)) =
+                    make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+        }
+    }
+    if (!ok && lane == 0) set_error(P.error, CB_ERR_TIMEOUT);
+    __syncwarp();
+    tc::fence_before();
+    tc::cluster_sync();
+    if (warp < kEpilogueWarps) {
+        const int share = kTileM / P.parts, columns = BN / 4;
+        constexpr float scale = kScaleA / (kScaleX * kScaleX);
+        __half* out = P.out_hi + T.b * P.out_batch;
+        for (int i = threadIdx.x; i < share * columns; i += kEpilogueWarps * 32) {
+            const int r = rank * share + i % share, c4 = i / share;  // lanes along the rows
+            const uint32_t at = tc::smem_addr(sums + r * BN + ((c4 ^ (r & 15)) << 2));
+            float4 part[kPartsMost];
+#pragma unroll
+            for (int k = 0; k < kPartsMost; ++k)
+                part[k] = k < P.parts ? tc::load_cluster(tc::in_block(at, k)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            float4 t = part[0];
+#pragma unroll
+            for (int k = 1; k < kPartsMost; ++k) {
+                t.x += part[k].x;
+                t.y += part[k].y;
+                t.z += part[k].z;
+                t.w += part[k].w;
+            }
+            const int row = T.i * kTileM + r, col = T.j * BN + c4 * 4, block = col / kTileM;
+            if (row >= P.m || col >= P.n || block > T.i) continue;
+            const __half2 h0 = __floats2half2_rn(t.x * scale, t.y * scale), h1 = __floats2half2_rn(t.z * scale, t.w * scale);
+            uint2 w;
+            memcpy(&w.x, &h0, 4);
+            memcpy(&w.y, &h1, 4);
+            *reinterpret_cast<uint2*>(out + static_cast<int64_t>(row) * P.out_ld + col) = w;  // rows are padded to 64
+            if (block < T.i) {
+                const __half h[4] = {__low2half(h0), __high2half(h0), __low2half(h1), __high2half(h1)};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) out[static_cast<int64_t>(col + e) * P.out_ld + row] = h[e];
+            }
+        }
+    }
+    tc::cluster_sync();  // no block ends while others read its sums
+    tc::fence_after();
+    if (warp == kEpilogueWarps) tc::tmem_free<1>(tmem, BN);
+}
+
 // ---------------------------------------------------------------- small matrices in one launch
 
-// Up to 128 x 2048: all steps of a matrix in one kernel, by a cluster of blocks that each keep
-// up to 256 columns of X in shared memory (fp16, for the products) and in TMEM (fp32, a X as
+// Up to 128 x 3 K: all steps of a matrix in one kernel, by a cluster of blocks that each keep
+// up to 384 columns of X in shared memory (fp16, for the products) and in TMEM (fp32, a X as
 // the sums that B X is added to). The Gram matrix of the blocks' columns is added up
 // across the cluster, in a fixed order, a share of its rows in each block; A A and B are
 // taken by every block for itself. What is left of a step is a chain of three products
 // of half a microsecond and their epilogues, in which a thread of TN / 128 has 32 columns of
 // its row at a time: 512 threads a block (128 x 256, five steps: 34 us, 42 with 256), or 256 of
 // two blocks per SM where narrow matrices would otherwise queue (300 of 128 x 128: 34 us, 47).
-constexpr int kSmallRows = 128, kSmallCols = 256, kSmallCluster = 8;
+constexpr int kSmallRows = 128, kSmallCols = 384, kSmallCluster = 8;
 constexpr uint32_t kSlab = 128 * 128;  // bytes of 128 rows of 64 values
 
 struct SmallArgs {
@@ -953,7 +1109,7 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
     __syncthreads();
     tc::fence_after();
     const uint32_t lanes = static_cast<uint32_t>(warp % 4 * 32) << 16;
-    const uint32_t sum_x = tmem_at, sum_a = tmem_at + columns / 2;
+    const uint32_t sum_x = tmem_at, sum_a = tmem_at + columns - 128;
     begin_kernel();
 
     // The update: a thread has row `row` of X, and 32 of every NT / 4 of the block's columns.
@@ -1136,10 +1292,12 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
         handed_over();
         if (threadIdx.x == 0) {  // X <- (a X +) B X
             tc::fence_after();
-            const uint32_t shape = tc::mma_shape(128, P.cols, true);
-            for (int x = 0; x < 8; ++x)
-                tc::mma_f16<1>(sum_x, tc::operand_k_major(a_at + x / 4 * kSlab + x % 4 * 32),
-                               tc::operand_mn_major(x_at + x * 2048, kSlab), shape, two_term || x > 0);
+            for (int c = 0; c < P.cols; c += 256) {  // as many columns as one product takes
+                const uint32_t shape = tc::mma_shape(128, P.cols - c < 256 ? P.cols - c : 256, true);
+                for (int x = 0; x < 8; ++x)
+                    tc::mma_f16<1>(sum_x + c, tc::operand_k_major(a_at + x / 4 * kSlab + x % 4 * 32),
+                                   tc::operand_mn_major(x_at + c / 64 * kSlab + x * 2048, kSlab), shape, two_term || x > 0);
+            }
             tc::mma_commit<1>(tc::smem_addr(&done));
         }
         products_done();
@@ -1301,6 +1459,32 @@ bool shared_memory(KernelT kernel, size_t bytes) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)) == cudaSuccess;
 }
 
+// As launch(), by clusters of `cluster` blocks.
+template <class... Params, class... Args>
+bool launch_clusters(void (*kernel)(Params...), int cluster, int64_t grid, int block, size_t smem, cudaStream_t s,
+                     const Args&... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(grid));
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2]{};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...) == cudaSuccess;
+}
+bool launch_split(const CUtensorMap& rows, ProductArgs P, cudaStream_t s) {
+    set_tiles<kGram>(P, kTileM, 64);
+    constexpr size_t smem = kStages<64> * kStageBytes<64> + 1024;
+    static const bool ready = shared_memory(muon_split_kernel, smem);
+    return ready && launch_clusters(muon_split_kernel, P.parts, P.tiles * P.batch * P.parts, kProductThreads, smem, s, rows, P);
+}
+
 template <int BN, Product WHAT>
 bool launch_product(const CUtensorMap& left, const CUtensorMap& right, ProductArgs P, int sms, cudaStream_t s) {
     set_tiles<WHAT>(P, kTileM, BN);
@@ -1345,6 +1529,13 @@ bool launch_best(const Operand& left, const Operand& right, const ProductArgs& P
         return (tiles_of<WHAT>(P.m, P.n, height, width) * P.batch + at_once - 1) / at_once * ksteps * step + fixed;
     };
     int64_t best = time(kTileM, 64, sms, 590, 7000);
+    if constexpr (WHAT == kGram) {
+        if (P.parts > 1) {
+            const int64_t blocks = tiles_of<kGram>(P.m, P.n, kTileM, 64) * P.batch * P.parts;
+            const int64_t split = (blocks + sms - 1) / sms * ((ksteps + P.parts - 1) / P.parts * 590 + 11000);
+            return split < best ? launch_split(left.box64, P, s) : launch_product<64, WHAT>(left.box64, right.box64, P, sms, s);
+        }
+    }
     int width = 64;
     const int64_t t128 = time(kTileM, 128, sms, 630, 8900);
     if (t128 < best) best = t128, width = 128;
@@ -1364,20 +1555,9 @@ bool launch_small(const MatrixIn& in, const SmallArgs& P, int32_t batch, cudaStr
     const size_t most = (kSmallCols / 64 + 2) * kSlab + (CLUSTER ? 128 * 128 * 4 : 0) + 1024;
     static const bool ready = shared_memory(muon_small_kernel<CLUSTER, NT>, most);
     if (!ready) return false;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(static_cast<unsigned>(batch) * P.blocks);
-    cfg.blockDim = dim3(NT);
-    cfg.dynamicSmemBytes = (P.cols / 64 + 2) * kSlab + (CLUSTER ? 128 * 128 * 4 : 0) + 1024;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[2]{};
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = P.blocks;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = CLUSTER ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, muon_small_kernel<CLUSTER, NT>, in, P) == cudaSuccess;
+    const size_t smem = (P.cols / 64 + 2) * kSlab + (CLUSTER ? 128 * 128 * 4 : 0) + 1024;
+    return launch_clusters(muon_small_kernel<CLUSTER, NT>, P.blocks, static_cast<int64_t>(batch) * P.blocks, NT, smem, s,
+                           in, P);
 }
 
 bool valid_dtype(int d) { return d == CB_F32 || d == CB_F16 || d == CB_BF16; }
@@ -1492,6 +1672,7 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
         P.error = error;
         P.m = P.n = static_cast<int32_t>(w.p);
         P.k = static_cast<int32_t>(w.q);
+        P.parts = gram_parts(w.p, w.q);
         P.out_hi = gram;
         P.out_batch = a_batch;
         P.out_ld = lda;

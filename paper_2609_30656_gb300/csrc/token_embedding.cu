@@ -79,6 +79,45 @@ __global__ void __launch_bounds__(kLookupThreads, kLookupBlocks) token_lookup_ke
     }
 }
 
+// Rows that no vector fits (an odd number of halves, or an odd address): a warp takes 256
+// consecutive values of a row, a lane every 32nd, so that a load of 2 bytes a lane is still
+// one line, and a row's index is worked out once for 8 values a lane. (One value at a time in
+// the kernel above: 217K rows of 1613 halves 1111 us, most of it arithmetic on indices.)
+constexpr int kOddValues = 8;
+template <int IN, int OUT>
+__global__ void __launch_bounds__(kLookupThreads) token_lookup_odd_kernel(const LookupArgs P, int32_t dim) {
+    begin_kernel();
+    const uint64_t w = (static_cast<uint64_t>(blockIdx.x) * kLookupThreads + threadIdx.x) / 32;
+    const uint64_t row = w / P.pieces;
+    if (row >= P.tokens.n) return;
+    const int lane = threadIdx.x & 31, col = static_cast<int>(w - row * P.pieces) * 32 * kOddValues + lane;
+    const int64_t token = P.tokens.load(static_cast<uint32_t>(row));
+    const bool valid = token >= 0 && token < P.tokens.rows;
+    if (!valid && P.error && col == 0) set_error(P.error, CB_ERR_INDEX_OOB);
+    const char* from = static_cast<const char*>(P.table) + (token * P.row_stride + col) * dtype_bytes(IN);
+    char* to = static_cast<char*>(P.out) + (P.out_at.at(static_cast<uint32_t>(row)) + col) * dtype_bytes(OUT);
+    Piece<IN, 1> x[kOddValues];
+#pragma unroll
+    for (int k = 0; k < kOddValues; ++k)
+        x[k] = valid && col + 32 * k < dim ? load_piece<IN, 1>(from + 32 * k * dtype_bytes(IN)) : zero_piece<IN, 1>();
+#pragma unroll
+    for (int k = 0; k < kOddValues; ++k) {
+        if (col + 32 * k < dim) {
+            float f[1];
+            widen<IN, 1>(x[k], f);
+            f[0] *= P.scale;
+            store_piece<OUT, 1>(to + 32 * k * dtype_bytes(OUT), f);
+        }
+    }
+}
+template <int IN, int OUT>
+void launch_lookup_odd(LookupArgs P, int32_t dim, cudaStream_t s) {
+    P.pieces = static_cast<uint32_t>((dim + 32 * kOddValues - 1) / (32 * kOddValues));
+    const uint64_t warps = static_cast<uint64_t>(P.tokens.n) * P.pieces, per = kLookupThreads / 32;
+    launch(token_lookup_odd_kernel<IN, OUT>, dim3(static_cast<unsigned>((warps + per - 1) / per)), dim3(kLookupThreads), 0,
+           s, P, dim);
+}
+
 template <int IN, int OUT, int V>
 void launch_lookup(LookupArgs P, int32_t dim, cudaStream_t s) {
     P.pieces = static_cast<uint32_t>(dim / V);
@@ -91,7 +130,7 @@ template <int IN, int OUT>
 void launch_lookup(const LookupArgs& P, int32_t dim, int v, cudaStream_t s) {
     if (v == 8) launch_lookup<IN, OUT, 8>(P, dim, s);
     else if (v == 4) launch_lookup<IN, OUT, 4>(P, dim, s);
-    else launch_lookup<IN, OUT, 1>(P, dim, s);
+    else launch_lookup_odd<IN, OUT>(P, dim, s);
 }
 template <int IN>
 void launch_lookup(const LookupArgs& P, int32_t dim, int v, int out_dtype, cudaStream_t s) {

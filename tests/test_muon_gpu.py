@@ -103,6 +103,17 @@ def test_stacks_are_their_matrices(batch, m, n):
             check(got[i], reference(g[i]), tolerance(BF16))
 
 
+@pytest.mark.parametrize("batch,m,n", [(40, 144, 1600), (9, 300, 3200), (12, 200, 3100)])
+def test_long_rows_give_the_same_bits_alone_and_in_a_stack(batch, m, n):
+    # The sum over a long side is shared by blocks, or not, by the number of matrices.
+    g = _updates((batch, m, n), BF16, 30)
+    got = mu().newton_schulz(g)
+    for i in (0, batch - 1):
+        assert torch.equal(got[i], mu().newton_schulz(g[i]))
+        assert torch.equal(got[i].t(), mu().newton_schulz(g[i].t().contiguous()))
+    check(got[0], reference(g[0]), tolerance(BF16))
+
+
 @pytest.mark.parametrize("m,n", [(60, 130), (300, 520)])
 def test_transposes_and_strides(m, n):
     g = _updates((m, n), F32, 6)
