@@ -21,7 +21,8 @@ namespace {
 // that load the next tokens ahead (more registers, fewer warps).
 constexpr int kLookupThreads = 128;
 constexpr int kLookupBlocks = 16;
-constexpr int kLookupPieces = 4;  // pieces in flight per thread
+// Pieces in flight per thread; 8 fp32 values are two loads.
+template <int IN, int V> constexpr int kLookupPieces = IN == CB_F32 && V == 8 ? 2 : 4;
 
 struct LookupArgs {
     Tokens tokens;
@@ -39,15 +40,16 @@ struct LookupArgs {
 // are consecutive, and each thread has its loads in flight together.
 template <int IN, int OUT, int V>
 __global__ void __launch_bounds__(kLookupThreads, kLookupBlocks) token_lookup_kernel(const LookupArgs P) {
+    constexpr int kPieces = kLookupPieces<IN, V>;
     begin_kernel();
-    const uint64_t first = static_cast<uint64_t>(blockIdx.x) * (kLookupThreads * kLookupPieces);
+    const uint64_t first = static_cast<uint64_t>(blockIdx.x) * (kLookupThreads * kPieces);
     const uint32_t row0 = static_cast<uint32_t>(first / P.pieces);
     const uint32_t within = static_cast<uint32_t>(first - static_cast<uint64_t>(row0) * P.pieces) + threadIdx.x;
-    Piece<IN, V> x[kLookupPieces];
-    uint32_t row[kLookupPieces], piece[kLookupPieces];
-    int64_t token[kLookupPieces];
+    Piece<IN, V> x[kPieces];
+    uint32_t row[kPieces], piece[kPieces];
+    int64_t token[kPieces];
 #pragma unroll
-    for (int u = 0; u < kLookupPieces; ++u) {
+    for (int u = 0; u < kPieces; ++u) {
         const uint32_t k = within + u * kLookupThreads;
         const uint32_t r = k / P.pieces;
         row[u] = row0 + r;
@@ -55,7 +57,7 @@ __global__ void __launch_bounds__(kLookupThreads, kLookupBlocks) token_lookup_ke
         token[u] = row[u] < P.tokens.n ? P.tokens.load(row[u]) : 0;
     }
 #pragma unroll
-    for (int u = 0; u < kLookupPieces; ++u) {
+    for (int u = 0; u < kPieces; ++u) {
         const bool valid = token[u] >= 0 && token[u] < P.tokens.rows;
         x[u] = zero_piece<IN, V>();
         if (row[u] < P.tokens.n) {
@@ -67,7 +69,7 @@ __global__ void __launch_bounds__(kLookupThreads, kLookupBlocks) token_lookup_ke
         }
     }
 #pragma unroll
-    for (int u = 0; u < kLookupPieces; ++u) {
+    for (int u = 0; u < kPieces; ++u) {
         if (row[u] < P.tokens.n) {
             float f[V];
             widen<IN, V>(x[u], f);
@@ -79,58 +81,66 @@ __global__ void __launch_bounds__(kLookupThreads, kLookupBlocks) token_lookup_ke
     }
 }
 
-// Rows that no vector fits (an odd number of halves, or an odd address): a warp takes 256
-// consecutive values of a row, a lane every 32nd, so that a load of 2 bytes a lane is still
-// one line, and a row's index is worked out once for 8 values a lane. (One value at a time in
-// the kernel above: 217K rows of 1613 halves 1111 us, most of it arithmetic on indices.)
-constexpr int kOddValues = 8;
-template <int IN, int OUT>
+// Rows that no vector of 4 values fits (a length or an address that is odd, or twice an odd
+// number: V = 1 or 2): a warp takes 256 V consecutive values of a row, a lane every 32nd piece
+// of V, so that loads of 2 or 4 bytes a lane are still whole lines, and a row's index is worked
+// out once for 8 pieces a lane. (One value at a time in the kernel above: 131072 rows of 1613
+// halves 600 us, most of it arithmetic on indices, and 233 so.)
+constexpr int kOddPieces = 8;
+template <int IN, int OUT, int V>
 __global__ void __launch_bounds__(kLookupThreads) token_lookup_odd_kernel(const LookupArgs P, int32_t dim) {
     begin_kernel();
     const uint64_t w = (static_cast<uint64_t>(blockIdx.x) * kLookupThreads + threadIdx.x) / 32;
     const uint64_t row = w / P.pieces;
     if (row >= P.tokens.n) return;
-    const int lane = threadIdx.x & 31, col = static_cast<int>(w - row * P.pieces) * 32 * kOddValues + lane;
+    const int lane = threadIdx.x & 31, col = (static_cast<int>(w - row * P.pieces) * 32 * kOddPieces + lane) * V;
     const int64_t token = P.tokens.load(static_cast<uint32_t>(row));
     const bool valid = token >= 0 && token < P.tokens.rows;
     if (!valid && P.error && col == 0) set_error(P.error, CB_ERR_INDEX_OOB);
     const char* from = static_cast<const char*>(P.table) + (token * P.row_stride + col) * dtype_bytes(IN);
     char* to = static_cast<char*>(P.out) + (P.out_at.at(static_cast<uint32_t>(row)) + col) * dtype_bytes(OUT);
-    Piece<IN, 1> x[kOddValues];
+    Piece<IN, V> x[kOddPieces];
 #pragma unroll
-    for (int k = 0; k < kOddValues; ++k)
-        x[k] = valid && col + 32 * k < dim ? load_piece<IN, 1>(from + 32 * k * dtype_bytes(IN)) : zero_piece<IN, 1>();
+    for (int k = 0; k < kOddPieces; ++k)
+        x[k] = valid && col + 32 * V * k < dim ? load_piece<IN, V>(from + 32 * V * k * dtype_bytes(IN)) : zero_piece<IN, V>();
 #pragma unroll
-    for (int k = 0; k < kOddValues; ++k) {
-        if (col + 32 * k < dim) {
-            float f[1];
-            widen<IN, 1>(x[k], f);
-            f[0] *= P.scale;
-            store_piece<OUT, 1>(to + 32 * k * dtype_bytes(OUT), f);
+    for (int k = 0; k < kOddPieces; ++k) {
+        if (col + 32 * V * k < dim) {
+            float f[V];
+            widen<IN, V>(x[k], f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) f[i] *= P.scale;
+            store_piece<OUT, V>(to + 32 * V * k * dtype_bytes(OUT), f);
         }
     }
 }
-template <int IN, int OUT>
+template <int IN, int OUT, int V>
 void launch_lookup_odd(LookupArgs P, int32_t dim, cudaStream_t s) {
-    P.pieces = static_cast<uint32_t>((dim + 32 * kOddValues - 1) / (32 * kOddValues));
+    P.pieces = static_cast<uint32_t>((dim + 32 * V * kOddPieces - 1) / (32 * V * kOddPieces));
     const uint64_t warps = static_cast<uint64_t>(P.tokens.n) * P.pieces, per = kLookupThreads / 32;
-    launch(token_lookup_odd_kernel<IN, OUT>, dim3(static_cast<unsigned>((warps + per - 1) / per)), dim3(kLookupThreads), 0,
-           s, P, dim);
+    launch(token_lookup_odd_kernel<IN, OUT, V>, dim3(static_cast<unsigned>((warps + per - 1) / per)), dim3(kLookupThreads),
+           0, s, P, dim);
 }
 
 template <int IN, int OUT, int V>
 void launch_lookup(LookupArgs P, int32_t dim, cudaStream_t s) {
     P.pieces = static_cast<uint32_t>(dim / V);
     const uint64_t total = static_cast<uint64_t>(P.tokens.n) * P.pieces;
-    const uint64_t per = kLookupThreads * kLookupPieces;
+    const uint64_t per = kLookupThreads * kLookupPieces<IN, V>;
     launch(token_lookup_kernel<IN, OUT, V>, dim3(static_cast<unsigned>((total + per - 1) / per)), dim3(kLookupThreads), 0,
            s, P);
 }
 template <int IN, int OUT>
 void launch_lookup(const LookupArgs& P, int32_t dim, int v, cudaStream_t s) {
-    if (v == 8) launch_lookup<IN, OUT, 8>(P, dim, s);
-    else if (v == 4) launch_lookup<IN, OUT, 4>(P, dim, s);
-    else launch_lookup_odd<IN, OUT>(P, dim, s);
+    if constexpr (IN != CB_F32 || OUT != CB_F32) {
+        if (v == 8) {
+            launch_lookup<IN, OUT, 8>(P, dim, s);
+            return;
+        }
+    }
+    if (v == 4) launch_lookup<IN, OUT, 4>(P, dim, s);
+    else if (v == 2) launch_lookup_odd<IN, OUT, 2>(P, dim, s);
+    else launch_lookup_odd<IN, OUT, 1>(P, dim, s);
 }
 template <int IN>
 void launch_lookup(const LookupArgs& P, int32_t dim, int v, int out_dtype, cudaStream_t s) {
@@ -156,7 +166,7 @@ struct GradArgs {
 };
 
 // The columns of a lane in a slab of a row: J pieces of V values, 32 pieces apart.
-template <int V> constexpr int kLanePieces = V == 1 ? 4 : 1;
+template <int V> constexpr int kLanePieces = V <= 2 ? 4 : 1;
 template <int V> constexpr int kSlab = 32 * V * kLanePieces<V>;
 template <int DT, int V>
 struct LanePieces {
@@ -204,6 +214,8 @@ struct Sum {
             if (col + j * 32 * V >= dim) break;
             if constexpr (V == 1) {
                 *p = f[j][0];
+            } else if constexpr (V == 2) {
+                *reinterpret_cast<float2*>(p) = make_float2(f[j][0], f[j][1]);
             } else {
 #pragma unroll
                 for (int i = 0; i < V; i += 4)
@@ -218,6 +230,10 @@ struct Sum {
             if (col + j * 32 * V >= dim) break;
             if constexpr (V == 1) {
                 f[j][0] += *p;
+            } else if constexpr (V == 2) {
+                const float2 x = *reinterpret_cast<const float2*>(p);
+                f[j][0] += x.x;
+                f[j][1] += x.y;
             } else {
 #pragma unroll
                 for (int i = 0; i < V; i += 4) {
@@ -392,7 +408,8 @@ static_assert(kKeysPerThread * kKeyThreads == kSortTileKeys && kKeyThreads >= kR
 // Pairs (key, position), a tile of the sort per block, with the first pass's digit counts of
 // the tile; the later passes' counts are cleared, and the sort's description of its one
 // "table" (keys from 0) and tiles written. `touched` (cleared before, or null) gets a 1 for
-// every row with a token.
+// every row with a token: a table of the tile's latest keys keeps most of a hot token's stores
+// from being made, which all go to one place (131072 skewed tokens: 16 -> 6 us).
 struct SortBuffers {
     uint32_t *keys[2], *positions[2];
     Chunk* tiles;
@@ -402,8 +419,10 @@ struct SortBuffers {
     uint8_t* touched;  // [rows], padded to 8
 };
 __global__ void __launch_bounds__(kKeyThreads) token_keys_kernel(const GradArgs P, const SortBuffers S, int passes) {
-    __shared__ uint32_t sh[kRadixDigits];
+    constexpr int kSeen = 4096;
+    __shared__ uint32_t sh[kRadixDigits], seen[kSeen];
     if (threadIdx.x < kRadixDigits) sh[threadIdx.x] = 0;
+    for (int i = threadIdx.x; i < kSeen; i += kKeyThreads) seen[i] = ~0u;
     begin_kernel();
     const uint32_t n = P.tokens.n, tile = blockIdx.x, tiles = gridDim.x;
     const uint32_t first = tile * static_cast<uint32_t>(kSortTileKeys);
@@ -423,7 +442,13 @@ __global__ void __launch_bounds__(kKeyThreads) token_keys_kernel(const GradArgs 
             S.keys[0][first + k] = key;
             S.positions[0][first + k] = first + k;
             atomicAdd(&sh[key & (kRadixDigits - 1)], 1u);
-            if (S.touched && key < P.tokens.rows) S.touched[key] = 1;  // by any number of threads: one value
+            if (S.touched && key < P.tokens.rows) {
+                volatile uint32_t* last = seen + (key & (kSeen - 1));
+                if (*last != key) {
+                    *last = key;
+                    S.touched[key] = 1;  // by any number of threads: one value
+                }
+            }
         }
     }
     __syncthreads();
@@ -562,7 +587,6 @@ __global__ void __launch_bounds__(kReduceThreads) token_join_kernel(const GradAr
     __shared__ __align__(16) float part[kReduceWarps][kSlab<V>];
     begin_kernel();
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    const uint32_t n = P.tokens.n;
     const uint32_t chunk0 = blockIdx.x / slabs * kJoinChunks;
     const int slab = static_cast<int>(blockIdx.x % slabs), base = slab * kSlab<V>, col = base + lane * V;
     const uint32_t mine = chunk0 + lane;
@@ -780,6 +804,7 @@ template <int DT>
 void launch_grad(const GradArgs& P, const GradWorkspace& w, char* base, int v, int sms, cudaStream_t s) {
     if (v == 8) launch_grad<DT, 8>(P, w, base, sms, s);
     else if (v == 4) launch_grad<DT, 4>(P, w, base, sms, s);
+    else if (v == 2) launch_grad<DT, 2>(P, w, base, sms, s);
     else launch_grad<DT, 1>(P, w, base, sms, s);
 }
 
@@ -839,13 +864,13 @@ extern "C" cb_status cb_token_forward(const void* table, cb_dtype table_dtype, i
     P.out = out;
     P.scale = scale;
     P.error = error;
-    // Pieces of 8 values where one side is in 16 bits (16 bytes there), of 4 otherwise or where
-    // only 4 fit the strides and addresses, else single values.
+    // Pieces of 8 values where one side is in 16 bits (16 bytes there), of 4 otherwise, and of
+    // half as many until they fit the row, the strides and the addresses.
     const int64_t s1 = length > 1 ? out_stride : 0, s0 = sequences > 1 ? out_sequence_stride : 0;
     const int64_t table_stride = rows > 1 ? row_stride : 0;
     int v = table_dtype == CB_F32 && out_dtype == CB_F32 ? 4 : 8;
     while (v > 1 && !(takes(table, table_dtype, dim, table_stride, 0, v) && takes(out, out_dtype, dim, s0, s1, v)))
-        v = v == 8 ? 4 : 1;
+        v /= 2;
     if (table_dtype == CB_F32) launch_lookup<CB_F32>(P, dim, v, out_dtype, stream);
     else if (table_dtype == CB_F16) launch_lookup<CB_F16>(P, dim, v, out_dtype, stream);
     else launch_lookup<CB_BF16>(P, dim, v, out_dtype, stream);
@@ -895,7 +920,7 @@ extern "C" cb_status cb_token_backward(const void* grad_out, cb_dtype go_dtype, 
     const int64_t row_stride = rows > 1 ? grad_stride : 0;
     int v = go_dtype == CB_F32 && grad_dtype == CB_F32 ? 4 : 8;
     while (v > 1 && !(takes(grad_out, go_dtype, dim, s0, s1, v) && takes(grad, grad_dtype, dim, row_stride, 0, v)))
-        v = v == 8 ? 4 : 1;
+        v /= 2;
     int sms = 0;
     if (!current_sms(&sms)) return CB_ERR_CUDA;
     char* base = static_cast<char*>(workspace);

@@ -6,7 +6,7 @@
 
 namespace cbtbe {
 
-// V consecutive values of type DT at `p`, which is aligned to their size (V = 1, 4 or 8).
+// V consecutive values of type DT at `p`, which is aligned to their size (V = 1, 2, 4 or 8).
 template <int DT, int V>
 struct Piece {
     static constexpr int kBytes = V * (DT == CB_F32 ? 4 : 2);

@@ -104,6 +104,18 @@ def test_lookup_strided_operands():
     assert torch.equal(swapped.transpose(0, 1), table[tokens])
 
 
+@pytest.mark.parametrize("dim", [2, 6, 62, 66, 258, 514, 1030])
+@pytest.mark.parametrize("dtype,out", [(F32, F32), (BF16, BF16), (F16, F32), (F32, F16)])
+def test_rows_of_twice_an_odd_number(dim, dtype, out):
+    table = _randn((120, dim), dtype, 40)
+    for n in (70, 3000):
+        tokens = _randint(120, (n,), 41)
+        got = te().token_forward(table, tokens, scale=3.0, out_dtype=out)
+        assert torch.equal(got, (table[tokens].float() * 3.0).to(out))
+        go = _randn((n, dim), dtype, 42)
+        check_backward(te().token_backward(go, tokens, 120, scale=0.5, out_dtype=out), go, tokens, 120, 0.5)
+
+
 @pytest.mark.parametrize("dim", [64, 63])
 def test_lookup_out_of_range_tokens_give_zeros_and_an_error(dim):
     table = _randn((20, dim), F32, 7)
