@@ -103,6 +103,18 @@ def test_stacks_are_their_matrices(batch, m, n):
             check(got[i], reference(g[i]), tolerance(BF16))
 
 
+@pytest.mark.parametrize("batch,m,n", [(170, 64, 100), (3, 100, 384), (2, 100, 385), (5, 70, 1500), (2, 120, 3000),
+                                       (2, 100, 3300)])
+def test_narrow_stacks(batch, m, n):
+    # One block per matrix (of 256 or 512 threads), clusters of 2, 4 and 8, and beyond them.
+    g = _updates((batch, m, n), BF16, 31, "low")
+    got = mu().newton_schulz(g)
+    for i in (0, batch - 1):
+        assert torch.equal(got[i], mu().newton_schulz(g[i]))
+        check(got[i], reference(g[i]), tolerance(BF16))
+    assert torch.equal(mu().newton_schulz(g.mT.contiguous()).mT, got)
+
+
 @pytest.mark.parametrize("batch,m,n", [(40, 144, 1600), (9, 300, 3200), (12, 200, 3100)])
 def test_long_rows_give_the_same_bits_alone_and_in_a_stack(batch, m, n):
     # The sum over a long side is shared by blocks, or not, by the number of matrices.
