@@ -52,26 +52,44 @@ __device__ __forceinline__ Tile tile_at(const ProductArgs& P, int64_t t) {
     return T;
 }
 
-__device__ __forceinline__ void unpack_halves(const uint4* p, float (&v)[32]) {
+// 32 halves of a lane's row in two accesses of 32 bytes: whole sectors, where halves of them
+// would be fetched twice (the shared memory of these kernels leaves little for L1) and written in two.
+struct Halves {
+    uint32_t w[16];
+};
+__device__ __forceinline__ Halves load_halves(const __half* p) {
+    Halves h;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        float f[8];
-        unpack<CB_F16>(p[k], f);
+    for (int k = 0; k < 16; k += 8)
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(h.w[k]), "=r"(h.w[k + 1]), "=r"(h.w[k + 2]), "=r"(h.w[k + 3]), "=r"(h.w[k + 4]),
+                       "=r"(h.w[k + 5]), "=r"(h.w[k + 6]), "=r"(h.w[k + 7])
+                     : "l"(p + 2 * k)
+                     : "memory");
+    return h;
+}
+__device__ __forceinline__ void unpack_halves(const Halves& h, float (&v)[32]) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[8 * k + e] = f[e];
+    for (int k = 0; k < 16; ++k) {
+        __half2 x;
+        memcpy(&x, &h.w[k], 4);
+        const float2 f = __half22float2(x);
+        v[2 * k] = f.x;
+        v[2 * k + 1] = f.y;
     }
 }
 __device__ __forceinline__ void store_halves(__half* p, const float (&v)[32]) {
+    uint32_t w[16];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        uint32_t w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const __half2 h = __floats2half2_rn(v[8 * k + 2 * e], v[8 * k + 2 * e + 1]);
-            memcpy(&w[e], &h, 4);
-        }
-        reinterpret_cast<uint4*>(p)[k] = make_uint4(w[0], w[1], w[2], w[3]);
+    for (int k = 0; k < 16; ++k) {
+        const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+        memcpy(&w[k], &h, 4);
     }
+#pragma unroll
+    for (int k = 0; k < 16; k += 8)
+        asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(w[k]), "r"(w[k + 1]), "r"(w[k + 2]),
+                     "r"(w[k + 3]), "r"(w[k + 4]), "r"(w[k + 5]), "r"(w[k + 6]), "r"(w[k + 7]), "l"(p + 2 * k)
+                     : "memory");
 }
 
 // 16 columns of a warp's 32 rows into the caller's matrix, through shared memory so that
@@ -132,20 +150,14 @@ __device__ __forceinline__ void finish_result(const ProductArgs& P, int batch, i
 
 // What the result at a lane's 32 columns has added to it: loaded a turn ahead of its use.
 struct Term {
-    uint4 hi[4], lo[4];
+    Halves hi, lo;
 };
 template <Product WHAT>
 __device__ __forceinline__ void load_term(const ProductArgs& P, int batch, int row, int col, Term& t) {
     if (row >= P.m || col >= P.n || WHAT == kGram || (WHAT != kPoly && P.a == 0.f)) return;
     const int64_t at = batch * P.term_batch + static_cast<int64_t>(row) * P.term_ld + col;
-    const uint4* hi = reinterpret_cast<const uint4*>(P.term_hi + at);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) t.hi[k] = hi[k];
-    if (WHAT != kPoly && P.term_lo) {
-        const uint4* lo = reinterpret_cast<const uint4*>(P.term_lo + at);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) t.lo[k] = lo[k];
-    }
+    t.hi = load_halves(P.term_hi + at);
+    if (WHAT != kPoly && P.term_lo) t.lo = load_halves(P.term_lo + at);
 }
 
 // 32 columns [col, col + 32) of row `row` of a tile's result: `v` holds the products' sums.
