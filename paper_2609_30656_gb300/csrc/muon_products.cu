@@ -678,11 +678,13 @@ bool launch_pairs(const CUtensorMap& left, const CUtensorMap& right, ProductArgs
 // The tiles with the least time, in clocks: rounds of tiles over the GPU, each the steps of 64
 // of K that it takes, and what a kernel takes besides. Fitted to all three products at sizes
 // of 200 to 4096, each with tiles of one kind forced, in clocks a step: 590 (128 x 64), 630 (128
-// x 128), 654 to 692 (256 x 160 to 256 by a pair; about 700 at any width where B is MN-major; the
-// tensor cores need 320 to 512 of them: shared memory and the way there bound it). Whole calls
-// with the kind chosen, and with the best single kind: 1024 x 1024 138 us (64 wide), 4 x 1024 x
-// 1024 201 us (128; 223 by pairs, 279 at 64), 2048 x 2048 283 us, 4096 x 4096 1060 us (pairs;
-// 1661 at 128, 2860 at 64).
+// x 128), 654 to 692 (256 x 160 to 256 by a pair; about 700 at any width where B is MN-major, and
+// the narrowest of as many rounds is best by a little); the tensor cores need 128, 256 and 320 to
+// 512 of them: an SM takes in some 55 bytes a clock. The choice was within 7 us of the best
+// single kind for each of the products in all of 16 sizes. What others would cost there, for
+// five steps: 1024 x 1024 137 us (64 wide; 143 with 128 and 156 with pairs in the update alone), 4 x
+// 1024 x 1024 181 us (128 and pairs; 234 at 64, 191 at 128), 2048 x 2048 259 us (290 at 128, 380
+// at 64).
 template <Product WHAT>
 bool launch_best(const Operand& left, const Operand& right, const ProductArgs& P, int sms, cudaStream_t s) {
     const int64_t ksteps = (P.k + kTileK - 1) / kTileK;
@@ -705,7 +707,7 @@ bool launch_best(const Operand& left, const Operand& right, const ProductArgs& P
     for (int w = 160; w <= kPairWidth; w += 32) {
         const int64_t t = kSymmetric<WHAT> ? time(kPairM, w, sms / 2, 590 + 2 * w / 5, 6000 + 30 * w)
                                            : time(kPairM, w, sms / 2, 700, 13700);
-        if (t < best || (pair && t == best)) best = t, width = w, pair = true;
+        if (t < best) best = t, width = w, pair = true;
     }
     if (pair) return launch_pairs<WHAT>(left.box128, kSymmetric<WHAT> ? right.box128 : right.box64, P, width, sms, s);
     if (width == 128) return launch_tiles<128, WHAT>(left.box64, right.box64, P, sms, s);
