@@ -134,8 +134,8 @@ __device__ __forceinline__ float2 inverse_norm(const SquareSum* partial, int blo
 constexpr int kCastTile = 64;
 
 // X_0 = kScaleX u / (||u|| + eps) as hi + lo, [p, ld] rows: u as it lies, or transposed.
-// A block takes a 64 x 64 tile of u, a thread four times 4 consecutive values of it (V = 4: in
-// one load each) and of X, one row of tiles after another: blocks (column tile, first row tile,
+// A block takes a 64 x 64 tile of u, a thread 16 values of it in runs of 4, or of 8 (V = 4 or 8: in
+// one load or two each), and of X, one row of tiles after another: blocks (column tile, first row tile,
 // matrix). Rows of X are padded to 64 values, so its tiles are stored whole along a row.
 template <bool TRANSPOSED, int V>
 __global__ void __launch_bounds__(256, 4) muon_cast_kernel(MatrixIn in, const SquareSum* __restrict__ partial, int norm_blocks,
@@ -146,24 +146,25 @@ __global__ void __launch_bounds__(256, 4) muon_cast_kernel(MatrixIn in, const Sq
     const int b = blockIdx.z, c0 = blockIdx.x * kCastTile;
     const char* g = static_cast<const char*>(in.g) + b * in.g_batch * dtype_bytes(in.dtype);
     const float* mom = in.momentum ? in.momentum + b * in.m_batch : nullptr;
-    const int c = (threadIdx.x & 15) * 4, rq = threadIdx.x >> 4;
+    constexpr int N = V == 8 ? 8 : 4, R = 16 / N, kLanes = kCastTile / N, kDown = 256 / kLanes;  // R runs of N values
+    const int c = threadIdx.x % kLanes * N, rq = threadIdx.x / kLanes;
     float2 f = make_float2(0.f, 0.f);
     for (int r0 = blockIdx.y * kCastTile; r0 < in.rows; r0 += gridDim.y * kCastTile) {
-        float v[4][4], m[4][4];
+        float v[R][N], m[R][N];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int64_t row = r0 + rq + 16 * k;
+        for (int k = 0; k < R; ++k) {
+            const int64_t row = r0 + rq + kDown * k;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[k][e] = m[k][e] = 0.f;
+            for (int e = 0; e < N; ++e) v[k][e] = m[k][e] = 0.f;
             if (row >= in.rows) continue;
-            if constexpr (V == 4) {
+            if constexpr (V > 1) {
                 if (c0 + c < in.cols) {
-                    load_values<4>(g, row * in.g_row + c0 + c, in.dtype, v[k]);
-                    if (mom) load_values<4>(mom, row * in.m_row + c0 + c, CB_F32, m[k]);
+                    load_values<V>(g, row * in.g_row + c0 + c, in.dtype, v[k]);
+                    if (mom) load_values<V>(mom, row * in.m_row + c0 + c, CB_F32, m[k]);
                 }
             } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
+                for (int e = 0; e < N; ++e)
                     if (c0 + c + e < in.cols) {
                         v[k][e] = load_value(g, row * in.g_row + c0 + c + e, in.dtype);
                         if (mom) m[k][e] = mom[row * in.m_row + c0 + c + e];
@@ -172,45 +173,50 @@ __global__ void __launch_bounds__(256, 4) muon_cast_kernel(MatrixIn in, const Sq
         }
         if (mom) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < R; ++k)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[k][e] = in.nesterov ? mix_momentum(m[k][e], v[k][e], in.beta) : m[k][e];
+                for (int e = 0; e < N; ++e) v[k][e] = in.nesterov ? mix_momentum(m[k][e], v[k][e], in.beta) : m[k][e];
         }
         if (r0 == static_cast<int>(blockIdx.y) * kCastTile)  // behind the first tile's loads
             f = inverse_norm(partial + static_cast<int64_t>(b) * kNormBlocks, norm_blocks, eps);
-        auto put = [&](int64_t at, const float (&x)[4]) {
-            uint32_t h[2], l[2];
+        auto put = [&](int64_t at, const float (&x)[N]) {
+            uint32_t h[N / 2], l[N / 2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
+            for (int e = 0; e < N / 2; ++e) {
                 const __half2 top = __floats2half2_rn(x[2 * e], x[2 * e + 1]);
                 const float2 back = __half22float2(top);
                 const __half2 rest = __floats2half2_rn(x[2 * e] - back.x, x[2 * e + 1] - back.y);
                 memcpy(&h[e], &top, 4);
                 memcpy(&l[e], &rest, 4);
             }
-            *reinterpret_cast<uint2*>(hi + at) = make_uint2(h[0], h[1]);
-            *reinterpret_cast<uint2*>(lo + at) = make_uint2(l[0], l[1]);
+            if constexpr (N == 8) {
+                *reinterpret_cast<uint4*>(hi + at) = make_uint4(h[0], h[1], h[2], h[3]);
+                *reinterpret_cast<uint4*>(lo + at) = make_uint4(l[0], l[1], l[2], l[3]);
+            } else {
+                *reinterpret_cast<uint2*>(hi + at) = make_uint2(h[0], h[1]);
+                *reinterpret_cast<uint2*>(lo + at) = make_uint2(l[0], l[1]);
+            }
         };
         const int64_t base = b * x_batch;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int row = r0 + rq + 16 * k;
-            float x[4];
+        for (int k = 0; k < R; ++k) {
+            const int row = r0 + rq + kDown * k;
+            float x[N];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
+            for (int e = 0; e < N; ++e) {
                 x[e] = (v[k][e] * f.x) * f.y;
-                if constexpr (TRANSPOSED) tile[rq + 16 * k][c + e] = x[e];
+                if constexpr (TRANSPOSED) tile[rq + kDown * k][c + e] = x[e];
             }
             if (!TRANSPOSED && row < in.rows) put(base + static_cast<int64_t>(row) * ld + c0 + c, x);
         }
         if constexpr (TRANSPOSED) {
             __syncthreads();
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int col = c0 + rq + 16 * k;  // value (row, col) of u is X[col, row]
-                float x[4];
+            for (int k = 0; k < R; ++k) {
+                const int col = c0 + rq + kDown * k;  // value (row, col) of u is X[col, row]
+                float x[N];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = tile[c + e][rq + 16 * k];
+                for (int e = 0; e < N; ++e) x[e] = tile[c + e][rq + kDown * k];
                 if (col < in.cols) put(base + static_cast<int64_t>(col) * ld + r0 + c, x);
             }
             __syncthreads();
@@ -353,8 +359,10 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
                          batch);
     const int64_t x_batch = w.p * w.ldx, a_batch = w.p * w.lda;
     const int ldx = static_cast<int>(w.ldx), lda = static_cast<int>(w.lda);
-    auto cast = tall ? (vector ? muon_cast_kernel<true, 4> : muon_cast_kernel<true, 1>)
-                     : (vector ? muon_cast_kernel<false, 4> : muon_cast_kernel<false, 1>);
+    auto cast = tall ? (wide ? muon_cast_kernel<true, 8> : vector ? muon_cast_kernel<true, 4> : muon_cast_kernel<true, 1>)
+                     : (wide     ? muon_cast_kernel<false, 8>
+                        : vector ? muon_cast_kernel<false, 4>
+                                 : muon_cast_kernel<false, 1>);
     launch(cast, cast_grid, dim3(256), 0, s, in, static_cast<const SquareSum*>(partial), norm_blocks, eps, hi[0], lo[0], ldx,
            x_batch);
 
