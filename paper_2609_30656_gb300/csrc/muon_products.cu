@@ -9,7 +9,15 @@ namespace {
 
 constexpr int kTileM = 128, kTileK = 64;
 constexpr int kEpilogueWarps = 8;  // two for each quarter of TMEM's lanes, every other 32 columns each
-constexpr int kProductThreads = (kEpilogueWarps + 2) * 32;  // + a copying warp, + a multiplying warp
+// Two warps copy, every other stage each: waiting for a stage, arming its barrier and issuing its
+// copies takes a thread 107 + 58 + 66 clocks a copy. The multiplying warp's loop counts as much:
+// it runs as a whole and elects a lane to issue, so that operands are in registers that the warp
+// shares, adds to descriptors built once, and tests the next stage's barrier while it issues. With
+// one lane in a branch that built them (250 clocks to issue four products, 98 to see a barrier,
+// 85 to commit) a step of 64 of K took 600 clocks at any width: five steps of 1024 x 1024 137
+// us and 110 so, of 2048 x 2048 257 and 219, of 4 x 1024 x 4096 386 and 333.
+constexpr int kCopyWarps = 2, kMultiplyWarp = kEpilogueWarps + kCopyWarps;
+constexpr int kProductThreads = (kMultiplyWarp + 1) * 32;
 constexpr uint32_t kBoxBytes = 64 * 64 * 2;                 // 64 rows of 64 fp16
 template <int BN> constexpr int kStages = BN == 128 ? 6 : 8;
 // Sums of a tile in TMEM: two of its width, or of every part's.
@@ -271,7 +279,7 @@ muon_product_kernel(const __grid_constant__ CUtensorMap left, const __grid_const
     __shared__ uint64_t full[S], empty[S], ready[2], drained[2];
     __shared__ uint32_t tmem_at;
     __shared__ __align__(16) float stage[WHAT == kResult ? kEpilogueWarps * kStageFloats : 4];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
             tc::barrier_init(tc::smem_addr(full + s), 1);
@@ -296,13 +304,14 @@ muon_product_kernel(const __grid_constant__ CUtensorMap left, const __grid_const
     const int per = kSums > BN ? (ksteps + P.parts - 1) / P.parts : ksteps;  // of a part
     bool ok = true;
 
-    if (warp == kEpilogueWarps) {
-        if (lane == 0) {  // copies
-            int s = 0;
+    if (warp >= kEpilogueWarps && warp < kMultiplyWarp) {
+        if (tc::elect()) {  // copies
+            int s = warp - kEpilogueWarps, first = s;  // stage, and step of K, of the block's next tile
             uint32_t phase = 0;
             for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
                 const Tile T = tile_at<kTileM, WHAT>(P, t);
-                for (int k = 0; k < ksteps; ++k) {
+                int k = first;
+                for (; k < ksteps; k += kCopyWarps) {
                     if (!(ok = tc::barrier_wait(tc::smem_addr(empty + s), phase ^ 1))) break;
                     const uint32_t bar = tc::smem_addr(full + s);
                     uint32_t at = tc::smem_addr(ring) + s * kStageBytes<BN>;
@@ -315,46 +324,53 @@ muon_product_kernel(const __grid_constant__ CUtensorMap left, const __grid_const
                         if constexpr (kSymmetric<WHAT>) tc::tma_load(at, &right, bar, k * kTileK, T.j * BN + x * 64, T.b);
                         else tc::tma_load(at, &right, bar, T.j * BN + x * 64, k * kTileK, T.b);
                     }
-                    if (++s == S) s = 0, phase ^= 1;
+                    if ((s += kCopyWarps) >= S) s -= S, phase ^= 1;
                 }
+                first = k - ksteps;
             }
             // Copies in flight land before the block's shared memory goes away: those of
             // stages that were never multiplied, after a wait that ran out.
             if (!ok)
-                for (int x = 0; x < S; ++x) {
-                    if (--s < 0) s = S - 1, phase ^= 1;
+                for (int x = 0; x < S; x += kCopyWarps) {
+                    if ((s -= kCopyWarps) < 0) s += S, phase ^= 1;
                     if (!tc::barrier_wait(tc::smem_addr(full + s), phase)) break;
                 }
         }
-    } else if (warp == kEpilogueWarps + 1) {
-        if (lane == 0) {  // products
-            constexpr uint32_t shape = tc::mma_shape(kTileM, BN, !kSymmetric<WHAT>);
-            int s = 0, acc = 0;
-            uint32_t phase = 0, acc_phase = 0;
-            for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
-                if (!(ok = tc::barrier_wait(tc::smem_addr(drained + acc), acc_phase ^ 1))) break;
+    } else if (warp == kMultiplyWarp) {
+        // products
+        constexpr uint32_t shape = tc::mma_shape(kTileM, BN, !kSymmetric<WHAT>);
+        constexpr uint32_t step_b = kSymmetric<WHAT> ? 32 : 2048;  // of 16 of K
+        const uint32_t base = tc::smem_addr(ring);
+        const uint64_t first_a = tc::operand_k_major(base);
+        const uint64_t first_b = kSymmetric<WHAT> ? tc::operand_k_major(base + kTileM * kTileK * 2)
+                                                  : tc::operand_mn_major(base + kTileM * kTileK * 2, kBoxBytes);
+        const bool one = tc::elect();
+        int s = 0, acc = 0;
+        uint32_t phase = 0, acc_phase = 0;
+        bool here = false;  // the next stage's copies, polled while this one's products are issued
+        for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
+            if (!(ok = tc::barrier_wait(tc::smem_addr(drained + acc), acc_phase ^ 1))) break;
+            tc::fence_after();
+            uint32_t sums = tmem + acc * kSums;
+            int within = 0;  // steps done of a part
+            for (int k = 0; k < ksteps; ++k) {
+                if (!here && !(ok = tc::barrier_wait(tc::smem_addr(full + s), phase))) break;
                 tc::fence_after();
-                uint32_t sums = tmem + acc * kSums;
-                int within = 0;  // steps done of a part
-                for (int k = 0; k < ksteps; ++k) {
-                    if (!(ok = tc::barrier_wait(tc::smem_addr(full + s), phase))) break;
-                    tc::fence_after();
-                    if (kSums > BN && within == per) within = 0, sums += BN;
-                    const uint32_t at = tc::smem_addr(ring) + s * kStageBytes<BN>, bt = at + kTileM * kTileK * 2;
+                if (kSums > BN && within == per) within = 0, sums += BN;
+                const uint64_t da = tc::advance(first_a, s * kStageBytes<BN>), db = tc::advance(first_b, s * kStageBytes<BN>);
+                const uint32_t done = tc::smem_addr(empty + s);
+                if (++s == S) s = 0, phase ^= 1;
+                here = tc::barrier_test(tc::smem_addr(full + s), phase);
+                if (one) {
 #pragma unroll
-                    for (int x = 0; x < kTileK / 16; ++x) {
-                        const uint64_t da = tc::operand_k_major(at + x * 32);
-                        const uint64_t db = kSymmetric<WHAT> ? tc::operand_k_major(bt + x * 32)
-                                                            : tc::operand_mn_major(bt + x * 2048, kBoxBytes);
-                        tc::mma_f16<1>(sums, da, db, shape, within > 0 || x > 0);
-                    }
-                    ++within;
-                    tc::mma_commit<1>(tc::smem_addr(empty + s));
-                    if (++s == S) s = 0, phase ^= 1;
+                    for (int x = 0; x < kTileK / 16; ++x)
+                        tc::mma_f16<1>(sums, tc::advance(da, x * 32), tc::advance(db, x * step_b), shape, within > 0 || x > 0);
+                    tc::mma_commit<1>(done);
+                    if (k + 1 == ksteps) tc::mma_commit<1>(tc::smem_addr(ready + acc));
                 }
-                tc::mma_commit<1>(tc::smem_addr(ready + acc));
-                if (++acc == 2) acc = 0, acc_phase ^= 1;
+                ++within;
             }
+            if (++acc == 2) acc = 0, acc_phase ^= 1;
         }
     } else {  // epilogue
         int acc = 0;
@@ -399,7 +415,7 @@ muon_pair_kernel(const __grid_constant__ CUtensorMap left, const __grid_constant
     __shared__ uint64_t full[S], empty[S], ready[2], drained[2];
     __shared__ uint32_t tmem_at;
     __shared__ __align__(16) float stage[WHAT == kResult ? kEpilogueWarps * kStageFloats : 4];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const int rank = static_cast<int>(tc::cluster_rank());
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
@@ -425,14 +441,15 @@ muon_pair_kernel(const __grid_constant__ CUtensorMap left, const __grid_constant
     const int ksteps = (P.k + kTileK - 1) / kTileK, half = P.width / 2;
     bool ok = true;
 
-    if (warp == kEpilogueWarps) {
-        if (lane == 0) {  // copies
-            int s = 0;
+    if (warp >= kEpilogueWarps && warp < kMultiplyWarp) {
+        if (tc::elect()) {  // copies
+            int s = warp - kEpilogueWarps, k0 = s;  // stage, and step of K, of the pair's next tile
             uint32_t phase = 0;
             for (int64_t t = first; t < total && ok; t += step) {
                 const Tile T = tile_at<kPairM, WHAT>(P, t);
                 const int row = T.i * kPairM + rank * 128, col = T.j * P.width + rank * half;
-                for (int k = 0; k < ksteps; ++k) {
+                int k = k0;
+                for (; k < ksteps; k += kCopyWarps) {
                     if (!(ok = tc::barrier_wait(tc::smem_addr(empty + s), phase ^ 1))) break;
                     const uint32_t bar = tc::in_first_block(tc::smem_addr(full + s));
                     uint32_t at = tc::smem_addr(ring) + s * kPairStageBytes;
@@ -445,38 +462,47 @@ muon_pair_kernel(const __grid_constant__ CUtensorMap left, const __grid_constant
                         tc::tma_load_pair(at, &right, bar, col, k * kTileK, T.b);
                         tc::tma_load_pair(at + kBoxBytes, &right, bar, col + 64, k * kTileK, T.b);
                     }
-                    if (++s == S) s = 0, phase ^= 1;
+                    if ((s += kCopyWarps) >= S) s -= S, phase ^= 1;
                 }
+                k0 = k - ksteps;
             }
             if (!ok && rank == 0)  // copies in flight land before the blocks' shared memory goes away
-                for (int x = 0; x < S; ++x) {
-                    if (--s < 0) s = S - 1, phase ^= 1;
+                for (int x = 0; x < S; x += kCopyWarps) {
+                    if ((s -= kCopyWarps) < 0) s += S, phase ^= 1;
                     if (!tc::barrier_wait(tc::smem_addr(full + s), phase)) break;
                 }
         }
-    } else if (warp == kEpilogueWarps + 1) {
-        if (lane == 0 && rank == 0) {  // products of both blocks
+    } else if (warp == kMultiplyWarp) {
+        if (rank == 0) {  // products of both blocks
             const uint32_t shape = tc::mma_shape(kPairM, P.width, !kSymmetric<WHAT>);
+            constexpr uint32_t step_b = kSymmetric<WHAT> ? 32 : 2048;  // of 16 of K
+            const uint32_t base = tc::smem_addr(ring);
+            const uint64_t first_a = tc::operand_k_major(base);
+            const uint64_t first_b = kSymmetric<WHAT> ? tc::operand_k_major(base + 2 * kBoxBytes)
+                                                      : tc::operand_mn_major(base + 2 * kBoxBytes, kBoxBytes);
+            const bool one = tc::elect();
             int s = 0, acc = 0;
             uint32_t phase = 0, acc_phase = 0;
+            bool here = false;  // the next stage's copies, polled while this one's products are issued
             for (int64_t t = first; t < total && ok; t += step) {
                 if (!(ok = tc::barrier_wait(tc::smem_addr(drained + acc), acc_phase ^ 1))) break;
                 tc::fence_after();
                 for (int k = 0; k < ksteps; ++k) {
-                    if (!(ok = tc::barrier_wait(tc::smem_addr(full + s), phase))) break;
+                    if (!here && !(ok = tc::barrier_wait(tc::smem_addr(full + s), phase))) break;
                     tc::fence_after();
-                    const uint32_t at = tc::smem_addr(ring) + s * kPairStageBytes, bt = at + 2 * kBoxBytes;
-#pragma unroll
-                    for (int x = 0; x < kTileK / 16; ++x) {
-                        const uint64_t da = tc::operand_k_major(at + x * 32);
-                        const uint64_t db = kSymmetric<WHAT> ? tc::operand_k_major(bt + x * 32)
-                                                             : tc::operand_mn_major(bt + x * 2048, kBoxBytes);
-                        tc::mma_f16<2>(tmem + acc * kPairWidth, da, db, shape, k > 0 || x > 0);
-                    }
-                    tc::mma_commit<2>(tc::smem_addr(empty + s));
+                    const uint64_t da = tc::advance(first_a, s * kPairStageBytes), db = tc::advance(first_b, s * kPairStageBytes);
+                    const uint32_t done = tc::smem_addr(empty + s);
                     if (++s == S) s = 0, phase ^= 1;
+                    here = tc::barrier_test(tc::smem_addr(full + s), phase);
+                    if (one) {
+#pragma unroll
+                        for (int x = 0; x < kTileK / 16; ++x)
+                            tc::mma_f16<2>(tmem + acc * kPairWidth, tc::advance(da, x * 32), tc::advance(db, x * step_b), shape,
+                                           k > 0 || x > 0);
+                        tc::mma_commit<2>(done);
+                        if (k + 1 == ksteps) tc::mma_commit<2>(tc::smem_addr(ready + acc));
+                    }
                 }
-                tc::mma_commit<2>(tc::smem_addr(ready + acc));
                 if (++acc == 2) acc = 0, acc_phase ^= 1;
             }
         }
@@ -513,7 +539,7 @@ muon_split_kernel(const __grid_constant__ CUtensorMap rows, const ProductArgs P)
     float* sums = reinterpret_cast<float*>(ring);  // [128][64], once the products are done
     __shared__ uint64_t full[S], empty[S], ready;
     __shared__ uint32_t tmem_at;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
             tc::barrier_init(tc::smem_addr(full + s), 1);
@@ -535,10 +561,10 @@ muon_split_kernel(const __grid_constant__ CUtensorMap rows, const ProductArgs P)
     const int first = rank * per, count = max(0, min(per, all - first));
     bool ok = true;
 
-    if (warp == kEpilogueWarps) {
-        if (lane == 0) {  // copies
-            int k = 0;
-            for (; k < count; ++k) {
+    if (warp >= kEpilogueWarps && warp < kMultiplyWarp) {
+        if (tc::elect()) {  // copies
+            int k = warp - kEpilogueWarps;
+            for (; k < count; k += kCopyWarps) {
                 const int s = k % S;
                 if (!(ok = tc::barrier_wait(tc::smem_addr(empty + s), (k / S & 1) ^ 1))) break;
                 const uint32_t bar = tc::smem_addr(full + s);
@@ -550,24 +576,26 @@ muon_split_kernel(const __grid_constant__ CUtensorMap rows, const ProductArgs P)
                 tc::tma_load(at + 2 * kBoxBytes, &rows, bar, x, T.j * BN, T.b);
             }
             if (!ok)  // copies in flight land before the block's shared memory goes away
-                for (int x = max(0, k - S); x < k; ++x)
-                    if (!tc::barrier_wait(tc::smem_addr(full + x % S), x / S & 1)) break;
+                for (int x = k - S; x < k; x += kCopyWarps)
+                    if (x >= 0 && !tc::barrier_wait(tc::smem_addr(full + x % S), x / S & 1)) break;
         }
-    } else if (warp == kEpilogueWarps + 1) {
-        if (lane == 0) {  // products
-            constexpr uint32_t shape = tc::mma_shape(kTileM, BN, false);
-            for (int k = 0; k < count && ok; ++k) {
-                const int s = k % S;
-                if (!(ok = tc::barrier_wait(tc::smem_addr(full + s), k / S & 1))) break;
-                tc::fence_after();
-                const uint32_t at = tc::smem_addr(ring) + s * kStageBytes<BN>, bt = at + 2 * kBoxBytes;
+    } else if (warp == kMultiplyWarp) {
+        // products
+        constexpr uint32_t shape = tc::mma_shape(kTileM, BN, false);
+        const uint64_t first_a = tc::operand_k_major(tc::smem_addr(ring)), first_b = tc::advance(first_a, 2 * kBoxBytes);
+        const bool one = tc::elect();
+        for (int k = 0; k < count && ok; ++k) {
+            const int s = k % S;
+            if (!(ok = tc::barrier_wait(tc::smem_addr(full + s), k / S & 1))) break;
+            tc::fence_after();
+            const uint64_t da = tc::advance(first_a, s * kStageBytes<BN>), db = tc::advance(first_b, s * kStageBytes<BN>);
+            if (one) {
 #pragma unroll
                 for (int x = 0; x < kTileK / 16; ++x)
-                    tc::mma_f16<1>(tmem, tc::operand_k_major(at + x * 32), tc::operand_k_major(bt + x * 32), shape,
-                                   k > 0 || x > 0);
+                    tc::mma_f16<1>(tmem, tc::advance(da, x * 32), tc::advance(db, x * 32), shape, k > 0 || x > 0);
                 tc::mma_commit<1>(tc::smem_addr(empty + s));
+                if (k + 1 == count) tc::mma_commit<1>(tc::smem_addr(&ready));
             }
-            if (ok && count > 0) tc::mma_commit<1>(tc::smem_addr(&ready));
         }
     } else {
         const int row = warp % 4 * 32 + lane, c = warp / 4 * 32;

@@ -14,6 +14,15 @@ __device__ __forceinline__ uint32_t smem_addr(const void* p) {
     return static_cast<uint32_t>(__cvta_generic_to_shared(p));
 }
 
+// One lane of the calling warp, which is converged: what it issues for all takes its operands
+// from registers that the warp shares, where a branch on the lane's number has each of them
+// moved there first.
+__device__ __forceinline__ bool elect() {
+    uint32_t on;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(on));
+    return on != 0;
+}
+
 // ---------------------------------------------------------------- mbarriers
 
 __device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) {
@@ -32,6 +41,16 @@ __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
         "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+// The same without the suspension: whether it is complete now.
+__device__ __forceinline__ bool barrier_test(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(ok)
         : "r"(bar), "r"(parity)
         : "memory");
@@ -140,6 +159,9 @@ __device__ __forceinline__ uint64_t operand_k_major(uint32_t addr) { return oper
 __device__ __forceinline__ uint64_t operand_mn_major(uint32_t addr, uint32_t block) {
     return operand(addr, block, 1024);
 }
+
+// The operand `bytes` further on in shared memory.
+__device__ __forceinline__ uint64_t advance(uint64_t operand, uint32_t bytes) { return operand + (bytes >> 4); }
 
 // fp16 x fp16 into fp32, M x N, A K-major, B K-major or MN-major.
 __host__ __device__ constexpr uint32_t mma_shape(int m, int n, bool b_mn_major) {
