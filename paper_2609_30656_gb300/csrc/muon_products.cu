@@ -704,37 +704,34 @@ bool launch_pairs(const CUtensorMap& left, const CUtensorMap& right, ProductArgs
 }
 
 // The tiles with the least time, in clocks: rounds of tiles over the GPU, each the steps of 64
-// of K that it takes, and what a kernel takes besides. Fitted to all three products at sizes
-// of 200 to 4096, each with tiles of one kind forced, in clocks a step: 590 (128 x 64), 630 (128
-// x 128), 654 to 692 (256 x 160 to 256 by a pair; about 700 at any width where B is MN-major, and
-// the narrowest of as many rounds is best by a little); the tensor cores need 128, 256 and 320 to
-// 512 of them: an SM takes in some 55 bytes a clock. The choice was within 7 us of the best
-// single kind for each of the products in all of 16 sizes. What others would cost there, for
-// five steps: 1024 x 1024 137 us (64 wide; 143 with 128 and 156 with pairs in the update alone), 4 x
-// 1024 x 1024 181 us (128 and pairs; 234 at 64, 191 at 128), 2048 x 2048 259 us (290 at 128, 380
-// at 64).
+// of K that it takes, and what a kernel takes besides (launch, first copies, last epilogue).
+// Fitted to all three products at 16 sizes of 200 to 4096, each with tiles of one kind forced: a
+// step is 320 clocks at 128 x 64 and 330 at 128 x 128 (the tensor cores need 192 and 256), and
+// two a column by pairs, which is what the tensor cores need. The choice was within 1.5 us of
+// the best kind for each of the products in nearly all. What another would cost, in five steps: 1024 x 1024
+// 110 us (64 wide; 128 in any one product 4 to 8 more, pairs of 256 17 to 25), 4 x 1024 x 1024 162 (128,
+// the update by pairs of 256; 64 in any one 6 to 20 more), 2048 x 2048 222 (the same; 64 18 to 55 more).
 template <Product WHAT>
 bool launch_best(const Operand& left, const Operand& right, const ProductArgs& P, int sms, cudaStream_t s) {
     const int64_t ksteps = (P.k + kTileK - 1) / kTileK;
     auto time = [&](int height, int width, int at_once, int64_t step, int64_t fixed) {
         return (tiles_of<WHAT>(P.m, P.n, height, width) * P.batch + at_once - 1) / at_once * ksteps * step + fixed;
     };
-    int64_t best = time(kTileM, 64, sms, 590, 7000);
+    int64_t best = time(kTileM, 64, sms, 320, 6500);
     if constexpr (WHAT == kGram) {
         if (P.parts > 1) {
             const int64_t blocks = tiles_of<kGram>(P.m, P.n, kTileM, 64) * P.batch * P.parts;
-            const int64_t split = (blocks + sms - 1) / sms * ((ksteps + P.parts - 1) / P.parts * 590 + 11000);
+            const int64_t split = (blocks + sms - 1) / sms * ((ksteps + P.parts - 1) / P.parts * 320 + 10500);
             return split < best ? launch_split(left.box64, P, s)
                                 : launch_tiles<64, WHAT>(left.box64, right.box64, P, sms, s);
         }
     }
     int width = 64;
-    const int64_t t128 = time(kTileM, 128, sms, 630, 8900);
+    const int64_t t128 = time(kTileM, 128, sms, 330, 8000);
     if (t128 < best) best = t128, width = 128;
     bool pair = false;
     for (int w = 160; w <= kPairWidth; w += 32) {
-        const int64_t t = kSymmetric<WHAT> ? time(kPairM, w, sms / 2, 590 + 2 * w / 5, 6000 + 30 * w)
-                                           : time(kPairM, w, sms / 2, 700, 13700);
+        const int64_t t = time(kPairM, w, sms / 2, 2 * w + 10, 6200 + 20 * w);
         if (t < best) best = t, width = w, pair = true;
     }
     if (pair) return launch_pairs<WHAT>(left.box128, kSymmetric<WHAT> ? right.box128 : right.box64, P, width, sms, s);
