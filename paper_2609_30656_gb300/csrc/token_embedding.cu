@@ -14,15 +14,17 @@ namespace {
 
 // ---------------------------------------------------------------- lookup
 
-// 128 threads of 4 pieces and 16 blocks per SM (32 registers a thread, every warp that an SM
-// holds): a block is a chain of a token's load, a row's load and a store, so bytes in flight
-// decide. 262144 rows of 8 KB: 450 us, 5.7 TB/s; 504 with 6 blocks of 256 threads, 462 with
-// 8, 530 with 2 or 8 pieces a thread, 526 with 32 blocks of 64, 655 with resident blocks
-// that load the next tokens ahead (more registers, fewer warps).
+// 128 threads of up to 64 bytes each and 16 blocks per SM (32 registers a thread, every warp
+// that an SM holds): a block is a chain of a token's load, a row's load and a store, so bytes
+// in flight decide. 262144 rows of 8 KB: 444 us, 5.7 TB/s. In pieces of 16 bytes: 450 us, and
+// 504 with 6 blocks of 256 threads, 462 with 8, 530 with 2 or 8 pieces a thread, 526 with 32
+// blocks of 64, 655 with resident blocks that load the next tokens ahead (more registers,
+// fewer warps). Pieces of 32 bytes on the wider side halve the arithmetic on indices per byte:
+// 131072 rows of 1024 bf16 into fp32 135 -> 125 us, 8192 of 2048 bf16 18.4 -> 16.4.
 constexpr int kLookupThreads = 128;
 constexpr int kLookupBlocks = 16;
-// Pieces in flight per thread; 8 fp32 values are two loads.
-template <int IN, int V> constexpr int kLookupPieces = IN == CB_F32 && V == 8 ? 2 : 4;
+// Pieces in flight per thread.
+template <int IN, int V> constexpr int kLookupPieces = V * (IN == CB_F32 ? 4 : 2) == 32 ? 2 : 4;
 
 struct LookupArgs {
     Tokens tokens;
@@ -132,13 +134,14 @@ void launch_lookup(LookupArgs P, int32_t dim, cudaStream_t s) {
 }
 template <int IN, int OUT>
 void launch_lookup(const LookupArgs& P, int32_t dim, int v, cudaStream_t s) {
-    if constexpr (IN != CB_F32 || OUT != CB_F32) {
-        if (v == 8) {
-            launch_lookup<IN, OUT, 8>(P, dim, s);
+    if constexpr (IN != CB_F32 && OUT != CB_F32) {
+        if (v == 16) {
+            launch_lookup<IN, OUT, 16>(P, dim, s);
             return;
         }
     }
-    if (v == 4) launch_lookup<IN, OUT, 4>(P, dim, s);
+    if (v == 8) launch_lookup<IN, OUT, 8>(P, dim, s);
+    else if (v == 4) launch_lookup<IN, OUT, 4>(P, dim, s);
     else if (v == 2) launch_lookup_odd<IN, OUT, 2>(P, dim, s);
     else launch_lookup_odd<IN, OUT, 1>(P, dim, s);
 }
@@ -821,9 +824,9 @@ bool current_sms(int* sms) {
 bool valid_dtype(int d) { return d == CB_F32 || d == CB_F16 || d == CB_BF16; }
 
 // A row-major operand whose rows are taken in pieces of v values: v divides its dim and
-// strides, and a piece is aligned to its size (at most 16 bytes).
+// strides, and a piece is aligned to its size.
 bool takes(const void* p, int dtype, int32_t dim, int64_t s0, int64_t s1, int v) {
-    const int64_t bytes = min64(16, static_cast<int64_t>(v) * dtype_bytes(dtype));
+    const int64_t bytes = static_cast<int64_t>(v) * dtype_bytes(dtype);
     return dim % v == 0 && s0 % v == 0 && s1 % v == 0 && reinterpret_cast<uintptr_t>(p) % bytes == 0;
 }
 
@@ -864,11 +867,11 @@ extern "C" cb_status cb_token_forward(const void* table, cb_dtype table_dtype, i
     P.out = out;
     P.scale = scale;
     P.error = error;
-    // Pieces of 8 values where one side is in 16 bits (16 bytes there), of 4 otherwise, and of
-    // half as many until they fit the row, the strides and the addresses.
+    // Pieces of 32 bytes on the wider side, and of half as many values until they fit the
+    // row, the strides and the addresses.
     const int64_t s1 = length > 1 ? out_stride : 0, s0 = sequences > 1 ? out_sequence_stride : 0;
     const int64_t table_stride = rows > 1 ? row_stride : 0;
-    int v = table_dtype == CB_F32 && out_dtype == CB_F32 ? 4 : 8;
+    int v = table_dtype == CB_F32 || out_dtype == CB_F32 ? 8 : 16;
     while (v > 1 && !(takes(table, table_dtype, dim, table_stride, 0, v) && takes(out, out_dtype, dim, s0, s1, v)))
         v /= 2;
     if (table_dtype == CB_F32) launch_lookup<CB_F32>(P, dim, v, out_dtype, stream);

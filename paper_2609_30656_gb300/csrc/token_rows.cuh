@@ -6,7 +6,8 @@
 
 namespace cbtbe {
 
-// V consecutive values of type DT at `p`, which is aligned to their size (V = 1, 2, 4 or 8).
+// V consecutive values of type DT at `p`, which is aligned to their size (V = 1, 2, 4, 8, or
+// 16 of 16 bits: 2 to 32 bytes).
 template <int DT, int V>
 struct Piece {
     static constexpr int kBytes = V * (DT == CB_F32 ? 4 : 2);
@@ -30,6 +31,11 @@ __device__ __forceinline__ Piece<DT, V> load_piece(const void* p) {
         const uint2 v = load_as<READ_ONLY, uint2>(p);
         x.w[0] = v.x;
         x.w[1] = v.y;
+    } else if constexpr (B == 32 && READ_ONLY) {
+        asm("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+            : "=r"(x.w[0]), "=r"(x.w[1]), "=r"(x.w[2]), "=r"(x.w[3]), "=r"(x.w[4]), "=r"(x.w[5]), "=r"(x.w[6]),
+              "=r"(x.w[7])
+            : "l"(p));
     } else {
 #pragma unroll
         for (int i = 0; i < B / 16; ++i) {
@@ -93,7 +99,11 @@ __device__ __forceinline__ void store_piece(void* p, const float (&f)[V]) {
         }
         if constexpr (B == 4) *static_cast<uint32_t*>(p) = w[0];
         else if constexpr (B == 8) __stcs(static_cast<uint2*>(p), make_uint2(w[0], w[1]));
-        else {
+        else if constexpr (B == 32) {
+            asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(w[0]), "r"(w[1]), "r"(w[2]),
+                         "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "l"(p)
+                         : "memory");
+        } else {
 #pragma unroll
             for (int i = 0; i < B / 16; ++i)
                 __stcs(static_cast<uint4*>(p) + i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));

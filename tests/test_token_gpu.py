@@ -104,6 +104,38 @@ def test_lookup_strided_operands():
     assert torch.equal(swapped.transpose(0, 1), table[tokens])
 
 
+def _rows_at(values, dtype, skip, stride):
+    """`values` in rows `stride` apart, the first `skip` values into an allocation."""
+    n, dim = values.shape
+    flat = torch.zeros(skip + n * stride, dtype=dtype, device=DEV)
+    assert flat.data_ptr() % 256 == 0
+    view = flat[skip:].view(n, stride)[:, :dim]
+    view.copy_(values)
+    return view
+
+
+@pytest.mark.parametrize("skip", [1, 2, 4, 8, 16])
+@pytest.mark.parametrize("pad", [0, 4, 8, 16])
+@pytest.mark.parametrize("dtype,out", [(F32, F32), (F32, BF16), (BF16, F32), (F16, F16), (BF16, BF16)])
+def test_bases_and_strides_of_every_alignment(skip, pad, dtype, out):
+    """Each width of piece that the base address or the stride of one operand rules out."""
+    rows, dim, n = 90, 96, 70
+    tokens = _randint(rows, (n,), 60)
+    plain = _randn((rows, dim), dtype, 61)
+    want = (plain[tokens].float() * 1.5).to(out)
+    room = torch.zeros(n, dim, dtype=out, device=DEV)
+    for table, into in [(_rows_at(plain, dtype, skip, dim + pad), room), (plain, _rows_at(room, out, skip, dim + pad))]:
+        into.fill_(7)
+        te().token_forward(table, tokens, scale=1.5, out=into)
+        assert torch.equal(into, want)
+    go = _randn((n, dim), dtype, 62)
+    grad = torch.zeros(rows, dim, dtype=out, device=DEV)
+    for g, into in [(_rows_at(go, dtype, skip, dim + pad), grad), (go, _rows_at(grad, out, skip, dim + pad))]:
+        into.fill_(7)
+        te().token_backward(g, tokens, rows, scale=1.5, out=into)
+        check_backward(into, go, tokens, rows, 1.5)
+
+
 @pytest.mark.parametrize("dim", [2, 6, 62, 66, 258, 514, 1030])
 @pytest.mark.parametrize("dtype,out", [(F32, F32), (BF16, BF16), (F16, F32), (F32, F16)])
 def test_rows_of_twice_an_odd_number(dim, dtype, out):
