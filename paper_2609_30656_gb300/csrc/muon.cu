@@ -305,6 +305,8 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
     const bool vector = vectors_of(4), wide = vectors_of(8);
     const bool user_vector = in.cols % 4 == 0 && out.row_stride % 4 == 0 && (batch == 1 || out.batch_stride % 4 == 0) &&
                              aligned(out.data, 4 * dtype_bytes(out.dtype));
+    const bool user_sectors = !tall && out.dtype != CB_F32 && in.cols % 16 == 0 && out.row_stride % 16 == 0 &&
+                              (batch == 1 || out.batch_stride % 16 == 0) && aligned(out.data, 32);
     const Workspace w = layout(batch, in.rows, in.cols);
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < static_cast<int64_t>(w.bytes)) return CB_ERR_CAPACITY;
     char* base = static_cast<char*>(workspace);
@@ -409,6 +411,7 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
             P.user_dtype = out.dtype;
             P.transposed = tall;
             P.user_vector = user_vector;
+            P.user_sectors = user_sectors;
             P.weights = out.weights;
             P.keep = out.keep;
             P.rate = out.rate;

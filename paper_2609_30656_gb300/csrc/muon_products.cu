@@ -60,20 +60,28 @@ __device__ __forceinline__ Tile tile_at(const ProductArgs& P, int64_t t) {
     return T;
 }
 
-// 32 halves of a lane's row in two accesses of 32 bytes: whole sectors, where halves of them
-// would be fetched twice (the shared memory of these kernels leaves little for L1) and written in two.
+// 32 bytes, a whole sector, of one lane: halves of them would be fetched twice (the shared
+// memory of these kernels leaves little for L1) and written in two.
+__device__ __forceinline__ void load_sector(const void* p, uint32_t* w) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(p)
+                 : "memory");
+}
+__device__ __forceinline__ void store_sector(void* p, const uint32_t* w) {
+    asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                 "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "l"(p)
+                 : "memory");
+}
+
+// 32 halves of a lane's row.
 struct Halves {
     uint32_t w[16];
 };
 __device__ __forceinline__ Halves load_halves(const __half* p) {
     Halves h;
-#pragma unroll
-    for (int k = 0; k < 16; k += 8)
-        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                     : "=r"(h.w[k]), "=r"(h.w[k + 1]), "=r"(h.w[k + 2]), "=r"(h.w[k + 3]), "=r"(h.w[k + 4]),
-                       "=r"(h.w[k + 5]), "=r"(h.w[k + 6]), "=r"(h.w[k + 7])
-                     : "l"(p + 2 * k)
-                     : "memory");
+    load_sector(p, h.w);
+    load_sector(p + 16, h.w + 8);
     return h;
 }
 __device__ __forceinline__ void unpack_halves(const Halves& h, float (&v)[32]) {
@@ -93,11 +101,53 @@ __device__ __forceinline__ void store_halves(__half* p, const float (&v)[32]) {
         const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
         memcpy(&w[k], &h, 4);
     }
+    store_sector(p, w);
+    store_sector(p + 16, w + 8);
+}
+
+// 32 columns of a lane's row into a matrix of 16 bits whose rows are whole sectors. (Through
+// shared memory a row of 16 columns is one sector that four lanes share: a step of 4 x 1024 x
+// 4096 398 us, and 364 so. Columns of 16 fp32 values are two: no faster without.)
+template <int DT>
+__device__ __forceinline__ void finish_row(const ProductArgs& P, int batch, int row, int col, float (&v)[32]) {
+    if (row >= P.m) return;
+    uint16_t* p = static_cast<uint16_t*>(P.user) + batch * P.user_batch + row * P.user_row + col;
 #pragma unroll
-    for (int k = 0; k < 16; k += 8)
-        asm volatile("st.global.v8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"r"(w[k]), "r"(w[k + 1]), "r"(w[k + 2]),
-                     "r"(w[k + 3]), "r"(w[k + 4]), "r"(w[k + 5]), "r"(w[k + 6]), "r"(w[k + 7]), "l"(p + 2 * k)
-                     : "memory");
+    for (int k = 0; k < 32; ++k) v[k] *= 1.f / kScaleX;
+    if (P.weights) {
+        uint32_t w[16];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (col + 16 * k < P.n) load_sector(p + 16 * k, w + 8 * k);
+#pragma unroll
+        for (int k = 0; k < 32; ++k) {
+            const uint32_t half = k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffffu;
+            float x;
+            if constexpr (DT == CB_BF16) {
+                x = __uint_as_float(half << 16);
+            } else {
+                const uint16_t bits = static_cast<uint16_t>(half);
+                __half h;
+                memcpy(&h, &bits, 2);
+                x = __half2float(h);
+            }
+            v[k] = fmaf(-P.rate, v[k], P.keep * x);
+        }
+    }
+    uint32_t w[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        if constexpr (DT == CB_BF16) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+            memcpy(&w[k], &h, 4);
+        } else {
+            const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+            memcpy(&w[k], &h, 4);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        if (col + 16 * k < P.n) store_sector(p + 16 * k, w + 8 * k);
 }
 
 // 16 columns of a warp's 32 rows into the caller's matrix, through shared memory so that
@@ -219,6 +269,9 @@ __device__ __forceinline__ void finish(const ProductArgs& P, int batch, int row,
                 store_halves(P.out_lo + at, v);
             }
         }
+    } else if (P.user_sectors) {
+        if (P.user_dtype == CB_BF16) finish_row<CB_BF16>(P, batch, row, col, v);
+        else finish_row<CB_F16>(P, batch, row, col, v);
     } else {
 #pragma unroll
         for (int h = 0; h < 32; h += 16) {
@@ -227,6 +280,17 @@ __device__ __forceinline__ void finish(const ProductArgs& P, int batch, int row,
             else finish_result<CB_F16>(P, batch, row, col + h, v + h, stage, lane);
         }
     }
+}
+
+// Brings the caller's weights at a warp's columns of a tile into L2 while the tile before it
+// is finished. Only transposed ones, of which a warp reads 16 short rows at a time: a step of
+// 4 x 4096 x 1024 in bf16 431 us without and 412 with; others are no faster for it.
+__device__ __forceinline__ void fetch_weights(const ProductArgs& P, int batch, int row0, int col0, int width, int warp,
+                                              int lane) {
+    if (row0 >= P.m) return;
+    const char* user = static_cast<const char*>(P.user) + (batch * P.user_batch + row0) * dtype_bytes(P.user_dtype);
+    for (int c = col0 + warp / 4 * 32 + lane; c < min(col0 + width, P.n); c += 64)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(user + c * P.user_row * dtype_bytes(P.user_dtype)));
 }
 
 // The epilogue of a tile: a warp's rows row0 .. row0 + 31, every other 32 columns. Those that no
@@ -375,7 +439,14 @@ muon_product_kernel(const __grid_constant__ CUtensorMap left, const __grid_const
     } else {  // epilogue
         int acc = 0;
         uint32_t acc_phase = 0;
+        auto fetch = [&](int64_t t) {
+            if (WHAT != kResult || !P.weights || !P.transposed || t >= total) return;
+            const Tile T = tile_at<kTileM, WHAT>(P, t);
+            fetch_weights(P, T.b, T.i * kTileM + warp % 4 * 32, T.j * BN, BN, warp, lane);
+        };
+        fetch(blockIdx.x);
         for (int64_t t = blockIdx.x; t < total && ok; t += gridDim.x) {
+            fetch(t + gridDim.x);
             const Tile T = tile_at<kTileM, WHAT>(P, t);
             finish_tile<WHAT>(P, T.b, T.i * kTileM + warp % 4 * 32, T.j * BN, BN, tmem + acc * kSums,
                               tc::smem_addr(ready + acc), acc_phase, stage + (WHAT == kResult ? warp * kStageFloats : 0), warp,
@@ -509,7 +580,14 @@ muon_pair_kernel(const __grid_constant__ CUtensorMap left, const __grid_constant
     } else {  // epilogue
         int acc = 0;
         uint32_t acc_phase = 0;
+        auto fetch = [&](int64_t t) {
+            if (WHAT != kResult || !P.weights || !P.transposed || t >= total) return;
+            const Tile T = tile_at<kPairM, WHAT>(P, t);
+            fetch_weights(P, T.b, T.i * kPairM + rank * 128 + warp % 4 * 32, T.j * P.width, P.width, warp, lane);
+        };
+        fetch(first);
         for (int64_t t = first; t < total && ok; t += step) {
+            fetch(t + step);
             const Tile T = tile_at<kPairM, WHAT>(P, t);
             finish_tile<WHAT>(P, T.b, T.i * kPairM + rank * 128 + warp % 4 * 32, T.j * P.width, P.width,
                               tmem + acc * kPairWidth, tc::smem_addr(ready + acc), acc_phase,

@@ -236,6 +236,27 @@ def test_step_adjustments_and_strided_weights(adjust, scale):
     assert torch.equal(mom, grad)
 
 
+@pytest.mark.parametrize("skip", [1, 2, 4, 8, 16])
+@pytest.mark.parametrize("pad", [0, 4, 8, 16])
+@pytest.mark.parametrize("m,n", [(160, 272), (272, 160), (150, 424)])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_weights_of_every_alignment_get_the_same_bits(skip, pad, m, n, dtype):
+    """How a row may be read and written is no part of what is computed: the weights of an
+    aligned stack and those at any other base and stride are equal, and nothing around them moves."""
+    grad = _updates((2, m, n), BF16, 50)
+    start = _updates((2, m, n), F32, 51).mul(1e3).to(dtype)
+    plain, momentum = start.clone(), torch.zeros(2, m, n, device=DEV)
+    mu().muon_step(plain, grad, momentum, lr=0.02, weight_decay=0.1)
+    flat = torch.full((skip + 2 * m * (n + pad),), 7.0, device=DEV).to(dtype)
+    weight = flat[skip:].view(2, m, n + pad)[..., :n]
+    weight.copy_(start)
+    momentum.zero_()
+    mu().muon_step(weight, grad, momentum, lr=0.02, weight_decay=0.1)
+    assert torch.equal(weight, plain) and not torch.equal(plain, start)
+    weight.fill_(7.0)
+    assert bool((flat == 7.0).all())
+
+
 @pytest.mark.parametrize("m,n", [(96, 120), (700, 400)])
 def test_deterministic_on_any_stream_and_in_a_graph(m, n):
     g = _updates((4, m, n), BF16, 16)
