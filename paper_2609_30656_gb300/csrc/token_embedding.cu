@@ -283,11 +283,33 @@ __device__ __forceinline__ void finish_row(const GradArgs& P, int64_t row, int c
         }
     }
 }
-template <int V>
-__device__ __forceinline__ void zero_row(const GradArgs& P, int64_t row, int lane) {
-    Sum<V> zero;
-    zero.clear();
-    for (int col = lane * V; col < P.dim; col += kSlab<V>) finish_row<V>(P, row, col, zero);
+// Zeros to `bytes` (even) of a span that starts at any even address, by a warp: 32 bytes a
+// lane between the edges of whole sectors.
+__device__ __forceinline__ void zero_span(char* p, int64_t bytes, int lane) {
+    const int64_t head = min64(bytes, -reinterpret_cast<uintptr_t>(p) & 31), body = (bytes - head) / 32;
+    const int tail = static_cast<int>(bytes - head - body * 32);
+    if (2 * lane < head) *reinterpret_cast<uint16_t*>(p + 2 * lane) = 0;
+    p += head;
+#pragma unroll 4
+    for (int64_t i = lane; i < body; i += 32)
+        asm volatile("st.global.v8.b32 [%0], {%1, %1, %1, %1, %1, %1, %1, %1};" ::"l"(p + 32 * i), "r"(0) : "memory");
+    if (2 * lane < tail) *reinterpret_cast<uint16_t*>(p + body * 32 + 2 * lane) = 0;
+}
+// Zeros to the rows r0 + k (k < 8) whose bit is set in `empty`: neighbours without a gap as one
+// span, so that short rows and rows of odd lengths fill a warp's stores too. (A row at a time in
+// stores of its own alignment, 64 rows a block: 28 tokens into 88621 rows of 1998 fp32 124
+// us, 20 into 59384 of 3688 halves 74.)
+constexpr int kFillWarpRows = 8;
+struct Rows {
+    char* data;
+    int64_t pitch, used;  // bytes
+};
+__device__ __forceinline__ void zero_rows(const Rows& g, int64_t r0, uint32_t empty, int lane) {
+    while (empty) {
+        const int k = __ffs(empty) - 1, count = g.pitch == g.used ? __ffs(~(empty >> k)) - 1 : 1;
+        zero_span(g.data + (r0 + k) * g.pitch, count * g.used, lane);
+        empty &= ~(((1u << count) - 1u) << k);
+    }
 }
 
 // The sort key of a token: its row, or `rows` (after all rows) for one without gradient.
@@ -303,8 +325,7 @@ constexpr int kMatchThreads = 256;
 constexpr int kMatchWarps = kMatchThreads / 32;
 constexpr uint32_t kMatchTokens = 2048;  // most tokens of a call without a sort
 constexpr int kMatchSlabs = 8;           // slabs of a row per block
-constexpr int kFillRows = 64;            // rows of the gradient per zeroing block
-constexpr int kFillWarpRows = 8;         // rows per zeroing warp at a time
+constexpr int kFillRows = kMatchWarps * kFillWarpRows;  // most rows of the gradient per zeroing block
 
 // One block per (token, group of slabs): the first position of its token sums all of the
 // token's positions, in order; other blocks end at once. The blocks after those write zeros
@@ -312,7 +333,7 @@ constexpr int kFillWarpRows = 8;         // rows per zeroing warp at a time
 // tokens in a few loads, and the call is one launch.
 template <int DT, int V>
 __global__ void __launch_bounds__(kMatchThreads) token_match_kernel(const GradArgs P, uint32_t token_blocks,
-                                                                    int slab_groups) {
+                                                                    int slab_groups, Rows grad, int fill_rows) {
     __shared__ uint16_t list[kMatchTokens];
     __shared__ int counts[kMatchWarps];
     __shared__ int touched[kFillRows];
@@ -321,16 +342,17 @@ __global__ void __launch_bounds__(kMatchThreads) token_match_kernel(const GradAr
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     const uint32_t n = P.tokens.n;
     if (blockIdx.x >= token_blocks) {
-        const int64_t r0 = static_cast<int64_t>(blockIdx.x - token_blocks) * kFillRows;
+        const int64_t r0 = static_cast<int64_t>(blockIdx.x - token_blocks) * fill_rows;
         if (threadIdx.x < kFillRows) touched[threadIdx.x] = 0;
         __syncthreads();
         for (uint32_t j = threadIdx.x; j < n; j += kMatchThreads) {
             const int64_t r = static_cast<int64_t>(token_key(P, P.tokens.load(j), false)) - r0;
-            if (r >= 0 && r < kFillRows) touched[r] = 1;
+            if (r >= 0 && r < fill_rows) touched[r] = 1;
         }
         __syncthreads();
-        for (int r = wid; r < kFillRows && r0 + r < P.tokens.rows; r += kMatchWarps)
-            if (!touched[r]) zero_row<V>(P, r0 + r, lane);
+        const int mine = fill_rows / kMatchWarps, first = wid * mine;  // of a warp: at most kFillWarpRows
+        const bool zero = lane < mine && r0 + first + lane < P.tokens.rows && !touched[first + min(lane, mine - 1)];
+        zero_rows(grad, r0 + first, __ballot_sync(kFull, zero), lane);
         return;
     }
     const uint32_t i = blockIdx.x / slab_groups;
@@ -487,21 +509,13 @@ __global__ void __launch_bounds__(256) token_clear_kernel(uint2* words, int64_t 
 // token_keys_kernel only, is launched after the sort's last pass without waiting for it, and
 // waits at its end for those after it. Blocks stay for the whole kernel (a block that waited
 // at its end would keep a later one from starting).
-template <class T>
-__global__ void __launch_bounds__(256) token_fill_kernel(char* grad, int64_t row_bytes, int64_t used_bytes, int64_t rows,
-                                                         const uint8_t* __restrict__ touched) {
+__global__ void __launch_bounds__(256) token_fill_kernel(Rows grad, int64_t rows, const uint8_t* __restrict__ touched) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31;
     const int64_t step = gridDim.x * 8ll * kFillWarpRows;
     for (int64_t r0 = (blockIdx.x * 8ll + threadIdx.x / 32) * kFillWarpRows; r0 < rows; r0 += step) {
-        const uint2 flags = __ldcg(reinterpret_cast<const uint2*>(touched + r0));  // kFillWarpRows of them
-        for (int k = 0; k < kFillWarpRows && r0 + k < rows; ++k) {
-            if ((k < 4 ? flags.x >> 8 * k : flags.y >> 8 * (k - 4)) & 0xff) continue;
-            T* p = reinterpret_cast<T*>(grad + (r0 + k) * row_bytes);
-            const int count = static_cast<int>(used_bytes / sizeof(T));
-#pragma unroll 4
-            for (int i = lane; i < count; i += 32) p[i] = T{};
-        }
+        const bool zero = lane < kFillWarpRows && r0 + lane < rows && !__ldcg(touched + r0 + min(lane, kFillWarpRows - 1));
+        zero_rows(grad, r0, __ballot_sync(kFull, zero), lane);
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");
 }
@@ -706,32 +720,32 @@ GradWorkspace grad_layout(int64_t n, int64_t rows, int32_t dim) {
     return w;
 }
 
+Rows grad_rows(const GradArgs& P) {
+    const int64_t elem = dtype_bytes(P.grad_dtype);
+    return {static_cast<char*>(P.grad), P.grad_stride * elem, P.dim * elem};
+}
+
+// Bytes that a zeroing block of a match takes (and 8 to 64 rows): many blocks more than run at once.
+constexpr int64_t kFillBytes = 128 << 10;
 template <int DT, int V>
 void launch_match(const GradArgs& P, cudaStream_t s) {
     const int groups = (P.dim + kSlab<V> * kMatchSlabs - 1) / (kSlab<V> * kMatchSlabs);
     const uint32_t token_blocks = P.tokens.n * groups;
-    const int64_t fill = P.accumulate ? 0 : (P.tokens.rows + kFillRows - 1) / kFillRows;
+    const Rows grad = grad_rows(P);
+    int fill_rows = kFillRows;
+    while (fill_rows > kMatchWarps && fill_rows * grad.used > kFillBytes) fill_rows /= 2;
+    const int64_t fill = P.accumulate ? 0 : (P.tokens.rows + fill_rows - 1) / fill_rows;
     if (token_blocks + fill == 0) return;
     launch(token_match_kernel<DT, V>, dim3(static_cast<unsigned>(token_blocks + fill)), dim3(kMatchThreads), 0, s, P,
-           token_blocks, groups);
+           token_blocks, groups, grad, fill_rows);
 }
 
-template <class T>
 void launch_fill(const GradArgs& P, const uint8_t* touched, int sms, cudaStream_t s) {
-    const int64_t elem = dtype_bytes(P.grad_dtype), warps = (P.tokens.rows + kFillWarpRows - 1) / kFillWarpRows;
-    static const int resident = resident_blocks(token_fill_kernel<T>, 256);
+    const int64_t warps = (P.tokens.rows + kFillWarpRows - 1) / kFillWarpRows;
+    static const int resident = resident_blocks(token_fill_kernel, 256);
     const int64_t most = static_cast<int64_t>(sms) * resident;
-    launch(token_fill_kernel<T>, dim3(static_cast<unsigned>(min64((warps + 7) / 8, most))), dim3(256), 0, s,
-           static_cast<char*>(P.grad), P.grad_stride * elem, P.dim * elem, P.tokens.rows, touched);
-}
-// Rows in the widest stores that divide them and their distance.
-void launch_fill(const GradArgs& P, const uint8_t* touched, int sms, cudaStream_t s) {
-    const int64_t elem = dtype_bytes(P.grad_dtype);
-    const uint64_t all = static_cast<uint64_t>(P.grad_stride * elem) | static_cast<uint64_t>(P.dim * elem) |
-                         reinterpret_cast<uintptr_t>(P.grad);
-    if (all % 16 == 0) launch_fill<uint4>(P, touched, sms, s);
-    else if (all % 4 == 0) launch_fill<uint32_t>(P, touched, sms, s);
-    else launch_fill<uint16_t>(P, touched, sms, s);
+    launch(token_fill_kernel, dim3(static_cast<unsigned>(min64((warps + 7) / 8, most))), dim3(256), 0, s, grad_rows(P),
+           P.tokens.rows, touched);
 }
 
 template <int DT, int V>
