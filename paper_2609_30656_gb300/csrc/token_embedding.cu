@@ -325,7 +325,7 @@ constexpr int kMatchThreads = 256;
 constexpr int kMatchWarps = kMatchThreads / 32;
 constexpr uint32_t kMatchTokens = 2048;  // most tokens of a call without a sort
 constexpr int kMatchSlabs = 8;           // slabs of a row per block
-constexpr int kFillRows = kMatchWarps * kFillWarpRows;  // most rows of the gradient per zeroing block
+constexpr int kFillRows = 512;           // most rows of the gradient per zeroing block
 
 // One block per (token, group of slabs): the first position of its token sums all of the
 // token's positions, in order; other blocks end at once. The blocks after those write zeros
@@ -336,23 +336,25 @@ __global__ void __launch_bounds__(kMatchThreads) token_match_kernel(const GradAr
                                                                     int slab_groups, Rows grad, int fill_rows) {
     __shared__ uint16_t list[kMatchTokens];
     __shared__ int counts[kMatchWarps];
-    __shared__ int touched[kFillRows];
+    __shared__ uint8_t touched[kFillRows];
     __shared__ __align__(16) float part[kMatchWarps][kSlab<V>];
     begin_kernel();
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     const uint32_t n = P.tokens.n;
     if (blockIdx.x >= token_blocks) {
         const int64_t r0 = static_cast<int64_t>(blockIdx.x - token_blocks) * fill_rows;
-        if (threadIdx.x < kFillRows) touched[threadIdx.x] = 0;
+        for (int r = threadIdx.x; r < fill_rows; r += kMatchThreads) touched[r] = 0;
         __syncthreads();
         for (uint32_t j = threadIdx.x; j < n; j += kMatchThreads) {
             const int64_t r = static_cast<int64_t>(token_key(P, P.tokens.load(j), false)) - r0;
             if (r >= 0 && r < fill_rows) touched[r] = 1;
         }
         __syncthreads();
-        const int mine = fill_rows / kMatchWarps, first = wid * mine;  // of a warp: at most kFillWarpRows
-        const bool zero = lane < mine && r0 + first + lane < P.tokens.rows && !touched[first + min(lane, mine - 1)];
-        zero_rows(grad, r0 + first, __ballot_sync(kFull, zero), lane);
+        const int mine = min(fill_rows / kMatchWarps, kFillWarpRows);  // of a warp at a time
+        for (int r = wid * mine; r < fill_rows; r += kMatchWarps * mine) {
+            const bool zero = lane < mine && r0 + r + lane < P.tokens.rows && !touched[r + min(lane, mine - 1)];
+            zero_rows(grad, r0 + r, __ballot_sync(kFull, zero), lane);
+        }
         return;
     }
     const uint32_t i = blockIdx.x / slab_groups;
@@ -725,15 +727,18 @@ Rows grad_rows(const GradArgs& P) {
     return {static_cast<char*>(P.grad), P.grad_stride * elem, P.dim * elem};
 }
 
-// Bytes that a zeroing block of a match takes (and 8 to 64 rows): many blocks more than run at once.
-constexpr int64_t kFillBytes = 128 << 10;
+// A zeroing block of a match takes 8 to 512 rows: at most these bytes, so that blocks many more
+// than run at once share them evenly, of short rows as few blocks as fill the GPU, since each
+// looks at all tokens.
+constexpr int64_t kFillBytes = 128 << 10, kFillBlocks = 304;
 template <int DT, int V>
 void launch_match(const GradArgs& P, cudaStream_t s) {
     const int groups = (P.dim + kSlab<V> * kMatchSlabs - 1) / (kSlab<V> * kMatchSlabs);
     const uint32_t token_blocks = P.tokens.n * groups;
     const Rows grad = grad_rows(P);
     int fill_rows = kFillRows;
-    while (fill_rows > kMatchWarps && fill_rows * grad.used > kFillBytes) fill_rows /= 2;
+    while (fill_rows > kMatchWarps && (fill_rows * grad.used > kFillBytes || P.tokens.rows < kFillBlocks * fill_rows))
+        fill_rows /= 2;
     const int64_t fill = P.accumulate ? 0 : (P.tokens.rows + fill_rows - 1) / fill_rows;
     if (token_blocks + fill == 0) return;
     launch(token_match_kernel<DT, V>, dim3(static_cast<unsigned>(token_blocks + fill)), dim3(kMatchThreads), 0, s, P,
