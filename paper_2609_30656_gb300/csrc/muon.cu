@@ -305,8 +305,9 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
     const bool vector = vectors_of(4), wide = vectors_of(8);
     const bool user_vector = in.cols % 4 == 0 && out.row_stride % 4 == 0 && (batch == 1 || out.batch_stride % 4 == 0) &&
                              aligned(out.data, 4 * dtype_bytes(out.dtype));
-    const bool user_sectors = !tall && out.dtype != CB_F32 && in.cols % 16 == 0 && out.row_stride % 16 == 0 &&
-                              (batch == 1 || out.batch_stride % 16 == 0) && aligned(out.data, 32);
+    const int sector = 32 / dtype_bytes(out.dtype);  // values
+    const bool user_sectors = !tall && in.cols % sector == 0 && out.row_stride % sector == 0 &&
+                              (batch == 1 || out.batch_stride % sector == 0) && aligned(out.data, 32);
     const Workspace w = layout(batch, in.rows, in.cols);
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < static_cast<int64_t>(w.bytes)) return CB_ERR_CAPACITY;
     char* base = static_cast<char*>(workspace);

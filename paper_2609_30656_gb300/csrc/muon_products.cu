@@ -105,49 +105,61 @@ __device__ __forceinline__ void store_halves(__half* p, const float (&v)[32]) {
     store_sector(p + 16, w + 8);
 }
 
-// 32 columns of a lane's row into a matrix of 16 bits whose rows are whole sectors. (Through
-// shared memory a row of 16 columns is one sector that four lanes share: a step of 4 x 1024 x
-// 4096 398 us, and 364 so. Columns of 16 fp32 values are two: no faster without.)
+// 32 columns of a lane's row into the caller's matrix where its rows are whole sectors: no
+// exchange between lanes. (Through shared memory, 16 columns at a time: bf16 weights, of which
+// four lanes then share a sector, a step of 4 x 1024 x 4096 398 us, and 365 so; fp32 ones 389
+// and 386, 8 x 512 x 2048 239 and 234.)
 template <int DT>
 __device__ __forceinline__ void finish_row(const ProductArgs& P, int batch, int row, int col, float (&v)[32]) {
+    constexpr int kBytes = DT == CB_F32 ? 4 : 2, V = 32 / kBytes;  // values of a sector
     if (row >= P.m) return;
-    uint16_t* p = static_cast<uint16_t*>(P.user) + batch * P.user_batch + row * P.user_row + col;
+    char* p = static_cast<char*>(P.user) + (batch * P.user_batch + row * P.user_row + col) * kBytes;
 #pragma unroll
-    for (int k = 0; k < 32; ++k) v[k] *= 1.f / kScaleX;
-    if (P.weights) {
+    for (int c = 0; c < 32; c += 2 * V) {  // two sectors at a time: all four of fp32 take registers that there are not
         uint32_t w[16];
+        if (P.weights) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                if (col + c + k * V < P.n) load_sector(p + (c + k * V) * kBytes, w + 8 * k);
+        }
+#pragma unroll
+        for (int k = 0; k < 2 * V; ++k) {
+            float x = v[c + k] * (1.f / kScaleX);
+            if (P.weights) {
+                float old;
+                if constexpr (DT == CB_F32) {
+                    old = __uint_as_float(w[k]);
+                } else {
+                    const uint32_t half = k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffffu;
+                    if constexpr (DT == CB_BF16) {
+                        old = __uint_as_float(half << 16);
+                    } else {
+                        const uint16_t bits = static_cast<uint16_t>(half);
+                        __half h;
+                        memcpy(&h, &bits, 2);
+                        old = __half2float(h);
+                    }
+                }
+                x = fmaf(-P.rate, x, P.keep * old);
+            }
+            v[c + k] = x;
+        }
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            if constexpr (DT == CB_F32) {
+                w[k] = __float_as_uint(v[c + k]);
+            } else if constexpr (DT == CB_BF16) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+                memcpy(&w[k], &h, 4);
+            } else {
+                const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+                memcpy(&w[k], &h, 4);
+            }
+        }
 #pragma unroll
         for (int k = 0; k < 2; ++k)
-            if (col + 16 * k < P.n) load_sector(p + 16 * k, w + 8 * k);
-#pragma unroll
-        for (int k = 0; k < 32; ++k) {
-            const uint32_t half = k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffffu;
-            float x;
-            if constexpr (DT == CB_BF16) {
-                x = __uint_as_float(half << 16);
-            } else {
-                const uint16_t bits = static_cast<uint16_t>(half);
-                __half h;
-                memcpy(&h, &bits, 2);
-                x = __half2float(h);
-            }
-            v[k] = fmaf(-P.rate, v[k], P.keep * x);
-        }
+            if (col + c + k * V < P.n) store_sector(p + (c + k * V) * kBytes, w + 8 * k);
     }
-    uint32_t w[16];
-#pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        if constexpr (DT == CB_BF16) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-            memcpy(&w[k], &h, 4);
-        } else {
-            const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
-            memcpy(&w[k], &h, 4);
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-        if (col + 16 * k < P.n) store_sector(p + 16 * k, w + 8 * k);
 }
 
 // 16 columns of a warp's 32 rows into the caller's matrix, through shared memory so that
@@ -270,7 +282,8 @@ __device__ __forceinline__ void finish(const ProductArgs& P, int batch, int row,
             }
         }
     } else if (P.user_sectors) {
-        if (P.user_dtype == CB_BF16) finish_row<CB_BF16>(P, batch, row, col, v);
+        if (P.user_dtype == CB_F32) finish_row<CB_F32>(P, batch, row, col, v);
+        else if (P.user_dtype == CB_BF16) finish_row<CB_BF16>(P, batch, row, col, v);
         else finish_row<CB_F16>(P, batch, row, col, v);
     } else {
 #pragma unroll
