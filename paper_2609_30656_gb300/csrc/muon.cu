@@ -305,6 +305,8 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
     const bool vector = vectors_of(4), wide = vectors_of(8);
     const bool user_vector = in.cols % 4 == 0 && out.row_stride % 4 == 0 && (batch == 1 || out.batch_stride % 4 == 0) &&
                              aligned(out.data, 4 * dtype_bytes(out.dtype));
+    const bool user_wide = out.dtype != CB_F32 && in.cols % 8 == 0 && out.row_stride % 8 == 0 &&
+                           (batch == 1 || out.batch_stride % 8 == 0) && aligned(out.data, 16);
     const int sector = 32 / dtype_bytes(out.dtype);  // values
     const bool user_sectors = !tall && in.cols % sector == 0 && out.row_stride % sector == 0 &&
                               (batch == 1 || out.batch_stride % sector == 0) && aligned(out.data, 32);
@@ -411,7 +413,7 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
             P.user_row = out.row_stride;
             P.user_dtype = out.dtype;
             P.transposed = tall;
-            P.user_vector = user_vector;
+            P.user_vector = user_wide ? 8 : user_vector ? 4 : 0;
             P.user_sectors = user_sectors;
             P.weights = out.weights;
             P.keep = out.keep;

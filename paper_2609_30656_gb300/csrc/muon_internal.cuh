@@ -226,7 +226,7 @@ struct ProductArgs {
     int64_t user_batch, user_row;
     int32_t user_dtype;
     int32_t transposed;       // value (i, j) of C is value (j, i) of the caller's
-    int32_t user_vector;      // its rows can be taken 4 values at a time
+    int32_t user_vector;      // its rows can be taken 4, or 8 (of 16 bits), values at a time; or 0
     int32_t user_sectors;     // it is not transposed and its rows are whole pieces of 32 bytes
     int32_t weights;          // W <- keep W - rate O, instead of O
     float keep, rate;

@@ -105,6 +105,20 @@ __device__ __forceinline__ void store_halves(__half* p, const float (&v)[32]) {
     store_sector(p + 16, w + 8);
 }
 
+// Two values rounded to 16 bits.
+template <int DT>
+__device__ __forceinline__ uint32_t pack(float x, float y) {
+    uint32_t w;
+    if constexpr (DT == CB_BF16) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+        memcpy(&w, &h, 4);
+    } else {
+        const __half2 h = __floats2half2_rn(x, y);
+        memcpy(&w, &h, 4);
+    }
+    return w;
+}
+
 // 32 columns of a lane's row into the caller's matrix where its rows are whole sectors: no
 // exchange between lanes. (Through shared memory, 16 columns at a time: bf16 weights, of which
 // four lanes then share a sector, a step of 4 x 1024 x 4096 398 us, and 365 so; fp32 ones 389
@@ -146,15 +160,8 @@ __device__ __forceinline__ void finish_row(const ProductArgs& P, int batch, int 
         }
 #pragma unroll
         for (int k = 0; k < 16; ++k) {
-            if constexpr (DT == CB_F32) {
-                w[k] = __float_as_uint(v[c + k]);
-            } else if constexpr (DT == CB_BF16) {
-                const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-                memcpy(&w[k], &h, 4);
-            } else {
-                const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
-                memcpy(&w[k], &h, 4);
-            }
+            if constexpr (DT == CB_F32) w[k] = __float_as_uint(v[c + k]);
+            else w[k] = pack<DT>(v[2 * k], v[2 * k + 1]);
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k)
@@ -163,9 +170,10 @@ __device__ __forceinline__ void finish_row(const ProductArgs& P, int batch, int 
 }
 
 // 16 columns of a warp's 32 rows into the caller's matrix, through shared memory so that
-// lanes run along the caller's rows, 4 values each: loads (of weights) first, then stores.
+// lanes run along the caller's rows, V values each: loads (of weights) first, then stores. 16 bytes
+// a lane where rows allow them: a step of 4 x 4096 x 1024 in bf16 387 us, and 413 with 8.
 constexpr int kStageFloats = 32 * 20;  // rows of 16 (or, transposed, 32) values padded to 20 (36)
-template <int DT>
+template <int DT, int V>
 __device__ __forceinline__ void finish_result(const ProductArgs& P, int batch, int row, int col, const float* v,
                                               float* stage, int lane) {
     char* user = static_cast<char*>(P.user) + batch * P.user_batch * dtype_bytes(DT);
@@ -181,38 +189,47 @@ __device__ __forceinline__ void finish_result(const ProductArgs& P, int batch, i
     __syncwarp();
     const int row0 = P.transposed ? col : row - lane, col0 = P.transposed ? row - lane : col;
     const int rows = P.transposed ? P.n : P.m, cols = P.transposed ? P.m : P.n;  // of the caller's matrix
-    const int wide = P.transposed ? 8 : 4, pitch = P.transposed ? 36 : 20;       // lanes per row
-    const int c = lane % wide * 4, r = lane / wide, step = 32 / wide;
+    constexpr int N = 16 / V;                                                     // pieces of V values a lane
+    const int wide = (P.transposed ? 32 : 16) / V, pitch = P.transposed ? 36 : 20;  // lanes per row
+    const int c = lane % wide * V, r = lane / wide, step = 32 / wide;
     const int64_t at = static_cast<int64_t>(row0 + r) * P.user_row + col0 + c, down = step * P.user_row;
-    float w[4][4] = {};
+    float w[N][V] = {};
     if (P.weights) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < N; ++k) {
             if (row0 + r + k * step >= rows) break;
             if (P.user_vector) {
-                if (col0 + c < cols) load_values<4>(user, at + k * down, DT, w[k]);
+                if (col0 + c < cols) load_values<V>(user, at + k * down, DT, w[k]);
             } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
+                for (int e = 0; e < V; ++e)
                     if (col0 + c + e < cols) w[k][e] = load_value(user, at + k * down + e, DT);
             }
         }
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < N; ++k) {
         if (row0 + r + k * step >= rows) break;
-        const float4 s = *reinterpret_cast<const float4*>(stage + (r + k * step) * pitch + c);
-        float x[4] = {s.x, s.y, s.z, s.w};
+        float x[V];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < V; e += 4) {
+            const float4 s = *reinterpret_cast<const float4*>(stage + (r + k * step) * pitch + c + e);
+            x[e] = s.x, x[e + 1] = s.y, x[e + 2] = s.z, x[e + 3] = s.w;
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
             x[e] *= 1.f / kScaleX;
             if (P.weights) x[e] = fmaf(-P.rate, x[e], P.keep * w[k][e]);
         }
         if (P.user_vector) {
-            if (col0 + c < cols) store_values4<DT>(user, at + k * down, x);
+            if (col0 + c < cols) {
+                if constexpr (V == 4) store_values4<DT>(user, at + k * down, x);
+                else *reinterpret_cast<uint4*>(user + 2 * (at + k * down)) =
+                    make_uint4(pack<DT>(x[0], x[1]), pack<DT>(x[2], x[3]), pack<DT>(x[4], x[5]), pack<DT>(x[6], x[7]));
+            }
         } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
+            for (int e = 0; e < V; ++e)
                 if (col0 + c + e < cols) store_value(user, at + k * down + e, x[e], DT);
         }
     }
@@ -288,16 +305,19 @@ __device__ __forceinline__ void finish(const ProductArgs& P, int batch, int row,
     } else {
 #pragma unroll
         for (int h = 0; h < 32; h += 16) {
-            if (P.user_dtype == CB_F32) finish_result<CB_F32>(P, batch, row, col + h, v + h, stage, lane);
-            else if (P.user_dtype == CB_BF16) finish_result<CB_BF16>(P, batch, row, col + h, v + h, stage, lane);
-            else finish_result<CB_F16>(P, batch, row, col + h, v + h, stage, lane);
+            const bool wide = P.user_vector == 8;
+            if (P.user_dtype == CB_F32) finish_result<CB_F32, 4>(P, batch, row, col + h, v + h, stage, lane);
+            else if (P.user_dtype == CB_BF16 && wide) finish_result<CB_BF16, 8>(P, batch, row, col + h, v + h, stage, lane);
+            else if (P.user_dtype == CB_BF16) finish_result<CB_BF16, 4>(P, batch, row, col + h, v + h, stage, lane);
+            else if (wide) finish_result<CB_F16, 8>(P, batch, row, col + h, v + h, stage, lane);
+            else finish_result<CB_F16, 4>(P, batch, row, col + h, v + h, stage, lane);
         }
     }
 }
 
 // Brings the caller's weights at a warp's columns of a tile into L2 while the tile before it
 // is finished. Only transposed ones, of which a warp reads 16 short rows at a time: a step of
-// 4 x 4096 x 1024 in bf16 431 us without and 412 with; others are no faster for it.
+// 4 x 4096 x 1024 in bf16 392 us without and 383 with; others are no faster for it.
 __device__ __forceinline__ void fetch_weights(const ProductArgs& P, int batch, int row0, int col0, int width, int warp,
                                               int lane) {
     if (row0 >= P.m) return;
