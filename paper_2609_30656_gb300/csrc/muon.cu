@@ -12,14 +12,19 @@
 // Numbers. The products take fp16 operands and sum in fp32. fp16 rather than bf16:
 // both run at one rate, every matrix here is bounded (|x| <= ||X||_2 <= about 1.3 under
 // the usual coefficients), so the exponent's range is not needed, and the three more
-// bits are: rounding X puts noise into its small singular directions, which the first
-// steps multiply by a each (1.2e-2 off the exact result in the 2-norm with bf16, 3e-3
-// with fp16, sizes 128 to 2048). The rest of that noise goes by keeping X as the sum of
-// two fp16 values, X = hi + lo, for the term a X of the first two steps (1e-3); the
-// products take hi alone, since their error is filtered by B, which vanishes on the
-// small directions. From the third step on the term is folded into B (B + a I), and X is
-// hi alone. X is held times 2^10 and A and B times 2^8 (powers of two: exact), which
-// keeps their small values out of fp16's subnormal range and leaves a factor of 40 and
+// bits are. Rounding X puts noise into its small singular directions, which every
+// step multiplies by a while they are small; updates are like that, a few strong directions
+// over a floor that still grows in the last step. So X is kept as the sum of two fp16 values,
+// X = hi + lo, 22 bits, for the term a X, and the products take hi alone: their error is
+// filtered by B, which vanishes on the small directions. B is rounded with a multiple of I added
+// that keeps its diagonal small (diagonal_shift), which is taken off the term again:
+//     X' = (B + s I) hi + (a - s) hi + a lo.
+// Off the exact result in the 2-norm, usual coefficients, 64 x 128 to 1024 x 1024: singular values of 1
+// for one direction, an eighth or half of them over a floor of 1e-2 to 1e-6, 2e-4 to 2.0e-3; of Gaussian
+// matrices 1.3e-3 to 1.5e-3; all alike 1.0e-3 to 2.5e-3 (the roundings of equal diagonals add up). With lo
+// in the first two steps only and a I in B after them: 1.4e-2 over a floor; with no shift: all alike
+// 4.2e-3; in bf16 8 times as much. X is held times 2^10 and A and B times 2^8 (powers of two: exact),
+// which keeps their small values out of fp16's subnormal range and leaves a factor of 20 and
 // more below its largest value.
 //
 // The norm. Squares are summed in three classes of magnitude, each scaled to stay in
@@ -375,7 +380,6 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
     for (int k = 0; k < steps; ++k) {
         const int now = k & 1, next = now ^ 1;
         const float a = coefficients[3 * k], b = coefficients[3 * k + 1], c = coefficients[3 * k + 2];
-        const bool two_term = k < kTwoTerm;
         ProductArgs P{};
         P.batch = batch;
         P.error = error;
@@ -387,22 +391,22 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
         P.out_ld = lda;
         sent &= launch_product(kGram, op_x[now], op_x[now], P, sms, s);
         P.k = P.m;
-        P.a = two_term ? 0.f : a;
+        P.a = a;
         P.b = b;
         P.c = c;
+        P.shift = diagonal_shift(b, c);
         P.term_hi = gram;
         P.term_batch = a_batch;
         P.term_ld = lda;
         P.out_hi = poly;
         sent &= launch_product(kPoly, op_gram, op_gram, P, sms, s);
         P.n = static_cast<int32_t>(w.q);
-        P.a = two_term ? a : 0.f;
         P.term_hi = hi[now];
-        P.term_lo = two_term ? lo[now] : nullptr;
+        P.term_lo = lo[now];
         P.term_batch = x_batch;
         P.term_ld = ldx;
         P.out_hi = hi[next];
-        P.out_lo = k + 1 < kTwoTerm ? lo[next] : nullptr;
+        P.out_lo = lo[next];
         P.out_batch = x_batch;
         P.out_ld = ldx;
         if (k + 1 < steps) {

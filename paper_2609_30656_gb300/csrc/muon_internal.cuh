@@ -15,8 +15,15 @@ namespace muon {
 
 constexpr float kScaleX = 1024.f;  // X is stored times this,
 constexpr float kScaleA = 256.f;   // A and B times this
-constexpr int kTwoTerm = 2;        // steps whose term a X takes hi + lo
 constexpr int kMaxSteps = 64;
+
+// What is added to the diagonal of B before it is rounded, and taken off a: the largest power of
+// two not above -(b + c), so that on directions of singular value 1, where B is b + c, and on those that
+// are still small, where it is 0, little is left to round (fp16's spacing halves below a power of
+// two). 0 where b + c >= 0; 16 at most, which leaves B its range.
+__host__ __device__ __forceinline__ float diagonal_shift(float b, float c) {
+    return b + c < 0.f ? fminf(ldexpf(1.f, ilogbf(-(b + c))), 16.f) : 0.f;
+}
 
 // ---------------------------------------------------------------- norm and momentum
 
@@ -188,8 +195,8 @@ __device__ __forceinline__ float2 inverse_norm(const SquareSum& t, float eps) {
 
 enum Product {
     kGram,    // A = X X^T                          (symmetric)
-    kPoly,    // B = b A + c A A (+ a I)            (symmetric)
-    kUpdate,  // X' = (a X +) B X
+    kPoly,    // B = b A + c A A + shift I          (symmetric)
+    kUpdate,  // X' = (a - shift) hi + a lo + B hi
     kResult   // the same, into the caller's matrix
 };
 template <Product WHAT> constexpr bool kSymmetric = WHAT == kGram || WHAT == kPoly;
@@ -212,13 +219,13 @@ struct ProductArgs {
     int32_t width;            // columns of a tile
     int32_t parts;            // kGram: parts of K summed apart (gram_parts)
     int64_t tiles;            // per matrix
-    float a, b, c;            // the step's coefficients (a = 0: no term a X, or a I)
+    float a, b, c, shift;     // the step's coefficients, diagonal_shift(b, c)
     const __half* term_hi;    // kPoly: A; kUpdate, kResult: X
-    const __half* term_lo;    // or null
+    const __half* term_lo;    // kUpdate, kResult
     int64_t term_batch;
     int32_t term_ld;
     __half* out_hi;
-    __half* out_lo;           // or null
+    __half* out_lo;           // kUpdate
     int64_t out_batch;
     int32_t out_ld;
     // kResult

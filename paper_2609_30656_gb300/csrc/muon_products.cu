@@ -241,10 +241,10 @@ struct Term {
 };
 template <Product WHAT>
 __device__ __forceinline__ void load_term(const ProductArgs& P, int batch, int row, int col, Term& t) {
-    if (row >= P.m || col >= P.n || WHAT == kGram || (WHAT != kPoly && P.a == 0.f)) return;
+    if (row >= P.m || col >= P.n || WHAT == kGram) return;
     const int64_t at = batch * P.term_batch + static_cast<int64_t>(row) * P.term_ld + col;
     t.hi = load_halves(P.term_hi + at);
-    if (WHAT != kPoly && P.term_lo) t.lo = load_halves(P.term_lo + at);
+    if (WHAT != kPoly) t.lo = load_halves(P.term_lo + at);
 }
 
 // 32 columns [col, col + 32) of row `row` of a tile's result: `v` holds the products' sums.
@@ -259,7 +259,7 @@ __device__ __forceinline__ void finish(const ProductArgs& P, int batch, int row,
     } else if constexpr (WHAT == kPoly) {
         float t[32];
         unpack_halves(term.hi, t);
-        const float c = P.c / kScaleA, diagonal = P.a * kScaleA;
+        const float c = P.c / kScaleA, diagonal = P.shift * kScaleA;
 #pragma unroll
         for (int k = 0; k < 32; ++k) {
             v[k] = fmaf(c, v[k], P.b * t[k]);
@@ -268,17 +268,14 @@ __device__ __forceinline__ void finish(const ProductArgs& P, int batch, int row,
     } else {
 #pragma unroll
         for (int k = 0; k < 32; ++k) v[k] *= 1.f / kScaleA;
-        if (P.a != 0.f) {
-            float t[32];
-            if (P.term_lo) {
-                unpack_halves(term.lo, t);
+        float t[32];
+        unpack_halves(term.lo, t);
 #pragma unroll
-                for (int k = 0; k < 32; ++k) v[k] = fmaf(P.a, t[k], v[k]);
-            }
-            unpack_halves(term.hi, t);
+        for (int k = 0; k < 32; ++k) v[k] = fmaf(P.a, t[k], v[k]);
+        unpack_halves(term.hi, t);
+        const float a = P.a - P.shift;
 #pragma unroll
-            for (int k = 0; k < 32; ++k) v[k] = fmaf(P.a, t[k], v[k]);
-        }
+        for (int k = 0; k < 32; ++k) v[k] = fmaf(a, t[k], v[k]);
     }
     if constexpr (kSymmetric<WHAT>) {
         __half* out = P.out_hi + batch * P.out_batch;
@@ -292,11 +289,9 @@ __device__ __forceinline__ void finish(const ProductArgs& P, int batch, int row,
         if (live) {
             const int64_t at = batch * P.out_batch + static_cast<int64_t>(row) * P.out_ld + col;
             store_halves(P.out_hi + at, v);
-            if (P.out_lo) {
 #pragma unroll
-                for (int k = 0; k < 32; ++k) v[k] -= __half2float(__float2half_rn(v[k]));
-                store_halves(P.out_lo + at, v);
-            }
+            for (int k = 0; k < 32; ++k) v[k] -= __half2float(__float2half_rn(v[k]));
+            store_halves(P.out_lo + at, v);
         }
     } else if (P.user_sectors) {
         if (P.user_dtype == CB_F32) finish_row<CB_F32>(P, batch, row, col, v);

@@ -6,8 +6,8 @@ namespace muon {
 namespace {
 
 // Up to 128 x 3 K: all steps of a matrix in one kernel, by a cluster of blocks that each keep
-// up to 384 columns of X in shared memory (fp16, for the products) and in TMEM (fp32, a X as
-// the sums that B X is added to). The Gram matrix of the blocks' columns is added up
+// up to 384 columns of X in shared memory (fp16, for the products) and in TMEM (fp32, the term
+// that B X is added to). The Gram matrix of the blocks' columns is added up
 // across the cluster, in a fixed order, a share of its rows in each block; A A and B are
 // taken by every block for itself. What is left of a step is a chain of three products
 // of half a microsecond and their epilogues, in which a thread takes 32 columns of its row at a
@@ -123,15 +123,20 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
     }
     __syncthreads();
     const float2 f = factor;
+    // What step `step` adds B hi to: (a - shift) hi + a lo = a X - shift hi, times kScaleA.
+    auto to_term = [&](float (&v)[32], int step) {
+        const float* p = P.coefficients + 3 * step;
+        const float a = p[0] * kScaleA, shift = diagonal_shift(p[1], p[2]) * kScaleA;
+#pragma unroll
+        for (int k = 0; k < 32; ++k) v[k] = fmaf(a, v[k], -shift * __half2float(__float2half_rn(v[k])));
+    };
     for (int c = first; c < P.cols; c += NT / 4) {
         float v[32];
         tc::tmem_load32(sum_x + lanes + c, v);
 #pragma unroll
         for (int k = 0; k < 32; ++k) v[k] = (v[k] * f.x) * f.y;
         store_slab32(X + c / 64 * kSlab, row, c % 64, v);
-        const float a = P.coefficients[0] * kScaleA;
-#pragma unroll
-        for (int k = 0; k < 32; ++k) v[k] *= a;
+        to_term(v, 0);
         tc::tmem_store32(sum_x + lanes + c, v);
     }
 
@@ -151,8 +156,8 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
     };
     const uint32_t x_at = tc::smem_addr(X), a_at = tc::smem_addr(A);
     for (int step = 0; step < P.steps; ++step) {
-        const float a = P.coefficients[3 * step], bb = P.coefficients[3 * step + 1], cc = P.coefficients[3 * step + 2];
-        const bool two_term = step < kTwoTerm;
+        const float bb = P.coefficients[3 * step + 1], cc = P.coefficients[3 * step + 2];
+        const float diagonal = diagonal_shift(bb, cc) * kScaleA;
         handed_over();
         if (threadIdx.x == 0) {  // A = X X^T
             tc::fence_after();
@@ -228,19 +233,19 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     v[k + e] = fmaf(cc / kScaleA, v[k + e], bb * t[e]);
-                    if (!two_term && row == c + k + e) v[k + e] += a * kScaleA;
+                    if (row == c + k + e) v[k + e] += diagonal;
                 }
             }
             store_slab32(A + c / 64 * kSlab, row, c % 64, v);
         }
         handed_over();
-        if (threadIdx.x == 0) {  // X <- (a X +) B X
+        if (threadIdx.x == 0) {  // X <- (a - shift) hi + a lo + B hi
             tc::fence_after();
             for (int c = 0; c < P.cols; c += 256) {  // as many columns as one product takes
                 const uint32_t shape = tc::mma_shape(128, P.cols - c < 256 ? P.cols - c : 256, true);
                 for (int x = 0; x < 8; ++x)
                     tc::mma_f16<1>(sum_x + c, tc::operand_k_major(a_at + x / 4 * kSlab + x % 4 * 32),
-                                   tc::operand_mn_major(x_at + c / 64 * kSlab + x * 2048, kSlab), shape, two_term || x > 0);
+                                   tc::operand_mn_major(x_at + c / 64 * kSlab + x * 2048, kSlab), shape, true);
             }
             tc::mma_commit<1>(tc::smem_addr(&done));
         }
@@ -253,12 +258,8 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
 #pragma unroll
                 for (int k = 0; k < 32; ++k) v[k] *= 1.f / kScaleA;
                 store_slab32(X + c / 64 * kSlab, row, c % 64, v);
-                if (step + 1 < kTwoTerm) {
-                    const float next = P.coefficients[3 * step + 3] * kScaleA;
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) v[k] *= next;
-                    tc::tmem_store32(sum_x + lanes + c, v);
-                }
+                to_term(v, step + 1);
+                tc::tmem_store32(sum_x + lanes + c, v);
             } else if (row < P.p) {
                 char* user = static_cast<char*>(P.user) + b * P.user_batch * dtype_bytes(P.user_dtype);
                 const bool vector = P.user_vector && !P.transposed;
