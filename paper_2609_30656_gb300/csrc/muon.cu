@@ -28,7 +28,8 @@
 // more below its largest value.
 //
 // The norm. Squares are summed in three classes of magnitude, each scaled to stay in
-// range, so that no finite matrix overflows or underflows it.
+// range, so that no finite matrix overflows or underflows it; where more than one
+// counts they are joined in fp64.
 //
 // Layout in the workspace: X as [p, q] with rows padded to 64 values, A and B as [p, p]
 // likewise. The transposition of a tall matrix is done where it is read (muon_cast_kernel) and

@@ -28,9 +28,9 @@ __host__ __device__ __forceinline__ float diagonal_shift(float b, float c) {
 // ---------------------------------------------------------------- norm and momentum
 
 // x^2 summed by magnitude: |x| >= 2^40 times 2^-160, |x| < 2^-40 times 2^160, the rest
-// as it is, with what its additions and squares round off kept beside it: the norm then is
-// the same whatever the order of its sum (for a transposed or strided matrix, too). A NaN
-// goes with the rest.
+// as it is, with what its additions and squares round off kept beside it: the norm of
+// values in this middle range then is the same whatever the order of its sum (for a transposed or
+// strided matrix, too); the outer classes are plain sums. A NaN goes with the rest.
 struct SquareSum {
     float mid = 0.f, rest = 0.f, big = 0.f, small = 0.f;
     __device__ __forceinline__ void add_mid(float x) {  // the exact error of a sum of two floats
@@ -179,7 +179,8 @@ __device__ __forceinline__ float update_value(const MatrixIn& in, float g, float
 // norm takes it out of range; in fp64 only where fp32's range asks for it.
 __device__ __forceinline__ float2 inverse_norm(const SquareSum& t, float eps) {
     const float mid = t.mid + t.rest;
-    if (t.big == 0.f && mid >= 0x1p-60f)  // the small class is below fp32's precision then
+    // Up to 2^38 values below 2^-40 are 2^-42 of the sum: nothing beside 2^-16 in fp32.
+    if (t.big == 0.f && (t.small == 0.f || mid >= 0x1p-16f) && mid >= 0x1p-60f)
         return make_float2(1.f, kScaleX / (sqrtf(mid) + eps));
     const double norm = sqrt(static_cast<double>(mid) + static_cast<double>(t.big) * 0x1p160 +
                              static_cast<double>(t.small) * 0x1p-160) + static_cast<double>(eps);

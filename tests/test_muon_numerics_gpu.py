@@ -1,4 +1,5 @@
-"""Accuracy of Newton-Schulz updates over the spectra that training gives them (GPU), against 64 bits.
+"""Accuracy of Newton-Schulz updates over the spectra that training gives them and over
+magnitudes (GPU), against 64 bits.
 
 Limit. u = 2^-11 is fp16's rounding unit, u / sqrt(3) the root mean square of a rounding. With
 B(s) = b s^2 + c s^4 and singular values s of at most 1.2, a step adds, relative to X,
@@ -83,3 +84,32 @@ def test_decaying_singular_values(m, n, power):
     s = torch.arange(1, m + 1, dtype=torch.float64, device=DEV) ** -power
     g = with_singular_values(s, n, 5)
     check(mu().newton_schulz(g, out_dtype=F32), reference(g))
+
+
+# ----------------------------------------------------------------------------- magnitudes
+
+def _plain_norm_matters(g, eps=0.0):
+    check(mu().newton_schulz(g, eps=eps, out_dtype=F32), reference(g, eps=eps))
+
+
+@pytest.mark.parametrize("std", [2e-12, 1e-12, 6e-13, 3e-13])
+@pytest.mark.parametrize("shape", [(2048, 2048), (128, 3000)])
+def test_values_about_two_to_the_minus_40(std, shape):
+    """Where the norm's classes of magnitude meet, each with a good part of the sum."""
+    _plain_norm_matters(torch.randn(shape, generator=_gen(7), device=DEV).mul(std))
+
+
+@pytest.mark.parametrize("shape", [(4096, 4096), (120, 3000)])
+@pytest.mark.parametrize("floor,spike", [(2.0 ** -41, 2.0 ** -30), (2.0 ** -45, 2.0 ** -36), (2.0 ** -60, 2.0 ** -39)])
+def test_a_power_of_two_times_a_matrix_has_its_factor(shape, floor, spike):
+    """One value of the middle class above many of the small one, and the same in the middle class alone."""
+    g = torch.full(shape, floor, device=DEV)
+    g[3, 70] = spike
+    want = mu().newton_schulz(g.mul(2.0 ** 38), eps=0.0, out_dtype=F32).double()
+    got = mu().newton_schulz(g, eps=0.0, out_dtype=F32).double()
+    assert ((got - want).norm() / want.norm()).item() <= LIMIT
+
+
+@pytest.mark.parametrize("shape", [(1024, 1024), (100, 600)])
+def test_values_about_two_to_the_40(shape):
+    _plain_norm_matters(torch.randn(shape, generator=_gen(8), device=DEV).mul(2.0 ** 40))
