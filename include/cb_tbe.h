@@ -410,16 +410,16 @@ cb_status cb_fm_backward(const float* y, const float* grad_fm, int32_t batch, in
  *               outside [0, rows). Such a token gives a row of zeros and no gradient.
  * Errors: CB_ERR_INVALID_ARG before any GPU work, CB_ERR_CUDA if a launch fails. Nothing is
  * allocated and nothing waits, so the calls can be captured into a CUDA graph. Deterministic. */
-cb_status cb_token_forward(const void* table, cb_dtype table_dtype, int64_t rows, int32_t dim,
+cb_status cb_token_forward(const void* table, cb_dtype table_dtype, int64_t rows, int64_t dim,
                            int64_t row_stride, const void* tokens, cb_index_dtype idx_dtype,
-                           int32_t sequences, int32_t length, int64_t token_sequence_stride,
+                           int64_t sequences, int64_t length, int64_t token_sequence_stride,
                            int64_t token_stride, float scale, void* out, cb_dtype out_dtype,
                            int64_t out_sequence_stride, int64_t out_stride, int* error,
                            cudaStream_t stream);
 
 /* Bytes of workspace that cb_token_backward needs for num_tokens = sequences * length (0 for
- * small calls). The contents need not be kept between calls. */
-int64_t cb_token_backward_workspace_bytes(int64_t num_tokens, int64_t rows, int32_t dim);
+ * small calls, and for sizes that it refuses). The contents need not be kept between calls. */
+int64_t cb_token_backward_workspace_bytes(int64_t num_tokens, int64_t rows, int64_t dim);
 
 /* The table's gradient, every row written: zeros for a row without a token; or
  * (accumulate != 0) added to the gradient that is there, rows without a token left alone,
@@ -430,8 +430,8 @@ int64_t cb_token_backward_workspace_bytes(int64_t num_tokens, int64_t rows, int3
  *                least (CB_ERR_CAPACITY otherwise); in use until the call's work is done */
 cb_status cb_token_backward(const void* grad_out, cb_dtype go_dtype, int64_t go_sequence_stride,
                             int64_t go_stride, const void* tokens, cb_index_dtype idx_dtype,
-                            int32_t sequences, int32_t length, int64_t token_sequence_stride,
-                            int64_t token_stride, int64_t rows, int32_t dim, float scale,
+                            int64_t sequences, int64_t length, int64_t token_sequence_stride,
+                            int64_t token_stride, int64_t rows, int64_t dim, float scale,
                             int64_t padding_idx, int accumulate, void* grad, cb_dtype grad_dtype,
                             int64_t grad_stride, void* workspace, int64_t workspace_bytes, int* error,
                             cudaStream_t stream);
@@ -462,8 +462,8 @@ cb_status cb_token_backward(const void* grad_out, cb_dtype go_dtype, int64_t go_
  *               inside a product ran out; the output is then incomplete
  * Errors: CB_ERR_INVALID_ARG before any GPU work; CB_ERR_CUDA if a launch fails or the driver's
  * tensor-map encoder cannot be reached. Nothing is allocated. Deterministic. */
-int64_t cb_muon_workspace_bytes(int32_t batch, int32_t rows, int32_t cols);
-cb_status cb_muon_orthogonalise(const void* g, cb_dtype g_dtype, int32_t batch, int32_t rows, int32_t cols,
+int64_t cb_muon_workspace_bytes(int64_t batch, int64_t rows, int64_t cols);  /* 0 for sizes refused */
+cb_status cb_muon_orthogonalise(const void* g, cb_dtype g_dtype, int64_t batch, int64_t rows, int64_t cols,
                                 int64_t g_batch_stride, int64_t g_row_stride, float eps,
                                 const float* coefficients, int32_t steps, void* out, cb_dtype out_dtype,
                                 int64_t out_batch_stride, int64_t out_row_stride, void* workspace,
@@ -476,8 +476,8 @@ cb_status cb_muon_orthogonalise(const void* g, cb_dtype g_dtype, int32_t batch, 
  * once to its type. lr, weight_decay, update_scale: any value but NaN; beta >= 0. */
 cb_status cb_muon_step(void* weights, cb_dtype w_dtype, int64_t w_batch_stride, int64_t w_row_stride,
                        const void* g, cb_dtype g_dtype, int64_t g_batch_stride, int64_t g_row_stride,
-                       float* momentum, int64_t m_batch_stride, int64_t m_row_stride, int32_t batch,
-                       int32_t rows, int32_t cols, float lr, float weight_decay, float beta, int nesterov,
+                       float* momentum, int64_t m_batch_stride, int64_t m_row_stride, int64_t batch,
+                       int64_t rows, int64_t cols, float lr, float weight_decay, float beta, int nesterov,
                        float eps, const float* coefficients, int32_t steps, float update_scale,
                        void* workspace, int64_t workspace_bytes, int* error, cudaStream_t stream);
 

@@ -236,6 +236,11 @@ struct Workspace {
     int64_t p, q, ldx, lda;
     size_t hi[2], lo[2], gram, poly, partial, error, bytes;
 };
+// Sizes come in 64 bits, so that one past 32 is refused and not cut off on its way here.
+bool valid_sizes(int64_t batch, int64_t rows, int64_t cols) {
+    return batch >= 0 && batch <= 65535 && rows >= 0 && rows <= (1 << 20) && cols >= 0 && cols <= (1 << 20) &&
+           (batch == 0 || rows * cols <= (int64_t(1) << 38) / batch);
+}
 Workspace layout(int32_t batch, int32_t rows, int32_t cols) {
     Workspace w;
     w.p = rows < cols ? rows : cols;
@@ -285,8 +290,6 @@ bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) %
 
 cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const float* coefficients, int32_t steps,
                         const Result& out, void* workspace, int64_t workspace_bytes, int* error, cudaStream_t s) {
-    if (batch < 0 || in.rows < 0 || in.cols < 0 || batch > 65535 || in.rows > (1 << 20) || in.cols > (1 << 20))
-        return CB_ERR_INVALID_ARG;
     if (steps < 1 || steps > kMaxSteps || !coefficients || !(eps >= 0.f) || !valid_dtype(in.dtype) ||
         !valid_dtype(out.dtype))
         return CB_ERR_INVALID_ARG;
@@ -295,7 +298,7 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
     if (batch == 0 || in.rows == 0 || in.cols == 0) return CB_OK;
     const int64_t matrix = static_cast<int64_t>(in.rows) * in.cols;
     if (!in.g || !out.data || in.g_row < in.cols || out.row_stride < in.cols ||
-        (batch > 1 && (in.g_batch < 0 || out.batch_stride < matrix)) || matrix > (int64_t(1) << 38) / batch)
+        (batch > 1 && (in.g_batch < 0 || out.batch_stride < matrix)))
         return CB_ERR_INVALID_ARG;
     if (in.momentum && (in.m_row < in.cols || (batch > 1 && in.m_batch < matrix))) return CB_ERR_INVALID_ARG;
     if (!aligned(in.g, dtype_bytes(in.dtype)) || !aligned(out.data, dtype_bytes(out.dtype)) ||
@@ -433,36 +436,39 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
 }  // namespace muon
 }  // namespace cbtbe
 
-extern "C" int64_t cb_muon_workspace_bytes(int32_t batch, int32_t rows, int32_t cols) {
-    if (batch <= 0 || rows <= 0 || cols <= 0) return 0;
-    return static_cast<int64_t>(cbtbe::muon::layout(batch, rows, cols).bytes);
+extern "C" int64_t cb_muon_workspace_bytes(int64_t batch, int64_t rows, int64_t cols) {
+    using namespace cbtbe::muon;
+    if (!valid_sizes(batch, rows, cols) || batch == 0 || rows == 0 || cols == 0) return 0;
+    return static_cast<int64_t>(
+        layout(static_cast<int32_t>(batch), static_cast<int32_t>(rows), static_cast<int32_t>(cols)).bytes);
 }
 
-extern "C" cb_status cb_muon_orthogonalise(const void* g, cb_dtype g_dtype, int32_t batch, int32_t rows, int32_t cols,
+extern "C" cb_status cb_muon_orthogonalise(const void* g, cb_dtype g_dtype, int64_t batch, int64_t rows, int64_t cols,
                                            int64_t g_batch_stride, int64_t g_row_stride, float eps,
                                            const float* coefficients, int32_t steps, void* out, cb_dtype out_dtype,
                                            int64_t out_batch_stride, int64_t out_row_stride, void* workspace,
                                            int64_t workspace_bytes, int* error, cudaStream_t stream) {
     using namespace cbtbe::muon;
+    if (!valid_sizes(batch, rows, cols)) return CB_ERR_INVALID_ARG;
     MatrixIn in{};
     in.g = g;
     in.g_batch = g_batch_stride;
     in.g_row = g_row_stride;
     in.dtype = g_dtype;
-    in.rows = rows;
-    in.cols = cols;
+    in.rows = static_cast<int32_t>(rows);
+    in.cols = static_cast<int32_t>(cols);
     const Result r{out, out_dtype, out_batch_stride, out_row_stride, false, 0.f, 0.f};
-    return orthogonalise(in, batch, eps, coefficients, steps, r, workspace, workspace_bytes, error, stream);
+    return orthogonalise(in, static_cast<int32_t>(batch), eps, coefficients, steps, r, workspace, workspace_bytes, error, stream);
 }
 
 extern "C" cb_status cb_muon_step(void* weights, cb_dtype w_dtype, int64_t w_batch_stride, int64_t w_row_stride,
                                   const void* g, cb_dtype g_dtype, int64_t g_batch_stride, int64_t g_row_stride,
-                                  float* momentum, int64_t m_batch_stride, int64_t m_row_stride, int32_t batch,
-                                  int32_t rows, int32_t cols, float lr, float weight_decay, float beta, int nesterov,
+                                  float* momentum, int64_t m_batch_stride, int64_t m_row_stride, int64_t batch,
+                                  int64_t rows, int64_t cols, float lr, float weight_decay, float beta, int nesterov,
                                   float eps, const float* coefficients, int32_t steps, float update_scale,
                                   void* workspace, int64_t workspace_bytes, int* error, cudaStream_t stream) {
     using namespace cbtbe::muon;
-    if (!(lr == lr) || !(weight_decay == weight_decay) || !(beta >= 0.f) || !(update_scale == update_scale))
+    if (!valid_sizes(batch, rows, cols) || !(lr == lr) || !(weight_decay == weight_decay) || !(beta >= 0.f) || !(update_scale == update_scale))
         return CB_ERR_INVALID_ARG;
     if (!momentum && batch > 0 && rows > 0 && cols > 0) return CB_ERR_INVALID_ARG;
     MatrixIn in{};
@@ -473,12 +479,12 @@ extern "C" cb_status cb_muon_step(void* weights, cb_dtype w_dtype, int64_t w_bat
     in.m_batch = m_batch_stride;
     in.m_row = m_row_stride;
     in.dtype = g_dtype;
-    in.rows = rows;
-    in.cols = cols;
+    in.rows = static_cast<int32_t>(rows);
+    in.cols = static_cast<int32_t>(cols);
     in.beta = beta;
     in.nesterov = nesterov;
     const Result r{weights, w_dtype, w_batch_stride, w_row_stride, true,
                    static_cast<float>(1.0 - static_cast<double>(lr) * weight_decay),
                    static_cast<float>(static_cast<double>(lr) * update_scale)};
-    return orthogonalise(in, batch, eps, coefficients, steps, r, workspace, workspace_bytes, error, stream);
+    return orthogonalise(in, static_cast<int32_t>(batch), eps, coefficients, steps, r, workspace, workspace_bytes, error, stream);
 }

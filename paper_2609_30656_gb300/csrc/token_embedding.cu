@@ -846,16 +846,18 @@ bool valid_dtype(int d) { return d == CB_F32 || d == CB_F16 || d == CB_BF16; }
 
 // A row-major operand whose rows are taken in pieces of v values: v divides its dim and
 // strides, and a piece is aligned to its size.
-bool takes(const void* p, int dtype, int32_t dim, int64_t s0, int64_t s1, int v) {
+bool takes(const void* p, int dtype, int64_t dim, int64_t s0, int64_t s1, int v) {
     const int64_t bytes = static_cast<int64_t>(v) * dtype_bytes(dtype);
     return dim % v == 0 && s0 % v == 0 && s1 % v == 0 && reinterpret_cast<uintptr_t>(p) % bytes == 0;
 }
 
-// Sequences x length tokens, and the values of a row at each: strides that do not overlap.
-bool valid_tokens(const void* tokens, int idx_dtype, int32_t sequences, int32_t length) {
+// Sizes come in 64 bits, so that one past 32 is refused and not cut off on its way here.
+constexpr int64_t kTokensBelow = int64_t(1) << 30, kRowsBelow = int64_t(1) << 31, kDimMost = int64_t(1) << 20;
+bool valid_sizes(int64_t rows, int64_t dim) { return rows >= 0 && rows < kRowsBelow && dim >= 0 && dim <= kDimMost; }
+bool valid_tokens(const void* tokens, int idx_dtype, int64_t sequences, int64_t length) {
     return (idx_dtype == CB_I32 || idx_dtype == CB_I64) && sequences >= 0 && length >= 0 &&
-           static_cast<int64_t>(sequences) * length < (int64_t(1) << 30) &&
-           (static_cast<int64_t>(sequences) * length == 0 ||
+           (sequences == 0 || length <= (kTokensBelow - 1) / sequences) &&
+           (sequences == 0 || length == 0 ||
             (tokens && reinterpret_cast<uintptr_t>(tokens) % (idx_dtype == CB_I32 ? 4 : 8) == 0));
 }
 bool aligned_to(const void* p, int dtype) { return reinterpret_cast<uintptr_t>(p) % dtype_bytes(dtype) == 0; }
@@ -863,17 +865,16 @@ bool aligned_to(const void* p, int dtype) { return reinterpret_cast<uintptr_t>(p
 }  // namespace
 }  // namespace cbtbe
 
-extern "C" cb_status cb_token_forward(const void* table, cb_dtype table_dtype, int64_t rows, int32_t dim,
-                                      int64_t row_stride, const void* tokens, cb_index_dtype idx_dtype, int32_t sequences,
-                                      int32_t length, int64_t token_sequence_stride, int64_t token_stride, float scale,
+extern "C" cb_status cb_token_forward(const void* table, cb_dtype table_dtype, int64_t rows, int64_t dim,
+                                      int64_t row_stride, const void* tokens, cb_index_dtype idx_dtype, int64_t sequences,
+                                      int64_t length, int64_t token_sequence_stride, int64_t token_stride, float scale,
                                       void* out, cb_dtype out_dtype, int64_t out_sequence_stride, int64_t out_stride,
                                       int* error, cudaStream_t stream) {
     using namespace cbtbe;
     if (!valid_tokens(tokens, idx_dtype, sequences, length) || !valid_dtype(table_dtype) || !valid_dtype(out_dtype) ||
-        rows < 0 || rows >= (int64_t(1) << 31) || dim < 0 || dim > (1 << 20) || !(scale == scale) ||
-        reinterpret_cast<uintptr_t>(error) % 4)
+        !valid_sizes(rows, dim) || !(scale == scale) || reinterpret_cast<uintptr_t>(error) % 4)
         return CB_ERR_INVALID_ARG;
-    const int64_t n = static_cast<int64_t>(sequences) * length;
+    const int64_t n = sequences * length;
     if (n == 0 || dim == 0) return CB_OK;
     if (!out || (rows > 0 && !table) || (rows > 1 && row_stride < dim) || !aligned_to(table, table_dtype) ||
         !aligned_to(out, out_dtype) || (length > 1 && out_stride < dim) ||
@@ -895,35 +896,36 @@ extern "C" cb_status cb_token_forward(const void* table, cb_dtype table_dtype, i
     int v = table_dtype == CB_F32 || out_dtype == CB_F32 ? 8 : 16;
     while (v > 1 && !(takes(table, table_dtype, dim, table_stride, 0, v) && takes(out, out_dtype, dim, s0, s1, v)))
         v /= 2;
-    if (table_dtype == CB_F32) launch_lookup<CB_F32>(P, dim, v, out_dtype, stream);
-    else if (table_dtype == CB_F16) launch_lookup<CB_F16>(P, dim, v, out_dtype, stream);
-    else launch_lookup<CB_BF16>(P, dim, v, out_dtype, stream);
+    const int32_t d = static_cast<int32_t>(dim);
+    if (table_dtype == CB_F32) launch_lookup<CB_F32>(P, d, v, out_dtype, stream);
+    else if (table_dtype == CB_F16) launch_lookup<CB_F16>(P, d, v, out_dtype, stream);
+    else launch_lookup<CB_BF16>(P, d, v, out_dtype, stream);
     return cudaGetLastError() == cudaSuccess ? CB_OK : CB_ERR_CUDA;
 }
 
-extern "C" int64_t cb_token_backward_workspace_bytes(int64_t num_tokens, int64_t rows, int32_t dim) {
-    if (num_tokens <= 0 || rows < 0 || dim <= 0) return 0;
-    return static_cast<int64_t>(cbtbe::grad_layout(num_tokens, rows, dim).bytes);
+extern "C" int64_t cb_token_backward_workspace_bytes(int64_t num_tokens, int64_t rows, int64_t dim) {
+    using namespace cbtbe;
+    if (num_tokens <= 0 || num_tokens >= kTokensBelow || !valid_sizes(rows, dim) || dim == 0) return 0;
+    return static_cast<int64_t>(grad_layout(num_tokens, rows, static_cast<int32_t>(dim)).bytes);
 }
 
 extern "C" cb_status cb_token_backward(const void* grad_out, cb_dtype go_dtype, int64_t go_sequence_stride,
-                                       int64_t go_stride, const void* tokens, cb_index_dtype idx_dtype, int32_t sequences,
-                                       int32_t length, int64_t token_sequence_stride, int64_t token_stride, int64_t rows,
-                                       int32_t dim, float scale, int64_t padding_idx, int accumulate, void* grad,
+                                       int64_t go_stride, const void* tokens, cb_index_dtype idx_dtype, int64_t sequences,
+                                       int64_t length, int64_t token_sequence_stride, int64_t token_stride, int64_t rows,
+                                       int64_t dim, float scale, int64_t padding_idx, int accumulate, void* grad,
                                        cb_dtype grad_dtype, int64_t grad_stride, void* workspace, int64_t workspace_bytes,
                                        int* error, cudaStream_t stream) {
     using namespace cbtbe;
     if (!valid_tokens(tokens, idx_dtype, sequences, length) || !valid_dtype(go_dtype) || !valid_dtype(grad_dtype) ||
-        rows < 0 || rows >= (int64_t(1) << 31) || dim < 0 || dim > (1 << 20) || !(scale == scale) ||
-        reinterpret_cast<uintptr_t>(error) % 4)
+        !valid_sizes(rows, dim) || !(scale == scale) || reinterpret_cast<uintptr_t>(error) % 4)
         return CB_ERR_INVALID_ARG;
-    const int64_t n = static_cast<int64_t>(sequences) * length;
+    const int64_t n = sequences * length;
     if (dim == 0 || (n == 0 && (accumulate || rows == 0))) return CB_OK;
     if ((rows > 0 && !grad) || (n > 0 && !grad_out) || (rows > 1 && grad_stride < dim) ||
         !aligned_to(grad_out, go_dtype) || !aligned_to(grad, grad_dtype) ||
         (length > 1 && go_stride < 0) || (sequences > 1 && go_sequence_stride < 0))
         return CB_ERR_INVALID_ARG;
-    const GradWorkspace w = grad_layout(n, rows, dim);
+    const GradWorkspace w = grad_layout(n, rows, static_cast<int32_t>(dim));
     if (w.bytes > 0 && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 ||
                         workspace_bytes < static_cast<int64_t>(w.bytes)))
         return CB_ERR_CAPACITY;
@@ -933,7 +935,7 @@ extern "C" cb_status cb_token_backward(const void* grad_out, cb_dtype go_dtype, 
     P.padding = padding_idx;
     P.grad_out = grad_out;
     P.go_at = positions(sequences, length, go_sequence_stride, go_stride);
-    P.dim = dim;
+    P.dim = static_cast<int32_t>(dim);
     P.scale = scale;
     P.grad = grad;
     P.grad_stride = grad_stride;

@@ -33,10 +33,10 @@ def _library() -> ctypes.CDLL:
     if _bound is None:
         lib = tbe.load_library()
         p, i32, i64, f32, c = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_int
-        lib.cb_muon_orthogonalise.argtypes = [p, c, i32, i32, i32, i64, i64, f32, p, i32, p, c, i64, i64, p, i64, p, p]
-        lib.cb_muon_step.argtypes = [p, c, i64, i64, p, c, i64, i64, p, i64, i64, i32, i32, i32, f32, f32, f32, c,
+        lib.cb_muon_orthogonalise.argtypes = [p, c, i64, i64, i64, i64, i64, f32, p, i32, p, c, i64, i64, p, i64, p, p]
+        lib.cb_muon_step.argtypes = [p, c, i64, i64, p, c, i64, i64, p, i64, i64, i64, i64, i64, f32, f32, f32, c,
                                      f32, p, i32, f32, p, i64, p, p]
-        lib.cb_muon_workspace_bytes.argtypes = [i32, i32, i32]
+        lib.cb_muon_workspace_bytes.argtypes = [i64, i64, i64]
         lib.cb_muon_orthogonalise.restype = lib.cb_muon_step.restype = c
         lib.cb_muon_workspace_bytes.restype = i64
         _bound = lib

@@ -27,11 +27,11 @@ def _library() -> ctypes.CDLL:
     global _bound
     if _bound is None:
         lib = tbe.load_library()
-        p, i32, i64, f32, c = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_int
-        lib.cb_token_forward.argtypes = [p, c, i64, i32, i64, p, c, i32, i32, i64, i64, f32, p, c, i64, i64, p, p]
-        lib.cb_token_backward.argtypes = [p, c, i64, i64, p, c, i32, i32, i64, i64, i64, i32, f32, i64, c, p, c, i64,
+        p, i64, f32, c = ctypes.c_void_p, ctypes.c_int64, ctypes.c_float, ctypes.c_int
+        lib.cb_token_forward.argtypes = [p, c, i64, i64, i64, p, c, i64, i64, i64, i64, f32, p, c, i64, i64, p, p]
+        lib.cb_token_backward.argtypes = [p, c, i64, i64, p, c, i64, i64, i64, i64, i64, i64, f32, i64, c, p, c, i64,
                                           p, i64, p, p]
-        lib.cb_token_backward_workspace_bytes.argtypes = [i64, i64, i32]
+        lib.cb_token_backward_workspace_bytes.argtypes = [i64, i64, i64]
         lib.cb_token_forward.restype = lib.cb_token_backward.restype = c
         lib.cb_token_backward_workspace_bytes.restype = i64
         _bound = lib
