@@ -454,8 +454,8 @@ cb_status cb_token_backward(const void* grad_out, cb_dtype go_dtype, int64_t go_
  *               r * g_row_stride, rows contiguous, g_row_stride >= cols
  *   batch, rows, cols  each may be 0 (nothing is done); batch <= 65535, rows, cols <= 2^20
  *   eps         >= 0;  coefficients: host array of 3 * steps finite values;  steps 1 .. 64
- *   out         device, of out_dtype, strides as for g, matrices apart by rows * cols at least;
- *               may be g itself, of one type and layout
+ *   out         device, of out_dtype, strides as for g, but no value in two rows (matrices
+ *               one after the other, or their rows in turn); may be g itself, of one type and layout
  *   workspace   device, 256-byte aligned, of cb_muon_workspace_bytes(...) at least
  *               (CB_ERR_CAPACITY otherwise); in use until the call's work is done
  *   error       device int, or NULL: set to CB_ERR_TIMEOUT (if it holds 0) when a bounded wait
@@ -472,7 +472,7 @@ cb_status cb_muon_orthogonalise(const void* g, cb_dtype g_dtype, int64_t batch, 
 /* The optimizer step, for every matrix W with momentum M (fp32) and gradient G:
  *   M <- beta M + G;   U = G + beta M (nesterov != 0) or M;   O = the above of U;
  *   W <- (1 - lr weight_decay) W - lr update_scale O
- * M and W are written in place; O is added in fp32 from the last product's sums, and W rounded
+ * M and W are written in place, their strides as for `out`; O is added in fp32 from the last product's sums, and W rounded
  * once to its type. lr, weight_decay, update_scale: any value but NaN; beta >= 0. */
 cb_status cb_muon_step(void* weights, cb_dtype w_dtype, int64_t w_batch_stride, int64_t w_row_stride,
                        const void* g, cb_dtype g_dtype, int64_t g_batch_stride, int64_t g_row_stride,

@@ -297,10 +297,12 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
         if (!std::isfinite(coefficients[k])) return CB_ERR_INVALID_ARG;
     if (batch == 0 || in.rows == 0 || in.cols == 0) return CB_OK;
     const int64_t matrix = static_cast<int64_t>(in.rows) * in.cols;
-    if (!in.g || !out.data || in.g_row < in.cols || out.row_stride < in.cols ||
-        (batch > 1 && (in.g_batch < 0 || out.batch_stride < matrix)))
+    // What is written is written by many blocks at once: no value may be two matrices'.
+    if (!in.g || !out.data || in.g_row < in.cols || out.row_stride < in.cols || (batch > 1 && in.g_batch < 0) ||
+        !rows_apart(batch, out.batch_stride, in.rows, out.row_stride, in.cols))
         return CB_ERR_INVALID_ARG;
-    if (in.momentum && (in.m_row < in.cols || (batch > 1 && in.m_batch < matrix))) return CB_ERR_INVALID_ARG;
+    if (in.momentum && (in.m_row < in.cols || !rows_apart(batch, in.m_batch, in.rows, in.m_row, in.cols)))
+        return CB_ERR_INVALID_ARG;
     if (!aligned(in.g, dtype_bytes(in.dtype)) || !aligned(out.data, dtype_bytes(out.dtype)) ||
         !aligned(in.momentum, 4) || !aligned(error, 4))
         return CB_ERR_INVALID_ARG;

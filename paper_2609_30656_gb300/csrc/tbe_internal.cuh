@@ -123,6 +123,27 @@ constexpr unsigned long long kSplitArrival = 1ull << 34;
 __host__ __device__ __forceinline__ int64_t min64(int64_t a, int64_t b) { return a < b ? a : b; }
 __host__ __device__ __forceinline__ int64_t max64(int64_t a, int64_t b) { return a > b ? a : b; }
 
+// No two of outer x inner rows of `width` values, at o * outer_stride + i * inner_stride, share a
+// value. Mostly all of an outer index's rows lie before the next one's, or between two of one index
+// those of all the others; where neither holds the rows nearest to each other are looked for.
+inline bool rows_apart(int64_t outer, int64_t outer_stride, int64_t inner, int64_t inner_stride, int64_t width) {
+    using wide = __int128;  // strides are any 64-bit number
+    if (outer > 1 && outer_stride < width) return false;
+    if (inner > 1 && inner_stride < width) return false;
+    if (outer <= 1 || inner <= 1 || outer_stride >= static_cast<wide>(inner - 1) * inner_stride + width ||
+        inner_stride >= static_cast<wide>(outer - 1) * outer_stride + width)
+        return true;
+    const bool turn = inner < outer;
+    const int64_t n = turn ? inner : outer, m = turn ? outer : inner;
+    const wide step = turn ? inner_stride : outer_stride, other = turn ? outer_stride : inner_stride;
+    for (int64_t k = 1; k < n; ++k) {
+        const wide below = k * step / other;
+        if (below < m && k * step - below * other < width) return false;
+        if (below + 1 < m && (below + 1) * other - k * step < width) return false;
+    }
+    return true;
+}
+
 __device__ __forceinline__ void set_error(int* err, int code) { atomicCAS(err, 0, code); }
 
 __device__ __forceinline__ int64_t load_index(const void* p, int64_t i, int is32) {

@@ -78,6 +78,20 @@ def _check_error(error: torch.Tensor, index: int):
         raise ValueError("error must be an int32 tensor of one value on the device")
 
 
+def _rows_apart(batch: int, batch_stride: int, rows: int, row_stride: int, cols: int) -> bool:
+    """No value is in two rows: matrices one after the other, their rows in turn, or else no two rows too near."""
+    if batch_stride < cols:
+        return False
+    if batch_stride >= (rows - 1) * row_stride + cols or row_stride >= (batch - 1) * batch_stride + cols:
+        return True
+    (n, step), (m, other) = sorted(((batch, batch_stride), (rows, row_stride)))
+    for k in range(1, n):
+        below, rest = divmod(k * step, other)
+        if (below < m and rest < cols) or (below + 1 < m and other - rest < cols):
+            return False
+    return True
+
+
 def _layout(t: torch.Tensor):
     """(batch stride, row stride, rows contiguous, no two values in one place) in values; a
     dimension of one has the stride of a whole one."""
@@ -90,7 +104,7 @@ def _layout(t: torch.Tensor):
     many = t.dim() == 3 and shape[0] > 1
     batch = stride[0] if many else rows * row
     in_rows = (cols <= 1 or stride[-1] == 1) and row >= cols
-    return batch, row, in_rows, in_rows and (not many or batch >= rows * cols)
+    return batch, row, in_rows, in_rows and (not many or _rows_apart(shape[0], batch, rows, row, cols))
 
 
 def newton_schulz(g: torch.Tensor, out: torch.Tensor | None = None, out_dtype: torch.dtype = torch.bfloat16,
