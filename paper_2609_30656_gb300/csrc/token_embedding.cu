@@ -877,8 +877,7 @@ extern "C" cb_status cb_token_forward(const void* table, cb_dtype table_dtype, i
     const int64_t n = sequences * length;
     if (n == 0 || dim == 0) return CB_OK;
     if (!out || (rows > 0 && !table) || (rows > 1 && row_stride < dim) || !aligned_to(table, table_dtype) ||
-        !aligned_to(out, out_dtype) || (length > 1 && out_stride < dim) ||
-        (sequences > 1 && out_sequence_stride < dim))
+        !aligned_to(out, out_dtype) || !rows_apart(sequences, out_sequence_stride, length, out_stride, dim))
         return CB_ERR_INVALID_ARG;
     LookupArgs P{};
     P.tokens = {tokens, positions(sequences, length, token_sequence_stride, token_stride), static_cast<uint32_t>(n),

@@ -52,6 +52,16 @@ def test_matrices_that_are_written(lib):
     assert _step(lib, 2, 8, 4, (huge, huge - 1), (32, 4)) == INVALID
 
 
+def test_rows_of_a_lookup(lib):
+    def forward(seqs, s0, length, s1, out_dtype=0):
+        return lib.cb_token_forward(P(4096), 0, 10, 4, 4, P(8192), 1, seqs, length, 0, 0, 1.0, P(12288), out_dtype, s0, s1,
+                                    None, None)
+    for seqs, s0, length, s1 in STRIDES:
+        if not brute_apart(seqs, s0, length, s1, 4):
+            assert forward(seqs, s0, length, s1) == INVALID, (seqs, s0, length, s1)
+    assert forward(2, 2 ** 62, 8, 2 ** 62 - 1) == INVALID and forward(8, 4, 2 ** 20, 16) == INVALID
+
+
 def test_layouts_of_the_binding():
     from paper_2609_30656_gb300 import muon
     for batch, s0, rows, s1 in STRIDES:
