@@ -6,6 +6,8 @@
 //
 // Both move rows and do an operation or two per value: HBM's bandwidth is their bound,
 // launches and dependent loads at a few tokens.
+#include <cmath>
+
 #include "token_rows.cuh"
 #include "tbe_launch.h"
 
@@ -101,6 +103,7 @@ __global__ void __launch_bounds__(kLookupThreads) token_lookup_odd_kernel(const 
     if (!valid && P.error && col == 0) set_error(P.error, CB_ERR_INDEX_OOB);
     const char* from = static_cast<const char*>(P.table) + (token * P.row_stride + col) * dtype_bytes(IN);
     char* to = static_cast<char*>(P.out) + (P.out_at.at(static_cast<uint32_t>(row)) + col) * dtype_bytes(OUT);
+    const float scale = valid ? P.scale : 0.f;  // zeros for no row of the table, whatever the scale
     Piece<IN, V> x[kOddPieces];
 #pragma unroll
     for (int k = 0; k < kOddPieces; ++k)
@@ -111,7 +114,7 @@ __global__ void __launch_bounds__(kLookupThreads) token_lookup_odd_kernel(const 
             float f[V];
             widen<IN, V>(x[k], f);
 #pragma unroll
-            for (int i = 0; i < V; ++i) f[i] *= P.scale;
+            for (int i = 0; i < V; ++i) f[i] *= scale;
             store_piece<OUT, V>(to + 32 * V * k * dtype_bytes(OUT), f);
         }
     }
@@ -895,6 +898,9 @@ extern "C" cb_status cb_token_forward(const void* table, cb_dtype table_dtype, i
     int v = table_dtype == CB_F32 || out_dtype == CB_F32 ? 8 : 16;
     while (v > 1 && !(takes(table, table_dtype, dim, table_stride, 0, v) && takes(out, out_dtype, dim, s0, s1, v)))
         v /= 2;
+    // The zeros of a token out of range times infinity: the kernel for odd rows leaves them zeros (the
+    // other has no register to spare for it).
+    if (std::isinf(scale)) v = static_cast<int>(min64(v, 2));
     const int32_t d = static_cast<int32_t>(dim);
     if (table_dtype == CB_F32) launch_lookup<CB_F32>(P, d, v, out_dtype, stream);
     else if (table_dtype == CB_F16) launch_lookup<CB_F16>(P, d, v, out_dtype, stream);

@@ -1,4 +1,5 @@
-"""Token lookups into outputs whose rows lie in turn, or between one another's; refusals of rows in one place (GPU)."""
+"""Token lookups into outputs whose rows lie in turn, or between one another's; refusals of rows in one place; infinite
+scales (GPU)."""
 
 import pytest
 import torch
@@ -36,3 +37,17 @@ def test_rows_in_one_place_are_refused():
     table, tokens = _randn((50, 8), 2), torch.arange(4, device=DEV).view(2, 2)
     with pytest.raises(tbe.CbTbeError):
         te().token_forward(table, tokens, out=torch.zeros(32, device=DEV).as_strided((2, 2, 8), (8, 8, 1)))
+
+
+@pytest.mark.parametrize("dim", [1024, 64, 12, 6, 63])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("scale", [float("inf"), -float("inf"), 2.0])
+def test_tokens_out_of_range_give_zeros_whatever_the_scale(dim, dtype, scale):
+    table = _randn((50, dim), 3).to(dtype)
+    table[7] = 0
+    tokens = torch.tensor([[3, -1, 50, 7], [2 ** 40, 8, -2 ** 40, 49]], device=DEV)
+    got = te().token_forward(table, tokens, scale=scale)
+    inside = (tokens >= 0) & (tokens < 50)
+    assert not got[~inside].any() and not got[~inside].isnan().any()
+    want = (table[tokens[inside]].float() * scale).to(dtype)
+    assert torch.equal(got[inside].nan_to_num(9.0), want.nan_to_num(9.0))  # 0 * inf is NaN, as multiplied
