@@ -171,7 +171,8 @@ __device__ __forceinline__ void begin_kernel() {
 }
 // A kernel of a chain whose next kernels need nothing of it may let them launch before
 // its own wait; a kernel further on that does not wait at its beginning then runs beside
-// this one (and waits at its end, so that those after it are behind all of them).
+// this one (and waits at its end, so that those after it are behind all of them). What such a
+// kernel reads it has to acquire by itself: only a wait makes an earlier kernel's stores visible.
 __device__ __forceinline__ void begin_kernel_released() {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");

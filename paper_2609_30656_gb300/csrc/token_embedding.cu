@@ -449,6 +449,7 @@ struct SortBuffers {
     TableDev* table;
     int64_t *first_tile, *num_tiles, *table_pos;  // [2], [1], [2]
     uint8_t* touched;  // [rows], padded to 8
+    uint32_t* keyed;   // with `touched`: blocks that have set their flags (cleared before)
 };
 __global__ void __launch_bounds__(kKeyThreads) token_keys_kernel(const GradArgs P, const SortBuffers S, int passes) {
     constexpr int kSeen = 4096;
@@ -484,6 +485,9 @@ __global__ void __launch_bounds__(kKeyThreads) token_keys_kernel(const GradArgs 
         }
     }
     __syncthreads();
+    // This block's flags, and what its launch waited for, before the count: see token_fill_kernel.
+    if (S.touched && threadIdx.x == 0)
+        asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(S.keyed) : "memory");
     if (threadIdx.x < kRadixDigits) {
         S.digits[tile * kRadixDigits + threadIdx.x] = sh[threadIdx.x];
         for (int p = 1; p < passes; ++p)
@@ -516,8 +520,17 @@ __global__ void __launch_bounds__(256) token_clear_kernel(uint2* words, int64_t 
 // token_keys_kernel only, is launched after the sort's last pass without waiting for it, and
 // waits at its end for those after it. Blocks stay for the whole kernel (a block that waited
 // at its end would keep a later one from starting).
-__global__ void __launch_bounds__(256) token_fill_kernel(Rows grad, int64_t rows, const uint8_t* __restrict__ touched) {
+// The sort's first pass lets the next kernels launch once it has waited for the keys, so these are done
+// when this kernel begins; that their stores are visible here too, without a wait of its own, rests on
+// the key blocks' count, released after the flags and acquired before they are read. A thread that
+// does not find all of them waits for the whole chain first.
+__global__ void __launch_bounds__(256) token_fill_kernel(Rows grad, int64_t rows, const uint8_t* touched,
+                                                         const uint32_t* keyed, uint32_t key_blocks) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    uint32_t done;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(done) : "l"(keyed) : "memory");
+    if (done != key_blocks) asm volatile("griddepcontrol.wait;" ::: "memory");
+    __syncwarp();
     const int lane = threadIdx.x & 31;
     const int64_t step = gridDim.x * 8ll * kFillWarpRows;
     for (int64_t r0 = (blockIdx.x * 8ll + threadIdx.x / 32) * kFillWarpRows; r0 < rows; r0 += step) {
@@ -718,7 +731,7 @@ GradWorkspace grad_layout(int64_t n, int64_t rows, int32_t dim) {
     w.table = take(sizeof(TableDev));
     w.scalars = take(5 * 8);
     w.touched_words = (rows + 7) / 8;
-    w.touched = take(w.touched_words * 8);
+    w.touched = take((w.touched_words + 1) * 8);  // and the count of key blocks
     w.chunk = grad_chunk(n, dim);
     const int64_t chunks = (n + w.chunk - 1) / w.chunk;
     w.head = take(chunks * dim * 4);
@@ -750,12 +763,12 @@ void launch_match(const GradArgs& P, cudaStream_t s) {
            token_blocks, groups, grad, fill_rows);
 }
 
-void launch_fill(const GradArgs& P, const uint8_t* touched, int sms, cudaStream_t s) {
+void launch_fill(const GradArgs& P, const SortBuffers& B, uint32_t key_blocks, int sms, cudaStream_t s) {
     const int64_t warps = (P.tokens.rows + kFillWarpRows - 1) / kFillWarpRows;
     static const int resident = resident_blocks(token_fill_kernel, 256);
     const int64_t most = static_cast<int64_t>(sms) * resident;
     launch(token_fill_kernel, dim3(static_cast<unsigned>(min64((warps + 7) / 8, most))), dim3(256), 0, s, grad_rows(P),
-           P.tokens.rows, touched);
+           P.tokens.rows, static_cast<const uint8_t*>(B.touched), static_cast<const uint32_t*>(B.keyed), key_blocks);
 }
 
 template <int DT, int V>
@@ -775,8 +788,10 @@ void launch_sorted(const GradArgs& P, const GradWorkspace& w, char* base, int sm
     const bool few = w.num_tiles <= kFewSortTiles, fill = !P.accumulate && P.tokens.rows > 0;
     if (fill) {
         B.touched = reinterpret_cast<uint8_t*>(base + w.touched);
-        launch(token_clear_kernel, dim3(static_cast<unsigned>(min64(sms, (w.touched_words + 255) / 256))), dim3(256), 0,
-               s, reinterpret_cast<uint2*>(B.touched), w.touched_words);
+        B.keyed = reinterpret_cast<uint32_t*>(B.touched + w.touched_words * 8);
+        const int64_t words = w.touched_words + 1;
+        launch(token_clear_kernel, dim3(static_cast<unsigned>(min64(sms, (words + 255) / 256))), dim3(256), 0, s,
+               reinterpret_cast<uint2*>(B.touched), words);
     }
     launch(token_keys_kernel, dim3(static_cast<unsigned>(w.num_tiles)), dim3(kKeyThreads), 0, s, P, B, w.passes);
     const int64_t words = w.num_tiles * kRadixDigits;
@@ -805,7 +820,7 @@ void launch_sorted(const GradArgs& P, const GradWorkspace& w, char* base, int sm
         S.release = few && fill && p > 0;
         launch_radix_pass(S, w.num_tiles, s);
     }
-    if (fill) launch_fill(P, B.touched, sms, s);
+    if (fill) launch_fill(P, B, static_cast<uint32_t>(w.num_tiles), sms, s);
     Sorted R{};
     R.keys = B.keys[w.passes & 1];
     R.positions = B.positions[w.passes & 1];
