@@ -587,7 +587,7 @@ __global__ void __launch_bounds__(kReduceThreads) token_reduce_kernel(const Grad
 #pragma unroll
                 for (int u = 0; u < kReduceRows; ++u) {
                     const uint32_t row = __shfl_sync(kFull, key, j0 + u);
-                    if (here >> u & 1 && row != none)
+                    if (here >> u & 1 && row != none && col < P.dim)  // a slab may reach past the row, and the tensor
                         prefetch_l1(static_cast<const char*>(P.grad) + (row * P.grad_stride + col) * dtype_bytes(P.grad_dtype));
                 }
             }
