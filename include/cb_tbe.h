@@ -459,7 +459,8 @@ cb_status cb_token_backward(const void* grad_out, cb_dtype go_dtype, int64_t go_
  *   workspace   device, 256-byte aligned, of cb_muon_workspace_bytes(...) at least
  *               (CB_ERR_CAPACITY otherwise); in use until the call's work is done
  *   error       device int, or NULL: set to CB_ERR_TIMEOUT (if it holds 0) when a bounded wait
- *               inside a product ran out; the output is then incomplete
+ *               inside a product ran out; the output, or the weights, are then left as they were,
+ *               but for what the last product had finished (the momentum has been stepped)
  * Errors: CB_ERR_INVALID_ARG before any GPU work; CB_ERR_CUDA if a launch fails or the driver's
  * tensor-map encoder cannot be reached. Nothing is allocated. Deterministic. */
 int64_t cb_muon_workspace_bytes(int64_t batch, int64_t rows, int64_t cols);  /* 0 for sizes refused */

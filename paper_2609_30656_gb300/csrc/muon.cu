@@ -49,9 +49,10 @@ constexpr int kNormBlocks = 304;  // most blocks (and partial sums) per matrix
 // m <- beta m + g in place, and a block's part of the squares of the update u
 // (g; m; or g + beta m). Blocks (x of a matrix, matrix).
 template <int V>
-__global__ void __launch_bounds__(kNormThreads) muon_norm_kernel(MatrixIn in, SquareSum* __restrict__ partial) {
+__global__ void __launch_bounds__(kNormThreads) muon_norm_kernel(MatrixIn in, SquareSum* __restrict__ partial, int* fault) {
     begin_kernel();
     const int b = blockIdx.y;
+    if (b == 0 && blockIdx.x == 0 && threadIdx.x == 0) *fault = 0;  // for the call's products
     const char* g = static_cast<const char*>(in.g) + b * in.g_batch * dtype_bytes(in.dtype);
     float* mom = in.momentum ? in.momentum + b * in.m_batch : nullptr;
     const int vecs = in.cols / V;
@@ -234,7 +235,7 @@ __global__ void __launch_bounds__(256, 4) muon_cast_kernel(MatrixIn in, const Sq
 
 struct Workspace {
     int64_t p, q, ldx, lda;
-    size_t hi[2], lo[2], gram, poly, partial, error, bytes;
+    size_t hi[2], lo[2], gram, poly, partial, fault, bytes;
 };
 // Sizes come in 64 bits, so that one past 32 is refused and not cut off on its way here.
 bool valid_sizes(int64_t batch, int64_t rows, int64_t cols) {
@@ -262,7 +263,7 @@ Workspace layout(int32_t batch, int32_t rows, int32_t cols) {
     w.gram = take(a);
     w.poly = take(a);
     w.partial = take(small ? 0 : static_cast<int64_t>(batch) * kNormBlocks * static_cast<int64_t>(sizeof(SquareSum)));
-    w.error = take(4);
+    w.fault = take(4);
     w.bytes = at;
     return w;
 }
@@ -324,7 +325,6 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
     const Workspace w = layout(batch, in.rows, in.cols);
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < static_cast<int64_t>(w.bytes)) return CB_ERR_CAPACITY;
     char* base = static_cast<char*>(workspace);
-    if (!error) error = reinterpret_cast<int*>(base + w.error);  // any value: read by nobody
     if (const int blocks = small_blocks(w.p, w.q)) {
         SmallArgs P{};
         P.p = static_cast<int32_t>(w.p);
@@ -356,6 +356,7 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
     __half* gram = reinterpret_cast<__half*>(base + w.gram);
     __half* poly = reinterpret_cast<__half*>(base + w.poly);
     SquareSum* partial = reinterpret_cast<SquareSum*>(base + w.partial);
+    int* fault = reinterpret_cast<int*>(base + w.fault);
 
     Operand op_x[2], op_gram, op_poly;
     if (!op_x[0].set(hi[0], w.q, w.p, batch, w.ldx) || !op_x[1].set(hi[1], w.q, w.p, batch, w.ldx) ||
@@ -366,9 +367,9 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
     const int norm_blocks = static_cast<int>(
         max64(1, min64(min64(kNormBlocks, 2 * sms / batch), (matrix + 8 * 1024 - 1) / (8 * 1024))));
     const dim3 norm_grid(norm_blocks, batch);
-    if (wide) launch(muon_norm_kernel<8>, norm_grid, dim3(kNormThreads), 0, s, in, partial);
-    else if (vector) launch(muon_norm_kernel<4>, norm_grid, dim3(kNormThreads), 0, s, in, partial);
-    else launch(muon_norm_kernel<1>, norm_grid, dim3(kNormThreads), 0, s, in, partial);
+    if (wide) launch(muon_norm_kernel<8>, norm_grid, dim3(kNormThreads), 0, s, in, partial, fault);
+    else if (vector) launch(muon_norm_kernel<4>, norm_grid, dim3(kNormThreads), 0, s, in, partial, fault);
+    else launch(muon_norm_kernel<1>, norm_grid, dim3(kNormThreads), 0, s, in, partial, fault);
     const int cast_cols = (in.cols + kCastTile - 1) / kCastTile, cast_rows = (in.rows + kCastTile - 1) / kCastTile;
     const dim3 cast_grid(cast_cols,
                          static_cast<unsigned>(max64(1, min64(cast_rows, 8 * sms / (static_cast<int64_t>(cast_cols) * batch)))),
@@ -389,6 +390,7 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
         ProductArgs P{};
         P.batch = batch;
         P.error = error;
+        P.fault = fault;
         P.m = P.n = static_cast<int32_t>(w.p);
         P.k = static_cast<int32_t>(w.q);
         P.parts = gram_parts(w.p, w.q);

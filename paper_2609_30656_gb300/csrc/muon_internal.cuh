@@ -238,7 +238,8 @@ struct ProductArgs {
     int32_t user_sectors;     // it is not transposed and its rows are whole pieces of 32 bytes
     int32_t weights;          // W <- keep W - rate O, instead of O
     float keep, rate;
-    int* error;
+    int* error;               // the caller's, or null
+    int* fault;               // this call's own: not 0 once a wait ran out; the last product then writes nothing
 };
 
 // A matrix of the workspace as an operand, by the boxes that a kernel copies.
@@ -265,7 +266,7 @@ struct SmallArgs {
     int32_t user_dtype, user_vector, in_vector;
     int32_t weights;
     float keep, rate;
-    int* error;
+    int* error;              // or null
 };
 
 // Blocks per matrix of muon_small_kernel (a power of two), 0 where it does not apply.

@@ -326,7 +326,7 @@ __device__ __forceinline__ void fetch_weights(const ProductArgs& P, int batch, i
 template <Product WHAT>
 __device__ __forceinline__ void finish_tile(const ProductArgs& P, int batch, int row0, int col0, int width, uint32_t tmem,
                                             uint32_t ready, uint32_t parity, float* stage, int warp, int lane, bool& ok,
-                                            int parts = 1) {
+                                            bool write = true, int parts = 1) {
     const int row = row0 + lane;
     auto skip = [&](int c) { return c >= width || col0 + c >= P.n || (kSymmetric<WHAT> && (col0 + c) / kTileM > row0 / kTileM); };
     int c = warp / 4 * 32;
@@ -349,10 +349,22 @@ __device__ __forceinline__ void finish_tile(const ProductArgs& P, int batch, int
             }
         }
         if (!skip(c + 64)) load_term<WHAT>(P, batch, row, col0 + c + 64, next);
-        finish<WHAT>(P, batch, row, col0 + c, v, term, stage, lane);
+        if (write) finish<WHAT>(P, batch, row, col0 + c, v, term, stage, lane);
     }
     tc::fence_before();
     __syncwarp();
+}
+
+// A wait of this thread ran out. Products after this one go on with what is there, but the last one finds the
+// call's word set and leaves the caller's matrix as it is.
+__device__ __forceinline__ void report_timeout(const ProductArgs& P) {
+    set_error(P.fault, CB_ERR_TIMEOUT);
+    if (P.error) set_error(P.error, CB_ERR_TIMEOUT);
+}
+template <Product WHAT>
+__device__ __forceinline__ bool may_write(const ProductArgs& P) {  // a whole warp
+    if constexpr (WHAT != kResult) return true;
+    return __all_sync(kFull, __ldcg(P.fault) == 0);
 }
 
 // C = A B in tiles of 128 x BN, tile after tile by each block. Operand A is K-major; B is
@@ -467,6 +479,7 @@ muon_product_kernel(const __grid_constant__ CUtensorMap left, const __grid_const
     } else {  // epilogue
         int acc = 0;
         uint32_t acc_phase = 0;
+        const bool write = may_write<WHAT>(P);
         auto fetch = [&](int64_t t) {
             if (WHAT != kResult || !P.weights || !P.transposed || t >= total) return;
             const Tile T = tile_at<kTileM, WHAT>(P, t);
@@ -478,13 +491,13 @@ muon_product_kernel(const __grid_constant__ CUtensorMap left, const __grid_const
             const Tile T = tile_at<kTileM, WHAT>(P, t);
             finish_tile<WHAT>(P, T.b, T.i * kTileM + warp % 4 * 32, T.j * BN, BN, tmem + acc * kSums,
                               tc::smem_addr(ready + acc), acc_phase, stage + (WHAT == kResult ? warp * kStageFloats : 0), warp,
-                              lane, ok, kSums > BN ? (ksteps + per - 1) / per : 1);
+                              lane, ok, write, kSums > BN ? (ksteps + per - 1) / per : 1);
             if (!ok) break;
             if (lane == 0) tc::barrier_arrive(tc::smem_addr(drained + acc));
             if (++acc == 2) acc = 0, acc_phase ^= 1;
         }
     }
-    if (!ok && lane == 0) set_error(P.error, CB_ERR_TIMEOUT);
+    if (!ok) report_timeout(P);  // the copying lane, or a whole warp
     __syncwarp();
     tc::fence_before();
     __syncthreads();
@@ -609,6 +622,7 @@ muon_pair_kernel(const __grid_constant__ CUtensorMap left, const __grid_constant
     } else {  // epilogue
         int acc = 0;
         uint32_t acc_phase = 0;
+        const bool write = may_write<WHAT>(P);
         auto fetch = [&](int64_t t) {
             if (WHAT != kResult || !P.weights || !P.transposed || t >= total) return;
             const Tile T = tile_at<kPairM, WHAT>(P, t);
@@ -620,13 +634,13 @@ muon_pair_kernel(const __grid_constant__ CUtensorMap left, const __grid_constant
             const Tile T = tile_at<kPairM, WHAT>(P, t);
             finish_tile<WHAT>(P, T.b, T.i * kPairM + rank * 128 + warp % 4 * 32, T.j * P.width, P.width,
                               tmem + acc * kPairWidth, tc::smem_addr(ready + acc), acc_phase,
-                              stage + (WHAT == kResult ? warp * kStageFloats : 0), warp, lane, ok);
+                              stage + (WHAT == kResult ? warp * kStageFloats : 0), warp, lane, ok, write);
             if (!ok) break;
             if (lane == 0) tc::barrier_arrive_cluster(tc::in_first_block(tc::smem_addr(drained + acc)));
             if (++acc == 2) acc = 0, acc_phase ^= 1;
         }
     }
-    if (!ok && lane == 0) set_error(P.error, CB_ERR_TIMEOUT);
+    if (!ok) report_timeout(P);  // the copying lane, or a whole warp
     __syncwarp();
     tc::fence_before();
     tc::cluster_sync();  // neither block ends while the other may signal its barriers
@@ -721,7 +735,7 @@ muon_split_kernel(const __grid_constant__ CUtensorMap rows, const ProductArgs P)
                     make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
         }
     }
-    if (!ok && lane == 0) set_error(P.error, CB_ERR_TIMEOUT);
+    if (!ok) report_timeout(P);  // the copying lane, or a whole warp
     __syncwarp();
     tc::fence_before();
     tc::cluster_sync();

@@ -39,12 +39,14 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
     __shared__ uint64_t done;
     __shared__ uint32_t tmem_at;
     __shared__ float2 factor;
+    __shared__ int failed;  // a wait ran out, here or (after a step's sums are exchanged) in the cluster
     __shared__ __align__(16) float squares[NT / 32 + 1][4];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CLUSTER ? static_cast<int>(tc::cluster_rank()) : 0;
     const int b = blockIdx.x / P.blocks;
     const uint32_t columns = P.cols <= 128 ? 256 : 512;
     if (threadIdx.x == 0) {
+        failed = 0;
         tc::barrier_init(tc::smem_addr(&done), 1);
         tc::barrier_init_fence();
     }
@@ -140,8 +142,8 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
         tc::tmem_store32(sum_x + lanes + c, v);
     }
 
-    // A wait that ran out is reported, and the rest is then computed without waiting: the
-    // cluster's blocks stay in step.
+    // After a wait that ran out a thread waits no more and issues no products, but goes through the rest
+    // with the others, so that the cluster's blocks stay in step; nothing is written at the end.
     bool ok = true;
     uint32_t phase = 0;
     auto handed_over = [&] {  // what all threads stored, to the tensor core
@@ -150,7 +152,10 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
         __syncthreads();
     };
     auto products_done = [&] {
-        ok = ok && tc::barrier_wait(tc::smem_addr(&done), phase);
+        if (ok && !tc::barrier_wait(tc::smem_addr(&done), phase)) {
+            ok = false;
+            failed = 1;
+        }
         phase ^= 1;
         tc::fence_after();
     };
@@ -159,7 +164,7 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
         const float bb = P.coefficients[3 * step + 1], cc = P.coefficients[3 * step + 2];
         const float diagonal = diagonal_shift(bb, cc) * kScaleA;
         handed_over();
-        if (threadIdx.x == 0) {  // A = X X^T
+        if (threadIdx.x == 0 && ok) {  // A = X X^T
             tc::fence_after();
             constexpr uint32_t shape = tc::mma_shape(128, 128, false);
             for (int x = 0; x < P.cols / 16; ++x) {
@@ -186,6 +191,9 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
         }
         if constexpr (CLUSTER) {
             tc::cluster_sync();
+            if (threadIdx.x == 0)
+                for (int k = 0; k < P.blocks; ++k)
+                    if (tc::load_cluster_int(tc::in_block(tc::smem_addr(&failed), k)) != 0) failed = 1;
             const int share = 128 / P.blocks;  // rows that this block adds up, for all
             for (int i = threadIdx.x; i < share * 32; i += NT) {
                 const int r = rank * share + i / 32, c4 = i % 32;
@@ -213,7 +221,7 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
             tc::cluster_sync();
         }
         handed_over();
-        if (threadIdx.x == 0) {  // A A
+        if (threadIdx.x == 0 && ok) {  // A A
             tc::fence_after();
             constexpr uint32_t shape = tc::mma_shape(128, 128, false);
             for (int x = 0; x < 8; ++x) {
@@ -239,7 +247,7 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
             store_slab32(A + c / 64 * kSlab, row, c % 64, v);
         }
         handed_over();
-        if (threadIdx.x == 0) {  // X <- (a - shift) hi + a lo + B hi
+        if (threadIdx.x == 0 && ok) {  // X <- (a - shift) hi + a lo + B hi
             tc::fence_after();
             for (int c = 0; c < P.cols; c += 256) {  // as many columns as one product takes
                 const uint32_t shape = tc::mma_shape(128, P.cols - c < 256 ? P.cols - c : 256, true);
@@ -260,7 +268,7 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
                 store_slab32(X + c / 64 * kSlab, row, c % 64, v);
                 to_term(v, step + 1);
                 tc::tmem_store32(sum_x + lanes + c, v);
-            } else if (row < P.p) {
+            } else if (row < P.p && ok && !failed) {
                 char* user = static_cast<char*>(P.user) + b * P.user_batch * dtype_bytes(P.user_dtype);
                 const bool vector = P.user_vector && !P.transposed;
 #pragma unroll
@@ -299,7 +307,7 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
             }
         }
     }
-    if (!ok && lane == 0) set_error(P.error, CB_ERR_TIMEOUT);
+    if (!ok && P.error) set_error(P.error, CB_ERR_TIMEOUT);
     tc::fence_before();
     __syncthreads();
     tc::fence_after();

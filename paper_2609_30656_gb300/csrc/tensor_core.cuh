@@ -59,8 +59,8 @@ __device__ __forceinline__ bool barrier_test(uint32_t bar, uint32_t parity) {
 // Waits for the phase `parity` of `bar` to complete; false when the polls run out
 // (a poll suspends the thread for up to microseconds, so the limit is seconds).
 constexpr uint32_t kPolls = 1u << 21;
-__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity) {
-    for (uint32_t i = 0; i < kPolls; ++i)
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, uint32_t polls = kPolls) {
+    for (uint32_t i = 0; i < polls; ++i)
         if (barrier_try(bar, parity)) return true;
     return false;
 }
@@ -232,6 +232,11 @@ __device__ __forceinline__ float4 load_cluster(uint32_t addr) {
                  : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
                  : "r"(addr)
                  : "memory");
+    return v;
+}
+__device__ __forceinline__ int load_cluster_int(uint32_t addr) {
+    int v;
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
     return v;
 }
 __device__ __forceinline__ void store_cluster(uint32_t addr, uint2 v) {
