@@ -335,6 +335,7 @@ cb_status orthogonalise(const MatrixIn& in, int32_t batch, float eps, const floa
         P.steps = steps;
         P.eps = eps;
         for (int k = 0; k < 3 * steps; ++k) P.coefficients[k] = coefficients[k];
+        for (int k = 0; k < steps; ++k) P.shift[k] = diagonal_shift(coefficients[3 * k + 1], coefficients[3 * k + 2]);
         P.user = out.data;
         P.user_batch = out.batch_stride;
         P.user_row = out.row_stride;

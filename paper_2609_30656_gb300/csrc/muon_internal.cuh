@@ -21,8 +21,8 @@ constexpr int kMaxSteps = 64;
 // two not above -(b + c), so that on directions of singular value 1, where B is b + c, and on those that
 // are still small, where it is 0, little is left to round (fp16's spacing halves below a power of
 // two). 0 where b + c >= 0; 16 at most, which leaves B its range.
-__host__ __device__ __forceinline__ float diagonal_shift(float b, float c) {
-    return b + c < 0.f ? fminf(ldexpf(1.f, ilogbf(-(b + c))), 16.f) : 0.f;
+inline float diagonal_shift(float b, float c) {
+    return b + c < 0.f ? std::fmin(std::ldexp(1.f, std::ilogb(-(b + c))), 16.f) : 0.f;
 }
 
 // ---------------------------------------------------------------- norm and momentum
@@ -260,7 +260,7 @@ struct SmallArgs {
     int32_t p, q, cols;      // X [p, q], columns per block (a multiple of 64)
     int32_t transposed, blocks, steps;
     float eps;
-    float coefficients[3 * kMaxSteps];
+    float coefficients[3 * kMaxSteps], shift[kMaxSteps];
     void* user;
     int64_t user_batch, user_row;
     int32_t user_dtype, user_vector, in_vector;

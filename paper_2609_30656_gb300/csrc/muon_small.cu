@@ -127,8 +127,7 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
     const float2 f = factor;
     // What step `step` adds B hi to: (a - shift) hi + a lo = a X - shift hi, times kScaleA.
     auto to_term = [&](float (&v)[32], int step) {
-        const float* p = P.coefficients + 3 * step;
-        const float a = p[0] * kScaleA, shift = diagonal_shift(p[1], p[2]) * kScaleA;
+        const float a = P.coefficients[3 * step] * kScaleA, shift = P.shift[step] * kScaleA;
 #pragma unroll
         for (int k = 0; k < 32; ++k) v[k] = fmaf(a, v[k], -shift * __half2float(__float2half_rn(v[k])));
     };
@@ -162,7 +161,7 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
     const uint32_t x_at = tc::smem_addr(X), a_at = tc::smem_addr(A);
     for (int step = 0; step < P.steps; ++step) {
         const float bb = P.coefficients[3 * step + 1], cc = P.coefficients[3 * step + 2];
-        const float diagonal = diagonal_shift(bb, cc) * kScaleA;
+        const float diagonal = P.shift[step] * kScaleA;
         handed_over();
         if (threadIdx.x == 0 && ok) {  // A = X X^T
             tc::fence_after();
