@@ -46,7 +46,10 @@ def _library() -> ctypes.CDLL:
 def _coefficients(coefficients, steps: int):
     """A C array of 3 * steps values: one triple for all steps, or one for each."""
     key = (coefficients, steps) if type(coefficients) is tuple else None
-    array = _coefficient_arrays.get(key)
+    try:
+        array = _coefficient_arrays.get(key)
+    except TypeError:  # a tuple of lists
+        key = array = None
     if array is not None:
         return array
     if steps < 1:
