@@ -60,7 +60,8 @@ def _coefficients(coefficients, steps: int):
     if len(rows) != steps or any(not hasattr(r, "__len__") or len(r) != 3 for r in rows):
         raise ValueError("coefficients must be one triple, or one triple for each step")
     array = (ctypes.c_float * (3 * steps))(*[float(x) for r in rows for x in r])
-    if key is not None and all(isinstance(x, (float, int, tuple)) for x in coefficients):
+    # Kept only where nothing in it can change.
+    if key is not None and all(type(r) is tuple and all(type(x) in (float, int) for x in r) for r in rows):
         if len(_coefficient_arrays) >= 64:
             _coefficient_arrays.clear()
         _coefficient_arrays[key] = array
