@@ -111,11 +111,11 @@ def _layout(t: torch.Tensor):
     return batch, row, in_rows, in_rows and (not many or _rows_apart(shape[0], batch, rows, row, cols))
 
 
-def newton_schulz(g: torch.Tensor, out: torch.Tensor | None = None, out_dtype: torch.dtype = torch.bfloat16,
+def newton_schulz(g: torch.Tensor, out: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
                   steps: int = 5, coefficients=COEFFICIENTS, eps: float = 1e-7,
                   error: torch.Tensor | None = None) -> torch.Tensor:
     """The approximate orthogonal factor of g, or of each matrix of a stack
-    (cb_muon_orthogonalise).
+    (cb_muon_orthogonalise), bf16 unless out or out_dtype is of another type.
 
     X = g / (||g||_F + eps), then `steps` times X <- a X + (b A + c A A) X with A = X X^T.
     The products are in fp16 with fp32 sums, 2e-4 to 2.5e-3 off the exact result in the 2-norm (all
@@ -129,10 +129,13 @@ def newton_schulz(g: torch.Tensor, out: torch.Tensor | None = None, out_dtype: t
         _check_error(error, index)
     layout = _layout(g)
     if out is None:
+        out_dtype = out_dtype or torch.bfloat16
         if not layout[2] and _layout(g.mT)[2]:
             out = torch.empty(g.mT.shape, dtype=out_dtype, device=g.device).mT
         else:
             out = torch.empty(g.shape, dtype=out_dtype, device=g.device)
+    elif out_dtype is not None and out.dtype != out_dtype:
+        raise TypeError(f"out must be {out_dtype}")
     out_kind = _check_matrix(out, "out")
     out_layout = _layout(out)
     if out.get_device() != index or out.shape != g.shape or not (out_layout[3] or _layout(out.mT)[3]):

@@ -125,10 +125,11 @@ def token_forward(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0,
 
 def token_backward(grad_out: torch.Tensor, tokens: torch.Tensor, num_rows: int, scale: float = 1.0,
                    padding_idx: int | None = None, out: torch.Tensor | None = None,
-                   out_dtype: torch.dtype = torch.float32, accumulate: bool = False,
+                   out_dtype: torch.dtype | None = None, accumulate: bool = False,
                    error: torch.Tensor | None = None) -> torch.Tensor:
     """The gradient of token_forward with respect to the table, [num_rows, dim]:
-    out[v] = scale * (sum of grad_out over the positions whose token is v) (cb_token_backward).
+    out[v] = scale * (sum of grad_out over the positions whose token is v) (cb_token_backward),
+    fp32 unless out or out_dtype is of another type.
 
     With accumulate=True that is added to `out` in place and rows without a token are left
     alone; otherwise every row is written. Positions that hold padding_idx give nothing, nor
@@ -153,10 +154,12 @@ def token_backward(grad_out: torch.Tensor, tokens: torch.Tensor, num_rows: int, 
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs the gradient to add to")
-        out = torch.empty(num_rows, dim, dtype=out_dtype, device=grad_out.device)
+        out = torch.empty(num_rows, dim, dtype=out_dtype or torch.float32, device=grad_out.device)
     else:
         if out.get_device() != index or out.shape != (num_rows, dim):
             raise ValueError("out must be [num_rows, dim] on the gradient's device")
+        if out_dtype is not None and out.dtype != out_dtype:
+            raise TypeError(f"out must be {out_dtype}")
         if num_rows > 1:
             row_stride = out.stride(0)
         if (dim > 1 and out.stride(1) != 1) or row_stride < dim:
