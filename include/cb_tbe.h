@@ -402,7 +402,7 @@ cb_status cb_fm_backward(const float* y, const float* grad_fm, int32_t batch, in
  *               needs no copy). sequences * length < 2^30; either may be 0.
  *   table       device [rows, dim] of table_dtype, row v at v * row_stride values,
  *               row_stride >= dim; rows < 2^31, dim <= 2^20. Any alignment of its type;
- *               rows in multiples of 16 bytes that start on 16 bytes are moved fastest.
+ *               rows in multiples of 32 bytes, in the wider type, that start on 32 bytes are moved fastest.
  *   out, grad_out  device, row (s, l) at s * ..._sequence_stride + l * ..._stride values,
  *               each row contiguous; rows of `out` must not overlap (those of grad_out may).
  *   scale       any value but NaN
@@ -447,9 +447,12 @@ cb_status cb_token_backward(const void* grad_out, cb_dtype go_dtype, int64_t go_
  * which moves every singular value towards 1 and keeps the singular vectors. The usual
  * coefficients are (3.4445, -4.7750, 2.0315), five times. The products are taken in fp16 with
  * fp32 sums; in the 2-norm the result of the usual coefficients is 2e-4 to 2.5e-3 off the exact
- * one, by the matrix's singular values. They hold as long as
- * singular values stay below about 40 throughout; coefficients that let them grow beyond give
- * infinities. A matrix with an infinity or a NaN gives NaNs, a matrix of zeros gives zeros.
+ * one, by the matrix's singular values (up to 1.3e-2 where elements are alike and round alike,
+ * as in a constant matrix: in the singular value, not in its vectors). X, A and
+ * B = b A + c A A + d I are held in fp16 (d: the largest power of two not above -(b + c), 16 at most, or
+ * 0), so singular values have to stay below 15.9 up to the last step, and |b s^2 + c s^4 + d| below
+ * 255 in every step; the usual coefficients keep s below 1.3 and the other below 3. Coefficients
+ * that let them grow beyond give infinities or NaNs. A matrix with an infinity or a NaN gives NaNs, a matrix of zeros gives zeros.
  *   g           device, of g_dtype: matrix i at i * g_batch_stride values, row r at
  *               r * g_row_stride, rows contiguous, g_row_stride >= cols
  *   batch, rows, cols  each may be 0 (nothing is done); batch <= 65535, rows, cols <= 2^20

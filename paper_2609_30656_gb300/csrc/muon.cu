@@ -21,11 +21,12 @@
 //     X' = (B + s I) hi + (a - s) hi + a lo.
 // Off the exact result in the 2-norm, usual coefficients, 64 x 128 to 1024 x 1024: singular values of 1
 // for one direction, an eighth or half of them over a floor of 1e-2 to 1e-6, 2e-4 to 2.0e-3; of Gaussian
-// matrices 1.3e-3 to 1.5e-3; all alike 1.0e-3 to 2.5e-3 (the roundings of equal diagonals add up). With lo
+// matrices 1.3e-3 to 1.5e-3; all alike 1.0e-3 to 2.5e-3 (the roundings of equal diagonals add up); constant
+// matrices, all of whose roundings add up, 1.3e-2 at the most. With lo
 // in the first two steps only and a I in B after them: 1.4e-2 over a floor; with no shift: all alike
 // 4.2e-3; in bf16 8 times as much. X is held times 2^10 and A and B times 2^8 (powers of two: exact),
-// which keeps their small values out of fp16's subnormal range and leaves a factor of 20 and
-// more below its largest value.
+// which keeps their small values out of fp16's subnormal range and leaves a factor of 40 and
+// more below its largest value: X up to 63, A and B up to 255 in any element.
 //
 // The norm. Squares are summed in three classes of magnitude, each scaled to stay in
 // range, so that no finite matrix overflows or underflows it; where more than one

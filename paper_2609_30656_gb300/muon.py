@@ -119,7 +119,7 @@ def newton_schulz(g: torch.Tensor, out: torch.Tensor | None = None, out_dtype: t
 
     X = g / (||g||_F + eps), then `steps` times X <- a X + (b A + c A A) X with A = X X^T.
     The products are in fp16 with fp32 sums, 2e-4 to 2.5e-3 off the exact result in the 2-norm (all
-    singular values alike: the most), which is why the default output type is bf16; a wider
+    singular values alike: the most; a constant matrix 1.3e-2), which is why the default output type is bf16; a wider
     one is not more exact than that. out may be g. A g whose columns are
     contiguous (a transposed view) is taken as it lies."""
     lib = _bound or _library()

@@ -1,5 +1,5 @@
-"""Accuracy of Newton-Schulz updates over the spectra that training gives them and over
-magnitudes (GPU), against 64 bits.
+"""Accuracy of Newton-Schulz updates over the spectra that training gives them, over
+magnitudes, and at the limits of fp16 (GPU), against 64 bits.
 
 Limit. u = 2^-11 is fp16's rounding unit, u / sqrt(3) the root mean square of a rounding. With
 B(s) = b s^2 + c s^4 and singular values s of at most 1.2, a step adds, relative to X,
@@ -113,3 +113,40 @@ def test_a_power_of_two_times_a_matrix_has_its_factor(shape, floor, spike):
 @pytest.mark.parametrize("shape", [(1024, 1024), (100, 600)])
 def test_values_about_two_to_the_40(shape):
     _plain_norm_matters(torch.randn(shape, generator=_gen(8), device=DEV).mul(2.0 ** 40))
+
+
+# ----------------------------------------------------------------------------- range
+
+def _one_value(m, n):
+    g = torch.zeros(m, n, device=DEV)
+    g[5, 7] = 1.0
+    return g
+
+
+@pytest.mark.parametrize("m,n", [(60, 100), (150, 220)])
+def test_singular_values_up_to_the_limit_of_a(m, n):
+    """A = s^2 up to 255.9: a step that takes s to 15.9 and one that takes it back."""
+    g = _one_value(m, n)
+    for top in (15.9, 16.1):
+        table = ((top, 0.0, 0.0), (0.05, 0.0, 0.0))
+        got = mu().newton_schulz(g, steps=2, coefficients=table, out_dtype=F32)
+        if top < 16:
+            # one value: hi + lo to 2^-22, three products in fp32
+            want = reference(g, table)
+            assert (got.double() - want).abs().max().item() <= 2.0 ** -20
+        else:
+            assert not bool(got.isfinite().all())  # and no plausible number
+
+
+@pytest.mark.parametrize("m,n", [(60, 100), (150, 220)])
+def test_polynomials_up_to_the_limit_of_b(m, n):
+    """b s^2 + d of -254 and of -258 (s = 3, d = 16), with an `a` that takes most of it off again."""
+    g = _one_value(m, n)
+    for b in (-30.0, -30.5):
+        table = ((3.0, 0.0, 0.0), (-9.0 * b + 0.25, b, 0.0))
+        got = mu().newton_schulz(g, steps=2, coefficients=table, out_dtype=F32)
+        if b == -30.0:
+            # B's rounding, half of fp16's spacing of 32 of 2^8 B, times s; A = 9 and X = 3 have few bits
+            assert (got.double() - reference(g, table)).abs().max().item() <= 3 * 16 / 256 + 2.0 ** -10
+        else:
+            assert not bool(got.isfinite().all())
