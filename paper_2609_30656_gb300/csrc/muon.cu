@@ -53,7 +53,6 @@ template <int V>
 __global__ void __launch_bounds__(kNormThreads) muon_norm_kernel(MatrixIn in, SquareSum* __restrict__ partial, int* fault) {
     begin_kernel();
     const int b = blockIdx.y;
-    if (b == 0 && blockIdx.x == 0 && threadIdx.x == 0) *fault = 0;  // for the call's products
     const char* g = static_cast<const char*>(in.g) + b * in.g_batch * dtype_bytes(in.dtype);
     float* mom = in.momentum ? in.momentum + b * in.m_batch : nullptr;
     const int vecs = in.cols / V;
@@ -114,6 +113,7 @@ __global__ void __launch_bounds__(kNormThreads) muon_norm_kernel(MatrixIn in, Sq
 #pragma unroll
         for (int w = 1; w < kNormThreads / 32; ++w) s.add(sh[w]);
         partial[static_cast<int64_t>(b) * kNormBlocks + blockIdx.x] = s;
+        if (b == 0 && blockIdx.x == 0) *fault = 0;  // for the call's products
     }
 }
 
