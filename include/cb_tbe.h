@@ -446,7 +446,7 @@ cb_status cb_token_backward(const void* grad_out, cb_dtype go_dtype, int64_t go_
  *
  * which moves every singular value towards 1 and keeps the singular vectors. The usual
  * coefficients are (3.4445, -4.7750, 2.0315), five times. The products are taken in fp16 with
- * fp32 sums; in the 2-norm the result of the usual coefficients is 2e-4 to 2.5e-3 off the exact
+ * fp32 sums; in the 2-norm the result of the usual coefficients is 2e-4 to 2.8e-3 off the exact
  * one, by the matrix's singular values (up to 1.3e-2 where elements are alike and round alike,
  * as in a constant matrix: in the singular value, not in its vectors). X, A and
  * B = b A + c A A + d I are held in fp16 (d: the largest power of two not above -(b + c), 16 at most, or

@@ -19,13 +19,17 @@
 // filtered by B, which vanishes on the small directions. B is rounded with a multiple of I added
 // that keeps its diagonal small (diagonal_shift), which is taken off the term again:
 //     X' = (B + s I) hi + (a - s) hi + a lo.
-// Off the exact result in the 2-norm, usual coefficients, 64 x 128 to 1024 x 1024: singular values of 1
-// for one direction, an eighth or half of them over a floor of 1e-2 to 1e-6, 2e-4 to 2.0e-3; of Gaussian
-// matrices 1.3e-3 to 1.5e-3; all alike 1.0e-3 to 2.5e-3 (the roundings of equal diagonals add up); constant
-// matrices, all of whose roundings add up, 1.3e-2 at the most. With lo
-// in the first two steps only and a I in B after them: 1.4e-2 over a floor; with no shift: all alike
-// 4.2e-3; in bf16 8 times as much. X is held times 2^10 and A and B times 2^8 (powers of two: exact),
-// which keeps their small values out of fp16's subnormal range and leaves a factor of 40 and
+// Off the exact result in the 2-norm (260 matrices of random sizes, shorter side 16 to 1100, usual
+// coefficients): singular values of 1 for one direction, an eighth, half or nine tenths of them over
+// a floor of 1e-6 to 1e-1, at most 1.9e-3, 1.7e-3, 2.4e-3 and 2.8e-3; Gaussian matrices 2.2e-3; singular
+// values all alike 2.7e-3 (the roundings of equal diagonals add up); medians 4e-4 to 1.7e-3. Constant
+// matrices, all of whose roundings add up, 1.3e-2. With lo in the first two steps only and a I in
+// B after them, 1.4e-2 over a floor; with no shift 4.2e-3 for values all alike; in bf16 8 times as much.
+// Keeping lo throughout costs traffic in the updates' epilogues: a step of 4 x 1024 x 4096 383 -> 444 us, five
+// steps of 1024 x 1024 109 -> 111, of 2048 x 2048 218 -> 231, of 4096 x 4096 1099 -> 1144, of 128 x 256
+// 44 -> 47. (Times at the kernels compare forms with lo in two steps.)
+// X is held times 2^10 and A and B times 2^8 (powers of two: exact), which keeps their small
+// values out of fp16's subnormal range and leaves a factor of 40 and
 // more below its largest value: X up to 63, A and B up to 255 in any element.
 //
 // The norm. Squares are summed in three classes of magnitude, each scaled to stay in

@@ -290,7 +290,11 @@ __device__ __forceinline__ void finish(const ProductArgs& P, int batch, int row,
             const int64_t at = batch * P.out_batch + static_cast<int64_t>(row) * P.out_ld + col;
             store_halves(P.out_hi + at, v);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) v[k] -= __half2float(__float2half_rn(v[k]));
+            for (int k = 0; k < 32; k += 2) {  // two conversions at once, the same as those stored
+                const float2 hi = __half22float2(__floats2half2_rn(v[k], v[k + 1]));
+                v[k] -= hi.x;
+                v[k + 1] -= hi.y;
+            }
             store_halves(P.out_lo + at, v);
         }
     } else if (P.user_sectors) {

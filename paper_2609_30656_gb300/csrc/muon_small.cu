@@ -129,7 +129,11 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
     auto to_term = [&](float (&v)[32], int step) {
         const float a = P.coefficients[3 * step] * kScaleA, shift = P.shift[step] * kScaleA;
 #pragma unroll
-        for (int k = 0; k < 32; ++k) v[k] = fmaf(a, v[k], -shift * __half2float(__float2half_rn(v[k])));
+        for (int k = 0; k < 32; k += 2) {  // two conversions at once: one at a time they take a quarter of the step
+            const float2 hi = __half22float2(__floats2half2_rn(v[k], v[k + 1]));
+            v[k] = fmaf(a, v[k], -shift * hi.x);
+            v[k + 1] = fmaf(a, v[k + 1], -shift * hi.y);
+        }
     };
     for (int c = first; c < P.cols; c += NT / 4) {
         float v[32];

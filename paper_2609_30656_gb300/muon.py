@@ -1,6 +1,7 @@
 """Orthogonalised matrix updates: Newton-Schulz products, and the optimizer step around them.
 
-The Python binding of ``cb_muon_orthogonalise`` / ``cb_muon_step`` (include/cb_tbe.h):
+The Python binding of ``cb_muon_orthogonalise`` / ``cb_muon_step`` (include/cb_tbe.h). As the
+library's other calls these compute and write in place; autograd records nothing of them.
 
     o = newton_schulz(g)                                  # about U V^T of g = U S V^T
     muon_step(weight, grad, momentum, lr=3e-4, weight_decay=0.1)
@@ -118,7 +119,7 @@ def newton_schulz(g: torch.Tensor, out: torch.Tensor | None = None, out_dtype: t
     (cb_muon_orthogonalise), bf16 unless out or out_dtype is of another type.
 
     X = g / (||g||_F + eps), then `steps` times X <- a X + (b A + c A A) X with A = X X^T.
-    The products are in fp16 with fp32 sums, 2e-4 to 2.5e-3 off the exact result in the 2-norm (all
+    The products are in fp16 with fp32 sums, 2e-4 to 2.8e-3 off the exact result in the 2-norm (most or all
     singular values alike: the most; a constant matrix 1.3e-2), which is why the default output type is bf16; a wider
     one is not more exact than that. out may be g. A g whose columns are
     contiguous (a transposed view) is taken as it lies."""
@@ -185,7 +186,7 @@ def muon_step(weight: torch.Tensor, grad: torch.Tensor, momentum: torch.Tensor, 
         weight <- (1 - lr weight_decay) weight - lr update_scale(adjust) newton_schulz(u)
 
     weight and grad: fp32 / fp16 / bf16; momentum: fp32 (a running sum keeps its 32 bits).
-    The three have one shape; weight and momentum have contiguous rows."""
+    The three have one shape; weight and momentum have contiguous rows (a grad that has not is copied)."""
     lib = _bound or _library()
     index = weight.get_device()
     kinds = [_check_matrix(t, what) for t, what in ((weight, "weight"), (grad, "grad"), (momentum, "momentum"))]
