@@ -217,10 +217,7 @@ __device__ __forceinline__ uint32_t in_first_block(uint32_t addr) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
     return r;
 }
-// What a block's waits on the other's arrivals order is TMEM (by the tcgen05 fences around them)
-// and shared memory that the tensor core and TMA alone touch, so the default scope will do: a
-// wait that acquires from the cluster takes hundreds of clocks, once for every tile of K.
-// Values of another block of the cluster, at the place of `addr` here.
+// The place of `addr` here in another block of the cluster, and its values.
 __device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {
     uint32_t r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
@@ -245,6 +242,9 @@ __device__ __forceinline__ void store_cluster(uint32_t addr, uint2 v) {
 // This thread's shared-memory stores, before the tensor core reads them (and a barrier between).
 __device__ __forceinline__ void fence_to_tensor_core() { asm volatile("fence.proxy.async;" ::: "memory"); }
 
+// An arrival at the other block's barrier. What the waits on it order is TMEM (by the tcgen05 fences
+// around them) and shared memory that the tensor core and TMA alone touch, so the default scope will do: a
+// wait that acquires from the cluster takes hundreds of clocks, once for every tile of K.
 __device__ __forceinline__ void barrier_arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }

@@ -5,7 +5,8 @@ The Python binding of ``cb_token_forward`` / ``cb_token_backward`` (include/cb_t
     x = token_forward(table, tokens, scale=math.sqrt(dim))        # [..., dim]
     dE = token_backward(grad_x, tokens, table.shape[0], scale=math.sqrt(dim))
 
-Every value is computed in fp32 and rounded once to the output's type. All work is
+Autograd records nothing of them: the second is the first's derivative, called by hand. Every
+value is computed in fp32 and rounded once to the output's type. All work is
 enqueued on the current stream of the tensors' device; nothing waits.
 """
 

@@ -19,16 +19,16 @@ def _noise(shape, seed):
     return torch.randn(shape, generator=_gen(seed), device=DEV).mul(1e-3)
 
 
-SHAPES = [(1, 1001, 1400),   # 64 for the symmetric products, 64 for the update
-          (40, 130, 263),    # 128, 64, 128
-          (8, 700, 700),     # pairs of 192 for the symmetric products
-          (4, 1050, 1050),   # pairs of 224 for them
-          (200, 130, 263),   # pairs of 160 for X X^T
-          (6, 900, 1803),    # pairs of 256 for X X^T
-          (2, 900, 1803),    # pairs of 224 for the update
-          (5, 1050, 1471),   # pairs of 256 for the update
+SHAPES = [(1, 1001, 1400),   # tiles of 64 for the symmetric products, 128 for the update
+          (40, 130, 263),    # 128 for X X^T, 64
+          (8, 700, 700),     # pairs of 192 for the symmetric products, 128
+          (4, 1050, 1050),   # pairs of 224 for them, 160
+          (200, 130, 263),   # pairs of 160 for X X^T and the update, 128
+          (6, 900, 1803),    # pairs of 256 for X X^T, 128, 160
+          (2, 900, 1803),    # 64, pairs of 224 for the update
+          (5, 1050, 1471),   # 128, pairs of 256 for the update
           (1, 2050, 2900),   # pairs for all three: 160, 160, 192
-          (1, 2600, 3300)]   # 256 for all three
+          (1, 2600, 3300)]   # and 256
 
 
 @pytest.mark.parametrize("batch,m,n", SHAPES)
