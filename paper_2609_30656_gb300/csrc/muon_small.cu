@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(NT) muon_small_kernel(const MatrixIn in, const
     auto to_term = [&](float (&v)[32], int step) {
         const float a = P.coefficients[3 * step] * kScaleA, shift = P.shift[step] * kScaleA;
 #pragma unroll
-        for (int k = 0; k < 32; k += 2) {  // two conversions at once: one at a time they take a quarter of the step
+        for (int k = 0; k < 32; k += 2) {  // two conversions at once, the same as those stored
             const float2 hi = __half22float2(__floats2half2_rn(v[k], v[k + 1]));
             v[k] = fmaf(a, v[k], -shift * hi.x);
             v[k + 1] = fmaf(a, v[k + 1], -shift * hi.y);
