@@ -485,6 +485,74 @@ cb_status cb_muon_step(void* weights, cb_dtype w_dtype, int64_t w_batch_stride, 
                        float eps, const float* coefficients, int32_t steps, float update_scale,
                        void* workspace, int64_t workspace_bytes, int* error, cudaStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Layer normalisation of rows, and its backward pass (not in the paper; for the blocks of a sequence
+ * model over the looked-up rows). For each row x of dim values:
+ *
+ *   mean = sum x / dim;  rstd = 1 / sqrt(sum (x - mean)^2 / dim + eps)
+ *   out  = weight * (x - mean) * rstd + bias
+ *   grad_x = rstd * (g - mean(g) - xh * mean(g * xh)),  g = weight * grad_out, xh = (x - mean) * rstd
+ *   grad_weight = sum over rows of grad_out * xh,  grad_bias = sum over rows of grad_out
+ *
+ * in fp32, rounded once to the output's type. Sums over rows are taken in one order for a given
+ * size and alignment: deterministic.
+ *   x, out, grad_out, grad_x  device, row r at r * ..._row_stride values, each row contiguous, strides
+ *               >= dim. dim <= 2^20, rows < 2^40; either may be 0. Any alignment of the type; where all rows of all
+ *               tensors lie alike within 16 bytes they are moved fastest. out may be x, and grad_x either
+ *               input, of one type and layout.
+ *   weight, bias  device [dim], contiguous, or NULL (1 and 0)
+ *   mean, rstd  device fp32 [rows]; the forward writes each that is not NULL, the backward reads both
+ *   eps         >= 0
+ *   grad_weight, grad_bias  device fp32 [dim], every value written; NULL where not wanted
+ *   workspace   device, 256-byte aligned, of the size below at least (CB_ERR_CAPACITY otherwise; not read where
+ *               neither sum is wanted); in use until the call's work is done
+ * Errors: CB_ERR_INVALID_ARG before any GPU work, CB_ERR_CUDA if a launch fails. Nothing is allocated, nothing waits. */
+cb_status cb_layer_norm_forward(const void* x, cb_dtype x_dtype, int64_t rows, int64_t dim, int64_t x_row_stride,
+                                const void* weight, cb_dtype weight_dtype, const void* bias, cb_dtype bias_dtype,
+                                float eps, void* out, cb_dtype out_dtype, int64_t out_row_stride, float* mean,
+                                float* rstd, cudaStream_t stream);
+int64_t cb_layer_norm_backward_workspace_bytes(int64_t rows, int64_t dim);
+cb_status cb_layer_norm_backward(const void* grad_out, const void* x, cb_dtype dtype, int64_t rows, int64_t dim,
+                                 int64_t grad_out_row_stride, int64_t x_row_stride, const float* mean,
+                                 const float* rstd, const void* weight, cb_dtype weight_dtype, void* grad_x,
+                                 cb_dtype grad_x_dtype, int64_t grad_x_row_stride, float* grad_weight,
+                                 float* grad_bias, void* workspace, int64_t workspace_bytes, cudaStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * The 2-norm over all gradients of a model, and clipping to it (not in the paper):
+ *
+ *   norm = sqrt(sum over all tensors of x^2);  f = min(1, max_norm / (norm + eps));  out = f * x
+ *
+ * The norm is summed from fp32 in a fixed order with its rounding errors kept, in fp64 at the end: no overflow
+ * or underflow that the norm itself does not have; deterministic. x * f is rounded once to the output's type. A NaN gives a
+ * NaN norm and NaNs everywhere, an infinity an infinite norm and f = 0 (NaN where the infinity was): a
+ * caller who wants to skip such a step looks at the norm.
+ *   tensors     host array, read before the call returns (it may be captured into a CUDA graph)
+ *     data, out   device, `rows` rows of `cols` contiguous values, row r at r * row_stride (out_row_stride) values; out
+ *                 may be data itself (of one type and layout): values are then written only where f < 1.
+ *                 cb_grad_norm does not look at out.
+ *     count       device int64, or NULL: how many of the values there are (one row only), as for the values of
+ *                 a row-sparse gradient and its num_floats; those behind it are neither read nor written
+ *   Values that are written may not be in a second tensor of the list: CB_ERR_INVALID_ARG.
+ *   max_norm, eps  >= 0
+ *   norm        device fp32 (cb_grad_clip: or NULL)
+ *   workspace   device, 256-byte aligned, of cb_grad_norm_workspace_bytes(num_tensors) at least
+ *               (CB_ERR_CAPACITY otherwise); in use until the call's work is done
+ * Errors: CB_ERR_INVALID_ARG before any GPU work; CB_ERR_OOM if the host has no memory for its table;
+ * CB_ERR_CUDA if a launch fails. No device memory is allocated, nothing waits. */
+typedef struct {
+    const void* data;
+    void* out;
+    const int64_t* count;
+    int64_t rows, cols, row_stride, out_row_stride;
+    cb_dtype dtype, out_dtype;
+} cb_grad_tensor;
+int64_t cb_grad_norm_workspace_bytes(int64_t num_tensors);
+cb_status cb_grad_norm(const cb_grad_tensor* tensors, int64_t num_tensors, float* norm, void* workspace,
+                       int64_t workspace_bytes, cudaStream_t stream);
+cb_status cb_grad_clip(const cb_grad_tensor* tensors, int64_t num_tensors, float max_norm, float eps, float* norm,
+                       void* workspace, int64_t workspace_bytes, cudaStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif
