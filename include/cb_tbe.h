@@ -553,6 +553,72 @@ cb_status cb_grad_norm(const cb_grad_tensor* tensors, int64_t num_tensors, float
 cb_status cb_grad_clip(const cb_grad_tensor* tensors, int64_t num_tensors, float max_norm, float eps, float* norm,
                        void* workspace, int64_t workspace_bytes, cudaStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Causal attention within the sessions of a packed batch, to a window of the last tokens and to the
+ * first few of the session (not in the paper; the blocks of a sequence model). Sessions lie behind one another,
+ * session i is tokens offsets[i] .. offsets[i + 1] - 1, as bags do. Token t of a session that begins at s sees
+ * token j, s <= j <= t, where t - j < window or j - s < sinks; query head h reads key and value head
+ * h / (heads / kv_heads):
+ *
+ *   S_tj = scale q_t . k_j;  lse_t = log(sum_j exp S_tj);  out_t = sum_j exp(S_tj - lse_t) v_j
+ *   P = exp(S - lse),  dP_tj = grad_out_t . v_j,  delta_t = grad_out_t . out_t,  dS = P (dP - delta)
+ *   grad_q_t = scale sum_j dS_tj k_j;  grad_k_j = scale sum_t dS_tj q_t;  grad_v_j = sum_t P_tj grad_out_t
+ *
+ * Products of fp16 and bf16 rows are summed in fp32 by the tensor cores, P and dS rounded to the rows' type as
+ * their operands (scores, lse, sums and outputs' sums stay in fp32); those of fp32 rows are fp32 throughout. The
+ * tensor cores take rows of a multiple of 8 and at most 128 values, addresses and strides in multiples of 16
+ * bytes; other rows, up to 256 values, go key by key and are far slower. Deterministic.
+ *   q, k, v, out, grad_...  device, of one type; head h of token t at t * ..._token_stride + h * ..._head_stride
+ *               values, each row contiguous. What is written shares no value with anything else of the call.
+ *   offsets     device, idx_dtype, [sequences + 1]. They need not begin at 0 or end at `tokens`: a token of no
+ *               session gets zeros (lse: -infinity).
+ *   tokens, sequences < 2^31 - 1024, heads <= 65535, a multiple of kv_heads
+ *   window >= 1 (2^31 or more: all tokens before), sinks >= 0, scale: any value but NaN
+ *   lse         device fp32 [heads, tokens], contiguous; the forward writes it unless NULL, the backward reads it
+ *   workspace   device, 256-byte aligned, of the size below at least (CB_ERR_CAPACITY otherwise); in use until
+ *               the call's work is done
+ *   error       device int, or NULL: set (if it holds 0) to CB_ERR_BAD_OFFSETS where offsets decrease or are outside
+ *               [0, tokens]: results then have no meaning, but every access stays in bounds; to CB_ERR_TIMEOUT if
+ *               a bounded wait ran out, the results then are not whole
+ * Errors: CB_ERR_INVALID_ARG before any GPU work; CB_ERR_CUDA if a launch fails or the driver's
+ * tensor-map encoder cannot be reached. Nothing is allocated, nothing waits. */
+int64_t cb_attention_workspace_bytes(int64_t tokens, int32_t heads, int backward);  /* 0 for sizes refused */
+cb_status cb_attention_forward(const void* q, const void* k, const void* v, cb_dtype dtype, int64_t tokens,
+                               int32_t heads, int32_t kv_heads, int32_t dim, int64_t q_token_stride,
+                               int64_t q_head_stride, int64_t k_token_stride, int64_t k_head_stride,
+                               int64_t v_token_stride, int64_t v_head_stride, const void* offsets,
+                               cb_index_dtype idx_dtype, int64_t sequences, int64_t window, int64_t sinks,
+                               float scale, void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse,
+                               void* workspace, int64_t workspace_bytes, int* error, cudaStream_t stream);
+cb_status cb_attention_backward(const void* grad_out, const void* q, const void* k, const void* v, const void* out,
+                                const float* lse, cb_dtype dtype, int64_t tokens, int32_t heads, int32_t kv_heads,
+                                int32_t dim, int64_t go_token_stride, int64_t go_head_stride, int64_t q_token_stride,
+                                int64_t q_head_stride, int64_t k_token_stride, int64_t k_head_stride,
+                                int64_t v_token_stride, int64_t v_head_stride, int64_t out_token_stride,
+                                int64_t out_head_stride, const void* offsets, cb_index_dtype idx_dtype,
+                                int64_t sequences, int64_t window, int64_t sinks, float scale, void* grad_q,
+                                void* grad_k, void* grad_v, int64_t dq_token_stride, int64_t dq_head_stride,
+                                int64_t dk_token_stride, int64_t dk_head_stride, int64_t dv_token_stride,
+                                int64_t dv_head_stride, void* workspace, int64_t workspace_bytes, int* error,
+                                cudaStream_t stream);
+
+/* The same for one new token of each session, the last one in its cache: session b has lengths[b] tokens
+ * there, position p at k_cache + b * k_sequence_stride + p * k_token_stride + head * k_head_stride values (v_cache
+ * alike), and its query sees position p where lengths[b] - 1 - p < window or p < sinks. A session without tokens gets zeros.
+ *   lengths     device, idx_dtype, [sequences], 0 .. capacity; one outside sets `error` (if it holds 0) to
+ *               CB_ERR_INDEX_OOB and counts as none
+ * The rest as above. */
+int64_t cb_attention_step_workspace_bytes(int64_t sequences, int32_t heads, int32_t kv_heads, int32_t dim,
+                                          int64_t capacity, int64_t window, int64_t sinks);
+cb_status cb_attention_step(const void* q, const void* k_cache, const void* v_cache, cb_dtype dtype,
+                            int64_t sequences, int64_t capacity, int32_t heads, int32_t kv_heads, int32_t dim,
+                            int64_t q_sequence_stride, int64_t q_head_stride, int64_t k_sequence_stride,
+                            int64_t k_token_stride, int64_t k_head_stride, int64_t v_sequence_stride,
+                            int64_t v_token_stride, int64_t v_head_stride, const void* lengths,
+                            cb_index_dtype idx_dtype, int64_t window, int64_t sinks, float scale, void* out,
+                            int64_t out_sequence_stride, int64_t out_head_stride, void* workspace,
+                            int64_t workspace_bytes, int* error, cudaStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -7,4 +7,4 @@ inputs. Importing this package does not load the CUDA library; constructing a
 ``TBE`` does, and fails loudly if the library has not been built.
 """
 
-__all__ = ["workloads", "tbe", "token_embedding", "muon", "layer_norm", "clip", "next_item"]
+__all__ = ["workloads", "tbe", "token_embedding", "muon", "layer_norm", "clip", "window_attention", "next_item"]

@@ -24,7 +24,8 @@ SOURCES = ["cb_tbe.cu", "tbe_plan.cu", "tbe_forward.cu", "tbe_forward_f32.cu", "
            "fm_interaction.cu", "tbe_weight_grad.cu", "tbe_backward_apply.cu", "kjt_replicate.cu",
            "tbe_reduce_f16.cu", "tbe_reduce_bf16.cu", "tbe_reduce_f32.cu", "gather_ceiling.cu",
            "token_embedding.cu", "muon.cu", "muon_products.cu", "muon_small.cu",
-           "layer_norm.cu", "layer_norm_f32.cu", "layer_norm_f16.cu", "layer_norm_bf16.cu", "clip.cu"]
+           "layer_norm.cu", "layer_norm_f32.cu", "layer_norm_f16.cu", "layer_norm_bf16.cu", "clip.cu",
+           "window_attention.cu", "window_attention_step.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

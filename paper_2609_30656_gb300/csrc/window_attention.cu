@@ -1,0 +1,243 @@
+// window_attention.cu -- windowed attention over packed sessions (include/cb_tbe.h): where each
+// token's session begins, the kernels for rows that the tensor cores' do not take (fp32, lengths that are no
+// multiple of 8 or over 128, unaligned), and the entry points.
+#include "window_attention.cuh"
+
+#include <algorithm>
+#include <cmath>
+
+namespace cbtbe {
+namespace attention {
+namespace {
+
+constexpr int kWarps = 8;
+
+// The session of each token, by a search over the offsets. Offsets that decrease or leave [0, tokens]
+// set the error word; what is stored stays within the tokens all the same.
+__global__ void __launch_bounds__(256) attention_rows_kernel(const Shape S) {
+    begin_kernel();
+    const int64_t step = static_cast<int64_t>(gridDim.x) * blockDim.x;
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+    for (int64_t t = first; t < S.tokens; t += step) {
+        int64_t lo = 0, hi = S.sequences + 1;  // the first offset above t
+        while (lo < hi) {
+            const int64_t mid = (lo + hi) / 2;
+            if (load_index(S.offsets, mid, S.offsets32) <= t) lo = mid + 1;
+            else hi = mid;
+        }
+        int64_t s = t, e = t;
+        if (lo > 0 && lo <= S.sequences) {
+            s = max64(0, min64(load_index(S.offsets, lo - 1, S.offsets32), t));
+            e = max64(t + 1, min64(load_index(S.offsets, lo, S.offsets32), S.tokens));
+        }
+        S.start[t] = static_cast<int32_t>(s);
+        S.end[t] = static_cast<int32_t>(e);
+    }
+    if (!S.error) return;
+    for (int64_t i = first; i <= S.sequences; i += step) {
+        const int64_t here = load_index(S.offsets, i, S.offsets32);
+        const int64_t before = i ? load_index(S.offsets, i - 1, S.offsets32) : 0;
+        if (here < before || here < 0 || here > S.tokens) set_error(S.error, CB_ERR_BAD_OFFSETS);
+    }
+}
+
+// A warp for a head of a token, key after key.
+template <int DT>
+__global__ void __launch_bounds__(kWarps * 32) attention_rowwise_kernel(const Forward F) {
+    begin_kernel();
+    const Shape& S = F.S;
+    for (int64_t w = warp_id_global(); w < S.tokens * S.heads; w += warps_in_grid()) {
+        const int64_t t = w / S.heads;
+        const int h = static_cast<int>(w - t * S.heads);
+        float o[kLaneValues], lse;
+        row_output<DT>(F, t, h, o, lse);
+        store_row<DT>(F.out, t, h, S.dim, o);
+        if (F.lse && (threadIdx.x & 31) == 0) F.lse[h * S.tokens + t] = lse;
+    }
+}
+
+// delta_t = do_t . o_t for a head of a token.
+template <int DT>
+__global__ void __launch_bounds__(kWarps * 32) attention_delta_rowwise_kernel(const Backward B) {
+    begin_kernel();
+    const Shape& S = B.S;
+    for (int64_t w = warp_id_global(); w < S.tokens * S.heads; w += warps_in_grid()) {
+        const int64_t t = w / S.heads;
+        const int h = static_cast<int>(w - t * S.heads);
+        float a[kLaneValues], b[kLaneValues];
+        load_row<DT>(B.go, t, h, S.dim, a);
+        load_row<DT>(B.out, t, h, S.dim, b);
+        const float d = dot(a, b);
+        if ((threadIdx.x & 31) == 0) B.delta[h * S.tokens + t] = d;
+    }
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kWarps * 32) attention_dq_rowwise_kernel(const Backward B) {
+    begin_kernel();
+    const Shape& S = B.S;
+    for (int64_t w = warp_id_global(); w < S.tokens * S.heads; w += warps_in_grid()) {
+        const int64_t t = w / S.heads;
+        const int h = static_cast<int>(w - t * S.heads);
+        float dq[kLaneValues];
+        row_dq<DT>(B, t, h, dq);
+        store_row<DT>(B.dq, t, h, S.dim, dq);
+    }
+}
+
+// A warp for a head of a key, over the heads that share it and the tokens that see it.
+template <int DT>
+__global__ void __launch_bounds__(kWarps * 32) attention_dkv_rowwise_kernel(const Backward B) {
+    begin_kernel();
+    const Shape& S = B.S;
+    for (int64_t w = warp_id_global(); w < S.tokens * S.kv_heads; w += warps_in_grid()) {
+        const int64_t j = w / S.kv_heads;
+        const int kv = static_cast<int>(w - j * S.kv_heads);
+        float dk[kLaneValues], dv[kLaneValues];
+        row_dkv<DT>(B, j, kv, dk, dv);
+        store_row<DT>(B.dk, j, kv, S.dim, dk);
+        store_row<DT>(B.dv, j, kv, S.dim, dv);
+    }
+}
+
+template <int DT>
+void launch_forward_rowwise(const Forward& F, cudaStream_t s) {
+    launch(attention_rowwise_kernel<DT>, dim3(warp_grid(F.S.tokens * F.S.heads, 1 << 20)), dim3(kWarps * 32), 0, s, F);
+}
+template <int DT>
+void launch_backward_rowwise(const Backward& B, cudaStream_t s) {
+    const dim3 rows(warp_grid(B.S.tokens * B.S.heads, 1 << 20)), keys(warp_grid(B.S.tokens * B.S.kv_heads, 1 << 20));
+    launch(attention_delta_rowwise_kernel<DT>, rows, dim3(kWarps * 32), 0, s, B);
+    launch(attention_dq_rowwise_kernel<DT>, rows, dim3(kWarps * 32), 0, s, B);
+    launch(attention_dkv_rowwise_kernel<DT>, keys, dim3(kWarps * 32), 0, s, B);
+}
+
+bool type_ok(int t) { return t == CB_F32 || t == CB_F16 || t == CB_BF16; }
+constexpr int64_t kMostTokens = (int64_t{1} << 31) - 1024, kMostStride = int64_t{1} << 40;
+
+bool heads_ok(const Shape& S, const Heads& h, int heads, bool written) {
+    const int size = S.dtype == CB_F32 ? 4 : 2;
+    if (!h.data || reinterpret_cast<uintptr_t>(h.data) % size || h.token < 0 || h.head < 0 || h.token > kMostStride ||
+        h.head > kMostStride)
+        return false;
+    return !written || rows_apart(S.tokens, h.token, heads, h.head, S.dim);
+}
+cb_status sizes_ok(const Shape& S) {
+    if (!type_ok(S.dtype) || S.tokens < 0 || S.tokens > kMostTokens || S.sequences < 0 || S.sequences > kMostTokens ||
+        S.heads < 1 || S.kv_heads < 1 || S.heads > 65535 || S.heads % S.kv_heads || S.dim < 1 || S.dim > kMaxDim ||
+        S.window < 1 || S.sinks < 0 || !(S.scale == S.scale) || !S.offsets ||
+        reinterpret_cast<uintptr_t>(S.offsets) % (S.offsets32 ? 4 : 8) || reinterpret_cast<uintptr_t>(S.error) % 4)
+        return CB_ERR_INVALID_ARG;
+    return CB_OK;
+}
+Shape shape(int dtype, int64_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, const void* offsets, int idx, int64_t sequences,
+            int64_t window, int64_t sinks, float scale, int* error) {
+    Shape S{};
+    S.tokens = tokens;
+    S.sequences = sequences;
+    S.window = std::min<int64_t>(window, kMostTokens);
+    S.heads = heads;
+    S.kv_heads = kv_heads;
+    S.group = kv_heads > 0 ? heads / kv_heads : 0;
+    S.dim = dim;
+    S.sinks = sinks < 0 ? -1 : static_cast<int32_t>(std::min<int64_t>(sinks, kMostTokens));
+    S.dtype = dtype;
+    S.scale = scale;
+    S.offsets = idx == CB_I32 || idx == CB_I64 ? offsets : nullptr;
+    S.offsets32 = idx == CB_I32;
+    S.error = error;
+    return S;
+}
+bool workspace_ok(const void* w, int64_t bytes, int64_t need) {
+    return w && reinterpret_cast<uintptr_t>(w) % 256 == 0 && bytes >= need;
+}
+void set_rows(Shape& S, void* workspace, cudaStream_t s) {
+    S.start = static_cast<int32_t*>(workspace);
+    S.end = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + rows_bytes(S.tokens));
+    const int64_t n = std::max(S.tokens, S.sequences + 1);
+    launch(attention_rows_kernel, dim3(static_cast<unsigned>(std::min<int64_t>((n + 255) / 256, 1 << 16))), dim3(256), 0, s, S);
+}
+
+}  // namespace
+
+bool tensor_core_rows(const Shape& S, const Heads& h) {
+    return S.dtype != CB_F32 && S.dim % 8 == 0 && S.dim <= 128 && reinterpret_cast<uintptr_t>(h.data) % 16 == 0 &&
+           h.token % 8 == 0 && h.head % 8 == 0;
+}
+
+}  // namespace attention
+}  // namespace cbtbe
+
+extern "C" int64_t cb_attention_workspace_bytes(int64_t tokens, int32_t heads, int backward) {
+    using namespace cbtbe::attention;
+    if (tokens <= 0 || tokens > kMostTokens || heads < 1) return 0;
+    return static_cast<int64_t>(2 * rows_bytes(tokens) + (backward ? rows_bytes(tokens * heads) : 0));
+}
+
+extern "C" cb_status cb_attention_forward(const void* q, const void* k, const void* v, cb_dtype dtype, int64_t tokens,
+                                          int32_t heads, int32_t kv_heads, int32_t dim, int64_t q_token_stride,
+                                          int64_t q_head_stride, int64_t k_token_stride, int64_t k_head_stride,
+                                          int64_t v_token_stride, int64_t v_head_stride, const void* offsets,
+                                          cb_index_dtype idx_dtype, int64_t sequences, int64_t window, int64_t sinks,
+                                          float scale, void* out, int64_t out_token_stride, int64_t out_head_stride, float* lse,
+                                          void* workspace, int64_t workspace_bytes, int* error, cudaStream_t stream) {
+    using namespace cbtbe::attention;
+    Forward F{};
+    F.S = shape(dtype, tokens, heads, kv_heads, dim, offsets, idx_dtype, sequences, window, sinks, scale, error);
+    if (sizes_ok(F.S) != CB_OK) return CB_ERR_INVALID_ARG;
+    if (tokens == 0) return CB_OK;
+    F.q = {q, q_token_stride, q_head_stride};
+    F.k = {k, k_token_stride, k_head_stride};
+    F.v = {v, v_token_stride, v_head_stride};
+    F.out = {out, out_token_stride, out_head_stride};
+    F.lse = lse;
+    if (!heads_ok(F.S, F.q, heads, false) || !heads_ok(F.S, F.k, kv_heads, false) || !heads_ok(F.S, F.v, kv_heads, false) ||
+        !heads_ok(F.S, F.out, heads, true) || reinterpret_cast<uintptr_t>(lse) % 4)
+        return CB_ERR_INVALID_ARG;
+    if (!workspace_ok(workspace, workspace_bytes, cb_attention_workspace_bytes(tokens, heads, 0))) return CB_ERR_CAPACITY;
+    set_rows(F.S, workspace, stream);
+    bool ok = true;
+    if (dtype == CB_F32) launch_forward_rowwise<CB_F32>(F, stream);
+    else if (dtype == CB_F16) launch_forward_rowwise<CB_F16>(F, stream);
+    else launch_forward_rowwise<CB_BF16>(F, stream);
+    return cudaGetLastError() == cudaSuccess && ok ? CB_OK : CB_ERR_CUDA;
+}
+
+extern "C" cb_status cb_attention_backward(const void* grad_out, const void* q, const void* k, const void* v, const void* out,
+                                           const float* lse, cb_dtype dtype, int64_t tokens, int32_t heads, int32_t kv_heads,
+                                           int32_t dim, int64_t go_token_stride, int64_t go_head_stride, int64_t q_token_stride,
+                                           int64_t q_head_stride, int64_t k_token_stride, int64_t k_head_stride,
+                                           int64_t v_token_stride, int64_t v_head_stride, int64_t out_token_stride,
+                                           int64_t out_head_stride, const void* offsets, cb_index_dtype idx_dtype,
+                                           int64_t sequences, int64_t window, int64_t sinks, float scale, void* grad_q,
+                                           void* grad_k, void* grad_v, int64_t dq_token_stride, int64_t dq_head_stride,
+                                           int64_t dk_token_stride, int64_t dk_head_stride, int64_t dv_token_stride,
+                                           int64_t dv_head_stride, void* workspace, int64_t workspace_bytes, int* error,
+                                           cudaStream_t stream) {
+    using namespace cbtbe::attention;
+    Backward B{};
+    B.S = shape(dtype, tokens, heads, kv_heads, dim, offsets, idx_dtype, sequences, window, sinks, scale, error);
+    if (sizes_ok(B.S) != CB_OK) return CB_ERR_INVALID_ARG;
+    if (tokens == 0) return CB_OK;
+    B.go = {grad_out, go_token_stride, go_head_stride};
+    B.q = {q, q_token_stride, q_head_stride};
+    B.k = {k, k_token_stride, k_head_stride};
+    B.v = {v, v_token_stride, v_head_stride};
+    B.out = {out, out_token_stride, out_head_stride};
+    B.dq = {grad_q, dq_token_stride, dq_head_stride};
+    B.dk = {grad_k, dk_token_stride, dk_head_stride};
+    B.dv = {grad_v, dv_token_stride, dv_head_stride};
+    B.lse = lse;
+    if (!heads_ok(B.S, B.go, heads, false) || !heads_ok(B.S, B.q, heads, false) || !heads_ok(B.S, B.k, kv_heads, false) ||
+        !heads_ok(B.S, B.v, kv_heads, false) || !heads_ok(B.S, B.out, heads, false) || !heads_ok(B.S, B.dq, heads, true) ||
+        !heads_ok(B.S, B.dk, kv_heads, true) || !heads_ok(B.S, B.dv, kv_heads, true) || !lse ||
+        reinterpret_cast<uintptr_t>(lse) % 4)
+        return CB_ERR_INVALID_ARG;
+    if (!workspace_ok(workspace, workspace_bytes, cb_attention_workspace_bytes(tokens, heads, 1))) return CB_ERR_CAPACITY;
+    set_rows(B.S, workspace, stream);
+    B.delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * rows_bytes(tokens));
+    if (dtype == CB_F32) launch_backward_rowwise<CB_F32>(B, stream);
+    else if (dtype == CB_F16) launch_backward_rowwise<CB_F16>(B, stream);
+    else launch_backward_rowwise<CB_BF16>(B, stream);
+    return cudaGetLastError() == cudaSuccess ? CB_OK : CB_ERR_CUDA;
+}

@@ -1,0 +1,187 @@
+// window_attention.cuh -- what the kernels of windowed attention over packed sessions share.
+//
+//   token t of a session [s, e) sees token j, s <= j <= t, where t - j < window or j - s < sinks
+//   S_tj = scale q_t . k_j,  lse_t = log sum_j exp S_tj,  P = exp(S - lse),  o_t = sum_j P_tj v_j
+//   dv_j = sum_t P_tj do_t,  dP_tj = do_t . v_j,  delta_t = do_t . o_t,  dS = P (dP - delta)
+//   dq_t = scale sum_j dS_tj k_j,  dk_j = scale sum_t dS_tj q_t
+//
+// A tile of 128 tokens of the packed batch may hold many sessions: which token a row may see is a matter of
+// where its session begins, which one small kernel looks up for every token first.
+#pragma once
+
+#include "token_rows.cuh"
+
+namespace cbtbe {
+namespace attention {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct Heads {  // head h of token t at t * token + h * head values
+    const void* data;
+    int64_t token, head;
+};
+
+struct Shape {
+    int64_t tokens, sequences, window;
+    int32_t heads, kv_heads, group, dim, sinks, dtype;
+    float scale;
+    const void* offsets;
+    int32_t offsets32;
+    int32_t* start;  // [tokens] where the token's session begins, and
+    int32_t* end;    // [tokens] ends; both t for a token t of no session
+    int* error;      // or null
+};
+
+// Sum over a warp, in every lane.
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) v += __shfl_xor_sync(kFull, v, off);
+    return v;
+}
+
+struct Forward {
+    Shape S;
+    Heads q, k, v, out;
+    float* lse;  // [heads, tokens], or null
+};
+struct Backward {
+    Shape S;
+    Heads go, q, k, v, out, dq, dk, dv;
+    const float* lse;
+    float* delta;  // [heads, tokens]
+};
+
+// ---------------------------------------------------------------- a row at a time
+
+// Rows of any type and length up to 256, by a warp that goes key by key, in fp32. The tensor-core kernels
+// turn to it for a row whose result is not finite: their tiles multiply what a row does not see by
+// zeros, which infinities and NaNs of other sessions, or of unused memory, survive.
+constexpr int kMaxDim = 256, kLaneValues = kMaxDim / 32;
+
+// A row of up to 256 values, value lane + 32 i in v[i].
+template <int DT>
+__device__ __forceinline__ void load_row(const Heads& h, int64_t token, int head, int dim, float (&v)[kLaneValues]) {
+    const int64_t at = token * h.token + head * h.head;
+#pragma unroll
+    for (int i = 0; i < kLaneValues; ++i) {
+        const int c = (threadIdx.x & 31) + 32 * i;
+        v[i] = 0.f;
+        if (c < dim) {
+            if constexpr (DT == CB_F32) v[i] = static_cast<const float*>(h.data)[at + c];
+            else v[i] = widen<DT>(static_cast<const uint16_t*>(h.data)[at + c]);
+        }
+    }
+}
+template <int DT>
+__device__ __forceinline__ void store_row(const Heads& h, int64_t token, int head, int dim, const float (&v)[kLaneValues]) {
+    const int64_t at = token * h.token + head * h.head;
+    void* data = const_cast<void*>(h.data);
+#pragma unroll
+    for (int i = 0; i < kLaneValues; ++i) {
+        const int c = (threadIdx.x & 31) + 32 * i;
+        if (c >= dim) continue;
+        if constexpr (DT == CB_F32) static_cast<float*>(data)[at + c] = v[i];
+        else static_cast<uint16_t*>(data)[at + c] = static_cast<uint16_t>(narrow<DT>(v[i]));
+    }
+}
+__device__ __forceinline__ float dot(const float (&a)[kLaneValues], const float (&b)[kLaneValues]) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < kLaneValues; ++i) s = fmaf(a[i], b[i], s);
+    return warp_sum(s);
+}
+__device__ __forceinline__ void add_scaled(float (&a)[kLaneValues], float f, const float (&b)[kLaneValues]) {
+#pragma unroll
+    for (int i = 0; i < kLaneValues; ++i) a[i] = fmaf(f, b[i], a[i]);
+}
+
+// What token t sees: [start, sinks_end) and [first, t].
+struct Seen {
+    int64_t start, sinks_end, first;
+};
+__device__ __forceinline__ Seen seen_by(const Shape& S, int64_t t) {
+    Seen a;
+    a.start = S.start[t];
+    a.first = max64(a.start, t - S.window + 1);
+    a.sinks_end = min64(a.start + S.sinks, a.first);
+    return a;
+}
+
+// Head h of token t: its output, and its lse.
+template <int DT>
+__device__ __forceinline__ void row_output(const Forward& F, int64_t t, int h, float (&o)[kLaneValues], float& lse) {
+    const Shape& S = F.S;
+    const int kv = h / S.group;
+    float q[kLaneValues], k[kLaneValues], v[kLaneValues];
+    float most = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kLaneValues; ++i) o[i] = 0.f;
+    lse = -INFINITY;
+    if (S.end[t] <= t) return;
+    const Seen a = seen_by(S, t);
+    load_row<DT>(F.q, t, h, S.dim, q);
+    for (int64_t j = a.start < a.sinks_end ? a.start : a.first; j <= t; j = j + 1 == a.sinks_end ? a.first : j + 1) {
+        load_row<DT>(F.k, j, kv, S.dim, k);
+        load_row<DT>(F.v, j, kv, S.dim, v);
+        const float s = dot(q, k) * (S.scale * kLog2e);
+        const float top = fmaxf(most, s), keep = most == top ? 1.f : exp2f(most - top), p = exp2f(s - top);
+        sum = fmaf(sum, keep, p);
+#pragma unroll
+        for (int i = 0; i < kLaneValues; ++i) o[i] = fmaf(o[i], keep, p * v[i]);
+        most = top;
+    }
+#pragma unroll
+    for (int i = 0; i < kLaneValues; ++i) o[i] /= sum;
+    lse = (most + log2f(sum)) * kLn2;
+}
+template <int DT>
+__device__ __forceinline__ void row_dq(const Backward& B, int64_t t, int h, float (&dq)[kLaneValues]) {
+    const Shape& S = B.S;
+    const int kv = h / S.group;
+    float q[kLaneValues], go[kLaneValues], k[kLaneValues], v[kLaneValues];
+#pragma unroll
+    for (int i = 0; i < kLaneValues; ++i) dq[i] = 0.f;
+    if (S.end[t] <= t) return;
+    const Seen a = seen_by(S, t);
+    load_row<DT>(B.q, t, h, S.dim, q);
+    load_row<DT>(B.go, t, h, S.dim, go);
+    const float lse = B.lse[h * S.tokens + t], delta = B.delta[h * S.tokens + t];
+    for (int64_t j = a.start < a.sinks_end ? a.start : a.first; j <= t; j = j + 1 == a.sinks_end ? a.first : j + 1) {
+        load_row<DT>(B.k, j, kv, S.dim, k);
+        load_row<DT>(B.v, j, kv, S.dim, v);
+        const float p = exp2f((dot(q, k) * S.scale - lse) * kLog2e);
+        add_scaled(dq, p * (dot(go, v) - delta) * S.scale, k);
+    }
+}
+// Head kv of key j, over the heads that share it and the tokens that see it.
+template <int DT>
+__device__ __forceinline__ void row_dkv(const Backward& B, int64_t j, int kv, float (&dk)[kLaneValues], float (&dv)[kLaneValues]) {
+    const Shape& S = B.S;
+    float q[kLaneValues], go[kLaneValues], k[kLaneValues], v[kLaneValues];
+#pragma unroll
+    for (int i = 0; i < kLaneValues; ++i) dk[i] = dv[i] = 0.f;
+    const int64_t end = S.end[j];
+    if (end <= j) return;
+    const int64_t last = j - S.start[j] < S.sinks ? end : min64(end, j + S.window);
+    load_row<DT>(B.k, j, kv, S.dim, k);
+    load_row<DT>(B.v, j, kv, S.dim, v);
+    for (int h = kv * S.group; h < (kv + 1) * S.group; ++h)
+        for (int64_t t = j; t < last; ++t) {
+            load_row<DT>(B.q, t, h, S.dim, q);
+            load_row<DT>(B.go, t, h, S.dim, go);
+            const float p = exp2f((dot(q, k) * S.scale - B.lse[h * S.tokens + t]) * kLog2e);
+            add_scaled(dv, p, go);
+            add_scaled(dk, p * (dot(go, v) - B.delta[h * S.tokens + t]) * S.scale, q);
+        }
+}
+
+inline size_t rows_bytes(int64_t tokens) { return static_cast<size_t>((tokens * 4 + 255) / 256 * 256); }
+
+// The tensor-core kernels (window_attention_forward.cu, window_attention_backward.cu); they want fp16 or
+// bf16, rows of a multiple of 8 and at most 128 values, addresses and strides in multiples of 16 bytes.
+bool tensor_core_rows(const Shape& S, const Heads& h);
+bool launch_forward(const Forward& F, cudaStream_t s);
+bool launch_backward(const Backward& B, cudaStream_t s);
+
+}  // namespace attention
+}  // namespace cbtbe
