@@ -113,6 +113,7 @@ void launch_backward_rowwise(const Backward& B, cudaStream_t s) {
 }
 
 bool type_ok(int t) { return t == CB_F32 || t == CB_F16 || t == CB_BF16; }
+constexpr int64_t kMostTmaStride = int64_t{1} << 38;  // values: 2^40 bytes are refused
 constexpr int64_t kMostTokens = (int64_t{1} << 31) - 1024, kMostStride = int64_t{1} << 40;
 
 bool heads_ok(const Shape& S, const Heads& h, int heads, bool written) {
@@ -160,9 +161,10 @@ void set_rows(Shape& S, void* workspace, cudaStream_t s) {
 
 }  // namespace
 
-bool tensor_core_rows(const Shape& S, const Heads& h) {
+bool tensor_core_rows(const Shape& S, const Heads& h, int heads) {
     return S.dtype != CB_F32 && S.dim % 8 == 0 && S.dim <= 128 && reinterpret_cast<uintptr_t>(h.data) % 16 == 0 &&
-           h.token % 8 == 0 && h.head % 8 == 0;
+           (S.tokens <= 1 || (h.token % 8 == 0 && h.token >= S.dim && h.token < kMostTmaStride)) &&
+           (heads <= 1 || (h.head % 8 == 0 && h.head >= S.dim && h.head < kMostTmaStride));
 }
 
 }  // namespace attention
@@ -197,7 +199,10 @@ extern "C" cb_status cb_attention_forward(const void* q, const void* k, const vo
     if (!workspace_ok(workspace, workspace_bytes, cb_attention_workspace_bytes(tokens, heads, 0))) return CB_ERR_CAPACITY;
     set_rows(F.S, workspace, stream);
     bool ok = true;
-    if (dtype == CB_F32) launch_forward_rowwise<CB_F32>(F, stream);
+    if (tensor_core_rows(F.S, F.q, heads) && tensor_core_rows(F.S, F.k, kv_heads) && tensor_core_rows(F.S, F.v, kv_heads) &&
+        tensor_core_rows(F.S, F.out, heads))
+        ok = launch_forward(F, stream);
+    else if (dtype == CB_F32) launch_forward_rowwise<CB_F32>(F, stream);
     else if (dtype == CB_F16) launch_forward_rowwise<CB_F16>(F, stream);
     else launch_forward_rowwise<CB_BF16>(F, stream);
     return cudaGetLastError() == cudaSuccess && ok ? CB_OK : CB_ERR_CUDA;

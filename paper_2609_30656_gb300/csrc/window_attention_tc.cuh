@@ -1,0 +1,202 @@
+// window_attention_tc.cuh -- what the tensor-core kernels of windowed attention share: tiles of
+// 128 rows by TMA, products with an operand in TMEM, what a tile of rows sees, and its masks.
+#pragma once
+
+#include "tensor_core.cuh"
+#include "window_attention.cuh"
+
+namespace cbtbe {
+namespace attention {
+
+constexpr int kTile = 128;                       // rows (tokens) of a tile
+constexpr uint32_t kBoxBytes = kTile * 64 * 2;   // 64 values of each, as TMA copies them
+template <int D> constexpr uint32_t kRowsBytes = D / 64 * kBoxBytes;
+
+// ---------------------------------------------------------------- instructions
+
+// D (+)= A B over 16 values of K, A of 128 rows in TMEM (two values a column).
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t shape, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(shape), "r"(static_cast<uint32_t>(add))
+        : "memory");
+}
+// tc::mma_shape of bf16 operands.
+template <bool BF16>
+__host__ __device__ constexpr uint32_t mma_shape(int m, int n, bool b_mn_major) {
+    return tc::mma_shape(m, n, b_mn_major) | (BF16 ? 1u << 7 | 1u << 10 : 0u);
+}
+
+#define CB_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define CB_R32(r, i) CB_R8(r, i), CB_R8(r, i + 8), CB_R8(r, i + 16), CB_R8(r, i + 24)
+
+// 64 columns of the warp's 32 lanes; they have arrived when the call returns.
+__device__ __forceinline__ void tmem_load64(uint32_t addr, uint32_t (&r)[64]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+        "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+        "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : CB_R32(r, 0), CB_R32(r, 32)
+        : "r"(addr)
+        : "memory");
+}
+// 32 columns, without the wait for them (tmem_store_wait).
+__device__ __forceinline__ void tmem_store32_begin(uint32_t addr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+        "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]),
+        "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// a * b + c and a + b of two values at once.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+        "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+        "mul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    uint32_t r;
+    if constexpr (BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// Registers of a thread from here on, by all warps of a group of four.
+template <int N>
+__device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+// `count` threads at barrier `id` (1 .. 15).
+__device__ __forceinline__ void named_barrier(int id, int count) {
+    asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(count) : "memory");
+}
+
+__device__ __forceinline__ void tma_store(const CUtensorMap* map, uint32_t src, int32_t x, int32_t y, int32_t z) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(
+                     reinterpret_cast<uint64_t>(map)),
+                 "r"(src), "r"(x), "r"(y), "r"(z)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_store_done() {  // read from shared memory
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+}
+
+// A tile of `D` columns: head `head`, tokens from `token` on.
+template <int D>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int token) {
+#pragma unroll
+    for (int x = 0; x < D / 64; ++x) tc::tma_load(dst + x * kBoxBytes, map, bar, x * 64, head, token);
+}
+
+// Byte of columns 8 c .. 8 c + 7 (16 bytes) of row r in a tile as TMA lays it out.
+__device__ __forceinline__ uint32_t tile_byte(int r, int c) {
+    return static_cast<uint32_t>(c >> 3) * kBoxBytes + static_cast<uint32_t>(r) * 128 + static_cast<uint32_t>(((c & 7) ^ (r & 7)) << 4);
+}
+
+// ---------------------------------------------------------------- what rows see
+
+// Bits i of columns [a, b) among the 32 from `first` on.
+__device__ __forceinline__ uint32_t range_bits(int a, int b, int first) {
+    const int lo = max(a - first, 0), hi = min(b - first, 32);
+    if (lo >= hi) return 0u;
+    return (hi >= 32 ? ~0u : (1u << hi) - 1u) & ~((1u << lo) - 1u);
+}
+
+// Two intervals of positions: a row's tokens in sight, or (for a key) the rows that see it.
+struct TwoRanges {
+    int a0, a1, b0, b1;
+    __device__ __forceinline__ uint32_t bits(int first) const { return range_bits(a0, a1, first) | range_bits(b0, b1, first); }
+    __device__ __forceinline__ bool all(int first, int n) const { return a0 <= first && a1 >= first + n; }
+    __device__ __forceinline__ bool none(int first, int n) const {
+        return (a1 <= first || a0 >= first + n || a0 >= a1) && (b1 <= first || b0 >= first + n || b0 >= b1);
+    }
+};
+
+// The keys that the rows of a tile see: [lo, hi), and before that the first tokens of the
+// session that the tile begins in, [s0, s1). All empty where the tile has no token of a session.
+struct Sight {
+    int lo, hi, s0, s1;
+};
+// By the 128 threads of the tile's rows (thread's row: `t`), joined by `sight_of` behind a barrier.
+struct SightParts {
+    int lo[4], hi[4], s0[4];
+};
+struct Row {
+    int start, first;  // of the session, and of the window; both t + 1 where t is of no session
+    bool real;
+};
+__device__ __forceinline__ Row row_of(const Shape& S, int64_t t) {
+    Row r{0, 0, false};
+    if (t < S.tokens && S.end[t] > t) {
+        r.start = S.start[t];
+        r.first = static_cast<int>(max64(r.start, t - S.window + 1));
+        r.real = true;
+    }
+    return r;
+}
+__device__ __forceinline__ void note_row(SightParts& P, const Row& r, int t, int warp, int lane) {
+    const int lo = __reduce_min_sync(kFull, r.real ? r.first : INT32_MAX);
+    const int hi = __reduce_max_sync(kFull, r.real ? t + 1 : 0);
+    const int s0 = __reduce_min_sync(kFull, r.real ? r.start : INT32_MAX);
+    if (lane == 0) {
+        P.lo[warp] = lo;
+        P.hi[warp] = hi;
+        P.s0[warp] = s0;
+    }
+}
+__device__ __forceinline__ Sight sight_of(const SightParts& P, int sinks) {
+    Sight s;
+    s.lo = min(min(P.lo[0], P.lo[1]), min(P.lo[2], P.lo[3]));
+    s.hi = max(max(P.hi[0], P.hi[1]), max(P.hi[2], P.hi[3]));
+    const int s0 = min(min(P.s0[0], P.s0[1]), min(P.s0[2], P.s0[3]));
+    s.s0 = s.s1 = 0;
+    if (s.hi == 0) s.lo = 0;
+    else if (s0 < s.lo) {
+        s.s0 = s0;
+        s.s1 = static_cast<int>(min64(static_cast<int64_t>(s0) + sinks, s.lo));
+    }
+    return s;
+}
+__host__ __device__ __forceinline__ int tiles_of(int n) { return (n + kTile - 1) / kTile; }
+
+bool tile_map(CUtensorMap* map, const Heads& h, int64_t tokens, int32_t heads, int32_t dim, int32_t dtype);
+
+}  // namespace attention
+}  // namespace cbtbe

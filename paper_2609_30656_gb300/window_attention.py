@@ -68,7 +68,7 @@ def _rows(t: torch.Tensor) -> torch.Tensor:
     if t.shape[-1] > 1 and stride[-1] != 1:
         return t.contiguous()
     if t.dtype != torch.float32 and t.shape[-1] % 8 == 0 and t.shape[-1] <= 128:  # the tensor cores' copies: 16 bytes
-        if t.data_ptr() % 16 or any(s % 8 for s, n in zip(stride[:-1], t.shape) if n > 1):
+        if t.data_ptr() % 16 or any(s % 8 or s < t.shape[-1] for s, n in zip(stride[:-1], t.shape) if n > 1):
             return t.clone(memory_format=torch.contiguous_format)
     return t
 

@@ -134,8 +134,15 @@ def test_infinities_and_nan_behind_the_mask_stay_there(dtype):
         t[130] = float("inf")
     out2, lse2 = wa.window_attention(q2, k2, v2, off, 30, 0, stats=True)
     grads2 = wa.window_attention_backward(go2, q2, k2, v2, out2, lse2, off, 30, 0)
-    for a, b in ((out, out2), *zip(grads, grads2)):
-        assert torch.equal(a[:100], b[:100]) and torch.equal(a[190:], b[190:])
+    # Rows of the other sessions that share a tile with it may be computed another way (with P and dS unrounded): within the
+    # same bounds, not always the same bits.
+    want = reference(q, k, v, visible(310, lens, 30, 0), 0.125, go)
+    apart = torch.ones(310, dtype=torch.bool, device=DEV)
+    apart[100:190] = False
+    for name, a, b in zip(("out", "dq", "dk", "dv"), (out, *grads), (out2, *grads2)):
+        for got in (a, b):
+            check(got[apart], (want[name][0][apart], want[name][1][apart]), name)
+    check(lse2[:, apart], (want["lse"][0][:, apart], want["lse"][1][:, apart]))
     assert out2[130:160].isnan().any()
 
 
