@@ -1,10 +1,11 @@
 // window_attention.cu -- windowed attention over packed sessions (include/cb_tbe.h): where each
 // token's session begins, the kernels for rows that the tensor cores' do not take (fp32, lengths that are no
 // multiple of 8 or over 128, unaligned), and the entry points.
-#include "window_attention.cuh"
+#include "window_attention_tc.cuh"
 
 #include <algorithm>
 #include <cmath>
+#include <cudaTypedefs.h>
 
 namespace cbtbe {
 namespace attention {
@@ -33,6 +34,7 @@ __global__ void __launch_bounds__(256) attention_rows_kernel(const Shape S) {
         S.start[t] = static_cast<int32_t>(s);
         S.end[t] = static_cast<int32_t>(e);
     }
+    if (S.largest && first == 0) *S.largest = 0u;
     if (!S.error) return;
     for (int64_t i = first; i <= S.sequences; i += step) {
         const int64_t here = load_index(S.offsets, i, S.offsets32);
@@ -152,15 +154,45 @@ Shape shape(int dtype, int64_t tokens, int32_t heads, int32_t kv_heads, int32_t 
 bool workspace_ok(const void* w, int64_t bytes, int64_t need) {
     return w && reinterpret_cast<uintptr_t>(w) % 256 == 0 && bytes >= need;
 }
-void set_rows(Shape& S, void* workspace, cudaStream_t s) {
+void set_rows(Shape& S, void* workspace, uint32_t* largest, cudaStream_t s) {
     S.start = static_cast<int32_t*>(workspace);
     S.end = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + rows_bytes(S.tokens));
+    S.largest = largest;
     const int64_t n = std::max(S.tokens, S.sequences + 1);
     launch(attention_rows_kernel, dim3(static_cast<unsigned>(std::min<int64_t>((n + 255) / 256, 1 << 16))), dim3(256), 0, s, S);
 }
 
+PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
+    static PFN_cuTensorMapEncodeTiled_v12000 encode = [] {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            fn = nullptr;
+        }
+        return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
+    }();
+    return encode;
+}
+
 }  // namespace
 
+// [tokens][heads][dim] in boxes of 64 values of 128 tokens of one head; what is outside reads as zeros.
+bool tile_map(CUtensorMap* map, const Heads& h, int64_t tokens, int32_t heads, int32_t dim, int32_t dtype) {
+    if (!tensor_map_encoder()) return false;
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(tokens)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(heads > 1 ? h.head : dim) * 2,
+                                   static_cast<cuuint64_t>(tokens > 1 ? h.token : dim) * 2};
+    const cuuint32_t box[3] = {64, 1, kTile};
+    const cuuint32_t step[3] = {1, 1, 1};
+    return tensor_map_encoder()(map, dtype == CB_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
+                                const_cast<void*>(h.data), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Rows that TMA can copy: 16-byte addresses and strides, no two rows in one place.
 bool tensor_core_rows(const Shape& S, const Heads& h, int heads) {
     return S.dtype != CB_F32 && S.dim % 8 == 0 && S.dim <= 128 && reinterpret_cast<uintptr_t>(h.data) % 16 == 0 &&
            (S.tokens <= 1 || (h.token % 8 == 0 && h.token >= S.dim && h.token < kMostTmaStride)) &&
@@ -173,7 +205,7 @@ bool tensor_core_rows(const Shape& S, const Heads& h, int heads) {
 extern "C" int64_t cb_attention_workspace_bytes(int64_t tokens, int32_t heads, int backward) {
     using namespace cbtbe::attention;
     if (tokens <= 0 || tokens > kMostTokens || heads < 1) return 0;
-    return static_cast<int64_t>(2 * rows_bytes(tokens) + (backward ? rows_bytes(tokens * heads) : 0));
+    return static_cast<int64_t>(2 * rows_bytes(tokens) + (backward ? rows_bytes(tokens * heads) + 256 : 0));
 }
 
 extern "C" cb_status cb_attention_forward(const void* q, const void* k, const void* v, cb_dtype dtype, int64_t tokens,
@@ -197,7 +229,7 @@ extern "C" cb_status cb_attention_forward(const void* q, const void* k, const vo
         !heads_ok(F.S, F.out, heads, true) || reinterpret_cast<uintptr_t>(lse) % 4)
         return CB_ERR_INVALID_ARG;
     if (!workspace_ok(workspace, workspace_bytes, cb_attention_workspace_bytes(tokens, heads, 0))) return CB_ERR_CAPACITY;
-    set_rows(F.S, workspace, stream);
+    set_rows(F.S, workspace, nullptr, stream);
     bool ok = true;
     if (tensor_core_rows(F.S, F.q, heads) && tensor_core_rows(F.S, F.k, kv_heads) && tensor_core_rows(F.S, F.v, kv_heads) &&
         tensor_core_rows(F.S, F.out, heads))
@@ -239,10 +271,15 @@ extern "C" cb_status cb_attention_backward(const void* grad_out, const void* q, 
         reinterpret_cast<uintptr_t>(lse) % 4)
         return CB_ERR_INVALID_ARG;
     if (!workspace_ok(workspace, workspace_bytes, cb_attention_workspace_bytes(tokens, heads, 1))) return CB_ERR_CAPACITY;
-    set_rows(B.S, workspace, stream);
     B.delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * rows_bytes(tokens));
-    if (dtype == CB_F32) launch_backward_rowwise<CB_F32>(B, stream);
+    set_rows(B.S, workspace, reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(B.delta) + rows_bytes(tokens * heads)), stream);
+    bool ok = true;
+    bool fast = true;
+    for (const Heads* x : {&B.go, &B.q, &B.out, &B.dq}) fast = fast && tensor_core_rows(B.S, *x, heads);
+    for (const Heads* x : {&B.k, &B.v, &B.dk, &B.dv}) fast = fast && tensor_core_rows(B.S, *x, kv_heads);
+    if (fast) ok = launch_backward(B, stream);
+    else if (dtype == CB_F32) launch_backward_rowwise<CB_F32>(B, stream);
     else if (dtype == CB_F16) launch_backward_rowwise<CB_F16>(B, stream);
     else launch_backward_rowwise<CB_BF16>(B, stream);
-    return cudaGetLastError() == cudaSuccess ? CB_OK : CB_ERR_CUDA;
+    return cudaGetLastError() == cudaSuccess && ok ? CB_OK : CB_ERR_CUDA;
 }

@@ -29,6 +29,7 @@ struct Shape {
     int32_t offsets32;
     int32_t* start;  // [tokens] where the token's session begins, and
     int32_t* end;    // [tokens] ends; both t for a token t of no session
+    uint32_t* largest;  // backward: the bits of the largest finite |grad_out| (of fp16 rows)
     int* error;      // or null
 };
 

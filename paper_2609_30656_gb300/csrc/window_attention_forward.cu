@@ -11,7 +11,6 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
-#include <cudaTypedefs.h>
 
 #include "muon_internal.cuh"
 
@@ -26,55 +25,6 @@ template <int D> constexpr size_t kShared = 1024 + (2 + kStages<D>) * kRowsBytes
 // threads hold a row of 128 scores: 256 x 208 + 128 x 72 of the block's 384 x 168.
 constexpr int kMoreRegisters = 208, kFewerRegisters = 72;
 constexpr float kRise = 8.f;  // how far, in powers of two, exponents may lie above the maximum they began with
-
-struct Work {
-    int token[2], head[2], kv;
-    bool same_tokens;
-};
-
-// The blocks of keys of a work item, in order: first tokens of tile 0's session, of tile 1's (or of both
-// at once), then what the windows reach.
-struct Blocks {
-    Sight x[2];
-    int sinks0, sinks1, base, count;
-    bool shared;
-    struct Block {
-        int at;          // first key
-        bool use[2];
-        int from[2], to[2];  // keys of it that count, for each tile
-    };
-    __device__ __forceinline__ Blocks(const Sight& a, const Sight& b) {
-        x[0] = a;
-        x[1] = b;
-        shared = a.s0 == b.s0 && a.s1 == b.s1;
-        sinks0 = tiles_of(a.s1 - a.s0);
-        sinks1 = shared ? 0 : tiles_of(b.s1 - b.s0);
-        base = a.hi == 0 ? b.lo : (b.hi == 0 ? a.lo : min(a.lo, b.lo));
-        count = sinks0 + sinks1 + tiles_of(max(max(a.hi, b.hi) - base, 0));
-    }
-    __device__ __forceinline__ Block at(int i) const {
-        Block k;
-        if (i < sinks0 + sinks1) {
-            const int t = i < sinks0 ? 0 : 1;
-            k.at = x[t].s0 + (i - (t ? sinks0 : 0)) * kTile;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                k.use[u] = u == t || shared;
-                k.from[u] = x[u].s0;
-                k.to[u] = x[u].s1;
-            }
-            return k;
-        }
-        k.at = base + (i - sinks0 - sinks1) * kTile;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            k.use[u] = k.at < x[u].hi && k.at + kTile > x[u].lo;
-            k.from[u] = x[u].lo;
-            k.to[u] = x[u].hi;
-        }
-        return k;
-    }
-};
 
 template <bool BF16, int D>
 __device__ __noinline__ void output_again(const Forward& F, int64_t t, int h, unsigned char* tile, int r) {
@@ -102,19 +52,7 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
     __shared__ uint32_t tmem_at;
     __shared__ SightParts parts[2];
     const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    Work W;
-    if (pair_heads) {
-        const int pairs = F.S.heads / 2, tile = static_cast<int>(blockIdx.x / pairs), p = static_cast<int>(blockIdx.x - static_cast<unsigned>(tile) * pairs);
-        W.token[0] = W.token[1] = tile * kTile;
-        W.head[0] = 2 * p;
-        W.head[1] = 2 * p + 1;
-    } else {
-        const int tile = static_cast<int>(blockIdx.x / F.S.heads), h = static_cast<int>(blockIdx.x - static_cast<unsigned>(tile) * F.S.heads);
-        W.token[0] = tile * 2 * kTile;
-        W.token[1] = W.token[0] + kTile;
-        W.head[0] = W.head[1] = h;
-    }
-    W.kv = W.head[0] / F.S.group;
+    const Work W = work_of(F.S, blockIdx.x, pair_heads);
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
@@ -383,44 +321,15 @@ bool launch_typed(const Forward& F, cudaStream_t s) {
         return false;
     static std::atomic<uint64_t> devices{0};
     if (!muon::shared_memory(attention_forward_kernel<D, BF16>, kShared<D>, devices)) return false;
-    const bool pair_heads = S.group % 2 == 0;
-    const int64_t tiles = (S.tokens + kTile - 1) / kTile;
-    const int64_t grid = pair_heads ? tiles * (S.heads / 2) : (tiles + 1) / 2 * S.heads;
+    const bool pair_heads = pairs_heads(S);
+    const int64_t grid = work_items(S);
     if (grid > INT32_MAX) return false;
     launch(attention_forward_kernel<D, BF16>, dim3(static_cast<unsigned>(grid)), dim3(kThreads), kShared<D>, s, qm, km, vm, om, F,
            pair_heads);
     return true;
 }
 
-PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
-    static PFN_cuTensorMapEncodeTiled_v12000 encode = [] {
-        void* fn = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q) != cudaSuccess ||
-            q != cudaDriverEntryPointSuccess) {
-            cudaGetLastError();
-            fn = nullptr;
-        }
-        return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
-    }();
-    return encode;
-}
-
 }  // namespace
-
-// [tokens][heads][dim] in boxes of 64 values of 128 tokens of one head; what is outside reads as zeros.
-bool tile_map(CUtensorMap* map, const Heads& h, int64_t tokens, int32_t heads, int32_t dim, int32_t dtype) {
-    if (!tensor_map_encoder()) return false;
-    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(tokens)};
-    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(heads > 1 ? h.head : dim) * 2,
-                                   static_cast<cuuint64_t>(tokens > 1 ? h.token : dim) * 2};
-    const cuuint32_t box[3] = {64, 1, kTile};
-    const cuuint32_t step[3] = {1, 1, 1};
-    return tensor_map_encoder()(map, dtype == CB_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
-                                const_cast<void*>(h.data), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
 
 bool launch_forward(const Forward& F, cudaStream_t s) {
     if (F.S.dtype == CB_BF16) return F.S.dim <= 64 ? launch_typed<64, true>(F, s) : launch_typed<128, true>(F, s);

@@ -196,6 +196,75 @@ __device__ __forceinline__ Sight sight_of(const SightParts& P, int sinks) {
 }
 __host__ __device__ __forceinline__ int tiles_of(int n) { return (n + kTile - 1) / kTile; }
 
+// ---------------------------------------------------------------- two tiles of queries and their keys
+
+// Two tiles that read one head of keys and values: the same tokens of two heads that share it,
+// where heads share in twos (then their keys are the same); else 256 tokens of one head.
+inline bool pairs_heads(const Shape& S) { return S.group % 2 == 0; }
+inline int64_t work_items(const Shape& S) {
+    const int64_t tiles = (S.tokens + kTile - 1) / kTile;
+    return pairs_heads(S) ? tiles * (S.heads / 2) : (tiles + 1) / 2 * S.heads;
+}
+struct Work {
+    int token[2], head[2], kv;
+};
+__device__ __forceinline__ Work work_of(const Shape& S, unsigned item, bool pair_heads) {
+    Work W;
+    const unsigned per = static_cast<unsigned>(pair_heads ? S.heads / 2 : S.heads), tile = item / per;
+    const int p = static_cast<int>(item - tile * per);
+    W.head[0] = pair_heads ? 2 * p : p;
+    W.head[1] = pair_heads ? 2 * p + 1 : p;
+    W.token[0] = static_cast<int>(tile) * (pair_heads ? kTile : 2 * kTile);
+    W.token[1] = pair_heads ? W.token[0] : W.token[0] + kTile;
+    W.kv = W.head[0] / S.group;
+    return W;
+}
+
+// The blocks of keys of a work item, in order: first tokens of tile 0's session, of tile 1's (or of both
+// at once), then what the windows reach.
+struct Blocks {
+    Sight x[2];
+    int sinks0, sinks1, base, count;
+    bool shared;
+    struct Block {
+        int at;          // first key
+        bool use[2];
+        int from[2], to[2];  // keys of it that count, for each tile
+    };
+    __device__ __forceinline__ Blocks(const Sight& a, const Sight& b) {
+        x[0] = a;
+        x[1] = b;
+        shared = a.s0 == b.s0 && a.s1 == b.s1;
+        sinks0 = tiles_of(a.s1 - a.s0);
+        sinks1 = shared ? 0 : tiles_of(b.s1 - b.s0);
+        base = a.hi == 0 ? b.lo : (b.hi == 0 ? a.lo : min(a.lo, b.lo));
+        count = sinks0 + sinks1 + tiles_of(max(max(a.hi, b.hi) - base, 0));
+    }
+    __device__ __forceinline__ Block at(int i) const {
+        Block k;
+        if (i < sinks0 + sinks1) {
+            const int t = i < sinks0 ? 0 : 1;
+            k.at = x[t].s0 + (i - (t ? sinks0 : 0)) * kTile;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                k.use[u] = u == t || shared;
+                k.from[u] = x[u].s0;
+                k.to[u] = x[u].s1;
+            }
+            return k;
+        }
+        k.at = base + (i - sinks0 - sinks1) * kTile;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            k.use[u] = k.at < x[u].hi && k.at + kTile > x[u].lo;
+            k.from[u] = x[u].lo;
+            k.to[u] = x[u].hi;
+        }
+        return k;
+    }
+};
+
+// A tensor's tiles for TMA.
 bool tile_map(CUtensorMap* map, const Heads& h, int64_t tokens, int32_t heads, int32_t dim, int32_t dtype);
 
 }  // namespace attention
