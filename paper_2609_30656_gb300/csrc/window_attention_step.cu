@@ -1,8 +1,10 @@
 // window_attention_step.cu -- windowed attention of one new token for each session over a cache of keys
 // and values (include/cb_tbe.h).
+#include "muon_internal.cuh"
 #include "window_attention.cuh"
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 namespace cbtbe {
@@ -92,9 +94,293 @@ __global__ void __launch_bounds__(kWarps * 32) attention_step_rowwise_kernel(con
     }
 }
 
+// ---------------------------------------------------------------- 16-bit rows in whole 16-byte pieces
+
+// The keys and values of a session are read once, by the 16 heads at most that share them: bytes bound it, and what
+// counts is how many are on their way. A block of four warps has a part of the keys of one head of keys; each warp
+// copies its own tiles of 16 keys and values ahead (cp.async, three tiles of 8 KB) and waits for no other.
+// Scores and sums are small products (mma.sync, 16 x 8 x 16, the queries of the sharing heads as rows): on the
+// CUDA cores 16 bytes of keys would cost 16 multiplications for every head. The warps' sums are joined at the block's end, the
+// parts' by a second kernel, both in order.
+constexpr int kStepWarps = 4, kStepKeys = 16, kStepStages = 3, kStepHeads = 16;
+template <int D> constexpr int kStepRow = D * 2;  // bytes
+template <int D> constexpr int kStepTile = 2 * kStepKeys * kStepRow<D>;
+template <int D> constexpr size_t kStepShared = static_cast<size_t>(kStepWarps) * kStepStages * kStepTile<D>;
+
+struct Parts {
+    int32_t parts, head_blocks;
+    float* sums;  // [sequences][heads][parts][dim + 2]: sums of values, the maximum, the sum of weights; null for one part
+};
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    uint32_t r;
+    if constexpr (BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool in) {  // zeros where not `in`
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_begun() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+__device__ __forceinline__ void load_matrices(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ void load_matrices_turned(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+template <bool BF16>
+__device__ __forceinline__ void multiply(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if constexpr (BF16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kStepWarps * 32, 2)
+attention_step_kernel(const Step A, const Parts P) {
+    constexpr int kPieces = D / 8, kPerLane = kStepKeys * kPieces / 32;
+    constexpr float kShift = BF16 ? 0.f : 8.f;  // fp16 holds weights times 2^8: small ones keep their digits
+    extern __shared__ __align__(128) unsigned char tiles[];
+    begin_kernel();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    // Parts of one session and head are neighbours, then heads that read the same lines of the cache.
+    int64_t w = blockIdx.x;
+    const int part = static_cast<int>(w % P.parts);
+    w /= P.parts;
+    const int head_block = static_cast<int>(w % P.head_blocks);
+    w /= P.head_blocks;
+    const int kv = static_cast<int>(w % A.kv_heads);
+    const int64_t b = w / A.kv_heads;
+    const int head0 = kv * A.group + head_block * kStepHeads, heads = min(A.group - head_block * kStepHeads, kStepHeads);
+    const int n = static_cast<int>(length_of(A, b)), first = static_cast<int>(max64(0, n - A.window));
+    const int sinks = min(A.sinks, first), seen = sinks + (n - first);
+    // This part's share of the keys in sight, in whole tiles; and this warp's tiles of it.
+    const int tiles_all = (seen + kStepKeys - 1) / kStepKeys, share = (tiles_all + P.parts - 1) / P.parts;
+    const int tile0 = min(part * share, tiles_all), tile1 = min(tile0 + share, tiles_all);
+    const char* keys = static_cast<const char*>(k_of(A, b)) + kv * A.k_head * 2;
+    const char* values = static_cast<const char*>(v_of(A, b)) + kv * A.v_head * 2;
+    const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(tiles)) + warp * kStepStages * kStepTile<D>;
+    // 16 bytes c of row r: 8 neighbouring rows at one c are in 8 different places of 128 bytes.
+    auto place = [&](int r, int c) { return static_cast<uint32_t>(r * kStepRow<D> + ((c ^ (r & 7)) << 4)); };
+    auto copy = [&](int tile, int stage) {
+        if (tile < tile1) {
+            const uint32_t to = mine + stage * kStepTile<D>;
+#pragma unroll
+            for (int x = 0; x < kPerLane; ++x) {
+                const int at = x * 32 + lane, r = at / kPieces, c = at % kPieces;
+                const int i = tile * kStepKeys + r;
+                const int64_t pos = i < sinks ? i : first + (i - sinks);
+                const bool in = i < seen && c * 8 < A.dim;
+                copy16(to + place(r, c), in ? keys + (pos * A.k_token + c * 8) * 2 : keys, in);
+                copy16(to + kStepTile<D> / 2 + place(r, c), in ? values + (pos * A.v_token + c * 8) * 2 : values, in);
+            }
+        }
+        copies_begun();
+    };
+#pragma unroll
+    for (int s = 0; s < kStepStages - 1; ++s) copy(tile0 + warp + s * kStepWarps, s);
+
+    // The queries: rows lane / 4 and lane / 4 + 8 of 16, columns (lane % 4) * 2 and 8 on, of every 16.
+    uint32_t q[D / 16][4];
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int r = lane / 4 + (x & 1) * 8, c = k * 16 + (x >> 1) * 8 + lane % 4 * 2;
+            q[k][x] = 0u;
+            if (r < heads && c < A.dim) {
+                const uint16_t* p = static_cast<const uint16_t*>(A.q) + b * A.q_seq + static_cast<int64_t>(head0 + r) * A.q_head + c;
+                q[k][x] = static_cast<uint32_t>(p[0]) | static_cast<uint32_t>(p[1]) << 16;
+            }
+        }
+    const float c = fmaxf(fabsf(A.scale) * kLog2e, 1e-30f), sign = A.scale < 0.f ? -1.f : 1.f;
+    float o[D / 8][4] = {}, most[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+    int stage = 0;
+    for (int tile = tile0 + warp; tile < tile1; tile += kStepWarps) {
+        copies_done<kStepStages - 2>();
+        __syncwarp();
+        const uint32_t at = mine + stage * kStepTile<D>;
+        float s[2][4] = {};
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+            uint32_t m[4];  // keys 0 .. 7 by values 0 .. 7 and 8 .. 15 of these 16, keys 8 .. 15 alike
+            load_matrices(at + place((lane & 7) + (lane >> 4) * 8, k * 2 + (lane >> 3 & 1)), m);
+            multiply<BF16>(s[0], q[k], m[0], m[1]);
+            multiply<BF16>(s[1], q[k], m[2], m[3]);
+        }
+        const int left = seen - tile * kStepKeys;  // keys of the tile
+        float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[x][i] = x * 8 + lane % 4 * 2 + (i & 1) < left ? s[x][i] * sign : -INFINITY;
+                top[i >> 1] = fmaxf(top[i >> 1], s[x][i]);
+            }
+        float keep[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            top[i] = fmaxf(top[i], __shfl_xor_sync(kFull, top[i], 1));
+            top[i] = fmaxf(top[i], __shfl_xor_sync(kFull, top[i], 2));
+            top[i] = fmaxf(top[i], most[i]);
+            keep[i] = top[i] == most[i] ? 1.f : exp2f((most[i] - top[i]) * c);
+            most[i] = top[i];
+            sum[i] *= keep[i];
+        }
+        if (__any_sync(kFull, keep[0] != 1.f || keep[1] != 1.f)) {
+#pragma unroll
+            for (int d = 0; d < D / 8; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[d][i] *= keep[i >> 1];
+        }
+        const float base[2] = {kShift - (top[0] == -INFINITY ? 0.f : top[0] * c), kShift - (top[1] == -INFINITY ? 0.f : top[1] * c)};
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[x][i] = exp2f(fmaf(s[x][i], c, base[i >> 1]));
+                sum[i >> 1] += s[x][i];
+            }
+        const uint32_t p[4] = {pack<BF16>(s[0][0], s[0][1]), pack<BF16>(s[0][2], s[0][3]), pack<BF16>(s[1][0], s[1][1]),
+                               pack<BF16>(s[1][2], s[1][3])};
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) {
+            uint32_t m[4];  // values 0 .. 7 of these 16 by keys 0 .. 7 and 8 .. 15, values 8 .. 15 alike
+            load_matrices_turned(at + kStepTile<D> / 2 + place((lane & 7) + (lane >> 3 & 1) * 8, d * 2 + (lane >> 4)), m);
+            multiply<BF16>(o[2 * d], p, m[0], m[1]);
+            multiply<BF16>(o[2 * d + 1], p, m[2], m[3]);
+        }
+        __syncwarp();
+        copy(tile + (kStepStages - 1) * kStepWarps, stage == 0 ? kStepStages - 1 : stage - 1);
+        if (++stage == kStepStages) stage = 0;
+    }
+    copies_done<0>();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        sum[i] += __shfl_xor_sync(kFull, sum[i], 1);
+        sum[i] += __shfl_xor_sync(kFull, sum[i], 2);
+    }
+    // The warps' sums, joined in order.
+    constexpr int kJoin = D + 4;  // floats of a head
+    static_assert(kStepWarps * kStepHeads * kJoin * 4 <= kStepShared<D>, "");
+    float* joined = reinterpret_cast<float*>(tiles);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        float* to = joined + (warp * kStepHeads + lane / 4 + i * 8) * kJoin;
+#pragma unroll
+        for (int d = 0; d < D / 8; ++d) {
+            to[d * 8 + lane % 4 * 2] = o[d][2 * i];
+            to[d * 8 + lane % 4 * 2 + 1] = o[d][2 * i + 1];
+        }
+        if (lane % 4 == 0) {
+            to[D] = most[i];
+            to[D + 1] = sum[i];
+        }
+    }
+    __syncthreads();
+    for (int x = threadIdx.x; x < heads * D; x += kStepWarps * 32) {
+        const int h = x / D, d = x % D;
+        if (d >= A.dim) continue;
+        float top = -INFINITY, total = 0.f, value = 0.f;
+        for (int y = 0; y < kStepWarps; ++y) top = fmaxf(top, joined[(y * kStepHeads + h) * kJoin + D]);
+        for (int y = 0; y < kStepWarps; ++y) {
+            const float* from = joined + (y * kStepHeads + h) * kJoin;
+            if (from[D + 1] == 0.f) continue;  // no key
+            const float f = from[D] == top ? 1.f : exp2f((from[D] - top) * c);
+            total = fmaf(from[D + 1], f, total);
+            value = fmaf(from[d], f, value);
+        }
+        const int64_t row = b * A.heads + head0 + h;
+        if (P.sums) {
+            float* to = P.sums + (row * P.parts + part) * (A.dim + 2);
+            to[d] = value;
+            if (d == 0) {
+                to[A.dim] = top;
+                to[A.dim + 1] = total;
+            }
+        } else {
+            const float r = n > 0 ? value / total : 0.f;
+            static_cast<uint16_t*>(A.out)[b * A.out_seq + static_cast<int64_t>(head0 + h) * A.out_head + d] =
+                static_cast<uint16_t>(narrow<BF16 ? CB_BF16 : CB_F16>(r));
+        }
+    }
+}
+
+// The parts' sums of a head of a session, joined by a block.
+template <bool BF16>
+__global__ void __launch_bounds__(128) attention_step_join_kernel(const Step A, const Parts P) {
+    begin_kernel();
+    const float c = fmaxf(fabsf(A.scale) * kLog2e, 1e-30f);
+    const int64_t row = blockIdx.x, b = row / A.heads;
+    const int h = static_cast<int>(row - b * A.heads), d = threadIdx.x;
+    if (d >= A.dim) return;
+    const float* from = P.sums + row * P.parts * (A.dim + 2);
+    float top = -INFINITY, total = 0.f, value = 0.f;
+    for (int y = 0; y < P.parts; ++y) top = fmaxf(top, __ldcg(from + y * (A.dim + 2) + A.dim));
+    for (int y = 0; y < P.parts; ++y) {
+        const float* at = from + y * (A.dim + 2);
+        const float sum = __ldcg(at + A.dim + 1), most = __ldcg(at + A.dim);
+        if (sum == 0.f) continue;
+        const float f = most == top ? 1.f : exp2f((most - top) * c);
+        total = fmaf(sum, f, total);
+        value = fmaf(__ldcg(at + d), f, value);
+    }
+    const float r = total == 0.f ? 0.f : value / total;
+    static_cast<uint16_t*>(A.out)[b * A.out_seq + static_cast<int64_t>(h) * A.out_head + d] =
+        static_cast<uint16_t>(narrow<BF16 ? CB_BF16 : CB_F16>(r));
+}
+
+int sm_count() {
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+        return 152;
+    return sms;
+}
+
+// Parts of the keys of a session: so many that the blocks make a dozen rounds of the GPU's two blocks an SM
+// (the last round then idles little of it), none of fewer than 256 keys.
+int parts_of(int64_t sequences, int32_t kv_heads, int32_t group, int64_t capacity, int64_t window, int64_t sinks) {
+    const int64_t blocks = sequences * kv_heads * ((group + kStepHeads - 1) / kStepHeads);
+    const int64_t seen = std::min(capacity, window > capacity ? capacity : window + std::min(sinks, capacity));
+    const int64_t wanted = (static_cast<int64_t>(sm_count()) * 2 * 12 + blocks - 1) / blocks;
+    return static_cast<int>(std::max<int64_t>(1, std::min(wanted, seen / 256)));
+}
+
+template <int D, bool BF16>
+bool launch_step(const Step& A, const Parts& P, cudaStream_t s) {
+    static std::atomic<uint64_t> devices{0};
+    if (!muon::shared_memory(attention_step_kernel<D, BF16>, kStepShared<D>, devices)) return false;
+    const int64_t grid = A.sequences * A.kv_heads * P.head_blocks * P.parts;
+    if (grid > INT32_MAX || A.sequences * A.heads > INT32_MAX) return false;
+    launch(attention_step_kernel<D, BF16>, dim3(static_cast<unsigned>(grid)), dim3(kStepWarps * 32), kStepShared<D>, s, A, P);
+    if (P.sums)
+        launch(attention_step_join_kernel<BF16>, dim3(static_cast<unsigned>(A.sequences * A.heads)), dim3(128), 0, s, A, P);
+    return true;
+}
+
 bool type_ok(int t) { return t == CB_F32 || t == CB_F16 || t == CB_BF16; }
 constexpr int64_t kMost = int64_t{1} << 40;
 bool stride_ok(int64_t s) { return s >= 0 && s <= kMost; }
+bool sizes_ok(int64_t sequences, int64_t capacity, int32_t heads, int32_t kv_heads, int32_t dim, int64_t window, int64_t sinks) {
+    return sequences >= 0 && sequences < (int64_t{1} << 31) && capacity >= 0 && capacity < (int64_t{1} << 31) && heads >= 1 &&
+           heads <= 65535 && kv_heads >= 1 && heads % kv_heads == 0 && dim >= 1 && dim <= kMaxDim && window >= 1 && sinks >= 0;
+}
 
 }  // namespace
 }  // namespace attention
@@ -102,7 +388,10 @@ bool stride_ok(int64_t s) { return s >= 0 && s <= kMost; }
 
 extern "C" int64_t cb_attention_step_workspace_bytes(int64_t sequences, int32_t heads, int32_t kv_heads, int32_t dim,
                                                      int64_t capacity, int64_t window, int64_t sinks) {
-    return 0;
+    using namespace cbtbe::attention;
+    if (!sizes_ok(sequences, capacity, heads, kv_heads, dim, window, sinks) || sequences == 0) return 0;
+    const int parts = parts_of(sequences, kv_heads, heads / kv_heads, capacity, window, sinks);
+    return parts > 1 ? sequences * heads * parts * (dim + 2) * 4 : 0;
 }
 
 extern "C" cb_status cb_attention_step(const void* q, const void* k_cache, const void* v_cache, cb_dtype dtype,
@@ -114,9 +403,7 @@ extern "C" cb_status cb_attention_step(const void* q, const void* k_cache, const
                                        int64_t out_sequence_stride, int64_t out_head_stride, void* workspace,
                                        int64_t workspace_bytes, int* error, cudaStream_t stream) {
     using namespace cbtbe::attention;
-    if (!type_ok(dtype) || sequences < 0 || sequences >= (int64_t{1} << 31) || capacity < 0 || capacity >= (int64_t{1} << 31) ||
-        heads < 1 || heads > 65535 || kv_heads < 1 || heads % kv_heads || dim < 1 || dim > kMaxDim || window < 1 || sinks < 0 ||
-        !(scale == scale) || (idx_dtype != CB_I32 && idx_dtype != CB_I64) || reinterpret_cast<uintptr_t>(error) % 4)
+    if (!type_ok(dtype) || !sizes_ok(sequences, capacity, heads, kv_heads, dim, window, sinks) || !(scale == scale) || (idx_dtype != CB_I32 && idx_dtype != CB_I64) || reinterpret_cast<uintptr_t>(error) % 4)
         return CB_ERR_INVALID_ARG;
     for (const int64_t s : {q_sequence_stride, q_head_stride, k_sequence_stride, k_token_stride, k_head_stride,
                             v_sequence_stride, v_token_stride, v_head_stride, out_sequence_stride, out_head_stride})
@@ -158,6 +445,20 @@ extern "C" cb_status cb_attention_step(const void* q, const void* k_cache, const
     A.lengths = lengths;
     A.lengths32 = idx_dtype == CB_I32;
     A.error = error;
+    bool fast = dtype != CB_F32 && dim % 8 == 0 && dim <= 128;
+    for (const int64_t x : {k_sequence_stride, k_token_stride, k_head_stride, v_sequence_stride, v_token_stride, v_head_stride})
+        fast = fast && x % 8 == 0;
+    fast = fast && reinterpret_cast<uintptr_t>(k_cache) % 16 == 0 && reinterpret_cast<uintptr_t>(v_cache) % 16 == 0;
+    if (fast) {
+        Parts P{};
+        P.parts = parts_of(sequences, kv_heads, A.group, capacity, window, sinks);
+        P.head_blocks = (A.group + kStepHeads - 1) / kStepHeads;
+        P.sums = P.parts > 1 ? static_cast<float*>(workspace) : nullptr;
+        bool ok;
+        if (dtype == CB_BF16) ok = dim <= 64 ? launch_step<64, true>(A, P, stream) : launch_step<128, true>(A, P, stream);
+        else ok = dim <= 64 ? launch_step<64, false>(A, P, stream) : launch_step<128, false>(A, P, stream);
+        return cudaGetLastError() == cudaSuccess && ok ? CB_OK : CB_ERR_CUDA;
+    }
     const dim3 grid(static_cast<unsigned>(std::min<int64_t>(sequences * heads, 1 << 20)));
     if (dtype == CB_F32) cbtbe::launch(attention_step_rowwise_kernel<CB_F32>, grid, dim3(kWarps * 32), 0, stream, A);
     else if (dtype == CB_F16) cbtbe::launch(attention_step_rowwise_kernel<CB_F16>, grid, dim3(kWarps * 32), 0, stream, A);
