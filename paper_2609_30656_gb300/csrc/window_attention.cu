@@ -178,6 +178,14 @@ PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
 
 }  // namespace
 
+int sm_count() {
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+        return 152;
+    return sms;
+}
+
 // [tokens][heads][dim] in boxes of 64 values of 128 tokens of one head; what is outside reads as zeros.
 bool tile_map(CUtensorMap* map, const Heads& h, int64_t tokens, int32_t heads, int32_t dim, int32_t dtype) {
     if (!tensor_map_encoder()) return false;

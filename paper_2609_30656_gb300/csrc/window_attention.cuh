@@ -181,6 +181,7 @@ inline size_t rows_bytes(int64_t tokens) { return static_cast<size_t>((tokens * 
 // The tensor-core kernels (window_attention_forward.cu, window_attention_backward.cu); they want fp16 or
 // bf16, rows of a multiple of 8 and at most 128 values, addresses and strides in multiples of 16 bytes.
 bool tensor_core_rows(const Shape& S, const Heads& h, int heads);
+int sm_count();  // of the current device
 bool launch_forward(const Forward& F, cudaStream_t s);
 bool launch_backward(const Backward& B, cudaStream_t s);
 

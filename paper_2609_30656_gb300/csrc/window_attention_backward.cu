@@ -347,7 +347,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
                 __syncwarp();
                 dq_again<BF16, D>(B, W.token[mine] + other, W.head[mine], tile, other);
             }
-            tc::fence_to_tensor_core();
+            fence_to_tma();
         }
         named_barrier(1 + mine, 128);
         if (ok && row == 0 && W.token[mine] < B.S.tokens) {
@@ -623,7 +623,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                 __syncwarp();
                 dkv_again<BF16, D>(B, first + other, kv, half, tile, other);
             }
-            tc::fence_to_tensor_core();
+            fence_to_tma();
         }
         named_barrier(1 + half, 128);
         if (ok && row == 0) {

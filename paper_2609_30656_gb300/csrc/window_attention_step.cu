@@ -345,14 +345,6 @@ __global__ void __launch_bounds__(128) attention_step_join_kernel(const Step A, 
         static_cast<uint16_t>(narrow<BF16 ? CB_BF16 : CB_F16>(r));
 }
 
-int sm_count() {
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-        return 152;
-    return sms;
-}
-
 // Parts of the keys of a session: so many that the blocks make a dozen rounds of the GPU's two blocks an SM
 // (the last round then idles little of it), none of fewer than 256 keys.
 int parts_of(int64_t sequences, int32_t kv_heads, int32_t group, int64_t capacity, int64_t window, int64_t sinks) {

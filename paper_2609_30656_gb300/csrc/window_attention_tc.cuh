@@ -44,6 +44,15 @@ __device__ __forceinline__ void tmem_load64(uint32_t addr, uint32_t (&r)[64]) {
         : "r"(addr)
         : "memory");
 }
+// 16 columns, without the wait for them (tmem_store_wait).
+__device__ __forceinline__ void tmem_store16_begin(uint32_t addr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(addr)
+        : "memory");
+}
 // 32 columns, without the wait for them (tmem_store_wait).
 __device__ __forceinline__ void tmem_store32_begin(uint32_t addr, const uint32_t (&r)[32]) {
     asm volatile(
@@ -56,8 +65,28 @@ __device__ __forceinline__ void tmem_store32_begin(uint32_t addr, const uint32_t
         "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(addr)
         : "memory");
 }
+// 8 columns times f.
+__device__ __forceinline__ void scale8(uint32_t addr, float f) {
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : CB_R8(r, 0)
+                 : "r"(addr)
+                 : "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};\n\ttcgen05.wait::st.sync.aligned;" ::"r"(
+                     r[0]),
+                 "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(addr)
+                 : "memory");
+}
 __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// The largest of three.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -107,6 +136,9 @@ __device__ __forceinline__ void named_barrier(int id, int count) {
     asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(count) : "memory");
 }
 
+// This thread's stores to shared memory, before TMA reads them (and a barrier between). Only those: the fence over all
+// memory waits for the thread's stores to global memory too, 1500 clocks.
+__device__ __forceinline__ void fence_to_tma() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tma_store(const CUtensorMap* map, uint32_t src, int32_t x, int32_t y, int32_t z) {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(
                      reinterpret_cast<uint64_t>(map)),
@@ -132,12 +164,13 @@ __device__ __forceinline__ uint32_t tile_byte(int r, int c) {
 
 // ---------------------------------------------------------------- what rows see
 
-// Bits i of columns [a, b) among the 32 from `first` on.
-__device__ __forceinline__ uint32_t range_bits(int a, int b, int first) {
-    const int lo = max(a - first, 0), hi = min(b - first, 32);
-    if (lo >= hi) return 0u;
-    return (hi >= 32 ? ~0u : (1u << hi) - 1u) & ~((1u << lo) - 1u);
+// Bits i of columns [a, b) among the 32 from `first` on. (The instruction's shifts by 32 and more give 0.)
+__device__ __forceinline__ uint32_t ones_from(int bit) {
+    uint32_t r;
+    asm("shl.b32 %0, %1, %2;" : "=r"(r) : "r"(~0u), "r"(max(bit, 0)));
+    return r;
 }
+__device__ __forceinline__ uint32_t range_bits(int a, int b, int first) { return ones_from(a - first) & ~ones_from(b - first); }
 
 // Two intervals of positions: a row's tokens in sight, or (for a key) the rows that see it.
 struct TwoRanges {
@@ -263,6 +296,46 @@ struct Blocks {
         return k;
     }
 };
+
+// What a block's warps need to know of an item, found out ahead by one of them.
+struct Item {
+    Work W;
+    Sight sight[2];
+    int begin[2];                // of the session that the tile begins in
+    unsigned char row[2][kTile];  // where a row's session begins: that many tokens into the tile, or kBefore, or kNowhere
+};
+constexpr int kBefore = 254, kNowhere = 255;
+__device__ __forceinline__ void look_ahead(const Shape& S, Item& it, int x, int token, int lane) {
+    int lo = INT32_MAX, hi = 0, s0 = INT32_MAX;
+#pragma unroll
+    for (int k = 0; k < kTile / 32; ++k) {
+        const int t = token + k * 32 + lane;
+        const Row r = row_of(S, t);
+        it.row[x][k * 32 + lane] = static_cast<unsigned char>(!r.real ? kNowhere : (r.start < token ? kBefore : r.start - token));
+        if (!r.real) continue;
+        lo = min(lo, r.first);
+        hi = max(hi, t + 1);
+        s0 = min(s0, r.start);
+    }
+    SightParts P;
+    P.lo[0] = P.lo[1] = P.lo[2] = P.lo[3] = __reduce_min_sync(kFull, lo);
+    P.hi[0] = P.hi[1] = P.hi[2] = P.hi[3] = __reduce_max_sync(kFull, hi);
+    P.s0[0] = P.s0[1] = P.s0[2] = P.s0[3] = __reduce_min_sync(kFull, s0);
+    if (lane == 0) {
+        it.sight[x] = sight_of(P, S.sinks);
+        it.begin[x] = P.s0[0];
+    }
+}
+__device__ __forceinline__ Row row_in(const Shape& S, const Item& it, int x, int row) {
+    const int code = it.row[x][row];
+    Row r{0, 0, code != kNowhere};
+    if (r.real) {
+        const int t = it.W.token[x] + row;
+        r.start = code == kBefore ? it.begin[x] : it.W.token[x] + code;
+        r.first = static_cast<int>(max64(r.start, t - S.window + 1));
+    }
+    return r;
+}
 
 // A tensor's tiles for TMA.
 bool tile_map(CUtensorMap* map, const Heads& h, int64_t tokens, int32_t heads, int32_t dim, int32_t dtype);
