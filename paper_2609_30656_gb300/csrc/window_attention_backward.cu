@@ -23,8 +23,10 @@ namespace cbtbe {
 namespace attention {
 namespace {
 
-constexpr int kWorkWarps = 8, kCopyWarp = 8, kMultiplyWarp = 9, kStatWarp = 10, kThreads = 384;
-constexpr int kMoreRegisters = 208, kFewerRegisters = 72;  // 256 x 208 + 128 x 72 of 384 x 168
+constexpr int kWorkWarps = 8, kCopyWarp = 8, kMultiplyWarp = 9, kThreads = 384;
+constexpr int kAheadWarp = 10, kStoreWarp = 11;  // over queries
+constexpr int kStatWarp = 10;                    // over keys
+constexpr int kMoreRegisters = 208, kFewerRegisters = 88;  // 256 x 208 + 128 x 88 of 384 x 168
 
 template <bool BF16> constexpr float kPShift = BF16 ? 0.f : 12.f;
 template <bool BF16>
@@ -92,8 +94,9 @@ __device__ __noinline__ void dkv_again(const Backward& B, int64_t j, int kv, boo
 // A row of sums from TMEM, times `by`, into its tile in shared memory; whether all are finite.
 template <int D, bool BF16>
 __device__ __forceinline__ bool finish_row(uint32_t at, float by, bool real, unsigned char* tile, int row) {
-    bool finite = true;
-#pragma unroll
+    const float2 by2 = make_float2(by, by), zero2 = make_float2(0.f, 0.f);
+    float2 check = zero2;  // stays 0 while all is finite
+#pragma unroll 1
     for (int d = 0; d < D; d += 32) {
         float o[32];
         tc::tmem_load32(at + d, o);
@@ -102,14 +105,14 @@ __device__ __forceinline__ bool finish_row(uint32_t at, float by, bool real, uns
             uint32_t w[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const float lo = real ? o[k + 2 * u] * by : 0.f, hi = real ? o[k + 2 * u + 1] * by : 0.f;
-                finite &= fabsf(lo) < INFINITY && fabsf(hi) < INFINITY;
-                w[u] = pack2<BF16>(lo, hi);
+                const float2 x = real ? mul2(make_float2(o[k + 2 * u], o[k + 2 * u + 1]), by2) : zero2;
+                check = fma2(x, zero2, check);
+                w[u] = pack2<BF16>(x.x, x.y);
             }
             *reinterpret_cast<uint4*>(tile + tile_byte(row, (d + k) / 8)) = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
-    return finite;
+    return check.x + check.y == 0.f;
 }
 template <int D>
 __device__ __forceinline__ void zero_row(unsigned char* tile, int row) {
@@ -119,95 +122,144 @@ __device__ __forceinline__ void zero_row(unsigned char* tile, int row) {
 
 // ---------------------------------------------------------------- dQ
 
-constexpr int kQueryStages = 3;
-template <int D> constexpr size_t kQueryShared = 1024 + (4 + kQueryStages) * kRowsBytes<D>;
+constexpr int kKeyBuffers = 2;  // of keys; one of values
+template <int D> constexpr size_t kQueryShared = 1024 + (4 + kKeyBuffers + 1) * kRowsBytes<D>;
 
-// As the forward, two tiles of queries a block. A tile's S, dP and dS take turns in the same columns of TMEM (P stays in
-// the row's thread meanwhile), so that two tiles fit with their dQ: one's products run beside the other's exponentials.
+// As the forward, two tiles of queries a block, which stays and takes its share of the work. A tile's S, dP and dS take turns in
+// the same columns of TMEM (P stays in the row's thread meanwhile), so that two tiles fit with their dQ: one's products run
+// beside the other's exponentials. Keys are needed at both ends of a block (S, dQ), values in between (dP): two
+// places for keys and one for values let both come a block ahead.
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constant__ CUtensorMap km,
                     const __grid_constant__ CUtensorMap vm, const __grid_constant__ CUtensorMap gm,
-                    const __grid_constant__ CUtensorMap dqm, const __grid_constant__ Backward B, const bool pair_heads) {
-    constexpr int S = kQueryStages;
+                    const __grid_constant__ CUtensorMap dqm, const __grid_constant__ Backward B, const bool pair_heads,
+                    const int items) {
     constexpr uint32_t kRows = kRowsBytes<D>;
     extern __shared__ unsigned char dynamic[];
     unsigned char* queries = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~uintptr_t(1023));
-    unsigned char* ring = queries + 4 * kRows;  // Q and dO of tile 0, of tile 1
-    __shared__ uint64_t q_full, full[S], empty[S], scores[2], taken[2], grads[2], slopes[2], done;
+    unsigned char* grads_out = queries + 2 * kRows;  // dO, and dQ in its place
+    unsigned char* keys = queries + 4 * kRows;
+    unsigned char* values = keys + kKeyBuffers * kRows;
+    __shared__ uint64_t q_full, q_empty, g_full[2], stored[2], k_full[2], k_empty[2], v_full, v_empty;
+    __shared__ uint64_t scores[2], taken[2], grads[2], slopes[2], sums[2], staged[2], item_full[2], item_empty[2];
     __shared__ uint32_t tmem_at;
-    __shared__ SightParts parts[2];
+    __shared__ Item info[2];
     const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    const Work W = work_of(B.S, blockIdx.x, pair_heads);
 
     if (threadIdx.x == 0) {
-        tc::barrier_init(tc::smem_addr(&q_full), 1);
+        for (uint64_t* b : {&q_full, &q_empty, &v_full, &v_empty}) tc::barrier_init(tc::smem_addr(b), 1);
         for (int i = 0; i < 2; ++i) {
-            tc::barrier_init(tc::smem_addr(scores + i), 1);
-            tc::barrier_init(tc::smem_addr(taken + i), 4);
-            tc::barrier_init(tc::smem_addr(grads + i), 1);
-            tc::barrier_init(tc::smem_addr(slopes + i), 4);
+            for (uint64_t* b : {g_full, stored, k_full, k_empty, scores, grads, sums, item_full}) tc::barrier_init(tc::smem_addr(b + i), 1);
+            for (uint64_t* b : {taken, slopes, staged}) tc::barrier_init(tc::smem_addr(b + i), 4);
+            tc::barrier_init(tc::smem_addr(item_empty + i), kWorkWarps + 3);
         }
-        for (int i = 0; i < S; ++i) {
-            tc::barrier_init(tc::smem_addr(full + i), 1);
-            tc::barrier_init(tc::smem_addr(empty + i), 1);
-        }
-        tc::barrier_init(tc::smem_addr(&done), 1);
         tc::barrier_init_fence();
         for (const CUtensorMap* m : {&qm, &km, &vm, &gm, &dqm}) tc::tma_prefetch(m);
     }
     if (warp == kMultiplyWarp) tc::tmem_alloc<1>(tc::smem_addr(&tmem_at), 512);
-    begin_kernel();
-    const int mine = warp >> 2 & 1, row = threadIdx.x & 127;  // of the work warps
-    const int64_t t = W.token[mine] + row;
-    Row r{0, 0, false};
-    if (warp < kWorkWarps) {
-        r = row_of(B.S, t);
-        note_row(parts[mine], r, static_cast<int>(t), warp & 3, lane);
-    }
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
     const uint32_t tmem = tmem_at;
-    const Blocks blocks(sight_of(parts[0], B.S.sinks), sight_of(parts[1], B.S.sinks));
+    begin_kernel();
+    const int first = static_cast<int>(blockIdx.x), stride = static_cast<int>(gridDim.x);
+    const int rounds = (items - first + stride - 1) / stride;
     bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return ok = tc::barrier_wait(tc::smem_addr(bar), parity & 1); };
+    // The n-th item; the caller is done with it at item_done.
+    auto item_of = [&](int n) -> const Item& {
+        wait(item_full + (n & 1), n >> 1);
+        return info[n & 1];
+    };
+    auto item_done = [&](int n) { tc::barrier_arrive(tc::smem_addr(item_empty + (n & 1))); };
 
     if (warp >= kWorkWarps) {
         registers_down<kFewerRegisters>();
-        if (warp == kCopyWarp && tc::elect()) {
-            if (blocks.count > 0) {
-                tc::barrier_expect(tc::smem_addr(&q_full), 4 * kRows);
+        if (warp == kAheadWarp) {
+            for (int n = 0; n < rounds; ++n) {
+                const Work W = work_of(B.S, first + n * stride, pair_heads);
+                if (!(ok = warp_wait(item_empty + (n & 1), (n >> 1) ^ 1))) break;
+                Item& it = info[n & 1];
+                if (lane == 0) it.W = W;
+                look_ahead(B.S, it, 0, W.token[0], lane);
+                look_ahead(B.S, it, 1, W.token[1], lane);
+                warp_arrive(item_full + (n & 1));
+            }
+        } else if (warp == kStoreWarp && tc::elect()) {
+            for (int n = 0; n < rounds; ++n) {
+                const Work W = item_of(n).W;
+                if (!ok) break;
+                item_done(n);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    load_tile<D>(tc::smem_addr(queries) + 2 * i * kRows, &qm, tc::smem_addr(&q_full), W.head[i], W.token[i]);
-                    load_tile<D>(tc::smem_addr(queries) + (2 * i + 1) * kRows, &gm, tc::smem_addr(&q_full), W.head[i], W.token[i]);
+                for (int x = 0; x < 2; ++x) {
+                    if (!wait(staged + x, n)) break;
+                    if (W.token[x] < B.S.tokens)
+#pragma unroll
+                        for (int d = 0; d < D / 64; ++d)
+                            tma_store(&dqm, tc::smem_addr(grads_out) + x * kRows + d * kBoxBytes, d * 64, W.head[x], W.token[x]);
+                    tma_store_done();
+                    tc::barrier_arrive(tc::smem_addr(stored + x));
                 }
+                if (!ok) break;
             }
-            int s = 0, issued = 0;
-            uint32_t phase = 0;
-            for (int i = 0; i < 2 * blocks.count; ++i) {
-                if (!(ok = tc::barrier_wait(tc::smem_addr(empty + s), phase ^ 1))) break;
-                const uint32_t bar = tc::smem_addr(full + s);
-                tc::barrier_expect(bar, kRows);
-                load_tile<D>(tc::smem_addr(ring) + s * kRows, i & 1 ? &vm : &km, bar, W.kv, blocks.at(i >> 1).at);
-                ++issued;
-                if (++s == S) s = 0, phase ^= 1;
+        } else if (warp == kCopyWarp && tc::elect()) {
+            int i_all = 0, n = 0, loaded_q = 0, loaded_g[2] = {0, 0}, loaded_k = 0, loaded_v = 0;
+            for (; n < rounds && ok; ++n) {
+                const Item& it = item_of(n);
+                if (!ok) break;
+                const Work W = it.W;
+                const Blocks blocks(it.sight[0], it.sight[1]);
+                item_done(n);
+                if (!wait(&q_empty, n ^ 1)) break;
+                tc::barrier_expect(tc::smem_addr(&q_full), 2 * kRows);
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    load_tile<D>(tc::smem_addr(queries) + x * kRows, &qm, tc::smem_addr(&q_full), W.head[x], W.token[x]);
+                ++loaded_q;
+                auto load_keys = [&](int i) {
+                    const int b = (i_all + i) & 1;
+                    if (!wait(k_empty + b, ((i_all + i) >> 1) ^ 1)) return;
+                    tc::barrier_expect(tc::smem_addr(k_full + b), kRows);
+                    load_tile<D>(tc::smem_addr(keys) + b * kRows, &km, tc::smem_addr(k_full + b), W.kv, blocks.at(i).at);
+                    ++loaded_k;
+                };
+                if (blocks.count > 0) load_keys(0);
+#pragma unroll
+                for (int x = 0; x < 2 && ok; ++x) {  // the dQ before has left its place
+                    if (!wait(stored + x, n ^ 1)) break;
+                    tc::barrier_expect(tc::smem_addr(g_full + x), kRows);
+                    load_tile<D>(tc::smem_addr(grads_out) + x * kRows, &gm, tc::smem_addr(g_full + x), W.head[x], W.token[x]);
+                    ++loaded_g[x];
+                }
+                for (int i = 0; i < blocks.count && ok; ++i) {
+                    if (!wait(&v_empty, (i_all + i) ^ 1)) break;
+                    tc::barrier_expect(tc::smem_addr(&v_full), kRows);
+                    load_tile<D>(tc::smem_addr(values), &vm, tc::smem_addr(&v_full), W.kv, blocks.at(i).at);
+                    ++loaded_v;
+                    if (i + 1 < blocks.count) load_keys(i + 1);
+                }
+                i_all += blocks.count;
             }
-            if (!ok)  // copies in flight land before the block's shared memory goes away
-                for (int i = max(0, issued - S); i < issued; ++i)
-                    if (!tc::barrier_wait(tc::smem_addr(full + i % S), i / S & 1)) break;
-        }
-        if (warp == kMultiplyWarp) {
+            if (!ok) {  // copies in flight land before the block's shared memory goes away
+                auto land = [&](uint64_t* bar, int parity) { tc::barrier_wait(tc::smem_addr(bar), parity & 1); };
+                if (loaded_q) land(&q_full, loaded_q - 1);
+                for (int x = 0; x < 2; ++x)
+                    if (loaded_g[x]) land(g_full + x, loaded_g[x] - 1);
+                if (loaded_v) land(&v_full, loaded_v - 1);
+                for (int k = max(0, loaded_k - 2); k < loaded_k; ++k) land(k_full + (k & 1), k >> 1);
+            }
+        } else if (warp == kMultiplyWarp) {
             constexpr uint32_t shape_s = mma_shape<BF16>(kTile, kTile, false), shape_q = mma_shape<BF16>(kTile, D, true);
             const bool one = tc::elect();
-            const uint32_t q0 = tc::smem_addr(queries), k0 = tc::smem_addr(ring);
-            int s = 0;
-            uint32_t phase = 0, taken_phase[2] = {0, 0}, slopes_phase[2] = {0, 0};
-            bool begun[2] = {false, false};
-            auto next = [&] { if (++s == S) s = 0, phase ^= 1; };
-            auto multiply = [&](int x, uint32_t left, uint32_t stage, uint64_t* bar) {  // Q_x K^T or dO_x V^T
+            const uint64_t q0 = tc::operand_k_major(tc::smem_addr(queries)), g0 = tc::operand_k_major(tc::smem_addr(grads_out));
+            const uint64_t k0 = tc::operand_k_major(tc::smem_addr(keys)), v0 = tc::operand_k_major(tc::smem_addr(values));
+            const uint64_t turned0 = tc::operand_mn_major(tc::smem_addr(keys), kBoxBytes);
+            int i_all = 0;
+            uint32_t taken_turn[2] = {0, 0}, slopes_turn[2] = {0, 0};
+            auto multiply = [&](int x, uint64_t a, uint64_t b, uint64_t* bar) {  // Q_x K^T or dO_x V^T
                 if (!one) return;
-                const uint64_t a = tc::operand_k_major(q0 + left * kRows), b = tc::operand_k_major(k0 + stage * kRows);
+                a = tc::advance(a, x * kRows);
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
                     const uint32_t off = k / 4 * kBoxBytes + k % 4 * 32;
@@ -215,146 +267,173 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
                 }
                 tc::mma_commit<1>(tc::smem_addr(bar + x));
             };
-            uint32_t k_stage = 0;
-            if (blocks.count > 0) {
-                ok = tc::barrier_wait(tc::smem_addr(&q_full), 0) && tc::barrier_wait(tc::smem_addr(full), 0);
+            auto multiply_grads = [&](int x) {  // dP_x, once S_x has been read from its columns
+                if (!wait(taken + x, taken_turn[x])) return false;
+                taken_turn[x] ^= 1;
                 tc::fence_after();
-                if (ok) {
-                    const Blocks::Block b = blocks.at(0);
+                multiply(x, g0, v0, grads);
+                return true;
+            };
+            auto add_keys = [&](int x, int buffer, bool add) {  // dQ_x += dS_x K
+                if (!wait(slopes + x, slopes_turn[x])) return false;
+                slopes_turn[x] ^= 1;
+                tc::fence_after();
+                const uint64_t b = tc::advance(turned0, buffer * kRows);
+                if (one)
 #pragma unroll
-                    for (int x = 0; x < 2; ++x)
-                        if (b.use[x]) multiply(x, 2 * x, 0, scores);
-                    next();
-                }
-            }
-            for (int i = 0; i < blocks.count && ok; ++i) {
-                const Blocks::Block b = blocks.at(i), c = blocks.at(i + 1);
-                const bool more = i + 1 < blocks.count;
-                const uint32_t v_stage = s;
-                if (!(ok = tc::barrier_wait(tc::smem_addr(full + s), phase))) break;
-                next();
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    if (!b.use[x]) continue;
-                    if (!(ok = tc::barrier_wait(tc::smem_addr(taken + x), taken_phase[x]))) break;
-                    taken_phase[x] ^= 1;
+                    for (int k = 0; k < kTile / 16; ++k)
+                        mma_tmem(tmem + 256 + x * D, tmem + x * 128 + k * 8, tc::advance(b, k * 2048), shape_q, add || k > 0);
+                return true;
+            };
+            // In turns dQ of one tile, dP of the other, S of the first: each finds its operands ready while the one
+            // before runs.
+            for (int n = 0; n < rounds && ok; ++n) {
+                const Item& it = item_of(n);
+                if (!ok) break;
+                const Blocks blocks(it.sight[0], it.sight[1]);
+                warp_arrive(item_empty + (n & 1));
+                if (!wait(&q_full, n)) break;
+                bool begun[2] = {false, false}, use[2] = {false, false};
+                if (blocks.count > 0) {
+                    if (!wait(k_full + (i_all & 1), i_all >> 1)) break;
                     tc::fence_after();
-                    multiply(x, 2 * x + 1, v_stage, grads);
+                    const uint64_t key = tc::advance(k0, (i_all & 1) * kRows);
+                    const Blocks::Block b = blocks.at(0);
+                    use[0] = b.use[0];
+                    use[1] = b.use[1];
+                    if (use[0]) multiply(0, q0, key, scores);
+                    if (!wait(g_full, n) || !wait(g_full + 1, n) || !wait(&v_full, i_all)) break;
+                    if (use[0] && !multiply_grads(0)) break;
+                    if (use[1]) multiply(1, q0, key, scores);
                 }
-                if (!ok) break;
-                if (one) tc::mma_commit<1>(tc::smem_addr(empty + v_stage));
-                const uint32_t next_k = s;
-                if (more) {
-                    if (!(ok = tc::barrier_wait(tc::smem_addr(full + s), phase))) break;
-                    next();
-                }
-                const uint64_t keys = tc::operand_mn_major(k0 + k_stage * kRows, kBoxBytes);
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    if (b.use[x]) {
-                        if (!(ok = tc::barrier_wait(tc::smem_addr(slopes + x), slopes_phase[x]))) break;
-                        slopes_phase[x] ^= 1;
-                        tc::fence_after();
-                        if (one)
-#pragma unroll
-                            for (int k = 0; k < kTile / 16; ++k)
-                                mma_tmem(tmem + 256 + x * D, tmem + x * 128 + k * 8, tc::advance(keys, k * 2048), shape_q, begun[x] || k > 0);
-                        begun[x] = true;
+                if (blocks.count <= 1 && one) tc::mma_commit<1>(tc::smem_addr(&q_empty));
+                for (int i = 0; i < blocks.count; ++i, ++i_all) {
+                    const bool more = i + 1 < blocks.count;
+                    const Blocks::Block c = blocks.at(i + 1);
+                    const int here = i_all & 1, there = here ^ 1;
+                    const bool next0 = more && c.use[0], next1 = more && c.use[1];
+                    if (use[0] && !add_keys(0, here, begun[0])) break;
+                    begun[0] |= use[0];
+                    if (use[1] && !multiply_grads(1)) break;
+                    if (one) {
+                        tc::mma_commit<1>(tc::smem_addr(&v_empty));
+                        if (!more) tc::mma_commit<1>(tc::smem_addr(sums));
                     }
-                    if (more && c.use[x]) multiply(x, 2 * x, next_k, scores);
+                    if (more && !wait(k_full + there, (i_all + 1) >> 1)) break;
+                    const uint64_t key = tc::advance(k0, there * kRows);
+                    if (next0) multiply(0, q0, key, scores);
+                    if (use[1] && !add_keys(1, here, begun[1])) break;
+                    begun[1] |= use[1];
+                    if (one) tc::mma_commit<1>(tc::smem_addr(k_empty + here));
+                    if (more) {
+                        if (!wait(&v_full, i_all + 1)) break;
+                        if (next0 && !multiply_grads(0)) break;
+                        if (next1) multiply(1, q0, key, scores);
+                        if (one && i + 2 == blocks.count) tc::mma_commit<1>(tc::smem_addr(&q_empty));  // the last scores
+                    } else if (one) {
+                        tc::mma_commit<1>(tc::smem_addr(sums + 1));
+                    }
+                    use[0] = next0;
+                    use[1] = next1;
                 }
-                if (!ok) break;
-                if (one) {
-                    tc::mma_commit<1>(tc::smem_addr(empty + k_stage));
-                    if (!more) tc::mma_commit<1>(tc::smem_addr(&done));
-                }
-                k_stage = next_k;
             }
         }
     } else {
         registers_up<kMoreRegisters>();
+        const int mine = warp >> 2, row = threadIdx.x & 127;
         const float c = B.S.scale * kLog2e, f = slope_scale<BF16>(B.S);
-        float lse = 0.f, delta = 0.f;
-        if (r.real) {
-            lse = -B.lse[W.head[mine] * B.S.tokens + t] * kLog2e;
-            delta = -B.delta[W.head[mine] * B.S.tokens + t] * f;
-        }
         const uint32_t lanes = static_cast<uint32_t>(warp % 4 * 32) << 16;
         const uint32_t s_at = tmem + mine * 128 + lanes, q_at = tmem + 256 + mine * D + lanes;
-        const TwoRanges sees{r.first, r.real ? static_cast<int>(t) + 1 : 0, r.start,
-                             r.real ? static_cast<int>(min64(static_cast<int64_t>(r.start) + B.S.sinks, r.first)) : 0};
-        const float2 c2 = make_float2(c, c), lse2 = make_float2(lse, lse), f2 = make_float2(f, f), delta2 = make_float2(delta, delta);
-        uint32_t phase = 0;
-        bool any = false;
-        for (int i = 0; i < blocks.count; ++i) {
-            const Blocks::Block b = blocks.at(i);
-            if (!b.use[mine]) continue;
-            any = true;
-            if (!(ok = tc::barrier_wait(tc::smem_addr(scores + mine), phase))) break;
-            tc::fence_after();
-            const bool whole = __all_sync(kFull, b.from[mine] <= b.at && b.to[mine] >= b.at + kTile && sees.all(b.at, kTile));
-            uint32_t bits[4];
-#pragma unroll
-            for (int w = 0; w < 4; ++w)
-                bits[w] = whole ? ~0u : sees.bits(b.at + w * 32) & range_bits(b.from[mine], b.to[mine], b.at + w * 32);
-            uint32_t p[2][64];
-            tmem_load64(s_at, p[0]);
-            tmem_load64(s_at + 64, p[1]);
-            tc::fence_before();
-            __syncwarp();
-            if (lane == 0) tc::barrier_arrive(tc::smem_addr(taken + mine));
-#pragma unroll
-            for (int k = 0; k < 128; k += 2) {
-                uint32_t &lo = p[k / 64][k % 64], &hi = p[k / 64][k % 64 + 1];
-                const float2 x = fma2(make_float2(__uint_as_float(lo), __uint_as_float(hi)), c2, lse2);
-                lo = __float_as_uint(exp2_fast(x.x));
-                hi = __float_as_uint(exp2_fast(x.y));
+        const float2 c2 = make_float2(c, c), f2 = make_float2(f, f);
+        uint32_t phase = 0, sums_phase = 0;
+        for (int n = 0; n < rounds; ++n) {
+            if (!(ok = warp_wait(item_full + (n & 1), n >> 1))) break;
+            const Item& it = info[n & 1];
+            const int t = it.W.token[mine] + row, head = it.W.head[mine];
+            const Row r = row_in(B.S, it, mine, row);
+            float lse = 0.f, delta = 0.f;
+            if (r.real) {
+                lse = -B.lse[head * B.S.tokens + t] * kLog2e;
+                delta = -B.delta[head * B.S.tokens + t] * f;
             }
-            if (!(ok = tc::barrier_wait(tc::smem_addr(grads + mine), phase))) break;
-            phase ^= 1;
-            tc::fence_after();
+            const float2 lse2 = make_float2(lse, lse), delta2 = make_float2(delta, delta);
+            // What all of the warp's rows see whole.
+            const int whole0 = __reduce_max_sync(kFull, r.real ? r.first : INT32_MAX);
+            const int whole1 = __reduce_min_sync(kFull, r.real ? t + 1 : 0);
+            const Sight& own = it.sight[mine];
+            const Blocks blocks(it.sight[0], it.sight[1]);
+            const int sink_blocks = tiles_of(own.s1 - own.s0), main0 = blocks.base + max(own.lo - blocks.base, 0) / kTile * kTile;
+            const int count = sink_blocks + tiles_of(max(own.hi - main0, 0)), all_count = blocks.count;
+            for (int i = 0; i < count; ++i) {
+                const int at = i < sink_blocks ? own.s0 + i * kTile : main0 + (i - sink_blocks) * kTile;
+                const bool whole = i >= sink_blocks && at >= whole0 && at + kTile <= whole1;
+                if (!(ok = warp_wait(scores + mine, phase))) break;
+                tc::fence_after();
+                uint32_t p[2][64];
+                tmem_load64(s_at, p[0]);
+                tmem_load64(s_at + 64, p[1]);
+                tc::fence_before();
+                warp_arrive(taken + mine);
 #pragma unroll
-            for (int w = 0; w < 2; ++w) {
-                uint32_t d[64], packed[32];
-                tmem_load64(s_at + w * 64, d);
-#pragma unroll
-                for (int k = 0; k < 64; k += 2) {
-                    float2 x = fma2(make_float2(__uint_as_float(d[k]), __uint_as_float(d[k + 1])), f2, delta2);
-                    x = mul2(x, make_float2(__uint_as_float(p[w][k]), __uint_as_float(p[w][k + 1])));
-                    if (!whole) {
-                        x.x = bits[w * 2 + k / 32] >> k % 32 & 1 ? x.x : 0.f;
-                        x.y = bits[w * 2 + k / 32] >> (k % 32 + 1) & 1 ? x.y : 0.f;
-                    }
-                    packed[k / 2] = pack2<BF16>(x.x, x.y);
+                for (int k = 0; k < 128; k += 2) {
+                    uint32_t &lo = p[k / 64][k % 64], &hi = p[k / 64][k % 64 + 1];
+                    const float2 x = fma2(make_float2(__uint_as_float(lo), __uint_as_float(hi)), c2, lse2);
+                    lo = __float_as_uint(exp2_fast(x.x));
+                    hi = __float_as_uint(exp2_fast(x.y));
                 }
-                tmem_store32_begin(s_at + w * 32, packed);
+                if (!whole) {
+                    const int from = i < sink_blocks ? own.s0 : own.lo, to = i < sink_blocks ? own.s1 : own.hi;
+                    const TwoRanges sees{r.first, r.real ? t + 1 : 0, r.start,
+                                         r.real ? static_cast<int>(min64(static_cast<int64_t>(r.start) + B.S.sinks, r.first)) : 0};
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t bits = sees.bits(at + w * 32) & range_bits(from, to, at + w * 32);
+                        if (__all_sync(kFull, bits == ~0u)) continue;
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if (!(bits >> k & 1)) p[w / 2][w % 2 * 32 + k] = 0u;
+                    }
+                }
+                if (!(ok = warp_wait(grads + mine, phase))) break;
+                phase ^= 1;
+                tc::fence_after();
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    float d[32];
+                    uint32_t packed[16];
+                    tc::tmem_load32(s_at + w * 32, d);
+#pragma unroll
+                    for (int k = 0; k < 32; k += 2) {
+                        const float2 x = fma2(make_float2(d[k], d[k + 1]), f2, delta2);
+                        const float2 y = mul2(x, make_float2(__uint_as_float(p[w / 2][w % 2 * 32 + k]), __uint_as_float(p[w / 2][w % 2 * 32 + k + 1])));
+                        packed[k / 2] = pack2<BF16>(y.x, y.y);
+                    }
+                    tmem_store16_begin(s_at + w * 16, packed);
+                }
+                tmem_store_wait();
+                tc::fence_before();
+                warp_arrive(slopes + mine);
             }
-            tmem_store_wait();
-            tc::fence_before();
-            __syncwarp();
-            if (lane == 0) tc::barrier_arrive(tc::smem_addr(slopes + mine));
-        }
-        if (ok && any) ok = tc::barrier_wait(tc::smem_addr(&done), 0);
-        if (ok && blocks.count > 0) ok = tc::barrier_wait(tc::smem_addr(&q_full), 0);
-        tc::fence_after();
-        unsigned char* tile = queries + 2 * mine * kRows;
-        if (ok) {
+            if (!ok) break;
+            if (all_count > 0) {
+                if (!(ok = warp_wait(sums + mine, sums_phase))) break;
+                sums_phase ^= 1;
+            }
+            if (!(ok = warp_wait(g_full + mine, n))) break;  // its place is dQ's now
+            tc::fence_after();
+            unsigned char* tile = grads_out + mine * kRows;
             bool finite = true;
-            if (any) finite = finish_row<D, BF16>(q_at, B.S.scale / f, r.real, tile, row);
+            if (count > 0) finite = finish_row<D, BF16>(q_at, B.S.scale / f, r.real, tile, row);
             else zero_row<D>(tile, row);
             for (uint32_t left = __ballot_sync(kFull, !finite); left; left &= left - 1) {
-                const int other = (row & ~31) + __ffs(left) - 1;
+                const int other = __ffs(left) - 1;
                 __syncwarp();
-                dq_again<BF16, D>(B, W.token[mine] + other, W.head[mine], tile, other);
+                dq_again<BF16, D>(B, __shfl_sync(kFull, t, other), head, tile, (row & ~31) + other);
             }
             fence_to_tma();
-        }
-        named_barrier(1 + mine, 128);
-        if (ok && row == 0 && W.token[mine] < B.S.tokens) {
-#pragma unroll
-            for (int x = 0; x < D / 64; ++x)
-                tma_store(&dqm, tc::smem_addr(tile) + x * kBoxBytes, x * 64, W.head[mine], W.token[mine]);
-            tma_store_done();
+            tc::fence_before();
+            warp_arrive(staged + mine);
+            warp_arrive(item_empty + (n & 1));
         }
     }
     if (!ok && B.S.error) set_error(B.S.error, CB_ERR_TIMEOUT);
@@ -461,7 +540,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
             int s = 0, h = 0, i = 0;
             uint32_t phase = 0;
             for (int64_t n = 0; n < count; ++n) {
-                if (!(ok = tc::barrier_wait(tc::smem_addr(stat_empty + s), phase ^ 1))) break;
+                if (!(ok = warp_wait(stat_empty + s, phase ^ 1))) break;
 #pragma unroll
                 for (int k = 0; k < kTile / 32; ++k) {
                     const int64_t t = first + static_cast<int64_t>(i) * kTile + k * 32 + lane;
@@ -469,8 +548,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                     stats[s][0][k * 32 + lane] = t < B.S.tokens ? kPShift<BF16> - B.lse[at] * kLog2e : 0.f;
                     stats[s][1][k * 32 + lane] = t < B.S.tokens ? -B.delta[at] * f : 0.f;
                 }
-                __syncwarp();
-                if (lane == 0) tc::barrier_arrive(tc::smem_addr(stat_full + s));
+                warp_arrive(stat_full + s);
                 if (++s == kStatStages) s = 0, phase ^= 1;
                 if (++i == blocks) i = 0, ++h;
             }
@@ -544,9 +622,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
             const int at = first + i * kTile + half * 64;
             if (++i == blocks) i = 0;
             const bool whole = __all_sync(kFull, seen.all(at, 64));
-            const uint32_t bits[2] = {seen.bits(at), seen.bits(at + 32)};
-            if (!(ok = tc::barrier_wait(tc::smem_addr(stat_full + s), stat_phase))) break;
-            if (!(ok = tc::barrier_wait(tc::smem_addr(&scores), phase))) break;
+            if (!(ok = warp_wait(stat_full + s, stat_phase))) break;
+            if (!(ok = warp_wait(&scores, phase))) break;
             tc::fence_after();
             uint32_t p[64], packed[32];
             tmem_load64(s_at, p);
@@ -561,25 +638,24 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                 x.y = exp2_fast(x.y);
                 y.x = exp2_fast(y.x);
                 y.y = exp2_fast(y.y);
-                if (!whole) {
-                    x.x = bits[k / 32] >> k % 32 & 1 ? x.x : 0.f;
-                    x.y = bits[k / 32] >> (k % 32 + 1) & 1 ? x.y : 0.f;
-                    y.x = bits[k / 32] >> (k % 32 + 2) & 1 ? y.x : 0.f;
-                    y.y = bits[k / 32] >> (k % 32 + 3) & 1 ? y.y : 0.f;
-                }
-                packed[k / 2] = pack2<BF16>(x.x, x.y);
-                packed[k / 2 + 1] = pack2<BF16>(y.x, y.y);
                 p[k] = __float_as_uint(x.x);
                 p[k + 1] = __float_as_uint(x.y);
                 p[k + 2] = __float_as_uint(y.x);
                 p[k + 3] = __float_as_uint(y.y);
             }
+            if (!whole) {
+                const uint32_t bits[2] = {seen.bits(at), seen.bits(at + 32)};
+#pragma unroll
+                for (int k = 0; k < 64; ++k)
+                    if (!(bits[k / 32] >> k % 32 & 1)) p[k] = 0u;
+            }
+#pragma unroll
+            for (int k = 0; k < 64; k += 2) packed[k / 2] = pack2<BF16>(__uint_as_float(p[k]), __uint_as_float(p[k + 1]));
             tmem_store32_begin(s_at, packed);
             tmem_store_wait();
             tc::fence_before();
-            __syncwarp();
-            if (lane == 0) tc::barrier_arrive(tc::smem_addr(&weights));
-            if (!(ok = tc::barrier_wait(tc::smem_addr(&grads), phase))) break;
+            warp_arrive(&weights);
+            if (!(ok = warp_wait(&grads, phase))) break;
             tc::fence_after();
             uint32_t d[64];
             tmem_load64(g_at, d);
@@ -590,27 +666,18 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                 float2 y = fma2(make_float2(__uint_as_float(d[k + 2]), __uint_as_float(d[k + 3])), f2, make_float2(l.z, l.w));
                 x = mul2(x, make_float2(__uint_as_float(p[k]), __uint_as_float(p[k + 1])));
                 y = mul2(y, make_float2(__uint_as_float(p[k + 2]), __uint_as_float(p[k + 3])));
-                if (!whole) {
-                    x.x = bits[k / 32] >> k % 32 & 1 ? x.x : 0.f;
-                    x.y = bits[k / 32] >> (k % 32 + 1) & 1 ? x.y : 0.f;
-                    y.x = bits[k / 32] >> (k % 32 + 2) & 1 ? y.x : 0.f;
-                    y.y = bits[k / 32] >> (k % 32 + 3) & 1 ? y.y : 0.f;
-                }
                 packed[k / 2] = pack2<BF16>(x.x, x.y);
                 packed[k / 2 + 1] = pack2<BF16>(y.x, y.y);
             }
             tmem_store32_begin(g_at, packed);
             tmem_store_wait();
             tc::fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                tc::barrier_arrive(tc::smem_addr(&slopes));
-                tc::barrier_arrive(tc::smem_addr(stat_empty + s));
-            }
+            warp_arrive(&slopes);
+            warp_arrive(stat_empty + s);
             if (++s == kStatStages) s = 0, stat_phase ^= 1;
         }
         // The first four warps finish dV, the others dK, in the place of V and K.
-        if (ok && count > 0) ok = tc::barrier_wait(tc::smem_addr(&done), 0);
+        if (ok && count > 0) ok = warp_wait(&done, 0);
         tc::fence_after();
         unsigned char* tile = keys + (half ? 0 : kRows);
         if (ok) {
@@ -655,12 +722,12 @@ bool launch_typed(const Backward& B, cudaStream_t s) {
         !muon::shared_memory(attention_dkv_kernel<D, BF16>, kKeyShared<D>, dkv_devices))
         return false;
     const int64_t key_tiles = (S.tokens + kTile - 1) / kTile * S.kv_heads, items = work_items(S);
-    if (items > INT32_MAX || key_tiles > INT32_MAX) return false;
+    if (items > INT32_MAX / 2 || key_tiles > INT32_MAX) return false;
     launch(attention_delta_kernel<D, BF16>, dim3(warp_grid((S.tokens * S.heads * D / 8 + 31) / 32, 152 * 32)), dim3(256), 0, s, B);
     launch(attention_dkv_kernel<D, BF16>, dim3(static_cast<unsigned>(key_tiles)), dim3(kThreads), kKeyShared<D>, s, qm, km, vm, gm,
            dkm, dvm, B);
-    launch(attention_dq_kernel<D, BF16>, dim3(static_cast<unsigned>(items)), dim3(kThreads), kQueryShared<D>, s, qm, km, vm, gm, dqm,
-           B, pairs_heads(S));
+    launch(attention_dq_kernel<D, BF16>, dim3(static_cast<unsigned>(std::min<int64_t>(items, sm_count()))), dim3(kThreads),
+           kQueryShared<D>, s, qm, km, vm, gm, dqm, B, pairs_heads(S), static_cast<int>(items));
     return true;
 }
 

@@ -120,13 +120,12 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
         if (warp == kAheadWarp) {
             for (int n = 0; n < rounds; ++n) {
                 const Work W = work_of(F.S, first + n * stride, pair_heads);
-                if (!(ok = tc::barrier_wait(tc::smem_addr(item_empty + (n & 1)), (n >> 1 & 1) ^ 1))) break;
+                if (!(ok = warp_wait(item_empty + (n & 1), (n >> 1) ^ 1))) break;
                 Item& it = info[n & 1];
                 if (lane == 0) it.W = W;
                 look_ahead(F.S, it, 0, W.token[0], lane);
                 look_ahead(F.S, it, 1, W.token[1], lane);
-                __syncwarp();
-                if (lane == 0) tc::barrier_arrive(tc::smem_addr(item_full + (n & 1)));
+                warp_arrive(item_full + (n & 1));
             }
         } else if (warp == kStoreWarp && tc::elect()) {
             for (int n = 0; n < rounds && ok; ++n) {
@@ -199,8 +198,7 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
                 const Item& it = item_of(n);
                 if (!ok) break;
                 const Blocks blocks(it.sight[0], it.sight[1]);
-                __syncwarp();
-                if (lane == 0) item_done(n);
+                warp_arrive(item_empty + (n & 1));
                 if (!(ok = tc::barrier_wait(tc::smem_addr(&q_full), n & 1))) break;
                 bool begun[2] = {false, false}, use[2] = {false, false};
                 if (blocks.count > 0) {
@@ -276,8 +274,8 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
         const uint32_t s_at = tmem + mine * 128 + lanes, o_at = tmem + 256 + mine * D + lanes;
         uint32_t phase = 0, sums_phase = 0;
         for (int n = 0; n < rounds; ++n) {
-            const Item& it = item_of(n);
-            if (!ok) break;
+            if (!(ok = warp_wait(item_full + (n & 1), n >> 1))) break;
+            const Item& it = info[n & 1];
             const int t = it.W.token[mine] + row, head = it.W.head[mine];
             const Row r = row_in(F.S, it, mine, row);
             // What all of the warp's rows see whole.
@@ -293,7 +291,7 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
             float2 sum0 = make_float2(0.f, 0.f), sum1 = make_float2(0.f, 0.f);
             for (int i = 0; i < count; ++i) {
                 const int at = i < sink_blocks ? own.s0 + i * kTile : main0 + (i - sink_blocks) * kTile;
-                if (!(ok = tc::barrier_wait(tc::smem_addr(scores + mine), phase))) break;
+                if (!(ok = warp_wait(scores + mine, phase))) break;
                 phase ^= 1;
                 tc::fence_after();
                 uint32_t v[2][64], p[16];
@@ -343,17 +341,16 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
                     if ((w + 1) % (4 / kParts)) continue;
                     tmem_store_wait();
                     tc::fence_before();
-                    __syncwarp();
-                    if (lane == 0) tc::barrier_arrive(tc::smem_addr(part[mine] + (w + 1) / (4 / kParts) - 1));
+                    warp_arrive(part[mine] + (w + 1) / (4 / kParts) - 1);
                 }
             }
             if (ok && it_blocks > 0) {
-                ok = tc::barrier_wait(tc::smem_addr(sums + mine), sums_phase);
+                ok = warp_wait(sums + mine, sums_phase);
                 sums_phase ^= 1;
             }
             tc::fence_after();
             // The tiles take turns in the output's place, once the store before has read it.
-            if (!ok || !(ok = tc::barrier_wait(tc::smem_addr(&stored), mine ^ 1))) break;
+            if (!ok || !(ok = warp_wait(&stored, mine ^ 1))) break;
             const float2 both = add2(sum0, sum1);
             const float sum = both.x + both.y;
             const float inv = sum == 0.f ? 0.f : 1.f / sum;  // a NaN stays one
@@ -383,11 +380,8 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
             }
             fence_to_tma();
             tc::fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                tc::barrier_arrive(tc::smem_addr(staged + mine));
-                item_done(n);
-            }
+            warp_arrive(staged + mine);
+            warp_arrive(item_empty + (n & 1));
             if (F.lse && t < F.S.tokens)
                 F.lse[head * F.S.tokens + t] = r.real ? ((most == -INFINITY ? 0.f : most * c) + __log2f(sum) - kShift<BF16>) * kLn2 : -INFINITY;
         }

@@ -162,6 +162,20 @@ __device__ __forceinline__ uint32_t tile_byte(int r, int c) {
     return static_cast<uint32_t>(c >> 3) * kBoxBytes + static_cast<uint32_t>(r) * 128 + static_cast<uint32_t>(((c & 7) ^ (r & 7)) << 4);
 }
 
+// ---------------------------------------------------------------- whole warps
+
+// A whole warp waits, and is together again after it: instructions that want the warp converged may
+// follow (a poll that ends for one lane before another leaves it to the compiler where they meet).
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) {
+    return __all_sync(kFull, tc::barrier_wait(tc::smem_addr(bar), parity & 1));
+}
+// One arrival for the warp, behind what its lanes did.
+__device__ __forceinline__ void warp_arrive(uint64_t* bar) {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) tc::barrier_arrive(tc::smem_addr(bar));
+    __syncwarp();
+}
+
 // ---------------------------------------------------------------- what rows see
 
 // Bits i of columns [a, b) among the 32 from `first` on. (The instruction's shifts by 32 and more give 0.)
