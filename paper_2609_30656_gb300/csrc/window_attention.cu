@@ -34,7 +34,7 @@ __global__ void __launch_bounds__(256) attention_rows_kernel(const Shape S) {
         S.start[t] = static_cast<int32_t>(s);
         S.end[t] = static_cast<int32_t>(e);
     }
-    if (S.largest && first == 0) *S.largest = 0u;
+    if (S.largest && first < 3) S.largest[first] = 0u;  // and the two counters of the order
     if (!S.error) return;
     for (int64_t i = first; i <= S.sequences; i += step) {
         const int64_t here = load_index(S.offsets, i, S.offsets32);
@@ -213,7 +213,7 @@ bool tensor_core_rows(const Shape& S, const Heads& h, int heads) {
 extern "C" int64_t cb_attention_workspace_bytes(int64_t tokens, int32_t heads, int backward) {
     using namespace cbtbe::attention;
     if (tokens <= 0 || tokens > kMostTokens || heads < 1) return 0;
-    return static_cast<int64_t>(2 * rows_bytes(tokens) + (backward ? rows_bytes(tokens * heads) + 256 : 0));
+    return static_cast<int64_t>(2 * rows_bytes(tokens) + (backward ? rows_bytes(tokens * heads) + 256 + rows_bytes(tiles_of(static_cast<int>(tokens))) : 0));
 }
 
 extern "C" cb_status cb_attention_forward(const void* q, const void* k, const void* v, cb_dtype dtype, int64_t tokens,
@@ -280,7 +280,9 @@ extern "C" cb_status cb_attention_backward(const void* grad_out, const void* q, 
         return CB_ERR_INVALID_ARG;
     if (!workspace_ok(workspace, workspace_bytes, cb_attention_workspace_bytes(tokens, heads, 1))) return CB_ERR_CAPACITY;
     B.delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * rows_bytes(tokens));
-    set_rows(B.S, workspace, reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(B.delta) + rows_bytes(tokens * heads)), stream);
+    uint32_t* words = reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(B.delta) + rows_bytes(tokens * heads));
+    B.order = {reinterpret_cast<int32_t*>(words + 1), words + 2, reinterpret_cast<int32_t*>(words + 64)};
+    set_rows(B.S, workspace, words, stream);
     bool ok = true;
     bool fast = true;
     for (const Heads* x : {&B.go, &B.q, &B.out, &B.dq}) fast = fast && tensor_core_rows(B.S, *x, heads);

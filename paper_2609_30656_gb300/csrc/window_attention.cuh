@@ -45,11 +45,19 @@ struct Forward {
     Heads q, k, v, out;
     float* lse;  // [heads, tokens], or null
 };
+// The order in which tiles of keys are taken: those that the most queries see, then the others. (Their results do not
+// depend on it.)
+struct Order {
+    int32_t* long_tiles;  // how many, and next item to take: 0 before
+    uint32_t* next;
+    int32_t* tiles;       // [tiles of 128 tokens]
+};
 struct Backward {
     Shape S;
     Heads go, q, k, v, out, dq, dk, dv;
     const float* lse;
     float* delta;  // [heads, tokens]
+    Order order;
 };
 
 // ---------------------------------------------------------------- a row at a time

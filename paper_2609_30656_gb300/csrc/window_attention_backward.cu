@@ -24,9 +24,12 @@ namespace attention {
 namespace {
 
 constexpr int kWorkWarps = 8, kCopyWarp = 8, kMultiplyWarp = 9, kThreads = 384;
-constexpr int kAheadWarp = 10, kStoreWarp = 11;  // over queries
-constexpr int kStatWarp = 10;                    // over keys
-constexpr int kMoreRegisters = 208, kFewerRegisters = 88;  // 256 x 208 + 128 x 88 of 384 x 168
+constexpr int kAheadWarp = 10;
+constexpr int kStoreWarp = 11;  // over queries
+constexpr int kStatWarp = 11;   // over keys
+// Registers of the threads that work and of the others, of 384 x 168 at launch: what leaves either fewest spills (with
+// shared memory taken, little of L1 is left, and a spilled register costs hundreds of clocks).
+constexpr int kQueryMore = 208, kQueryFewer = 88, kKeyMore = 208, kKeyFewer = 88;
 
 template <bool BF16> constexpr float kPShift = BF16 ? 0.f : 12.f;
 template <bool BF16>
@@ -34,6 +37,16 @@ __device__ __forceinline__ float slope_scale(const Shape& S) {
     if constexpr (BF16) return 1.f;
     const uint32_t bits = *S.largest;
     return bits == 0 ? 1.f : exp2f(static_cast<float>(4 - ilogbf(__uint_as_float(bits))));
+}
+
+// Behind the last token that sees key j, 0 for a token of no session.
+__device__ __forceinline__ int seen_until(const Shape& S, int64_t j) {
+    if (j >= S.tokens || S.end[j] <= j) return 0;
+    return static_cast<int>(j - S.start[j] < S.sinks ? S.end[j] : min64(S.end[j], j + S.window));
+}
+// Seen by more than three windows of queries, or a few thousand.
+__device__ __forceinline__ bool is_long(const Shape& S, int first, int until) {
+    return until - first > max64(3 * S.window, 0) + 2048;
 }
 
 // delta, and the largest |grad_out|: 16 bytes a lane, D / 8 lanes a row.
@@ -61,6 +74,16 @@ __global__ void __launch_bounds__(256) attention_delta_kernel(const Backward B) 
 #pragma unroll
         for (int off = kLanes / 2; off >= 1; off >>= 1) sum += __shfl_xor_sync(kFull, sum, off);
         if (i < rows && lane % kLanes == 0) B.delta[h * S.tokens + t] = sum;
+    }
+    // Tiles of keys that many more queries see than their windows say (a session's first tokens): listed, to be taken first.
+    const int tiles = tiles_of(static_cast<int>(S.tokens));
+    for (int64_t w = warp_id_global(); w < tiles; w += warps_in_grid()) {
+        const int from = static_cast<int>(w) * kTile;
+        int until = 0;
+#pragma unroll
+        for (int k = 0; k < kTile / 32; ++k) until = max(until, seen_until(S, from + k * 32 + lane));
+        until = __reduce_max_sync(kFull, until);
+        if (lane == 0 && is_long(S, from, until)) B.order.tiles[atomicAdd(B.order.long_tiles, 1)] = static_cast<int>(w);
     }
     if constexpr (!BF16) {
         const uint32_t most = __reduce_max_sync(kFull, __float_as_uint(largest));
@@ -142,7 +165,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
     unsigned char* keys = queries + 4 * kRows;
     unsigned char* values = keys + kKeyBuffers * kRows;
     __shared__ uint64_t q_full, q_empty, g_full[2], stored[2], k_full[2], k_empty[2], v_full, v_empty;
-    __shared__ uint64_t scores[2], taken[2], grads[2], slopes[2], sums[2], staged[2], item_full[2], item_empty[2];
+    __shared__ uint64_t scores[2], taken[2], grads[2], slopes[2][2], sums[2], staged[2], item_full[2], item_empty[2];
     __shared__ uint32_t tmem_at;
     __shared__ Item info[2];
     const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
@@ -151,7 +174,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
         for (uint64_t* b : {&q_full, &q_empty, &v_full, &v_empty}) tc::barrier_init(tc::smem_addr(b), 1);
         for (int i = 0; i < 2; ++i) {
             for (uint64_t* b : {g_full, stored, k_full, k_empty, scores, grads, sums, item_full}) tc::barrier_init(tc::smem_addr(b + i), 1);
-            for (uint64_t* b : {taken, slopes, staged}) tc::barrier_init(tc::smem_addr(b + i), 4);
+            for (uint64_t* b : {taken, slopes[0], slopes[1], staged}) tc::barrier_init(tc::smem_addr(b + i), 4);
             tc::barrier_init(tc::smem_addr(item_empty + i), kWorkWarps + 3);
         }
         tc::barrier_init_fence();
@@ -166,8 +189,9 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
     const int first = static_cast<int>(blockIdx.x), stride = static_cast<int>(gridDim.x);
     const int rounds = (items - first + stride - 1) / stride;
     bool ok = true;
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return ok = tc::barrier_wait(tc::smem_addr(bar), parity & 1); };
-    // The n-th item; the caller is done with it at item_done.
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return ok = tc::barrier_wait(tc::smem_addr(bar), parity & 1); };  // one thread
+    auto meet = [&](uint64_t* bar, uint32_t parity) { return ok = warp_wait(bar, parity); };                          // a whole warp
+    // The n-th item, for one thread; it is done with it at item_done.
     auto item_of = [&](int n) -> const Item& {
         wait(item_full + (n & 1), n >> 1);
         return info[n & 1];
@@ -175,7 +199,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
     auto item_done = [&](int n) { tc::barrier_arrive(tc::smem_addr(item_empty + (n & 1))); };
 
     if (warp >= kWorkWarps) {
-        registers_down<kFewerRegisters>();
+        registers_down<kQueryFewer>();
         if (warp == kAheadWarp) {
             for (int n = 0; n < rounds; ++n) {
                 const Work W = work_of(B.S, first + n * stride, pair_heads);
@@ -250,63 +274,73 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
                 for (int k = max(0, loaded_k - 2); k < loaded_k; ++k) land(k_full + (k & 1), k >> 1);
             }
         } else if (warp == kMultiplyWarp) {
-            constexpr uint32_t shape_s = mma_shape<BF16>(kTile, kTile, false), shape_q = mma_shape<BF16>(kTile, D, true);
             const bool one = tc::elect();
+            constexpr uint32_t shape_s = mma_shape<BF16>(kTile, kTile, false), shape_q = mma_shape<BF16>(kTile, D, true);
             const uint64_t q0 = tc::operand_k_major(tc::smem_addr(queries)), g0 = tc::operand_k_major(tc::smem_addr(grads_out));
             const uint64_t k0 = tc::operand_k_major(tc::smem_addr(keys)), v0 = tc::operand_k_major(tc::smem_addr(values));
             const uint64_t turned0 = tc::operand_mn_major(tc::smem_addr(keys), kBoxBytes);
             int i_all = 0;
             uint32_t taken_turn[2] = {0, 0}, slopes_turn[2] = {0, 0};
+            auto commit = [&](uint64_t* bar) {
+                if (one) tc::mma_commit<1>(tc::smem_addr(bar));
+                __syncwarp();
+            };
             auto multiply = [&](int x, uint64_t a, uint64_t b, uint64_t* bar) {  // Q_x K^T or dO_x V^T
-                if (!one) return;
                 a = tc::advance(a, x * kRows);
+                if (one) {
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t off = k / 4 * kBoxBytes + k % 4 * 32;
-                    tc::mma_f16<1>(tmem + x * 128, tc::advance(a, off), tc::advance(b, off), shape_s, k > 0);
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint32_t off = k / 4 * kBoxBytes + k % 4 * 32;
+                        tc::mma_f16<1>(tmem + x * 128, tc::advance(a, off), tc::advance(b, off), shape_s, k > 0);
+                    }
+                    tc::mma_commit<1>(tc::smem_addr(bar + x));
                 }
-                tc::mma_commit<1>(tc::smem_addr(bar + x));
+                __syncwarp();
             };
             auto multiply_grads = [&](int x) {  // dP_x, once S_x has been read from its columns
-                if (!wait(taken + x, taken_turn[x])) return false;
+                if (!meet(taken + x, taken_turn[x])) return false;
                 taken_turn[x] ^= 1;
                 tc::fence_after();
                 multiply(x, g0, v0, grads);
                 return true;
             };
             auto add_keys = [&](int x, int buffer, bool add) {  // dQ_x += dS_x K
-                if (!wait(slopes + x, slopes_turn[x])) return false;
-                slopes_turn[x] ^= 1;
-                tc::fence_after();
                 const uint64_t b = tc::advance(turned0, buffer * kRows);
-                if (one)
 #pragma unroll
-                    for (int k = 0; k < kTile / 16; ++k)
-                        mma_tmem(tmem + 256 + x * D, tmem + x * 128 + k * 8, tc::advance(b, k * 2048), shape_q, add || k > 0);
+                for (int h = 0; h < 2; ++h) {  // half of the keys, then the other half
+                    if (!meet(slopes[x] + h, slopes_turn[x])) return false;
+                    tc::fence_after();
+                    if (one)
+#pragma unroll
+                        for (int k = 4 * h; k < 4 * h + 4; ++k)
+                            mma_tmem(tmem + 256 + x * D, tmem + x * 128 + k * 8, tc::advance(b, k * 2048), shape_q, add || k > 0);
+                    __syncwarp();
+                }
+                slopes_turn[x] ^= 1;
                 return true;
             };
             // In turns dQ of one tile, dP of the other, S of the first: each finds its operands ready while the one
             // before runs.
             for (int n = 0; n < rounds && ok; ++n) {
-                const Item& it = item_of(n);
-                if (!ok) break;
+                if (!meet(item_full + (n & 1), n >> 1)) break;
+                const Item& it = info[n & 1];
                 const Blocks blocks(it.sight[0], it.sight[1]);
                 warp_arrive(item_empty + (n & 1));
-                if (!wait(&q_full, n)) break;
+                if (!meet(&q_full, n)) break;
                 bool begun[2] = {false, false}, use[2] = {false, false};
                 if (blocks.count > 0) {
-                    if (!wait(k_full + (i_all & 1), i_all >> 1)) break;
+                    if (!meet(k_full + (i_all & 1), i_all >> 1)) break;
                     tc::fence_after();
                     const uint64_t key = tc::advance(k0, (i_all & 1) * kRows);
                     const Blocks::Block b = blocks.at(0);
                     use[0] = b.use[0];
                     use[1] = b.use[1];
                     if (use[0]) multiply(0, q0, key, scores);
-                    if (!wait(g_full, n) || !wait(g_full + 1, n) || !wait(&v_full, i_all)) break;
+                    if (!meet(g_full, n) || !meet(g_full + 1, n) || !meet(&v_full, i_all)) break;
                     if (use[0] && !multiply_grads(0)) break;
                     if (use[1]) multiply(1, q0, key, scores);
                 }
-                if (blocks.count <= 1 && one) tc::mma_commit<1>(tc::smem_addr(&q_empty));
+                if (blocks.count <= 1) commit(&q_empty);
                 for (int i = 0; i < blocks.count; ++i, ++i_all) {
                     const bool more = i + 1 < blocks.count;
                     const Blocks::Block c = blocks.at(i + 1);
@@ -315,23 +349,21 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
                     if (use[0] && !add_keys(0, here, begun[0])) break;
                     begun[0] |= use[0];
                     if (use[1] && !multiply_grads(1)) break;
-                    if (one) {
-                        tc::mma_commit<1>(tc::smem_addr(&v_empty));
-                        if (!more) tc::mma_commit<1>(tc::smem_addr(sums));
-                    }
-                    if (more && !wait(k_full + there, (i_all + 1) >> 1)) break;
+                    commit(&v_empty);
+                    if (!more) commit(sums);
+                    if (more && !meet(k_full + there, (i_all + 1) >> 1)) break;
                     const uint64_t key = tc::advance(k0, there * kRows);
                     if (next0) multiply(0, q0, key, scores);
                     if (use[1] && !add_keys(1, here, begun[1])) break;
                     begun[1] |= use[1];
-                    if (one) tc::mma_commit<1>(tc::smem_addr(k_empty + here));
+                    commit(k_empty + here);
                     if (more) {
-                        if (!wait(&v_full, i_all + 1)) break;
+                        if (!meet(&v_full, i_all + 1)) break;
                         if (next0 && !multiply_grads(0)) break;
                         if (next1) multiply(1, q0, key, scores);
-                        if (one && i + 2 == blocks.count) tc::mma_commit<1>(tc::smem_addr(&q_empty));  // the last scores
-                    } else if (one) {
-                        tc::mma_commit<1>(tc::smem_addr(sums + 1));
+                        if (i + 2 == blocks.count) commit(&q_empty);  // the last scores
+                    } else {
+                        commit(sums + 1);
                     }
                     use[0] = next0;
                     use[1] = next1;
@@ -339,7 +371,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
             }
         }
     } else {
-        registers_up<kMoreRegisters>();
+        registers_up<kQueryMore>();
         const int mine = warp >> 2, row = threadIdx.x & 127;
         const float c = B.S.scale * kLog2e, f = slope_scale<BF16>(B.S);
         const uint32_t lanes = static_cast<uint32_t>(warp % 4 * 32) << 16;
@@ -409,10 +441,11 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
                         packed[k / 2] = pack2<BF16>(y.x, y.y);
                     }
                     tmem_store16_begin(s_at + w * 16, packed);
+                    if (w % 2 == 0) continue;
+                    tmem_store_wait();
+                    tc::fence_before();
+                    warp_arrive(slopes[mine] + w / 2);
                 }
-                tmem_store_wait();
-                tc::fence_before();
-                warp_arrive(slopes + mine);
             }
             if (!ok) break;
             if (all_count > 0) {
@@ -449,10 +482,18 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
 constexpr int kKeyStages = 4, kStatStages = 4;
 template <int D> constexpr size_t kKeyShared = 1024 + (2 + kKeyStages) * kRowsBytes<D>;
 
+// A tile of keys and the queries that see one of them.
+struct KeyItem {
+    int first, kv;    // token, head
+    int blocks;       // of 128 queries from `first` on, for each head that shares the keys; -1: no more items
+    int last[kTile];  // behind the last token that sees the key, 0 for one of no session
+};
+
 // A block has 128 keys of a head and takes the queries that see one of them, 128 at a time, for every head that
 // shares the keys. S^T and dP^T have a key a lane, so that P^T and dS^T are operands from TMEM as they are; a warp takes
 // half of the queries of its 32 keys. The products of a block follow one another as their operands
-// come: S, dP | dV, S' (while dS is worked out) | dK, dP' (while P' is).
+// come: S, dP | dV, S' (while dS is worked out) | dK, dP' (while P' is). Blocks stay and take the next tile
+// from a counter, those with the most queries first: a session's first keys are seen to its end.
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constant__ CUtensorMap km,
@@ -463,17 +504,16 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
     constexpr uint32_t kRows = kRowsBytes<D>;
     extern __shared__ unsigned char dynamic[];
     unsigned char* keys = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~uintptr_t(1023));
-    unsigned char* ring = keys + 2 * kRows;  // K, V
-    __shared__ uint64_t kv_full, full[S], empty[S], scores, weights, grads, slopes, done, stat_full[kStatStages], stat_empty[kStatStages];
+    unsigned char* ring = keys + 2 * kRows;  // K and V, and dK and dV in their place
+    __shared__ uint64_t kv_full, stored, staged[2], full[S], empty[S], scores, weights, grads, slopes, done;
+    __shared__ uint64_t stat_full[kStatStages], stat_empty[kStatStages], item_full[2], item_empty[2];
     __shared__ uint32_t tmem_at;
-    __shared__ int last_of[4];
+    __shared__ KeyItem info[2];
     __shared__ __align__(16) float stats[kStatStages][2][kTile];  // -lse log2 e (+ shift) and -delta (times the slopes' scale)
     const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-    const int tile_index = static_cast<int>(blockIdx.x / static_cast<unsigned>(B.S.kv_heads));
-    const int kv = static_cast<int>(blockIdx.x - static_cast<unsigned>(tile_index) * B.S.kv_heads), first = tile_index * kTile;
 
     if (threadIdx.x == 0) {
-        for (uint64_t* b : {&kv_full, &scores, &grads, &done}) tc::barrier_init(tc::smem_addr(b), 1);
+        for (uint64_t* b : {&kv_full, &stored, &scores, &grads, &done}) tc::barrier_init(tc::smem_addr(b), 1);
         for (uint64_t* b : {&weights, &slopes}) tc::barrier_init(tc::smem_addr(b), kWorkWarps);
         for (int i = 0; i < S; ++i) {
             tc::barrier_init(tc::smem_addr(full + i), 1);
@@ -483,207 +523,301 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
             tc::barrier_init(tc::smem_addr(stat_full + i), 1);
             tc::barrier_init(tc::smem_addr(stat_empty + i), kWorkWarps);
         }
+        for (int i = 0; i < 2; ++i) {
+            tc::barrier_init(tc::smem_addr(staged + i), 4);
+            tc::barrier_init(tc::smem_addr(item_full + i), 1);
+            tc::barrier_init(tc::smem_addr(item_empty + i), kWorkWarps + 4);
+        }
         tc::barrier_init_fence();
         for (const CUtensorMap* m : {&qm, &km, &vm, &gm, &dkm, &dvm}) tc::tma_prefetch(m);
     }
     if (warp == kMultiplyWarp) tc::tmem_alloc<1>(tc::smem_addr(&tmem_at), 512);
-    begin_kernel();
-    const int row = threadIdx.x & 127, half = warp >> 2 & 1;
-    const int64_t j = first + row;
-    int last = 0;  // behind the last token that sees key j
-    bool real = false;
-    if (warp < kWorkWarps && j < B.S.tokens && B.S.end[j] > j) {
-        real = true;
-        last = static_cast<int>(j - B.S.start[j] < B.S.sinks ? B.S.end[j] : min64(B.S.end[j], j + B.S.window));
-    }
-    if (warp < 4) {
-        const int most = __reduce_max_sync(kFull, last);
-        if (lane == 0) last_of[warp] = most;
-    }
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
     const uint32_t tmem = tmem_at;
-    const int until = max(max(last_of[0], last_of[1]), max(last_of[2], last_of[3]));
-    const int blocks = tiles_of(max(until - first, 0));  // of queries, for each head
-    const int64_t count = static_cast<int64_t>(blocks) * B.S.group;
-    const int head0 = kv * B.S.group;
+    begin_kernel();
     bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return ok = tc::barrier_wait(tc::smem_addr(bar), parity & 1); };  // one thread
+    auto meet = [&](uint64_t* bar, uint32_t parity) { return ok = warp_wait(bar, parity); };                          // a whole warp
 
     if (warp >= kWorkWarps) {
-        registers_down<kFewerRegisters>();
-        if (warp == kCopyWarp && tc::elect()) {
-            if (count > 0) {
+        registers_down<kKeyFewer>();
+        if (warp == kAheadWarp) {  // the next item, and the results of the one before
+            const int kv_heads = B.S.kv_heads, tiles = tiles_of(static_cast<int>(B.S.tokens)), longer = *B.order.long_tiles * kv_heads;
+            const int64_t all = static_cast<int64_t>(longer) + static_cast<int64_t>(tiles) * kv_heads;
+            auto store = [&](int n) {  // of the n-th item
+                const int first = info[n & 1].first, kv = info[n & 1].kv;
+                if (!(ok = warp_wait(staged, n) && warp_wait(staged + 1, n))) return;
+                if (lane == 0) {
+#pragma unroll
+                    for (int x = 0; x < D / 64; ++x) {
+                        tma_store(&dkm, tc::smem_addr(keys) + x * kBoxBytes, x * 64, kv, first);
+                        tma_store(&dvm, tc::smem_addr(keys) + kRows + x * kBoxBytes, x * 64, kv, first);
+                    }
+                    tma_store_done();
+                }
+                __syncwarp();
+                warp_arrive(&stored);
+                warp_arrive(item_empty + (n & 1));
+            };
+            for (int n = 0;; ++n) {
+                int first = 0, kv = 0, until = 0, last[kTile / 32];
+                bool some = false;
+                while (!some) {
+                    unsigned w = 0;
+                    if (lane == 0) w = atomicAdd(B.order.next, 1u);
+                    w = __shfl_sync(kFull, w, 0);
+                    if (w >= all) break;
+                    const int index = w < static_cast<unsigned>(longer) ? static_cast<int>(w) : static_cast<int>(w) - longer;
+                    const int tile = w < static_cast<unsigned>(longer) ? B.order.tiles[index / kv_heads] : index / kv_heads;
+                    kv = index % kv_heads;
+                    first = tile * kTile;
+                    until = 0;
+#pragma unroll
+                    for (int k = 0; k < kTile / 32; ++k) {
+                        last[k] = seen_until(B.S, first + k * 32 + lane);
+                        until = max(until, last[k]);
+                    }
+                    until = __reduce_max_sync(kFull, until);
+                    some = w < static_cast<unsigned>(longer) || !is_long(B.S, first, until);
+                }
+                // The place of the item before the last one: its results are stored first.
+                if (n >= 2) {
+                    store(n - 2);
+                    if (!ok) break;
+                }
+                if (!(ok = warp_wait(item_empty + (n & 1), (n >> 1) ^ 1))) break;
+                KeyItem& it = info[n & 1];
+                if (lane == 0) {
+                    it.first = first;
+                    it.kv = kv;
+                    it.blocks = some ? tiles_of(max(until - first, 0)) : -1;
+                }
+                if (some)
+#pragma unroll
+                    for (int k = 0; k < kTile / 32; ++k) it.last[k * 32 + lane] = last[k];
+                warp_arrive(item_full + (n & 1));
+                if (!some) {
+                    if (n >= 1) store(n - 1);
+                    break;
+                }
+            }
+        } else if (warp == kCopyWarp && tc::elect()) {
+            int s = 0, n = 0;
+            uint32_t phase = 0;
+            int64_t issued = 0;
+            for (;; ++n) {
+                if (!wait(item_full + (n & 1), n >> 1)) break;
+                const KeyItem& it = info[n & 1];
+                const int first = it.first, kv = it.kv, blocks = it.blocks;
+                tc::barrier_arrive(tc::smem_addr(item_empty + (n & 1)));
+                if (blocks < 0) break;
+                int64_t m = 0;
+                auto load = [&] {  // the next tile of the ring
+                    if (!wait(empty + s, phase ^ 1)) return false;
+                    const int b = static_cast<int>(m >> 1), h = b / blocks, i = b - h * blocks;
+                    tc::barrier_expect(tc::smem_addr(full + s), kRows);
+                    load_tile<D>(tc::smem_addr(ring) + s * kRows, m & 1 ? &gm : &qm, tc::smem_addr(full + s), kv * B.S.group + h,
+                                 first + i * kTile);
+                    ++m;
+                    ++issued;
+                    if (++s == S) s = 0, phase ^= 1;
+                    return true;
+                };
+                const int64_t all = 2 * static_cast<int64_t>(blocks) * B.S.group;
+                // The first queries come while the results before leave the keys' place.
+                while (m < 2 && m < all && load()) {}
+                if (!ok || !wait(&stored, n ^ 1)) break;
                 tc::barrier_expect(tc::smem_addr(&kv_full), 2 * kRows);
                 load_tile<D>(tc::smem_addr(keys), &km, tc::smem_addr(&kv_full), kv, first);
                 load_tile<D>(tc::smem_addr(keys) + kRows, &vm, tc::smem_addr(&kv_full), kv, first);
+                while (m < all && load()) {}
+                if (!ok) {
+                    tc::barrier_wait(tc::smem_addr(&kv_full), n & 1);
+                    break;
+                }
             }
-            int s = 0, h = 0, i = 0;
-            uint32_t phase = 0;
-            int64_t issued = 0;
-            for (int64_t n = 0; n < 2 * count; ++n) {
-                if (!(ok = tc::barrier_wait(tc::smem_addr(empty + s), phase ^ 1))) break;
-                const uint32_t bar = tc::smem_addr(full + s);
-                tc::barrier_expect(bar, kRows);
-                load_tile<D>(tc::smem_addr(ring) + s * kRows, n & 1 ? &gm : &qm, bar, head0 + h, first + i * kTile);
-                ++issued;
-                if (++s == S) s = 0, phase ^= 1;
-                if (n & 1)
-                    if (++i == blocks) i = 0, ++h;
-            }
-            if (!ok)
-                for (int64_t n = max64(0, issued - S); n < issued; ++n)
-                    if (!tc::barrier_wait(tc::smem_addr(full + n % S), n / S & 1)) break;
-        }
-        if (warp == kStatWarp) {
+            if (!ok)  // copies in flight land before the block's shared memory goes away
+                for (int64_t i = max64(0, issued - S); i < issued; ++i)
+                    if (!tc::barrier_wait(tc::smem_addr(full + i % S), i / S & 1)) break;
+        } else if (warp == kStatWarp) {
             const float f = slope_scale<BF16>(B.S) * exp2f(-kPShift<BF16>);
-            int s = 0, h = 0, i = 0;
+            int s = 0;
             uint32_t phase = 0;
-            for (int64_t n = 0; n < count; ++n) {
-                if (!(ok = warp_wait(stat_empty + s, phase ^ 1))) break;
+            for (int n = 0; ok; ++n) {
+                if (!(ok = warp_wait(item_full + (n & 1), n >> 1))) break;
+                const int first = info[n & 1].first, kv = info[n & 1].kv, blocks = info[n & 1].blocks;
+                warp_arrive(item_empty + (n & 1));
+                if (blocks < 0) break;
+                for (int h = 0; h < B.S.group && ok; ++h) {
+                    const int64_t row = static_cast<int64_t>(kv * B.S.group + h) * B.S.tokens;
+                    for (int i = 0; i < blocks; ++i) {
+                        if (!(ok = warp_wait(stat_empty + s, phase ^ 1))) break;
 #pragma unroll
-                for (int k = 0; k < kTile / 32; ++k) {
-                    const int64_t t = first + static_cast<int64_t>(i) * kTile + k * 32 + lane;
-                    const int64_t at = (head0 + h) * B.S.tokens + t;
-                    stats[s][0][k * 32 + lane] = t < B.S.tokens ? kPShift<BF16> - B.lse[at] * kLog2e : 0.f;
-                    stats[s][1][k * 32 + lane] = t < B.S.tokens ? -B.delta[at] * f : 0.f;
+                        for (int k = 0; k < kTile / 32; ++k) {
+                            const int64_t t = first + static_cast<int64_t>(i) * kTile + k * 32 + lane;
+                            stats[s][0][k * 32 + lane] = t < B.S.tokens ? kPShift<BF16> - B.lse[row + t] * kLog2e : 0.f;
+                            stats[s][1][k * 32 + lane] = t < B.S.tokens ? -B.delta[row + t] * f : 0.f;
+                        }
+                        warp_arrive(stat_full + s);
+                        if (++s == kStatStages) s = 0, phase ^= 1;
+                    }
                 }
-                warp_arrive(stat_full + s);
-                if (++s == kStatStages) s = 0, phase ^= 1;
-                if (++i == blocks) i = 0, ++h;
             }
-        }
-        if (warp == kMultiplyWarp && count > 0) {
-            constexpr uint32_t shape_s = mma_shape<BF16>(kTile, kTile, false), shape_d = mma_shape<BF16>(kTile, D, true);
+        } else if (warp == kMultiplyWarp) {
             const bool one = tc::elect();
-            const uint32_t k0 = tc::smem_addr(keys), q0 = tc::smem_addr(ring);
+            constexpr uint32_t shape_s = mma_shape<BF16>(kTile, kTile, false), shape_d = mma_shape<BF16>(kTile, D, true);
+            const uint64_t k0 = tc::operand_k_major(tc::smem_addr(keys)), q0 = tc::operand_k_major(tc::smem_addr(ring));
+            const uint64_t turned0 = tc::operand_mn_major(tc::smem_addr(ring), kBoxBytes);
+            auto commit = [&](uint64_t* bar) {
+                if (one) tc::mma_commit<1>(tc::smem_addr(bar));
+                __syncwarp();
+            };
             auto multiply = [&](uint32_t left, int stage, uint32_t to, uint64_t* bar) {  // K Q^T or V dO^T
-                if (!one) return;
-                const uint64_t a = tc::operand_k_major(k0 + left * kRows), b = tc::operand_k_major(q0 + stage * kRows);
+                const uint64_t a = tc::advance(k0, left * kRows), b = tc::advance(q0, stage * kRows);
+                if (one) {
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t off = k / 4 * kBoxBytes + k % 4 * 32;
-                    tc::mma_f16<1>(tmem + to, tc::advance(a, off), tc::advance(b, off), shape_s, k > 0);
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint32_t off = k / 4 * kBoxBytes + k % 4 * 32;
+                        tc::mma_f16<1>(tmem + to, tc::advance(a, off), tc::advance(b, off), shape_s, k > 0);
+                    }
+                    tc::mma_commit<1>(tc::smem_addr(bar));
                 }
-                tc::mma_commit<1>(tc::smem_addr(bar));
+                __syncwarp();
             };
             auto accumulate = [&](uint32_t from, int stage, uint32_t to, bool add) {  // P^T dO or dS^T Q
-                if (!one) return;
-                const uint64_t b = tc::operand_mn_major(q0 + stage * kRows, kBoxBytes);
+                const uint64_t b = tc::advance(turned0, stage * kRows);
+                if (one)
 #pragma unroll
-                for (int k = 0; k < kTile / 16; ++k)  // half of the queries in columns 0 .. 31, half in 64 .. 95
-                    mma_tmem(tmem + to, tmem + from + k / 4 * 64 + k % 4 * 8, tc::advance(b, k * 2048), shape_d, add || k > 0);
+                    for (int k = 0; k < kTile / 16; ++k)  // half of the queries in columns 0 .. 31, half in 64 .. 95
+                        mma_tmem(tmem + to, tmem + from + k / 4 * 64 + k % 4 * 8, tc::advance(b, k * 2048), shape_d, add || k > 0);
+                __syncwarp();
             };
-            auto wait = [&](uint64_t* bar, int64_t n) { return tc::barrier_wait(tc::smem_addr(bar), static_cast<uint32_t>(n & 1)); };
-            // The tile of turn m in the ring (Q of block n: m = 2 n, dO: 2 n + 1).
-            auto wait_full = [&](int64_t m) { return tc::barrier_wait(tc::smem_addr(full + m % S), static_cast<uint32_t>(m / S & 1)); };
-            ok = tc::barrier_wait(tc::smem_addr(&kv_full), 0) && wait_full(0) && wait_full(1);
-            tc::fence_after();
-            if (ok) {
-                multiply(0, 0, 0, &scores);
-                multiply(1, 1, 128, &grads);
-            }
-            for (int64_t n = 0; n < count && ok; ++n) {
-                const int q = static_cast<int>(2 * n % S), g = q + 1, q_next = static_cast<int>((2 * n + 2) % S);
-                const bool more = n + 1 < count;
-                if (!(ok = wait(&weights, n))) break;
+            uint32_t turn = 0;  // blocks before: block `turn` has its Q in the ring's tile 2 turn, dO in 2 turn + 1
+            auto tile_here = [&](uint32_t m) { return meet(full + m % S, m / S); };
+            for (int n = 0; ok; ++n) {
+                if (!meet(item_full + (n & 1), n >> 1)) break;
+                const int blocks = info[n & 1].blocks;
+                warp_arrive(item_empty + (n & 1));
+                if (blocks < 0) break;
+                const int64_t count = static_cast<int64_t>(blocks) * B.S.group;
+                if (!meet(&kv_full, n)) break;
+                if (count == 0) continue;
+                if (!tile_here(2 * turn)) break;
                 tc::fence_after();
-                accumulate(0, g, 256, n > 0);
-                if (more) {
-                    if (!(ok = wait_full(2 * n + 2))) break;
-                    multiply(0, q_next, 0, &scores);
-                }
-                if (!(ok = wait(&slopes, n))) break;
-                tc::fence_after();
-                accumulate(128, q, 256 + D, n > 0);
-                if (one) {
-                    tc::mma_commit<1>(tc::smem_addr(empty + q));
-                    tc::mma_commit<1>(tc::smem_addr(empty + g));
-                }
-                if (more) {
-                    if (!(ok = wait_full(2 * n + 3))) break;
-                    multiply(1, q_next + 1, 128, &grads);
-                } else if (one) {
-                    tc::mma_commit<1>(tc::smem_addr(&done));
+                multiply(0, 2 * turn % S, 0, &scores);
+                if (!tile_here(2 * turn + 1)) break;
+                multiply(1, 2 * turn % S + 1, 128, &grads);
+                for (int64_t i = 0; i < count; ++i, ++turn) {
+                    const int q = static_cast<int>(2 * turn % S), g = q + 1, q_next = static_cast<int>((2 * turn + 2) % S);
+                    const bool more = i + 1 < count;
+                    if (!meet(&weights, turn)) break;
+                    tc::fence_after();
+                    accumulate(0, g, 256, i > 0);
+                    commit(empty + g);
+                    if (more) {
+                        if (!tile_here(2 * turn + 2)) break;
+                        multiply(0, q_next, 0, &scores);
+                    }
+                    if (!meet(&slopes, turn)) break;
+                    tc::fence_after();
+                    accumulate(128, q, 256 + D, i > 0);
+                    commit(empty + q);
+                    if (more) {
+                        if (!tile_here(2 * turn + 3)) break;
+                        multiply(1, q_next + 1, 128, &grads);
+                    } else {
+                        commit(&done);
+                    }
                 }
             }
         }
     } else {
-        registers_up<kMoreRegisters>();
-        const float c = B.S.scale * kLog2e, f = slope_scale<BF16>(B.S) * exp2f(-kPShift<BF16>);
+        registers_up<kKeyMore>();
+        const int row = threadIdx.x & 127, half = warp >> 2;
+        const float scale_s = slope_scale<BF16>(B.S);
+        const float c = B.S.scale * kLog2e, f = scale_s * exp2f(-kPShift<BF16>);
         const float2 c2 = make_float2(c, c), f2 = make_float2(f, f);
         const uint32_t lanes = static_cast<uint32_t>(warp % 4 * 32) << 16;
         const uint32_t s_at = tmem + lanes + half * 64, g_at = s_at + 128;
-        const TwoRanges seen{static_cast<int>(j), last, 0, 0};
-        int s = 0, i = 0;
-        uint32_t stat_phase = 0;
-        for (int64_t n = 0; n < count; ++n) {
-            const uint32_t phase = static_cast<uint32_t>(n & 1);
-            const int at = first + i * kTile + half * 64;
-            if (++i == blocks) i = 0;
-            const bool whole = __all_sync(kFull, seen.all(at, 64));
-            if (!(ok = warp_wait(stat_full + s, stat_phase))) break;
-            if (!(ok = warp_wait(&scores, phase))) break;
+        int s = 0;
+        uint32_t stat_phase = 0, turn = 0, items_with_blocks = 0;
+        for (int n = 0;; ++n) {
+            if (!(ok = warp_wait(item_full + (n & 1), n >> 1))) break;
+            const KeyItem& it = info[n & 1];
+            const int first = it.first, kv = it.kv, blocks = it.blocks, last = blocks < 0 ? 0 : it.last[row];
+            warp_arrive(item_empty + (n & 1));
+            if (blocks < 0) break;
+            const TwoRanges seen{first + row, last, 0, 0};
+            // Queries that see all of the warp's keys.
+            const int whole0 = first + (row | 31), whole1 = __reduce_min_sync(kFull, last);
+            const int64_t count = static_cast<int64_t>(blocks) * B.S.group;
+            int i = 0;
+            for (int64_t b = 0; b < count; ++b, ++turn) {
+                const int at = first + i * kTile + half * 64;
+                if (++i == blocks) i = 0;
+                if (!(ok = warp_wait(stat_full + s, stat_phase))) break;
+                if (!(ok = warp_wait(&scores, turn))) break;
+                tc::fence_after();
+                uint32_t p[64], packed[32];
+                tmem_load64(s_at, p);
+                const float4* lse = reinterpret_cast<const float4*>(stats[s][0] + half * 64);
+                const float4* delta = reinterpret_cast<const float4*>(stats[s][1] + half * 64);
+#pragma unroll
+                for (int k = 0; k < 64; k += 4) {
+                    const float4 l = lse[k / 4];
+                    const float2 x = fma2(make_float2(__uint_as_float(p[k]), __uint_as_float(p[k + 1])), c2, make_float2(l.x, l.y));
+                    const float2 y = fma2(make_float2(__uint_as_float(p[k + 2]), __uint_as_float(p[k + 3])), c2, make_float2(l.z, l.w));
+                    p[k] = __float_as_uint(exp2_fast(x.x));
+                    p[k + 1] = __float_as_uint(exp2_fast(x.y));
+                    p[k + 2] = __float_as_uint(exp2_fast(y.x));
+                    p[k + 3] = __float_as_uint(exp2_fast(y.y));
+                }
+                if (at < whole0 || at + 64 > whole1) {
+                    const uint32_t bits[2] = {seen.bits(at), seen.bits(at + 32)};
+#pragma unroll
+                    for (int k = 0; k < 64; ++k)
+                        if (!(bits[k / 32] >> k % 32 & 1)) p[k] = 0u;
+                }
+#pragma unroll
+                for (int k = 0; k < 64; k += 2) packed[k / 2] = pack2<BF16>(__uint_as_float(p[k]), __uint_as_float(p[k + 1]));
+                tmem_store32_begin(s_at, packed);
+                tmem_store_wait();
+                tc::fence_before();
+                warp_arrive(&weights);
+                if (!(ok = warp_wait(&grads, turn))) break;
+                tc::fence_after();
+                uint32_t d[64];
+                tmem_load64(g_at, d);
+#pragma unroll
+                for (int k = 0; k < 64; k += 4) {
+                    const float4 l = delta[k / 4];
+                    float2 x = fma2(make_float2(__uint_as_float(d[k]), __uint_as_float(d[k + 1])), f2, make_float2(l.x, l.y));
+                    float2 y = fma2(make_float2(__uint_as_float(d[k + 2]), __uint_as_float(d[k + 3])), f2, make_float2(l.z, l.w));
+                    x = mul2(x, make_float2(__uint_as_float(p[k]), __uint_as_float(p[k + 1])));
+                    y = mul2(y, make_float2(__uint_as_float(p[k + 2]), __uint_as_float(p[k + 3])));
+                    packed[k / 2] = pack2<BF16>(x.x, x.y);
+                    packed[k / 2 + 1] = pack2<BF16>(y.x, y.y);
+                }
+                tmem_store32_begin(g_at, packed);
+                tmem_store_wait();
+                tc::fence_before();
+                warp_arrive(&slopes);
+                warp_arrive(stat_empty + s);
+                if (++s == kStatStages) s = 0, stat_phase ^= 1;
+            }
+            if (!ok) break;
+            // The first four warps finish dV, the others dK, in the place of V and K.
+            if (count > 0) {
+                if (!(ok = warp_wait(&done, items_with_blocks))) break;
+                ++items_with_blocks;
+            }
+            if (!(ok = warp_wait(&kv_full, n))) break;
             tc::fence_after();
-            uint32_t p[64], packed[32];
-            tmem_load64(s_at, p);
-            const float4* lse = reinterpret_cast<const float4*>(stats[s][0] + half * 64);
-            const float4* delta = reinterpret_cast<const float4*>(stats[s][1] + half * 64);
-#pragma unroll
-            for (int k = 0; k < 64; k += 4) {
-                const float4 l = lse[k / 4];
-                float2 x = fma2(make_float2(__uint_as_float(p[k]), __uint_as_float(p[k + 1])), c2, make_float2(l.x, l.y));
-                float2 y = fma2(make_float2(__uint_as_float(p[k + 2]), __uint_as_float(p[k + 3])), c2, make_float2(l.z, l.w));
-                x.x = exp2_fast(x.x);
-                x.y = exp2_fast(x.y);
-                y.x = exp2_fast(y.x);
-                y.y = exp2_fast(y.y);
-                p[k] = __float_as_uint(x.x);
-                p[k + 1] = __float_as_uint(x.y);
-                p[k + 2] = __float_as_uint(y.x);
-                p[k + 3] = __float_as_uint(y.y);
-            }
-            if (!whole) {
-                const uint32_t bits[2] = {seen.bits(at), seen.bits(at + 32)};
-#pragma unroll
-                for (int k = 0; k < 64; ++k)
-                    if (!(bits[k / 32] >> k % 32 & 1)) p[k] = 0u;
-            }
-#pragma unroll
-            for (int k = 0; k < 64; k += 2) packed[k / 2] = pack2<BF16>(__uint_as_float(p[k]), __uint_as_float(p[k + 1]));
-            tmem_store32_begin(s_at, packed);
-            tmem_store_wait();
-            tc::fence_before();
-            warp_arrive(&weights);
-            if (!(ok = warp_wait(&grads, phase))) break;
-            tc::fence_after();
-            uint32_t d[64];
-            tmem_load64(g_at, d);
-#pragma unroll
-            for (int k = 0; k < 64; k += 4) {
-                const float4 l = delta[k / 4];
-                float2 x = fma2(make_float2(__uint_as_float(d[k]), __uint_as_float(d[k + 1])), f2, make_float2(l.x, l.y));
-                float2 y = fma2(make_float2(__uint_as_float(d[k + 2]), __uint_as_float(d[k + 3])), f2, make_float2(l.z, l.w));
-                x = mul2(x, make_float2(__uint_as_float(p[k]), __uint_as_float(p[k + 1])));
-                y = mul2(y, make_float2(__uint_as_float(p[k + 2]), __uint_as_float(p[k + 3])));
-                packed[k / 2] = pack2<BF16>(x.x, x.y);
-                packed[k / 2 + 1] = pack2<BF16>(y.x, y.y);
-            }
-            tmem_store32_begin(g_at, packed);
-            tmem_store_wait();
-            tc::fence_before();
-            warp_arrive(&slopes);
-            warp_arrive(stat_empty + s);
-            if (++s == kStatStages) s = 0, stat_phase ^= 1;
-        }
-        // The first four warps finish dV, the others dK, in the place of V and K.
-        if (ok && count > 0) ok = warp_wait(&done, 0);
-        tc::fence_after();
-        unsigned char* tile = keys + (half ? 0 : kRows);
-        if (ok) {
+            unsigned char* tile = keys + (half ? 0 : kRows);
             bool finite = true;
-            const float by = half ? B.S.scale / slope_scale<BF16>(B.S) : exp2f(-kPShift<BF16>);
-            if (count > 0) finite = finish_row<D, BF16>(tmem + lanes + 256 + half * D, by, real, tile, row);
+            if (count > 0) finite = finish_row<D, BF16>(tmem + lanes + 256 + half * D, half ? B.S.scale / scale_s : exp2f(-kPShift<BF16>), last > 0, tile, row);
             else zero_row<D>(tile, row);
             for (uint32_t left = __ballot_sync(kFull, !finite); left; left &= left - 1) {
                 const int other = (row & ~31) + __ffs(left) - 1;
@@ -691,13 +825,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                 dkv_again<BF16, D>(B, first + other, kv, half, tile, other);
             }
             fence_to_tma();
-        }
-        named_barrier(1 + half, 128);
-        if (ok && row == 0) {
-#pragma unroll
-            for (int x = 0; x < D / 64; ++x)
-                tma_store(half ? &dkm : &dvm, tc::smem_addr(tile) + x * kBoxBytes, x * 64, kv, first);
-            tma_store_done();
+            tc::fence_before();
+            warp_arrive(staged + half);
         }
     }
     if (!ok && B.S.error) set_error(B.S.error, CB_ERR_TIMEOUT);
@@ -722,10 +851,10 @@ bool launch_typed(const Backward& B, cudaStream_t s) {
         !muon::shared_memory(attention_dkv_kernel<D, BF16>, kKeyShared<D>, dkv_devices))
         return false;
     const int64_t key_tiles = (S.tokens + kTile - 1) / kTile * S.kv_heads, items = work_items(S);
-    if (items > INT32_MAX / 2 || key_tiles > INT32_MAX) return false;
+    if (items > INT32_MAX / 2 || key_tiles > INT32_MAX / 4) return false;
     launch(attention_delta_kernel<D, BF16>, dim3(warp_grid((S.tokens * S.heads * D / 8 + 31) / 32, 152 * 32)), dim3(256), 0, s, B);
-    launch(attention_dkv_kernel<D, BF16>, dim3(static_cast<unsigned>(key_tiles)), dim3(kThreads), kKeyShared<D>, s, qm, km, vm, gm,
-           dkm, dvm, B);
+    launch(attention_dkv_kernel<D, BF16>, dim3(static_cast<unsigned>(std::min<int64_t>(key_tiles, sm_count()))), dim3(kThreads),
+           kKeyShared<D>, s, qm, km, vm, gm, dkm, dvm, B);
     launch(attention_dq_kernel<D, BF16>, dim3(static_cast<unsigned>(std::min<int64_t>(items, sm_count()))), dim3(kThreads),
            kQueryShared<D>, s, qm, km, vm, gm, dqm, B, pairs_heads(S), static_cast<int>(items));
     return true;

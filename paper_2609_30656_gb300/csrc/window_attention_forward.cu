@@ -29,8 +29,8 @@ constexpr int kSoftmaxWarps = 8, kCopyWarp = 8, kMultiplyWarp = 9, kAheadWarp = 
 template <int D> constexpr int kStages = D == 64 ? 4 : 2;  // of the values of a block and the keys of the next
 template <int D> constexpr size_t kShared = 1024 + (3 + 2 * kStages<D>) * kRowsBytes<D>;  // queries, those, output
 // Of the 168 registers that a thread is launched with, the other warps give some to the softmax warps, whose
-// threads hold a row of 128 scores: 256 x 232 + 128 x 40 of the block's 384 x 168.
-constexpr int kMoreRegisters = 232, kFewerRegisters = 40;
+// threads hold a row of 128 scores: 256 x 216 + 128 x 72 of the block's 384 x 168.
+constexpr int kMoreRegisters = 216, kFewerRegisters = 72;
 // How far, in powers of two, weights may lie above 1. A bf16 has fp32's range, and n of them their sums'; fp16 holds
 // weights times 2^6, so that small ones keep their digits, up to 2^14.
 constexpr int kParts = 2;  // in which P goes to the tensor cores
@@ -107,7 +107,7 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
     begin_kernel();
     const int first = static_cast<int>(blockIdx.x), stride = static_cast<int>(gridDim.x);
     bool ok = true;
-    // The n-th item; the caller is done with it at item_done.
+    // The n-th item, for one thread; it is done with it at item_done.
     auto item_of = [&](int n) -> const Item& {
         ok = tc::barrier_wait(tc::smem_addr(item_full + (n & 1)), n >> 1 & 1);
         return info[n & 1];
@@ -179,42 +179,49 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
                 if (queries_issued) tc::barrier_wait(tc::smem_addr(&q_full), (queries_issued - 1) & 1);
             }
         } else if (warp == kMultiplyWarp) {
-            constexpr uint32_t shape_s = mma_shape<BF16>(kTile, kTile, false), shape_o = mma_shape<BF16>(kTile, D, true);
             const bool one = tc::elect();
+            constexpr uint32_t shape_s = mma_shape<BF16>(kTile, kTile, false), shape_o = mma_shape<BF16>(kTile, D, true);
             const uint64_t q0 = tc::operand_k_major(tc::smem_addr(queries));
             const uint64_t k0 = tc::operand_k_major(tc::smem_addr(ring) + kRows), v0 = tc::operand_mn_major(tc::smem_addr(ring), kBoxBytes);
             int s = 0;  // stage of the next copies
             uint32_t phase = 0, p_phase[2] = {0, 0};
+            auto commit = [&](uint64_t* bar) {
+                if (one) tc::mma_commit<1>(tc::smem_addr(bar));
+                __syncwarp();
+            };
             auto multiply_scores = [&](int x, uint32_t stage) {  // S_x = Q_x K^T
                 const uint64_t a = tc::advance(q0, x * kRows), b = tc::advance(k0, stage * 2 * kRows);
+                if (one) {
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t off = k / 4 * kBoxBytes + k % 4 * 32;
-                    tc::mma_f16<1>(tmem + x * 128, tc::advance(a, off), tc::advance(b, off), shape_s, k > 0);
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint32_t off = k / 4 * kBoxBytes + k % 4 * 32;
+                        tc::mma_f16<1>(tmem + x * 128, tc::advance(a, off), tc::advance(b, off), shape_s, k > 0);
+                    }
+                    tc::mma_commit<1>(tc::smem_addr(scores + x));
                 }
-                tc::mma_commit<1>(tc::smem_addr(scores + x));
+                __syncwarp();
             };
             for (int n = 0; n < rounds && ok; ++n) {
-                const Item& it = item_of(n);
-                if (!ok) break;
+                if (!(ok = warp_wait(item_full + (n & 1), n >> 1))) break;
+                const Item& it = info[n & 1];
                 const Blocks blocks(it.sight[0], it.sight[1]);
                 warp_arrive(item_empty + (n & 1));
-                if (!(ok = tc::barrier_wait(tc::smem_addr(&q_full), n & 1))) break;
+                if (!(ok = warp_wait(&q_full, n))) break;
                 bool begun[2] = {false, false}, use[2] = {false, false};
                 if (blocks.count > 0) {
-                    if (!(ok = tc::barrier_wait(tc::smem_addr(full + s), phase))) break;
+                    if (!(ok = warp_wait(full + s, phase))) break;
                     tc::fence_after();
                     const Blocks::Block b = blocks.at(0);
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
                         use[x] = b.use[x];
-                        if (one && use[x]) multiply_scores(x, s);
+                        if (use[x]) multiply_scores(x, s);
                     }
-                    if (one) tc::mma_commit<1>(tc::smem_addr(empty + s));
+                    commit(empty + s);
                     if (++s == S) s = 0, phase ^= 1;
-                    if (!(ok = tc::barrier_wait(tc::smem_addr(full + s), phase))) break;
+                    if (!(ok = warp_wait(full + s, phase))) break;
                 }
-                if (blocks.count <= 1 && one) tc::mma_commit<1>(tc::smem_addr(&q_empty));
+                if (blocks.count <= 1) commit(&q_empty);
                 // Only a few products are queued: what can be found out ahead is, while there are some.
                 bool next0 = blocks.count > 1 && blocks.at(1).use[0], next1 = blocks.count > 1 && blocks.at(1).use[1];
                 for (int i = 0; i < blocks.count; ++i) {
@@ -226,34 +233,31 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
                         if (use[x]) {
 #pragma unroll
                             for (int h = 0; h < kParts; ++h) {
-                                if (!(ok = tc::barrier_wait(tc::smem_addr(part[x] + h), p_phase[x]))) break;
+                                if (!(ok = warp_wait(part[x] + h, p_phase[x]))) break;
                                 tc::fence_after();
                                 if (one)
 #pragma unroll
                                     for (int k = 8 / kParts * h; k < 8 / kParts * (h + 1); ++k)
                                         mma_tmem(tmem + 256 + x * D, tmem + x * 128 + k * 8, tc::advance(v, k * 2048), shape_o,
                                                  begun[x] || k > 0);
+                                __syncwarp();
                             }
                             if (!ok) break;
                             p_phase[x] ^= 1;
                             begun[x] = true;
                         }
                         use[x] = x ? next1 : next0;
-                        if (one) {
-                            if (use[x]) multiply_scores(x, stage);
-                            if (!more) tc::mma_commit<1>(tc::smem_addr(sums + x));
-                        }
+                        if (use[x]) multiply_scores(x, stage);
+                        if (!more) commit(sums + x);
                         if (x == 0) {
                             if (++s == S) s = 0, phase ^= 1;
-                            if (more && !(ok = tc::barrier_wait(tc::smem_addr(full + s), phase))) break;
+                            if (more && !(ok = warp_wait(full + s, phase))) break;
                             next0 = i + 2 < blocks.count;
                         }
                     }
                     if (!ok) break;
-                    if (one) {
-                        tc::mma_commit<1>(tc::smem_addr(empty + stage));
-                        if (i + 2 == blocks.count) tc::mma_commit<1>(tc::smem_addr(&q_empty));  // the last scores
-                    }
+                    commit(empty + stage);
+                    if (i + 2 == blocks.count) commit(&q_empty);  // the last scores
                     if (next0) {
                         const Blocks::Block b = blocks.at(i + 2);
                         next0 = b.use[0];

@@ -164,8 +164,12 @@ __device__ __forceinline__ uint32_t tile_byte(int r, int c) {
 
 // ---------------------------------------------------------------- whole warps
 
-// A whole warp waits, and is together again after it: instructions that want the warp converged may
-// follow (a poll that ends for one lane before another leaves it to the compiler where they meet).
+// A whole warp waits, and is together again after it: instructions that want the warp converged may follow.
+//
+// Products are issued by one lane of a warp that is together before and after (an `if` and __syncwarp): what they take is
+// then in registers that the warp shares; a thread in a branch of its own moves each value there first and could not keep the
+// tensor cores busy. Without the __syncwarp the other lanes would poll the next barrier while the one issues: they
+// can change the shared registers under it, and fall two phases of a barrier behind.
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) {
     return __all_sync(kFull, tc::barrier_wait(tc::smem_addr(bar), parity & 1));
 }
