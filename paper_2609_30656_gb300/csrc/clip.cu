@@ -23,9 +23,10 @@ namespace clip {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPieces = 4;                              // of 8 values a thread has in flight
-constexpr int kChunk = kThreads * kPieces * 8;          // values
-constexpr int kBlocksAnSm = 6;
+template <int DT> constexpr int kPieces = DT == CB_F32 ? 4 : 8;       // of 8 values a thread has in flight: 128 bytes
+template <int DT> constexpr int kChunk = kThreads * kPieces<DT> * 8;  // values: 32 KB
+__host__ __device__ constexpr int chunk_values(int dtype) { return dtype == CB_F32 ? kChunk<CB_F32> : kChunk<CB_BF16>; }
+constexpr int kBlocksAnSm = 4;                           // resident, of both passes: a second round of blocks would leave most SMs idle
 constexpr int64_t kMostValues = int64_t{1} << 40;       // of a tensor
 constexpr int64_t kMostTensors = 1 << 20;
 
@@ -60,12 +61,10 @@ __device__ __forceinline__ int find_entry(const Table<N>& T, int64_t chunk) {
     return lo;
 }
 
-// A thread's pieces of a chunk. Pieces of 8 values begin where the tensor has a multiple of 8 values'
-// bytes (16 or 32) behind it in memory: `lead` values come before the first of them, value by value.
-struct Span {
-    int64_t base;  // the chunk's first piece
-    __device__ __forceinline__ int64_t at(int p) const { return base + (static_cast<int64_t>(p) * kThreads + threadIdx.x) * 8; }
-};
+// Pieces of 8 values begin where the tensor has a multiple of 8 values' bytes (16 or 32) behind it in
+// memory: `lead` values come before the first of them, value by value, as do those behind the last whole piece. A
+// thread has pieces kStep values apart.
+constexpr int kStep = kThreads * 8;
 __device__ __forceinline__ int lead_of(const void* p, int dtype) {
     const uintptr_t a = reinterpret_cast<uintptr_t>(p);
     return dtype == CB_F32 ? static_cast<int>((32 - a % 32) % 32 / 4) : static_cast<int>((16 - a % 16) % 16 / 2);
@@ -75,6 +74,11 @@ __device__ __forceinline__ int64_t count_of(const Entry& e) {
     const int64_t c = *e.count;
     return c < 0 ? 0 : (c < e.n ? c : e.n);
 }
+// Whole pieces of a thread with `left` values from its first one on.
+template <int DT>
+__device__ __forceinline__ int whole_pieces(int64_t left) {
+    return left < 8 ? 0 : static_cast<int>(min64(kPieces<DT>, (left - 8) / kStep + 1));
+}
 __device__ __forceinline__ int64_t place(int64_t i, int64_t cols, int64_t row, bool dense) {
     if (dense) return i;
     const int64_t r = i / cols;
@@ -82,48 +86,57 @@ __device__ __forceinline__ int64_t place(int64_t i, int64_t cols, int64_t row, b
 }
 
 template <int DT>
+__device__ __forceinline__ void piece_squares(const Piece<DT, 8>& x, muon::SquareSum& s) {
+    float f[8], sum = 0.f;
+    widen<DT, 8>(x, f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum = fmaf(f[i], f[i], sum);
+    // In this range neither an overflow nor squares below fp32's normal numbers matter. Else (zeros, an
+    // infinity or a NaN too) by magnitude.
+    if (sum >= 0x1p-110f && sum < 0x1p83f) {
+        s.add_mid(sum);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (f[i] != 0.f) s.add(f[i]);
+    }
+}
+template <int DT>
 __device__ __forceinline__ void chunk_squares(const Entry& e, int64_t chunk, muon::SquareSum& s) {
-    const int64_t n = count_of(e), first = (chunk - e.chunk) * kChunk;
+    const int64_t n = count_of(e), first = (chunk - e.chunk) * kChunk<DT>;
     const bool dense = e.cols >= e.n;
     const char* in = static_cast<const char*>(e.in);
     constexpr int kSize = DT == CB_F32 ? 4 : 2;
     const int lead = lead_of(in, DT);
     if (!dense) {
-        for (int64_t i = first + threadIdx.x; i < first + kChunk && i < n; i += kThreads)
+        for (int64_t i = first + threadIdx.x; i < first + kChunk<DT> && i < n; i += kThreads)
             s.add(muon::load_value(in, place(i, e.cols, e.in_row, false), DT));
         return;
     }
     if (first == 0 && static_cast<int>(threadIdx.x) < lead && static_cast<int64_t>(threadIdx.x) < n)
         s.add(muon::load_value(in, threadIdx.x, DT));
-    const Span S{first + lead};
-    Piece<DT, 8> x[kPieces];
+    const int64_t at = first + lead + threadIdx.x * 8;
+    const int pieces = whole_pieces<DT>(n - at);
+    const char* mine = in + at * kSize;
+    if (pieces == kPieces<DT>) {  // all on their way at once
+        Piece<DT, 8> x[kPieces<DT>];
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p)
-        x[p] = S.at(p) + 8 <= n ? load_piece<DT, 8, false>(in + S.at(p) * kSize) : zero_piece<DT, 8>();
+        for (int p = 0; p < kPieces<DT>; ++p) x[p] = load_piece<DT, 8, false>(mine + p * kStep * kSize);
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p) {
-        float f[8];
-        widen<DT, 8>(x[p], f);
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fmaf(f[i], f[i], sum);
-        // In this range neither an overflow nor squares below fp32's normal numbers matter. Else (zeros, an
-        // infinity or a NaN too) by magnitude.
-        if (sum >= 0x1p-110f && sum < 0x1p83f) {
-            s.add_mid(sum);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (f[i] != 0.f) s.add(f[i]);
-        }
-        if (S.at(p) < n && S.at(p) + 8 > n)  // the values behind the last piece
-            for (int64_t i = S.at(p); i < n; ++i) s.add(muon::load_value(in, i, DT));
+        for (int p = 0; p < kPieces<DT>; ++p) piece_squares<DT>(x[p], s);
+    } else {
+#pragma unroll 1
+        for (int p = 0; p < pieces; ++p) piece_squares<DT>(load_piece<DT, 8, false>(mine + p * kStep * kSize), s);
     }
+    // The values behind the last whole piece, in the tensor's last chunk.
+    const int64_t end = min64(first + lead + kChunk<DT>, n);
+    const int64_t rest = end - (end - lead) % 8 + threadIdx.x;
+    if (end == n && threadIdx.x < 8 && rest < n && rest >= first + lead) s.add(muon::load_value(in, rest, DT));
 }
 
 // First pass: a block's sums of its chunks.
 template <int N>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kBlocksAnSm)
 clip_norm_kernel(const __grid_constant__ Table<N> T, float4* partial) {
     __shared__ float4 joined[kThreads / 32];
     begin_kernel();
@@ -175,44 +188,59 @@ clip_finish_kernel(const float4* partial, int parts, float* norm) {
     if (threadIdx.x == 0) *norm = static_cast<float>(n);
 }
 
-template <int DT, int OT>
+template <int DT>
+__device__ __forceinline__ void store_scaled(const Piece<DT, 8>& x, float f, char* to, int dtype) {
+    float v[8];
+    widen<DT, 8>(x, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= f;
+    if (dtype == CB_F32) store_piece<CB_F32, 8>(to, v);
+    else if (dtype == CB_BF16) store_piece<CB_BF16, 8>(to, v);
+    else store_piece<CB_F16, 8>(to, v);
+}
+template <int DT>
 __device__ __forceinline__ void chunk_scaled(const Entry& e, int64_t chunk, float f) {
-    const int64_t n = count_of(e), first = (chunk - e.chunk) * kChunk;
+    const int64_t n = count_of(e), first = (chunk - e.chunk) * kChunk<DT>;
     const char* in = static_cast<const char*>(e.in);
     char* out = static_cast<char*>(e.out);
-    constexpr int kIn = DT == CB_F32 ? 4 : 2, kOut = OT == CB_F32 ? 4 : 2;
+    const int to = e.out_dtype;
+    constexpr int kIn = DT == CB_F32 ? 4 : 2;
     const int lead = lead_of(in, DT);
     const bool dense = e.cols >= e.n;
-    if (!dense || lead != lead_of(out, OT)) {
-        for (int64_t i = first + threadIdx.x; i < first + kChunk && i < n; i += kThreads)
+    if (!dense || lead != lead_of(out, to)) {
+        for (int64_t i = first + threadIdx.x; i < first + kChunk<DT> && i < n; i += kThreads)
             muon::store_value(out, place(i, e.cols, e.out_row, dense),
-                              muon::load_value(in, place(i, e.cols, e.in_row, dense), DT) * f, OT);
+                              muon::load_value(in, place(i, e.cols, e.in_row, dense), DT) * f, to);
         return;
     }
     if (first == 0 && static_cast<int>(threadIdx.x) < lead && static_cast<int64_t>(threadIdx.x) < n)
-        muon::store_value(out, threadIdx.x, muon::load_value(in, threadIdx.x, DT) * f, OT);
-    const Span S{first + lead};
-    Piece<DT, 8> x[kPieces];
+        muon::store_value(out, threadIdx.x, muon::load_value(in, threadIdx.x, DT) * f, to);
+    const int64_t at = first + lead + threadIdx.x * 8;
+    const int pieces = whole_pieces<DT>(n - at);
+    const char* mine = in + at * kIn;
+    const int size = to == CB_F32 ? 4 : 2;
+    char* target = out + at * size;
+    if (pieces == kPieces<DT>) {  // all on their way at once
+        Piece<DT, 8> x[kPieces<DT>];
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p)
-        if (S.at(p) + 8 <= n) x[p] = load_piece<DT, 8, false>(in + S.at(p) * kIn);
+        for (int p = 0; p < kPieces<DT>; ++p) x[p] = load_piece<DT, 8, false>(mine + p * kStep * kIn);
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p) {
-        if (S.at(p) + 8 <= n) {
-            float v[8];
-            widen<DT, 8>(x[p], v);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] *= f;
-            store_piece<OT, 8>(out + S.at(p) * kOut, v);
-        } else {
-            for (int64_t i = S.at(p); i < n; ++i) muon::store_value(out, i, muon::load_value(in, i, DT) * f, OT);
-        }
+        for (int p = 0; p < kPieces<DT>; ++p) store_scaled<DT>(x[p], f, target + p * kStep * size, to);
+    } else {
+#pragma unroll 1
+        for (int p = 0; p < pieces; ++p)
+            store_scaled<DT>(load_piece<DT, 8, false>(mine + p * kStep * kIn), f, target + p * kStep * size, to);
     }
+    // The values behind the last whole piece, in the tensor's last chunk.
+    const int64_t end = min64(first + lead + kChunk<DT>, n);
+    const int64_t rest = end - (end - lead) % 8 + threadIdx.x;
+    if (end == n && threadIdx.x < 8 && rest < n && rest >= first + lead)
+        muon::store_value(out, rest, muon::load_value(in, rest, DT) * f, to);
 }
 
 // Second pass: the norm, the factor, and the values times it.
 template <int N>
-__global__ void __launch_bounds__(kThreads, 4)
+__global__ void __launch_bounds__(kThreads, kBlocksAnSm)
 clip_scale_kernel(const __grid_constant__ Table<N> T, const float4* partial, int parts, float max_norm, float eps,
                   float* norm) {
     begin_kernel();
@@ -225,17 +253,9 @@ clip_scale_kernel(const __grid_constant__ Table<N> T, const float4* partial, int
         const int64_t c = T.chunks - 1 - k;
         const Entry& e = T.e[find_entry(T, c)];
         if (f == 1.f && e.in == e.out) continue;
-        switch (e.in_dtype * 3 + e.out_dtype) {
-            case CB_F32 * 3 + CB_F32: chunk_scaled<CB_F32, CB_F32>(e, c, f); break;
-            case CB_F32 * 3 + CB_F16: chunk_scaled<CB_F32, CB_F16>(e, c, f); break;
-            case CB_F32 * 3 + CB_BF16: chunk_scaled<CB_F32, CB_BF16>(e, c, f); break;
-            case CB_F16 * 3 + CB_F32: chunk_scaled<CB_F16, CB_F32>(e, c, f); break;
-            case CB_F16 * 3 + CB_F16: chunk_scaled<CB_F16, CB_F16>(e, c, f); break;
-            case CB_F16 * 3 + CB_BF16: chunk_scaled<CB_F16, CB_BF16>(e, c, f); break;
-            case CB_BF16 * 3 + CB_F32: chunk_scaled<CB_BF16, CB_F32>(e, c, f); break;
-            case CB_BF16 * 3 + CB_F16: chunk_scaled<CB_BF16, CB_F16>(e, c, f); break;
-            default: chunk_scaled<CB_BF16, CB_BF16>(e, c, f); break;
-        }
+        if (e.in_dtype == CB_F32) chunk_scaled<CB_F32>(e, c, f);
+        else if (e.in_dtype == CB_BF16) chunk_scaled<CB_BF16>(e, c, f);
+        else chunk_scaled<CB_F16>(e, c, f);
     }
 }
 
@@ -326,7 +346,7 @@ void launch_pass(const Entry* e, int tensors, const float4* partial, int at, int
     for (int i = 0; i < tensors; ++i) {
         T.e[i] = e[i];
         T.e[i].chunk = T.chunks;
-        T.chunks += (e[i].n + kChunk - 1) / kChunk;
+        T.chunks += (e[i].n + chunk_values(e[i].in_dtype) - 1) / chunk_values(e[i].in_dtype);
     }
     const int grid = grid_blocks(T.chunks);
     if (blocks) *blocks = grid;

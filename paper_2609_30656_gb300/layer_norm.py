@@ -67,19 +67,25 @@ def _as_rows(t: torch.Tensor):
     return (t, step) if step >= shape[-1] else None
 
 
+# One kernel or two are launched, so on small batches the binding's own time is the call's: contiguous
+# tensors, the usual ones, are told apart first.
 def _param(t: torch.Tensor | None, what: str, dim: int, index: int):
     if t is None:
         return None, 0
-    if t.get_device() != index or t.shape != (dim,) or (dim > 1 and t.stride(0) != 1):
+    kind = tbe._DTYPES.get(t.dtype)
+    if t.get_device() != index or t.dim() != 1 or t.numel() != dim or not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous, [dim], on the device of x")
-    return t.data_ptr(), _dtype(t, what)
+    if kind is None:
+        raise ValueError(f"unsupported {what} dtype {t.dtype}")
+    return t.data_ptr(), kind
 
 
 def _output(like: torch.Tensor, out: torch.Tensor | None, out_dtype: torch.dtype | None, index: int, what: str):
     """(tensor, row stride) of a result in the shape of `like`."""
+    shape = like.shape
     if out is None:
-        return torch.empty(like.shape, dtype=out_dtype or like.dtype, device=like.device), like.shape[-1]
-    if out.get_device() != index or out.shape != like.shape:
+        return torch.empty(shape, dtype=out_dtype or like.dtype, device=like.device), shape[-1]
+    if out.get_device() != index or out.shape != shape:
         raise ValueError(f"{what} must have x's shape and device")
     if out_dtype is not None and out.dtype != out_dtype:
         raise TypeError(f"{what} must be {out_dtype}")
@@ -102,19 +108,25 @@ def layer_norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.
     if index < 0 or x.dim() < 1:
         raise ValueError("x must be a CUDA tensor [..., dim]")
     kind = _dtype(x, "x")
-    dim = x.shape[-1]
+    shape = x.shape
+    dim = shape[-1]
     w, w_kind = _param(weight, "weight", dim, index)
     b, b_kind = _param(bias, "bias", dim, index)
+    fresh = out is None
     out, out_step = _output(x, out, out_dtype, index, "out")
     out_kind = _dtype(out, "output")
-    if out.data_ptr() == x.data_ptr() and x.numel() and (out.dtype != x.dtype or out.stride() != x.stride()):
+    if not fresh and out.data_ptr() == x.data_ptr() and x.numel() and (out.dtype != x.dtype or out.stride() != x.stride()):
         raise ValueError("out may be x, but not share its memory in another type or layout")
-    rows_of = _as_rows(x)
-    x, step = rows_of if rows_of is not None else (x.contiguous(), dim)
+    step = dim
+    if not x.is_contiguous():
+        rows_of = _as_rows(x)
+        x, step = rows_of if rows_of is not None else (x.contiguous(), dim)
     rows = x.numel() // dim if dim else 0
     mean = rstd = None
     if stats:
-        mean, rstd = torch.empty((2, *x.shape[:-1]), dtype=torch.float32, device=x.device).unbind(0)
+        device = x.device
+        mean = torch.empty(shape[:-1], dtype=torch.float32, device=device)
+        rstd = torch.empty(shape[:-1], dtype=torch.float32, device=device)
         if not dim:
             mean.zero_()
             rstd.fill_(float("inf") if eps == 0 else eps ** -0.5)
@@ -147,15 +159,19 @@ def layer_norm_backward(grad_out: torch.Tensor, x: torch.Tensor, mean: torch.Ten
         if t.get_device() != index or t.dtype != torch.float32 or t.shape != x.shape[:-1]:
             raise ValueError(f"{what} must be fp32, x.shape[:-1], on the device of x")
     w, w_kind = _param(weight, "weight", dim, index)
+    given = out is not None
     out, out_step = _output(x, out, out_dtype, index, "out")
     out_kind = _dtype(out, "gradient")
-    for t in (x, grad_out):
+    for t in (x, grad_out) if given else ():
         if out.data_ptr() == t.data_ptr() and t.numel() and (out.dtype != t.dtype or out.stride() != t.stride()):
             raise ValueError("out may be grad_out or x, but not share its memory in another type or layout")
-    rows_of = _as_rows(x)
-    x, step = rows_of if rows_of is not None else (x.contiguous(), dim)
-    rows_of = _as_rows(grad_out)
-    go, go_step = rows_of if rows_of is not None else (grad_out.contiguous(), dim)
+    go, go_step, step = grad_out, dim, dim
+    if not x.is_contiguous():
+        rows_of = _as_rows(x)
+        x, step = rows_of if rows_of is not None else (x.contiguous(), dim)
+    if not go.is_contiguous():
+        rows_of = _as_rows(go)
+        go, go_step = rows_of if rows_of is not None else (go.contiguous(), dim)
     mean, rstd = mean.contiguous(), rstd.contiguous()
     rows = x.numel() // dim if dim else 0
     dweight = torch.empty(dim, dtype=torch.float32, device=x.device) if weight is not None else None
