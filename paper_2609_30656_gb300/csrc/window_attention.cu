@@ -151,6 +151,22 @@ Shape shape(int dtype, int64_t tokens, int32_t heads, int32_t kv_heads, int32_t 
     S.error = error;
     return S;
 }
+// The backward pass's workspace: bytes before each part of it, and all.
+struct Layout {
+    size_t delta, words, list, split, sums, bytes;
+    int64_t room;
+};
+Layout layout(int64_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, int64_t window, int64_t sinks) {
+    Layout L;
+    L.room = parts_room(tokens, kv_heads, dim, window, sinks);
+    L.delta = 2 * rows_bytes(tokens);
+    L.words = L.delta + rows_bytes(tokens * heads);
+    L.list = L.words + 256;
+    L.split = L.list + rows_bytes(2 * L.room);
+    L.sums = L.split + (L.room ? rows_bytes(tiles_of(static_cast<int>(tokens))) : 0);
+    L.bytes = L.sums + static_cast<size_t>(parts_bytes(L.room, kv_heads, dim));
+    return L;
+}
 bool workspace_ok(const void* w, int64_t bytes, int64_t need) {
     return w && reinterpret_cast<uintptr_t>(w) % 256 == 0 && bytes >= need;
 }
@@ -210,10 +226,13 @@ bool tensor_core_rows(const Shape& S, const Heads& h, int heads) {
 }  // namespace attention
 }  // namespace cbtbe
 
-extern "C" int64_t cb_attention_workspace_bytes(int64_t tokens, int32_t heads, int backward) {
+extern "C" int64_t cb_attention_workspace_bytes(int64_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, int64_t window,
+                                                int64_t sinks, int backward) {
     using namespace cbtbe::attention;
-    if (tokens <= 0 || tokens > kMostTokens || heads < 1) return 0;
-    return static_cast<int64_t>(2 * rows_bytes(tokens) + (backward ? rows_bytes(tokens * heads) + 256 + rows_bytes(tiles_of(static_cast<int>(tokens))) : 0));
+    if (tokens <= 0 || tokens > kMostTokens || heads < 1 || heads > 65535 || kv_heads < 1 || dim < 1 || dim > kMaxDim ||
+        window < 1 || sinks < 0)
+        return 0;
+    return static_cast<int64_t>(backward ? layout(tokens, heads, kv_heads, dim, window, sinks).bytes : 2 * rows_bytes(tokens));
 }
 
 extern "C" cb_status cb_attention_forward(const void* q, const void* k, const void* v, cb_dtype dtype, int64_t tokens,
@@ -236,7 +255,7 @@ extern "C" cb_status cb_attention_forward(const void* q, const void* k, const vo
     if (!heads_ok(F.S, F.q, heads, false) || !heads_ok(F.S, F.k, kv_heads, false) || !heads_ok(F.S, F.v, kv_heads, false) ||
         !heads_ok(F.S, F.out, heads, true) || reinterpret_cast<uintptr_t>(lse) % 4)
         return CB_ERR_INVALID_ARG;
-    if (!workspace_ok(workspace, workspace_bytes, cb_attention_workspace_bytes(tokens, heads, 0))) return CB_ERR_CAPACITY;
+    if (!workspace_ok(workspace, workspace_bytes, cb_attention_workspace_bytes(tokens, heads, kv_heads, dim, window, sinks, 0))) return CB_ERR_CAPACITY;
     set_rows(F.S, workspace, nullptr, stream);
     bool ok = true;
     if (tensor_core_rows(F.S, F.q, heads) && tensor_core_rows(F.S, F.k, kv_heads) && tensor_core_rows(F.S, F.v, kv_heads) &&
@@ -278,10 +297,13 @@ extern "C" cb_status cb_attention_backward(const void* grad_out, const void* q, 
         !heads_ok(B.S, B.dk, kv_heads, true) || !heads_ok(B.S, B.dv, kv_heads, true) || !lse ||
         reinterpret_cast<uintptr_t>(lse) % 4)
         return CB_ERR_INVALID_ARG;
-    if (!workspace_ok(workspace, workspace_bytes, cb_attention_workspace_bytes(tokens, heads, 1))) return CB_ERR_CAPACITY;
-    B.delta = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * rows_bytes(tokens));
-    uint32_t* words = reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(B.delta) + rows_bytes(tokens * heads));
-    B.order = {reinterpret_cast<int32_t*>(words + 1), words + 2, reinterpret_cast<int32_t*>(words + 64)};
+    if (!workspace_ok(workspace, workspace_bytes, cb_attention_workspace_bytes(tokens, heads, kv_heads, dim, window, sinks, 1))) return CB_ERR_CAPACITY;
+    const Layout L = layout(tokens, heads, kv_heads, dim, window, sinks);
+    char* base = static_cast<char*>(workspace);
+    B.delta = reinterpret_cast<float*>(base + L.delta);
+    uint32_t* words = reinterpret_cast<uint32_t*>(base + L.words);
+    B.order = {reinterpret_cast<int32_t*>(words + 1), words + 2, static_cast<int32_t>(L.room), reinterpret_cast<int2*>(base + L.list),
+               reinterpret_cast<int32_t*>(base + L.split), reinterpret_cast<float*>(base + L.sums)};
     set_rows(B.S, workspace, words, stream);
     bool ok = true;
     bool fast = true;

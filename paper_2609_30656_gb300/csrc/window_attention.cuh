@@ -45,12 +45,14 @@ struct Forward {
     Heads q, k, v, out;
     float* lse;  // [heads, tokens], or null
 };
-// The order in which tiles of keys are taken: those that the most queries see, then the others. (Their results do not
-// depend on it.)
+// How the tiles of keys are taken: those in parts first, then the others. (Results do not depend on who takes what.)
 struct Order {
-    int32_t* long_tiles;  // how many, and next item to take: 0 before
-    uint32_t* next;
-    int32_t* tiles;       // [tiles of 128 tokens]
+    int32_t* parts;       // how many parts there are, and
+    uint32_t* next;       // the next item to take: 0 before
+    int32_t room;         // parts there is room for; 0: no tile is taken in parts
+    int2* list;           // [room] tile (-1: none) and which of its parts
+    int32_t* split;       // [tiles of 128 tokens] parts of each, 0 for one taken whole
+    float* sums;          // [room][kv_heads][2][128][64 or 128] dV and dK of each
 };
 struct Backward {
     Shape S;
@@ -190,6 +192,8 @@ inline size_t rows_bytes(int64_t tokens) { return static_cast<size_t>((tokens * 
 // bf16, rows of a multiple of 8 and at most 128 values, addresses and strides in multiples of 16 bytes.
 bool tensor_core_rows(const Shape& S, const Heads& h, int heads);
 int sm_count();  // of the current device
+int64_t parts_room(int64_t tokens, int32_t kv_heads, int32_t dim, int64_t window, int64_t sinks);
+int64_t parts_bytes(int64_t room, int32_t kv_heads, int32_t dim);
 bool launch_forward(const Forward& F, cudaStream_t s);
 bool launch_backward(const Backward& B, cudaStream_t s);
 

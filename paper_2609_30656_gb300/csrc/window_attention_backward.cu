@@ -44,9 +44,14 @@ __device__ __forceinline__ int seen_until(const Shape& S, int64_t j) {
     if (j >= S.tokens || S.end[j] <= j) return 0;
     return static_cast<int>(j - S.start[j] < S.sinks ? S.end[j] : min64(S.end[j], j + S.window));
 }
-// Seen by more than three windows of queries, or a few thousand.
-__device__ __forceinline__ bool is_long(const Shape& S, int first, int until) {
-    return until - first > max64(3 * S.window, 0) + 2048;
+// A tile of keys whose queries go far beyond their windows (a session's first keys are seen to its end) is
+// taken in parts of so many blocks of queries, whose sums are joined by attention_parts_kernel.
+__host__ __device__ __forceinline__ int part_blocks(int64_t window) {
+    return static_cast<int>(max64(16, min64(window, int64_t{1} << 30) / kTile + 2));
+}
+__device__ __forceinline__ int parts_of(const Shape& S, int blocks) {
+    const int per = part_blocks(S.window);
+    return blocks <= 2 * per ? 0 : (blocks + per - 1) / per;
 }
 
 // delta, and the largest |grad_out|: 16 bytes a lane, D / 8 lanes a row.
@@ -75,15 +80,26 @@ __global__ void __launch_bounds__(256) attention_delta_kernel(const Backward B) 
         for (int off = kLanes / 2; off >= 1; off >>= 1) sum += __shfl_xor_sync(kFull, sum, off);
         if (i < rows && lane % kLanes == 0) B.delta[h * S.tokens + t] = sum;
     }
-    // Tiles of keys that many more queries see than their windows say (a session's first tokens): listed, to be taken first.
-    const int tiles = tiles_of(static_cast<int>(S.tokens));
+    // Tiles of keys that are taken in parts, where there is room for their sums: which part of which tile each is.
+    const int tiles = B.order.room ? tiles_of(static_cast<int>(S.tokens)) : 0;
     for (int64_t w = warp_id_global(); w < tiles; w += warps_in_grid()) {
         const int from = static_cast<int>(w) * kTile;
         int until = 0;
 #pragma unroll
         for (int k = 0; k < kTile / 32; ++k) until = max(until, seen_until(S, from + k * 32 + lane));
         until = __reduce_max_sync(kFull, until);
-        if (lane == 0 && is_long(S, from, until)) B.order.tiles[atomicAdd(B.order.long_tiles, 1)] = static_cast<int>(w);
+        int parts = parts_of(S, tiles_of(max(until - from, 0))), slot = 0;
+        if (lane == 0 && parts) {
+            slot = atomicAdd(B.order.parts, parts);
+            if (slot + parts > B.order.room) {  // the tile in one piece; the places stay empty
+                for (int p = slot; p < B.order.room; ++p) B.order.list[p] = make_int2(-1, 0);
+                parts = 0;
+            }
+        }
+        slot = __shfl_sync(kFull, slot, 0);
+        parts = __shfl_sync(kFull, parts, 0);
+        for (int p = lane; p < parts; p += 32) B.order.list[slot + p] = make_int2(static_cast<int>(w), p);
+        if (lane == 0) B.order.split[w] = parts;
     }
     if constexpr (!BF16) {
         const uint32_t most = __reduce_max_sync(kFull, __float_as_uint(largest));
@@ -485,7 +501,8 @@ template <int D> constexpr size_t kKeyShared = 1024 + (2 + kKeyStages) * kRowsBy
 // A tile of keys and the queries that see one of them.
 struct KeyItem {
     int first, kv;    // token, head
-    int blocks;       // of 128 queries from `first` on, for each head that shares the keys; -1: no more items
+    int from, blocks; // of 128 queries, from token `from` on, for each head that shares the keys; -1: no more items
+    int place;        // -1, or the part's in the list
     int last[kTile];  // behind the last token that sees the key, 0 for one of no session
 };
 
@@ -544,12 +561,13 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
     if (warp >= kWorkWarps) {
         registers_down<kKeyFewer>();
         if (warp == kAheadWarp) {  // the next item, and the results of the one before
-            const int kv_heads = B.S.kv_heads, tiles = tiles_of(static_cast<int>(B.S.tokens)), longer = *B.order.long_tiles * kv_heads;
-            const int64_t all = static_cast<int64_t>(longer) + static_cast<int64_t>(tiles) * kv_heads;
+            const int kv_heads = B.S.kv_heads, tiles = tiles_of(static_cast<int>(B.S.tokens));
+            const int64_t listed = B.order.room ? static_cast<int64_t>(min(*B.order.parts, B.order.room)) * kv_heads : 0;
+            const int64_t all = listed + static_cast<int64_t>(tiles) * kv_heads;
             auto store = [&](int n) {  // of the n-th item
                 const int first = info[n & 1].first, kv = info[n & 1].kv;
                 if (!(ok = warp_wait(staged, n) && warp_wait(staged + 1, n))) return;
-                if (lane == 0) {
+                if (lane == 0 && info[n & 1].place < 0) {
 #pragma unroll
                     for (int x = 0; x < D / 64; ++x) {
                         tma_store(&dkm, tc::smem_addr(keys) + x * kBoxBytes, x * 64, kv, first);
@@ -562,16 +580,27 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                 warp_arrive(item_empty + (n & 1));
             };
             for (int n = 0;; ++n) {
-                int first = 0, kv = 0, until = 0, last[kTile / 32];
+                int first = 0, kv = 0, until = 0, part = 0, place = -1, last[kTile / 32];
                 bool some = false;
                 while (!some) {
                     unsigned w = 0;
                     if (lane == 0) w = atomicAdd(B.order.next, 1u);
                     w = __shfl_sync(kFull, w, 0);
                     if (w >= all) break;
-                    const int index = w < static_cast<unsigned>(longer) ? static_cast<int>(w) : static_cast<int>(w) - longer;
-                    const int tile = w < static_cast<unsigned>(longer) ? B.order.tiles[index / kv_heads] : index / kv_heads;
-                    kv = index % kv_heads;
+                    const int64_t index = w < listed ? w : w - listed;
+                    int tile = static_cast<int>(index / kv_heads);
+                    kv = static_cast<int>(index % kv_heads);
+                    place = -1;
+                    if (w < listed) {
+                        place = tile;
+                        const int2 entry = B.order.list[place];
+                        tile = entry.x;
+                        part = entry.y;
+                        some = tile >= 0;
+                    } else {
+                        some = !B.order.room || B.order.split[tile] == 0;
+                    }
+                    if (!some) continue;
                     first = tile * kTile;
                     until = 0;
 #pragma unroll
@@ -580,7 +609,6 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                         until = max(until, last[k]);
                     }
                     until = __reduce_max_sync(kFull, until);
-                    some = w < static_cast<unsigned>(longer) || !is_long(B.S, first, until);
                 }
                 // The place of the item before the last one: its results are stored first.
                 if (n >= 2) {
@@ -592,7 +620,10 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                 if (lane == 0) {
                     it.first = first;
                     it.kv = kv;
-                    it.blocks = some ? tiles_of(max(until - first, 0)) : -1;
+                    it.place = place;
+                    const int blocks = tiles_of(max(until - first, 0)), per = part_blocks(B.S.window);
+                    it.from = place < 0 ? first : first + part * per * kTile;
+                    it.blocks = !some ? -1 : (place < 0 ? blocks : max(min(per, blocks - part * per), 0));
                 }
                 if (some)
 #pragma unroll
@@ -610,7 +641,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
             for (;; ++n) {
                 if (!wait(item_full + (n & 1), n >> 1)) break;
                 const KeyItem& it = info[n & 1];
-                const int first = it.first, kv = it.kv, blocks = it.blocks;
+                const int first = it.first, from = it.from, kv = it.kv, blocks = it.blocks;
                 tc::barrier_arrive(tc::smem_addr(item_empty + (n & 1)));
                 if (blocks < 0) break;
                 int64_t m = 0;
@@ -619,7 +650,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                     const int b = static_cast<int>(m >> 1), h = b / blocks, i = b - h * blocks;
                     tc::barrier_expect(tc::smem_addr(full + s), kRows);
                     load_tile<D>(tc::smem_addr(ring) + s * kRows, m & 1 ? &gm : &qm, tc::smem_addr(full + s), kv * B.S.group + h,
-                                 first + i * kTile);
+                                 from + i * kTile);
                     ++m;
                     ++issued;
                     if (++s == S) s = 0, phase ^= 1;
@@ -647,7 +678,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
             uint32_t phase = 0;
             for (int n = 0; ok; ++n) {
                 if (!(ok = warp_wait(item_full + (n & 1), n >> 1))) break;
-                const int first = info[n & 1].first, kv = info[n & 1].kv, blocks = info[n & 1].blocks;
+                const int from = info[n & 1].from, kv = info[n & 1].kv, blocks = info[n & 1].blocks;
                 warp_arrive(item_empty + (n & 1));
                 if (blocks < 0) break;
                 for (int h = 0; h < B.S.group && ok; ++h) {
@@ -656,7 +687,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                         if (!(ok = warp_wait(stat_empty + s, phase ^ 1))) break;
 #pragma unroll
                         for (int k = 0; k < kTile / 32; ++k) {
-                            const int64_t t = first + static_cast<int64_t>(i) * kTile + k * 32 + lane;
+                            const int64_t t = from + static_cast<int64_t>(i) * kTile + k * 32 + lane;
                             stats[s][0][k * 32 + lane] = t < B.S.tokens ? kPShift<BF16> - B.lse[row + t] * kLog2e : 0.f;
                             stats[s][1][k * 32 + lane] = t < B.S.tokens ? -B.delta[row + t] * f : 0.f;
                         }
@@ -746,7 +777,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
         for (int n = 0;; ++n) {
             if (!(ok = warp_wait(item_full + (n & 1), n >> 1))) break;
             const KeyItem& it = info[n & 1];
-            const int first = it.first, kv = it.kv, blocks = it.blocks, last = blocks < 0 ? 0 : it.last[row];
+            const int first = it.first, from = it.from, kv = it.kv, blocks = it.blocks, place = it.place, last = blocks < 0 ? 0 : it.last[row];
             warp_arrive(item_empty + (n & 1));
             if (blocks < 0) break;
             const TwoRanges seen{first + row, last, 0, 0};
@@ -755,7 +786,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
             const int64_t count = static_cast<int64_t>(blocks) * B.S.group;
             int i = 0;
             for (int64_t b = 0; b < count; ++b, ++turn) {
-                const int at = first + i * kTile + half * 64;
+                const int at = from + i * kTile + half * 64;
                 if (++i == blocks) i = 0;
                 if (!(ok = warp_wait(stat_full + s, stat_phase))) break;
                 if (!(ok = warp_wait(&scores, turn))) break;
@@ -816,6 +847,19 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
             if (!(ok = warp_wait(&kv_full, n))) break;
             tc::fence_after();
             unsigned char* tile = keys + (half ? 0 : kRows);
+            if (place >= 0) {  // sums in fp32, joined by another kernel
+                float* to = B.order.sums + ((static_cast<int64_t>(place) * B.S.kv_heads + kv) * 2 + half) * kTile * D + row * D;
+#pragma unroll 1
+                for (int d = 0; d < D; d += 32) {
+                    float o[32] = {};
+                    if (count > 0) tc::tmem_load32(tmem + lanes + 256 + half * D + d, o);
+#pragma unroll
+                    for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(to + d + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+                }
+                tc::fence_before();
+                warp_arrive(staged + half);
+                continue;
+            }
             bool finite = true;
             if (count > 0) finite = finish_row<D, BF16>(tmem + lanes + 256 + half * D, half ? B.S.scale / scale_s : exp2f(-kPShift<BF16>), last > 0, tile, row);
             else zero_row<D>(tile, row);
@@ -837,6 +881,45 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
     if (warp == kMultiplyWarp) tc::tmem_free<1>(tmem, 512);
 }
 
+// The sums of a tile's parts, in order: a block for a tile and head, a warp for a row at a time.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256) attention_parts_kernel(const Backward B) {
+    constexpr int DT = BF16 ? CB_BF16 : CB_F16, N = D / 32;
+    begin_kernel();
+    const int listed = min(*B.order.parts, B.order.room), lane = threadIdx.x & 31;
+    const float by[2] = {exp2f(-kPShift<BF16>), B.S.scale / slope_scale<BF16>(B.S)};
+    for (int64_t w = blockIdx.x; w < static_cast<int64_t>(listed) * B.S.kv_heads; w += gridDim.x) {
+        const int place = static_cast<int>(w / B.S.kv_heads), kv = static_cast<int>(w % B.S.kv_heads);
+        const int2 entry = B.order.list[place];
+        if (entry.x < 0 || entry.y != 0) continue;
+        const int parts = B.order.split[entry.x];
+        for (int row = threadIdx.x / 32; row < kTile; row += 8) {
+            const int64_t j = static_cast<int64_t>(entry.x) * kTile + row;
+            if (j >= B.S.tokens) break;
+            const bool real = B.S.end[j] > j;
+            float v[2][kLaneValues] = {};
+            bool finite = true;
+            for (int p = 0; p < parts && real; ++p)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float* from = B.order.sums + (((static_cast<int64_t>(place) + p) * B.S.kv_heads + kv) * 2 + h) * kTile * D + row * D;
+#pragma unroll
+                    for (int i = 0; i < N; ++i) v[h][i] += __ldcg(from + lane + 32 * i);
+                }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    v[h][i] *= by[h];
+                    finite &= fabsf(v[h][i]) < INFINITY || lane + 32 * i >= B.S.dim;
+                }
+            if (!__all_sync(kFull, finite)) row_dkv<DT>(B, j, kv, v[1], v[0]);
+            store_row<DT>(B.dv, j, kv, B.S.dim, v[0]);
+            store_row<DT>(B.dk, j, kv, B.S.dim, v[1]);
+        }
+    }
+}
+
 template <int D, bool BF16>
 bool launch_typed(const Backward& B, cudaStream_t s) {
     const Shape& S = B.S;
@@ -855,12 +938,27 @@ bool launch_typed(const Backward& B, cudaStream_t s) {
     launch(attention_delta_kernel<D, BF16>, dim3(warp_grid((S.tokens * S.heads * D / 8 + 31) / 32, 152 * 32)), dim3(256), 0, s, B);
     launch(attention_dkv_kernel<D, BF16>, dim3(static_cast<unsigned>(std::min<int64_t>(key_tiles, sm_count()))), dim3(kThreads),
            kKeyShared<D>, s, qm, km, vm, gm, dkm, dvm, B);
+    if (B.order.room)
+        launch(attention_parts_kernel<D, BF16>, dim3(static_cast<unsigned>(std::min<int64_t>(static_cast<int64_t>(B.order.room) * S.kv_heads, 8 * sm_count()))),
+               dim3(256), 0, s, B);
     launch(attention_dq_kernel<D, BF16>, dim3(static_cast<unsigned>(std::min<int64_t>(items, sm_count()))), dim3(kThreads),
            kQueryShared<D>, s, qm, km, vm, gm, dqm, B, pairs_heads(S), static_cast<int>(items));
     return true;
 }
 
 }  // namespace
+
+int64_t parts_room(int64_t tokens, int32_t kv_heads, int32_t dim, int64_t window, int64_t sinks) {
+    const int64_t tiles = (tokens + kTile - 1) / kTile, per = part_blocks(window);
+    if (sinks == 0 || dim > 128 || tiles <= 2 * per) return 0;
+    // A session's first keys lie in at most so many tiles, each seen by its blocks, two per - 1 of them or more a part.
+    const int64_t most = (std::min(sinks, tokens) / kTile + 2) * ((tiles + per - 1) / per * 2);
+    const int64_t bytes = static_cast<int64_t>(kv_heads) * 2 * kTile * (dim <= 64 ? 64 : 128) * 4;
+    return std::min(most, std::max<int64_t>((int64_t{256} << 20) / bytes, 1));
+}
+int64_t parts_bytes(int64_t room, int32_t kv_heads, int32_t dim) {
+    return room * kv_heads * 2 * kTile * (dim <= 64 ? 64 : 128) * 4;
+}
 
 bool launch_backward(const Backward& B, cudaStream_t s) {
     if (B.S.dtype == CB_BF16) return B.S.dim <= 64 ? launch_typed<64, true>(B, s) : launch_typed<128, true>(B, s);

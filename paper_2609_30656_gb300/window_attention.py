@@ -42,7 +42,7 @@ def _library() -> ctypes.CDLL:
                                               p, p, p, *[i64] * 6, p, i64, p, p]
         lib.cb_attention_step.argtypes = [p, p, p, c, i64, i64, i32, i32, i32, *[i64] * 8, p, c, i64, i64, f32, p, i64, i64,
                                           p, i64, p, p]
-        lib.cb_attention_workspace_bytes.argtypes = [i64, i32, c]
+        lib.cb_attention_workspace_bytes.argtypes = [i64, i32, i32, i32, i64, i64, c]
         lib.cb_attention_step_workspace_bytes.argtypes = [i64, i32, i32, i32, i64, i64, i64]
         for name in EXPORTS:
             getattr(lib, name).restype = i64 if name.endswith("bytes") else c
@@ -138,7 +138,7 @@ def window_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets:
         if _rows(out) is not out:
             to = torch.empty(out.shape, dtype=out.dtype, device=out.device)
         with tbe._OnDevice(index):
-            nbytes = lib.cb_attention_workspace_bytes(tokens, heads, 0)
+            nbytes = lib.cb_attention_workspace_bytes(tokens, heads, kv_heads, dim, window, sinks, 0)
             work = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
             status = lib.cb_attention_forward(
                 q.data_ptr(), k.data_ptr(), v.data_ptr(), kind, tokens, heads, kv_heads, dim, *_strides(q), *_strides(k),
@@ -181,7 +181,7 @@ def window_attention_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torch.
         ins = [_rows(t) for t in (grad_out, q, k, v, out)]
         lse = lse.contiguous()
         with tbe._OnDevice(index):
-            nbytes = lib.cb_attention_workspace_bytes(tokens, heads, 1)
+            nbytes = lib.cb_attention_workspace_bytes(tokens, heads, kv_heads, dim, window, sinks, 1)
             work = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
             status = lib.cb_attention_backward(
                 *[t.data_ptr() for t in ins], lse.data_ptr(), kind, tokens, heads, kv_heads, dim,
