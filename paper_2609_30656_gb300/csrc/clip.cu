@@ -26,7 +26,8 @@ constexpr int kThreads = 256;
 template <int DT> constexpr int kPieces = DT == CB_F32 ? 4 : 8;       // of 8 values a thread has in flight: 128 bytes
 template <int DT> constexpr int kChunk = kThreads * kPieces<DT> * 8;  // values: 32 KB
 __host__ __device__ constexpr int chunk_values(int dtype) { return dtype == CB_F32 ? kChunk<CB_F32> : kChunk<CB_BF16>; }
-constexpr int kBlocksAnSm = 4;                           // resident, of both passes: a second round of blocks would leave most SMs idle
+// Resident, of both passes: a second round of blocks would leave most SMs idle.
+constexpr int kBlocksAnSm = 4;
 constexpr int64_t kMostValues = int64_t{1} << 40;       // of a tensor
 constexpr int64_t kMostTensors = 1 << 20;
 
@@ -303,10 +304,12 @@ cb_status check(const cb_grad_tensor* t, int64_t tensors, bool scale, std::vecto
     entries.reserve(static_cast<size_t>(tensors));
     for (int64_t i = 0; i < tensors; ++i) {
         const cb_grad_tensor& g = t[i];
-        if (!type_ok(g.dtype) || g.rows < 0 || g.cols < 0 || g.rows > kMostValues || g.cols > kMostValues) return CB_ERR_INVALID_ARG;
+        if (!type_ok(g.dtype) || g.rows < 0 || g.cols < 0 || g.rows > kMostValues || g.cols > kMostValues)
+            return CB_ERR_INVALID_ARG;
         if (g.rows > 0 && g.cols > kMostValues / g.rows) return CB_ERR_INVALID_ARG;
         if (g.rows > 1 && (g.row_stride < g.cols || g.row_stride > kMostValues / g.rows)) return CB_ERR_INVALID_ARG;
-        if (scale && (!type_ok(g.out_dtype) || (g.rows > 1 && (g.out_row_stride < g.cols || g.out_row_stride > kMostValues / g.rows))))
+        if (scale && (!type_ok(g.out_dtype) ||
+                      (g.rows > 1 && (g.out_row_stride < g.cols || g.out_row_stride > kMostValues / g.rows))))
             return CB_ERR_INVALID_ARG;
         if (g.count && (g.rows > 1 || reinterpret_cast<uintptr_t>(g.count) % 8)) return CB_ERR_INVALID_ARG;
         if (g.rows == 0 || g.cols == 0) continue;

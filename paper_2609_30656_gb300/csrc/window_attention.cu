@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cudaTypedefs.h>
+#include <initializer_list>
 
 namespace cbtbe {
 namespace attention {
@@ -34,7 +35,7 @@ __global__ void __launch_bounds__(256) attention_rows_kernel(const Shape S) {
         S.start[t] = static_cast<int32_t>(s);
         S.end[t] = static_cast<int32_t>(e);
     }
-    if (S.largest && first < 3) S.largest[first] = 0u;  // and the two counters of the order
+    if (S.largest && first < 4) S.largest[first] = 0u;  // and the order's three words
     if (!S.error) return;
     for (int64_t i = first; i <= S.sequences; i += step) {
         const int64_t here = load_index(S.offsets, i, S.offsets32);
@@ -96,7 +97,7 @@ __global__ void __launch_bounds__(kWarps * 32) attention_dkv_rowwise_kernel(cons
         const int64_t j = w / S.kv_heads;
         const int kv = static_cast<int>(w - j * S.kv_heads);
         float dk[kLaneValues], dv[kLaneValues];
-        row_dkv<DT>(B, j, kv, dk, dv);
+        row_dkv<DT, true, true>(B, j, kv, dk, dv);
         store_row<DT>(B.dk, j, kv, S.dim, dk);
         store_row<DT>(B.dv, j, kv, S.dim, dv);
     }
@@ -125,6 +126,13 @@ bool heads_ok(const Shape& S, const Heads& h, int heads, bool written) {
         return false;
     return !written || rows_apart(S.tokens, h.token, heads, h.head, S.dim);
 }
+// Whether a result begins where one of the others, or of what is read, does: blocks read what others have written by then.
+bool in_one_place(std::initializer_list<const void*> written, std::initializer_list<const void*> read) {
+    for (auto w = written.begin(); w != written.end(); ++w)
+        if (std::find(w + 1, written.end(), *w) != written.end() || std::find(read.begin(), read.end(), *w) != read.end())
+            return true;
+    return false;
+}
 cb_status sizes_ok(const Shape& S) {
     if (!type_ok(S.dtype) || S.tokens < 0 || S.tokens > kMostTokens || S.sequences < 0 || S.sequences > kMostTokens ||
         S.heads < 1 || S.kv_heads < 1 || S.heads > 65535 || S.heads % S.kv_heads || S.dim < 1 || S.dim > kMaxDim ||
@@ -133,8 +141,8 @@ cb_status sizes_ok(const Shape& S) {
         return CB_ERR_INVALID_ARG;
     return CB_OK;
 }
-Shape shape(int dtype, int64_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, const void* offsets, int idx, int64_t sequences,
-            int64_t window, int64_t sinks, float scale, int* error) {
+Shape shape(int dtype, int64_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, const void* offsets, int idx,
+            int64_t sequences, int64_t window, int64_t sinks, float scale, int* error) {
     Shape S{};
     S.tokens = tokens;
     S.sequences = sequences;
@@ -253,9 +261,10 @@ extern "C" cb_status cb_attention_forward(const void* q, const void* k, const vo
     F.out = {out, out_token_stride, out_head_stride};
     F.lse = lse;
     if (!heads_ok(F.S, F.q, heads, false) || !heads_ok(F.S, F.k, kv_heads, false) || !heads_ok(F.S, F.v, kv_heads, false) ||
-        !heads_ok(F.S, F.out, heads, true) || reinterpret_cast<uintptr_t>(lse) % 4)
+        !heads_ok(F.S, F.out, heads, true) || reinterpret_cast<uintptr_t>(lse) % 4 || in_one_place({out, lse}, {q, k, v}))
         return CB_ERR_INVALID_ARG;
-    if (!workspace_ok(workspace, workspace_bytes, cb_attention_workspace_bytes(tokens, heads, kv_heads, dim, window, sinks, 0))) return CB_ERR_CAPACITY;
+    if (!workspace_ok(workspace, workspace_bytes, cb_attention_workspace_bytes(tokens, heads, kv_heads, dim, window, sinks, 0)))
+        return CB_ERR_CAPACITY;
     set_rows(F.S, workspace, nullptr, stream);
     bool ok = true;
     if (tensor_core_rows(F.S, F.q, heads) && tensor_core_rows(F.S, F.k, kv_heads) && tensor_core_rows(F.S, F.v, kv_heads) &&
@@ -295,14 +304,16 @@ extern "C" cb_status cb_attention_backward(const void* grad_out, const void* q, 
     if (!heads_ok(B.S, B.go, heads, false) || !heads_ok(B.S, B.q, heads, false) || !heads_ok(B.S, B.k, kv_heads, false) ||
         !heads_ok(B.S, B.v, kv_heads, false) || !heads_ok(B.S, B.out, heads, false) || !heads_ok(B.S, B.dq, heads, true) ||
         !heads_ok(B.S, B.dk, kv_heads, true) || !heads_ok(B.S, B.dv, kv_heads, true) || !lse ||
-        reinterpret_cast<uintptr_t>(lse) % 4)
+        reinterpret_cast<uintptr_t>(lse) % 4 || in_one_place({grad_q, grad_k, grad_v}, {grad_out, q, k, v, out, lse}))
         return CB_ERR_INVALID_ARG;
-    if (!workspace_ok(workspace, workspace_bytes, cb_attention_workspace_bytes(tokens, heads, kv_heads, dim, window, sinks, 1))) return CB_ERR_CAPACITY;
+    if (!workspace_ok(workspace, workspace_bytes, cb_attention_workspace_bytes(tokens, heads, kv_heads, dim, window, sinks, 1)))
+        return CB_ERR_CAPACITY;
     const Layout L = layout(tokens, heads, kv_heads, dim, window, sinks);
     char* base = static_cast<char*>(workspace);
     B.delta = reinterpret_cast<float*>(base + L.delta);
     uint32_t* words = reinterpret_cast<uint32_t*>(base + L.words);
-    B.order = {reinterpret_cast<int32_t*>(words + 1), words + 2, static_cast<int32_t>(L.room), reinterpret_cast<int2*>(base + L.list),
+    B.order = {reinterpret_cast<int32_t*>(words + 1), words + 2, words + 3, static_cast<int32_t>(L.room),
+               reinterpret_cast<int2*>(base + L.list),
                reinterpret_cast<int32_t*>(base + L.split), reinterpret_cast<float*>(base + L.sums)};
     set_rows(B.S, workspace, words, stream);
     bool ok = true;

@@ -47,8 +47,9 @@ struct Forward {
 };
 // How the tiles of keys are taken: those in parts first, then the others. (Results do not depend on who takes what.)
 struct Order {
-    int32_t* parts;       // how many parts there are, and
-    uint32_t* next;       // the next item to take: 0 before
+    int32_t* parts;       // how many parts there are,
+    uint32_t* next;       // the next item to take: 0 before,
+    uint32_t* done;       // blocks that have counted their tiles' parts: 0 before,
     int32_t room;         // parts there is room for; 0: no tile is taken in parts
     int2* list;           // [room] tile (-1: none) and which of its parts
     int32_t* split;       // [tiles of 128 tokens] parts of each, 0 for one taken whole
@@ -66,7 +67,8 @@ struct Backward {
 
 // Rows of any type and length up to 256, by a warp that goes key by key, in fp32. The tensor-core kernels
 // turn to it for a row whose result is not finite: their tiles multiply what a row does not see by
-// zeros, which infinities and NaNs of other sessions, or of unused memory, survive.
+// zeros, which infinities and NaNs of other sessions, or of unused memory, survive. A row whose sums have all become NaNs
+// is done: what follows cannot change it, and a batch of NaNs does not cost the row's whole session.
 constexpr int kMaxDim = 256, kLaneValues = kMaxDim / 32;
 
 // A row of up to 256 values, value lane + 32 i in v[i].
@@ -135,11 +137,13 @@ __device__ __forceinline__ void row_output(const Forward& F, int64_t t, int h, f
         load_row<DT>(F.k, j, kv, S.dim, k);
         load_row<DT>(F.v, j, kv, S.dim, v);
         const float s = dot(q, k) * (S.scale * kLog2e);
-        const float top = fmaxf(most, s), keep = most == top ? 1.f : exp2f(most - top), p = exp2f(s - top);
+        const float top = fmaxf(most, s), keep = most == top ? 1.f : exp2f(most - top);
+        const float p = s == -INFINITY ? 0.f : exp2f(s - top);
         sum = fmaf(sum, keep, p);
 #pragma unroll
         for (int i = 0; i < kLaneValues; ++i) o[i] = fmaf(o[i], keep, p * v[i]);
         most = top;
+        if (sum != sum) break;
     }
 #pragma unroll
     for (int i = 0; i < kLaneValues; ++i) o[i] /= sum;
@@ -160,12 +164,13 @@ __device__ __forceinline__ void row_dq(const Backward& B, int64_t t, int h, floa
     for (int64_t j = a.start < a.sinks_end ? a.start : a.first; j <= t; j = j + 1 == a.sinks_end ? a.first : j + 1) {
         load_row<DT>(B.k, j, kv, S.dim, k);
         load_row<DT>(B.v, j, kv, S.dim, v);
-        const float p = exp2f((dot(q, k) * S.scale - lse) * kLog2e);
-        add_scaled(dq, p * (dot(go, v) - delta) * S.scale, k);
+        const float slope = exp2f((dot(q, k) * S.scale - lse) * kLog2e) * (dot(go, v) - delta) * S.scale;
+        add_scaled(dq, slope, k);
+        if (slope != slope) break;
     }
 }
-// Head kv of key j, over the heads that share it and the tokens that see it.
-template <int DT>
+// Head kv of key j, over the heads that share it and the tokens that see it: dk (KEYS) or dv, or both.
+template <int DT, bool KEYS, bool VALUES>
 __device__ __forceinline__ void row_dkv(const Backward& B, int64_t j, int kv, float (&dk)[kLaneValues], float (&dv)[kLaneValues]) {
     const Shape& S = B.S;
     float q[kLaneValues], go[kLaneValues], k[kLaneValues], v[kLaneValues];
@@ -181,8 +186,13 @@ __device__ __forceinline__ void row_dkv(const Backward& B, int64_t j, int kv, fl
             load_row<DT>(B.q, t, h, S.dim, q);
             load_row<DT>(B.go, t, h, S.dim, go);
             const float p = exp2f((dot(q, k) * S.scale - B.lse[h * S.tokens + t]) * kLog2e);
-            add_scaled(dv, p, go);
-            add_scaled(dk, p * (dot(go, v) - B.delta[h * S.tokens + t]) * S.scale, q);
+            float slope = p;
+            if constexpr (VALUES) add_scaled(dv, p, go);
+            if constexpr (KEYS) {
+                slope = p * (dot(go, v) - B.delta[h * S.tokens + t]) * S.scale;
+                add_scaled(dk, slope, q);
+            }
+            if ((VALUES ? p : slope) != (VALUES ? p : slope)) return;
         }
 }
 

@@ -23,8 +23,7 @@ namespace cbtbe {
 namespace attention {
 namespace {
 
-constexpr int kWorkWarps = 8, kCopyWarp = 8, kMultiplyWarp = 9, kThreads = 384;
-constexpr int kAheadWarp = 10;
+constexpr int kWorkWarps = 8, kCopyWarp = 8, kMultiplyWarp = 9, kAheadWarp = 10, kThreads = 384;
 constexpr int kStoreWarp = 11;  // over queries
 constexpr int kStatWarp = 11;   // over keys
 // Registers of the threads that work and of the others, of 384 x 168 at launch: what leaves either fewest spills (with
@@ -54,9 +53,45 @@ __device__ __forceinline__ int parts_of(const Shape& S, int blocks) {
     return blocks <= 2 * per ? 0 : (blocks + per - 1) / per;
 }
 
+constexpr int kDeltaThreads = 256;
+// Which part of which tile has each place: the tiles in order, as far as there is room (so that the same tiles are
+// taken in parts every time: their sums are added in another order than a whole tile's). By a block.
+__device__ __forceinline__ void order_parts(const Backward& B) {
+    __shared__ int of_warp[kDeltaThreads / 32];
+    const Order& O = B.order;
+    const int tiles = tiles_of(static_cast<int>(B.S.tokens)), warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    int before = 0;
+    for (int first = 0; first < tiles; first += kDeltaThreads) {
+        const int tile = first + static_cast<int>(threadIdx.x);
+        const int parts = tile < tiles ? __ldcg(O.split + tile) : 0;
+        int up_to = parts;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int other = __shfl_up_sync(kFull, up_to, off);
+            if (lane >= off) up_to += other;
+        }
+        __syncthreads();
+        if (lane == 31) of_warp[warp] = up_to;
+        __syncthreads();
+        int all = 0, place = before + up_to - parts;
+        for (int w = 0; w < kDeltaThreads / 32; ++w) {
+            if (w < warp) place += of_warp[w];
+            all += of_warp[w];
+        }
+        if (parts && place + parts <= O.room) {
+            for (int p = 0; p < parts; ++p) O.list[place + p] = make_int2(tile, p);
+        } else if (parts) {  // in one piece; places that are left stay empty
+            for (int p = place; p < O.room; ++p) O.list[p] = make_int2(-1, 0);
+            O.split[tile] = 0;
+        }
+        before = min(before + all, 1 << 29);
+    }
+    if (threadIdx.x == 0) *O.parts = before;
+}
+
 // delta, and the largest |grad_out|: 16 bytes a lane, D / 8 lanes a row.
 template <int D, bool BF16>
-__global__ void __launch_bounds__(256) attention_delta_kernel(const Backward B) {
+__global__ void __launch_bounds__(kDeltaThreads) attention_delta_kernel(const Backward B) {
     constexpr int DT = BF16 ? CB_BF16 : CB_F16, kLanes = D / 8, kRowsAtOnce = 32 / kLanes;
     begin_kernel();
     const Shape& S = B.S;
@@ -80,7 +115,7 @@ __global__ void __launch_bounds__(256) attention_delta_kernel(const Backward B) 
         for (int off = kLanes / 2; off >= 1; off >>= 1) sum += __shfl_xor_sync(kFull, sum, off);
         if (i < rows && lane % kLanes == 0) B.delta[h * S.tokens + t] = sum;
     }
-    // Tiles of keys that are taken in parts, where there is room for their sums: which part of which tile each is.
+    // In how many parts each tile of keys is to be taken, where some may be.
     const int tiles = B.order.room ? tiles_of(static_cast<int>(S.tokens)) : 0;
     for (int64_t w = warp_id_global(); w < tiles; w += warps_in_grid()) {
         const int from = static_cast<int>(w) * kTile;
@@ -88,23 +123,21 @@ __global__ void __launch_bounds__(256) attention_delta_kernel(const Backward B) 
 #pragma unroll
         for (int k = 0; k < kTile / 32; ++k) until = max(until, seen_until(S, from + k * 32 + lane));
         until = __reduce_max_sync(kFull, until);
-        int parts = parts_of(S, tiles_of(max(until - from, 0))), slot = 0;
-        if (lane == 0 && parts) {
-            slot = atomicAdd(B.order.parts, parts);
-            if (slot + parts > B.order.room) {  // the tile in one piece; the places stay empty
-                for (int p = slot; p < B.order.room; ++p) B.order.list[p] = make_int2(-1, 0);
-                parts = 0;
-            }
-        }
-        slot = __shfl_sync(kFull, slot, 0);
-        parts = __shfl_sync(kFull, parts, 0);
-        for (int p = lane; p < parts; p += 32) B.order.list[slot + p] = make_int2(static_cast<int>(w), p);
-        if (lane == 0) B.order.split[w] = parts;
+        if (lane == 0) B.order.split[w] = parts_of(S, tiles_of(max(until - from, 0)));
     }
     if constexpr (!BF16) {
         const uint32_t most = __reduce_max_sync(kFull, __float_as_uint(largest));
         if (lane == 0 && most) atomicMax(S.largest, most);
     }
+    if (tiles == 0) return;
+    __shared__ bool last;  // of the blocks: every tile's number of parts is there
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) last = atomicAdd(B.order.done, 1u) == gridDim.x - 1;
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    order_parts(B);
 }
 
 template <bool BF16, int D>
@@ -124,10 +157,15 @@ __device__ __noinline__ void dq_again(const Backward& B, int64_t t, int h, unsig
 }
 template <bool BF16, int D>
 __device__ __noinline__ void dkv_again(const Backward& B, int64_t j, int kv, bool keys, unsigned char* tile, int r) {
+    constexpr int DT = BF16 ? CB_BF16 : CB_F16;
     float dk[kLaneValues], dv[kLaneValues];
-    row_dkv<BF16 ? CB_BF16 : CB_F16>(B, j, kv, dk, dv);
-    if (keys) put_row<BF16, D>(dk, tile, r);
-    else put_row<BF16, D>(dv, tile, r);
+    if (keys) {
+        row_dkv<DT, true, false>(B, j, kv, dk, dv);
+        put_row<BF16, D>(dk, tile, r);
+    } else {
+        row_dkv<DT, false, true>(B, j, kv, dk, dv);
+        put_row<BF16, D>(dv, tile, r);
+    }
 }
 
 // A row of sums from TMEM, times `by`, into its tile in shared memory; whether all are finite.
@@ -189,7 +227,8 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
     if (threadIdx.x == 0) {
         for (uint64_t* b : {&q_full, &q_empty, &v_full, &v_empty}) tc::barrier_init(tc::smem_addr(b), 1);
         for (int i = 0; i < 2; ++i) {
-            for (uint64_t* b : {g_full, stored, k_full, k_empty, scores, grads, sums, item_full}) tc::barrier_init(tc::smem_addr(b + i), 1);
+            for (uint64_t* b : {g_full, stored, k_full, k_empty, scores, grads, sums, item_full})
+                tc::barrier_init(tc::smem_addr(b + i), 1);
             for (uint64_t* b : {taken, slopes[0], slopes[1], staged}) tc::barrier_init(tc::smem_addr(b + i), 4);
             tc::barrier_init(tc::smem_addr(item_empty + i), kWorkWarps + 3);
         }
@@ -205,8 +244,9 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
     const int first = static_cast<int>(blockIdx.x), stride = static_cast<int>(gridDim.x);
     const int rounds = (items - first + stride - 1) / stride;
     bool ok = true;
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return ok = tc::barrier_wait(tc::smem_addr(bar), parity & 1); };  // one thread
-    auto meet = [&](uint64_t* bar, uint32_t parity) { return ok = warp_wait(bar, parity); };                          // a whole warp
+    // One thread waits, or a whole warp.
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return ok = tc::barrier_wait(tc::smem_addr(bar), parity & 1); };
+    auto meet = [&](uint64_t* bar, uint32_t parity) { return ok = warp_wait(bar, parity); };
     // The n-th item, for one thread; it is done with it at item_done.
     auto item_of = [&](int n) -> const Item& {
         wait(item_full + (n & 1), n >> 1);
@@ -453,7 +493,8 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
 #pragma unroll
                     for (int k = 0; k < 32; k += 2) {
                         const float2 x = fma2(make_float2(d[k], d[k + 1]), f2, delta2);
-                        const float2 y = mul2(x, make_float2(__uint_as_float(p[w / 2][w % 2 * 32 + k]), __uint_as_float(p[w / 2][w % 2 * 32 + k + 1])));
+                        const uint32_t* weight = p[w / 2] + w % 2 * 32 + k;
+                        const float2 y = mul2(x, make_float2(__uint_as_float(weight[0]), __uint_as_float(weight[1])));
                         packed[k / 2] = pack2<BF16>(y.x, y.y);
                     }
                     tmem_store16_begin(s_at + w * 16, packed);
@@ -555,8 +596,9 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
     const uint32_t tmem = tmem_at;
     begin_kernel();
     bool ok = true;
-    auto wait = [&](uint64_t* bar, uint32_t parity) { return ok = tc::barrier_wait(tc::smem_addr(bar), parity & 1); };  // one thread
-    auto meet = [&](uint64_t* bar, uint32_t parity) { return ok = warp_wait(bar, parity); };                          // a whole warp
+    // One thread waits, or a whole warp.
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return ok = tc::barrier_wait(tc::smem_addr(bar), parity & 1); };
+    auto meet = [&](uint64_t* bar, uint32_t parity) { return ok = warp_wait(bar, parity); };
 
     if (warp >= kWorkWarps) {
         registers_down<kKeyFewer>();
@@ -777,7 +819,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
         for (int n = 0;; ++n) {
             if (!(ok = warp_wait(item_full + (n & 1), n >> 1))) break;
             const KeyItem& it = info[n & 1];
-            const int first = it.first, from = it.from, kv = it.kv, blocks = it.blocks, place = it.place, last = blocks < 0 ? 0 : it.last[row];
+            const int first = it.first, from = it.from, kv = it.kv, blocks = it.blocks, place = it.place;
+            const int last = blocks < 0 ? 0 : it.last[row];
             warp_arrive(item_empty + (n & 1));
             if (blocks < 0) break;
             const TwoRanges seen{first + row, last, 0, 0};
@@ -798,8 +841,9 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
 #pragma unroll
                 for (int k = 0; k < 64; k += 4) {
                     const float4 l = lse[k / 4];
-                    const float2 x = fma2(make_float2(__uint_as_float(p[k]), __uint_as_float(p[k + 1])), c2, make_float2(l.x, l.y));
-                    const float2 y = fma2(make_float2(__uint_as_float(p[k + 2]), __uint_as_float(p[k + 3])), c2, make_float2(l.z, l.w));
+                    const float2 s0 = make_float2(__uint_as_float(p[k]), __uint_as_float(p[k + 1]));
+                    const float2 s1 = make_float2(__uint_as_float(p[k + 2]), __uint_as_float(p[k + 3]));
+                    const float2 x = fma2(s0, c2, make_float2(l.x, l.y)), y = fma2(s1, c2, make_float2(l.z, l.w));
                     p[k] = __float_as_uint(exp2_fast(x.x));
                     p[k + 1] = __float_as_uint(exp2_fast(x.y));
                     p[k + 2] = __float_as_uint(exp2_fast(y.x));
@@ -854,14 +898,16 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                     float o[32] = {};
                     if (count > 0) tc::tmem_load32(tmem + lanes + 256 + half * D + d, o);
 #pragma unroll
-                    for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(to + d + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+                    for (int k = 0; k < 32; k += 4)
+                        *reinterpret_cast<float4*>(to + d + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
                 }
                 tc::fence_before();
                 warp_arrive(staged + half);
                 continue;
             }
             bool finite = true;
-            if (count > 0) finite = finish_row<D, BF16>(tmem + lanes + 256 + half * D, half ? B.S.scale / scale_s : exp2f(-kPShift<BF16>), last > 0, tile, row);
+            const float by = half ? B.S.scale / scale_s : exp2f(-kPShift<BF16>);
+            if (count > 0) finite = finish_row<D, BF16>(tmem + lanes + 256 + half * D, by, last > 0, tile, row);
             else zero_row<D>(tile, row);
             for (uint32_t left = __ballot_sync(kFull, !finite); left; left &= left - 1) {
                 const int other = (row & ~31) + __ffs(left) - 1;
@@ -902,7 +948,8 @@ __global__ void __launch_bounds__(256) attention_parts_kernel(const Backward B) 
             for (int p = 0; p < parts && real; ++p)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const float* from = B.order.sums + (((static_cast<int64_t>(place) + p) * B.S.kv_heads + kv) * 2 + h) * kTile * D + row * D;
+                    const int64_t at = ((static_cast<int64_t>(place) + p) * B.S.kv_heads + kv) * 2 + h;
+                    const float* from = B.order.sums + at * kTile * D + row * D;
 #pragma unroll
                     for (int i = 0; i < N; ++i) v[h][i] += __ldcg(from + lane + 32 * i);
                 }
@@ -913,7 +960,7 @@ __global__ void __launch_bounds__(256) attention_parts_kernel(const Backward B) 
                     v[h][i] *= by[h];
                     finite &= fabsf(v[h][i]) < INFINITY || lane + 32 * i >= B.S.dim;
                 }
-            if (!__all_sync(kFull, finite)) row_dkv<DT>(B, j, kv, v[1], v[0]);
+            if (!__all_sync(kFull, finite)) row_dkv<DT, true, true>(B, j, kv, v[1], v[0]);
             store_row<DT>(B.dv, j, kv, B.S.dim, v[0]);
             store_row<DT>(B.dk, j, kv, B.S.dim, v[1]);
         }
@@ -935,12 +982,11 @@ bool launch_typed(const Backward& B, cudaStream_t s) {
         return false;
     const int64_t key_tiles = (S.tokens + kTile - 1) / kTile * S.kv_heads, items = work_items(S);
     if (items > INT32_MAX / 2 || key_tiles > INT32_MAX / 4) return false;
-    launch(attention_delta_kernel<D, BF16>, dim3(warp_grid((S.tokens * S.heads * D / 8 + 31) / 32, 152 * 32)), dim3(256), 0, s, B);
+    launch(attention_delta_kernel<D, BF16>, dim3(warp_grid((S.tokens * S.heads * D / 8 + 31) / 32, 152 * 32)), dim3(kDeltaThreads), 0, s, B);
     launch(attention_dkv_kernel<D, BF16>, dim3(static_cast<unsigned>(std::min<int64_t>(key_tiles, sm_count()))), dim3(kThreads),
            kKeyShared<D>, s, qm, km, vm, gm, dkm, dvm, B);
-    if (B.order.room)
-        launch(attention_parts_kernel<D, BF16>, dim3(static_cast<unsigned>(std::min<int64_t>(static_cast<int64_t>(B.order.room) * S.kv_heads, 8 * sm_count()))),
-               dim3(256), 0, s, B);
+    const int64_t joined = std::min<int64_t>(static_cast<int64_t>(B.order.room) * S.kv_heads, 8 * sm_count());
+    if (joined > 0) launch(attention_parts_kernel<D, BF16>, dim3(static_cast<unsigned>(joined)), dim3(256), 0, s, B);
     launch(attention_dq_kernel<D, BF16>, dim3(static_cast<unsigned>(std::min<int64_t>(items, sm_count()))), dim3(kThreads),
            kQueryShared<D>, s, qm, km, vm, gm, dqm, B, pairs_heads(S), static_cast<int>(items));
     return true;

@@ -75,7 +75,8 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
     unsigned char* queries = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~uintptr_t(1023));
     unsigned char* ring = queries + 2 * kRows;
     unsigned char* output = ring + 2 * S * kRows;  // of one tile after the other
-    __shared__ uint64_t q_full, q_empty, full[S], empty[S], scores[2], part[2][kParts], sums[2], staged[2], stored, item_full[2], item_empty[2];
+    __shared__ uint64_t q_full, q_empty, full[S], empty[S], scores[2], part[2][kParts], sums[2], staged[2], stored;
+    __shared__ uint64_t item_full[2], item_empty[2];
     __shared__ uint32_t tmem_at;
     __shared__ Item info[2];
     const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
@@ -182,7 +183,8 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
             const bool one = tc::elect();
             constexpr uint32_t shape_s = mma_shape<BF16>(kTile, kTile, false), shape_o = mma_shape<BF16>(kTile, D, true);
             const uint64_t q0 = tc::operand_k_major(tc::smem_addr(queries));
-            const uint64_t k0 = tc::operand_k_major(tc::smem_addr(ring) + kRows), v0 = tc::operand_mn_major(tc::smem_addr(ring), kBoxBytes);
+            const uint64_t k0 = tc::operand_k_major(tc::smem_addr(ring) + kRows);
+            const uint64_t v0 = tc::operand_mn_major(tc::smem_addr(ring), kBoxBytes);
             int s = 0;  // stage of the next copies
             uint32_t phase = 0, p_phase[2] = {0, 0};
             auto commit = [&](uint64_t* bar) {
@@ -321,8 +323,10 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
 #pragma unroll
                 for (int k = 0; k < 128; k += 8)
 #pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        top[u] = max3(top[u], __uint_as_float(v[k / 64][k % 64 + 2 * u]), __uint_as_float(v[k / 64][k % 64 + 2 * u + 1]));
+                    for (int u = 0; u < 4; ++u) {
+                        const uint32_t* two = v[k / 64] + k % 64 + 2 * u;
+                        top[u] = max3(top[u], __uint_as_float(two[0]), __uint_as_float(two[1]));
+                    }
                 const float highest = max3(fmaxf(top[0], top[1]), top[2], top[3]);
                 if (__any_sync(kFull, (highest - most) * c > kRise<BF16>)) {  // false for two infinities
                     const float raised = fmaxf(most, highest);
@@ -357,7 +361,7 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
             if (!ok || !(ok = warp_wait(&stored, mine ^ 1))) break;
             const float2 both = add2(sum0, sum1);
             const float sum = both.x + both.y;
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;  // a NaN stays one
+            const float inv = 1.f / sum;  // rows that see nothing do not use it
             const float2 inv2 = make_float2(inv, inv), zero2 = make_float2(0.f, 0.f);
             float2 check = zero2;  // stays 0 while all is finite
 #pragma unroll 1
@@ -386,8 +390,10 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
             tc::fence_before();
             warp_arrive(staged + mine);
             warp_arrive(item_empty + (n & 1));
-            if (F.lse && t < F.S.tokens)
-                F.lse[head * F.S.tokens + t] = r.real ? ((most == -INFINITY ? 0.f : most * c) + __log2f(sum) - kShift<BF16>) * kLn2 : -INFINITY;
+            if (F.lse && t < F.S.tokens) {
+                const float against = most == -INFINITY ? 0.f : most * c;
+                F.lse[head * F.S.tokens + t] = r.real ? (against + __log2f(sum) - kShift<BF16>) * kLn2 : -INFINITY;
+            }
         }
     }
     if (!ok && F.S.error) set_error(F.S.error, CB_ERR_TIMEOUT);

@@ -11,7 +11,6 @@ namespace cbtbe {
 namespace attention {
 namespace {
 
-
 constexpr int kWarps = 8;
 
 struct Step {
@@ -63,7 +62,8 @@ __global__ void __launch_bounds__(kWarps * 32) attention_step_rowwise_kernel(con
 #pragma unroll
             for (int x = 0; x < kLaneValues; ++x) s = fmaf(q[x], k[x], s);
             s = warp_sum(s) * (A.scale * kLog2e);
-            const float top = fmaxf(most, s), keep = most == top ? 1.f : exp2f(most - top), p = exp2f(s - top);
+            const float top = fmaxf(most, s), keep = most == top ? 1.f : exp2f(most - top);
+            const float p = s == -INFINITY ? 0.f : exp2f(s - top);
             sum = fmaf(sum, keep, p);
 #pragma unroll
             for (int x = 0; x < kLaneValues; ++x) o[x] = fmaf(o[x], keep, p * v[x]);
@@ -140,11 +140,13 @@ __device__ __forceinline__ void load_matrices_turned(uint32_t addr, uint32_t (&r
 template <bool BF16>
 __device__ __forceinline__ void multiply(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     if constexpr (BF16)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 "
+                     "{%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
     else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 "
+                     "{%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -203,7 +205,8 @@ attention_step_kernel(const Step A, const Parts P) {
             const int r = lane / 4 + (x & 1) * 8, c = k * 16 + (x >> 1) * 8 + lane % 4 * 2;
             q[k][x] = 0u;
             if (r < heads && c < A.dim) {
-                const uint16_t* p = static_cast<const uint16_t*>(A.q) + b * A.q_seq + static_cast<int64_t>(head0 + r) * A.q_head + c;
+                const uint16_t* p = static_cast<const uint16_t*>(A.q) + b * A.q_seq +
+                                    static_cast<int64_t>(head0 + r) * A.q_head + c;
                 q[k][x] = static_cast<uint32_t>(p[0]) | static_cast<uint32_t>(p[1]) << 16;
             }
         }
@@ -247,7 +250,8 @@ attention_step_kernel(const Step A, const Parts P) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[d][i] *= keep[i >> 1];
         }
-        const float base[2] = {kShift - (top[0] == -INFINITY ? 0.f : top[0] * c), kShift - (top[1] == -INFINITY ? 0.f : top[1] * c)};
+        const float base[2] = {kShift - (top[0] == -INFINITY ? 0.f : top[0] * c),
+                               kShift - (top[1] == -INFINITY ? 0.f : top[1] * c)};
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -340,7 +344,7 @@ __global__ void __launch_bounds__(128) attention_step_join_kernel(const Step A, 
         total = fmaf(sum, f, total);
         value = fmaf(__ldcg(at + d), f, value);
     }
-    const float r = total == 0.f ? 0.f : value / total;
+    const float r = length_of(A, b) > 0 ? value / total : 0.f;
     static_cast<uint16_t*>(A.out)[b * A.out_seq + static_cast<int64_t>(h) * A.out_head + d] =
         static_cast<uint16_t>(narrow<BF16 ? CB_BF16 : CB_F16>(r));
 }
@@ -395,7 +399,8 @@ extern "C" cb_status cb_attention_step(const void* q, const void* k_cache, const
                                        int64_t out_sequence_stride, int64_t out_head_stride, void* workspace,
                                        int64_t workspace_bytes, int* error, cudaStream_t stream) {
     using namespace cbtbe::attention;
-    if (!type_ok(dtype) || !sizes_ok(sequences, capacity, heads, kv_heads, dim, window, sinks) || !(scale == scale) || (idx_dtype != CB_I32 && idx_dtype != CB_I64) || reinterpret_cast<uintptr_t>(error) % 4)
+    if (!type_ok(dtype) || !sizes_ok(sequences, capacity, heads, kv_heads, dim, window, sinks) || !(scale == scale) ||
+        (idx_dtype != CB_I32 && idx_dtype != CB_I64) || reinterpret_cast<uintptr_t>(error) % 4)
         return CB_ERR_INVALID_ARG;
     for (const int64_t s : {q_sequence_stride, q_head_stride, k_sequence_stride, k_token_stride, k_head_stride,
                             v_sequence_stride, v_token_stride, v_head_stride, out_sequence_stride, out_head_stride})
@@ -405,7 +410,8 @@ extern "C" cb_status cb_attention_step(const void* q, const void* k_cache, const
     const uintptr_t mask = dtype == CB_F32 ? 3 : 1;
     if (!q || !out || !lengths || (capacity > 0 && (!k_cache || !v_cache)) || (reinterpret_cast<uintptr_t>(q) & mask) ||
         (reinterpret_cast<uintptr_t>(k_cache) & mask) || (reinterpret_cast<uintptr_t>(v_cache) & mask) ||
-        (reinterpret_cast<uintptr_t>(out) & mask) || reinterpret_cast<uintptr_t>(lengths) % (idx_dtype == CB_I32 ? 4 : 8))
+        (reinterpret_cast<uintptr_t>(out) & mask) || out == q || out == k_cache || out == v_cache ||
+        reinterpret_cast<uintptr_t>(lengths) % (idx_dtype == CB_I32 ? 4 : 8))
         return CB_ERR_INVALID_ARG;
     const int64_t need = cb_attention_step_workspace_bytes(sequences, heads, kv_heads, dim, capacity, window, sinks);
     if (need > 0 && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 || workspace_bytes < need)) return CB_ERR_CAPACITY;

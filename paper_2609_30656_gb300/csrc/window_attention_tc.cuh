@@ -28,7 +28,8 @@ __host__ __device__ constexpr uint32_t mma_shape(int m, int n, bool b_mn_major) 
     return tc::mma_shape(m, n, b_mn_major) | (BF16 ? 1u << 7 | 1u << 10 : 0u);
 }
 
-#define CB_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define CB_R8(r, i) \
+    "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
 #define CB_R32(r, i) CB_R8(r, i), CB_R8(r, i + 8), CB_R8(r, i + 16), CB_R8(r, i + 24)
 
 // 64 columns of the warp's 32 lanes; they have arrived when the call returns.
@@ -74,8 +75,8 @@ __device__ __forceinline__ void scale8(uint32_t addr, float f) {
                  : "memory");
 #pragma unroll
     for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * f);
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};\n\ttcgen05.wait::st.sync.aligned;" ::"r"(
-                     r[0]),
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};\n\t"
+                 "tcgen05.wait::st.sync.aligned;" ::"r"(r[0]),
                  "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(addr)
                  : "memory");
 }
@@ -131,11 +132,6 @@ __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sy
 template <int N>
 __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
-// `count` threads at barrier `id` (1 .. 15).
-__device__ __forceinline__ void named_barrier(int id, int count) {
-    asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(count) : "memory");
-}
-
 // This thread's stores to shared memory, before TMA reads them (and a barrier between). Only those: the fence over all
 // memory waits for the thread's stores to global memory too, 1500 clocks.
 __device__ __forceinline__ void fence_to_tma() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -159,7 +155,8 @@ __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, 
 
 // Byte of columns 8 c .. 8 c + 7 (16 bytes) of row r in a tile as TMA lays it out.
 __device__ __forceinline__ uint32_t tile_byte(int r, int c) {
-    return static_cast<uint32_t>(c >> 3) * kBoxBytes + static_cast<uint32_t>(r) * 128 + static_cast<uint32_t>(((c & 7) ^ (r & 7)) << 4);
+    return static_cast<uint32_t>(c >> 3) * kBoxBytes + static_cast<uint32_t>(r) * 128 +
+           static_cast<uint32_t>(((c & 7) ^ (r & 7)) << 4);
 }
 
 // ---------------------------------------------------------------- whole warps
@@ -194,20 +191,12 @@ __device__ __forceinline__ uint32_t range_bits(int a, int b, int first) { return
 struct TwoRanges {
     int a0, a1, b0, b1;
     __device__ __forceinline__ uint32_t bits(int first) const { return range_bits(a0, a1, first) | range_bits(b0, b1, first); }
-    __device__ __forceinline__ bool all(int first, int n) const { return a0 <= first && a1 >= first + n; }
-    __device__ __forceinline__ bool none(int first, int n) const {
-        return (a1 <= first || a0 >= first + n || a0 >= a1) && (b1 <= first || b0 >= first + n || b0 >= b1);
-    }
 };
 
 // The keys that the rows of a tile see: [lo, hi), and before that the first tokens of the
 // session that the tile begins in, [s0, s1). All empty where the tile has no token of a session.
 struct Sight {
     int lo, hi, s0, s1;
-};
-// By the 128 threads of the tile's rows (thread's row: `t`), joined by `sight_of` behind a barrier.
-struct SightParts {
-    int lo[4], hi[4], s0[4];
 };
 struct Row {
     int start, first;  // of the session, and of the window; both t + 1 where t is of no session
@@ -222,26 +211,12 @@ __device__ __forceinline__ Row row_of(const Shape& S, int64_t t) {
     }
     return r;
 }
-__device__ __forceinline__ void note_row(SightParts& P, const Row& r, int t, int warp, int lane) {
-    const int lo = __reduce_min_sync(kFull, r.real ? r.first : INT32_MAX);
-    const int hi = __reduce_max_sync(kFull, r.real ? t + 1 : 0);
-    const int s0 = __reduce_min_sync(kFull, r.real ? r.start : INT32_MAX);
-    if (lane == 0) {
-        P.lo[warp] = lo;
-        P.hi[warp] = hi;
-        P.s0[warp] = s0;
-    }
-}
-__device__ __forceinline__ Sight sight_of(const SightParts& P, int sinks) {
-    Sight s;
-    s.lo = min(min(P.lo[0], P.lo[1]), min(P.lo[2], P.lo[3]));
-    s.hi = max(max(P.hi[0], P.hi[1]), max(P.hi[2], P.hi[3]));
-    const int s0 = min(min(P.s0[0], P.s0[1]), min(P.s0[2], P.s0[3]));
-    s.s0 = s.s1 = 0;
-    if (s.hi == 0) s.lo = 0;
-    else if (s0 < s.lo) {
-        s.s0 = s0;
-        s.s1 = static_cast<int>(min64(static_cast<int64_t>(s0) + sinks, s.lo));
+// From the least `first`, the end of the last real row and the least `start` of a tile.
+__device__ __forceinline__ Sight sight_of(int lo, int hi, int start, int sinks) {
+    Sight s{hi == 0 ? 0 : lo, hi, 0, 0};
+    if (hi > 0 && start < lo) {
+        s.s0 = start;
+        s.s1 = static_cast<int>(min64(static_cast<int64_t>(start) + sinks, lo));
     }
     return s;
 }
@@ -335,13 +310,12 @@ __device__ __forceinline__ void look_ahead(const Shape& S, Item& it, int x, int 
         hi = max(hi, t + 1);
         s0 = min(s0, r.start);
     }
-    SightParts P;
-    P.lo[0] = P.lo[1] = P.lo[2] = P.lo[3] = __reduce_min_sync(kFull, lo);
-    P.hi[0] = P.hi[1] = P.hi[2] = P.hi[3] = __reduce_max_sync(kFull, hi);
-    P.s0[0] = P.s0[1] = P.s0[2] = P.s0[3] = __reduce_min_sync(kFull, s0);
+    lo = __reduce_min_sync(kFull, lo);
+    hi = __reduce_max_sync(kFull, hi);
+    s0 = __reduce_min_sync(kFull, s0);
     if (lane == 0) {
-        it.sight[x] = sight_of(P, S.sinks);
-        it.begin[x] = P.s0[0];
+        it.sight[x] = sight_of(lo, hi, s0, S.sinks);
+        it.begin[x] = s0;
     }
 }
 __device__ __forceinline__ Row row_in(const Shape& S, const Item& it, int x, int row) {

@@ -62,15 +62,18 @@ def _index(t: torch.Tensor, what: str, index: int) -> int:
     return kind
 
 
+def _fits(t: torch.Tensor) -> bool:
+    """Whether t's rows are contiguous and lie as the library's kernels for its type and size take them."""
+    stride, dim = t.stride(), t.shape[-1]
+    if dim > 1 and stride[-1] != 1:
+        return False
+    if t.dtype == torch.float32 or dim % 8 or dim > 128:
+        return True
+    return not (t.data_ptr() % 16 or any(s % 8 or s < dim for s, n in zip(stride[:-1], t.shape) if n > 1))  # TMA: 16 bytes
+
+
 def _rows(t: torch.Tensor) -> torch.Tensor:
-    """t with contiguous rows at distances that the library takes as they are; a copy where it has others."""
-    stride = t.stride()
-    if t.shape[-1] > 1 and stride[-1] != 1:
-        return t.contiguous()
-    if t.dtype != torch.float32 and t.shape[-1] % 8 == 0 and t.shape[-1] <= 128:  # the tensor cores' copies: 16 bytes
-        if t.data_ptr() % 16 or any(s % 8 or s < t.shape[-1] for s, n in zip(stride[:-1], t.shape) if n > 1):
-            return t.clone(memory_format=torch.contiguous_format)
-    return t
+    return t if _fits(t) else t.clone(memory_format=torch.contiguous_format)
 
 
 def _strides(t: torch.Tensor):
@@ -82,7 +85,7 @@ def _shape(window, sinks, scale, dim: int):
     window = ALL if window is None else window
     if window < 1 or sinks < 0:
         raise ValueError("window must be at least 1 and sinks at least 0")
-    return min(window, ALL), sinks, dim ** -0.5 if scale is None else scale
+    return min(window, ALL), min(sinks, ALL), dim ** -0.5 if scale is None else scale
 
 
 def _check_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor):
@@ -121,8 +124,9 @@ def window_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets:
 
     q: [tokens, heads, dim]; k, v: [tokens, kv_heads, dim]; slices of one projection's output are taken as they lie.
     offsets: int32 or int64 [sessions + 1]; tokens of no session give zeros. window None: all tokens before. scale:
-    dim ** -0.5 unless given. With stats=True the result is (out, lse), lse fp32 [heads, tokens], as the backward
-    pass takes it. error: an int32 tensor of one value on the device, set where offsets decrease or leave the tokens."""
+    dim ** -0.5 unless given. out shares no memory with q, k, v. With stats=True the result is (out, lse), lse fp32
+    [heads, tokens], as the backward pass takes it. error: an int32 tensor of one value on the device, set
+    where offsets decrease or leave the tokens."""
     lib = _bound or _library()
     index, kind, tokens, heads, kv_heads, dim = _check_packed(q, k, v)
     off_kind = _index(offsets, "offsets", index)
@@ -134,9 +138,8 @@ def window_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets:
     out = _output(out, q, "out")
     lse = torch.empty(heads, tokens, dtype=torch.float32, device=q.device) if stats else None
     if tokens:
-        q, k, v, to = _rows(q), _rows(k), _rows(v), out
-        if _rows(out) is not out:
-            to = torch.empty(out.shape, dtype=out.dtype, device=out.device)
+        q, k, v = _rows(q), _rows(k), _rows(v)
+        to = out if _fits(out) else torch.empty(out.shape, dtype=out.dtype, device=out.device)
         with tbe._OnDevice(index):
             nbytes = lib.cb_attention_workspace_bytes(tokens, heads, kv_heads, dim, window, sinks, 0)
             work = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
@@ -158,7 +161,8 @@ def window_attention_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torch.
     """The gradients (dq, dk, dv) of window_attention, from its inputs and its (out, lse) of stats=True
     (cb_attention_backward), in the inputs' type.
 
-    grads: three tensors to write them to (slices of one buffer, say), which share no memory with the inputs."""
+    grads: three tensors to write them to (slices of one buffer, say), which share no memory with the inputs or one
+    another."""
     lib = _bound or _library()
     index, kind, tokens, heads, kv_heads, dim = _check_packed(q, k, v)
     off_kind = _index(offsets, "offsets", index)
@@ -177,7 +181,7 @@ def window_attention_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torch.
         raise ValueError("grads must be three tensors")
     grads = tuple(_output(g, t, what) for g, t, what in zip(given, (q, k, v), ("dq", "dk", "dv")))
     if tokens:
-        to = tuple(g if _rows(g) is g else torch.empty(g.shape, dtype=g.dtype, device=g.device) for g in grads)
+        to = tuple(g if _fits(g) else torch.empty(g.shape, dtype=g.dtype, device=g.device) for g in grads)
         ins = [_rows(t) for t in (grad_out, q, k, v, out)]
         lse = lse.contiguous()
         with tbe._OnDevice(index):
@@ -203,7 +207,8 @@ def window_attention_step(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch
 
     q: [sessions, heads, dim]; k_cache, v_cache: [sessions, capacity, kv_heads, dim] in any strides with contiguous rows
     (a transposed [sessions, kv_heads, capacity, dim] too); lengths: int32 or int64 [sessions], the tokens of each,
-    the new one among them, 0 .. capacity (0: zeros). error: set to CB_ERR_INDEX_OOB by a length outside."""
+    the new one among them, 0 .. capacity (0: zeros). out shares no memory with the inputs. error:
+    set to CB_ERR_INDEX_OOB by a length outside."""
     lib = _bound or _library()
     index = q.get_device()
     if index < 0 or q.dim() != 3 or k_cache.dim() != 4:

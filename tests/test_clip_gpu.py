@@ -251,3 +251,19 @@ def test_values_past_32_bits():
     t[5] = 3.0
     assert clip.clip_grad_norm([t], 1.0).item() == pytest.approx(math.sqrt(21.0), rel=5 * U)
     assert t[-1].item() == pytest.approx(2.0 / math.sqrt(21.0), rel=2 ** -8) and t[5].item() > 0.6
+
+
+def test_one_place_is_written_once():
+    from paper_2609_30656_gb300 import tbe
+    clip = _clip()
+    g = _gen(12)
+    a, b = _rand(g, 40, 16), _rand(g, 40, 16)
+    was = a.clone()
+    for grads, out in (([a, b, a], None), ([a, a], [b, b]), ([a, b], [b, torch.empty_like(a)]), ([a[:8], a], None)):
+        with pytest.raises(tbe.CbTbeError):
+            clip.clip_grad_norm(grads, 0.1, out=out)
+    assert torch.equal(a, was)
+    # The norm of a list reads alone; empty tensors lie nowhere.
+    assert abs(clip.grad_norm([a, a]).item() - _norm([a, a])) <= 5 * U * _norm([a, a])
+    clip.clip_grad_norm([a[:0], a, a[:0]], 0.1)
+    _check_scaled(a, was, _norm([was]), 0.1, 1e-6)

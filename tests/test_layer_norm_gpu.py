@@ -181,7 +181,8 @@ def test_other_layouts_are_copied_or_refused():
                 lambda: ln.layer_norm(c, out=c[:1].expand(3, 8)), lambda: ln.layer_norm(c, out=c[:2]),
                 lambda: ln.layer_norm(c, weight=c), lambda: ln.layer_norm(c, weight=c[0].double()),
                 lambda: ln.layer_norm(c, bias=torch.ones(8)), lambda: ln.layer_norm(c.double()),
-                lambda: ln.layer_norm(torch.tensor(1.0, device=DEV)), lambda: ln.layer_norm(c.half(), out=c.half().float().half()[:, :7]),
+                lambda: ln.layer_norm(torch.tensor(1.0, device=DEV)),
+                lambda: ln.layer_norm(c.half(), out=c.half().float().half()[:, :7]),
                 lambda: ln.layer_norm_backward(c.half(), c, c[:, 0], c[:, 0]),
                 lambda: ln.layer_norm_backward(c, c, c[:, :1], c[:, 0]),
                 lambda: ln.layer_norm_backward(c, c, c[:, 0].half(), c[:, 0])):

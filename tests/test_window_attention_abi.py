@@ -45,11 +45,12 @@ def _forward(lib, **kw):
 
 BAD = [{"dtype": 3}, {"tokens": -1}, {"tokens": 2 ** 31}, {"heads": 0}, {"heads": 3}, {"heads": 65536}, {"kv": 0}, {"dim": 0},
        {"dim": 257}, {"off": None}, {"off": 8 * MB + 2}, {"idx": 2}, {"seqs": -1}, {"window": 0}, {"window": -5}, {"sinks": -1},
-       {"scale": NAN}, {"error": P(2)}, {"q": None}, {"k": None}, {"v": None}, {"q": MB + 1}, {"qt": -1}, {"kh": -1}, {"vt": 2 ** 41},
-       {"lse": 5 * MB + 2}]
+       {"scale": NAN}, {"error": P(2)}, {"q": None}, {"k": None}, {"v": None}, {"q": MB + 1}, {"qt": -1}, {"kh": -1},
+       {"vt": 2 ** 41}, {"lse": 5 * MB + 2}]
 
 
-@pytest.mark.parametrize("bad", BAD + [{"out": None}, {"ot": 63}, {"oh": 63}, {"ot": 192, "oh": 64}])
+@pytest.mark.parametrize("bad", BAD + [{"out": None}, {"ot": 63}, {"oh": 63}, {"ot": 192, "oh": 64},
+                                       {"out": MB}, {"out": 2 * MB}, {"out": 3 * MB}, {"lse": 4 * MB}])
 def test_forward_refuses_before_any_gpu_work(lib, bad):
     assert _forward(lib, **bad) == 1
 
@@ -70,13 +71,15 @@ def _backward(lib, **kw):
              gt=256, qt=256, kt=128, kh=64, vt=128, dqt=256, dkt=128, dvt=128)
     a.update(kw)
     return lib.cb_attention_backward(P(a["go"]), P(a["q"]), P(a["k"]), P(a["v"]), P(a["out"]), P(a["lse"]), a["dtype"], a["tokens"],
-                                     a["heads"], a["kv"], a["dim"], a["gt"], 64, a["qt"], 64, a["kt"], a["kh"], a["vt"], 64, 256, 64,
-                                     P(a["off"]), a["idx"], a["seqs"], a["window"], a["sinks"], a["scale"], P(a["dq"]), P(a["dk"]),
-                                     P(a["dv"]), a["dqt"], 64, a["dkt"], 64, a["dvt"], 64, P(a["work"]), a["nbytes"], a["error"], None)
+                                     a["heads"], a["kv"], a["dim"], a["gt"], 64, a["qt"], 64, a["kt"], a["kh"], a["vt"], 64, 256,
+                                     64, P(a["off"]), a["idx"], a["seqs"], a["window"], a["sinks"], a["scale"], P(a["dq"]), P(a["dk"]),
+                                     P(a["dv"]), a["dqt"], 64, a["dkt"], 64, a["dvt"], 64, P(a["work"]), a["nbytes"], a["error"],
+                                     None)
 
 
 @pytest.mark.parametrize("bad", BAD + [{"go": None}, {"out": None}, {"lse": None}, {"dq": None}, {"dk": None}, {"dv": None},
-                                       {"dqt": 200}, {"dkt": 100}, {"dvt": 63}, {"dq": 9 * MB + 1}])
+                                       {"dqt": 200}, {"dkt": 100}, {"dvt": 63}, {"dq": 9 * MB + 1},
+                                       {"dq": 2 * MB}, {"dk": 11 * MB}, {"dv": MB}, {"dq": 5 * MB}, {"dk": 6 * MB}])
 def test_backward_refuses_before_any_gpu_work(lib, bad):
     assert _backward(lib, **bad) == 1
 
@@ -102,14 +105,15 @@ def _step(lib, **kw):
     a = dict(COMMON, q=MB, k=2 * MB, v=3 * MB, out=4 * MB, capacity=100, qs=256, qh=64, ks=12800, kt=128, kh=64, vs=12800, vt=128,
              vh=64, os=256, oh=64)
     a.update(kw)
-    return lib.cb_attention_step(P(a["q"]), P(a["k"]), P(a["v"]), a["dtype"], a["seqs"], a["capacity"], a["heads"], a["kv"], a["dim"],
-                                 a["qs"], a["qh"], a["ks"], a["kt"], a["kh"], a["vs"], a["vt"], a["vh"], P(a["off"]), a["idx"],
+    return lib.cb_attention_step(P(a["q"]), P(a["k"]), P(a["v"]), a["dtype"], a["seqs"], a["capacity"], a["heads"], a["kv"],
+                                 a["dim"], a["qs"], a["qh"], a["ks"], a["kt"], a["kh"], a["vs"], a["vt"], a["vh"], P(a["off"]), a["idx"],
                                  a["window"], a["sinks"], a["scale"], P(a["out"]), a["os"], a["oh"], P(a["work"]), a["nbytes"],
                                  a["error"], None)
 
 
 @pytest.mark.parametrize("bad", [b for b in BAD if not {"tokens", "lse", "vt", "qt"} & set(b)] + [
-    {"out": None}, {"capacity": -1}, {"capacity": 2 ** 31}, {"os": 63}, {"oh": 10}, {"qs": -1}, {"ks": -1}, {"vt": 2 ** 41}])
+    {"out": None}, {"capacity": -1}, {"capacity": 2 ** 31}, {"os": 63}, {"oh": 10}, {"qs": -1}, {"ks": -1}, {"vt": 2 ** 41},
+    {"out": MB}, {"out": 2 * MB}, {"out": 3 * MB}])
 def test_step_refuses_before_any_gpu_work(lib, bad):
     assert _step(lib, **bad) == 1
 

@@ -403,3 +403,65 @@ def test_refusals():
         wa.window_attention(q, k, k, off, scale=float("nan"))
     with pytest.raises(Exception):
         wa.window_attention(q, k, k, off, out=q[:1].expand(10, 4, 64))
+
+
+def test_results_in_the_place_of_inputs_are_refused():
+    from paper_2609_30656_gb300 import tbe
+    wa = _wa()
+    g = _gen(40)
+    q, k, v, go = (_rand(g, 50, 2, 64, dtype=torch.bfloat16) for _ in range(4))
+    off = _offsets([50])
+    for t in (q, k, v):
+        with pytest.raises(tbe.CbTbeError):
+            wa.window_attention(q, k, v, off, 8, out=t)
+    out, lse = wa.window_attention(q, k, v, off, 8, stats=True)
+    a, b, c = (torch.empty_like(q) for _ in range(3))
+    for grads in ((a, b, b), (a, a, c), (q, b, c), (a, b, go), (out, b, c)):
+        with pytest.raises(tbe.CbTbeError):
+            wa.window_attention_backward(go, q, k, v, out, lse, off, 8, grads=grads)
+    with pytest.raises(tbe.CbTbeError):
+        wa.window_attention_step(q, k.view(50, 1, 2, 64), v.view(50, 1, 2, 64), off[:0].new_ones(50), 8, out=q)
+
+
+@pytest.mark.parametrize("dtype", [*HALVES, torch.float32], ids=str)
+@pytest.mark.parametrize("where", [0, 3, 100, 149])
+def test_keys_of_no_weight(where, dtype):
+    """A score of -inf has the weight 0, the first key's too; a row of only such ones is NaN, as the formula's 0 / 0."""
+    wa = _wa()
+    g = _gen(41)
+    q, k, v = (_rand(g, 150, 1, 64, dtype=dtype) for _ in range(3))
+    q[..., 0] = q[..., 0].abs() + 0.5
+    k[where, 0, 0] = -torch.inf
+    off = _offsets([150])
+    out, lse = wa.window_attention(q, k, v, off, 40, 2, stats=True)
+    seen = visible(150, [150], 40, 2)
+    alone = seen.sum(1) == 1
+    without = seen.clone()
+    without[:, where] = False
+    clean = k.clone()
+    clean[where] = 0
+    want = reference(q, clean, v, without, 0.125)
+    some = without.any(1)
+    check(out[some], (want["out"][0][some], want["out"][1][some]), "out")
+    check(lse[:, some], (want["lse"][0][:, some], want["lse"][1][:, some]), "lse")
+    assert (some | alone).all() and out[~some].isnan().all()
+    step = wa.window_attention_step(q, k.view(1, 150, 1, 64).expand(150, 150, 1, 64), v.view(1, 150, 1, 64).expand(150, 150, 1, 64),
+                                    torch.arange(1, 151, device=DEV), 40, 2)
+    check(step[some], (want["out"][0][some], want["out"][1][some]), "step")
+    assert step[~some].isnan().all()
+
+
+@pytest.mark.parametrize("heads,kv,window", [(2, 1, None), (4, 2, 3000)])
+def test_a_batch_of_nan_is_computed_in_time(heads, kv, window):
+    """Every row is computed again, a key at a time: a row of NaNs is done when its sums are."""
+    wa = _wa()
+    g = _gen(42)
+    T = 60000
+    q, k, v, go = (_rand(g, T, n, 64, dtype=torch.float16) for n in (heads, kv, kv, heads))
+    q.fill_(float("nan"))
+    off = _offsets([T])
+    error = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out, lse = wa.window_attention(q, k, v, off, window, 40, stats=True, error=error)
+    grads = wa.window_attention_backward(go, q, k, v, out, lse, off, window, 40, error=error)
+    assert error.item() == 0
+    assert all(t.isnan().all() for t in (out, lse, *grads))
