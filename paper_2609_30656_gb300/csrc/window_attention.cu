@@ -166,7 +166,7 @@ struct Layout {
 };
 Layout layout(int64_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, int64_t window, int64_t sinks) {
     Layout L;
-    L.room = parts_room(tokens, kv_heads, dim, window, sinks);
+    L.room = parts_room(tokens, heads, kv_heads, dim, window, sinks);
     L.delta = 2 * rows_bytes(tokens);
     L.words = L.delta + rows_bytes(tokens * heads);
     L.list = L.words + 256;

@@ -202,7 +202,7 @@ inline size_t rows_bytes(int64_t tokens) { return static_cast<size_t>((tokens * 
 // bf16, rows of a multiple of 8 and at most 128 values, addresses and strides in multiples of 16 bytes.
 bool tensor_core_rows(const Shape& S, const Heads& h, int heads);
 int sm_count();  // of the current device
-int64_t parts_room(int64_t tokens, int32_t kv_heads, int32_t dim, int64_t window, int64_t sinks);
+int64_t parts_room(int64_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, int64_t window, int64_t sinks);
 int64_t parts_bytes(int64_t room, int32_t kv_heads, int32_t dim);
 bool launch_forward(const Forward& F, cudaStream_t s);
 bool launch_backward(const Backward& B, cudaStream_t s);

@@ -44,12 +44,18 @@ __device__ __forceinline__ int seen_until(const Shape& S, int64_t j) {
     return static_cast<int>(j - S.start[j] < S.sinks ? S.end[j] : min64(S.end[j], j + S.window));
 }
 // A tile of keys whose queries go far beyond their windows (a session's first keys are seen to its end) is
-// taken in parts of so many blocks of queries, whose sums are joined by attention_parts_kernel.
-__host__ __device__ __forceinline__ int part_blocks(int64_t window) {
-    return static_cast<int>(max64(16, min64(window, int64_t{1} << 30) / kTile + 2));
+// taken in parts of so many blocks of queries, whose sums are joined by attention_parts_kernel: as many as a window
+// reaches, and enough to pay for the sums' way through memory. That is 16 times the heads that share the keys where there are
+// many tiles to fill the GPU with; with few the longest decides, and 16 altogether are enough.
+__host__ __device__ __forceinline__ int part_blocks(int64_t window, int group, int64_t tiles, int kv_heads) {
+    const int least = tiles * kv_heads < 8 * 152 ? (16 + group - 1) / group : 16;
+    return static_cast<int>(max64(least, min64(window, int64_t{1} << 30) / kTile + 2));
+}
+__device__ __forceinline__ int part_blocks(const Shape& S) {
+    return part_blocks(S.window, S.group, tiles_of(static_cast<int>(S.tokens)), S.kv_heads);
 }
 __device__ __forceinline__ int parts_of(const Shape& S, int blocks) {
-    const int per = part_blocks(S.window);
+    const int per = part_blocks(S);
     return blocks <= 2 * per ? 0 : (blocks + per - 1) / per;
 }
 
@@ -669,7 +675,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                     it.first = first;
                     it.kv = kv;
                     it.place = place;
-                    const int blocks = tiles_of(max(until - first, 0)), per = part_blocks(B.S.window);
+                    const int blocks = tiles_of(max(until - first, 0)), per = part_blocks(B.S);
                     it.from = place < 0 ? first : first + part * per * kTile;
                     it.blocks = !some ? -1 : (place < 0 ? blocks : max(min(per, blocks - part * per), 0));
                 }
@@ -1000,8 +1006,9 @@ bool launch_typed(const Backward& B, cudaStream_t s) {
 
 }  // namespace
 
-int64_t parts_room(int64_t tokens, int32_t kv_heads, int32_t dim, int64_t window, int64_t sinks) {
-    const int64_t tiles = (tokens + kTile - 1) / kTile, per = part_blocks(window);
+int64_t parts_room(int64_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, int64_t window, int64_t sinks) {
+    const int64_t tiles = (tokens + kTile - 1) / kTile;
+    const int64_t per = part_blocks(window, std::max(1, heads / kv_heads), tiles, kv_heads);
     if (sinks == 0 || dim > 128 || tiles <= 2 * per) return 0;
     // A session's first keys lie in at most so many tiles, each seen by its blocks, two per - 1 of them or more a part.
     const int64_t most = (std::min(sinks, tokens) / kTile + 2) * ((tiles + per - 1) / per * 2);

@@ -98,7 +98,7 @@ def test_workspace_sizes(lib):
     without, some = size(100000, 16, 4, 128, 256, 0, 1), size(100000, 16, 4, 128, 256, 4, 1)
     assert without < some <= without + (256 << 20) + (1 << 20)
     assert size(100000, 16, 4, 128, 256, 10 ** 9, 1) <= without + (256 << 20) + (1 << 20)
-    assert size(2000, 16, 4, 128, 256, 4, 1) == size(2000, 16, 4, 128, 256, 0, 1)
+    assert size(1000, 16, 4, 128, 256, 4, 1) == size(1000, 16, 4, 128, 256, 0, 1)
 
 
 def _step(lib, **kw):
