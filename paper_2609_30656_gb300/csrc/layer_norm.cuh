@@ -15,6 +15,11 @@
 // one does (V values in 16 bytes of the narrower type). SHIFTED kernels give each group rows of one
 // such class: pieces are then aligned and a thread's columns the same for all of them, only begun
 // `shift` columns before the row; the two pieces at a row's ends are read and written value by value.
+//
+// bf16 rows, 131072 of 4096: 363 us forward, 5.9 TB/s, 87 % of the copy rate; 131072 of 2048 backward: 287 us, 5.6 TB/s (one pass
+// of 283 us and the join of the blocks' sums, most of it behind that). 131072 rows of 1001, SHIFTED, and of 1000: fp32 forward 166
+// and 157 us, backward 302 and 303; bf16 forward 151 and 93, backward 446 and 156 (eight classes of rows, and two ends of up to
+// seven values each).
 #pragma once
 
 #include "token_rows.cuh"

@@ -13,6 +13,14 @@
 //
 // Blocks stay, one an SM, and take their share of the work: while a pair of tiles is finished, the queries and first keys of
 // the next are on their way, by a warp that looks ahead at what they see, one that copies, and one that stores.
+//
+// 65536 tokens in sessions of 8192, 16 heads of 128 over 4, window 2048, bf16: 740 us, 1.30 PFLOP/s (67 % of a library
+// product's rate; a key by key kernel took 247 ms). What bounds it: the products wait for the exponentials of a tile and
+// these for the products; Q, K and V are read from shared memory at 77 % of what it gives while products run. One block for
+// each pair of tiles took 879 us, one warp to issue for each tile 241 against 207 us at 16384 tokens, O written to global
+// memory by its threads 3900 clocks a tile. Small heads are bound by the exponentials (16 a clock and SM): 16384 tokens x 8
+// heads of 64, window 512: 49 us where heads share keys in fours and 51 where none does. Sessions of 60 tokens (30000 tokens x
+// 4 heads of 32, window 50) take 32 us: 3 blocks of keys a pair of tiles, whose latencies nothing hides.
 #include "window_attention_tc.cuh"
 
 #include <algorithm>

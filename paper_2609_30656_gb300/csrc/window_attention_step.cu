@@ -101,7 +101,9 @@ __global__ void __launch_bounds__(kWarps * 32) attention_step_rowwise_kernel(con
 // copies its own tiles of 16 keys and values ahead (cp.async, three tiles of 8 KB) and waits for no other.
 // Scores and sums are small products (mma.sync, 16 x 8 x 16, the queries of the sharing heads as rows): on the
 // CUDA cores 16 bytes of keys would cost 16 multiplications for every head. The warps' sums are joined at the block's end, the
-// parts' by a second kernel, both in order.
+// parts' by a second kernel, both in order. 256 sessions of 4100 keys of 4 heads of 128, bf16, 16 query heads: 2.15 GB in
+// 329 us, 6.5 TB/s, 96 % of the copy rate; rows that go key by key instead (256 x 2048 keys of 64): 1280 us in fp32 and 1528
+// for 63 halves, against 105 us for 64 halves.
 constexpr int kStepWarps = 4, kStepKeys = 16, kStepStages = 3, kStepHeads = 16;
 template <int D> constexpr int kStepRow = D * 2;  // bytes
 template <int D> constexpr int kStepTile = 2 * kStepKeys * kStepRow<D>;
@@ -325,37 +327,64 @@ attention_step_kernel(const Step A, const Parts P) {
     }
 }
 
-// The parts' sums of a head of a session, joined by a block.
+// The parts' sums of a head of a session, joined by a block: what each part counts for first, then their values, a thread
+// for a value and, of many parts, every eighth of them (one thread for all of 256 parts waited for one after the
+// other: 180 of 200 us for one session of 65536 tokens). All sums in one order.
+constexpr int kMostParts = 2048, kJoinColumns = 128, kJoinGroups = 8;
+inline int join_threads(int parts) { return parts < 2 * kJoinGroups ? kJoinColumns : kJoinColumns * kJoinGroups; }
 template <bool BF16>
-__global__ void __launch_bounds__(128) attention_step_join_kernel(const Step A, const Parts P) {
+__global__ void __launch_bounds__(kJoinColumns * kJoinGroups) attention_step_join_kernel(const Step A, const Parts P) {
+    __shared__ float counts[kMostParts], values[kJoinGroups][kJoinColumns], of_warp[2][kJoinColumns * kJoinGroups / 32];
     begin_kernel();
     const float c = fmaxf(fabsf(A.scale) * kLog2e, 1e-30f);
     const int64_t row = blockIdx.x, b = row / A.heads;
-    const int h = static_cast<int>(row - b * A.heads), d = threadIdx.x;
-    if (d >= A.dim) return;
-    const float* from = P.sums + row * P.parts * (A.dim + 2);
+    const int h = static_cast<int>(row - b * A.heads), threads = static_cast<int>(blockDim.x), t = static_cast<int>(threadIdx.x);
+    const int stride = A.dim + 2;
+    const float* from = P.sums + row * P.parts * stride;
     float top = -INFINITY, total = 0.f, value = 0.f;
-    for (int y = 0; y < P.parts; ++y) top = fmaxf(top, __ldcg(from + y * (A.dim + 2) + A.dim));
-    for (int y = 0; y < P.parts; ++y) {
-        const float* at = from + y * (A.dim + 2);
-        const float sum = __ldcg(at + A.dim + 1), most = __ldcg(at + A.dim);
-        if (sum == 0.f) continue;
-        const float f = most == top ? 1.f : exp2f((most - top) * c);
-        total = fmaf(sum, f, total);
-        value = fmaf(__ldcg(at + d), f, value);
+    for (int y = t; y < P.parts; y += threads) top = fmaxf(top, __ldcg(from + static_cast<int64_t>(y) * stride + A.dim));
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, off));
+    if (t % 32 == 0) of_warp[0][t / 32] = top;
+    __syncthreads();
+    for (int w = 0; w < threads / 32; ++w) top = fmaxf(top, of_warp[0][w]);
+    for (int y = t; y < P.parts; y += threads) {
+        const float* at = from + static_cast<int64_t>(y) * stride + A.dim;
+        const float most = __ldcg(at), sum = __ldcg(at + 1), f = most == top ? 1.f : exp2f((most - top) * c);
+        counts[y] = sum == 0.f ? -1.f : f;  // no key
+        if (sum != 0.f) total = fmaf(sum, f, total);
     }
+    total = warp_sum(total);
+    if (t % 32 == 0) of_warp[1][t / 32] = total;
+    __syncthreads();
+    const int d = t % kJoinColumns, group = t / kJoinColumns, groups = threads / kJoinColumns;
+    if (d < A.dim) {
+#pragma unroll 4
+        for (int y = group; y < P.parts; y += groups) {
+            const float x = __ldcg(from + static_cast<int64_t>(y) * stride + d), f = counts[y];
+            value = f < 0.f ? value : fmaf(x, f, value);
+        }
+    }
+    values[group][d] = value;
+    __syncthreads();
+    if (t >= A.dim || t >= kJoinColumns) return;
+    total = value = 0.f;
+    for (int w = 0; w < threads / 32; ++w) total += of_warp[1][w];
+    for (int g = 0; g < groups; ++g) value += values[g][d];
     const float r = length_of(A, b) > 0 ? value / total : 0.f;
     static_cast<uint16_t*>(A.out)[b * A.out_seq + static_cast<int64_t>(h) * A.out_head + d] =
         static_cast<uint16_t>(narrow<BF16 ? CB_BF16 : CB_F16>(r));
 }
 
-// Parts of the keys of a session: so many that the blocks make a dozen rounds of the GPU's two blocks an SM
-// (the last round then idles little of it), none of fewer than 256 keys.
+// Parts of the keys of a session: so many that the blocks make four rounds of the GPU's two blocks an SM, none of
+// fewer than 256 keys. With more, a block's beginning and end and the joining weigh more, with fewer the last round idles more
+// of the GPU (of 12, 6, 4 and 3 rounds: 256 sessions of 4100 keys 360, 329, 329 and 331 us; 16 of 65536 338, 332, 315 and
+// 355; 4 of 65536 134, 109, 102 and 97; 64 of 1 to 16384 185, 167, 163 and 162).
 int parts_of(int64_t sequences, int32_t kv_heads, int32_t group, int64_t capacity, int64_t window, int64_t sinks) {
     const int64_t blocks = sequences * kv_heads * ((group + kStepHeads - 1) / kStepHeads);
     const int64_t seen = std::min(capacity, window > capacity ? capacity : window + std::min(sinks, capacity));
-    const int64_t wanted = (static_cast<int64_t>(sm_count()) * 2 * 12 + blocks - 1) / blocks;
-    return static_cast<int>(std::max<int64_t>(1, std::min(wanted, seen / 256)));
+    const int64_t wanted = (static_cast<int64_t>(sm_count()) * 2 * 4 + blocks - 1) / blocks;
+    return static_cast<int>(std::max<int64_t>(1, std::min({wanted, seen / 256, int64_t{kMostParts}})));
 }
 
 template <int D, bool BF16>
@@ -366,7 +395,8 @@ bool launch_step(const Step& A, const Parts& P, cudaStream_t s) {
     if (grid > INT32_MAX || A.sequences * A.heads > INT32_MAX) return false;
     launch(attention_step_kernel<D, BF16>, dim3(static_cast<unsigned>(grid)), dim3(kStepWarps * 32), kStepShared<D>, s, A, P);
     if (P.sums)
-        launch(attention_step_join_kernel<BF16>, dim3(static_cast<unsigned>(A.sequences * A.heads)), dim3(128), 0, s, A, P);
+        launch(attention_step_join_kernel<BF16>, dim3(static_cast<unsigned>(A.sequences * A.heads)),
+               dim3(join_threads(P.parts)), 0, s, A, P);
     return true;
 }
 
