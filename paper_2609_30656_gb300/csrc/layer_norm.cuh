@@ -14,12 +14,11 @@
 // Rows whose length or stride is no multiple of 16 bytes still lie at every V-th row as the first
 // one does (V values in 16 bytes of the narrower type). SHIFTED kernels give each group rows of one
 // such class: pieces are then aligned and a thread's columns the same for all of them, only begun
-// `shift` columns before the row; the two pieces at a row's ends are read and written value by value.
+// `shift` columns before the row; the two pieces at a row's ends are written value by value (and read so in fp32).
 //
 // bf16 rows, 131072 of 4096: 363 us forward, 5.9 TB/s, 87 % of the copy rate; 131072 of 2048 backward: 287 us, 5.6 TB/s (one pass
 // of 283 us and the join of the blocks' sums, most of it behind that). 131072 rows of 1001, SHIFTED, and of 1000: fp32 forward 166
-// and 157 us, backward 302 and 303; bf16 forward 151 and 93, backward 446 and 156 (eight classes of rows, and two ends of up to
-// seven values each).
+// and 157 us, backward 302 and 303; bf16 forward 124 and 93, backward 305 and 156 (two ends of up to seven values each to write).
 #pragma once
 
 #include "token_rows.cuh"
@@ -91,6 +90,7 @@ __device__ __forceinline__ void group_sum(float (&v)[N], float* shared, int& tur
 template <int G> constexpr int kBlock = G == 32 ? 128 : G;
 
 // A thread's pieces of a row: V values each, piece p G * V columns behind piece p - 1.
+template <int DT, bool SHIFTED> constexpr bool kEnds = SHIFTED && (DT == CB_F16 || DT == CB_BF16);  // read whole (read_piece)
 template <int DT, int V, int G, bool SHIFTED>
 struct Columns {
     int first, dim;
@@ -100,6 +100,13 @@ struct Columns {
         return SHIFTED ? c >= 0 && c < dim : at(p) < dim;  // without a shift pieces are in whole
     }
     __device__ __forceinline__ bool whole(int p) const { return SHIFTED ? at(p) >= 0 && at(p) + V <= dim : at(p) < dim; }
+    __device__ __forceinline__ bool some(int p) const { return at(p) + V > 0 && at(p) < dim; }
+    // Values of a piece that are not the row's give 0.
+    __device__ __forceinline__ void mask(int p, float (&f)[V]) const {
+        if constexpr (kEnds<DT, SHIFTED>)
+#pragma unroll
+            for (int i = 0; i < V; ++i) f[i] = in(p, i) ? f[i] : 0.f;
+    }
 };
 
 template <int DT, int V> struct RowPiece { Piece<DT, V> v; };
@@ -107,12 +114,16 @@ template <int V> struct RowPiece<kAny, V> { uint32_t v; };
 
 template <int DT, int V, int G, bool SHIFTED>
 __device__ __forceinline__ void read_piece(RowPiece<DT, V>& to, const Columns<DT, V, G, SHIFTED>& C, int p, const void* x,
-                                           int64_t row, int dtype) {
+                                           int64_t row, int64_t all, int dtype) {
     if constexpr (DT == kAny) {
         to.v = C.in(p, 0) ? any_bits(x, row + C.at(p), dtype) : 0u;
     } else {
-        const char* at = static_cast<const char*>(x) + (row + C.at(p)) * kBytes<DT>;
-        if (C.whole(p)) {
+        // Halves at a row's end are read as a whole piece too, their neighbours with them (masked where they are used), but for
+        // the first and last of all, before and behind which there may be nothing: put together one by one they are waited for,
+        // before the row at hand is worked on (131072 rows of 1001 bf16 backward: 446 against 305 us). Words arrive by themselves.
+        const int64_t first = row + C.at(p);
+        const char* at = static_cast<const char*>(x) + first * kBytes<DT>;
+        if (C.whole(p) || (kEnds<DT, SHIFTED> && C.some(p) && first >= 0 && first + V <= all)) {
             to.v = load_piece<DT, V, false>(at);
         } else {
             to.v = zero_piece<DT, V>();
@@ -168,11 +179,12 @@ layer_norm_kernel(const Args A) {
     int64_t row = static_cast<int64_t>(blockIdx.x) * kAtOnce + threadIdx.x / G;
     const auto C = columns<DT, V, G, SHIFTED>(A, row);
     begin_kernel();
+    const int64_t all = (A.rows - 1) * A.x_row + A.dim;
     RowPiece<DT, V> next[P];
     auto load = [&](int64_t r) {
         if (r < A.rows)
 #pragma unroll
-            for (int p = 0; p < P; ++p) read_piece<DT, V, G, SHIFTED>(next[p], C, p, A.x, r * A.x_row, A.in_dtype);
+            for (int p = 0; p < P; ++p) read_piece<DT, V, G, SHIFTED>(next[p], C, p, A.x, r * A.x_row, all, A.in_dtype);
     };
     load(row);
     float w[kValues], b[kValues];
@@ -191,6 +203,7 @@ layer_norm_kernel(const Args A) {
         for (int p = 0; p < P; ++p) {
             float f[V];
             piece_values<DT, V>(next[p], f, A.in_dtype);
+            C.mask(p, f);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 v[p * V + i] = f[i];
@@ -234,14 +247,15 @@ layer_norm_backward_kernel(const Args A) {
     int64_t row = static_cast<int64_t>(blockIdx.x) * kAtOnce + threadIdx.x / G;
     const auto C = columns<DT, V, G, SHIFTED>(A, row);
     begin_kernel();
+    const int64_t all = (A.rows - 1) * A.x_row + A.dim, dy_all = (A.rows - 1) * A.dy_row + A.dim;
     RowPiece<DT, V> x_next[P], dy_next[P];
     float mean_next = 0.f, rstd_next = 0.f;
     auto load = [&](int64_t r) {
         if (r >= A.rows) return;
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            read_piece<DT, V, G, SHIFTED>(x_next[p], C, p, A.x, r * A.x_row, A.in_dtype);
-            read_piece<DT, V, G, SHIFTED>(dy_next[p], C, p, A.dy, r * A.dy_row, A.in_dtype);
+            read_piece<DT, V, G, SHIFTED>(x_next[p], C, p, A.x, r * A.x_row, all, A.in_dtype);
+            read_piece<DT, V, G, SHIFTED>(dy_next[p], C, p, A.dy, r * A.dy_row, dy_all, A.in_dtype);
         }
         mean_next = A.mean[r];
         rstd_next = A.rstd[r];
@@ -269,6 +283,7 @@ layer_norm_backward_kernel(const Args A) {
             float f[V], d[V];
             piece_values<DT, V>(x[p], f, A.in_dtype);
             piece_values<DT, V>(dy[p], d, A.in_dtype);
+            C.mask(p, d);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int k = p * V + i;

@@ -292,3 +292,25 @@ def test_offsets_past_32_bits():
     y, mean, rstd = ln.layer_norm(x, stats=True)
     check_forward(x, None, None, 1e-5, y, mean, rstd)
     assert math.isfinite(y.float().sum().item())
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("gap", [0, 1, 5])
+@pytest.mark.parametrize("dim", [1, 7, 33, 1001])
+def test_neighbours_at_a_rows_ends_stay_out_of_it(dim, gap, dtype):
+    """Odd rows share 16-byte pieces with the rows (or what lies between them) before and behind."""
+    from paper_2609_30656_gb300 import layer_norm as ln
+    g = torch.Generator(device=DEV)
+    g.manual_seed(dim)
+    x, dy = (torch.randn(41, dim + gap, generator=g, device=DEV).to(dtype) for _ in range(2))
+    w = torch.randn(dim, generator=g, device=DEV)
+    clean = [t.clone()[:, :dim] for t in (x, dy)]  # lying alike: a row's sums go by where it begins
+    for t in (x, dy):
+        t[::2] = float("nan")
+        t[:, dim:] = float("inf")
+    runs = []
+    for a, b in ((x[:, :dim], dy[:, :dim]), clean):
+        y, mean, rstd = ln.layer_norm(a, w, w, stats=True)
+        runs.append((y, mean, rstd, ln.layer_norm_backward(b, a, mean, rstd, w)[0]))
+    for got, want in zip(*runs):
+        assert torch.equal(got[1::2], want[1::2]) and got[::2].isnan().all()
