@@ -52,8 +52,9 @@ __device__ __forceinline__ int seen_until(const Shape& S, int64_t j) {
 // A tile of keys whose queries go far beyond their windows (a session's first keys are seen to its end) is
 // taken in parts of so many blocks of queries, whose sums are joined by attention_parts_kernel: as many as a window
 // reaches, and enough to pay for the sums' way through memory. That is 16 times the heads that share the keys where there are
-// many tiles to fill the GPU with; with few the longest decides, and 16 altogether are enough. One session of 23100 tokens: 1077
-// us in one piece, 149 in parts; 33 sessions of 27 to 2379 tokens x 8 heads over 2: 242 with the larger parts, 215 with the smaller.
+// many tiles to fill the GPU with; with few the longest decides, and 16 altogether are enough. One session of 23100
+// tokens: 1077 us in one piece, 149 in parts; 33 sessions of 27 to 2379 tokens x 8 heads over 2: 242 with the larger parts,
+// 215 with the smaller.
 __host__ __device__ __forceinline__ int part_blocks(int64_t window, int group, int64_t tiles, int kv_heads) {
     const int least = tiles * kv_heads < 8 * 152 ? (16 + group - 1) / group : 16;
     return static_cast<int>(max64(least, min64(window, int64_t{1} << 30) / kTile + 2));
@@ -1001,7 +1002,8 @@ bool launch_typed(const Backward& B, cudaStream_t s) {
         return false;
     const int64_t key_tiles = (S.tokens + kTile - 1) / kTile * S.kv_heads, items = work_items(S);
     if (items > INT32_MAX / 2 || key_tiles > INT32_MAX / 4) return false;
-    launch(attention_delta_kernel<D, BF16>, dim3(warp_grid((S.tokens * S.heads * D / 8 + 31) / 32, 8 * sm_count())), dim3(kDeltaThreads), 0, s, B);
+    launch(attention_delta_kernel<D, BF16>, dim3(warp_grid((S.tokens * S.heads * D / 8 + 31) / 32, 8 * sm_count())),
+           dim3(kDeltaThreads), 0, s, B);
     launch(attention_dkv_kernel<D, BF16>, dim3(static_cast<unsigned>(std::min<int64_t>(key_tiles, sm_count()))), dim3(kThreads),
            kKeyShared<D>, s, qm, km, vm, gm, dkm, dvm, B);
     const int64_t joined = std::min<int64_t>(static_cast<int64_t>(B.order.room) * S.kv_heads, 8 * sm_count());
