@@ -607,6 +607,7 @@ cb_status cb_attention_backward(const void* grad_out, const void* q, const void*
 /* The same for one new token of each session, the last one in its cache: session b has lengths[b] tokens
  * there, position p at k_cache + b * k_sequence_stride + p * k_token_stride + head * k_head_stride values (v_cache
  * alike), and its query sees position p where lengths[b] - 1 - p < window or p < sinks. A session without tokens gets zeros.
+ *   capacity    < 2^31 - 1024
  *   lengths     device, idx_dtype, [sequences], 0 .. capacity; one outside sets `error` (if it holds 0) to
  *               CB_ERR_INDEX_OOB and counts as none
  * The rest as above. */

@@ -83,7 +83,7 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
     unsigned char* queries = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~uintptr_t(1023));
     unsigned char* ring = queries + 2 * kRows;
     unsigned char* output = ring + 2 * S * kRows;  // of one tile after the other
-    __shared__ uint64_t q_full, q_empty, full[S], empty[S], scores[2], part[2][kParts], sums[2], staged[2], stored;
+    __shared__ uint64_t q_full, q_empty, full[S], empty[S], scores[2], part[2][kParts], sums[2], staged[2], stored[2];
     __shared__ uint64_t item_full[2], item_empty[2];
     __shared__ uint32_t tmem_at;
     __shared__ Item info[2];
@@ -92,12 +92,12 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
     if (threadIdx.x == 0) {
         tc::barrier_init(tc::smem_addr(&q_full), 1);
         tc::barrier_init(tc::smem_addr(&q_empty), 1);
-        tc::barrier_init(tc::smem_addr(&stored), 1);
         for (int i = 0; i < 2; ++i) {
             tc::barrier_init(tc::smem_addr(scores + i), 1);
             for (int k = 0; k < kParts; ++k) tc::barrier_init(tc::smem_addr(part[i] + k), 4);
             tc::barrier_init(tc::smem_addr(sums + i), 1);
             tc::barrier_init(tc::smem_addr(staged + i), 4);
+            tc::barrier_init(tc::smem_addr(stored + i), 1);
             tc::barrier_init(tc::smem_addr(item_full + i), 1);
             tc::barrier_init(tc::smem_addr(item_empty + i), kSoftmaxWarps + 3);
         }
@@ -149,7 +149,7 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
                         for (int d = 0; d < D / 64; ++d)
                             tma_store(&om, tc::smem_addr(output) + d * kBoxBytes, d * 64, W.head[x], W.token[x]);
                     tma_store_done();
-                    tc::barrier_arrive(tc::smem_addr(&stored));
+                    tc::barrier_arrive(tc::smem_addr(stored + x));
                 }
             }
         } else if (warp == kCopyWarp && tc::elect()) {
@@ -365,8 +365,10 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
                 sums_phase ^= 1;
             }
             tc::fence_after();
-            // The tiles take turns in the output's place, once the store before has read it.
-            if (!ok || !(ok = warp_wait(&stored, mine ^ 1))) break;
+            // The tiles take turns in the output's place, once the store before has read it. (Each waits for every phase of
+            // a barrier of its own: a wait that skips phases takes the one two before for its own, where items without a
+            // key follow one another.)
+            if (!ok || !(ok = warp_wait(stored + (mine ^ 1), mine ? n : n ^ 1))) break;
             const float2 both = add2(sum0, sum1);
             const float sum = both.x + both.y;
             const float inv = 1.f / sum;  // rows that see nothing do not use it
