@@ -415,8 +415,8 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
                     if (!meet(g_full, n) || !meet(g_full + 1, n) || !meet(&v_full, i_all)) break;
                     if (use[0] && !multiply_grads(0)) break;
                     if (use[1]) multiply(1, q0, key, scores);
-                } else if (!meet(g_full, n) || !meet(g_full + 1, n)) {  // no phase is skipped: a later wait could take it for its
-                    break;
+                } else if (!meet(g_full, n) || !meet(g_full + 1, n)) {
+                    break;  // no phase is skipped: a later wait could take it for its own
                 }
                 if (blocks.count <= 1) commit(&q_empty);
                 for (int i = 0; i < blocks.count; ++i, ++i_all) {

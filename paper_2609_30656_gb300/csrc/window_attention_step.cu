@@ -405,7 +405,8 @@ constexpr int64_t kMost = int64_t{1} << 40;
 bool stride_ok(int64_t s) { return s >= 0 && s <= kMost; }
 bool sizes_ok(int64_t sequences, int64_t capacity, int32_t heads, int32_t kv_heads, int32_t dim, int64_t window, int64_t sinks) {
     return sequences >= 0 && sequences < (int64_t{1} << 31) && capacity >= 0 && capacity < (int64_t{1} << 31) - 1024 &&
-           heads >= 1 && heads <= 65535 && kv_heads >= 1 && heads % kv_heads == 0 && dim >= 1 && dim <= kMaxDim && window >= 1 && sinks >= 0;
+           heads >= 1 && heads <= 65535 && kv_heads >= 1 && heads % kv_heads == 0 && dim >= 1 &&
+           dim <= kMaxDim && window >= 1 && sinks >= 0;
 }
 
 }  // namespace
