@@ -25,7 +25,8 @@ SOURCES = ["cb_tbe.cu", "tbe_plan.cu", "tbe_forward.cu", "tbe_forward_f32.cu", "
            "tbe_reduce_f16.cu", "tbe_reduce_bf16.cu", "tbe_reduce_f32.cu", "gather_ceiling.cu",
            "token_embedding.cu", "muon.cu", "muon_products.cu", "muon_small.cu",
            "layer_norm.cu", "layer_norm_f32.cu", "layer_norm_f16.cu", "layer_norm_bf16.cu", "clip.cu",
-           "window_attention.cu", "window_attention_step.cu", "window_attention_forward.cu", "window_attention_backward.cu"]
+           "window_attention.cu", "window_attention_step.cu", "window_attention_forward.cu", "window_attention_backward.cu",
+           "window_attention_again.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

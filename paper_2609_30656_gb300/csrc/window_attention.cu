@@ -35,7 +35,7 @@ __global__ void __launch_bounds__(256) attention_rows_kernel(const Shape S) {
         S.start[t] = static_cast<int32_t>(s);
         S.end[t] = static_cast<int32_t>(e);
     }
-    if (S.largest && first < 4) S.largest[first] = 0u;  // and the order's three words
+    if (S.words && first < kWords) S.words[first] = 0u;
     if (!S.error) return;
     for (int64_t i = first; i <= S.sequences; i += step) {
         const int64_t here = load_index(S.offsets, i, S.offsets32);
@@ -52,10 +52,13 @@ __global__ void __launch_bounds__(kWarps * 32) attention_rowwise_kernel(const Fo
     for (int64_t w = warp_id_global(); w < S.tokens * S.heads; w += warps_in_grid()) {
         const int64_t t = w / S.heads;
         const int h = static_cast<int>(w - t * S.heads);
-        float o[kLaneValues], lse;
-        row_output<DT>(F, t, h, o, lse);
+        float o[kLaneValues], most, sum;
+        row_output<DT>(F, t, h, 0, 1, o, most, sum);
+        const bool real = S.end[t] > t;
+#pragma unroll
+        for (int i = 0; i < kLaneValues; ++i) o[i] = real ? o[i] / sum : 0.f;
         store_row<DT>(F.out, t, h, S.dim, o);
-        if (F.lse && (threadIdx.x & 31) == 0) F.lse[h * S.tokens + t] = lse;
+        if (F.lse && (threadIdx.x & 31) == 0) F.lse[h * S.tokens + t] = real ? (most + log2f(sum)) * kLn2 : -INFINITY;
     }
 }
 
@@ -83,7 +86,7 @@ __global__ void __launch_bounds__(kWarps * 32) attention_dq_rowwise_kernel(const
         const int64_t t = w / S.heads;
         const int h = static_cast<int>(w - t * S.heads);
         float dq[kLaneValues];
-        row_dq<DT>(B, t, h, dq);
+        row_dq<DT>(B, t, h, 0, 1, dq);
         store_row<DT>(B.dq, t, h, S.dim, dq);
     }
 }
@@ -97,7 +100,7 @@ __global__ void __launch_bounds__(kWarps * 32) attention_dkv_rowwise_kernel(cons
         const int64_t j = w / S.kv_heads;
         const int kv = static_cast<int>(w - j * S.kv_heads);
         float dk[kLaneValues], dv[kLaneValues];
-        row_dkv<DT, true, true>(B, j, kv, dk, dv);
+        row_dkv<DT, true, true>(B, j, kv, 0, 1, dk, dv);
         store_row<DT>(B.dk, j, kv, S.dim, dk);
         store_row<DT>(B.dv, j, kv, S.dim, dv);
     }
@@ -159,29 +162,38 @@ Shape shape(int dtype, int64_t tokens, int32_t heads, int32_t kv_heads, int32_t 
     S.error = error;
     return S;
 }
-// The backward pass's workspace: bytes before each part of it, and all.
+// The workspace: bytes before each part of it, and all.
 struct Layout {
-    size_t delta, words, list, split, sums, bytes;
+    size_t words, again, delta, list, split, sums, bytes;
     int64_t room;
 };
-Layout layout(int64_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, int64_t window, int64_t sinks) {
-    Layout L;
+Layout layout(int64_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, int64_t window, int64_t sinks, bool backward) {
+    const int64_t tiles = tiles_of(static_cast<int>(tokens));
+    // A warp of the kernels notes 32 rows of a tile at most once for each result; the one that joins parts 16 keys.
+    const int64_t notes = dim % 8 || dim > 128 ? 0 : tiles * (4 * heads + (backward ? 8 * kv_heads : 0));
+    Layout L{};
+    L.words = 2 * rows_bytes(tokens);
+    L.again = L.words + 256;
+    L.delta = L.again + rows_bytes(4 * notes);
+    L.bytes = L.delta;
+    if (!backward) return L;
     L.room = parts_room(tokens, heads, kv_heads, dim, window, sinks);
-    L.delta = 2 * rows_bytes(tokens);
-    L.words = L.delta + rows_bytes(tokens * heads);
-    L.list = L.words + 256;
+    L.list = L.delta + rows_bytes(tokens * heads);
     L.split = L.list + rows_bytes(2 * L.room);
-    L.sums = L.split + (L.room ? rows_bytes(tiles_of(static_cast<int>(tokens))) : 0);
+    L.sums = L.split + (L.room ? rows_bytes(tiles) : 0);
     L.bytes = L.sums + static_cast<size_t>(parts_bytes(L.room, kv_heads, dim));
     return L;
 }
 bool workspace_ok(const void* w, int64_t bytes, int64_t need) {
     return w && reinterpret_cast<uintptr_t>(w) % 256 == 0 && bytes >= need;
 }
-void set_rows(Shape& S, void* workspace, uint32_t* largest, cudaStream_t s) {
-    S.start = static_cast<int32_t*>(workspace);
-    S.end = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + rows_bytes(S.tokens));
-    S.largest = largest;
+void set_rows(Shape& S, Again& again, void* workspace, const Layout& L, cudaStream_t s) {
+    char* base = static_cast<char*>(workspace);
+    S.start = reinterpret_cast<int32_t*>(base);
+    S.end = reinterpret_cast<int32_t*>(base + rows_bytes(S.tokens));
+    S.words = reinterpret_cast<uint32_t*>(base + L.words);
+    S.largest = S.words + kLargest;
+    again = {S.words + kAgainCount, reinterpret_cast<int4*>(base + L.again)};
     const int64_t n = std::max(S.tokens, S.sequences + 1);
     launch(attention_rows_kernel, dim3(static_cast<unsigned>(std::min<int64_t>((n + 255) / 256, 1 << 16))), dim3(256), 0, s, S);
 }
@@ -240,7 +252,7 @@ extern "C" int64_t cb_attention_workspace_bytes(int64_t tokens, int32_t heads, i
     if (tokens <= 0 || tokens > kMostTokens || heads < 1 || heads > 65535 || kv_heads < 1 || dim < 1 || dim > kMaxDim ||
         window < 1 || sinks < 0)
         return 0;
-    return static_cast<int64_t>(backward ? layout(tokens, heads, kv_heads, dim, window, sinks).bytes : 2 * rows_bytes(tokens));
+    return static_cast<int64_t>(layout(tokens, heads, kv_heads, dim, window, sinks, backward != 0).bytes);
 }
 
 extern "C" cb_status cb_attention_forward(const void* q, const void* k, const void* v, cb_dtype dtype, int64_t tokens,
@@ -265,7 +277,7 @@ extern "C" cb_status cb_attention_forward(const void* q, const void* k, const vo
         return CB_ERR_INVALID_ARG;
     if (!workspace_ok(workspace, workspace_bytes, cb_attention_workspace_bytes(tokens, heads, kv_heads, dim, window, sinks, 0)))
         return CB_ERR_CAPACITY;
-    set_rows(F.S, workspace, nullptr, stream);
+    set_rows(F.S, F.again, workspace, layout(tokens, heads, kv_heads, dim, window, sinks, false), stream);
     bool ok = true;
     if (tensor_core_rows(F.S, F.q, heads) && tensor_core_rows(F.S, F.k, kv_heads) && tensor_core_rows(F.S, F.v, kv_heads) &&
         tensor_core_rows(F.S, F.out, heads))
@@ -308,14 +320,13 @@ extern "C" cb_status cb_attention_backward(const void* grad_out, const void* q, 
         return CB_ERR_INVALID_ARG;
     if (!workspace_ok(workspace, workspace_bytes, cb_attention_workspace_bytes(tokens, heads, kv_heads, dim, window, sinks, 1)))
         return CB_ERR_CAPACITY;
-    const Layout L = layout(tokens, heads, kv_heads, dim, window, sinks);
+    const Layout L = layout(tokens, heads, kv_heads, dim, window, sinks, true);
     char* base = static_cast<char*>(workspace);
     B.delta = reinterpret_cast<float*>(base + L.delta);
-    uint32_t* words = reinterpret_cast<uint32_t*>(base + L.words);
-    B.order = {reinterpret_cast<int32_t*>(words + 1), words + 2, words + 3, static_cast<int32_t>(L.room),
-               reinterpret_cast<int2*>(base + L.list),
+    set_rows(B.S, B.again, workspace, L, stream);
+    B.order = {reinterpret_cast<int32_t*>(B.S.words + kOrderParts), B.S.words + kOrderNext, B.S.words + kOrderDone,
+               static_cast<int32_t>(L.room), reinterpret_cast<int2*>(base + L.list),
                reinterpret_cast<int32_t*>(base + L.split), reinterpret_cast<float*>(base + L.sums)};
-    set_rows(B.S, workspace, words, stream);
     bool ok = true;
     bool fast = true;
     for (const Heads* x : {&B.go, &B.q, &B.out, &B.dq}) fast = fast && tensor_core_rows(B.S, *x, heads);

@@ -33,9 +33,11 @@ struct Shape {
     int32_t offsets32;
     int32_t* start;  // [tokens] where the token's session begins, and
     int32_t* end;    // [tokens] ends; both t for a token t of no session
+    uint32_t* words;  // [kWords] in the workspace, 0 before the tensor-core kernels; or null
     uint32_t* largest;  // backward: the bits of the largest finite |grad_out| (of fp16 rows)
     int* error;      // or null
 };
+constexpr int kWords = 8, kLargest = 0, kOrderParts = 1, kOrderNext = 2, kOrderDone = 3, kAgainCount = 4;
 
 // Sum over a warp, in every lane.
 __device__ __forceinline__ float warp_sum(float v) {
@@ -44,10 +46,19 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
+// Rows whose result is not finite, noted by the tensor-core kernels for those that follow them (window_attention_again.cu):
+// the first of 32 tokens, the head (of keys for dK and dV), which of the 32, which result.
+struct Again {
+    uint32_t* count;  // notes: 0 before
+    int4* list;
+};
+enum Result { kOut = 0, kDq = 0, kDk = 1, kDv = 2, kDkAndDv = 3 };
+
 struct Forward {
     Shape S;
     Heads q, k, v, out;
     float* lse;  // [heads, tokens], or null
+    Again again;
 };
 // How the tiles of keys are taken: those in parts first, then the others. (Results do not depend on who takes what.)
 struct Order {
@@ -65,14 +76,17 @@ struct Backward {
     const float* lse;
     float* delta;  // [heads, tokens]
     Order order;
+    Again again;
 };
 
 // ---------------------------------------------------------------- a row at a time
 
-// Rows of any type and length up to 256, by a warp that goes key by key, in fp32. The tensor-core kernels
-// turn to it for a row whose result is not finite: their tiles multiply what a row does not see by
+// Rows of any type and length up to 256, by a warp that goes key by key, in fp32: all of the row (first 0, step 1), or
+// every step-th of its keys from the first-th on. The tensor-core kernels note a row whose result is not finite, and it is
+// computed again this way by a kernel behind them: their tiles multiply what a row does not see by
 // zeros, which infinities and NaNs of other sessions, or of unused memory, survive. A row whose sums have all become NaNs
-// is done: what follows cannot change it, and a batch of NaNs does not cost the row's whole session.
+// is done: what follows cannot change it, and a batch of NaNs does not cost the row's whole session. Warps that share a row
+// tell one another by `stop`.
 constexpr int kMaxDim = 256, kLaneValues = kMaxDim / 32;
 
 // A row of up to 256 values, value lane + 32 i in v[i].
@@ -112,32 +126,41 @@ __device__ __forceinline__ void add_scaled(float (&a)[kLaneValues], float f, con
     for (int i = 0; i < kLaneValues; ++i) a[i] = fmaf(f, b[i], a[i]);
 }
 
-// What token t sees: [start, sinks_end) and [first, t].
+// What token t sees: n tokens, the first `sinks` from `start` on, the others from `first` on. None for one of no session.
 struct Seen {
-    int64_t start, sinks_end, first;
+    int64_t start, sinks, first, n;
+    __device__ __forceinline__ int64_t at(int64_t i) const { return i < sinks ? start + i : first + (i - sinks); }
 };
 __device__ __forceinline__ Seen seen_by(const Shape& S, int64_t t) {
+    if (S.end[t] <= t) return {t, 0, t, 0};
     Seen a;
     a.start = S.start[t];
     a.first = max64(a.start, t - S.window + 1);
-    a.sinks_end = min64(a.start + S.sinks, a.first);
+    a.sinks = min64(S.sinks, a.first - a.start);
+    a.n = a.sinks + t + 1 - a.first;
     return a;
 }
+__device__ __forceinline__ bool stopped(const volatile int* stop) { return stop && *stop; }
+// The sums of these rows have become NaNs.
+__device__ __forceinline__ void stop_all(volatile int* stop) {
+    if (stop) *stop = 1;
+}
 
-// Head h of token t: its output, and its lse.
+// Head h of token t: the sum of its weights 2^(S - most), and of the values by them.
 template <int DT>
-__device__ __forceinline__ void row_output(const Forward& F, int64_t t, int h, float (&o)[kLaneValues], float& lse) {
+__device__ __forceinline__ void row_output(const Forward& F, int64_t t, int h, int first, int step, float (&o)[kLaneValues],
+                                           float& most, float& sum, volatile int* stop = nullptr) {
     const Shape& S = F.S;
     const int kv = h / S.group;
     float q[kLaneValues], k[kLaneValues], v[kLaneValues];
-    float most = -INFINITY, sum = 0.f;
+    most = -INFINITY;
+    sum = 0.f;
 #pragma unroll
     for (int i = 0; i < kLaneValues; ++i) o[i] = 0.f;
-    lse = -INFINITY;
-    if (S.end[t] <= t) return;
     const Seen a = seen_by(S, t);
     load_row<DT>(F.q, t, h, S.dim, q);
-    for (int64_t j = a.start < a.sinks_end ? a.start : a.first; j <= t; j = j + 1 == a.sinks_end ? a.first : j + 1) {
+    for (int64_t i = first; i < a.n && !stopped(stop); i += step) {
+        const int64_t j = a.at(i);
         load_row<DT>(F.k, j, kv, S.dim, k);
         load_row<DT>(F.v, j, kv, S.dim, v);
         const float s = dot(q, k) * (S.scale * kLog2e);
@@ -145,37 +168,37 @@ __device__ __forceinline__ void row_output(const Forward& F, int64_t t, int h, f
         const float p = s == -INFINITY ? 0.f : exp2f(s - top);
         sum = fmaf(sum, keep, p);
 #pragma unroll
-        for (int i = 0; i < kLaneValues; ++i) o[i] = fmaf(o[i], keep, p * v[i]);
+        for (int x = 0; x < kLaneValues; ++x) o[x] = fmaf(o[x], keep, p * v[x]);
         most = top;
-        if (sum != sum) break;
+        if (sum != sum) return stop_all(stop);
     }
-#pragma unroll
-    for (int i = 0; i < kLaneValues; ++i) o[i] /= sum;
-    lse = (most + log2f(sum)) * kLn2;
 }
 template <int DT>
-__device__ __forceinline__ void row_dq(const Backward& B, int64_t t, int h, float (&dq)[kLaneValues]) {
+__device__ __forceinline__ void row_dq(const Backward& B, int64_t t, int h, int first, int step, float (&dq)[kLaneValues],
+                                       volatile int* stop = nullptr) {
     const Shape& S = B.S;
     const int kv = h / S.group;
     float q[kLaneValues], go[kLaneValues], k[kLaneValues], v[kLaneValues];
 #pragma unroll
     for (int i = 0; i < kLaneValues; ++i) dq[i] = 0.f;
-    if (S.end[t] <= t) return;
     const Seen a = seen_by(S, t);
+    if (a.n == 0) return;
     load_row<DT>(B.q, t, h, S.dim, q);
     load_row<DT>(B.go, t, h, S.dim, go);
     const float lse = B.lse[h * S.tokens + t], delta = B.delta[h * S.tokens + t];
-    for (int64_t j = a.start < a.sinks_end ? a.start : a.first; j <= t; j = j + 1 == a.sinks_end ? a.first : j + 1) {
+    for (int64_t i = first; i < a.n && !stopped(stop); i += step) {
+        const int64_t j = a.at(i);
         load_row<DT>(B.k, j, kv, S.dim, k);
         load_row<DT>(B.v, j, kv, S.dim, v);
         const float slope = exp2f((dot(q, k) * S.scale - lse) * kLog2e) * (dot(go, v) - delta) * S.scale;
         add_scaled(dq, slope, k);
-        if (slope != slope) break;
+        if (slope != slope) return stop_all(stop);
     }
 }
 // Head kv of key j, over the heads that share it and the tokens that see it: dk (KEYS) or dv, or both.
 template <int DT, bool KEYS, bool VALUES>
-__device__ __forceinline__ void row_dkv(const Backward& B, int64_t j, int kv, float (&dk)[kLaneValues], float (&dv)[kLaneValues]) {
+__device__ __forceinline__ void row_dkv(const Backward& B, int64_t j, int kv, int first, int step, float (&dk)[kLaneValues],
+                                        float (&dv)[kLaneValues], volatile int* stop = nullptr) {
     const Shape& S = B.S;
     float q[kLaneValues], go[kLaneValues], k[kLaneValues], v[kLaneValues];
 #pragma unroll
@@ -185,8 +208,11 @@ __device__ __forceinline__ void row_dkv(const Backward& B, int64_t j, int kv, fl
     const int64_t last = j - S.start[j] < S.sinks ? end : min64(end, j + S.window);
     load_row<DT>(B.k, j, kv, S.dim, k);
     load_row<DT>(B.v, j, kv, S.dim, v);
-    for (int h = kv * S.group; h < (kv + 1) * S.group; ++h)
-        for (int64_t t = j; t < last; ++t) {
+    const int64_t n = last - j;
+    int64_t i = first;  // of the tokens that see it, head after head
+    for (int h = kv * S.group; h < (kv + 1) * S.group; ++h, i -= n)
+        for (; i < n && !stopped(stop); i += step) {
+            const int64_t t = j + i;
             load_row<DT>(B.q, t, h, S.dim, q);
             load_row<DT>(B.go, t, h, S.dim, go);
             const float p = exp2f((dot(q, k) * S.scale - B.lse[h * S.tokens + t]) * kLog2e);
@@ -196,8 +222,14 @@ __device__ __forceinline__ void row_dkv(const Backward& B, int64_t j, int kv, fl
                 slope = p * (dot(go, v) - B.delta[h * S.tokens + t]) * S.scale;
                 add_scaled(dk, slope, q);
             }
-            if ((VALUES ? p : slope) != (VALUES ? p : slope)) return;
+            if ((VALUES ? p : slope) != (VALUES ? p : slope)) return stop_all(stop);
         }
+}
+
+// By a whole warp, for the 32 tokens from `token` on.
+__device__ __forceinline__ void note_again(const Again& A, uint32_t rows, int64_t token, int head, Result which) {
+    if (rows && (threadIdx.x & 31) == 0)
+        A.list[atomicAdd(A.count, 1u)] = make_int4(static_cast<int>(token), head, static_cast<int>(rows), which);
 }
 
 inline size_t rows_bytes(int64_t tokens) { return static_cast<size_t>((tokens * 4 + 255) / 256 * 256); }
@@ -210,6 +242,8 @@ int64_t parts_room(int64_t tokens, int32_t heads, int32_t kv_heads, int32_t dim,
 int64_t parts_bytes(int64_t room, int32_t kv_heads, int32_t dim);
 bool launch_forward(const Forward& F, cudaStream_t s);
 bool launch_backward(const Backward& B, cudaStream_t s);
+void launch_again(const Forward& F, cudaStream_t s);  // behind them
+void launch_again(const Backward& B, cudaStream_t s);
 
 }  // namespace attention
 }  // namespace cbtbe

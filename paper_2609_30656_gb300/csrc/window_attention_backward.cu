@@ -16,7 +16,7 @@
 // third of dQ's time more). fp16 has five bits for exponents: P goes times 2^12, and dS times the
 // power of two that brings the largest gradient to 16 .. 32, so that small gradients (and loss scales) keep
 // their digits; a value that grows past fp16 all the same makes its row not finite, and such rows are computed
-// again key by key in fp32 (as are those that met an infinity or a NaN behind a mask).
+// again key by key in fp32 by a kernel behind these (as are those that met an infinity or a NaN behind a mask).
 #include "window_attention_tc.cuh"
 
 #include <algorithm>
@@ -158,34 +158,6 @@ __global__ void __launch_bounds__(kDeltaThreads) attention_delta_kernel(const Ba
     if (!last) return;
     __threadfence();
     order_parts(B);
-}
-
-template <bool BF16, int D>
-__device__ __forceinline__ void put_row(const float (&v)[kLaneValues], unsigned char* tile, int r) {
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-        const int c = (threadIdx.x & 31) + 32 * i;
-        *reinterpret_cast<uint16_t*>(tile + tile_byte(r, c / 8) + c % 8 * 2) =
-            static_cast<uint16_t>(narrow<BF16 ? CB_BF16 : CB_F16>(v[i]));
-    }
-}
-template <bool BF16, int D>
-__device__ __noinline__ void dq_again(const Backward& B, int64_t t, int h, unsigned char* tile, int r) {
-    float dq[kLaneValues];
-    row_dq<BF16 ? CB_BF16 : CB_F16>(B, t, h, dq);
-    put_row<BF16, D>(dq, tile, r);
-}
-template <bool BF16, int D>
-__device__ __noinline__ void dkv_again(const Backward& B, int64_t j, int kv, bool keys, unsigned char* tile, int r) {
-    constexpr int DT = BF16 ? CB_BF16 : CB_F16;
-    float dk[kLaneValues], dv[kLaneValues];
-    if (keys) {
-        row_dkv<DT, true, false>(B, j, kv, dk, dv);
-        put_row<BF16, D>(dk, tile, r);
-    } else {
-        row_dkv<DT, false, true>(B, j, kv, dk, dv);
-        put_row<BF16, D>(dv, tile, r);
-    }
 }
 
 // A row of sums from TMEM, times `by`, into its tile in shared memory; whether all are finite.
@@ -537,11 +509,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
             bool finite = true;
             if (count > 0) finite = finish_row<D, BF16>(q_at, B.S.scale / f, r.real, tile, row);
             else zero_row<D>(tile, row);
-            for (uint32_t left = __ballot_sync(kFull, !finite); left; left &= left - 1) {
-                const int other = __ffs(left) - 1;
-                __syncwarp();
-                dq_again<BF16, D>(B, __shfl_sync(kFull, t, other), head, tile, (row & ~31) + other);
-            }
+            note_again(B.again, __ballot_sync(kFull, !finite), t & ~31, head, kDq);
             fence_to_tma();
             tc::fence_before();
             warp_arrive(staged + mine);
@@ -931,11 +899,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
             const float by = half ? B.S.scale / scale_s : exp2f(-kPShift<BF16>);
             if (count > 0) finite = finish_row<D, BF16>(tmem + lanes + 256 + half * D, by, last > 0, tile, row);
             else zero_row<D>(tile, row);
-            for (uint32_t left = __ballot_sync(kFull, !finite); left; left &= left - 1) {
-                const int other = (row & ~31) + __ffs(left) - 1;
-                __syncwarp();
-                dkv_again<BF16, D>(B, first + other, kv, half, tile, other);
-            }
+            note_again(B.again, __ballot_sync(kFull, !finite), first + (row & ~31), kv, half ? kDk : kDv);
             fence_to_tma();
             tc::fence_before();
             warp_arrive(staged + half);
@@ -949,7 +913,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
     if (warp == kMultiplyWarp) tc::tmem_free<1>(tmem, 512);
 }
 
-// The sums of a tile's parts, in order: a block for a tile and head, a warp for a row at a time.
+// The sums of a tile's parts, in order: a block for a tile and head, a warp for 16 rows, one at a time.
 template <int D, bool BF16>
 __global__ void __launch_bounds__(256) attention_parts_kernel(const Backward B) {
     constexpr int DT = BF16 ? CB_BF16 : CB_F16, N = D / 32;
@@ -961,8 +925,11 @@ __global__ void __launch_bounds__(256) attention_parts_kernel(const Backward B) 
         const int2 entry = B.order.list[place];
         if (entry.x < 0 || entry.y != 0) continue;
         const int parts = B.order.split[entry.x];
-        for (int row = threadIdx.x / 32; row < kTile; row += 8) {
-            const int64_t j = static_cast<int64_t>(entry.x) * kTile + row;
+        const int64_t first = static_cast<int64_t>(entry.x) * kTile + threadIdx.x / 32 * 16;
+        uint32_t again = 0u;
+        for (int i = 0; i < 16; ++i) {
+            const int64_t j = first + i;
+            const int row = static_cast<int>(j % kTile);
             if (j >= B.S.tokens) break;
             const bool real = B.S.end[j] > j;
             float v[2][kLaneValues] = {};
@@ -982,10 +949,11 @@ __global__ void __launch_bounds__(256) attention_parts_kernel(const Backward B) 
                     v[h][i] *= by[h];
                     finite &= fabsf(v[h][i]) < INFINITY || lane + 32 * i >= B.S.dim;
                 }
-            if (!__all_sync(kFull, finite)) row_dkv<DT, true, true>(B, j, kv, v[1], v[0]);
+            if (!__all_sync(kFull, finite)) again |= 1u << (j & 31);
             store_row<DT>(B.dv, j, kv, B.S.dim, v[0]);
             store_row<DT>(B.dk, j, kv, B.S.dim, v[1]);
         }
+        note_again(B.again, again, first & ~int64_t{31}, kv, kDkAndDv);
     }
 }
 
@@ -1012,6 +980,7 @@ bool launch_typed(const Backward& B, cudaStream_t s) {
     if (joined > 0) launch(attention_parts_kernel<D, BF16>, dim3(static_cast<unsigned>(joined)), dim3(256), 0, s, B);
     launch(attention_dq_kernel<D, BF16>, dim3(static_cast<unsigned>(std::min<int64_t>(items, sm_count()))), dim3(kThreads),
            kQueryShared<D>, s, qm, km, vm, gm, dqm, B, pairs_heads(S), static_cast<int>(items));
+    launch_again(B, s);
     return true;
 }
 

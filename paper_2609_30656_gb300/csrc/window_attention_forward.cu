@@ -45,18 +45,6 @@ constexpr int kParts = 2;  // in which P goes to the tensor cores
 template <bool BF16> constexpr float kRise = BF16 ? 60.f : 8.f;
 template <bool BF16> constexpr float kShift = BF16 ? 0.f : 6.f;
 
-template <bool BF16, int D>
-__device__ __noinline__ void output_again(const Forward& F, int64_t t, int h, unsigned char* tile, int r) {
-    constexpr int DT = BF16 ? CB_BF16 : CB_F16;
-    float o[kLaneValues], lse;
-    row_output<DT>(F, t, h, o, lse);
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-        const int c = (threadIdx.x & 31) + 32 * i;
-        *reinterpret_cast<uint16_t*>(tile + tile_byte(r, c / 8) + c % 8 * 2) = static_cast<uint16_t>(narrow<DT>(o[i]));
-    }
-}
-
 // Weights 2^(s c + base) of 32 scores, packed, and their sums.
 template <bool BF16, int FROM>
 __device__ __forceinline__ void weigh(const uint32_t (&v)[64], float c, float base, uint32_t (&p)[16], float2& sum0, float2& sum1) {
@@ -390,12 +378,7 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
                     *reinterpret_cast<uint4*>(output + tile_byte(row, (d + k) / 8)) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
-            const bool again = !(check.x + check.y == 0.f);
-            for (uint32_t left = __ballot_sync(kFull, again); left; left &= left - 1) {
-                const int other = __ffs(left) - 1;
-                __syncwarp();
-                output_again<BF16, D>(F, __shfl_sync(kFull, t, other), head, output, (row & ~31) + other);
-            }
+            note_again(F.again, __ballot_sync(kFull, !(check.x + check.y == 0.f)), t & ~31, head, kOut);
             fence_to_tma();
             tc::fence_before();
             warp_arrive(staged + mine);
@@ -428,6 +411,7 @@ bool launch_typed(const Forward& F, cudaStream_t s) {
     if (items > INT32_MAX / 2) return false;
     launch(attention_forward_kernel<D, BF16>, dim3(static_cast<unsigned>(std::min<int64_t>(items, sm_count()))), dim3(kThreads),
            kShared<D>, s, qm, km, vm, om, F, pair_heads, static_cast<int>(items));
+    launch_again(F, s);
     return true;
 }
 
