@@ -169,7 +169,7 @@ struct Layout {
 };
 Layout layout(int64_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, int64_t window, int64_t sinks, bool backward) {
     const int64_t tiles = tiles_of(static_cast<int>(tokens));
-    // A warp of the kernels notes 32 rows of a tile at most once for each result; the one that joins parts 16 keys.
+    // 32 rows of a tile and head are noted at most once for each result.
     const int64_t notes = dim % 8 || dim > 128 ? 0 : tiles * (4 * heads + (backward ? 8 * kv_heads : 0));
     Layout L{};
     L.words = 2 * rows_bytes(tokens);

@@ -226,7 +226,7 @@ __device__ __forceinline__ void row_dkv(const Backward& B, int64_t j, int kv, in
         }
 }
 
-// By a whole warp, for the 32 tokens from `token` on.
+// For the 32 tokens from `token` on, by lane 0 of a warp.
 __device__ __forceinline__ void note_again(const Again& A, uint32_t rows, int64_t token, int head, Result which) {
     if (rows && (threadIdx.x & 31) == 0)
         A.list[atomicAdd(A.count, 1u)] = make_int4(static_cast<int>(token), head, static_cast<int>(rows), which);
