@@ -582,7 +582,7 @@ cb_status cb_grad_clip(const cb_grad_tensor* tensors, int64_t num_tensors, float
  *               a bounded wait ran out, the results then are not whole
  * Errors: CB_ERR_INVALID_ARG before any GPU work; CB_ERR_CUDA if a launch fails or the driver's
  * tensor-map encoder cannot be reached. Nothing is allocated, nothing waits. */
-/* 0 for sizes refused. 8 bytes a token, half a byte a token and head; the backward pass 4 bytes more a token and head, one
+/* 0 for sizes refused. 8 bytes a token, half a byte a token and head; the backward pass 5 bytes more a token and head, one
  * a token and head of keys, and up to 256 MB where sinks are seen by many. */
 int64_t cb_attention_workspace_bytes(int64_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, int64_t window,
                                      int64_t sinks, int backward);

@@ -164,7 +164,7 @@ Shape shape(int dtype, int64_t tokens, int32_t heads, int32_t kv_heads, int32_t 
 }
 // The workspace: bytes before each part of it, and all.
 struct Layout {
-    size_t words, again, delta, list, split, sums, bytes;
+    size_t words, again, delta, largest, list, split, sums, bytes;
     int64_t room;
 };
 Layout layout(int64_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, int64_t window, int64_t sinks, bool backward) {
@@ -178,7 +178,8 @@ Layout layout(int64_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, int6
     L.bytes = L.delta;
     if (!backward) return L;
     L.room = parts_room(tokens, heads, kv_heads, dim, window, sinks);
-    L.list = L.delta + rows_bytes(tokens * heads);
+    L.largest = L.delta + rows_bytes(tokens * heads);
+    L.list = L.largest + rows_bytes(tiles * heads * (kTile / 4));
     L.split = L.list + rows_bytes(2 * L.room);
     L.sums = L.split + (L.room ? rows_bytes(tiles) : 0);
     L.bytes = L.sums + static_cast<size_t>(parts_bytes(L.room, kv_heads, dim));
@@ -192,7 +193,6 @@ void set_rows(Shape& S, Again& again, void* workspace, const Layout& L, cudaStre
     S.start = reinterpret_cast<int32_t*>(base);
     S.end = reinterpret_cast<int32_t*>(base + rows_bytes(S.tokens));
     S.words = reinterpret_cast<uint32_t*>(base + L.words);
-    S.largest = S.words + kLargest;
     again = {S.words + kAgainCount, reinterpret_cast<int4*>(base + L.again)};
     const int64_t n = std::max(S.tokens, S.sequences + 1);
     launch(attention_rows_kernel, dim3(static_cast<unsigned>(std::min<int64_t>((n + 255) / 256, 1 << 16))), dim3(256), 0, s, S);
@@ -323,6 +323,8 @@ extern "C" cb_status cb_attention_backward(const void* grad_out, const void* q, 
     const Layout L = layout(tokens, heads, kv_heads, dim, window, sinks, true);
     char* base = static_cast<char*>(workspace);
     B.delta = reinterpret_cast<float*>(base + L.delta);
+    B.largest = reinterpret_cast<uint8_t*>(base + L.largest);
+    B.padded = static_cast<int64_t>(tiles_of(static_cast<int>(tokens))) * kTile;
     set_rows(B.S, B.again, workspace, L, stream);
     B.order = {reinterpret_cast<int32_t*>(B.S.words + kOrderParts), B.S.words + kOrderNext, B.S.words + kOrderDone,
                static_cast<int32_t>(L.room), reinterpret_cast<int2*>(base + L.list),

@@ -34,10 +34,9 @@ struct Shape {
     int32_t* start;  // [tokens] where the token's session begins, and
     int32_t* end;    // [tokens] ends; both t for a token t of no session
     uint32_t* words;  // [kWords] in the workspace, 0 before the tensor-core kernels; or null
-    uint32_t* largest;  // backward: the bits of the largest finite |grad_out| (of fp16 rows)
     int* error;      // or null
 };
-constexpr int kWords = 8, kLargest = 0, kOrderParts = 1, kOrderNext = 2, kOrderDone = 3, kAgainCount = 4;
+constexpr int kWords = 4, kOrderParts = 0, kOrderNext = 1, kOrderDone = 2, kAgainCount = 3;
 
 // Sum over a warp, in every lane.
 __device__ __forceinline__ float warp_sum(float v) {
@@ -75,6 +74,8 @@ struct Backward {
     Heads go, q, k, v, out, dq, dk, dv;
     const float* lse;
     float* delta;  // [heads, tokens]
+    uint8_t* largest;  // fp16: [heads, padded] the exponent (as of its fp32) of each row's largest finite |grad_out|, 0: all zeros
+    int64_t padded;    // tokens in whole tiles
     Order order;
     Again again;
 };

@@ -13,9 +13,10 @@
 //
 // P and dS are operands in the rows' type: dS's rounding adds to dQ and dK about what the rounding of the results does (off by
 // 2.5e-3 of their norm against 1.7e-3 in bf16, 3.2e-4 against 2.1e-4 in fp16; a second product for what it cuts off would be a
-// third of dQ's time more). fp16 has five bits for exponents: P goes times 2^12, and dS times the
-// power of two that brings the largest gradient to 16 .. 32, so that small gradients (and loss scales) keep
-// their digits; a value that grows past fp16 all the same makes its row not finite, and such rows are computed
+// third of dQ's time more). fp16 has five bits for exponents: P goes times 2^12, and dS times a power of two of the row's own,
+// which its thread takes out of the sums again. It brings the largest |grad_out| that the row's sums hold to 16 .. 32: of the
+// token itself for dQ, of the tokens that see the key for dK. So small gradients (and loss scales) keep
+// their digits, whatever those of other sessions, heads or tokens out of sight are; a value that grows past fp16 all the same makes its row not finite, and such rows are computed
 // again key by key in fp32 by a kernel behind these (as are those that met an infinity or a NaN behind a mask).
 #include "window_attention_tc.cuh"
 
@@ -37,11 +38,9 @@ constexpr int kStatWarp = 11;   // over keys
 constexpr int kQueryMore = 208, kQueryFewer = 88, kKeyMore = 208, kKeyFewer = 88;
 
 template <bool BF16> constexpr float kPShift = BF16 ? 0.f : 12.f;
-template <bool BF16>
-__device__ __forceinline__ float slope_scale(const Shape& S) {
-    if constexpr (BF16) return 1.f;
-    const uint32_t bits = *S.largest;
-    return bits == 0 ? 1.f : exp2f(static_cast<float>(4 - ilogbf(__uint_as_float(bits))));
+// The power of two that brings values of this exponent (a byte of Backward::largest) to 16 .. 32.
+__device__ __forceinline__ float slope_scale(uint32_t exponent) {
+    return exponent ? __uint_as_float((127 + 4 + 127 - exponent) << 23) : 1.f;
 }
 
 // Behind the last token that sees key j, 0 for a token of no session.
@@ -103,7 +102,7 @@ __device__ __forceinline__ void order_parts(const Backward& B) {
     if (threadIdx.x == 0) *O.parts = before;
 }
 
-// delta, and the largest |grad_out|: 16 bytes a lane, D / 8 lanes a row.
+// delta, and each row's largest |grad_out|: 16 bytes a lane, D / 8 lanes a row.
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kDeltaThreads) attention_delta_kernel(const Backward B) {
     constexpr int DT = BF16 ? CB_BF16 : CB_F16, kLanes = D / 8, kRowsAtOnce = 32 / kLanes;
@@ -111,9 +110,8 @@ __global__ void __launch_bounds__(kDeltaThreads) attention_delta_kernel(const Ba
     const Shape& S = B.S;
     const int lane = threadIdx.x & 31, c = lane % kLanes * 8;
     const int64_t rows = S.tokens * S.heads;
-    float largest = 0.f;
     for (int64_t i = warp_id_global() * kRowsAtOnce + lane / kLanes; i - lane / kLanes < rows; i += warps_in_grid() * kRowsAtOnce) {
-        float a[8] = {}, b[8] = {}, sum = 0.f;
+        float a[8] = {}, b[8] = {}, sum = 0.f, largest = 0.f;
         const int64_t t = i / S.heads;
         const int h = static_cast<int>(i - t * S.heads);
         if (i < rows && c < S.dim) {
@@ -128,6 +126,12 @@ __global__ void __launch_bounds__(kDeltaThreads) attention_delta_kernel(const Ba
 #pragma unroll
         for (int off = kLanes / 2; off >= 1; off >>= 1) sum += __shfl_xor_sync(kFull, sum, off);
         if (i < rows && lane % kLanes == 0) B.delta[h * S.tokens + t] = sum;
+        if constexpr (!BF16) {
+#pragma unroll
+            for (int off = kLanes / 2; off >= 1; off >>= 1) largest = fmaxf(largest, __shfl_xor_sync(kFull, largest, off));
+            if (i < rows && lane % kLanes == 0)
+                B.largest[h * B.padded + t] = static_cast<uint8_t>(__float_as_uint(largest) >> 23);
+        }
     }
     // In how many parts each tile of keys is to be taken, where some may be.
     const int tiles = B.order.room ? tiles_of(static_cast<int>(S.tokens)) : 0;
@@ -138,16 +142,6 @@ __global__ void __launch_bounds__(kDeltaThreads) attention_delta_kernel(const Ba
         for (int k = 0; k < kTile / 32; ++k) until = max(until, seen_until(S, from + k * 32 + lane));
         until = __reduce_max_sync(kFull, until);
         if (lane == 0) B.order.split[w] = parts_of(S, tiles_of(max(until - from, 0)));
-    }
-    if constexpr (!BF16) {  // an atomic a block: one for each warp of 39000 took 20 us by themselves
-        __shared__ uint32_t of_warp[kDeltaThreads / 32];
-        const uint32_t most = __reduce_max_sync(kFull, __float_as_uint(largest));
-        if (lane == 0) of_warp[threadIdx.x / 32] = most;
-        __syncthreads();
-        if (threadIdx.x < 32) {
-            const uint32_t all = __reduce_max_sync(kFull, lane < kDeltaThreads / 32 ? of_warp[lane] : 0u);
-            if (lane == 0 && all) atomicMax(S.largest, all);
-        }
     }
     if (tiles == 0) return;
     __shared__ bool last;  // of the blocks: every tile's number of parts is there
@@ -423,22 +417,23 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
     } else {
         registers_up<kQueryMore>();
         const int mine = warp >> 2, row = threadIdx.x & 127;
-        const float c = B.S.scale * kLog2e, f = slope_scale<BF16>(B.S);
+        const float c = B.S.scale * kLog2e;
         const uint32_t lanes = static_cast<uint32_t>(warp % 4 * 32) << 16;
         const uint32_t s_at = tmem + mine * 128 + lanes, q_at = tmem + 256 + mine * D + lanes;
-        const float2 c2 = make_float2(c, c), f2 = make_float2(f, f);
+        const float2 c2 = make_float2(c, c);
         uint32_t phase = 0, sums_phase = 0;
         for (int n = 0; n < rounds; ++n) {
             if (!(ok = warp_wait(item_full + (n & 1), n >> 1))) break;
             const Item& it = info[n & 1];
             const int t = it.W.token[mine] + row, head = it.W.head[mine];
             const Row r = row_in(B.S, it, mine, row);
-            float lse = 0.f, delta = 0.f;
+            float lse = 0.f, delta = 0.f, f = 1.f;
             if (r.real) {
+                if constexpr (!BF16) f = slope_scale(B.largest[head * B.padded + t]);
                 lse = -B.lse[head * B.S.tokens + t] * kLog2e;
                 delta = -B.delta[head * B.S.tokens + t] * f;
             }
-            const float2 lse2 = make_float2(lse, lse), delta2 = make_float2(delta, delta);
+            const float2 lse2 = make_float2(lse, lse), delta2 = make_float2(delta, delta), f2 = make_float2(f, f);
             // What all of the warp's rows see whole.
             const int whole0 = __reduce_max_sync(kFull, r.real ? r.first : INT32_MAX);
             const int whole1 = __reduce_min_sync(kFull, r.real ? t + 1 : 0);
@@ -535,7 +530,66 @@ struct KeyItem {
     int from, blocks; // of 128 queries, from token `from` on, for each head that shares the keys; -1: no more items
     int place;        // -1, or the part's in the list
     int last[kTile];  // behind the last token that sees the key, 0 for one of no session
+    float slope[kTile];  // fp16: what the key's dS goes times
 };
+
+// The largest of neighbours among 128 bytes, at level k of 2^k of them from each on (as far as there are some); so of any
+// interval in two readings. A warp builds it, four bytes a lane.
+struct Largest {
+    uint32_t level[8][kTile / 4];
+    __device__ __forceinline__ void build(uint32_t four, int lane) {
+        __syncwarp();
+        level[0][lane] = four;
+#pragma unroll
+        for (int k = 0; k < 7; ++k) {
+            const int words = max(1, (1 << k) / 4);
+            uint32_t next = __shfl_down_sync(kFull, four, words);
+            if (lane + words > 31) next = 0u;
+            if (k < 2) next = __funnelshift_r(four, next, 8 << k);
+            four = __vmaxu4(four, next);
+            level[k + 1][lane] = four;
+        }
+        __syncwarp();
+    }
+    __device__ __forceinline__ uint32_t of(int from, int to) const {  // from < to
+        const int k = 31 - __clz(to - from);
+        const uint8_t* bytes = reinterpret_cast<const uint8_t*>(level[k]);
+        return max(static_cast<uint32_t>(bytes[from]), static_cast<uint32_t>(bytes[to - (1 << k)]));
+    }
+};
+// The exponent of the largest |grad_out| among the tokens of an item that see the key, in all heads that share it: of
+// keys first + lane + 32 k, which tokens up to last[k] see. 128 bytes a block and head, of the block's 64 KB; by the warp that looks ahead.
+__device__ __forceinline__ void largest_seen(const Backward& B, Largest& table, int first, int kv, int from, int blocks, int until,
+                                             const int (&last)[kTile / 32], int lane, uint32_t (&largest)[kTile / 32]) {
+#pragma unroll
+    for (uint32_t& x : largest) x = 0u;
+    for (int i = 0; i < blocks; ++i) {
+        const int at = from + i * kTile, left = until - at - 4 * lane;  // tokens of this lane's four
+        const uint8_t* bytes = B.largest + static_cast<int64_t>(kv) * B.S.group * B.padded + at + 4 * lane;
+        uint32_t four = 0u;
+#pragma unroll 4
+        for (int h = 0; h < B.S.group; ++h) four = __vmaxu4(four, *reinterpret_cast<const uint32_t*>(bytes + h * B.padded));
+        if (left < 4) four &= left <= 0 ? 0u : (1u << 8 * left) - 1;
+        bool whole = true;
+#pragma unroll
+        for (int k = 0; k < kTile / 32; ++k) {
+            const int lo = max(first + k * 32 + lane - at, 0), hi = min(last[k] - at, kTile);
+            whole = whole && (lo >= hi || hi - lo == kTile);
+        }
+        whole = __all_sync(kFull, whole);
+        if (whole) {
+            const uint32_t two = __vmaxu2(four & 0xff00ff, four >> 8 & 0xff00ff);
+            four = __reduce_max_sync(kFull, max(two & 0xffff, two >> 16));
+        } else {
+            table.build(four, lane);
+        }
+#pragma unroll
+        for (int k = 0; k < kTile / 32; ++k) {
+            const int lo = max(first + k * 32 + lane - at, 0), hi = min(last[k] - at, kTile);
+            if (lo < hi) largest[k] = max(largest[k], whole ? four : table.of(lo, hi));
+        }
+    }
+}
 
 // A block has 128 keys of a head and takes the queries that see one of them, 128 at a time, for every head that
 // shares the keys. S^T and dP^T have a key a lane, so that P^T and dS^T are operands from TMEM as they are; a warp takes
@@ -557,7 +611,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
     __shared__ uint64_t stat_full[kStatStages], stat_empty[kStatStages], item_full[2], item_empty[2];
     __shared__ uint32_t tmem_at;
     __shared__ KeyItem info[2];
-    __shared__ __align__(16) float stats[kStatStages][2][kTile];  // -lse log2 e (+ shift) and -delta (times the slopes' scale)
+    __shared__ __align__(16) float stats[kStatStages][2][kTile];  // -lse log2 e (+ shift) and -delta
+    __shared__ Largest table;
     const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
@@ -642,6 +697,11 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                     }
                     until = __reduce_max_sync(kFull, until);
                 }
+                const int blocks = tiles_of(max(until - first, 0)), per = part_blocks(B.S);
+                const int from = place < 0 ? first : first + part * per * kTile;
+                const int count = !some ? -1 : (place < 0 ? blocks : max(min(per, blocks - part * per), 0));
+                uint32_t largest[kTile / 32];
+                if constexpr (!BF16) largest_seen(B, table, first, kv, from, count, until, last, lane, largest);
                 // The place of the item before the last one: its results are stored first.
                 if (n >= 2) {
                     store(n - 2);
@@ -653,13 +713,15 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                     it.first = first;
                     it.kv = kv;
                     it.place = place;
-                    const int blocks = tiles_of(max(until - first, 0)), per = part_blocks(B.S);
-                    it.from = place < 0 ? first : first + part * per * kTile;
-                    it.blocks = !some ? -1 : (place < 0 ? blocks : max(min(per, blocks - part * per), 0));
+                    it.from = from;
+                    it.blocks = count;
                 }
                 if (some)
 #pragma unroll
-                    for (int k = 0; k < kTile / 32; ++k) it.last[k * 32 + lane] = last[k];
+                    for (int k = 0; k < kTile / 32; ++k) {
+                        it.last[k * 32 + lane] = last[k];
+                        if constexpr (!BF16) it.slope[k * 32 + lane] = slope_scale(largest[k]);
+                    }
                 warp_arrive(item_full + (n & 1));
                 if (!some) {
                     if (n >= 1) store(n - 1);
@@ -705,7 +767,6 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                 for (int64_t i = max64(0, issued - S); i < issued; ++i)
                     if (!tc::barrier_wait(tc::smem_addr(full + i % S), i / S & 1)) break;
         } else if (warp == kStatWarp) {
-            const float f = slope_scale<BF16>(B.S) * exp2f(-kPShift<BF16>);
             int s = 0;
             uint32_t phase = 0;
             for (int n = 0; ok; ++n) {
@@ -721,7 +782,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                         for (int k = 0; k < kTile / 32; ++k) {
                             const int64_t t = from + static_cast<int64_t>(i) * kTile + k * 32 + lane;
                             stats[s][0][k * 32 + lane] = t < B.S.tokens ? kPShift<BF16> - B.lse[row + t] * kLog2e : 0.f;
-                            stats[s][1][k * 32 + lane] = t < B.S.tokens ? -B.delta[row + t] * f : 0.f;
+                            stats[s][1][k * 32 + lane] = t < B.S.tokens ? -B.delta[row + t] : 0.f;
                         }
                         warp_arrive(stat_full + s);
                         if (++s == kStatStages) s = 0, phase ^= 1;
@@ -799,9 +860,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
     } else {
         registers_up<kKeyMore>();
         const int row = threadIdx.x & 127, half = warp >> 2;
-        const float scale_s = slope_scale<BF16>(B.S);
-        const float c = B.S.scale * kLog2e, f = scale_s * exp2f(-kPShift<BF16>);
-        const float2 c2 = make_float2(c, c), f2 = make_float2(f, f);
+        const float c = B.S.scale * kLog2e;
+        const float2 c2 = make_float2(c, c);
         const uint32_t lanes = static_cast<uint32_t>(warp % 4 * 32) << 16;
         const uint32_t s_at = tmem + lanes + half * 64, g_at = s_at + 128;
         int s = 0;
@@ -811,6 +871,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
             const KeyItem& it = info[n & 1];
             const int first = it.first, from = it.from, kv = it.kv, blocks = it.blocks, place = it.place;
             const int last = blocks < 0 ? 0 : it.last[row];
+            const float scale_s = BF16 || blocks < 0 ? 1.f : it.slope[row], f = scale_s * exp2f(-kPShift<BF16>);
+            const float2 f2 = make_float2(f, f);
             warp_arrive(item_empty + (n & 1));
             if (blocks < 0) break;
             const TwoRanges seen{first + row, last, 0, 0};
@@ -858,8 +920,12 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
 #pragma unroll
                 for (int k = 0; k < 64; k += 4) {
                     const float4 l = delta[k / 4];
-                    float2 x = fma2(make_float2(__uint_as_float(d[k]), __uint_as_float(d[k + 1])), f2, make_float2(l.x, l.y));
-                    float2 y = fma2(make_float2(__uint_as_float(d[k + 2]), __uint_as_float(d[k + 3])), f2, make_float2(l.z, l.w));
+                    float2 x = add2(make_float2(__uint_as_float(d[k]), __uint_as_float(d[k + 1])), make_float2(l.x, l.y));
+                    float2 y = add2(make_float2(__uint_as_float(d[k + 2]), __uint_as_float(d[k + 3])), make_float2(l.z, l.w));
+                    if constexpr (!BF16) {
+                        x = mul2(x, f2);
+                        y = mul2(y, f2);
+                    }
                     x = mul2(x, make_float2(__uint_as_float(p[k]), __uint_as_float(p[k + 1])));
                     y = mul2(y, make_float2(__uint_as_float(p[k + 2]), __uint_as_float(p[k + 3])));
                     packed[k / 2] = pack2<BF16>(x.x, x.y);
@@ -881,7 +947,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
             if (!(ok = warp_wait(&kv_full, n))) break;
             tc::fence_after();
             unsigned char* tile = keys + (half ? 0 : kRows);
-            if (place >= 0) {  // sums in fp32, joined by another kernel
+            if (place >= 0) {  // sums in fp32, of dK without its scale of dS, joined by another kernel
+                const float by = half ? 1.f / scale_s : 1.f;
                 float* to = B.order.sums + ((static_cast<int64_t>(place) * B.S.kv_heads + kv) * 2 + half) * kTile * D + row * D;
 #pragma unroll 1
                 for (int d = 0; d < D; d += 32) {
@@ -889,7 +956,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                     if (count > 0) tc::tmem_load32(tmem + lanes + 256 + half * D + d, o);
 #pragma unroll
                     for (int k = 0; k < 32; k += 4)
-                        *reinterpret_cast<float4*>(to + d + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+                        *reinterpret_cast<float4*>(to + d + k) = make_float4(o[k] * by, o[k + 1] * by, o[k + 2] * by, o[k + 3] * by);
                 }
                 tc::fence_before();
                 warp_arrive(staged + half);
@@ -922,7 +989,7 @@ __global__ void __launch_bounds__(256) attention_parts_kernel(const Backward B) 
     if (threadIdx.x == 0) again = 0u;
     begin_kernel();
     const int listed = min(*B.order.parts, B.order.room), lane = threadIdx.x & 31;
-    const float by[2] = {exp2f(-kPShift<BF16>), B.S.scale / slope_scale<BF16>(B.S)};
+    const float by[2] = {exp2f(-kPShift<BF16>), B.S.scale};
     for (int64_t w = blockIdx.x; w < static_cast<int64_t>(listed) * B.S.kv_heads * kGroups; w += gridDim.x) {
         const int64_t head = w / kGroups;
         const int place = static_cast<int>(head / B.S.kv_heads), kv = static_cast<int>(head % B.S.kv_heads);
