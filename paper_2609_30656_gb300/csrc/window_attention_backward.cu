@@ -204,16 +204,16 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
     unsigned char* grads_out = queries + 2 * kRows;  // dO, and dQ in its place
     unsigned char* keys = queries + 4 * kRows;
     unsigned char* values = keys + kKeyBuffers * kRows;
-    __shared__ uint64_t q_full, q_empty, g_full[2], stored[2], k_full[2], k_empty[2], v_full, v_empty;
+    __shared__ uint64_t q_full, q_empty, g_full[2], stored[2], k_full[2], k_empty[2], k_landed[2], v_full, v_empty, v_landed;
     __shared__ uint64_t scores[2], taken[2], grads[2], slopes[2][2], sums[2], staged[2], item_full[2], item_empty[2];
     __shared__ uint32_t tmem_at;
     __shared__ Item info[2];
     const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        for (uint64_t* b : {&q_full, &q_empty, &v_full, &v_empty}) tc::barrier_init(tc::smem_addr(b), 1);
+        for (uint64_t* b : {&q_full, &q_empty, &v_full, &v_empty, &v_landed}) tc::barrier_init(tc::smem_addr(b), 1);
         for (int i = 0; i < 2; ++i) {
-            for (uint64_t* b : {g_full, stored, k_full, k_empty, scores, grads, sums, item_full})
+            for (uint64_t* b : {g_full, stored, k_full, k_empty, k_landed, scores, grads, sums, item_full})
                 tc::barrier_init(tc::smem_addr(b + i), 1);
             for (uint64_t* b : {taken, slopes[0], slopes[1], staged}) tc::barrier_init(tc::smem_addr(b + i), 4);
             tc::barrier_init(tc::smem_addr(item_empty + i), kWorkWarps + 3);
@@ -252,25 +252,38 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
                 look_ahead(B.S, it, 1, W.token[1], lane);
                 warp_arrive(item_full + (n & 1));
             }
-        } else if (warp == kStoreWarp && tc::elect()) {
-            for (int n = 0; n < rounds; ++n) {
-                const Work W = item_of(n).W;
-                if (!ok) break;
-                item_done(n);
+        } else if (warp == kStoreWarp) {
+            uint32_t k_turns = 0, v_turns = 0;
+            int begun = 0;  // blocks before the item's
+            for (int n = 0; n < rounds && ok; ++n) {
+                if (!meet(item_full + (n & 1), n >> 1)) break;
+                const Work W = info[n & 1].W;
+                const Blocks blocks(info[n & 1].sight[0], info[n & 1].sight[1]);
+                warp_arrive(item_empty + (n & 1));
+                auto clear = [&](int i, int count) {
+                    const uint32_t b = static_cast<uint32_t>(begun + i) & 1;
+                    return ok = clear_landed<D>(k_landed, k_full, b, k_turns, keys + b * kRows, count, lane) &&
+                                clear_landed<D>(&v_landed, &v_full, 0, v_turns, values, count, lane);
+                };
+                if (!blocks.to_clear(0, blocks.count, clear)) break;
+                begun += blocks.count;
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    if (!wait(staged + x, n)) break;
-                    if (W.token[x] < B.S.tokens)
+                    if (!meet(staged + x, n)) break;
+                    if (lane == 0) {
+                        if (W.token[x] < B.S.tokens)
 #pragma unroll
-                        for (int d = 0; d < D / 64; ++d)
-                            tma_store(&dqm, tc::smem_addr(grads_out) + x * kRows + d * kBoxBytes, d * 64, W.head[x], W.token[x]);
-                    tma_store_done();
-                    tc::barrier_arrive(tc::smem_addr(stored + x));
+                            for (int d = 0; d < D / 64; ++d)
+                                tma_store(&dqm, tc::smem_addr(grads_out) + x * kRows + d * kBoxBytes, d * 64, W.head[x], W.token[x]);
+                        tma_store_done();
+                    }
+                    warp_arrive(stored + x);
                 }
-                if (!ok) break;
             }
         } else if (warp == kCopyWarp && tc::elect()) {
             int i_all = 0, n = 0, loaded_q = 0, loaded_g[2] = {0, 0}, loaded_k = 0, loaded_v = 0;
+            int cleared_k[2] = {0, 0}, cleared_v = 0;  // tiles that land to be cleared
+            bool last_k[2] = {false, false}, last_v = false;  // whether the last was one
             for (; n < rounds && ok; ++n) {
                 const Item& it = item_of(n);
                 if (!ok) break;
@@ -286,9 +299,12 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
                 auto load_keys = [&](int i) {
                     const int b = (i_all + i) & 1;
                     if (!wait(k_empty + b, ((i_all + i) >> 1) ^ 1)) return;
-                    tc::barrier_expect(tc::smem_addr(k_full + b), kRows);
-                    load_tile<D>(tc::smem_addr(keys) + b * kRows, &km, tc::smem_addr(k_full + b), W.kv, blocks.at(i).at);
+                    const bool clear = blocks.counted(i) < kTile;
+                    const uint32_t bar = tc::smem_addr((clear ? k_landed : k_full) + b);
+                    tc::barrier_expect(bar, kRows);
+                    load_tile<D>(tc::smem_addr(keys) + b * kRows, &km, bar, W.kv, blocks.at(i).at);
                     ++loaded_k;
+                    cleared_k[b] += last_k[b] = clear;
                 };
                 if (blocks.count > 0) load_keys(0);
 #pragma unroll
@@ -300,9 +316,12 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
                 }
                 for (int i = 0; i < blocks.count && ok; ++i) {
                     if (!wait(&v_empty, (i_all + i) ^ 1)) break;
-                    tc::barrier_expect(tc::smem_addr(&v_full), kRows);
-                    load_tile<D>(tc::smem_addr(values), &vm, tc::smem_addr(&v_full), W.kv, blocks.at(i).at);
+                    const bool clear = blocks.counted(i) < kTile;
+                    const uint32_t bar = tc::smem_addr(clear ? &v_landed : &v_full);
+                    tc::barrier_expect(bar, kRows);
+                    load_tile<D>(tc::smem_addr(values), &vm, bar, W.kv, blocks.at(i).at);
                     ++loaded_v;
+                    cleared_v += last_v = clear;
                     if (i + 1 < blocks.count) load_keys(i + 1);
                 }
                 i_all += blocks.count;
@@ -312,8 +331,9 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap qm, const __grid_constan
                 if (loaded_q) land(&q_full, loaded_q - 1);
                 for (int x = 0; x < 2; ++x)
                     if (loaded_g[x]) land(g_full + x, loaded_g[x] - 1);
-                if (loaded_v) land(&v_full, loaded_v - 1);
-                for (int k = max(0, loaded_k - 2); k < loaded_k; ++k) land(k_full + (k & 1), k >> 1);
+                if (loaded_v) last_v ? land(&v_landed, cleared_v - 1) : land(&v_full, loaded_v - 1);
+                for (int k = max(0, loaded_k - 2); k < loaded_k; ++k)
+                    last_k[k & 1] ? land(k_landed + (k & 1), cleared_k[k & 1] - 1) : land(k_full + (k & 1), k >> 1);
             }
         } else if (warp == kMultiplyWarp) {
             const bool one = tc::elect();
@@ -528,6 +548,7 @@ template <int D> constexpr size_t kKeyShared = 1024 + (2 + kKeyStages) * kRowsBy
 struct KeyItem {
     int first, kv;    // token, head
     int from, blocks; // of 128 queries, from token `from` on, for each head that shares the keys; -1: no more items
+    int until;        // behind the last token that sees one of the keys
     int place;        // -1, or the part's in the list
     int last[kTile];  // behind the last token that sees the key, 0 for one of no session
     float slope[kTile];  // fp16: what the key's dS goes times
@@ -607,7 +628,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
     extern __shared__ unsigned char dynamic[];
     unsigned char* keys = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~uintptr_t(1023));
     unsigned char* ring = keys + 2 * kRows;  // K and V, and dK and dV in their place
-    __shared__ uint64_t kv_full, stored, staged[2], full[S], empty[S], scores, weights, grads, slopes, done;
+    __shared__ uint64_t kv_full, stored, staged[2], full[S], empty[S], landed[S], scores, weights, grads, slopes, done;
     __shared__ uint64_t stat_full[kStatStages], stat_empty[kStatStages], item_full[2], item_empty[2];
     __shared__ uint32_t tmem_at;
     __shared__ KeyItem info[2];
@@ -621,6 +642,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
         for (int i = 0; i < S; ++i) {
             tc::barrier_init(tc::smem_addr(full + i), 1);
             tc::barrier_init(tc::smem_addr(empty + i), 1);
+            tc::barrier_init(tc::smem_addr(landed + i), 1);
         }
         for (int i = 0; i < kStatStages; ++i) {
             tc::barrier_init(tc::smem_addr(stat_full + i), 1);
@@ -715,6 +737,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                     it.place = place;
                     it.from = from;
                     it.blocks = count;
+                    it.until = until;
                 }
                 if (some)
 #pragma unroll
@@ -730,23 +753,25 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
             }
         } else if (warp == kCopyWarp && tc::elect()) {
             int s = 0, n = 0;
-            uint32_t phase = 0;
-            int64_t issued = 0;
+            uint32_t phase = 0, used = 0, cleared = 0, turns = 0;  // stages: in use; whose copies land to be cleared, their phases
             for (;; ++n) {
                 if (!wait(item_full + (n & 1), n >> 1)) break;
                 const KeyItem& it = info[n & 1];
-                const int first = it.first, from = it.from, kv = it.kv, blocks = it.blocks;
+                const int first = it.first, from = it.from, kv = it.kv, blocks = it.blocks, until = it.until;
                 tc::barrier_arrive(tc::smem_addr(item_empty + (n & 1)));
                 if (blocks < 0) break;
                 int64_t m = 0;
                 auto load = [&] {  // the next tile of the ring
                     if (!wait(empty + s, phase ^ 1)) return false;
                     const int b = static_cast<int>(m >> 1), h = b / blocks, i = b - h * blocks;
-                    tc::barrier_expect(tc::smem_addr(full + s), kRows);
-                    load_tile<D>(tc::smem_addr(ring) + s * kRows, m & 1 ? &gm : &qm, tc::smem_addr(full + s), kv * B.S.group + h,
-                                 from + i * kTile);
+                    const bool clear = until - from - i * kTile < kTile;
+                    const uint32_t bar = tc::smem_addr((clear ? landed : full) + s);
+                    used |= 1u << s;
+                    cleared = (cleared & ~(1u << s)) | (clear ? 1u << s : 0u);
+                    turns ^= clear ? 1u << s : 0u;
+                    tc::barrier_expect(bar, kRows);
+                    load_tile<D>(tc::smem_addr(ring) + s * kRows, m & 1 ? &gm : &qm, bar, kv * B.S.group + h, from + i * kTile);
                     ++m;
-                    ++issued;
                     if (++s == S) s = 0, phase ^= 1;
                     return true;
                 };
@@ -764,28 +789,35 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                 }
             }
             if (!ok)  // copies in flight land before the block's shared memory goes away
-                for (int64_t i = max64(0, issued - S); i < issued; ++i)
-                    if (!tc::barrier_wait(tc::smem_addr(full + i % S), i / S & 1)) break;
+                for (int i = 0; i < S; ++i)  // of the stages, those from s on are a round behind
+                    if (used >> i & 1)
+                        cleared >> i & 1 ? tc::barrier_wait(tc::smem_addr(landed + i), turns >> i & 1 ^ 1)
+                                         : tc::barrier_wait(tc::smem_addr(full + i), phase ^ (i >= s));
         } else if (warp == kStatWarp) {
             int s = 0;
-            uint32_t phase = 0;
+            uint32_t phase = 0, turns = 0, turn = 0;
             for (int n = 0; ok; ++n) {
                 if (!(ok = warp_wait(item_full + (n & 1), n >> 1))) break;
-                const int from = info[n & 1].from, kv = info[n & 1].kv, blocks = info[n & 1].blocks;
+                const int from = info[n & 1].from, kv = info[n & 1].kv, blocks = info[n & 1].blocks, until = info[n & 1].until;
                 warp_arrive(item_empty + (n & 1));
                 if (blocks < 0) break;
                 for (int h = 0; h < B.S.group && ok; ++h) {
                     const int64_t row = static_cast<int64_t>(kv * B.S.group + h) * B.S.tokens;
-                    for (int i = 0; i < blocks; ++i) {
+                    for (int i = 0; i < blocks; ++i, ++turn) {
                         if (!(ok = warp_wait(stat_empty + s, phase ^ 1))) break;
 #pragma unroll
                         for (int k = 0; k < kTile / 32; ++k) {
                             const int64_t t = from + static_cast<int64_t>(i) * kTile + k * 32 + lane;
-                            stats[s][0][k * 32 + lane] = t < B.S.tokens ? kPShift<BF16> - B.lse[row + t] * kLog2e : 0.f;
-                            stats[s][1][k * 32 + lane] = t < B.S.tokens ? -B.delta[row + t] : 0.f;
+                            stats[s][0][k * 32 + lane] = t < until ? kPShift<BF16> - B.lse[row + t] * kLog2e : 0.f;
+                            stats[s][1][k * 32 + lane] = t < until ? -B.delta[row + t] : 0.f;
                         }
                         warp_arrive(stat_full + s);
                         if (++s == kStatStages) s = 0, phase ^= 1;
+                        const int seeing = until - from - i * kTile;  // tokens of the block that see a key
+                        if (seeing >= kTile) continue;
+                        for (uint32_t m = 2 * turn; m < 2 * turn + 2 && ok; ++m)  // their queries, their gradients
+                            ok = clear_landed<D>(landed, full, m % S, turns, ring + m % S * kRows, seeing, lane);
+                        if (!ok) break;
                     }
                 }
             }

@@ -71,7 +71,7 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
     unsigned char* queries = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~uintptr_t(1023));
     unsigned char* ring = queries + 2 * kRows;
     unsigned char* output = ring + 2 * S * kRows;  // of one tile after the other
-    __shared__ uint64_t q_full, q_empty, full[S], empty[S], scores[2], part[2][kParts], sums[2], staged[2], stored[2];
+    __shared__ uint64_t q_full, q_empty, full[S], empty[S], landed[S], scores[2], part[2][kParts], sums[2], staged[2], stored[2];
     __shared__ uint64_t item_full[2], item_empty[2];
     __shared__ uint32_t tmem_at;
     __shared__ Item info[2];
@@ -92,6 +92,7 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
         for (int i = 0; i < S; ++i) {
             tc::barrier_init(tc::smem_addr(full + i), 1);
             tc::barrier_init(tc::smem_addr(empty + i), 1);
+            tc::barrier_init(tc::smem_addr(landed + i), 1);
         }
         tc::barrier_init_fence();
         for (const CUtensorMap* m : {&qm, &km, &vm, &om}) tc::tma_prefetch(m);
@@ -124,26 +125,36 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
                 look_ahead(F.S, it, 1, W.token[1], lane);
                 warp_arrive(item_full + (n & 1));
             }
-        } else if (warp == kStoreWarp && tc::elect()) {
+        } else if (warp == kStoreWarp) {
+            uint32_t turns = 0;
+            int begun = 0;  // stages before the item's
             for (int n = 0; n < rounds && ok; ++n) {
-                const Work W = item_of(n).W;
-                if (!ok) break;
-                item_done(n);
+                if (!(ok = warp_wait(item_full + (n & 1), n >> 1))) break;
+                const Work W = info[n & 1].W;
+                const Blocks blocks(info[n & 1].sight[0], info[n & 1].sight[1]);
+                warp_arrive(item_empty + (n & 1));
+                auto clear = [&](int i, int keys) {  // of the values of block i, which come in the stage behind the first keys'
+                    const uint32_t s = static_cast<uint32_t>(begun + 1 + i) % S;
+                    return ok = clear_landed<D>(landed, full, s, turns, ring + s * 2 * kRows, keys, lane);
+                };
+                if (!blocks.to_clear(0, blocks.count, clear)) break;
+                begun += blocks.count ? blocks.count + 1 : 0;
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    if (!(ok = tc::barrier_wait(tc::smem_addr(staged + x), n & 1))) break;
-                    if (W.token[x] < F.S.tokens)
+                    if (!(ok = warp_wait(staged + x, n))) break;
+                    if (lane == 0) {
+                        if (W.token[x] < F.S.tokens)
 #pragma unroll
-                        for (int d = 0; d < D / 64; ++d)
-                            tma_store(&om, tc::smem_addr(output) + d * kBoxBytes, d * 64, W.head[x], W.token[x]);
-                    tma_store_done();
-                    tc::barrier_arrive(tc::smem_addr(stored + x));
+                            for (int d = 0; d < D / 64; ++d)
+                                tma_store(&om, tc::smem_addr(output) + d * kBoxBytes, d * 64, W.head[x], W.token[x]);
+                        tma_store_done();
+                    }
+                    warp_arrive(stored + x);
                 }
             }
         } else if (warp == kCopyWarp && tc::elect()) {
             int s = 0;
-            uint32_t phase = 0;
-            int64_t issued = 0;
+            uint32_t phase = 0, used = 0, cleared = 0, turns = 0;  // stages: in use; whose copies land to be cleared, their phases
             int queries_issued = 0;
             for (int n = 0; n < rounds && ok; ++n) {
                 const Item& it = item_of(n);
@@ -161,18 +172,22 @@ attention_forward_kernel(const __grid_constant__ CUtensorMap qm, const __grid_co
                 for (int i = -1; i < blocks.count; ++i) {
                     if (i < 0 && blocks.count == 0) continue;
                     if (!(ok = tc::barrier_wait(tc::smem_addr(empty + s), phase ^ 1))) break;
-                    const uint32_t bar = tc::smem_addr(full + s), at = tc::smem_addr(ring) + s * 2 * kRows;
-                    const bool keys = i + 1 < blocks.count;
+                    const bool clear = i >= 0 && blocks.counted(i) < kTile, keys = i + 1 < blocks.count;
+                    const uint32_t bar = tc::smem_addr((clear ? landed : full) + s), at = tc::smem_addr(ring) + s * 2 * kRows;
+                    used |= 1u << s;
+                    cleared = (cleared & ~(1u << s)) | (clear ? 1u << s : 0u);
+                    turns ^= clear ? 1u << s : 0u;
                     tc::barrier_expect(bar, i >= 0 && keys ? 2 * kRows : kRows);
                     if (i >= 0) load_tile<D>(at, &vm, bar, W.kv, blocks.at(i).at);
                     if (keys) load_tile<D>(at + kRows, &km, bar, W.kv, blocks.at(i + 1).at);
-                    ++issued;
                     if (++s == S) s = 0, phase ^= 1;
                 }
             }
             if (!ok) {  // copies in flight land before the block's shared memory goes away
-                for (int64_t i = max64(0, issued - S); i < issued; ++i)
-                    if (!tc::barrier_wait(tc::smem_addr(full + i % S), i / S & 1)) break;
+                for (int i = 0; i < S; ++i)  // of the stages, those from s on are a round behind
+                    if (used >> i & 1)
+                        cleared >> i & 1 ? tc::barrier_wait(tc::smem_addr(landed + i), turns >> i & 1 ^ 1)
+                                         : tc::barrier_wait(tc::smem_addr(full + i), phase ^ (i >= s));
                 if (queries_issued) tc::barrier_wait(tc::smem_addr(&q_full), (queries_issued - 1) & 1);
             }
         } else if (warp == kMultiplyWarp) {

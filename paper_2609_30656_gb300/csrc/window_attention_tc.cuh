@@ -177,6 +177,35 @@ __device__ __forceinline__ void warp_arrive(uint64_t* bar) {
     __syncwarp();
 }
 
+// Zeros in rows `from` .. 127 of a tile, by a whole warp, before the tile's products.
+//
+// The last block of an item holds tokens that none of its rows sees: of the next session, or of none. Their infinities and NaNs
+// would survive the zeros by which they are multiplied, and all of the item's rows would have to be computed again (a session of
+// 32768 tokens x 8 heads over 1 beside one of NaNs: backward 1730 ms, 13 with the rows cleared, 4.5 beside one of numbers).
+//
+// Such a tile lands on a barrier of its own (`landed`); a warp that has little else to do, the one that stores or over
+// keys the one that brings lse and delta, waits for it there, clears the rows and arrives where the tile's products wait for
+// any other's copy. (By the warp that issues the products these took 5 to 14 % longer in the backward pass, cleared tiles
+// or not; by the one that looks ahead 41 against 36 us where all sessions are short.)
+template <int D>
+__device__ __forceinline__ void clear_rows(unsigned char* tile, int from, int lane) {
+    for (int r = from + lane / 8; r < kTile; r += 4)  // a lane 16 bytes
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x)
+            *reinterpret_cast<uint4*>(tile + x * kBoxBytes + r * 128 + lane % 8 * 16) = make_uint4(0u, 0u, 0u, 0u);
+    fence_to_tma();
+}
+// For a warp: the barriers on which tiles to be cleared land, one for each place of a tile. `turns` has the phase of each.
+template <int D>
+__device__ __forceinline__ bool clear_landed(uint64_t* landed, uint64_t* full, uint32_t place, uint32_t& turns, unsigned char* tile,
+                                             int from, int lane) {
+    if (!warp_wait(landed + place, turns >> place)) return false;
+    turns ^= 1u << place;
+    clear_rows<D>(tile, from, lane);
+    warp_arrive(full + place);
+    return true;
+}
+
 // ---------------------------------------------------------------- what rows see
 
 // Bits i of columns [a, b) among the 32 from `first` on. (The instruction's shifts by 32 and more give 0.)
@@ -265,6 +294,25 @@ struct Blocks {
         sinks1 = shared ? 0 : tiles_of(b.s1 - b.s0);
         base = a.hi == 0 ? b.lo : (b.hi == 0 ? a.lo : min(a.lo, b.lo));
         count = sinks0 + sinks1 + tiles_of(max(max(a.hi, b.hi) - base, 0));
+    }
+    // Keys of block i, from its first on, that some row may see. Fewer than 128 only in the last of each kind.
+    __device__ __forceinline__ int counted(int i) const {
+        if (i < sinks0) return x[0].s1 - x[0].s0 - i * kTile;
+        i -= sinks0;
+        if (i < sinks1) return x[1].s1 - x[1].s0 - i * kTile;
+        return max(x[0].hi, x[1].hi) - base - (i - sinks1) * kTile;
+    }
+    // f(i, counted(i)) of the blocks i, from `from` to `to` - 1, that hold keys which no row sees.
+    template <class F>
+    __device__ __forceinline__ bool to_clear(int from, int to, F f) const {
+        const int last[3] = {sinks0 - 1, sinks0 + sinks1 - 1, count - 1};
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            const int i = last[k], keys = counted(i);
+            if (i < from || i >= to || (k && i == last[k - 1]) || keys >= kTile) continue;
+            if (!f(i, keys)) return false;
+        }
+        return true;
     }
     __device__ __forceinline__ Block at(int i) const {
         Block k;

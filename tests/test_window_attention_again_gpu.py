@@ -19,14 +19,14 @@ def _inputs(T, heads, kv, dim, dtype, seed=1):
     return [torch.randn(T, n, dim, generator=g, device=DEV).to(dtype) for n in (heads, kv, kv, heads)]
 
 
-def _both(q, k, v, go, lens, window, sinks):
-    """(out, lse, dq, dk, dv); what is not written would keep its 77s."""
+def _both(q, k, v, go, lens, window, sinks, take=None):
+    """(out, lse, dq, dk, dv); what is not written would keep its 77s. take(out, lse): what the backward pass gets of them."""
     from paper_2609_30656_gb300 import window_attention as wa
     off = torch.tensor([0] + lens, device=DEV).cumsum(0)
     error = torch.zeros(1, dtype=torch.int32, device=DEV)
     out, *grads = (torch.full_like(t, 77) for t in (q, q, k, v))
     _, lse = wa.window_attention(q, k, v, off, window, sinks, out=out, stats=True, error=error)
-    wa.window_attention_backward(go, q, k, v, out, lse, off, window, sinks, grads=grads, error=error)
+    wa.window_attention_backward(go, q, k, v, *(take(out, lse) if take else (out, lse)), off, window, sinks, grads=grads, error=error)
     assert error.item() == 0
     assert all((t != 77).all() for t in (out, *grads))  # as good as no value of these is 77 by itself
     return out, lse, *grads
@@ -144,3 +144,57 @@ def test_replays_begin_anew():
         assert all(torch.equal(a.nan_to_num(55), b.nan_to_num(55)) for a, b in zip(got, want))
         if not broken:
             assert all(torch.equal(a, b) for a, b in zip(got, clean))
+
+
+@pytest.mark.parametrize("dtype", HALVES, ids=str)
+@pytest.mark.parametrize("heads,kv,dim,window,sinks", [(2, 1, 64, None, 0), (4, 4, 128, None, 0), (8, 2, 72, 600, 5), (3, 3, 64, 40, 200)])
+@pytest.mark.parametrize("before,behind", [(300, 500), (0, 100), (130, 0)])
+def test_only_rows_in_reach_of_another_session_are_computed_again(before, behind, heads, kv, dim, window, sinks, dtype):
+    """Tiles that hold no token of a session of NaNs have the bits that they have beside one of numbers: their products meet
+    none. The first keys and queries of a tile's block of 128, or pair of them, may lie beside a neighbour's. The session's
+    rows there have other roundings, so both backward passes get one forward pass's."""
+    n = 4000
+    T = before + n + behind
+    q, k, v, go = _inputs(T, heads, kv, dim, dtype)
+    lens = [before, n, behind]
+    clean = _both(q, k, v, go, lens, window, sinks)
+    for t in (q, k, v, go):
+        t[:before] = float("nan")
+        t[before + n:] = float("nan")
+
+    def take(out, lse):
+        out, lse = out.clone(), lse.clone()
+        out[before:before + n], lse[:, before:before + n] = clean[0][before:before + n], clean[1][:, before:before + n]
+        return out, lse
+
+    broken = _both(q, k, v, go, lens, window, sinks, take)
+    inner = slice(-(-before // 256) * 256, (before + n) // 256 * 256 - 256)
+    for a, b in zip(clean[:1] + clean[2:], broken[:1] + broken[2:]):
+        assert torch.equal(a[inner], b[inner])
+
+
+@pytest.mark.parametrize("dtype", HALVES, ids=str)
+def test_unused_tokens_hold_anything(dtype):
+    """NaNs behind the last session and before the first one, as of a buffer that is larger than the batch, and beside the
+    first tokens that all see."""
+    q, k, v, go = _inputs(3000, 4, 2, 64, dtype)
+    from paper_2609_30656_gb300 import window_attention as wa
+    off = torch.tensor([100, 2100, 2500], device=DEV)
+
+    def both(take=None):
+        out, lse = wa.window_attention(q, k, v, off, 50, 4, stats=True)
+        return (out, lse.T, *wa.window_attention_backward(go, q, k, v, *(take or (out, lse)), off, 50, 4))
+
+    clean = both()
+    for t in (q, k, v, go):
+        t[:100] = t[2500:] = float("nan")
+    broken = both((clean[0], clean[1].T))
+    for a, b in zip(clean, broken):
+        assert torch.equal(a[256:2304], b[256:2304])
+        assert torch.equal(a[:100], b[:100]) and torch.equal(a[2500:], b[2500:])
+    # Of a session's keys 4 .. 127 the far tokens see none, whatever those hold.
+    v[150] = torch.inf
+    k[150] = torch.nan
+    far = both()
+    assert torch.equal(far[0][512:2048], clean[0][512:2048])
+    assert torch.equal(far[2][512:2048], clean[2][512:2048])
