@@ -52,13 +52,10 @@ __global__ void __launch_bounds__(kWarps * 32) attention_rowwise_kernel(const Fo
     for (int64_t w = warp_id_global(); w < S.tokens * S.heads; w += warps_in_grid()) {
         const int64_t t = w / S.heads;
         const int h = static_cast<int>(w - t * S.heads);
-        float o[kLaneValues], most, sum;
-        row_output<DT>(F, t, h, 0, 1, o, most, sum);
-        const bool real = S.end[t] > t;
-#pragma unroll
-        for (int i = 0; i < kLaneValues; ++i) o[i] = real ? o[i] / sum : 0.f;
+        float o[kLaneValues], lse;
+        row_output<DT>(F, t, h, o, lse);
         store_row<DT>(F.out, t, h, S.dim, o);
-        if (F.lse && (threadIdx.x & 31) == 0) F.lse[h * S.tokens + t] = real ? (most + log2f(sum)) * kLn2 : -INFINITY;
+        if (F.lse && (threadIdx.x & 31) == 0) F.lse[h * S.tokens + t] = lse;
     }
 }
 
@@ -86,7 +83,7 @@ __global__ void __launch_bounds__(kWarps * 32) attention_dq_rowwise_kernel(const
         const int64_t t = w / S.heads;
         const int h = static_cast<int>(w - t * S.heads);
         float dq[kLaneValues];
-        row_dq<DT>(B, t, h, 0, 1, dq);
+        row_dq<DT>(B, t, h, dq);
         store_row<DT>(B.dq, t, h, S.dim, dq);
     }
 }
@@ -100,7 +97,7 @@ __global__ void __launch_bounds__(kWarps * 32) attention_dkv_rowwise_kernel(cons
         const int64_t j = w / S.kv_heads;
         const int kv = static_cast<int>(w - j * S.kv_heads);
         float dk[kLaneValues], dv[kLaneValues];
-        row_dkv<DT, true, true>(B, j, kv, 0, 1, dk, dv);
+        row_dkv<DT>(B, j, kv, dk, dv);
         store_row<DT>(B.dk, j, kv, S.dim, dk);
         store_row<DT>(B.dv, j, kv, S.dim, dv);
     }

@@ -82,12 +82,8 @@ struct Backward {
 
 // ---------------------------------------------------------------- a row at a time
 
-// Rows of any type and length up to 256, by a warp that goes key by key, in fp32: all of the row (first 0, step 1), or
-// every step-th of its keys from the first-th on. The tensor-core kernels note a row whose result is not finite, and it is
-// computed again this way by a kernel behind them: their tiles multiply what a row does not see by
-// zeros, which infinities and NaNs of other sessions, or of unused memory, survive. A row whose sums have all become NaNs
-// is done: what follows cannot change it, and a batch of NaNs does not cost the row's whole session. Warps that share a row
-// tell one another by `stop`.
+// Rows of any type and length up to 256, by a warp that goes key by key, in fp32. A row whose sums have all become NaNs
+// is done: what follows cannot change it.
 constexpr int kMaxDim = 256, kLaneValues = kMaxDim / 32;
 
 // A row of up to 256 values, value lane + 32 i in v[i].
@@ -141,26 +137,26 @@ __device__ __forceinline__ Seen seen_by(const Shape& S, int64_t t) {
     a.n = a.sinks + t + 1 - a.first;
     return a;
 }
-__device__ __forceinline__ bool stopped(const volatile int* stop) { return stop && *stop; }
-// The sums of these rows have become NaNs.
-__device__ __forceinline__ void stop_all(volatile int* stop) {
-    if (stop) *stop = 1;
+// Behind the last token that sees key j, j for a token of no session.
+__device__ __forceinline__ int64_t seen_to(const Shape& S, int64_t j) {
+    const int64_t end = S.end[j];
+    return end <= j ? j : (j - S.start[j] < S.sinks ? end : min64(end, j + S.window));
 }
 
-// Head h of token t: the sum of its weights 2^(S - most), and of the values by them.
+// Head h of token t: its output, and its lse.
 template <int DT>
-__device__ __forceinline__ void row_output(const Forward& F, int64_t t, int h, int first, int step, float (&o)[kLaneValues],
-                                           float& most, float& sum, volatile int* stop = nullptr) {
+__device__ __forceinline__ void row_output(const Forward& F, int64_t t, int h, float (&o)[kLaneValues], float& lse) {
     const Shape& S = F.S;
     const int kv = h / S.group;
     float q[kLaneValues], k[kLaneValues], v[kLaneValues];
-    most = -INFINITY;
-    sum = 0.f;
+    float most = -INFINITY, sum = 0.f;
 #pragma unroll
     for (int i = 0; i < kLaneValues; ++i) o[i] = 0.f;
+    lse = -INFINITY;
     const Seen a = seen_by(S, t);
+    if (a.n == 0) return;
     load_row<DT>(F.q, t, h, S.dim, q);
-    for (int64_t i = first; i < a.n && !stopped(stop); i += step) {
+    for (int64_t i = 0; i < a.n; ++i) {
         const int64_t j = a.at(i);
         load_row<DT>(F.k, j, kv, S.dim, k);
         load_row<DT>(F.v, j, kv, S.dim, v);
@@ -171,12 +167,14 @@ __device__ __forceinline__ void row_output(const Forward& F, int64_t t, int h, i
 #pragma unroll
         for (int x = 0; x < kLaneValues; ++x) o[x] = fmaf(o[x], keep, p * v[x]);
         most = top;
-        if (sum != sum) return stop_all(stop);
+        if (sum != sum) break;
     }
+#pragma unroll
+    for (int i = 0; i < kLaneValues; ++i) o[i] /= sum;
+    lse = (most + log2f(sum)) * kLn2;
 }
 template <int DT>
-__device__ __forceinline__ void row_dq(const Backward& B, int64_t t, int h, int first, int step, float (&dq)[kLaneValues],
-                                       volatile int* stop = nullptr) {
+__device__ __forceinline__ void row_dq(const Backward& B, int64_t t, int h, float (&dq)[kLaneValues]) {
     const Shape& S = B.S;
     const int kv = h / S.group;
     float q[kLaneValues], go[kLaneValues], k[kLaneValues], v[kLaneValues];
@@ -187,43 +185,34 @@ __device__ __forceinline__ void row_dq(const Backward& B, int64_t t, int h, int 
     load_row<DT>(B.q, t, h, S.dim, q);
     load_row<DT>(B.go, t, h, S.dim, go);
     const float lse = B.lse[h * S.tokens + t], delta = B.delta[h * S.tokens + t];
-    for (int64_t i = first; i < a.n && !stopped(stop); i += step) {
+    for (int64_t i = 0; i < a.n; ++i) {
         const int64_t j = a.at(i);
         load_row<DT>(B.k, j, kv, S.dim, k);
         load_row<DT>(B.v, j, kv, S.dim, v);
         const float slope = exp2f((dot(q, k) * S.scale - lse) * kLog2e) * (dot(go, v) - delta) * S.scale;
         add_scaled(dq, slope, k);
-        if (slope != slope) return stop_all(stop);
+        if (slope != slope) break;
     }
 }
-// Head kv of key j, over the heads that share it and the tokens that see it: dk (KEYS) or dv, or both.
-template <int DT, bool KEYS, bool VALUES>
-__device__ __forceinline__ void row_dkv(const Backward& B, int64_t j, int kv, int first, int step, float (&dk)[kLaneValues],
-                                        float (&dv)[kLaneValues], volatile int* stop = nullptr) {
+// Head kv of key j, over the heads that share it and the tokens that see it.
+template <int DT>
+__device__ __forceinline__ void row_dkv(const Backward& B, int64_t j, int kv, float (&dk)[kLaneValues], float (&dv)[kLaneValues]) {
     const Shape& S = B.S;
     float q[kLaneValues], go[kLaneValues], k[kLaneValues], v[kLaneValues];
 #pragma unroll
     for (int i = 0; i < kLaneValues; ++i) dk[i] = dv[i] = 0.f;
-    const int64_t end = S.end[j];
-    if (end <= j) return;
-    const int64_t last = j - S.start[j] < S.sinks ? end : min64(end, j + S.window);
+    const int64_t last = seen_to(S, j);
+    if (last == j) return;
     load_row<DT>(B.k, j, kv, S.dim, k);
     load_row<DT>(B.v, j, kv, S.dim, v);
-    const int64_t n = last - j;
-    int64_t i = first;  // of the tokens that see it, head after head
-    for (int h = kv * S.group; h < (kv + 1) * S.group; ++h, i -= n)
-        for (; i < n && !stopped(stop); i += step) {
-            const int64_t t = j + i;
+    for (int h = kv * S.group; h < (kv + 1) * S.group; ++h)
+        for (int64_t t = j; t < last; ++t) {
             load_row<DT>(B.q, t, h, S.dim, q);
             load_row<DT>(B.go, t, h, S.dim, go);
             const float p = exp2f((dot(q, k) * S.scale - B.lse[h * S.tokens + t]) * kLog2e);
-            float slope = p;
-            if constexpr (VALUES) add_scaled(dv, p, go);
-            if constexpr (KEYS) {
-                slope = p * (dot(go, v) - B.delta[h * S.tokens + t]) * S.scale;
-                add_scaled(dk, slope, q);
-            }
-            if ((VALUES ? p : slope) != (VALUES ? p : slope)) return stop_all(stop);
+            add_scaled(dv, p, go);
+            add_scaled(dk, p * (dot(go, v) - B.delta[h * S.tokens + t]) * S.scale, q);
+            if (p != p) return;
         }
 }
 

@@ -181,7 +181,7 @@ __device__ __forceinline__ void warp_arrive(uint64_t* bar) {
 //
 // The last block of an item holds tokens that none of its rows sees: of the next session, or of none. Their infinities and NaNs
 // would survive the zeros by which they are multiplied, and all of the item's rows would have to be computed again (a session of
-// 32768 tokens x 8 heads over 1 beside one of NaNs: backward 1730 ms, 13 with the rows cleared, 4.5 beside one of numbers).
+// 32768 tokens x 8 heads over 1 beside one of NaNs: backward 1730 ms, 10 with the rows cleared, 4.5 beside one of numbers).
 //
 // Such a tile lands on a barrier of its own (`landed`); a warp that has little else to do, the one that stores or over
 // keys the one that brings lse and delta, waits for it there, clears the rows and arrives where the tile's products wait for
