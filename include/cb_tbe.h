@@ -569,7 +569,8 @@ cb_status cb_grad_clip(const cb_grad_tensor* tensors, int64_t num_tensors, float
  * tensor cores take rows of a multiple of 8 and at most 128 values, addresses and strides in multiples of 16
  * bytes; other rows, up to 256 values, go key by key and are far slower. Deterministic.
  *   q, k, v, out, grad_...  device, of one type; head h of token t at t * ..._token_stride + h * ..._head_stride
- *               values, each row contiguous. What is written shares no value with anything else of the call.
+ *               values, each row contiguous. What is written shares no value with anything else of the
+ *               call (CB_ERR_INVALID_ARG).
  *   offsets     device, idx_dtype, [sequences + 1]. They need not begin at 0 or end at `tokens`: a token of no
  *               session gets zeros (lse: -infinity).
  *   tokens, sequences < 2^31 - 1024, heads <= 65535, a multiple of kv_heads

@@ -1,12 +1,12 @@
 // window_attention.cu -- windowed attention over packed sessions (include/cb_tbe.h): where each
 // token's session begins, the kernels for rows that the tensor cores' do not take (fp32, lengths that are no
 // multiple of 8 or over 128, unaligned), and the entry points.
+#include "spans.h"
 #include "window_attention_tc.cuh"
 
 #include <algorithm>
 #include <cmath>
 #include <cudaTypedefs.h>
-#include <initializer_list>
 
 namespace cbtbe {
 namespace attention {
@@ -126,13 +126,12 @@ bool heads_ok(const Shape& S, const Heads& h, int heads, bool written) {
         return false;
     return !written || rows_apart(S.tokens, h.token, heads, h.head, S.dim);
 }
-// Whether a result begins where one of the others, or of what is read, does: blocks read what others have written by then.
-bool in_one_place(std::initializer_list<const void*> written, std::initializer_list<const void*> read) {
-    for (auto w = written.begin(); w != written.end(); ++w)
-        if (std::find(w + 1, written.end(), *w) != written.end() || std::find(read.begin(), read.end(), *w) != read.end())
-            return true;
-    return false;
+// The memory of a tensor. Blocks read what others have written by then, so results lie apart from what is read.
+Span span(const Shape& S, const Heads& h, int heads) {
+    const int64_t size = S.dtype == CB_F32 ? 4 : 2;
+    return Span(h.data, S.dim * size).by(S.tokens, h.token * size).by(heads, h.head * size);
 }
+Span offsets_span(const Shape& S) { return Span(S.offsets, (S.sequences + 1) * (S.offsets32 ? 4 : 8)); }
 cb_status sizes_ok(const Shape& S) {
     if (!type_ok(S.dtype) || S.tokens < 0 || S.tokens > kMostTokens || S.sequences < 0 || S.sequences > kMostTokens ||
         S.heads < 1 || S.kv_heads < 1 || S.heads > 65535 || S.heads % S.kv_heads || S.dim < 1 || S.dim > kMaxDim ||
@@ -270,10 +269,13 @@ extern "C" cb_status cb_attention_forward(const void* q, const void* k, const vo
     F.out = {out, out_token_stride, out_head_stride};
     F.lse = lse;
     if (!heads_ok(F.S, F.q, heads, false) || !heads_ok(F.S, F.k, kv_heads, false) || !heads_ok(F.S, F.v, kv_heads, false) ||
-        !heads_ok(F.S, F.out, heads, true) || reinterpret_cast<uintptr_t>(lse) % 4 || in_one_place({out, lse}, {q, k, v}))
+        !heads_ok(F.S, F.out, heads, true) || reinterpret_cast<uintptr_t>(lse) % 4)
         return CB_ERR_INVALID_ARG;
-    if (!workspace_ok(workspace, workspace_bytes, cb_attention_workspace_bytes(tokens, heads, kv_heads, dim, window, sinks, 0)))
-        return CB_ERR_CAPACITY;
+    const int64_t need = cb_attention_workspace_bytes(tokens, heads, kv_heads, dim, window, sinks, 0);
+    if (!workspace_ok(workspace, workspace_bytes, need)) return CB_ERR_CAPACITY;
+    if (cbtbe::overlap({span(F.S, F.out, heads), {lse, 4 * tokens * heads}, {workspace, need}, {error, 4}},
+                       {span(F.S, F.q, heads), span(F.S, F.k, kv_heads), span(F.S, F.v, kv_heads), offsets_span(F.S)}))
+        return CB_ERR_INVALID_ARG;
     set_rows(F.S, F.again, workspace, layout(tokens, heads, kv_heads, dim, window, sinks, false), stream);
     bool ok = true;
     if (tensor_core_rows(F.S, F.q, heads) && tensor_core_rows(F.S, F.k, kv_heads) && tensor_core_rows(F.S, F.v, kv_heads) &&
@@ -313,10 +315,14 @@ extern "C" cb_status cb_attention_backward(const void* grad_out, const void* q, 
     if (!heads_ok(B.S, B.go, heads, false) || !heads_ok(B.S, B.q, heads, false) || !heads_ok(B.S, B.k, kv_heads, false) ||
         !heads_ok(B.S, B.v, kv_heads, false) || !heads_ok(B.S, B.out, heads, false) || !heads_ok(B.S, B.dq, heads, true) ||
         !heads_ok(B.S, B.dk, kv_heads, true) || !heads_ok(B.S, B.dv, kv_heads, true) || !lse ||
-        reinterpret_cast<uintptr_t>(lse) % 4 || in_one_place({grad_q, grad_k, grad_v}, {grad_out, q, k, v, out, lse}))
+        reinterpret_cast<uintptr_t>(lse) % 4)
         return CB_ERR_INVALID_ARG;
-    if (!workspace_ok(workspace, workspace_bytes, cb_attention_workspace_bytes(tokens, heads, kv_heads, dim, window, sinks, 1)))
-        return CB_ERR_CAPACITY;
+    const int64_t need = cb_attention_workspace_bytes(tokens, heads, kv_heads, dim, window, sinks, 1);
+    if (!workspace_ok(workspace, workspace_bytes, need)) return CB_ERR_CAPACITY;
+    if (cbtbe::overlap({span(B.S, B.dq, heads), span(B.S, B.dk, kv_heads), span(B.S, B.dv, kv_heads), {workspace, need}, {error, 4}},
+                       {span(B.S, B.go, heads), span(B.S, B.q, heads), span(B.S, B.k, kv_heads), span(B.S, B.v, kv_heads),
+                        span(B.S, B.out, heads), {lse, 4 * tokens * heads}, offsets_span(B.S)}))
+        return CB_ERR_INVALID_ARG;
     const Layout L = layout(tokens, heads, kv_heads, dim, window, sinks, true);
     char* base = static_cast<char*>(workspace);
     B.delta = reinterpret_cast<float*>(base + L.delta);

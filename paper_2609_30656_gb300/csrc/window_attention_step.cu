@@ -1,6 +1,7 @@
 // window_attention_step.cu -- windowed attention of one new token for each session over a cache of keys
 // and values (include/cb_tbe.h).
 #include "muon_internal.cuh"
+#include "spans.h"
 #include "window_attention.cuh"
 
 #include <algorithm>
@@ -441,11 +442,21 @@ extern "C" cb_status cb_attention_step(const void* q, const void* k_cache, const
     const uintptr_t mask = dtype == CB_F32 ? 3 : 1;
     if (!q || !out || !lengths || (capacity > 0 && (!k_cache || !v_cache)) || (reinterpret_cast<uintptr_t>(q) & mask) ||
         (reinterpret_cast<uintptr_t>(k_cache) & mask) || (reinterpret_cast<uintptr_t>(v_cache) & mask) ||
-        (reinterpret_cast<uintptr_t>(out) & mask) || out == q || out == k_cache || out == v_cache ||
+        (reinterpret_cast<uintptr_t>(out) & mask) ||
         reinterpret_cast<uintptr_t>(lengths) % (idx_dtype == CB_I32 ? 4 : 8))
         return CB_ERR_INVALID_ARG;
     const int64_t need = cb_attention_step_workspace_bytes(sequences, heads, kv_heads, dim, capacity, window, sinks);
     if (need > 0 && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 || workspace_bytes < need)) return CB_ERR_CAPACITY;
+    auto span = [&](const void* p, int64_t sequence, int64_t token, int64_t head, int64_t tokens, int32_t n) {
+        const int64_t size = mask + 1;
+        return cbtbe::Span(p, dim * size).by(sequences, sequence * size).by(tokens, token * size).by(n, head * size);
+    };
+    if (cbtbe::overlap({span(out, out_sequence_stride, 0, out_head_stride, 1, heads), {workspace, need}, {error, 4}},
+                       {span(q, q_sequence_stride, 0, q_head_stride, 1, heads),
+                        span(k_cache, k_sequence_stride, k_token_stride, k_head_stride, capacity, kv_heads),
+                        span(v_cache, v_sequence_stride, v_token_stride, v_head_stride, capacity, kv_heads),
+                        {lengths, sequences * (idx_dtype == CB_I32 ? 4 : 8)}}))
+        return CB_ERR_INVALID_ARG;
     Step A{};
     A.q = q;
     A.k = k_cache;
