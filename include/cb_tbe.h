@@ -499,7 +499,7 @@ cb_status cb_muon_step(void* weights, cb_dtype w_dtype, int64_t w_batch_stride, 
  *   x, out, grad_out, grad_x  device, row r at r * ..._row_stride values, each row contiguous, strides
  *               >= dim. dim <= 2^20, rows < 2^40; either may be 0. Any alignment of the type; where all rows of all
  *               tensors lie alike within 16 bytes they are moved fastest. out may be x, and grad_x either
- *               input, of one type and layout.
+ *               input, of one type and layout; else what is written shares no memory with anything else of the call.
  *   weight, bias  device [dim], contiguous, or NULL (1 and 0)
  *   mean, rstd  device fp32 [rows]; the forward writes each that is not NULL, the backward reads both
  *   eps         >= 0

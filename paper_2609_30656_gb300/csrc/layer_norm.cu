@@ -1,6 +1,7 @@
 // layer_norm.cu -- layer normalisation of rows and its backward pass (include/cb_tbe.h): rows longer
 // than registers hold, the join of the weight's gradient, how a call's rows are read, the entry points.
 #include "layer_norm.cuh"
+#include "spans.h"
 
 #include <cmath>
 
@@ -124,6 +125,14 @@ bool sizes_ok(int64_t rows, int64_t dim) { return rows >= 0 && rows < (int64_t{1
 bool row_ok(int64_t rows, int64_t dim, int64_t stride) {
     return rows <= 1 || (stride >= dim && stride <= (INT64_MAX >> 4) / rows);
 }
+// The memory of a tensor of rows; of one that is written in an input's place, of one type and layout, none.
+Span span(const void* p, int dtype, int64_t rows, int64_t dim, int64_t stride) {
+    return Span(p, dim * size_of(dtype)).by(rows, stride * size_of(dtype));
+}
+Span vector(const void* p, int dtype, int64_t n) { return Span(p, n * size_of(dtype)); }
+bool in_place(const void* x, int dtype, int64_t stride, const void* out, int out_dtype, int64_t out_stride, int64_t rows) {
+    return x == out && dtype == out_dtype && (rows <= 1 || stride == out_stride);
+}
 cb_status launched() { return cudaGetLastError() == cudaSuccess ? CB_OK : CB_ERR_CUDA; }
 
 // Pieces of 16 bytes of the narrower type where all rows begin on them, or begin equally far behind
@@ -182,6 +191,12 @@ extern "C" cb_status cb_layer_norm_forward(const void* x, cb_dtype x_dtype, int6
         return CB_ERR_INVALID_ARG;
     if (rows == 0 || dim == 0) return CB_OK;
     if (!x || !out || !aligned(x, x_dtype) || !aligned(out, out_dtype)) return CB_ERR_INVALID_ARG;
+    if (cbtbe::overlap({span(out, out_dtype, rows, dim, out_row_stride), vector(mean, CB_F32, rows), vector(rstd, CB_F32, rows)},
+                       {in_place(x, x_dtype, x_row_stride, out, out_dtype, out_row_stride, rows)
+                            ? cbtbe::Span()
+                            : span(x, x_dtype, rows, dim, x_row_stride),
+                        vector(weight, weight_dtype, dim), vector(bias, bias_dtype, dim)}))
+        return CB_ERR_INVALID_ARG;
     Args A{};
     A.x = x;
     A.weight = weight;
@@ -228,6 +243,16 @@ extern "C" cb_status cb_layer_norm_backward(const void* grad_out, const void* x,
     if (sums && rows > 0 && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 ||
                              workspace_bytes < cb_layer_norm_backward_workspace_bytes(rows, dim)))
         return CB_ERR_CAPACITY;
+    auto input = [&](const void* p, int64_t stride) {
+        return in_place(p, dtype, stride, grad_x, grad_x_dtype, grad_x_row_stride, rows) ? cbtbe::Span()
+                                                                                        : span(p, dtype, rows, dim, stride);
+    };
+    if (cbtbe::overlap({span(grad_x, grad_x_dtype, rows, dim, grad_x_row_stride), vector(grad_weight, CB_F32, dim),
+                        vector(grad_bias, CB_F32, dim),
+                        {workspace, sums && rows > 0 ? cb_layer_norm_backward_workspace_bytes(rows, dim) : 0}},
+                       {input(grad_out, grad_out_row_stride), input(x, x_row_stride), vector(mean, CB_F32, rows),
+                        vector(rstd, CB_F32, rows), vector(weight, weight_dtype, dim)}))
+        return CB_ERR_INVALID_ARG;
     Args A{};
     A.x = x;
     A.dy = grad_out;

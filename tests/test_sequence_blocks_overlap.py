@@ -31,3 +31,23 @@ def test_backward(lib, bad):  # noqa: F811
     {"error": P(4 * MB)}, {"out": 2 * MB - 64}], ids=str)
 def test_step(lib, bad):  # noqa: F811
     assert _step(lib, **bad) == 1
+
+
+@pytest.mark.parametrize("bad", [
+    {"out": 4096 + 32}, {"out": 4096 - 32}, {"out": 4096, "od": 1}, {"out": 4096, "os_": 16}, {"out": 4096, "stride": 16},
+    {"out": 4096 + 4 * 15, "stride": 16, "os_": 16}, {"out": 8192 + 16}, {"out": 12288 - 64}, {"mean": 4096 + 64}, {"rstd": 20480 + 8},
+    {"mean": 16384}, {"rstd": 8192}], ids=str)
+def test_layer_norm(lib, bad):  # noqa: F811
+    from paper_2609_30656_gb300 import layer_norm
+    from tests.test_norm_and_clip_abi import _forward as forward
+    assert forward(layer_norm._library(), **bad) == 1
+
+
+@pytest.mark.parametrize("bad", [
+    {"dx": 4096 + 32}, {"dx": 8192 - 32}, {"dx": 8192, "dd": 1}, {"dx": 4096, "ds": 16}, {"dx": 20480}, {"dx": 12288 - 64},
+    {"dw": 24576 + 64}, {"db": 28672 + 28}, {"dw": 8192 + 32}, {"db": 16384}, {"work": 8192}, {"dx": 65536 + 32}, {"db": 65536}],
+    ids=str)
+def test_layer_norm_backward(lib, bad):  # noqa: F811
+    from paper_2609_30656_gb300 import layer_norm
+    from tests.test_norm_and_clip_abi import _backward as backward
+    assert backward(layer_norm._library(), **bad) == 1

@@ -71,3 +71,52 @@ def test_attention_between_its_inputs(dtype):
     lengths = torch.tensor([20, 3, 0, 1, 7, 19, 11], device=DEV)
     wa.window_attention_step(q, k, v, lengths, 5, 2, out=out)
     assert torch.equal(out, wa.window_attention_step(q.contiguous(), k.contiguous(), v.contiguous(), lengths, 5, 2))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_layer_norm_into_its_inputs(dtype):
+    from paper_2609_30656_gb300 import layer_norm as ln, tbe
+    room = _rand(40, 100, dtype=dtype)
+    x = room[:30]
+    for out in (room[1:31], room[5:35]):
+        with pytest.raises(tbe.CbTbeError):
+            ln.layer_norm(x, out=out)
+    y, mean, rstd = ln.layer_norm(x, stats=True)
+    for out in (room[1:31], room[10:40]):
+        with pytest.raises(tbe.CbTbeError):
+            ln.layer_norm_backward(y, x, mean, rstd, out=out)
+    # columns of one matrix
+    pair = torch.zeros(30, 250, dtype=dtype, device=DEV)
+    pair[:, 20:120] = x
+    with pytest.raises(tbe.CbTbeError):
+        ln.layer_norm(pair[:, 20:120], out=pair[:, 119:219])
+    want = ln.layer_norm(pair[:, 20:120], out=torch.zeros_like(pair)[:, 120:220])  # in the same order: alike in alignment
+    assert torch.equal(ln.layer_norm(pair[:, 20:120], out=pair[:, 120:220]), want)
+    assert (pair[:, :20] == 0).all() and (pair[:, 220:] == 0).all() and torch.equal(pair[:, 20:120], x)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32], ids=str)
+@pytest.mark.parametrize("dim,stride", [(41, 41), (1001, 1001), (1027, 1030), (72, 80), (7, 9), (4099, 4099), (18001, 18001)])
+def test_layer_norm_in_place(dim, stride, dtype):
+    """Odd rows of halves read whole pieces, with their neighbours' values, while those are written."""
+    from paper_2609_30656_gb300 import layer_norm as ln
+    w = _rand(dim, dtype=torch.float32, seed=3)
+
+    def wide(t):
+        room = torch.full((700, stride), 5.0, dtype=dtype, device=DEV)
+        room[:, :dim] = t
+        return room[:, :dim]
+
+    def kept(t):  # what lies between the rows
+        return (t.as_strided((700, stride), (stride, 1))[:, dim:] == 5).all()
+
+    x, go = wide(_rand(700, dim, dtype=dtype)), wide(_rand(700, dim, dtype=dtype, seed=2))
+    y, mean, rstd = ln.layer_norm(x, w, stats=True, out=wide(x))
+    want = ln.layer_norm_backward(go, x, mean, rstd, w, out=wide(x))
+    for _ in range(3):
+        a = wide(x)
+        assert torch.equal(ln.layer_norm(a, w, out=a), y) and kept(a)
+        for which in (0, 1):
+            views = wide(go), wide(x)
+            got = ln.layer_norm_backward(*views, mean, rstd, w, out=views[which])
+            assert all(torch.equal(s, t) for s, t in zip(got, want)) and kept(views[which])
