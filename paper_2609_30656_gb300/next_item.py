@@ -63,13 +63,13 @@ class NextItem:
     def _projected(self, x: torch.Tensor):
         """(normalised rows, mean, rstd, (q, k, v)) of rows x [tokens, dim]; the three are slices of one product."""
         n, mean, rstd = ln.layer_norm(x, self.gain, self.shift, stats=True)
-        return n, mean, rstd, (n @ self.w_qkv).to(torch.bfloat16).view(len(x), 3, self.heads, -1).unbind(1)
+        return n, mean, rstd, (n @ self.w_qkv).to(torch.bfloat16).view(len(x), 3, self.heads, self.dim // self.heads).unbind(1)
 
     def _attend(self, x: torch.Tensor, offsets: torch.Tensor):
         """x + attention, and what its backward pass needs."""
         n, mean, rstd, qkv = self._projected(x)
         out, lse = wa.window_attention(*qkv, offsets, self.window, self.sinks, stats=True)
-        o = out.view(len(x), -1).float()
+        o = out.view(len(x), self.dim).float()
         return x + o @ self.w_out, (x, n, mean, rstd, qkv, out, lse, o, offsets)
 
     def _attend_backward(self, d_y: torch.Tensor, saved):
@@ -78,7 +78,7 @@ class NextItem:
         d_out = (d_y @ self.w_out.T).to(torch.bfloat16).view(out.shape)
         d_qkv = torch.empty(len(x), 3, *out.shape[1:], dtype=torch.bfloat16, device=x.device)
         wa.window_attention_backward(d_out, *qkv, out, lse, offsets, self.window, self.sinks, grads=d_qkv.unbind(1))
-        d_qkv = d_qkv.view(len(x), -1).float()
+        d_qkv = d_qkv.view(len(x), 3 * self.dim).float()
         d_x, d_gain, d_shift = ln.layer_norm_backward(d_qkv @ self.w_qkv.T, x, mean, rstd, self.gain)
         return d_y + d_x, (n.T @ d_qkv, o.T @ d_y, d_gain, d_shift)
 
@@ -156,7 +156,7 @@ class Serving:
         self.cache[0, rows, self.lengths], self.cache[1, rows, self.lengths] = k, v
         self.lengths += 1
         out = wa.window_attention_step(q, self.cache[0], self.cache[1], self.lengths, m.window, m.sinks)
-        x = x + out.view(len(items), -1).float() @ m.w_out
+        x = x + out.view(len(items), m.dim).float() @ m.w_out
         return (x + (x @ m.w1).relu() @ m.w2) @ m.table.T / math.sqrt(m.dim)
 
 
