@@ -330,7 +330,7 @@ extern "C" cb_status cb_attention_backward(const void* grad_out, const void* q, 
     B.padded = static_cast<int64_t>(tiles_of(static_cast<int>(tokens))) * kTile;
     set_rows(B.S, B.again, workspace, L, stream);
     B.order = {reinterpret_cast<int32_t*>(B.S.words + kOrderParts), B.S.words + kOrderNext, B.S.words + kOrderDone,
-               static_cast<int32_t>(L.room), reinterpret_cast<int2*>(base + L.list),
+               static_cast<int32_t>(L.room), part_blocks(tokens, heads, kv_heads, window), reinterpret_cast<int2*>(base + L.list),
                reinterpret_cast<int32_t*>(base + L.split), reinterpret_cast<float*>(base + L.sums)};
     bool ok = true;
     bool fast = true;

@@ -65,6 +65,7 @@ struct Order {
     uint32_t* next;       // the next item to take: 0 before,
     uint32_t* done;       // blocks that have counted their tiles' parts: 0 before,
     int32_t room;         // parts there is room for; 0: no tile is taken in parts
+    int32_t part;         // blocks of queries of a part
     int2* list;           // [room] tile (-1: none) and which of its parts
     int32_t* split;       // [tiles of 128 tokens] parts of each, 0 for one taken whole
     float* sums;          // [room][kv_heads][2][128][64 or 128] dV and dK of each
@@ -228,6 +229,7 @@ inline size_t rows_bytes(int64_t tokens) { return static_cast<size_t>((tokens * 
 // bf16, rows of a multiple of 8 and at most 128 values, addresses and strides in multiples of 16 bytes.
 bool tensor_core_rows(const Shape& S, const Heads& h, int heads);
 int sm_count();  // of the current device
+int32_t part_blocks(int64_t tokens, int32_t heads, int32_t kv_heads, int64_t window);
 int64_t parts_room(int64_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, int64_t window, int64_t sinks);
 int64_t parts_bytes(int64_t room, int32_t kv_heads, int32_t dim);
 bool launch_forward(const Forward& F, cudaStream_t s);

@@ -54,15 +54,8 @@ __device__ __forceinline__ int seen_until(const Shape& S, int64_t j) {
 // many tiles to fill the GPU with; with few the longest decides, and 16 altogether are enough. One session of 23100
 // tokens: 1077 us in one piece, 149 in parts; 33 sessions of 27 to 2379 tokens x 8 heads over 2: 242 with the larger parts,
 // 215 with the smaller.
-__host__ __device__ __forceinline__ int part_blocks(int64_t window, int group, int64_t tiles, int kv_heads) {
-    const int least = tiles * kv_heads < 8 * 152 ? (16 + group - 1) / group : 16;
-    return static_cast<int>(max64(least, min64(window, int64_t{1} << 30) / kTile + 2));
-}
-__device__ __forceinline__ int part_blocks(const Shape& S) {
-    return part_blocks(S.window, S.group, tiles_of(static_cast<int>(S.tokens)), S.kv_heads);
-}
-__device__ __forceinline__ int parts_of(const Shape& S, int blocks) {
-    const int per = part_blocks(S);
+// (part_blocks, on the host, decides it for a call: few tiles are fewer than 8 an SM.)
+__device__ __forceinline__ int parts_of(int per, int blocks) {
     return blocks <= 2 * per ? 0 : (blocks + per - 1) / per;
 }
 
@@ -141,7 +134,7 @@ __global__ void __launch_bounds__(kDeltaThreads) attention_delta_kernel(const Ba
 #pragma unroll
         for (int k = 0; k < kTile / 32; ++k) until = max(until, seen_until(S, from + k * 32 + lane));
         until = __reduce_max_sync(kFull, until);
-        if (lane == 0) B.order.split[w] = parts_of(S, tiles_of(max(until - from, 0)));
+        if (lane == 0) B.order.split[w] = parts_of(B.order.part, tiles_of(max(until - from, 0)));
     }
     if (tiles == 0) return;
     __shared__ bool last;  // of the blocks: every tile's number of parts is there
@@ -719,7 +712,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
                     }
                     until = __reduce_max_sync(kFull, until);
                 }
-                const int blocks = tiles_of(max(until - first, 0)), per = part_blocks(B.S);
+                const int blocks = tiles_of(max(until - first, 0)), per = B.order.part;
                 const int from = place < 0 ? first : first + part * per * kTile;
                 const int count = !some ? -1 : (place < 0 ? blocks : max(min(per, blocks - part * per), 0));
                 uint32_t largest[kTile / 32];
@@ -1092,9 +1085,14 @@ bool launch_typed(const Backward& B, cudaStream_t s) {
 
 }  // namespace
 
+int32_t part_blocks(int64_t tokens, int32_t heads, int32_t kv_heads, int64_t window) {
+    const int64_t tiles = (tokens + kTile - 1) / kTile, group = std::max(1, heads / kv_heads);
+    const int64_t least = tiles * kv_heads < 8 * sm_count() ? (16 + group - 1) / group : 16;
+    return static_cast<int32_t>(std::max(least, std::min(window, int64_t{1} << 30) / kTile + 2));
+}
 int64_t parts_room(int64_t tokens, int32_t heads, int32_t kv_heads, int32_t dim, int64_t window, int64_t sinks) {
     const int64_t tiles = (tokens + kTile - 1) / kTile;
-    const int64_t per = part_blocks(window, std::max(1, heads / kv_heads), tiles, kv_heads);
+    const int64_t per = part_blocks(tokens, heads, kv_heads, window);
     if (sinks == 0 || dim > 128 || tiles <= 2 * per) return 0;
     // A session's first keys lie in at most so many tiles, each seen by its blocks, two per - 1 of them or more a part.
     const int64_t most = (std::min(sinks, tokens) / kTile + 2) * ((tiles + per - 1) / per * 2);
