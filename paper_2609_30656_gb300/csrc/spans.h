@@ -7,34 +7,36 @@
 
 namespace cbtbe {
 
+using wide = __int128;  // strides and counts are any that fit 64 bits
+
 // Rows of `width` bytes at begin + i * step, i < n, for up to three such strides (in bytes, not negative).
 struct Span {
     static constexpr int kLevels = 3;
     uintptr_t begin = 0;
-    __int128 width = 0;
+    wide end = 0;    // behind the last byte
+    wide width = 0;  // 0: nothing
     int levels = 0;
-    __int128 n[kLevels], step[kLevels];
+    int64_t n[kLevels], step[kLevels];
 
     Span() = default;
-    Span(const void* p, int64_t bytes) : begin(reinterpret_cast<uintptr_t>(p)), width(p ? bytes : 0) {}
+    Span(const void* p, int64_t bytes) : begin(reinterpret_cast<uintptr_t>(p)), end(begin), width(p && bytes > 0 ? bytes : 0) {
+        end += width;
+    }
     Span& by(int64_t count, int64_t stride_bytes) {
-        if (count <= 0) width = 0;
-        if (count > 1 && stride_bytes > 0) {
+        if (count <= 0) {
+            width = 0;
+        } else if (count > 1 && stride_bytes > 0 && width > 0) {
             n[levels] = count;
             step[levels++] = stride_bytes;
+            end += static_cast<wide>(count - 1) * stride_bytes;
         }
         return *this;
     }
+    bool reaches(const Span& o) const { return end > static_cast<wide>(o.begin) && o.end > static_cast<wide>(begin); }
 };
 
 namespace spans {
 
-using wide = __int128;
-inline wide extent(const Span& a) {
-    wide e = a.width;
-    for (int k = 0; k < a.levels; ++k) e += (a.n[k] - 1) * a.step[k];
-    return e;
-}
 // The largest stride first, each once, rows that follow one another without a gap as one.
 inline void tidy(Span& a) {
     for (int k = 1; k < a.levels; ++k)
@@ -53,7 +55,7 @@ inline void tidy(Span& a) {
         }
     while (a.levels && a.step[a.levels - 1] <= a.width) {
         --a.levels;
-        a.width += (a.n[a.levels] - 1) * a.step[a.levels];
+        a.width += static_cast<wide>(a.n[a.levels] - 1) * a.step[a.levels];
     }
 }
 inline wide floor_div(wide a, wide b) { return a / b - (a % b != 0 && a < 0); }
@@ -61,7 +63,7 @@ inline wide floor_div(wide a, wide b) { return a / b - (a % b != 0 && a < 0); }
 inline bool meet(const Span& a, const Span& b, const wide (&s)[2], int64_t& looks) {
     auto count = [&](const Span& x, int which) {
         for (int k = 0; k < x.levels; ++k)
-            if (x.step[k] == s[which]) return x.n[k];
+            if (x.step[k] == s[which]) return static_cast<wide>(x.n[k]);
         return wide{1};
     };
     const wide D = static_cast<wide>(b.begin) - static_cast<wide>(a.begin);
@@ -82,14 +84,12 @@ inline bool meet(const Span& a, const Span& b, const wide (&s)[2], int64_t& look
     return false;
 }
 inline bool share(const Span& a, const Span& b, int64_t& looks) {
-    if (static_cast<wide>(a.begin) + extent(a) <= static_cast<wide>(b.begin) ||
-        static_cast<wide>(b.begin) + extent(b) <= static_cast<wide>(a.begin))
-        return false;
+    if (!a.reaches(b)) return false;
     wide s[2] = {0, 0};
     int different = 0;
     for (const Span* x : {&a, &b})
         for (int k = 0; k < x->levels; ++k) {
-            if (std::find(s, s + std::min(different, 2), x->step[k]) != s + std::min(different, 2)) continue;
+            if (std::find(s, s + std::min(different, 2), static_cast<wide>(x->step[k])) != s + std::min(different, 2)) continue;
             if (different < 2) s[different] = x->step[k];
             ++different;
         }
@@ -99,13 +99,14 @@ inline bool share(const Span& a, const Span& b, int64_t& looks) {
     // Three strides or more: the rows of one, along its largest, by themselves.
     const bool of_a = a.levels && (!b.levels || a.n[0] <= b.n[0]);
     Span part = of_a ? a : b;
-    const wide n = part.n[0], step = part.step[0];
+    const int64_t n = part.n[0], step = part.step[0];
+    part.end -= static_cast<wide>(n - 1) * step;
     for (int k = 1; k < part.levels; ++k) {
         part.n[k - 1] = part.n[k];
         part.step[k - 1] = part.step[k];
     }
     --part.levels;
-    for (wide i = 0; i < n; ++i, part.begin += static_cast<uintptr_t>(step))
+    for (int64_t i = 0; i < n; ++i, part.begin += static_cast<uintptr_t>(step), part.end += step)
         if (--looks < 0 || share(of_a ? part : a, of_a ? b : part, looks)) return true;
     return false;
 }
@@ -114,8 +115,9 @@ inline bool share(const Span& a, const Span& b, int64_t& looks) {
 
 // Whether two tensors have a byte in common. Where they lie between one another in strides of three kinds and more it is looked
 // for up to 2^16 times, and taken for granted then.
-inline bool share(Span a, Span b) {
-    if (a.width <= 0 || b.width <= 0) return false;
+inline bool share(const Span& x, const Span& y) {
+    if (x.width <= 0 || y.width <= 0 || !x.reaches(y)) return false;
+    Span a = x, b = y;
     spans::tidy(a);
     spans::tidy(b);
     int64_t looks = 1 << 16;

@@ -10,8 +10,13 @@ token j, s <= j <= t, where t - j < window or j - s < sinks:
 
 Autograd records nothing of them: the second is the first's derivative, called by hand. fp16 and bf16
 go through the tensor cores (heads of a multiple of 8 and at most 128 values), with sums, scores and softmax in
-fp32; fp32 and other heads of up to 256 values go key by key, in fp32, and are far slower. All work is
-enqueued on the current stream of the tensors' device; nothing waits.
+fp32; fp32 and other heads of up to 256 values go key by key, in fp32, and are far slower, over thousands of tokens in
+sight than plain tensor operations would be. A row whose result is not finite is computed again that way, so a batch of
+infinities costs as much. All work is enqueued on the current stream of the tensors' device; nothing waits.
+
+``error``, everywhere: an int32 tensor of one value on the device, or None. A kernel sets it, if it holds 0, to the code of
+what it met: offsets or lengths out of range, or (CB_ERR_TIMEOUT) a wait within it that ran out, after which results are
+not whole. No input brings about the latter: it would be a fault of the library or the device.
 """
 
 from __future__ import annotations
@@ -125,8 +130,7 @@ def window_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets:
     q: [tokens, heads, dim]; k, v: [tokens, kv_heads, dim]; slices of one projection's output are taken as they lie.
     offsets: int32 or int64 [sessions + 1]; tokens of no session give zeros. window None: all tokens before. scale:
     dim ** -0.5 unless given. out shares no memory with q, k, v. With stats=True the result is (out, lse), lse fp32
-    [heads, tokens], as the backward pass takes it. error: an int32 tensor of one value on the device, set
-    where offsets decrease or leave the tokens."""
+    [heads, tokens], as the backward pass takes it. error: set where offsets decrease or leave the tokens."""
     lib = _bound or _library()
     index, kind, tokens, heads, kv_heads, dim = _check_packed(q, k, v)
     off_kind = _index(offsets, "offsets", index)
@@ -162,7 +166,7 @@ def window_attention_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torch.
     (cb_attention_backward), in the inputs' type.
 
     grads: three tensors to write them to (slices of one buffer, say), which share no memory with the inputs or one
-    another."""
+    another. error: as the forward pass."""
     lib = _bound or _library()
     index, kind, tokens, heads, kv_heads, dim = _check_packed(q, k, v)
     off_kind = _index(offsets, "offsets", index)
@@ -207,8 +211,8 @@ def window_attention_step(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch
 
     q: [sessions, heads, dim]; k_cache, v_cache: [sessions, capacity, kv_heads, dim] in any strides with contiguous rows
     (a transposed [sessions, kv_heads, capacity, dim] too); lengths: int32 or int64 [sessions], the tokens of each,
-    the new one among them, 0 .. capacity (0: zeros). out shares no memory with the inputs. error:
-    set to CB_ERR_INDEX_OOB by a length outside."""
+    the new one among them, 0 .. capacity (0: zeros). out shares no memory with the inputs. Caches of halves whose addresses or
+    strides are no multiples of 16 bytes go key by key, some 15 times slower. error: set to CB_ERR_INDEX_OOB by a length outside."""
     lib = _bound or _library()
     index = q.get_device()
     if index < 0 or q.dim() != 3 or k_cache.dim() != 4:
