@@ -7,17 +7,18 @@
 // (S^T, dP^T, dV and dK: four). One kernel would do with five, but dQ is then added up by many blocks: in fp32
 // in memory, in an order that changes its bits. Sums stay in TMEM, heads that share keys are summed by one block.
 //
-// 65536 tokens in sessions of 8192, 16 heads of 128 over 4, window 2048, bf16: 2460 us; delta 93 (the copy rate), over keys 1210
-// (1.73 PFLOP/s of its four products: 89 % of a library product's rate), over queries 950 (1.6), parts 23. Seven products for
-// five: the floor of five is 1243 us. (Key by key: 785 ms; a block for each tile: 3000 us.)
+// 65536 tokens in sessions of 8192, 16 heads of 128 over 4, window 2048, bf16: 2460 us; delta 92 (the copy rate), over keys 1240
+// (1.69 PFLOP/s of its four products, masked values too: 87 % of a library product's rate), over queries 942 (1.6), parts 24.
+// Seven products for five: the floor of five is 1243 us. (Key by key: 785 ms; a block for each tile: 3000 us.)
 //
 // P and dS are operands in the rows' type: dS's rounding adds to dQ and dK about what the rounding of the results does (off by
 // 2.5e-3 of their norm against 1.7e-3 in bf16, 3.2e-4 against 2.1e-4 in fp16; a second product for what it cuts off would be a
 // third of dQ's time more). fp16 has five bits for exponents: P goes times 2^12, and dS times a power of two of the row's own,
 // which its thread takes out of the sums again. It brings the largest |grad_out| that the row's sums hold to 16 .. 32: of the
-// token itself for dQ, of the tokens that see the key for dK. So small gradients (and loss scales) keep
-// their digits, whatever those of other sessions, heads or tokens out of sight are; a value that grows past fp16 all the same makes its row not finite, and such rows are computed
-// again key by key in fp32 by a kernel behind these (as are those that met an infinity or a NaN behind a mask).
+// token itself for dQ, of the tokens that see the key for dK. So small gradients (and loss scales) keep their digits, whatever
+// those of other sessions or of tokens out of sight are (with one factor for all, dQ of a session 2^-20 below another's was off by
+// ten times its bound). A value that grows past fp16 all the same makes its row not finite, and such rows are computed
+// again in fp32 by a kernel behind these (as are those that met an infinity or a NaN behind a mask).
 #include "window_attention_tc.cuh"
 
 #include <algorithm>
@@ -1026,7 +1027,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap qm, const __grid_consta
 }
 
 // The sums of a tile's parts, in order: a block for 32 rows of a tile and head, a warp for four of them, as many parts on their
-// way at once (33 sessions of 27 to 2379 tokens x 8 heads of 72 over 2: 16 us; of 128 rows a block 53, and 30 a part at a time).
+// way at once (33 sessions of 27 to 2379 tokens x 8 heads of 72 over 2: 22 us; of 128 rows a block 53).
 template <int D, bool BF16>
 __global__ void __launch_bounds__(256) attention_parts_kernel(const Backward B) {
     constexpr int DT = BF16 ? CB_BF16 : CB_F16, N = D / 32, kRowsAtOnce = 32, kGroups = kTile / kRowsAtOnce;
