@@ -127,7 +127,7 @@ bool row_ok(int64_t rows, int64_t dim, int64_t stride) {
 }
 // The memory of a tensor of rows; of one that is written in an input's place, of one type and layout, none.
 Span span(const void* p, int dtype, int64_t rows, int64_t dim, int64_t stride) {
-    return Span(p, dim * size_of(dtype)).by(rows, stride * size_of(dtype));
+    return Span(p, dim * size_of(dtype)).by(rows, rows > 1 ? stride * size_of(dtype) : 0);
 }
 Span vector(const void* p, int dtype, int64_t n) { return Span(p, n * size_of(dtype)); }
 bool in_place(const void* x, int dtype, int64_t stride, const void* out, int out_dtype, int64_t out_stride, int64_t rows) {
