@@ -533,7 +533,8 @@ cb_status cb_layer_norm_backward(const void* grad_out, const void* x, cb_dtype d
  *                 cb_grad_norm does not look at out.
  *     count       device int64, or NULL: how many of the values there are (one row only), as for the values of
  *                 a row-sparse gradient and its num_floats; those behind it are neither read nor written
- *   Values that are written may not be in a second tensor of the list: CB_ERR_INVALID_ARG.
+ *   Values that are written may not be in a second tensor of the list, nor where a count, the norm or the workspace is:
+ *   CB_ERR_INVALID_ARG.
  *   max_norm, eps  >= 0
  *   norm        device fp32 (cb_grad_clip: or NULL)
  *   workspace   device, 256-byte aligned, of cb_grad_norm_workspace_bytes(num_tensors) at least

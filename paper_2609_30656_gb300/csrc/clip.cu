@@ -17,6 +17,7 @@
 
 #include <algorithm>
 #include <exception>
+#include <utility>
 #include <vector>
 
 namespace cbtbe {
@@ -299,9 +300,9 @@ bool apart(std::vector<Range>& r) {
     return true;
 }
 
-cb_status check(const cb_grad_tensor* t, int64_t tensors, bool scale, std::vector<Entry>& entries) {
+// `ranges`: what else a call writes.
+cb_status check(const cb_grad_tensor* t, int64_t tensors, bool scale, std::vector<Entry>& entries, std::vector<Range> ranges) {
     if (tensors < 0 || (tensors > 0 && !t)) return CB_ERR_INVALID_ARG;
-    std::vector<Range> ranges;
     entries.reserve(static_cast<size_t>(tensors));
     for (int64_t i = 0; i < tensors; ++i) {
         const cb_grad_tensor& g = t[i];
@@ -336,6 +337,7 @@ cb_status check(const cb_grad_tensor* t, int64_t tensors, bool scale, std::vecto
         };
         const bool in_place = in == out && g.dtype == g.out_dtype && (g.rows == 1 || g.row_stride == g.out_row_stride);
         range(out, g.out_row_stride, size_of(e.out_dtype), true);
+        if (g.count) ranges.push_back({reinterpret_cast<uintptr_t>(g.count), reinterpret_cast<uintptr_t>(g.count + 1), 0, 8, i, false});
         if (!in_place) range(in, g.row_stride, size_of(g.dtype), false);
     }
     return apart(ranges) ? CB_OK : CB_ERR_INVALID_ARG;
@@ -361,10 +363,14 @@ void launch_pass(const Entry* e, int tensors, const float4* partial, int at, int
 cb_status run(const cb_grad_tensor* t, int64_t tensors, bool scale, float max_norm, float eps, float* norm, void* workspace,
               int64_t workspace_bytes, cudaStream_t stream) {
     std::vector<Entry> entries;
-    const cb_status status = check(t, tensors, scale, entries);
+    std::vector<Range> also;
+    const int64_t need = cb_grad_norm_workspace_bytes(tensors);
+    for (const auto& [p, bytes] : {std::pair<const void*, int64_t>{norm, 4}, {workspace, need}})
+        if (scale && p && bytes > 0)
+            also.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, 0, bytes, -1, true});
+    const cb_status status = check(t, tensors, scale, entries, std::move(also));
     if (status != CB_OK) return status;
     if (reinterpret_cast<uintptr_t>(norm) % 4 || (!scale && !norm)) return CB_ERR_INVALID_ARG;
-    const int64_t need = cb_grad_norm_workspace_bytes(tensors);
     if (need > 0 && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 || workspace_bytes < need)) return CB_ERR_CAPACITY;
     const float4* partial = static_cast<const float4*>(workspace);
     const int total = static_cast<int>(entries.size());

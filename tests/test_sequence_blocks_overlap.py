@@ -51,3 +51,13 @@ def test_layer_norm_backward(lib, bad):  # noqa: F811
     from paper_2609_30656_gb300 import layer_norm
     from tests.test_norm_and_clip_abi import _backward as backward
     assert backward(layer_norm._library(), **bad) == 1
+
+
+@pytest.mark.parametrize("entry,call", [
+    ({}, {"norm": 4096 + 8}), ({"out": 1 << 16}, {"norm": 4096}), ({"out": 1 << 16}, {"norm": (1 << 16) + 396}), ({}, {"work": 4096 - 256}),
+    ({"count": 4096 + 16}, {}), ({"count": (1 << 16) + 392, "out": 1 << 16}, {}), ({"count": 1 << 20}, {}), ({}, {"norm": 1 << 21})], ids=str)
+def test_clip(lib, entry, call):  # noqa: F811
+    """The norm, the workspace and the counts too."""
+    from paper_2609_30656_gb300 import clip
+    from tests.test_norm_and_clip_abi import _clip, _entry
+    assert _clip(clip._library(), _entry(**entry), **call) == 1
